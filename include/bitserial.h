@@ -423,6 +423,69 @@ int bs_selftest_wait_timeout(int polls, void* stream);
 int bs_l2_prefetch(const void* const* buffers, const size_t* bytes, int count, void* stream);
 
 /*
+ * Weights of 4 bits with a scale per group of the reduction, under activations of 16 bits (the paper has no counterpart: its activations are codes
+ * too; the codes and scales are those of the Section IV quantiser, one step s per group in place of one per tensor).
+ *       W[o][k] = s[o][k / group] * (q[o][k] - z[o][k / group])          G = ceil(K / group) groups in a row, the last one may be short
+ *   q  int8 codes: -8..7 where the weights have no zero points (z = 0), 0..15 where they have (z int8, 0..15)
+ *   s  of the activations' type (BS_F16 or BS_BF16)
+ * Supported: groups of 32 or 64, or of any multiple of 128 (one as wide as K: a scale per row); O, K up to 2^20, of any parity.
+ */
+typedef enum { BS_F32 = 0, BS_F16 = 1, BS_BF16 = 2 } bs_float_t;
+
+/*
+ * bs_w4_quantise -- float weights to codes, scales and zero points.
+ *   w       device, [O] rows of K values of w_type (BS_F32, BS_F16, BS_BF16), `ld` values apart
+ *   type    of the scales (BS_F16 or BS_BF16)
+ *   codes   device int8 [O][K];  scales  device [O][G];  zeros  device int8 [O][G], or NULL: no zero points
+ * Without zero points   s = type(max|w| / 7),               q = clip(round(w / s), -8, 7)
+ * with                  s = type((hi - lo) / 15), hi = max(0, max w), lo = min(0, min w),  z = clip(round(-lo / s), 0, 15),
+ *                       q = clip(round(w / s) + z, 0, 15)
+ * max, differences and the division that gives s in binary32; round is half-even of the exact quotient w / s.  s saturates at the type's largest value;
+ * where s is 0 (all weights 0, or smaller than the type holds) q = z = 0.  A NaN does not count for s and gets the lowest code.
+ */
+int bs_w4_quantise(const void* w, bs_float_t w_type, int O, int K, long long ld, int group, bs_float_t type, int8_t* codes,
+                   void* scales, int8_t* zeros, void* stream);
+
+/* Bytes of one prepared matrix (0 on bad input).  zeros: it has zero points. */
+size_t bs_w4_bytes(int O, int K, int group, int zeros);
+
+/*
+ * bs_w4_prepare -- lays codes, scales and zero points out for the products (once per matrix, off the hot path).  `matrices` of them at once (the experts
+ * of a layer): codes [matrices][O][K], scales and zeros [matrices][O][G], out  matrices * bs_w4_bytes(...) bytes, fully overwritten.
+ * The low four bits of a code (plus 8 where there are no zero points) and of a zero point are taken.
+ */
+int bs_w4_prepare(const int8_t* codes, const void* scales, const int8_t* zeros, int matrices, int O, int K, int group, void* out,
+                  void* stream);
+
+/*
+ * bs_w4_gemm -- y[m][o] = sum_k x[m][k] * W[o][k] + bias[o], one token (M = 1) or many.
+ *   x     device, [M] rows of K values of `type`, `ldx` values apart;  y  device, [M] rows of O values, `ldy` apart;  bias  device [O] or NULL
+ *   w     prepared matrix (its scales are of `type`)
+ *   workspace  bs_w4_gemm_workspace_bytes(M, K, ldx) bytes (0 unless the rows of x start off 16-byte boundaries; NULL then)
+ * Codes less their zero points are exact operands; products are summed in 32 bits over a group, scaled and added in 32 bits, rounded once.
+ * The same call gives the same bits every time.  M = 0 is BS_OK and does nothing.  M up to 2^20.
+ */
+size_t bs_w4_gemm_workspace_bytes(int M, int K, long long ldx);
+int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K, int group, int zeros, bs_float_t type,
+               const void* bias, void* y, long long ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bs_w4_moe -- a mixture-of-experts layer for a few tokens (any number is taken, 64 at a time: each further 64 read the experts' weights again).
+ *       logits[t][e] = sum_h x[t][h] * router[e][h];   the top_k experts of a token by their logits, ties to the lowest index
+ *       weight       = softmax of the logits over all experts; with `renormalise` over the chosen ones
+ *       y[t]         = sum over the choices of weight * Down_e (silu(Gate_e x[t]) * (Up_e x[t]))
+ *   x        device, [T] rows of H values of `type`, `ldx` values apart;  router  device [E][H] of `type`;  y  device [T][H]
+ *   gate, up prepared, E matrices of I rows and H columns each, group_up, zeros_up;  down  E matrices of H rows and I columns, group_down, zeros_down
+ *   experts  device int32 [T][top_k] and weights device float [T][top_k]: the choices, best first
+ *   workspace  bs_w4_moe_workspace_bytes(...) bytes; two calls that may run at the same time need one each
+ * Supported: E up to 512, top_k up to 32, T up to 16384.  Three launches; hidden values keep 16 bits of mantissa and the range of binary32.
+ */
+size_t bs_w4_moe_workspace_bytes(int T, int top_k, int H, int I, long long ldx);
+int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, int H, int I, const void* gate, const void* up,
+              int group_up, int zeros_up, const void* down, int group_down, int zeros_down, bs_float_t type, int top_k,
+              int renormalise, void* y, int32_t* experts, float* weights, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * bs_popc_rate -- register-only micro-benchmark of the SM population-count pipe: every thread runs
  * `iters` rounds of independent  acc += popc(x & y)  chains.  Writes the measured rate in
  * popc32(AND) word-operations per second to *wordops_per_s (HOST pointer).  Synchronises the device.

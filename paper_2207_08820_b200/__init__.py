@@ -9,6 +9,7 @@ import importlib
 
 _API_NAMES = ("bitpack_activations", "bitunpack_activations", "pack_weights", "bs_pack_rows",
               "bitserial_conv2d", "bitserial_gemm", "bs_check_status", "bs_popc_rate",
+              "quantise_w4", "prepare_w4", "gemm_w4", "moe_w4", "W4Weights",
               "UNSIGNED", "SIGNED", "BIPOLAR", "NCHW", "NHWC")
 
 

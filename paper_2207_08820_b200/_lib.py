@@ -167,6 +167,21 @@ def lib() -> ctypes.CDLL:
     L.bs_requant_bounds.argtypes = [i, ctypes.c_float, i, i, i, i, i, ctypes.POINTER(ctypes.c_float)]
     L.bs_selftest_wait_timeout.restype = i
     L.bs_selftest_wait_timeout.argtypes = [i, vp]
+    sz, ll = ctypes.c_size_t, ctypes.c_longlong
+    L.bs_w4_quantise.restype = i
+    L.bs_w4_quantise.argtypes = [vp, i, i, i, ll, i, i, vp, vp, vp, vp]
+    L.bs_w4_bytes.restype = sz
+    L.bs_w4_bytes.argtypes = [i] * 4
+    L.bs_w4_prepare.restype = i
+    L.bs_w4_prepare.argtypes = [vp, vp, vp, i, i, i, i, vp, vp]
+    L.bs_w4_gemm_workspace_bytes.restype = sz
+    L.bs_w4_gemm_workspace_bytes.argtypes = [i, i, ll]
+    L.bs_w4_gemm.restype = i
+    L.bs_w4_gemm.argtypes = [vp, ll, i, vp, i, i, i, i, i, vp, vp, ll, vp, sz, vp]
+    L.bs_w4_moe_workspace_bytes.restype = sz
+    L.bs_w4_moe_workspace_bytes.argtypes = [i, i, i, i, ll]
+    L.bs_w4_moe.restype = i
+    L.bs_w4_moe.argtypes = [vp, ll, i, vp, i, i, i, vp, vp, i, i, vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
     L.bs_popc_rate.restype = i
     L.bs_popc_rate.argtypes = [i, ctypes.POINTER(ctypes.c_double)]
     L.bs_status_string.restype = ctypes.c_char_p
@@ -181,4 +196,5 @@ EXPORTED = ("bs_packed_act_bytes", "bs_packed_wgt_bytes", "bs_packed_rows_bytes"
             "bitserial_gemm_noalloc", "bs_gemm_noalloc_max_scratch_bytes", "bs_selftest_dirty_noalloc_scratch",
             "bs_tc_weights_bytes", "bs_tc_weights_read_bytes", "bs_tc_prepare_weights", "bs_tc_supported", "bitserial_conv2d_tc", "bitserial_conv2d_tc_chained", "bs_tc_chain_workspace_bytes", "bitserial_conv2d_tc_chain", "bitserial_gemm_tc", "bs_sequence_create", "bs_sequence_create_ws", "bs_sequence_workspace_bytes", "bs_sequence_launches", "bs_sequence_layer_plan", "bs_sequence_input", "bs_sequence_run_ready", "bitpack_activations_operands", "bs_stem_codes_operands_f32", "bs_sequence_run", "bs_sequence_destroy", "bs_l2_prefetch",
             "bs_conv2d_f32", "bs_maxpool2d_f32", "bs_stem_codes_f32", "bs_stem_codes_supported", "bs_avgpool_codes_f32", "bs_fc_f32",
-            "bs_check_status", "bs_quantiser_bounds", "bs_requant_bounds", "bs_selftest_wait_timeout", "bs_popc_rate", "bs_status_string")
+            "bs_check_status", "bs_quantiser_bounds", "bs_requant_bounds", "bs_selftest_wait_timeout", "bs_popc_rate", "bs_status_string",
+            "bs_w4_quantise", "bs_w4_bytes", "bs_w4_prepare", "bs_w4_gemm_workspace_bytes", "bs_w4_gemm", "bs_w4_moe_workspace_bytes", "bs_w4_moe")

@@ -7,7 +7,7 @@ happens here and nothing falls back to PyTorch ops.
 from __future__ import annotations
 
 import ctypes
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -330,6 +330,76 @@ def fc_f32(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
         out = torch.empty(N, J, dtype=torch.float32, device=x.device)
     _check(lib().bs_fc_f32(_ptr(x), _ptr(w), _ptr(bias), N, K, J, _ptr(out), _stream_ptr(stream)), "bs_fc_f32")
     return out
+
+
+class W4Weights(NamedTuple):
+    """Weights of 4 bits with a scale per group, laid out for :func:`gemm_w4` and :func:`moe_w4` (:func:`prepare_w4`)."""
+    data: torch.Tensor      # uint8, ``matrices`` times ``bs_w4_bytes``
+    matrices: int           # experts, 1 for a single matrix
+    O: int
+    K: int
+    group: int
+    zeros: bool             # they have zero points
+    dtype: torch.dtype      # of the scales, and of the activations they go with
+
+
+_FLOAT_TYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _group(group: Optional[int], K: int) -> int:
+    return group if group is not None else -(-K // 128) * 128
+
+
+def quantise_w4(w: torch.Tensor, group: Optional[int] = 128, *, zeros: bool = False, dtype: Optional[torch.dtype] = None, stream=None):
+    """Float weights [..., O, K] to 4 bits, a scale (and with ``zeros`` a zero point) per ``group`` columns of a row (None: per row): returns (codes int8
+    [..., O, K], scales [..., O, G], zero points int8 [..., O, G] or None), with w ~ scales * (codes - zero points).  ``dtype``: of the scales,
+    float16 or bfloat16 (default: w's, bfloat16 where w is float32).  Rounding as stated at ``bs_w4_quantise``."""
+    if dtype is None:
+        dtype = w.dtype if w.dtype != torch.float32 else torch.bfloat16
+    if w.dim() < 2:
+        raise ValueError("weights of two or more dimensions expected")
+    st, codes, scales, z = native().w4_quantise(w, _group(group, w.shape[-1]), zeros, _FLOAT_TYPES.get(dtype, -1), stream)
+    _check(st, "bs_w4_quantise")
+    return codes, scales, z
+
+
+def prepare_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None, *, group: Optional[int] = 128, stream=None) -> W4Weights:
+    """Codes int8 [O, K] (or [E, O, K], the experts of a layer), scales float16 or bfloat16 [..., O, G] and int8 zero points [..., O, G] to the layout of the
+    products, once per matrix.  Codes are -8..7 without zero points, 0..15 with them."""
+    if codes.dim() not in (2, 3):
+        raise ValueError("codes [O, K] or [E, O, K] expected")
+    group = _group(group, codes.shape[-1])
+    st, data = native().w4_prepare(codes, scales, zeros, group, stream)
+    _check(st, "bs_w4_prepare")
+    return W4Weights(data, codes.shape[0] if codes.dim() == 3 else 1, codes.shape[-2], codes.shape[-1], group, zeros is not None, scales.dtype)
+
+
+def gemm_w4(x: torch.Tensor, w: W4Weights, bias: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x [..., K] float16 or bfloat16 times the transpose of weights of 4 bits [O, K], plus ``bias`` [O]: [..., O] of x's type (``bs_w4_gemm``).  One row
+    of x (a token) or many; the rows of a matrix may be apart.  No gradients."""
+    global launch_count
+    if w.matrices != 1:
+        raise ValueError("the weights of one matrix expected")
+    st, y = native().w4_gemm(x, w.data, w.O, w.K, w.group, w.zeros, _FLOAT_TYPES[w.dtype], bias, out, stream)
+    if st != 0:
+        raise BitserialError(st, "bs_w4_gemm")
+    launch_count += 1
+    return y
+
+
+def moe_w4(x: torch.Tensor, router: torch.Tensor, gate: W4Weights, up: W4Weights, down: W4Weights, top_k: int, *, renormalise: bool = True,
+           out: Optional[torch.Tensor] = None, stream=None):
+    """A mixture-of-experts layer for a few tokens (``bs_w4_moe``): x [..., H], ``router`` [E, H], experts ``gate`` and ``up`` [E, I, H], ``down`` [E, H, I].
+    Returns (y [..., H] of x's type, the chosen experts int32 [..., top_k], best first, and their weights float32 [..., top_k]).  No gradients."""
+    global launch_count
+    E, H = router.shape
+    if not (gate[1:] == up[1:] and gate.K == H and down[1:4] == (E, H, gate.O) and gate.matrices == E and gate.dtype == down.dtype):
+        raise ValueError("gate and up [E, I, H], down [E, H, I] of one type expected")
+    st, y, experts, weights = native().w4_moe(x, router, gate.data, up.data, down.data, gate.O, gate.group, gate.zeros, down.group, down.zeros,
+                                              _FLOAT_TYPES[gate.dtype], top_k, renormalise, out, stream)
+    _check(st, "bs_w4_moe")
+    launch_count += 2
+    return y, experts, weights
 
 
 def bs_check_status(stream=None) -> None:

@@ -3,6 +3,7 @@
 // about it is made here.
 #include <ATen/cuda/EmptyTensor.h>
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -301,8 +302,237 @@ PyObject* unchanged(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- 4-bit weights with a scale per group
+
+// The device of a call's tensors and its stream are the current ones while its memory is taken and its work enqueued: what the call allocates belongs
+// to the stream that it runs on.  `stream` argument: None (the device's current stream) or a torch stream of that device.
+struct OnStream {
+    c10::cuda::OptionalCUDAGuard device;
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    void* stream;
+    OnStream(const at::Tensor& x, PyObject* o)
+    {
+        if (!x.is_cuda()) mismatch("expected a contiguous CUDA tensor");
+        const c10::DeviceIndex at = x.get_device();
+        if (at != c10::cuda::current_device()) device.set_index(at);
+        if (o == Py_None) {
+            stream = c10::cuda::getCurrentCUDAStream(at).stream();
+            return;
+        }
+        const int64_t id = attribute(o, "stream_id"), index = attribute(o, "device_index"), type = attribute(o, "device_type");
+        if (index != at) mismatch("the stream belongs to another device than the tensors");
+        const c10::cuda::CUDAStream s = c10::cuda::CUDAStream::unpack3(id, static_cast<c10::DeviceIndex>(index), static_cast<c10::DeviceType>(type));
+        guard.reset_stream(s);
+        stream = s.stream();
+    }
+    static int64_t attribute(PyObject* o, const char* name)
+    {
+        PyObject* v = PyObject_GetAttrString(o, name);
+        if (!v) throw Fail();
+        const int64_t r = PyLong_AsLongLong(v);
+        Py_DECREF(v);
+        if (r == -1 && PyErr_Occurred()) throw Fail();
+        return r;
+    }
+};
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType t, const at::Tensor& like) { return at::detail::empty_cuda(shape, t, like.device(), std::nullopt); }
+void same_device(const at::Tensor& t, const at::Tensor& x) { if (t.device() != x.device()) mismatch("tensors on different devices"); }
+bs_float_t float_type(const at::Tensor& t)
+{
+    const at::ScalarType k = t.scalar_type();
+    if (k != at::kFloat && k != at::kHalf && k != at::kBFloat16) mismatch("float32, float16 or bfloat16 expected");
+    return k == at::kFloat ? BS_F32 : k == at::kHalf ? BS_F16 : BS_BF16;
+}
+// Rows of K values: a contiguous tensor, or a matrix whose rows are.  Returns how far apart they are.
+int64_t row_pitch(const at::Tensor& t, int64_t K)
+{
+    if (t.is_contiguous()) return K;
+    if (t.dim() != 2 || t.stride(1) != 1) mismatch("expected a contiguous tensor or a matrix with contiguous rows");
+    return t.size(0) == 1 ? K : t.stride(0);
+}
+int small(int64_t v) { if (v > 0x7fffffff) mismatch("tensor too large"); return static_cast<int>(v); }
+bool overlap(const at::Tensor& a, int64_t a_pitch, const at::Tensor& b, int64_t b_pitch)
+{
+    auto end = [](const at::Tensor& t, int64_t pitch) {
+        const int64_t K = t.size(-1), rows = t.numel() / K;
+        return static_cast<const char*>(t.const_data_ptr()) + ((rows - 1) * pitch + K) * t.element_size();
+    };
+    return static_cast<const char*>(a.const_data_ptr()) < end(b, b_pitch) && static_cast<const char*>(b.const_data_ptr()) < end(a, a_pitch);
+}
+const void* prepared_w4(const at::Tensor& t, const at::Tensor& x, int64_t matrices, int O, int K, int group, int zeros)
+{
+    const size_t bytes = bs_w4_bytes(O, K, group, zeros);
+    if (bytes == 0 || t.nbytes() != bytes * matrices) mismatch("prepared weights of another size");
+    same_device(t, x);
+    return pointer(t);
+}
+
+// w, group, zeros, type (bs_float_t of the scales), stream
+PyObject* w4_quantise(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 5);
+        const at::Tensor& w = tensor(a[0]);
+        if (w.dim() < 2 || w.numel() == 0) mismatch("weights of two or more dimensions, none of them zero, expected");
+        const int group = integer(a[1]), zeros = PyObject_IsTrue(a[2]);
+        const bs_float_t type = static_cast<bs_float_t>(integer(a[3])), from = float_type(w);
+        if (group <= 0 || (type != BS_F16 && type != BS_BF16)) mismatch("a positive group and scales of float16 or bfloat16 expected");
+        const OnStream on(w, a[4]);
+        const int K = small(w.size(-1)), O = small(w.numel() / K);
+        const int64_t ld = row_pitch(w, K);
+        std::vector<int64_t> shape(w.sizes().begin(), w.sizes().end());
+        const at::Tensor codes = fresh(shape, at::kChar, w);
+        shape.back() = (K + static_cast<int64_t>(group) - 1) / group;
+        const at::Tensor scales = fresh(shape, type == BS_F16 ? at::kHalf : at::kBFloat16, w);
+        at::Tensor z;
+        if (zeros) z = fresh(shape, at::kChar, w);
+        int rc;
+        {
+            NoGil free;
+            rc = bs_w4_quantise(w.const_data_ptr(), from, O, K, ld, group, type, static_cast<int8_t*>(codes.data_ptr()), scales.data_ptr(),
+                                zeros ? static_cast<int8_t*>(z.data_ptr()) : nullptr, on.stream);
+        }
+        return Py_BuildValue("(iNNN)", rc, give(codes), give(scales), give(z));
+    });
+}
+
+// codes [O, K] or [E, O, K], scales, zeros or None, group, stream
+PyObject* w4_prepare(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 5);
+        const at::Tensor &codes = tensor(a[0]), &scales = tensor(a[1]);
+        if (codes.scalar_type() != at::kChar || (codes.dim() != 2 && codes.dim() != 3) || codes.numel() == 0) mismatch("int8 codes [O, K] or [E, O, K] expected");
+        const int group = integer(a[3]);
+        if (group <= 0) mismatch("a positive group expected");
+        const int K = small(codes.size(-1)), O = small(codes.size(-2)), E = codes.dim() == 3 ? small(codes.size(0)) : 1;
+        const int64_t G = (K + static_cast<int64_t>(group) - 1) / group;
+        auto fits = [&](const at::Tensor& t) {
+            if (t.dim() != codes.dim() || t.size(-1) != G || t.size(-2) != O || (E > 1 && t.size(0) != E) || t.numel() != static_cast<int64_t>(E) * O * G)
+                mismatch("one scale (and zero point) per group of a row expected");
+            same_device(t, codes);
+        };
+        fits(scales);
+        if (float_type(scales) == BS_F32) mismatch("scales of float16 or bfloat16 expected");
+        const int8_t* z = nullptr;
+        if (a[2] != Py_None) {
+            const at::Tensor& t = tensor(a[2]);
+            if (t.scalar_type() != at::kChar) mismatch("int8 zero points expected");
+            fits(t);
+            z = static_cast<const int8_t*>(pointer(t));
+        }
+        const OnStream on(codes, a[4]);
+        const size_t bytes = bs_w4_bytes(O, K, group, z != nullptr);
+        if (bytes == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_ERR_UNSUPPORTED), Py_NewRef(Py_None));
+        const void *cp = pointer(codes), *sp = pointer(scales);
+        const at::Tensor out = fresh({static_cast<int64_t>(bytes * E)}, at::kByte, codes);
+        int rc;
+        {
+            NoGil free;
+            rc = bs_w4_prepare(static_cast<const int8_t*>(cp), sp, z, E, O, K, group, out.data_ptr(), on.stream);
+        }
+        return Py_BuildValue("(iN)", rc, give(out));
+    });
+}
+
+// x, prepared, O, K, group, zeros, type, bias or None, out or None, stream
+PyObject* w4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 10);
+        const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
+        const int O = integer(a[2]), K = integer(a[3]), group = integer(a[4]), zeros = integer(a[5]), type = integer(a[6]);
+        if (x.dim() < 1 || x.size(-1) != K) mismatch("the last dimension of x is not the weights' number of columns");
+        if (float_type(x) != type) mismatch("x is not of the scales' type");
+        const OnStream on(x, a[9]);
+        const void* wp = prepared_w4(w, x, 1, O, K, group, zeros);
+        const int M = small(x.numel() / K);
+        const int64_t ldx = row_pitch(x, K);
+        const void* bias = nullptr;
+        if (a[7] != Py_None) {
+            const at::Tensor& b = tensor(a[7]);
+            if (b.scalar_type() != x.scalar_type() || b.dim() != 1 || b.size(0) != O) mismatch("a bias of x's type, one value per row of the weights, expected");
+            same_device(b, x);
+            bias = pointer(b);
+        }
+        std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = O;
+        at::Tensor y;
+        int64_t ldy = O;
+        if (a[8] != Py_None) {
+            y = tensor(a[8]);
+            if (!y.is_cuda() || y.scalar_type() != x.scalar_type() || y.sizes() != at::IntArrayRef(shape)) mismatch("an output of x's type and the product's shape expected");
+            same_device(y, x);
+            ldy = row_pitch(y, O);
+            if (M > 0 && (overlap(y, ldy, x, ldx) || overlap(y, ldy, w, w.numel()))) mismatch("the output overlaps an input");
+        } else {
+            y = fresh(shape, x.scalar_type(), x);
+        }
+        if (M == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(y));
+        const size_t need_ws = bs_w4_gemm_workspace_bytes(M, K, ldx);
+        at::Tensor ws;
+        if (need_ws) ws = fresh({static_cast<int64_t>(need_ws)}, at::kByte, x);
+        void* yp = y.data_ptr();
+        int rc;
+        {
+            NoGil free;
+            rc = bs_w4_gemm(x.const_data_ptr(), ldx, M, wp, O, K, group, zeros, static_cast<bs_float_t>(type), bias, yp, ldy, need_ws ? ws.data_ptr() : nullptr, need_ws,
+                            on.stream);
+        }
+        return Py_BuildValue("(iN)", rc, give(y));
+    });
+}
+
+// x, router, gate, up, down, I, group_up, zeros_up, group_down, zeros_down, type, top_k, renormalise, out or None, stream
+PyObject* w4_moe(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 15);
+        const at::Tensor &x = tensor(a[0]), &router = tensor(a[1]);
+        const int I = integer(a[5]), gu = integer(a[6]), zu = integer(a[7]), gd = integer(a[8]), zd = integer(a[9]), type = integer(a[10]), top_k = integer(a[11]),
+                  renormalise = PyObject_IsTrue(a[12]);
+        if (router.dim() != 2 || router.numel() == 0) mismatch("a router [E, H] expected");
+        const int E = small(router.size(0)), H = small(router.size(1));
+        if (x.dim() < 1 || x.size(-1) != H) mismatch("the last dimension of x is not the router's number of columns");
+        if (float_type(x) != type || router.scalar_type() != x.scalar_type()) mismatch("x and the router are not of the scales' type");
+        if (top_k < 1 || top_k > E) mismatch("top_k is not between one and the number of experts");
+        const OnStream on(x, a[14]);
+        same_device(router, x);
+        const void* rp = pointer(router);
+        const void *gate = prepared_w4(tensor(a[2]), x, E, I, H, gu, zu), *up = prepared_w4(tensor(a[3]), x, E, I, H, gu, zu),
+                   *down = prepared_w4(tensor(a[4]), x, E, H, I, gd, zd);
+        const int T = small(x.numel() / H);
+        const int64_t ldx = row_pitch(x, H);
+        at::Tensor y;
+        if (a[13] != Py_None) {
+            y = tensor(a[13]);
+            if (y.scalar_type() != x.scalar_type() || y.sizes() != x.sizes()) mismatch("an output of x's type and shape expected");
+            same_device(y, x);
+            pointer(y);
+            if (T > 0 && overlap(y, H, x, ldx)) mismatch("the output overlaps an input");
+        } else {
+            y = fresh(x.sizes(), x.scalar_type(), x);
+        }
+        std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = top_k;
+        const at::Tensor experts = fresh(shape, at::kInt, x), weights = fresh(shape, at::kFloat, x);
+        if (T == 0) return Py_BuildValue("(iNNN)", static_cast<int>(BS_OK), give(y), give(experts), give(weights));
+        const size_t bytes = bs_w4_moe_workspace_bytes(T, top_k, H, I, ldx);
+        const at::Tensor ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, x);
+        void *yp = y.data_ptr(), *wsp = ws.data_ptr();
+        int rc;
+        {
+            NoGil free;
+            rc = bs_w4_moe(x.const_data_ptr(), ldx, T, rp, E, H, I, gate, up, gu, zu, down, gd, zd, static_cast<bs_float_t>(type), top_k, renormalise, yp,
+                           static_cast<int32_t*>(experts.data_ptr()), static_cast<float*>(weights.data_ptr()), wsp, bytes, on.stream);
+        }
+        return Py_BuildValue("(iNNN)", rc, give(y), give(experts), give(weights));
+    });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(conv2d), FAST(gemm), FAST(bitpack), FAST(bitpack_operands), FAST(sequence_run), FAST(unchanged), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {FAST(conv2d), FAST(gemm), FAST(bitpack), FAST(bitpack_operands), FAST(sequence_run), FAST(unchanged),
+                         FAST(w4_quantise), FAST(w4_prepare), FAST(w4_gemm), FAST(w4_moe), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,49 @@
+// Weights of 4 bits with a scale (and zero point) per group of the reduction, laid out for the tensor cores: shared by csrc/w4_*.cu.
+//
+// A prepared matrix of O rows and K columns is, one after the other,
+//   codes   [ceil(O/16)][ceil(K/128)] blocks of 1 KB: [t 0..3][row 0..15][word j 0..3], a word holds the stored codes (0..15) of columns
+//           32 j + 8 t + (0..7): nibble i < 4 is column 2 i, nibble i >= 4 column 2 (i - 4) + 1, so that (word >> 4 i) & 0x000f000f is a pair of
+//           neighbouring columns, one in each half.  16 bytes are one row's part of what lane t of a quad multiplies (mma.sync), and four of
+//           them are a row's 128 columns for the thread that owns the row (tensor memory); either way a warp reads whole lines.
+//   steps   [ceil(O/16)][G][8] entries of 4 bytes, G = ceil(K / group): the scales, of the activations' type, of rows r and r + 8 of a block, which are
+//           the rows that a lane of an mma.sync fragment owns; where the weights have zero points entries of 8 bytes, the second word with
+//           the two zero points in its halves.  Without zero points the codes are stored plus 8, and 8 is the zero.
+// Rows and columns beyond O and K hold the code that stands for zero, steps beyond O are zero.
+#pragma once
+#include "common.cuh"
+
+namespace bs {
+
+constexpr int W4_ROWS = 16, W4_COLS = 128, W4_BLOCK = W4_ROWS * W4_COLS / 2;
+constexpr int W4_MAX_DIM = 1 << 20;     // rows, columns and columns of a group
+
+struct W4Layout {
+    int O, K, group, zeros;     // zeros: the matrix has zero points
+    int rbs, cbs, G;            // blocks of rows, blocks of columns, groups of a row
+    __host__ __device__ size_t codes_bytes() const { return static_cast<size_t>(rbs) * cbs * W4_BLOCK; }
+    __host__ __device__ size_t bytes() const { return codes_bytes() + static_cast<size_t>(rbs) * G * (zeros ? 64 : 32); }
+};
+
+// Groups of 32 or 64 columns, or a multiple of 128: a block of columns then holds 4, 2 or 1 of them (or a part of one).
+inline bool w4_group_ok(int group) { return group == 32 || group == 64 || (group > 0 && group <= W4_MAX_DIM && group % 128 == 0); }
+
+inline bool w4_layout(int O, int K, int group, int zeros, W4Layout& l)
+{
+    if (O <= 0 || K <= 0 || O > W4_MAX_DIM || K > W4_MAX_DIM || !w4_group_ok(group)) return false;
+    l.O = O; l.K = K; l.group = group; l.zeros = zeros != 0;
+    l.rbs = ceil_div(O, W4_ROWS); l.cbs = ceil_div(K, W4_COLS); l.G = ceil_div(K, group);
+    return true;
+}
+
+// The arguments of a product, as every kernel of it takes them.
+struct W4Gemm {
+    const void* x;              // [M] rows of K values, `ldx` apart
+    const unsigned char* w;     // prepared matrix
+    const void* bias;           // [O] or null
+    void* y;                    // [M] rows of O values, `ldy` apart
+    long long ldx, ldy;
+    int M;
+    W4Layout l;
+};
+
+}  // namespace bs

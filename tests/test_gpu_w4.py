@@ -1,0 +1,380 @@
+"""Grouped 4-bit weights on the GPU: quantiser, layout, the product with 16-bit activations and the mixture-of-experts layer, against their definitions in
+64 bits (w4_reference.py).  Tolerances are the roundings': half a step of the output's type, and a step of the tensor cores' 32-bit sums for every
+addition."""
+import numpy as np
+import pytest
+import torch
+
+import w4_reference as ref
+from paper_2207_08820_b200 import api
+from paper_2207_08820_b200._lib import BitserialError
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+GUARD = 77.0
+
+
+def weights(rng, O, K, group, dtype, zeros, lead=()):
+    G = -(-K // group)
+    codes = torch.from_numpy(rng.integers(0 if zeros else -8, 16 if zeros else 8, (*lead, O, K)).astype(np.int8))
+    scales = torch.from_numpy(((rng.random((*lead, O, G)) + 0.5) * 0.2 / np.sqrt(K)).astype(np.float32)).to(dtype)
+    z = torch.from_numpy(rng.integers(0, 16, (*lead, O, G)).astype(np.int8)) if zeros else None
+    return codes, scales, z
+
+
+def prepared(w, group):
+    codes, scales, z = w
+    return api.prepare_w4(codes.cuda(), scales.cuda(), None if z is None else z.cuda(), group=group)
+
+
+def normal(rng, shape, dtype):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(dtype)
+
+
+def check_gemm(rng, M, O, K, group, dtype, zeros, bias):
+    w = weights(rng, O, K, group, dtype, zeros)
+    x, b = normal(rng, (M, K), dtype), normal(rng, (O,), dtype) if bias else None
+    want, far = ref.gemm(x, ref.matrix(*w, group), b, dtype)
+    # guard values around the output, its rows apart
+    pitch = (O + 7) // 8 * 8 + 8
+    room = torch.full((M + 2, pitch), GUARD, dtype=dtype, device="cuda")
+    out = room[1:M + 1, :O]
+    got = api.gemm_w4(x.cuda(), prepared(w, group), None if b is None else b.cuda(), out=out)
+    api.bs_check_status()
+    assert got.data_ptr() == out.data_ptr()
+    assert ((out.cpu().double() - want).abs() <= far).all(), ((out.cpu().double() - want).abs() / far).max()
+    room[1:M + 1, :O] = GUARD
+    assert (room == GUARD).all(), "written beside the output"
+
+
+# ------------------------------------------------------------------------------------------------------------------ quantiser
+
+@pytest.mark.parametrize("source", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("O,K,group", [(1, 1, 32), (3, 40, 32), (17, 128, 128), (5, 131, 64), (9, 1000, 256), (33, 513, 384), (64, 264, 128), (7, 4096, 4096)])
+def test_quantise(source, dtype, zeros, O, K, group):
+    rng = np.random.default_rng(O * K + group)
+    w = normal(rng, (O, K), source) * 0.05
+    codes, scales, z = api.quantise_w4(w.cuda(), group, zeros=zeros, dtype=dtype)
+    c, s, p = ref.quantise(w, group, zeros, dtype)
+    assert np.array_equal(scales.double().cpu().numpy(), s)
+    assert np.array_equal(codes.cpu().numpy(), c)
+    assert (z is None) == (not zeros) and (not zeros or np.array_equal(z.cpu().numpy(), p))
+    if not zeros:       # half a step, and what the rounding of the scale (2^-9 of 7 steps at most, bf16) takes from the largest ones
+        back = ref.matrix(codes.cpu(), scales.cpu(), None, group)
+        step = scales.cpu().double()[:, torch.arange(K) // group]
+        assert ((back - w.double()).abs() <= step * (0.5 + 7 * torch.finfo(dtype).eps)).all()
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_quantise_ties_and_extremes(zeros):
+    """Quotients on ties and beside them by less than a float tells apart; groups of zeros, of values below the type, above it, infinities and NaN."""
+    K = 32
+    rows = []
+    for s in (1.0, 0.75, 0.3203125):                 # the scale comes out as s: max / 7 (or the span / 15) is exact
+        row = np.zeros(K, np.float64)
+        row[0], row[1] = (15 * s, 0) if zeros else (7 * s, -7 * s)
+        n = 6 if zeros else 3
+        for i in range(10):
+            t = np.float32((0.5 + i % n) * s)
+            row[2 + 3 * i:5 + 3 * i] = [t, np.nextafter(t, np.float32(9)), np.nextafter(t, np.float32(-9))]
+        rows.append(row)
+    rows += [np.zeros(K), np.full(K, 1e-9), np.linspace(-1e30, 1e30, K), np.where(np.arange(K) == 3, np.inf, 1.0), np.where(np.arange(K) == 5, -np.inf, 1.0),
+             np.where(np.arange(K) == 7, np.nan, 1.0), np.full(K, np.nan), np.full(K, -2.0)]
+    w = torch.from_numpy(np.array(rows, np.float32))
+    for dtype in (BF16, F16):
+        for wide in (w, torch.cat([w, w[:, :1]], 1)[:, :K]):        # the second has rows of 33 floats: the other kernel
+            src = wide.cuda() if wide.is_contiguous() else torch.cat([w, w[:, :1]], 1).cuda()[:, :K]
+            codes, scales, z = api.quantise_w4(src, 32, zeros=zeros, dtype=dtype)
+            c, s, p = ref.quantise(w, 32, zeros, dtype)
+            assert np.array_equal(scales.double().cpu().numpy(), s)
+            assert np.array_equal(codes.cpu().numpy(), c)
+            assert not zeros or np.array_equal(z.cpu().numpy(), p)
+
+
+def test_quantise_experts_and_defaults():
+    rng = np.random.default_rng(5)
+    w = normal(rng, (3, 10, 96), BF16)
+    codes, scales, z = api.quantise_w4(w.cuda(), None)
+    assert codes.shape == (3, 10, 96) and scales.shape == (3, 10, 1) and scales.dtype == BF16 and z is None
+    one, s, _ = api.quantise_w4(w[1].cuda(), None)
+    assert torch.equal(codes[1], one) and torch.equal(scales[1], s)
+    assert api.quantise_w4(w.float().cuda())[1].dtype == BF16
+
+
+# -------------------------------------------------------------------------------------------------------------------- product
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("zeros,bias", [(False, False), (True, True)])
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+@pytest.mark.parametrize("M,O,K", [(1, 1, 1), (1, 17, 129), (2, 16, 128), (3, 40, 100), (8, 33, 1000), (9, 64, 1152), (16, 100, 333), (17, 130, 260), (33, 31, 2050)])
+def test_gemm_small(dtype, zeros, bias, group, M, O, K):
+    check_gemm(np.random.default_rng(M * O + K + group), M, O, K, group, dtype, zeros, bias)
+
+
+@pytest.mark.parametrize("M,O,K,group,dtype,zeros,bias", [
+    (1, 4096, 4096, 128, BF16, False, False), (1, 6000, 1536, 384, F16, True, True), (8, 5000, 2304, 64, BF16, True, False),
+    (31, 1383, 4611, 32, BF16, True, True), (64, 512, 4608, 128, F16, False, True), (65, 300, 640, 64, BF16, False, False),
+    (127, 257, 2304, 128, BF16, True, False), (128, 128, 576, 128, F16, False, False), (129, 640, 1024, 1024, BF16, False, True),
+    (200, 1024, 1000, 32, F16, True, True), (257, 384, 2056, 64, BF16, True, True), (300, 100, 264, 128, F16, False, False),
+    (513, 2000, 512, 256, BF16, True, True), (1000, 129, 1153, 128, F16, True, False)])
+def test_gemm_larger(M, O, K, group, dtype, zeros, bias):
+    check_gemm(np.random.default_rng(M + O + K), M, O, K, group, dtype, zeros, bias)
+
+
+@pytest.mark.parametrize("M", [1, 5, 20, 40, 150])
+@pytest.mark.parametrize("pitch", [200, 203, 208])
+def test_gemm_rows_apart(M, pitch):
+    """Rows of x that are slices of wider ones, on and off 16-byte boundaries; what lies between them is NaN."""
+    rng = np.random.default_rng(M + pitch)
+    K, O, group = 197, 48, 64
+    w = weights(rng, O, K, group, BF16, True)
+    x = normal(rng, (M, K), BF16)
+    wide = torch.full((M, pitch), float("nan"), dtype=BF16)
+    wide[:, :K] = x
+    want, far = ref.gemm(x, ref.matrix(*w, group), None, BF16)
+    y = api.gemm_w4(wide.cuda()[:, :K], prepared(w, group))
+    assert ((y.cpu().double() - want).abs() <= far).all()
+
+
+def test_gemm_leading_dimensions_and_no_rows():
+    rng = np.random.default_rng(1)
+    w = prepared(weights(rng, 40, 72, 32, F16, False), 32)
+    x = normal(rng, (2, 3, 72), F16).cuda()
+    y = api.gemm_w4(x, w)
+    assert y.shape == (2, 3, 40) and torch.equal(y.view(6, 40), api.gemm_w4(x.view(6, 72), w))
+    assert torch.equal(api.gemm_w4(x[0, 0], w), api.gemm_w4(x[:1, 0], w)[0])
+    assert api.gemm_w4(x[:0], w).shape == (0, 3, 40)
+
+
+@pytest.mark.parametrize("M", [5, 150])
+def test_gemm_special_values_stay_in_their_rows(M):
+    rng = np.random.default_rng(M)
+    w = weights(rng, 70, 300, 32, BF16, True)
+    x = normal(rng, (M, 300), BF16)
+    x[1, 7], x[3, 299] = float("inf"), float("nan")
+    w[1][4, 2] = float("inf")
+    want, far = ref.gemm(x, ref.matrix(*w, 32), None, BF16)
+    y = api.gemm_w4(x.cuda(), prepared(w, 32)).cpu().double()
+    fine = torch.isfinite(want)
+    assert torch.equal(torch.isfinite(y), fine)
+    assert ((y - want).abs()[fine] <= far[fine]).all()
+    assert fine[0].sum() == 69 and not fine[1].any() and not fine[3].any()
+
+
+@pytest.mark.parametrize("M,O,K", [(1, 2048, 2048), (16, 512, 1000), (64, 384, 2304), (300, 1000, 1152)])
+def test_gemm_same_bits_every_time(M, O, K):
+    rng = np.random.default_rng(M)
+    w = prepared(weights(rng, O, K, 64, BF16, True), 64)
+    x = normal(rng, (M, K), BF16).cuda()
+    first = api.gemm_w4(x, w)
+    for _ in range(20):
+        assert torch.equal(api.gemm_w4(x, w), first)
+
+
+@pytest.mark.parametrize("M,K", [(1, 512), (6, 515), (150, 512), (150, 515)])
+def test_gemm_captured_beside_other_calls(M, K):
+    """Two graphs of different products replayed in turn with eager calls between them: none reads what another keeps."""
+    rng = np.random.default_rng(M)
+    ws = [prepared(weights(rng, 200, K, 128, F16, False), 128) for _ in range(2)]
+    xs = [normal(rng, (M, K), F16).cuda() for _ in range(2)]
+    outs = [torch.empty(M, 200, dtype=F16, device="cuda") for _ in range(2)]
+    api.gemm_w4(xs[0], ws[0])
+    graphs = []
+    for x, w, out in zip(xs, ws, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            api.gemm_w4(x, w, out=out)
+        graphs.append(g)
+    for _ in range(3):
+        for x in xs:
+            x.copy_(normal(rng, (M, K), F16))
+        graphs[0].replay()
+        eager = api.gemm_w4(xs[1], ws[0])
+        graphs[1].replay()
+        want = [api.gemm_w4(x, w) for x, w in zip(xs, ws)]
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1])
+        assert torch.equal(eager, api.gemm_w4(xs[1], ws[0]))
+
+
+@pytest.mark.parametrize("M,K", [(3, 1024), (3, 1023), (140, 1023)])
+def test_gemm_on_another_stream(M, K):
+    rng = np.random.default_rng(K)
+    w = prepared(weights(rng, 300, K, 128, BF16, True), 128)
+    xs = [normal(rng, (M, K), BF16).cuda() for _ in range(8)]
+    want = [api.gemm_w4(x, w) for x in xs]
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    torch.cuda.synchronize()
+    got = [api.gemm_w4(x, w, stream=streams[i % 4]) for i, x in enumerate(xs)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_weights_prepared_and_used_at_once():
+    """The product that follows the set-up in a stream reads what it wrote, also where the memory held other weights before."""
+    rng = np.random.default_rng(8)
+    sets = [weights(rng, 512, 1024, 128, BF16, False) for _ in range(4)]
+    x = normal(rng, (2, 1024), BF16)
+    on = [[t.cuda() for t in s[:2]] for s in sets]
+    xd = x.cuda()
+    for _ in range(5):
+        got = [api.gemm_w4(xd, api.prepare_w4(c, s)) for c, s in on]
+        for y, s in zip(got, sets):
+            want, far = ref.gemm(x, ref.matrix(*s, 128), None, BF16)
+            assert ((y.cpu().double() - want).abs() <= far).all()
+
+
+# -------------------------------------------------------------------------------------------------------------------- experts
+
+def moe_case(rng, T, E, H, I, gu, gd, dtype, zu, zd):
+    gate, up = (weights(rng, I, H, gu, dtype, zu, (E,)) for _ in range(2))
+    return normal(rng, (T, H), dtype), normal(rng, (E, H), dtype) / np.sqrt(H), gate, up, weights(rng, H, I, gd, dtype, zd, (E,))
+
+
+def check_moe(x, router, gate, up, down, gu, gd, top_k, renormalise, xd=None):
+    dtype = x.dtype
+    want, far, experts, share = ref.moe(x, router, ref.matrix(*gate, gu), ref.matrix(*up, gu), ref.matrix(*down, gd), top_k, renormalise, dtype)
+    y, e, s = api.moe_w4(x.cuda() if xd is None else xd, router.cuda(), prepared(gate, gu), prepared(up, gu), prepared(down, gd), top_k, renormalise=renormalise)
+    assert torch.equal(e.cpu().long(), experts)
+    assert ((s.cpu().double() - share).abs() <= share * 2.0 ** -19).all()
+    assert ((y.cpu().double() - want).abs() <= far).all(), ((y.cpu().double() - want).abs() / far).max()
+    return y
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("T,E,top_k,H,I,gu,gd,zu,zd,renormalise", [
+    (1, 1, 1, 1, 1, 32, 32, False, False, True), (1, 4, 2, 128, 64, 128, 64, False, True, True), (3, 8, 8, 200, 48, 64, 32, True, False, False),
+    (8, 16, 2, 256, 136, 128, 128, False, False, True), (9, 5, 3, 131, 77, 32, 32, True, True, False), (17, 33, 4, 264, 130, 64, 128, False, True, True),
+    (37, 60, 4, 203, 141, 32, 64, True, True, False), (64, 128, 8, 160, 96, 128, 32, False, False, True), (65, 3, 2, 130, 150, 128, 128, True, False, True),
+    (150, 2, 1, 96, 40, 32, 32, False, True, False), (20, 512, 32, 64, 33, 64, 32, True, True, True)])
+def test_moe(dtype, T, E, top_k, H, I, gu, gd, zu, zd, renormalise):
+    rng = np.random.default_rng(T * E + H)
+    check_moe(*moe_case(rng, T, E, H, I, gu, gd, dtype, zu, zd), gu, gd, top_k, renormalise)
+
+
+def test_moe_larger_reductions():
+    rng = np.random.default_rng(3)
+    check_moe(*moe_case(rng, 5, 6, 2304, 1160, 128, 128, BF16, False, False), 128, 128, 2, True)
+
+
+@pytest.mark.parametrize("pitch", [72, 75])
+def test_moe_rows_apart(pitch):
+    rng = np.random.default_rng(pitch)
+    case = moe_case(rng, 11, 6, 70, 50, 32, 32, BF16, True, False)
+    wide = torch.full((11, pitch), float("nan"), dtype=BF16)
+    wide[:, :70] = case[0]
+    check_moe(*case, 32, 32, 3, True, xd=wide.cuda()[:, :70])
+
+
+def test_moe_ties_and_equal_experts():
+    """Equal logits: the lowest index first; all tokens to the same experts."""
+    rng = np.random.default_rng(4)
+    x, router, gate, up, down = moe_case(rng, 40, 9, 96, 64, 32, 32, F16, False, False)
+    router[:] = router[0]
+    check_moe(x, router, gate, up, down, 32, 32, 3, True)
+    check_moe(torch.zeros_like(x), router, gate, up, down, 32, 32, 3, False)
+
+
+def test_moe_special_values_stay_with_their_token():
+    rng = np.random.default_rng(6)
+    x, router, gate, up, down = moe_case(rng, 12, 6, 96, 64, 32, 32, BF16, False, False)
+    w = [prepared(p, 32) for p in (gate, up, down)]
+    good, _, _ = api.moe_w4(x.cuda(), router.cuda(), *w, 2)
+    bad = x.clone()
+    bad[3, 5], bad[7, 0] = float("nan"), float("inf")
+    y, e, _ = api.moe_w4(bad.cuda(), router.cuda(), *w, 2)
+    keep = [t for t in range(12) if t not in (3, 7)]
+    assert torch.equal(y[keep], good[keep]) and not torch.isfinite(y[3]).any() and not torch.isfinite(y[7]).any()
+    assert ((e >= 0) & (e < 6)).all() and (e[:, 0] != e[:, 1]).all()
+
+
+def test_moe_hidden_values_beyond_fp16():
+    """Hidden values far above what float16 holds, brought back by the last product."""
+    rng = np.random.default_rng(7)
+    x, router, gate, up, down = moe_case(rng, 3, 4, 128, 64, 128, 64, F16, False, False)
+    gate[1].mul_(200), up[1].mul_(200), down[1].copy_(torch.full_like(down[1], 2.0 ** -14))
+    y = check_moe(x, router, gate, up, down, 128, 64, 2, True)
+    assert torch.isfinite(y).all()
+
+
+def test_moe_same_bits_captured_and_on_streams():
+    rng = np.random.default_rng(9)
+    x, router, gate, up, down = moe_case(rng, 33, 16, 131, 90, 32, 32, BF16, True, True)
+    w = [prepared(p, 32) for p in (gate, up, down)]
+    xs = [x.cuda(), normal(rng, x.shape, BF16).cuda()]
+    r = router.cuda()
+    want = [[t.clone() for t in api.moe_w4(v, r, *w, 4)] for v in xs]
+    graphs, outs = [], []
+    for v in xs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(api.moe_w4(v, r, *w, 4))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in xs]
+    for _ in range(5):
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        sided = [api.moe_w4(v, r, *w, 4, stream=s) for v, s in zip(xs, streams)]
+        torch.cuda.synchronize()
+        for got in (outs, sided):
+            assert all(torch.equal(a, b) for o, q in zip(got, want) for a, b in zip(o, q))
+    assert api.moe_w4(xs[0][:0], r, *w, 4)[0].shape == (0, 131)
+
+
+# ---------------------------------------------------------------------------------------------------------------- run together
+
+def test_layers_of_a_decoder_step():
+    """As a program uses them: float weights quantised, prepared, a projection, experts on its outputs, a last projection."""
+    rng = np.random.default_rng(11)
+    H, I, E, T = 192, 128, 4, 3
+    plain = {n: normal(rng, s, F32) / np.sqrt(s[-1]) for n, s in dict(a=(H, H), gate=(E, I, H), up=(E, I, H), down=(E, H, I), b=(50, H)).items()}
+    q = {n: api.quantise_w4(w.cuda(), 64, zeros=n in ("a", "down")) for n, w in plain.items()}
+    w = {n: api.prepare_w4(*v, group=64) for n, v in q.items()}
+    m = {n: ref.matrix(*[None if t is None else t.cpu() for t in v], 64) for n, v in q.items()}
+    x, router = normal(rng, (T, H), BF16), normal(rng, (E, H), BF16)
+    h = api.gemm_w4(x.cuda(), w["a"])
+    want, far = ref.gemm(x, m["a"], None, BF16)
+    assert ((h.cpu().double() - want).abs() <= far).all()
+    y, experts, _ = api.moe_w4(h, router.cuda(), w["gate"], w["up"], w["down"], 2)
+    want, far, e, _ = ref.moe(h.cpu(), router, m["gate"], m["up"], m["down"], 2, True, BF16)
+    assert torch.equal(experts.cpu().long(), e) and ((y.cpu().double() - want).abs() <= far).all()
+    z = api.gemm_w4(y, w["b"])
+    want, far = ref.gemm(y.cpu(), m["b"], None, BF16)
+    assert ((z.cpu().double() - want).abs() <= far).all()
+
+
+def test_refusals_on_the_device():
+    rng = np.random.default_rng(2)
+    w = prepared(weights(rng, 32, 64, 32, BF16, False), 32)
+    x = normal(rng, (4, 64), BF16).cuda()
+    for bad in (x.half(), x.float(), x[:, :63], x.cpu(), x.t().contiguous().t()):
+        with pytest.raises(ValueError):
+            api.gemm_w4(bad, w)
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w, bias=torch.zeros(31, dtype=BF16, device="cuda"))
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w, out=torch.empty(4, 33, dtype=BF16, device="cuda"))
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w._replace(O=64))
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w, out=x[:, :32])
+    with pytest.raises(BitserialError):
+        api.gemm_w4(torch.zeros(4 * 64 + 1, dtype=BF16, device="cuda")[1:].view(4, 64), w)      # off a 16-byte boundary
+    with pytest.raises(BitserialError):
+        api.quantise_w4(x, 48)
+    with pytest.raises(ValueError):
+        api.prepare_w4(torch.zeros(4, 64, dtype=torch.int8, device="cuda"), torch.zeros(4, 3, dtype=BF16, device="cuda"), group=32)
+    e = prepared(weights(rng, 32, 64, 32, BF16, False, (2,)), 32)
+    d = prepared(weights(rng, 64, 32, 32, BF16, False, (2,)), 32)
+    router = normal(rng, (2, 64), BF16).cuda()
+    with pytest.raises(ValueError):
+        api.moe_w4(x, router, e, e, d, 3)
+    with pytest.raises(ValueError):
+        api.moe_w4(x, router, e, e, e, 1)
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, e)
+    api.moe_w4(x, router, e, e, d, 2)
+    api.bs_check_status()
