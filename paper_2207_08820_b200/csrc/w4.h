@@ -20,6 +20,7 @@ constexpr int W4_MAX_DIM = 1 << 20;     // rows, columns and columns of a group
 struct W4Layout {
     int O, K, group, zeros;     // zeros: the matrix has zero points
     int rbs, cbs, G;            // blocks of rows, blocks of columns, groups of a row
+    unsigned per_group;         // multiplier that divides a block's number by the blocks of a group, 0 where that is one
     __host__ __device__ size_t codes_bytes() const { return static_cast<size_t>(rbs) * cbs * W4_BLOCK; }
     __host__ __device__ size_t bytes() const { return codes_bytes() + static_cast<size_t>(rbs) * G * (zeros ? 64 : 32); }
 };
@@ -31,6 +32,9 @@ inline bool w4_layout(int O, int K, int group, int zeros, W4Layout& l)
 {
     if (O <= 0 || K <= 0 || O > W4_MAX_DIM || K > W4_MAX_DIM || !w4_group_ok(group)) return false;
     l.O = O; l.K = K; l.group = group; l.zeros = zeros != 0;
+    // ceil(2^32 / n) divides c exactly as long as c n < 2^32: both are at most 2^13
+    const unsigned n = group > W4_COLS ? group / W4_COLS : 1;
+    l.per_group = n == 1 ? 0 : static_cast<unsigned>(((1ull << 32) + n - 1) / n);
     l.rbs = ceil_div(O, W4_ROWS); l.cbs = ceil_div(K, W4_COLS); l.G = ceil_div(K, group);
     return true;
 }

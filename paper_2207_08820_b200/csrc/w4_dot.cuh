@@ -51,94 +51,98 @@ template <> struct W4Type<true> {
     }
 };
 
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
-
-// A block on its way through shared memory: a warp copies ahead into a ring of stages of its own and waits for nobody else.  A lane copies the codes of its
-// two rows, 16 bytes each, and of the (up to four) groups in the block one entry.
-template <int NG, bool ZEROS>
-struct W4Stage {
-    static constexpr int ENTRY = ZEROS ? 8 : 4, BYTES = W4_BLOCK + NG * 8 * ENTRY;
-
-    static __device__ __forceinline__ void copy(uint32_t dst, const unsigned char* matrix, const W4Layout& l, int rb, int cb, int lane)
-    {
-        const int r = lane >> 2, t = lane & 3;
-        const unsigned char* p = matrix + (static_cast<size_t>(rb) * l.cbs + cb) * W4_BLOCK + t * 256 + r * 16;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + lane * 16), "l"(p) : "memory");
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + 512 + lane * 16), "l"(p + 128) : "memory");
-        const int g = NG > 1 ? cb * NG + t : cb * 128 / l.group;
-        if (t < NG && g < l.G) {
-            const unsigned char* e = matrix + l.codes_bytes() + ((static_cast<size_t>(rb) * l.G + g) * 8 + r) * ENTRY;
-            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst + W4_BLOCK + (t * 8 + r) * ENTRY), "l"(e), "n"(ENTRY) : "memory");
-        }
-    }
-};
-__device__ __forceinline__ void ring_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void ring_wait()      // all but the youngest N groups have landed, for every lane of the warp
+// Read-only loads may move above the wait for the kernel before unless their address comes from behind it: pointers go through this there.
+template <typename T>
+__device__ __forceinline__ const T* behind_wait(const void* p)
 {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-    __syncwarp();
+    asm volatile("" : "+l"(p) : : "memory");
+    return static_cast<const T*>(p);
 }
 
-// What a lane needs of one block: the codes of its two rows, and the scales and zero points of the groups in it.  Groups behind the last one multiply
-// zeros of x only; their entries are what the ring held before, so their scales are cleared.
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int j) { return j == 0 ? v.x : j == 1 ? v.y : j == 2 ? v.z : v.w; }
+
+// What a lane needs of one block: the codes of its two rows, and the scales and zero points of the (up to four) groups in it.
 template <int NG, bool ZEROS>
 struct W4Tile {
     uint4 a, b;
     uint32_t scale[NG], zero[NG];
+};
 
-    __device__ __forceinline__ void take(uint32_t src, const W4Layout& l, int cb, int lane)
+// Where a lane finds the blocks of 16 rows.  Weights go straight to registers, a few blocks ahead of their use, and past L1, which x needs.
+template <int NG, bool ZEROS>
+struct W4Rows {
+    static constexpr int ENTRY = ZEROS ? 8 : 4;
+    const unsigned char *codes, *steps;
+
+    __device__ __forceinline__ W4Rows() {}
+    __device__ __forceinline__ W4Rows(const unsigned char* matrix, const W4Layout& l, int rb, int lane)
     {
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w) : "r"(src + lane * 16) : "memory");
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "r"(src + 512 + lane * 16) : "memory");
+        codes = matrix + static_cast<size_t>(rb) * l.cbs * W4_BLOCK + (lane & 3) * 256 + (lane >> 2) * 16;
+        steps = matrix + l.codes_bytes() + (static_cast<size_t>(rb) * l.G * 8 + (lane >> 2)) * ENTRY;
+    }
+    __device__ __forceinline__ void load(W4Tile<NG, ZEROS>& w, const W4Layout& l, int cb) const
+    {
+        const unsigned char* p = codes + static_cast<unsigned>(cb) * W4_BLOCK;
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.a.x), "=r"(w.a.y), "=r"(w.a.z), "=r"(w.a.w) : "l"(p));
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.b.x), "=r"(w.b.y), "=r"(w.b.z), "=r"(w.b.w) : "l"(p + 128));
+        const int g0 = NG > 1 ? cb * NG : l.per_group == 0 ? cb : static_cast<int>(__umulhi(cb, l.per_group));
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const uint32_t at = src + W4_BLOCK + (g * 8 + (lane >> 2)) * W4Stage<NG, ZEROS>::ENTRY;
-            if (ZEROS) {
-                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(scale[g]), "=r"(zero[g]) : "r"(at) : "memory");
-                zero[g] &= 0x000f000fu;     // what is left of an earlier block in an entry that has none stays a code
-            } else {
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(scale[g]) : "r"(at) : "memory");
-            }
-            if (NG > 1 && g > 0 && cb * NG + g >= l.G) scale[g] = 0;
+            // groups behind the last one multiply zeros of x: their scale is one too
+            const bool live = NG == 1 || g == 0 || g0 + g < l.G;
+            const unsigned char* e = steps + static_cast<unsigned>(live ? g0 + g : g0) * (8 * ENTRY);
+            if (ZEROS) asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.scale[g]), "=r"(w.zero[g]) : "l"(e));
+            else asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w.scale[g]) : "l"(e));
+            if (!live) w.scale[g] = 0;
         }
     }
 };
 
-// tot[n] += the block times x[n], n tiles of eight rows of x; x[n][j]: the lane's eight columns of word j.  x is of the type that X16 says, the scales
-// of S16's.
-template <bool X16, bool S16, int NG, bool ZEROS, int NT>
-__device__ __forceinline__ void w4_block(const W4Tile<NG, ZEROS>& w, const uint4 (&x)[NT][4], float (&tot)[NT][4])
+// tot[r][n] += RT blocks of different rows times n tiles of eight rows of x: x(n, j, term) are the lane's eight columns of word j, of which there are TERMS
+// to be added up.  x is of the type that X16 says, the scales of S16's.
+template <bool X16, bool S16, int TERMS, int RT, int NT, int NG, bool ZEROS, typename X>
+__device__ __forceinline__ void w4_blocks(const W4Tile<NG, ZEROS> (&w)[RT], const X& x, float (&tot)[RT][NT][4])
 {
     typedef W4Type<X16> Ty;
-    float acc[NT][4];
+    float acc[RT][NT][4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int g = j * NG / 4;
-        uint32_t z0 = Ty::BASE + 0x00080008u, z1 = z0;
-        if (ZEROS) {
-            z0 = Ty::BASE + __byte_perm(w.zero[g], 0, 0x1010);
-            z1 = Ty::BASE + __byte_perm(w.zero[g], 0, 0x3232);
-        }
-        if (j % (4 / NG) == 0) {
+        uint4 v[TERMS][NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
-        }
-        const uint32_t a = word_of(w.a, j), b = word_of(w.b, j);
-        const uint32_t a0 = Ty::centre(a, z0), a1 = Ty::centre(a >> 4, z0), a2 = Ty::centre(a >> 8, z0), a3 = Ty::centre(a >> 12, z0);
-        const uint32_t b0 = Ty::centre(b, z1), b1 = Ty::centre(b >> 4, z1), b2 = Ty::centre(b >> 8, z1), b3 = Ty::centre(b >> 12, z1);
+        for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            Ty::mma(acc[n], a0, b0, a1, b1, x[n][j].x, x[n][j].y);
-            Ty::mma(acc[n], a2, b2, a3, b3, x[n][j].z, x[n][j].w);
-        }
-        if ((j + 1) % (4 / NG) == 0) {      // the group's sums are scaled in 32 bits
-            const float s0 = W4Type<S16>::lo(w.scale[g]), s1 = W4Type<S16>::hi(w.scale[g]);
+            for (int n = 0; n < NT; ++n) v[t][n] = x(n, j, t);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                tot[n][0] = fmaf(acc[n][0], s0, tot[n][0]);
-                tot[n][1] = fmaf(acc[n][1], s0, tot[n][1]);
-                tot[n][2] = fmaf(acc[n][2], s1, tot[n][2]);
-                tot[n][3] = fmaf(acc[n][3], s1, tot[n][3]);
+        for (int r = 0; r < RT; ++r) {
+            uint32_t z0 = Ty::BASE + 0x00080008u, z1 = z0;
+            if (ZEROS) {
+                z0 = Ty::BASE + __byte_perm(w[r].zero[g], 0, 0x1010);
+                z1 = Ty::BASE + __byte_perm(w[r].zero[g], 0, 0x3232);
+            }
+            if (j % (4 / NG) == 0) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[r][n][0] = acc[r][n][1] = acc[r][n][2] = acc[r][n][3] = 0.f;
+            }
+            const uint32_t a = word_of(w[r].a, j), b = word_of(w[r].b, j);
+            const uint32_t a0 = Ty::centre(a, z0), a1 = Ty::centre(a >> 4, z0), a2 = Ty::centre(a >> 8, z0), a3 = Ty::centre(a >> 12, z0);
+            const uint32_t b0 = Ty::centre(b, z1), b1 = Ty::centre(b >> 4, z1), b2 = Ty::centre(b >> 8, z1), b3 = Ty::centre(b >> 12, z1);
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    Ty::mma(acc[r][n], a0, b0, a1, b1, v[t][n].x, v[t][n].y);
+                    Ty::mma(acc[r][n], a2, b2, a3, b3, v[t][n].z, v[t][n].w);
+                }
+            if ((j + 1) % (4 / NG) == 0) {      // the group's sums are scaled in 32 bits
+                const float s0 = W4Type<S16>::lo(w[r].scale[g]), s1 = W4Type<S16>::hi(w[r].scale[g]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    tot[r][n][0] = fmaf(acc[r][n][0], s0, tot[r][n][0]);
+                    tot[r][n][1] = fmaf(acc[r][n][1], s0, tot[r][n][1]);
+                    tot[r][n][2] = fmaf(acc[r][n][2], s1, tot[r][n][2]);
+                    tot[r][n][3] = fmaf(acc[r][n][3], s1, tot[r][n][3]);
+                }
             }
         }
     }
@@ -153,6 +157,20 @@ __device__ __forceinline__ uint4 load_x(const T* row, int k0, int K)
 #pragma unroll
     for (int i = 0; i < 8; ++i) e[i] = k0 + i < K ? __ldg(reinterpret_cast<const uint16_t*>(row) + k0 + i) : 0;
     return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+}
+
+// The lane's columns of block cb of a row: v[j] for word j.  `full`: the whole block lies before K.
+template <typename T>
+__device__ __forceinline__ void load_block_x(uint4 (&v)[4], const T* row, int cb, int K, bool full, int lane)
+{
+    const int k0 = cb * W4_COLS + 8 * (lane & 3);
+    if (full) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __ldg(reinterpret_cast<const uint4*>(row + k0 + 32 * j));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = load_x(row, k0 + 32 * j, K);
+    }
 }
 
 }  // namespace bs

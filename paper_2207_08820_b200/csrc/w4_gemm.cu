@@ -3,85 +3,78 @@
 // Few rows of x: bound by the weights' bytes.  w4_gemm_kernel streams them through shared memory, every warp a part of the reduction of 16 rows, and
 // multiplies with mma.sync (w4_dot.cuh), where eight rows of x cost what one does; products are exact, sums of a group in 32 bits, scaled in
 // 32 bits, and rounded once.
+#include <cstdlib>
+
 #include "w4_dot.cuh"
 
 namespace bs {
 namespace {
 
-constexpr int WARPS = 8, STAGES = 6;
+constexpr int MOST_WARPS = 8;
 
-// An item is 16 rows of the weights and 8 NT rows of x.  `split` warps of a CTA share an item's reduction, block by block in turn; a CTA works on
-// WARPS / split items at a time and goes on to others, whose blocks are on their way while the sums of the current ones are put together.
-template <bool F16, int NG, bool ZEROS, int NT>
-__global__ void __launch_bounds__(WARPS * 32, 2) w4_gemm_kernel(const __grid_constant__ W4Gemm g, int split)
+// A CTA owns 16 RT rows of the weights and 8 NT rows of x; its warps take the blocks of the reduction in turn.
+template <bool F16, int NG, bool ZEROS, int NT, int RT>
+__global__ void __launch_bounds__(MOST_WARPS * 32, NT * RT == 1 ? 3 : 2) w4_gemm_kernel(const __grid_constant__ W4Gemm g)
 {
     typedef typename W4Type<F16>::T T;
-    typedef W4Stage<NG, ZEROS> Stage;
-    extern __shared__ __align__(16) unsigned char ring[];      // [WARPS][STAGES] stages
-    __shared__ float part[WARPS][NT * 8][17];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m0 = blockIdx.y * NT * 8;
-    const int side = WARPS / split, sub = warp / split, k0 = warp % split;
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * STAGES * Stage::BYTES;
-    const unsigned char* w = dependent_begin(g.w);
-    // the blocks that this warp copies, STAGES - 1 ahead of the ones it multiplies
-    int crb = blockIdx.x * side + sub, ccb = k0, cslot = 0;
-    const bool some = k0 < g.l.cbs;
-    auto copy = [&] {
-        if (some && crb < g.l.rbs) {
-            Stage::copy(mine + cslot * Stage::BYTES, w, g.l, crb, ccb, lane);
-            ccb += split;
-            if (ccb >= g.l.cbs) { ccb = k0; crb += gridDim.x * side; }
-        }
-        ring_commit();
-        cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
-    };
-#pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) copy();
-    int slot = 0;
-    for (int first = blockIdx.x * side; first < g.l.rbs; first += gridDim.x * side) {
-        const int rb = first + sub;
-        float tot[NT][4];
+    constexpr int STAGES = (NT * RT == 1 ? 4 : NT * RT == 2 ? 3 : 2) - (NG == 4 && NT * RT < 4 ? 1 : 0), M = NT * 8, R = RT * W4_ROWS, PITCH = R + 1;
+    extern __shared__ float part[];         // [warps][M][PITCH]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, rb0 = blockIdx.x * RT, m0 = blockIdx.y * M;
+    const unsigned char* matrix = dependent_begin(g.w);
+    const T* x0 = behind_wait<T>(g.x);
+    W4Rows<NG, ZEROS> rows[RT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) tot[n][0] = tot[n][1] = tot[n][2] = tot[n][3] = 0.f;
-        if (rb < g.l.rbs) {
-            for (int cb = k0; cb < g.l.cbs; cb += split) {
+    for (int r = 0; r < RT; ++r) rows[r] = W4Rows<NG, ZEROS>(matrix, g.l, min(rb0 + r, g.l.rbs - 1), lane);
+    W4Tile<NG, ZEROS> w[STAGES][RT];
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+        if (warp + s * warps < g.l.cbs) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) rows[r].load(w[s][r], g.l, warp + s * warps);
+        }
+    const T* row[NT];       // lanes without a row of x compute the last one's again
+#pragma unroll
+    for (int n = 0; n < NT; ++n) row[n] = x0 + min(m0 + n * 8 + (lane >> 2), g.M - 1) * g.ldx;
+    float tot[RT][NT][4];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) tot[r][n][0] = tot[r][n][1] = tot[r][n][2] = tot[r][n][3] = 0.f;
+    const int full = g.l.K / W4_COLS;
+    for (int cb = warp; cb < g.l.cbs; cb += STAGES * warps) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) {
+            const int c = cb + s * warps;
+            if (c < g.l.cbs) {
                 uint4 x[NT][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const int m = m0 + n * 8 + (lane >> 2);
-                    const T* row = static_cast<const T*>(g.x) + m * g.ldx;
+                for (int n = 0; n < NT; ++n) load_block_x(x[n], row[n], c, g.l.K, c < full, lane);
+                w4_blocks<F16, F16, 1>(w[s], [&](int n, int j, int) { return x[n][j]; }, tot);
+                if (c + STAGES * warps < g.l.cbs) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[n][j] = m < g.M ? load_x(row, cb * 128 + 32 * j + 8 * (lane & 3), g.l.K) : make_uint4(0, 0, 0, 0);
+                    for (int r = 0; r < RT; ++r) rows[r].load(w[s][r], g.l, c + STAGES * warps);
                 }
-                ring_wait<STAGES - 2>();
-                W4Tile<NG, ZEROS> tile;
-                tile.take(mine + slot * Stage::BYTES, g.l, cb, lane);
-                slot = slot + 1 == STAGES ? 0 : slot + 1;
-                copy();     // into the stage before this one, which every lane has read: the warp met in ring_wait since
-                w4_block<F16, F16, NG, ZEROS, NT>(tile, x, tot);
             }
         }
+    }
+    float* mine = part + warp * M * PITCH;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int m = n * 8 + 2 * (lane & 3), r = lane >> 2;
-            part[warp][m][r] = tot[n][0];
-            part[warp][m + 1][r] = tot[n][1];
-            part[warp][m][r + 8] = tot[n][2];
-            part[warp][m + 1][r + 8] = tot[n][3];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[(n * 8 + 2 * (lane & 3) + (i & 1)) * PITCH + r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)] = tot[r][n][i];
         }
-        __syncthreads();
-        // the warps' parts are added in their order: the same bits every time
-        for (int i = threadIdx.x; i < side * NT * 8 * 16; i += WARPS * 32) {
-            const int q = i / (NT * 8 * 16), m = (i >> 4) % (NT * 8), r = i & 15, o = (first + q) * 16 + r;
-            if (m0 + m >= g.M || o >= g.l.O) continue;
-            float v = 0.f;
-            for (int k = 0; k < split; ++k) v += part[q * split + k][m][r];
-            if (g.bias) v += static_cast<float>(static_cast<const T*>(g.bias)[o]);
-            static_cast<T*>(g.y)[(m0 + m) * g.ldy + o] = W4Type<F16>::round(v);
-        }
-        __syncthreads();
+    __syncthreads();
+    // the warps' parts are added in their order: the same bits every time
+    for (int i = threadIdx.x; i < M * R; i += blockDim.x) {
+        const int m = i / R, r = i % R, o = rb0 * W4_ROWS + r;
+        if (m0 + m >= g.M || o >= g.l.O) continue;
+        float v = 0.f;
+        for (int k = 0; k < warps; ++k) v += part[(k * M + m) * PITCH + r];
+        if (g.bias) v += static_cast<float>(static_cast<const T*>(g.bias)[o]);
+        static_cast<T*>(g.y)[(m0 + m) * g.ldy + o] = W4Type<F16>::round(v);
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Rows of x that do not start on 16-byte boundaries, brought to ones that do, zeros behind K.
@@ -99,23 +92,33 @@ __global__ void __launch_bounds__(256) w4_align_rows_kernel(const uint16_t* x, l
     }
 }
 
-template <bool F16, int NG, bool ZEROS, int NT>
+template <bool F16, int NG, bool ZEROS, int NT, int RT>
 int launch_tile(const W4Gemm& g, int sms, cudaStream_t st)
 {
-    auto kernel = w4_gemm_kernel<F16, NG, ZEROS, NT>;
-    const size_t smem = WARPS * STAGES * W4Stage<NG, ZEROS>::BYTES;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    int split = WARPS;
-    while (split > 1 && split / 2 >= g.l.cbs) split /= 2;
-    const int ctas = ceil_div(g.l.rbs, WARPS / split);
-    return launch_dependent(kernel, dim3(ctas < 2 * sms ? ctas : 2 * sms, ceil_div(g.M, 8 * NT)), dim3(WARPS * 32), smem, st, g, split);
+    const int items = ceil_div(g.l.rbs, RT);
+    // enough warps for 16 an SM, each with two blocks of the reduction at least
+    int warps = MOST_WARPS;
+    while (warps > 1 && (2 * warps > g.l.cbs + 1 || static_cast<long long>(items) * warps / 2 >= 16ll * sms)) warps /= 2;
+#ifdef BS_TUNING
+    if (const char* e = getenv("BS_W4_WARPS")) warps = atoi(e);
+#endif
+    return launch_dependent(w4_gemm_kernel<F16, NG, ZEROS, NT, RT>, dim3(items, ceil_div(g.M, 8 * NT)), dim3(warps * 32),
+                            sizeof(float) * warps * NT * 8 * (RT * W4_ROWS + 1), st, g);
 }
 template <bool F16, int NG, bool ZEROS>
 int launch_rows(const W4Gemm& g, int sms, cudaStream_t st)
 {
-    if (g.M <= 8) return launch_tile<F16, NG, ZEROS, 1>(g, sms, st);
-    if (g.M <= 16) return launch_tile<F16, NG, ZEROS, 2>(g, sms, st);
-    return launch_tile<F16, NG, ZEROS, 4>(g, sms, st);
+#ifdef BS_TUNING
+    if (const char* e = getenv("BS_W4_RT")) {
+        const int rt = atoi(e);
+        if (g.M <= 8) return rt == 1 ? launch_tile<F16, NG, ZEROS, 1, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 1, 2>(g, sms, st);
+        if (g.M <= 16) return rt == 1 ? launch_tile<F16, NG, ZEROS, 2, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2, 2>(g, sms, st);
+        return rt == 1 ? launch_tile<F16, NG, ZEROS, 4, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 4, 2>(g, sms, st);
+    }
+#endif
+    if (g.M <= 8) return launch_tile<F16, NG, ZEROS, 1, 1>(g, sms, st);
+    if (g.M <= 16) return launch_tile<F16, NG, ZEROS, 2, 1>(g, sms, st);
+    return launch_tile<F16, NG, ZEROS, 4, 1>(g, sms, st);
 }
 template <bool F16>
 int launch(const W4Gemm& g, int sms, cudaStream_t st)

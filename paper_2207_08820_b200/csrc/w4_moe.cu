@@ -2,8 +2,8 @@
 //   route   logits = x R^T, the top_k experts of every token, their softmax weights
 //   gate    h[slot] = weight * silu(Gate_e x) * (Up_e x) for every slot (token, choice)
 //   down    y[token] = sum over its slots of Down_e h[slot]
-// Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), through
-// shared memory, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
+// Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), straight
+// into registers, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
 // of mantissa), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
 #include "w4_dot.cuh"
 
@@ -13,7 +13,7 @@ namespace {
 constexpr int PASS = 64;                    // tokens of a pass
 constexpr int MAX_EXPERTS = 512, MAX_TOP = 32;
 constexpr int ROUTE_CTAS = 8, ROUTE_WARPS = 16;     // CTAs of a cluster, a token each in the end; warps split the reduction
-constexpr int WARPS = 8, GATE_STAGES = 4, DOWN_STAGES = 6;
+constexpr int WARPS = 8;
 
 struct MoeArgs {
     const void *x, *router;
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     __shared__ unsigned long long keys[MAX_EXPERTS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x, m0 = blockIdx.y * 8;
     const T* x = static_cast<const T*>(dependent_begin(g.x));
-    const T* router = static_cast<const T*>(g.router);
+    const T* router = behind_wait<T>(g.router);
     const int tiles = (g.E + 15) / 16, steps = (g.H + 31) / 32;
     const int mx = m0 + (lane >> 2);
     // every CTA of the cluster runs before one writes to another's shared memory
@@ -140,233 +140,272 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     }
 }
 
-// The chosen experts of a pass of 64 tokens and their slots, made by every CTA for itself (at most 2048 slots).
-struct Chosen {
-    int count[MAX_EXPERTS];             // slots of an expert, then where its next one goes
-    int active[MAX_EXPERTS];            // experts that have slots, ascending
-    int first[MAX_EXPERTS + 1];         // where the slots of active expert i begin
+// The work of a pass of 64 tokens: jobs of an expert and up to J of its slots, made by every CTA for itself (at most 2048 slots).
+constexpr int MOST_JOBS = MAX_EXPERTS + PASS * MAX_TOP / 8;
+struct Jobs {
+    unsigned tokens[2][MAX_EXPERTS];    // which tokens chose an expert, a bit each
+    uint16_t begin[MAX_EXPERTS];        // where an expert's slots begin
+    uint16_t expert[MOST_JOBS];
+    uint16_t first[MOST_JOBS + 1];      // where the slots of a job begin
+    uint16_t slot[PASS * MAX_TOP];      // slot - first slot of the pass; by expert, then by token, in every CTA alike
+    uint8_t token[PASS * MAX_TOP];      // its token - first token of the pass
     int n;
-    uint16_t slot[PASS * MAX_TOP];      // slot - first slot of the pass
 };
 
-__device__ __forceinline__ void find_chosen(const MoeArgs& g, Chosen& c, int t0, int threads)
+template <int J>
+__device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int threads)
 {
     const int slots = (g.T - t0 < PASS ? g.T - t0 : PASS) * g.top_k;
     const int* experts = g.experts + static_cast<size_t>(t0) * g.top_k;
-    for (int e = threadIdx.x; e < g.E; e += threads) c.count[e] = 0;
+    for (int e = threadIdx.x; e < g.E; e += threads) c.tokens[0][e] = c.tokens[1][e] = 0;
     __syncthreads();
-    for (int s = threadIdx.x; s < slots; s += threads) atomicAdd(&c.count[experts[s]], 1);
+    for (int s = threadIdx.x; s < slots; s += threads) {
+        const int t = s / g.top_k;
+        atomicOr(&c.tokens[t >> 5][experts[s]], 1u << (t & 31));
+    }
     __syncthreads();
     if (threadIdx.x < 32) {
-        int n = 0, at = 0;
+        int jobs = 0, at = 0;
         for (int base = 0; base < g.E; base += 32) {
-            const int e = base + threadIdx.x, k = e < g.E ? c.count[e] : 0;
-            const unsigned has = __ballot_sync(0xffffffffu, k > 0);
-            int before = k;             // slots of this and the lower lanes
+            const int e = base + threadIdx.x, k = e < g.E ? __popc(c.tokens[0][e]) + __popc(c.tokens[1][e]) : 0, own = (k + J - 1) / J;
+            int before = own << 16 | k;             // jobs and slots of this and the lower lanes
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
                 const int v = __shfl_up_sync(0xffffffffu, before, d);
                 if (static_cast<int>(threadIdx.x) >= d) before += v;
             }
-            if (k > 0) {
-                const int i = n + __popc(has & ((1u << threadIdx.x) - 1));
-                c.active[i] = e;
-                c.first[i] = c.count[e] = at + before - k;
+            const int j0 = jobs + (before >> 16) - own, s0 = at + (before & 0xffff) - k;
+            if (e < g.E) c.begin[e] = static_cast<uint16_t>(s0);
+            for (int j = 0; j < own; ++j) {
+                c.expert[j0 + j] = static_cast<uint16_t>(e);
+                c.first[j0 + j] = static_cast<uint16_t>(s0 + j * J);
             }
-            n += __popc(has);
-            at += __shfl_sync(0xffffffffu, before, 31);
+            const int all = __shfl_sync(0xffffffffu, before, 31);
+            jobs += all >> 16;
+            at += all & 0xffff;
         }
-        if (threadIdx.x == 0) { c.n = n; c.first[n] = at; }
+        if (threadIdx.x == 0) { c.n = jobs; c.first[jobs] = static_cast<uint16_t>(at); }
     }
     __syncthreads();
-    // the order of an expert's slots is not fixed and does not matter: a slot's results come from its own column
-    for (int s = threadIdx.x; s < slots; s += threads) c.slot[atomicAdd(&c.count[experts[s]], 1)] = static_cast<uint16_t>(s);
+    for (int s = threadIdx.x; s < slots; s += threads) {
+        const int t = s / g.top_k, e = experts[s];
+        const unsigned lower = (1u << (t & 31)) - 1;
+        const int i = c.begin[e] + (t < 32 ? __popc(c.tokens[0][e] & lower) : __popc(c.tokens[0][e]) + __popc(c.tokens[1][e] & lower));
+        c.slot[i] = static_cast<uint16_t>(s);
+        c.token[i] = static_cast<uint8_t>(t);
+    }
     __syncthreads();
 }
 
-// h = weight * silu(gate) * up of 16 rows of an expert for 16 of its slots at a time; the warps take the blocks of the reduction in turn and copy the
-// blocks of the CTA's next items ahead.
-template <bool F16, int NG, bool ZEROS>
-__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g)
+// h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  `split` warps, a team, share the reduction of an item; the first blocks of a
+// team's next item are on their way while it puts the sums of the current one together.
+template <bool F16, int NG, bool ZEROS, int NT>
+__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g, int split)
 {
     typedef typename W4Type<F16>::T T;
-    typedef W4Stage<NG, ZEROS> Stage;
-    constexpr int NT = 2, STAGES = GATE_STAGES;
-    extern __shared__ __align__(16) unsigned char ring[];      // [WARPS][STAGES][gate, up]
-    __shared__ Chosen chosen;
-    __shared__ float part[WARPS][2][NT * 8][17];
+    constexpr int J = NT * 8, STAGES = 2;
+    __shared__ Jobs jobs;
+    __shared__ float part[WARPS][2][J][17];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * STAGES * 2 * Stage::BYTES;
+    const int team = warp / split, k0 = warp % split, teams = WARPS / split;
     const T* x = static_cast<const T*>(dependent_begin(g.xa ? g.xa : g.x));
     const long long ldx = g.xa ? g.ldxa : g.ldx;
-    find_chosen(g, chosen, t0, WARPS * 32);
+    find_jobs<J>(g, jobs, t0, WARPS * 32);
     const W4Layout& l = g.lu;
     const size_t matrix = l.bytes();
-    const int items = chosen.n * l.rbs;
-    auto slots = [&](int item) { const int a = item / l.rbs; return chosen.first[a + 1] - chosen.first[a]; };
-    // an item whose expert has more than 16 slots is gone through several times
-    int citem = blockIdx.x, ccb = warp, cslot = 0, cleft = citem < items ? slots(citem) : 0;
-    auto copy = [&] {
-        if (citem < items && warp < l.cbs) {
-            const int a = citem / l.rbs, rb = citem - a * l.rbs;
-            const size_t at = chosen.active[a] * matrix;
-            Stage::copy(mine + cslot * 2 * Stage::BYTES, g.gate + at, l, rb, ccb, lane);
-            Stage::copy(mine + cslot * 2 * Stage::BYTES + Stage::BYTES, g.up + at, l, rb, ccb, lane);
-            ccb += WARPS;
-            if (ccb >= l.cbs) {
-                ccb = warp;
-                cleft -= NT * 8;
-                if (cleft <= 0) {
-                    citem += gridDim.x;
-                    cleft = citem < items ? slots(citem) : 0;
-                }
+    const int items = jobs.n * l.rbs, full = l.K / W4_COLS;
+    W4Rows<NG, ZEROS> rows[2];
+    W4Tile<NG, ZEROS> w[STAGES][2];
+    auto begin = [&](int item) {
+        const int job = item / l.rbs, rb = item - job * l.rbs;
+        const size_t at = jobs.expert[job] * matrix;
+        rows[0] = W4Rows<NG, ZEROS>(g.gate + at, l, rb, lane);
+        rows[1] = W4Rows<NG, ZEROS>(g.up + at, l, rb, lane);
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s)
+            if (k0 + s * split < l.cbs) {
+                rows[0].load(w[s][0], l, k0 + s * split);
+                rows[1].load(w[s][1], l, k0 + s * split);
             }
-        }
-        ring_commit();
-        cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
     };
-#pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) copy();
-    int stage = 0;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
-        const int a = item / l.rbs, rb = item - a * l.rbs;
-        const int beg = chosen.first[a], n = chosen.first[a + 1] - beg;
-        for (int s0 = 0; s0 < n; s0 += NT * 8) {
-            const T* row[NT];
-            float tg[NT][1][4], tu[NT][1][4];
+    // neighbouring teams work on neighbouring rows: they share the tokens' x in L1
+    const int step = gridDim.x * teams;
+    int item = blockIdx.x * teams + team;
+    if (item < items) begin(item);
+    for (; item < items; item += step) {
+        const int job = item / l.rbs, rb = item - job * l.rbs, beg = jobs.first[job];
+        // a job's slots end where the next one's begin; lanes without a slot compute the last one's again
+        const int n = jobs.first[job + 1] - beg;
+        const T* row[NT];
 #pragma unroll
-            for (int k = 0; k < NT; ++k) {
-                const int s = s0 + k * 8 + (lane >> 2);
-                row[k] = s < n ? x + (t0 + chosen.slot[beg + s] / g.top_k) * ldx : nullptr;
+        for (int k = 0; k < NT; ++k) row[k] = x + (t0 + jobs.token[beg + min(k * 8 + (lane >> 2), n - 1)]) * ldx;
+        float tot[2][NT][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tg[k][0][i] = tu[k][0][i] = 0.f;
-            }
-            const bool wide = s0 + 8 < n;       // more than eight slots left
-            for (int cb = warp; cb < l.cbs; cb += WARPS) {
-                uint4 v[1][4];
+        for (int k = 0; k < NT; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) v[0][j] = row[0] ? load_x(row[0], cb * 128 + 32 * j + 8 * (lane & 3), l.K) : make_uint4(0, 0, 0, 0);
-                ring_wait<STAGES - 2>();
-                W4Tile<NG, ZEROS> gate, up;
-                gate.take(mine + stage * 2 * Stage::BYTES, l, cb, lane);
-                up.take(mine + stage * 2 * Stage::BYTES + Stage::BYTES, l, cb, lane);
-                stage = stage + 1 == STAGES ? 0 : stage + 1;
-                copy();
-                w4_block<F16, F16, NG, ZEROS, 1>(gate, v, tg[0]);
-                w4_block<F16, F16, NG, ZEROS, 1>(up, v, tu[0]);
-                if (wide) {
+            for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
+        for (int cb = k0; cb < l.cbs; cb += STAGES * split) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[0][j] = row[1] ? load_x(row[1], cb * 128 + 32 * j + 8 * (lane & 3), l.K) : make_uint4(0, 0, 0, 0);
-                    w4_block<F16, F16, NG, ZEROS, 1>(gate, v, tg[1]);
-                    w4_block<F16, F16, NG, ZEROS, 1>(up, v, tu[1]);
+            for (int s = 0; s < STAGES; ++s) {
+                const int c = cb + s * split;
+                if (c < l.cbs) {
+                    uint4 v[NT][4];
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
+                    w4_blocks<F16, F16, 1>(w[s], [&](int k, int j, int) { return v[k][j]; }, tot);
+                    if (c + STAGES * split < l.cbs) {
+                        rows[0].load(w[s][0], l, c + STAGES * split);
+                        rows[1].load(w[s][1], l, c + STAGES * split);
+                    }
                 }
             }
-#pragma unroll
-            for (int k = 0; k < NT; ++k) {
-                const int m = k * 8 + 2 * (lane & 3), r = lane >> 2;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    part[warp][0][m + (i & 1)][r + 8 * (i >> 1)] = tg[k][0][i];
-                    part[warp][1][m + (i & 1)][r + 8 * (i >> 1)] = tu[k][0][i];
-                }
-            }
-            __syncthreads();
-            const int m = threadIdx.x >> 4, r = threadIdx.x & 15, i = rb * 16 + r;
-            if (s0 + m < n && i < g.I) {
-                float gate = 0.f, up = 0.f;
-#pragma unroll
-                for (int k = 0; k < WARPS; ++k) {
-                    gate += part[k][0][m][r];
-                    up += part[k][1][m][r];
-                }
-                const size_t slot = static_cast<size_t>(t0) * g.top_k + chosen.slot[beg + s0 + m];
-                const float h = gate / (1.f + expf(-gate)) * up * g.weights[slot];
-                const __nv_bfloat16 hi = __float2bfloat16_rn(h);
-                g.hi[slot * g.ldh + i] = hi;
-                // an infinite or NaN value has no remainder
-                g.lo[slot * g.ldh + i] = isfinite(__bfloat162float(hi)) ? __float2bfloat16_rn(h - __bfloat162float(hi)) : __float2bfloat16_rn(0.f);
-            }
-            __syncthreads();
         }
+        if (item + step < items) begin(item + step);
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int m = k * 8 + 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
+                part[warp][0][m][r] = tot[0][k][i];
+                part[warp][1][m][r] = tot[1][k][i];
+            }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
+        for (int q = k0 * 32 + lane; q < J * 16; q += 32 * split) {
+            const int m = q >> 4, r = q & 15, i = rb * 16 + r;
+            if (m >= n || i >= g.I) continue;
+            float gate = 0.f, up = 0.f;
+            for (int k = 0; k < split; ++k) {
+                gate += part[team * split + k][0][m][r];
+                up += part[team * split + k][1][m][r];
+            }
+            const size_t slot = static_cast<size_t>(t0) * g.top_k + jobs.slot[beg + m];
+            const float h = gate / (1.f + expf(-gate)) * up * g.weights[slot];
+            const __nv_bfloat16 hi = __float2bfloat16_rn(h);
+            g.hi[slot * g.ldh + i] = hi;
+            // an infinite or NaN value has no remainder
+            g.lo[slot * g.ldh + i] = isfinite(__bfloat162float(hi)) ? __float2bfloat16_rn(h - __bfloat162float(hi)) : __float2bfloat16_rn(0.f);
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// y of 16 columns for the tokens of a pass: the warps share the blocks of all chosen experts, one run of them each, and add up per token in
-// shared memory of their own.
-template <bool F16, int NG, bool ZEROS>
-__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g)
+// y of 32 columns for the tokens of a pass: the warps of a cluster's CTAs share the blocks of all jobs, one run of them each, and add up per token in
+// shared memory of their own.  32 columns, because the hidden values of a slot are four times its weights' bytes.
+constexpr int DOWN_RT = 2, DOWN_ROWS = DOWN_RT * W4_ROWS;
+template <bool F16, int NG, bool ZEROS, int NT>
+__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int cluster)
 {
     typedef typename W4Type<F16>::T T;
-    typedef W4Stage<NG, ZEROS> Stage;
-    constexpr int STAGES = DOWN_STAGES;
-    extern __shared__ __align__(16) unsigned char ring[];      // [WARPS][STAGES] stages, then sums [WARPS][16][pitch]
-    __shared__ Chosen chosen;
-    float* sums = reinterpret_cast<float*>(ring + WARPS * STAGES * Stage::BYTES);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS, rb = blockIdx.x;
+    constexpr int J = NT * 8, STAGES = 2, RT = DOWN_RT;
+    extern __shared__ float sums[];         // [WARPS][DOWN_ROWS][pitch]
+    __shared__ Jobs jobs;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS, rb0 = blockIdx.x / cluster * RT, rank = blockIdx.x % cluster;
     const int tokens = g.T - t0 < PASS ? g.T - t0 : PASS, pitch = tokens + 1;
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + warp * STAGES * Stage::BYTES;
     const unsigned char* down = dependent_begin(g.down);
-    find_chosen(g, chosen, t0, WARPS * 32);
+    const __nv_bfloat16* hidden = behind_wait<__nv_bfloat16>(g.hi);
+    find_jobs<J>(g, jobs, t0, WARPS * 32);
     const W4Layout& l = g.ld;
     const size_t matrix = l.bytes();
-    float* own = sums + warp * 16 * pitch;
-    for (int i = lane; i < 16 * pitch; i += 32) own[i] = 0.f;
+    float* own = sums + warp * DOWN_ROWS * pitch;
+    for (int i = lane; i < DOWN_ROWS * pitch; i += 32) own[i] = 0.f;
     __syncwarp();
-    const int blocks = chosen.n * l.cbs, beg = static_cast<int>(static_cast<long long>(blocks) * warp / WARPS),
-              end = static_cast<int>(static_cast<long long>(blocks) * (warp + 1) / WARPS);
-    int cb = beg, ca = beg / l.cbs, cc = beg - ca * l.cbs, cslot = 0;
-    auto copy = [&] {
-        if (cb < end) {
-            Stage::copy(mine + cslot * Stage::BYTES, down + chosen.active[ca] * matrix, l, rb, cc, lane);
-            ++cb;
-            if (++cc == l.cbs) { cc = 0; ++ca; }
-        }
-        ring_commit();
-        cslot = cslot + 1 == STAGES ? 0 : cslot + 1;
+    const int full = l.K / W4_COLS, runs = cluster * WARPS, run = rank * WARPS + warp;
+    const long long blocks = static_cast<long long>(jobs.n) * l.cbs;
+    const int beg = static_cast<int>(blocks * run / runs), end = static_cast<int>(blocks * (run + 1) / runs);
+    W4Rows<NG, ZEROS> rows[RT];
+    W4Tile<NG, ZEROS> w[STAGES][RT];
+    int fjob = beg / l.cbs, fc = beg - fjob * l.cbs;        // the block that is fetched next
+    auto at = [&](int job) {
+        const unsigned char* p = down + jobs.expert[job] * matrix;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) rows[r] = W4Rows<NG, ZEROS>(p, l, min(rb0 + r, l.rbs - 1), lane);
     };
-#pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) copy();
-    int stage = 0, a = beg / l.cbs, c = beg - a * l.cbs;
-    for (int b = beg; b < end; ++b) {
-        const int first = chosen.first[a], n = chosen.first[a + 1] - first;
-        ring_wait<STAGES - 2>();
-        W4Tile<NG, ZEROS> tile;
-        tile.take(mine + stage * Stage::BYTES, l, c, lane);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
-        copy();
-        for (int s0 = 0; s0 < n; s0 += 8) {
-            const int k = s0 + (lane >> 2);
-            const size_t slot = static_cast<size_t>(t0) * g.top_k + (k < n ? chosen.slot[first + k] : 0);
-            float tot[1][4] = {{0, 0, 0, 0}};
-            uint4 hi[1][4], lo[1][4];
+    auto fetch = [&](W4Tile<NG, ZEROS> (&to)[RT]) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k0 = c * 128 + 32 * j + 8 * (lane & 3);
-                hi[0][j] = k < n ? load_x(g.hi + slot * g.ldh, k0, l.K) : make_uint4(0, 0, 0, 0);
-                lo[0][j] = k < n ? load_x(g.lo + slot * g.ldh, k0, l.K) : make_uint4(0, 0, 0, 0);
-            }
-            w4_block<false, F16, NG, ZEROS, 1>(tile, hi, tot);
-            w4_block<false, F16, NG, ZEROS, 1>(tile, lo, tot);
+        for (int r = 0; r < RT; ++r) rows[r].load(to[r], l, fc);
+    };
+    if (beg < end) at(fjob);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {       // lanes own different (row, slot): an expert has a token once
-                const int q = s0 + 2 * (lane & 3) + (i & 1);
-                if (q < n) own[((lane >> 2) + 8 * (i >> 1)) * pitch + chosen.slot[first + q] / g.top_k] += tot[0][i];
+    for (int s = 0; s < STAGES; ++s)
+        if (beg + s < end) {
+            fetch(w[s]);
+            if (++fc == l.cbs) { fc = 0; if (beg + s + 1 < end) at(++fjob); }
+        }
+    int job = beg / l.cbs, c = beg - job * l.cbs, first = 0, n = 0;
+    const __nv_bfloat16* row[NT];
+    const long long lo = g.lo - g.hi;
+    float tot[RT][NT][4];
+    auto begin = [&] {
+        first = jobs.first[job];
+        n = jobs.first[job + 1] - first;
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+            row[k] = hidden + (static_cast<size_t>(t0) * g.top_k + jobs.slot[first + min(k * 8 + (lane >> 2), n - 1)]) * g.ldh;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) tot[r][k][0] = tot[r][k][1] = tot[r][k][2] = tot[r][k][3] = 0.f;
+        }
+    };
+    if (beg < end) begin();
+    for (int b0 = beg; b0 < end; b0 += STAGES) {
+#pragma unroll
+        for (int s = 0; s < STAGES; ++s) {
+            const int b = b0 + s;
+            if (b < end) {
+                if (c < full) {
+                    const int k0 = c * W4_COLS + 8 * (lane & 3);
+                    w4_blocks<false, F16, 2>(w[s], [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + k0 + 32 * j)); }, tot);
+                } else {
+                    const int k0 = c * W4_COLS + 8 * (lane & 3);
+                    w4_blocks<false, F16, 2>(w[s], [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0), k0 + 32 * j, l.K); }, tot);
+                }
+                if (b + STAGES < end) {
+                    fetch(w[s]);
+                    if (++fc == l.cbs) { fc = 0; if (b + STAGES + 1 < end) at(++fjob); }
+                }
+                if (++c == l.cbs || b + 1 == end) {     // the end of the job, or of this warp's part of it
+#pragma unroll
+                    for (int k = 0; k < NT; ++k)
+#pragma unroll
+                        for (int r = 0; r < RT; ++r)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {       // lanes own different (row, slot): an expert has a token once
+                                const int q = k * 8 + 2 * (lane & 3) + (i & 1);
+                                if (q < n) own[(r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)) * pitch + jobs.token[first + q]] += tot[r][k][i];
+                            }
+                    __syncwarp();       // another job's slots meet the same tokens from other lanes
+                    c = 0;
+                    ++job;
+                    if (b + 1 < end) begin();
+                }
             }
         }
-        if (++c == l.cbs) { c = 0; ++a; }
-        __syncwarp();       // another expert's slots meet the same tokens from other lanes
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * tokens; i += WARPS * 32) {
-        const int m = i >> 4, r = i & 15, o = rb * 16 + r;
-        if (o >= g.H) continue;
+    for (int i = threadIdx.x; i < DOWN_ROWS * tokens; i += WARPS * 32) {
+        const int m = i / DOWN_ROWS, r = i % DOWN_ROWS, o = rb0 * W4_ROWS + r;
         float v = 0.f;
 #pragma unroll
-        for (int k = 0; k < WARPS; ++k) v += sums[(k * 16 + r) * pitch + m];
-        static_cast<T*>(g.y)[static_cast<size_t>(t0 + m) * g.H + o] = W4Type<F16>::round(v);
+        for (int k = 0; k < WARPS; ++k) v += sums[(k * DOWN_ROWS + r) * pitch + m];
+        if (cluster > 1) sums[r * pitch + m] = v;
+        else if (o < g.H) static_cast<T*>(g.y)[static_cast<size_t>(t0 + m) * g.H + o] = W4Type<F16>::round(v);
     }
+    if (cluster == 1) return;
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (rank == 0) {
+        for (int i = threadIdx.x; i < DOWN_ROWS * tokens; i += WARPS * 32) {
+            const int m = i / DOWN_ROWS, r = i % DOWN_ROWS, o = rb0 * W4_ROWS + r;
+            float v = sums[r * pitch + m];
+            for (int k = 1; k < cluster; ++k) {
+                uint32_t from = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[r * pitch + m]));
+                float part;
+                asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(from) : "r"(k));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(from) : "memory");
+                v += part;
+            }
+            if (o < g.H) static_cast<T*>(g.y)[static_cast<size_t>(t0 + m) * g.H + o] = W4Type<F16>::round(v);
+        }
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 template <typename K>
@@ -376,49 +415,68 @@ bool allow_smem(K kernel, size_t bytes)
     cudaGetLastError();
     return false;
 }
-template <bool F16, int NG, bool ZEROS>
-int launch_gate(const MoeArgs& g, int sms, cudaStream_t st)
-{
-    const long long slots = static_cast<long long>(g.T < PASS ? g.T : PASS) * g.top_k, items = (slots < g.E ? slots : g.E) * g.lu.rbs;
-    const size_t smem = static_cast<size_t>(WARPS) * GATE_STAGES * 2 * W4Stage<NG, ZEROS>::BYTES;
-    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS>, smem)) return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
-                            dim3(WARPS * 32), smem, st, g);
-}
-template <bool F16, int NG, bool ZEROS>
-int launch_down(const MoeArgs& g, cudaStream_t st)
-{
-    const int tokens = g.T < PASS ? g.T : PASS;
-    const size_t smem = static_cast<size_t>(WARPS) * (DOWN_STAGES * W4Stage<NG, ZEROS>::BYTES + sizeof(float) * 16 * (tokens + 1));
-    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS>, smem)) return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS>, dim3(g.ld.rbs, ceil_div(g.T, PASS)), dim3(WARPS * 32), smem, st, g);
-}
-template <bool F16>
-int launch_moe(const MoeArgs& g, int sms, cudaStream_t st)
+// Launch of a kernel of clusters that may begin while the one before it drains.
+template <typename... P, typename... A>
+int launch_clusters(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, A... args)
 {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(ROUTE_CTAS, ceil_div(g.T, 8));
-    cfg.blockDim = dim3(ROUTE_WARPS * 32);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = ROUTE_CTAS;
+    attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, w4_moe_route_kernel<F16>, g) != cudaSuccess) {
-        cudaGetLastError();
-        return BS_ERR_CUDA;
-    }
+    if (cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...) == cudaSuccess) return BS_OK;
+    cudaGetLastError();
+    return BS_ERR_CUDA;
+}
+template <bool F16, int NG, bool ZEROS, int NT>
+int launch_gate(const MoeArgs& g, int sms, cudaStream_t st)
+{
+    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k;
+    const long long items = static_cast<long long>(slots < g.E ? slots : g.E) * g.lu.rbs;
+    // enough warps for 16 an SM, each with two blocks of the reduction at least
+    int split = WARPS;
+    while (split > 1 && (2 * split > g.lu.cbs + 1 || items * split / 2 >= 16ll * sms)) split /= 2;
+    const long long ctas = (items * split + WARPS - 1) / WARPS;
+    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(ctas < 2 * sms ? ctas : 2 * sms), ceil_div(g.T, PASS)),
+                            dim3(WARPS * 32), 0, st, g, split);
+}
+template <bool F16, int NG, bool ZEROS, int NT>
+int launch_down(const MoeArgs& g, int sms, cudaStream_t st)
+{
+    const int tokens = g.T < PASS ? g.T : PASS, rows = ceil_div(g.ld.rbs, DOWN_RT);
+    const size_t smem = sizeof(float) * WARPS * DOWN_ROWS * (tokens + 1);
+    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
+    // CTAs of a cluster until two fill every SM
+    int cluster = 1;
+    while (cluster < 8 && rows * cluster * 2 <= 2 * sms) cluster *= 2;
+    return launch_clusters(w4_moe_down_kernel<F16, NG, ZEROS, NT>, dim3(rows * cluster, ceil_div(g.T, PASS)), WARPS * 32, smem, cluster, st, g, cluster);
+}
+template <bool F16, int NT>
+int launch_experts(const MoeArgs& g, int sms, cudaStream_t st)
+{
     int rc;
     const int nu = g.lu.group == 32 ? 4 : g.lu.group == 64 ? 2 : 1, nd = g.ld.group == 32 ? 4 : g.ld.group == 64 ? 2 : 1;
-    if (g.lu.zeros) rc = nu == 4 ? launch_gate<F16, 4, true>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, true>(g, sms, st) : launch_gate<F16, 1, true>(g, sms, st);
-    else rc = nu == 4 ? launch_gate<F16, 4, false>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, false>(g, sms, st) : launch_gate<F16, 1, false>(g, sms, st);
+    if (g.lu.zeros) rc = nu == 4 ? launch_gate<F16, 4, true, NT>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, true, NT>(g, sms, st) : launch_gate<F16, 1, true, NT>(g, sms, st);
+    else rc = nu == 4 ? launch_gate<F16, 4, false, NT>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, false, NT>(g, sms, st) : launch_gate<F16, 1, false, NT>(g, sms, st);
     if (rc != BS_OK) return rc;
-    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true>(g, st) : nd == 2 ? launch_down<F16, 2, true>(g, st) : launch_down<F16, 1, true>(g, st);
-    return nd == 4 ? launch_down<F16, 4, false>(g, st) : nd == 2 ? launch_down<F16, 2, false>(g, st) : launch_down<F16, 1, false>(g, st);
+    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true, NT>(g, sms, st) : nd == 2 ? launch_down<F16, 2, true, NT>(g, sms, st) : launch_down<F16, 1, true, NT>(g, sms, st);
+    return nd == 4 ? launch_down<F16, 4, false, NT>(g, sms, st) : nd == 2 ? launch_down<F16, 2, false, NT>(g, sms, st) : launch_down<F16, 1, false, NT>(g, sms, st);
+}
+template <bool F16>
+int launch_moe(const MoeArgs& g, int sms, cudaStream_t st)
+{
+    const int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
+    if (rc != BS_OK) return rc;
+    // a second job of an expert reads its weights again: jobs of 16 slots where more than eight are likely
+    return (g.T < PASS ? g.T : PASS) * g.top_k > 5 * g.E ? launch_experts<F16, 2>(g, sms, st) : launch_experts<F16, 1>(g, sms, st);
 }
 
 size_t hidden_bytes(int T, int top_k, int I) { return static_cast<size_t>(T) * top_k * ((static_cast<size_t>(I) + 7) / 8 * 8) * 2; }

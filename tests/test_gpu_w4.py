@@ -268,6 +268,21 @@ def test_moe_rows_apart(pitch):
     check_moe(*case, 32, 32, 3, True, xd=wide.cuda()[:, :70])
 
 
+@pytest.mark.parametrize("T,E,top_k", [(64, 16, 8), (64, 128, 8), (64, 3, 3), (130, 7, 2), (8, 1, 1)])
+def test_moe_writes_all_that_it_reads(T, E, top_k):
+    """Experts with many tokens, whose work is cut in several parts; the workspace's memory holds NaN before every call."""
+    rng = np.random.default_rng(T + E)
+    x, router, gate, up, down = moe_case(rng, T, E, 256, 144, 128, 64, BF16, False, False)
+    w = [prepared(p, q) for p, q in ((gate, 128), (up, 128), (down, 64))]
+    want, far, _, _ = ref.moe(x, router, ref.matrix(*gate, 128), ref.matrix(*up, 128), ref.matrix(*down, 64), top_k, True, BF16)
+    xd, rd = x.cuda(), router.cuda()
+    for _ in range(10):
+        poison = [torch.full((n << 10,), float("nan"), device="cuda") for n in (1, 8, 64, 128, 256, 512)]
+        del poison
+        y = api.moe_w4(xd, rd, *w, top_k)[0]
+        assert ((y.cpu().double() - want).abs() <= far).all()
+
+
 def test_moe_ties_and_equal_experts():
     """Equal logits: the lowest index first; all tokens to the same experts."""
     rng = np.random.default_rng(4)
