@@ -1,28 +1,29 @@
 // Weights of 4 bits with a scale (and zero point) per group of the reduction, laid out for the tensor cores: shared by csrc/w4_*.cu.
 //
-// A prepared matrix of O rows and K columns is, one after the other,
-//   codes   [ceil(O/16)][ceil(K/128)] blocks of 1 KB: [t 0..3][row 0..15][word j 0..3], a word holds the stored codes (0..15) of columns
-//           32 j + 8 t + (0..7): nibble i < 4 is column 2 i, nibble i >= 4 column 2 (i - 4) + 1, so that (word >> 4 i) & 0x000f000f is a pair of
-//           neighbouring columns, one in each half.  16 bytes are one row's part of what lane t of a quad multiplies (mma.sync), and four of
-//           them are a row's 128 columns for the thread that owns the row (tensor memory); either way a warp reads whole lines.
-//   steps   [ceil(O/16)][G][8] entries of 4 bytes, G = ceil(K / group): the scales, of the activations' type, of rows r and r + 8 of a block, which are
-//           the rows that a lane of an mma.sync fragment owns; where the weights have zero points entries of 8 bytes, the second word with
-//           the two zero points in its halves.  Without zero points the codes are stored plus 8, and 8 is the zero.
-// Rows and columns beyond O and K hold the code that stands for zero, steps beyond O are zero.
+// A prepared matrix of O rows and K columns is [ceil(O/16)][ceil(K/128)] blocks of 16 rows and 128 columns, each in one piece, which one bulk copy moves:
+//   codes  [t 0..3][16 bytes of a row, 16 rows]: word j of the 16 bytes holds the stored codes (0..15) of columns 32 j + 8 t + (0..7): nibble i < 4 is
+//          column 2 i, nibble i >= 4 column 2 (i - 4) + 1, so that (word >> 4 i) & 0x000f000f is a pair of neighbouring columns, one in each
+//          half.  The 16 bytes are one row's part of what lane t of a quad multiplies (mma.sync), and four of them are a row's 128 columns
+//          for the thread that owns the row (tensor memory).  Row r has place (r & 8) | ((r & 7) ^ 2 t): either way of reading meets
+//          every bank of shared memory once.
+//   steps  [groups in the block: 4, 2 or 1][8 entries of 4 bytes]: the scales, of the activations' type, of rows r and r + 8, which a lane of an mma.sync
+//          fragment owns; where the weights have zero points entries of 8 bytes, the second word with the two zero points in its
+//          halves.  Without zero points the codes are stored plus 8, and 8 is the zero.  A group of more than 128 columns has its
+//          entries in each of its blocks.
+// Columns beyond K meet zeros of x and hold code 0, rows beyond O too; the steps of groups and rows that do not exist are zero.
 #pragma once
 #include "common.cuh"
 
 namespace bs {
 
-constexpr int W4_ROWS = 16, W4_COLS = 128, W4_BLOCK = W4_ROWS * W4_COLS / 2;
+constexpr int W4_ROWS = 16, W4_COLS = 128, W4_CODES = W4_ROWS * W4_COLS / 2;     // bytes of a block's codes
 constexpr int W4_MAX_DIM = 1 << 20;     // rows, columns and columns of a group
 
 struct W4Layout {
     int O, K, group, zeros;     // zeros: the matrix has zero points
-    int rbs, cbs, G;            // blocks of rows, blocks of columns, groups of a row
-    unsigned per_group;         // multiplier that divides a block's number by the blocks of a group, 0 where that is one
-    __host__ __device__ size_t codes_bytes() const { return static_cast<size_t>(rbs) * cbs * W4_BLOCK; }
-    __host__ __device__ size_t bytes() const { return codes_bytes() + static_cast<size_t>(rbs) * G * (zeros ? 64 : 32); }
+    int rbs, cbs;               // blocks of rows, blocks of columns
+    int block;                  // bytes of a block
+    __host__ __device__ size_t bytes() const { return static_cast<size_t>(rbs) * cbs * block; }
 };
 
 // Groups of 32 or 64 columns, or a multiple of 128: a block of columns then holds 4, 2 or 1 of them (or a part of one).
@@ -32,10 +33,8 @@ inline bool w4_layout(int O, int K, int group, int zeros, W4Layout& l)
 {
     if (O <= 0 || K <= 0 || O > W4_MAX_DIM || K > W4_MAX_DIM || !w4_group_ok(group)) return false;
     l.O = O; l.K = K; l.group = group; l.zeros = zeros != 0;
-    // ceil(2^32 / n) divides c exactly as long as c n < 2^32: both are at most 2^13
-    const unsigned n = group > W4_COLS ? group / W4_COLS : 1;
-    l.per_group = n == 1 ? 0 : static_cast<unsigned>(((1ull << 32) + n - 1) / n);
-    l.rbs = ceil_div(O, W4_ROWS); l.cbs = ceil_div(K, W4_COLS); l.G = ceil_div(K, group);
+    l.rbs = ceil_div(O, W4_ROWS); l.cbs = ceil_div(K, W4_COLS);
+    l.block = W4_CODES + (group < W4_COLS ? W4_COLS / group : 1) * (zeros ? 64 : 32);
     return true;
 }
 
@@ -48,6 +47,7 @@ struct W4Gemm {
     long long ldx, ldy;
     int M;
     W4Layout l;
+    int* status;                // device status word
 };
 
 }  // namespace bs

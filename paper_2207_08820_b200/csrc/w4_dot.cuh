@@ -68,33 +68,65 @@ struct W4Tile {
     uint32_t scale[NG], zero[NG];
 };
 
-// Where a lane finds the blocks of 16 rows.  Weights go straight to registers, a few blocks ahead of their use, and past L1, which x needs.
-template <int NG, bool ZEROS>
-struct W4Rows {
-    static constexpr int ENTRY = ZEROS ? 8 : 4;
-    const unsigned char *codes, *steps;
+// Blocks on their way through shared memory: a warp copies ahead into a ring of STAGES of its own, RT blocks a stage, one bulk copy each, and waits for
+// nobody else.  (Loads into registers a few blocks ahead wait for one another: the waits of a warp are counted in six places only.)
+template <int NG, bool ZEROS, int RT, int STAGES>
+struct W4Ring {
+    static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * RT * BLOCK;
+    uint32_t base, bars;        // the barriers' memory holds nothing else: only an invalidated one may be written over
+    int in, out;                // stages that are filled and read next
+    unsigned phase, limit;      // parity of the round of `out`; polls of a wait, 1 after one has run out
 
-    __device__ __forceinline__ W4Rows() {}
-    __device__ __forceinline__ W4Rows(const unsigned char* matrix, const W4Layout& l, int rb, int lane)
+    __device__ __forceinline__ W4Ring(unsigned char* smem, uint64_t (&bar)[STAGES], int warp, int lane) : in(0), out(0), phase(0), limit(1u << 20)
     {
-        codes = matrix + static_cast<size_t>(rb) * l.cbs * W4_BLOCK + (lane & 3) * 256 + (lane >> 2) * 16;
-        steps = matrix + l.codes_bytes() + (static_cast<size_t>(rb) * l.G * 8 + (lane >> 2)) * ENTRY;
-    }
-    __device__ __forceinline__ void load(W4Tile<NG, ZEROS>& w, const W4Layout& l, int cb) const
-    {
-        const unsigned char* p = codes + static_cast<unsigned>(cb) * W4_BLOCK;
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.a.x), "=r"(w.a.y), "=r"(w.a.z), "=r"(w.a.w) : "l"(p));
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w.b.x), "=r"(w.b.y), "=r"(w.b.z), "=r"(w.b.w) : "l"(p + 128));
-        const int g0 = NG > 1 ? cb * NG : l.per_group == 0 ? cb : static_cast<int>(__umulhi(cb, l.per_group));
+        base = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * BYTES;
+        bars = static_cast<uint32_t>(__cvta_generic_to_shared(bar));
+        if (lane == 0) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            // groups behind the last one multiply zeros of x: their scale is one too
-            const bool live = NG == 1 || g == 0 || g0 + g < l.G;
-            const unsigned char* e = steps + static_cast<unsigned>(live ? g0 + g : g0) * (8 * ENTRY);
-            if (ZEROS) asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w.scale[g]), "=r"(w.zero[g]) : "l"(e));
-            else asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(w.scale[g]) : "l"(e));
-            if (!live) w.scale[g] = 0;
+            for (int s = 0; s < STAGES; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * s) : "memory");
+            asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
         }
+        __syncwarp();
+    }
+    // Fills the next stage with the blocks at p; every lane has read what it held.
+    __device__ __forceinline__ void put(const unsigned char* const (&p)[RT], int lane)
+    {
+        if (lane == 0) {
+            const uint32_t bar = bars + 8 * in;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(RT * BLOCK) : "memory");
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                             ::"r"(base + (in * RT + r) * BLOCK), "l"(p[r]), "n"(BLOCK), "r"(bar) : "memory");
+        }
+        in = in + 1 == STAGES ? 0 : in + 1;
+    }
+    // The blocks of the next stage that was filled.  A wait that runs out sets the status word; later ones then poll once.
+    __device__ __forceinline__ void get(W4Tile<NG, ZEROS> (&w)[RT], int lane, int* status)
+    {
+        const uint32_t bar = bars + 8 * out;
+        unsigned ok = 0;
+        for (unsigned it = 0; it < limit && !ok; ++it)
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
+        if (!ok) {
+            if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
+            limit = 1;
+        }
+        __syncwarp();
+        const int r8 = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const uint32_t block = base + (out * RT + r) * BLOCK, at = block + t * 256 + (r8 ^ 2 * t) * 16;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].a.x), "=r"(w[r].a.y), "=r"(w[r].a.z), "=r"(w[r].a.w) : "r"(at) : "memory");
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].b.x), "=r"(w[r].b.y), "=r"(w[r].b.z), "=r"(w[r].b.w) : "r"(at + 128) : "memory");
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint32_t step = block + W4_CODES + (g * 8 + r8) * ENTRY;
+                if (ZEROS) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[r].scale[g]), "=r"(w[r].zero[g]) : "r"(step) : "memory");
+                else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[r].scale[g]) : "r"(step) : "memory");
+            }
+        }
+        if (++out == STAGES) { out = 0; phase ^= 1; }
     }
 };
 

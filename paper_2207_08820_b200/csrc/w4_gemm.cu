@@ -10,28 +10,35 @@
 namespace bs {
 namespace {
 
-constexpr int MOST_WARPS = 8;
+constexpr int MOST_WARPS = 16;
 
 // A CTA owns 16 RT rows of the weights and 8 NT rows of x; its warps take the blocks of the reduction in turn.
-template <bool F16, int NG, bool ZEROS, int NT, int RT>
-__global__ void __launch_bounds__(MOST_WARPS * 32, NT * RT == 1 ? 3 : 2) w4_gemm_kernel(const __grid_constant__ W4Gemm g)
+template <bool F16, int NG, bool ZEROS, int NT, int RT, int STAGES>
+__global__ void __launch_bounds__(MOST_WARPS * 32, 1) w4_gemm_kernel(const __grid_constant__ W4Gemm g)
 {
     typedef typename W4Type<F16>::T T;
-    constexpr int STAGES = (NT * RT == 1 ? 4 : NT * RT == 2 ? 3 : 2) - (NG == 4 && NT * RT < 4 ? 1 : 0), M = NT * 8, R = RT * W4_ROWS, PITCH = R + 1;
-    extern __shared__ float part[];         // [warps][M][PITCH]
+    typedef W4Ring<NG, ZEROS, RT, STAGES> Ring;
+    constexpr int M = NT * 8, R = RT * W4_ROWS, PITCH = R + 1;
+    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps; in the end their sums, [warps][M][PITCH] floats
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, rb0 = blockIdx.x * RT, m0 = blockIdx.y * M;
+    __shared__ uint64_t bars[MOST_WARPS][STAGES];
+    Ring ring(smem, bars[warp], warp, lane);
+    const unsigned char* from[RT];
     const unsigned char* matrix = dependent_begin(g.w);
     const T* x0 = behind_wait<T>(g.x);
-    W4Rows<NG, ZEROS> rows[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) rows[r] = W4Rows<NG, ZEROS>(matrix, g.l, min(rb0 + r, g.l.rbs - 1), lane);
-    W4Tile<NG, ZEROS> w[STAGES][RT];
+    for (int r = 0; r < RT; ++r) from[r] = matrix + (static_cast<size_t>(min(rb0 + r, g.l.rbs - 1)) * g.l.cbs + warp) * Ring::BLOCK;
+    int left = (g.l.cbs - warp + warps - 1) / warps;       // blocks that this warp has still to fetch
+    auto put = [&] {
+        if (left > 0) {
+            ring.put(from, lane);
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-        if (warp + s * warps < g.l.cbs) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) rows[r].load(w[s][r], g.l, warp + s * warps);
+            for (int r = 0; r < RT; ++r) from[r] += warps * Ring::BLOCK;
+            --left;
         }
+    };
+#pragma unroll 1
+    for (int s = 0; s < STAGES - 1; ++s) put();
     const T* row[NT];       // lanes without a row of x compute the last one's again
 #pragma unroll
     for (int n = 0; n < NT; ++n) row[n] = x0 + min(m0 + n * 8 + (lane >> 2), g.M - 1) * g.ldx;
@@ -41,22 +48,17 @@ __global__ void __launch_bounds__(MOST_WARPS * 32, NT * RT == 1 ? 3 : 2) w4_gemm
 #pragma unroll
         for (int n = 0; n < NT; ++n) tot[r][n][0] = tot[r][n][1] = tot[r][n][2] = tot[r][n][3] = 0.f;
     const int full = g.l.K / W4_COLS;
-    for (int cb = warp; cb < g.l.cbs; cb += STAGES * warps) {
+    for (int cb = warp; cb < g.l.cbs; cb += warps) {
+        uint4 x[NT][4];
 #pragma unroll
-        for (int s = 0; s < STAGES; ++s) {
-            const int c = cb + s * warps;
-            if (c < g.l.cbs) {
-                uint4 x[NT][4];
-#pragma unroll
-                for (int n = 0; n < NT; ++n) load_block_x(x[n], row[n], c, g.l.K, c < full, lane);
-                w4_blocks<F16, F16, 1>(w[s], [&](int n, int j, int) { return x[n][j]; }, tot);
-                if (c + STAGES * warps < g.l.cbs) {
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) rows[r].load(w[s][r], g.l, c + STAGES * warps);
-                }
-            }
-        }
+        for (int n = 0; n < NT; ++n) load_block_x(x[n], row[n], cb, g.l.K, cb < full, lane);
+        W4Tile<NG, ZEROS> w[RT];
+        ring.get(w, lane, g.status);
+        put();      // into the stage before this one: its blocks have been multiplied
+        w4_blocks<F16, F16, 1>(w, [&](int n, int j, int) { return x[n][j]; }, tot);
     }
+    __syncthreads();
+    float* part = reinterpret_cast<float*>(smem);
     float* mine = part + warp * M * PITCH;
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -92,18 +94,21 @@ __global__ void __launch_bounds__(256) w4_align_rows_kernel(const uint16_t* x, l
     }
 }
 
-template <bool F16, int NG, bool ZEROS, int NT, int RT>
+template <bool F16, int NG, bool ZEROS, int NT, int RT, int STAGES>
 int launch_tile(const W4Gemm& g, int sms, cudaStream_t st)
 {
-    const int items = ceil_div(g.l.rbs, RT);
+    auto kernel = w4_gemm_kernel<F16, NG, ZEROS, NT, RT, STAGES>;
+    const int items = ceil_div(g.l.rbs, RT), tiles = ceil_div(g.M, 8 * NT);
     // enough warps for 16 an SM, each with two blocks of the reduction at least
     int warps = MOST_WARPS;
-    while (warps > 1 && (2 * warps > g.l.cbs + 1 || static_cast<long long>(items) * warps / 2 >= 16ll * sms)) warps /= 2;
+    while (warps > 1 && (2 * warps > g.l.cbs + 1 || static_cast<long long>(items) * tiles * warps / 2 >= 16ll * sms)) warps /= 2;
 #ifdef BS_TUNING
     if (const char* e = getenv("BS_W4_WARPS")) warps = atoi(e);
 #endif
-    return launch_dependent(w4_gemm_kernel<F16, NG, ZEROS, NT, RT>, dim3(items, ceil_div(g.M, 8 * NT)), dim3(warps * 32),
-                            sizeof(float) * warps * NT * 8 * (RT * W4_ROWS + 1), st, g);
+    const int ring = warps * W4Ring<NG, ZEROS, RT, STAGES>::BYTES, part = static_cast<int>(sizeof(float)) * warps * NT * 8 * (RT * W4_ROWS + 1);
+    const int smem = ring > part ? ring : part;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
+    return launch_dependent(kernel, dim3(items, tiles), dim3(warps * 32), smem, st, g);
 }
 template <bool F16, int NG, bool ZEROS>
 int launch_rows(const W4Gemm& g, int sms, cudaStream_t st)
@@ -111,14 +116,14 @@ int launch_rows(const W4Gemm& g, int sms, cudaStream_t st)
 #ifdef BS_TUNING
     if (const char* e = getenv("BS_W4_RT")) {
         const int rt = atoi(e);
-        if (g.M <= 8) return rt == 1 ? launch_tile<F16, NG, ZEROS, 1, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 1, 2>(g, sms, st);
-        if (g.M <= 16) return rt == 1 ? launch_tile<F16, NG, ZEROS, 2, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2, 2>(g, sms, st);
-        return rt == 1 ? launch_tile<F16, NG, ZEROS, 4, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 4, 2>(g, sms, st);
+        if (g.M <= 8) return rt == 1 ? launch_tile<F16, NG, ZEROS, 1, 1, 8>(g, sms, st) : launch_tile<F16, NG, ZEROS, 1, 2, 6>(g, sms, st);
+        if (g.M <= 16) return rt == 1 ? launch_tile<F16, NG, ZEROS, 2, 1, 8>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2, 2, 4>(g, sms, st);
+        return rt == 1 ? launch_tile<F16, NG, ZEROS, 4, 1, 4>(g, sms, st) : launch_tile<F16, NG, ZEROS, 4, 2, 4>(g, sms, st);
     }
 #endif
-    if (g.M <= 8) return launch_tile<F16, NG, ZEROS, 1, 1>(g, sms, st);
-    if (g.M <= 16) return launch_tile<F16, NG, ZEROS, 2, 1>(g, sms, st);
-    return launch_tile<F16, NG, ZEROS, 4, 1>(g, sms, st);
+    if (g.M <= 8) return launch_tile<F16, NG, ZEROS, 1, 2, 4>(g, sms, st);
+    if (g.M <= 16) return launch_tile<F16, NG, ZEROS, 2, 2, 4>(g, sms, st);
+    return launch_tile<F16, NG, ZEROS, 4, 2, 4>(g, sms, st);
 }
 template <bool F16>
 int launch(const W4Gemm& g, int sms, cudaStream_t st)
@@ -152,7 +157,8 @@ extern "C" int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, in
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (!rows_aligned(M, ldx) && (!workspace || workspace_bytes < bs_w4_gemm_workspace_bytes(M, K, ldx))) return BS_ERR_INVALID_ARG;
     const int sms = device_sm_count();
-    if (sms <= 0) return BS_ERR_CUDA;
+    g.status = status_device_ptr();
+    if (sms <= 0 || !g.status) return BS_ERR_CUDA;
     if (!rows_aligned(M, ldx)) {
         const int ldo = (K + 7) & ~7;
         const long long want = (static_cast<long long>(M) * (ldo / 8) + 255) / 256, most = static_cast<long long>(sms) * 8;

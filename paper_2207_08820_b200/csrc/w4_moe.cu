@@ -2,8 +2,8 @@
 //   route   logits = x R^T, the top_k experts of every token, their softmax weights
 //   gate    h[slot] = weight * silu(Gate_e x) * (Up_e x) for every slot (token, choice)
 //   down    y[token] = sum over its slots of Down_e h[slot]
-// Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), straight
-// into registers, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
+// Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), through
+// shared memory, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
 // of mantissa), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
 #include "w4_dot.cuh"
 
@@ -13,7 +13,7 @@ namespace {
 constexpr int PASS = 64;                    // tokens of a pass
 constexpr int MAX_EXPERTS = 512, MAX_TOP = 32;
 constexpr int ROUTE_CTAS = 8, ROUTE_WARPS = 16;     // CTAs of a cluster, a token each in the end; warps split the reduction
-constexpr int WARPS = 8;
+constexpr int WARPS = 8, GATE_STAGES = 4, DOWN_STAGES = 4;
 
 struct MoeArgs {
     const void *x, *router;
@@ -26,6 +26,7 @@ struct MoeArgs {
     long long ldxa;
     __nv_bfloat16 *hi, *lo;                 // [T top_k][ldh]
     int ldh;
+    int* status;                            // device status word
     int* experts;
     float* weights;
     void* y;
@@ -197,42 +198,56 @@ __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int
     __syncthreads();
 }
 
-// h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  `split` warps, a team, share the reduction of an item; the first blocks of a
-// team's next item are on their way while it puts the sums of the current one together.
+// h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  `split` warps, a team, share the reduction of an item; the blocks of their
+// next items are on their way while they put the sums of the current one together.
 template <bool F16, int NG, bool ZEROS, int NT>
 __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g, int split)
 {
     typedef typename W4Type<F16>::T T;
-    constexpr int J = NT * 8, STAGES = 2;
+    typedef W4Ring<NG, ZEROS, 2, GATE_STAGES> Ring;
+    constexpr int J = NT * 8;
+    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps
     __shared__ Jobs jobs;
     __shared__ float part[WARPS][2][J][17];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
     const int team = warp / split, k0 = warp % split, teams = WARPS / split;
+    __shared__ uint64_t bars[WARPS][GATE_STAGES];
+    Ring ring(smem, bars[warp], warp, lane);
     const T* x = static_cast<const T*>(dependent_begin(g.xa ? g.xa : g.x));
     const long long ldx = g.xa ? g.ldxa : g.ldx;
     find_jobs<J>(g, jobs, t0, WARPS * 32);
     const W4Layout& l = g.lu;
     const size_t matrix = l.bytes();
     const int items = jobs.n * l.rbs, full = l.K / W4_COLS;
-    W4Rows<NG, ZEROS> rows[2];
-    W4Tile<NG, ZEROS> w[STAGES][2];
-    auto begin = [&](int item) {
-        const int job = item / l.rbs, rb = item - job * l.rbs;
-        const size_t at = jobs.expert[job] * matrix;
-        rows[0] = W4Rows<NG, ZEROS>(g.gate + at, l, rb, lane);
-        rows[1] = W4Rows<NG, ZEROS>(g.up + at, l, rb, lane);
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s)
-            if (k0 + s * split < l.cbs) {
-                rows[0].load(w[s][0], l, k0 + s * split);
-                rows[1].load(w[s][1], l, k0 + s * split);
-            }
-    };
     // neighbouring teams work on neighbouring rows: they share the tokens' x in L1
     const int step = gridDim.x * teams;
-    int item = blockIdx.x * teams + team;
-    if (item < items) begin(item);
-    for (; item < items; item += step) {
+    // the blocks that are fetched next
+    int fitem = blockIdx.x * teams + team, fc = k0;
+    const unsigned char* from[2];
+    auto locate = [&] {
+        const int job = fitem / l.rbs, rb = fitem - job * l.rbs;
+        const size_t at = jobs.expert[job] * matrix + (static_cast<size_t>(rb) * l.cbs + k0) * Ring::BLOCK;
+        from[0] = g.gate + at;
+        from[1] = g.up + at;
+    };
+    if (k0 >= l.cbs) fitem = items;
+    if (fitem < items) locate();
+    auto put = [&] {
+        if (fitem >= items) return;
+        ring.put(from, lane);
+        fc += split;
+        if (fc < l.cbs) {
+            from[0] += split * Ring::BLOCK;
+            from[1] += split * Ring::BLOCK;
+        } else {
+            fc = k0;
+            fitem += step;
+            if (fitem < items) locate();
+        }
+    };
+#pragma unroll 1
+    for (int s = 0; s < GATE_STAGES - 1; ++s) put();
+    for (int item = blockIdx.x * teams + team; item < items; item += step) {
         const int job = item / l.rbs, rb = item - job * l.rbs, beg = jobs.first[job];
         // a job's slots end where the next one's begin; lanes without a slot compute the last one's again
         const int n = jobs.first[job + 1] - beg;
@@ -244,23 +259,15 @@ __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_gate_kernel(const __grid
         for (int k = 0; k < NT; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
-        for (int cb = k0; cb < l.cbs; cb += STAGES * split) {
+        for (int c = k0; c < l.cbs; c += split) {
+            uint4 v[NT][4];
 #pragma unroll
-            for (int s = 0; s < STAGES; ++s) {
-                const int c = cb + s * split;
-                if (c < l.cbs) {
-                    uint4 v[NT][4];
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
-                    w4_blocks<F16, F16, 1>(w[s], [&](int k, int j, int) { return v[k][j]; }, tot);
-                    if (c + STAGES * split < l.cbs) {
-                        rows[0].load(w[s][0], l, c + STAGES * split);
-                        rows[1].load(w[s][1], l, c + STAGES * split);
-                    }
-                }
-            }
+            for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
+            W4Tile<NG, ZEROS> w[2];
+            ring.get(w, lane, g.status);
+            put();      // into the stage before this one: its blocks have been multiplied
+            w4_blocks<F16, F16, 1>(w, [&](int k, int j, int) { return v[k][j]; }, tot);
         }
-        if (item + step < items) begin(item + step);
 #pragma unroll
         for (int k = 0; k < NT; ++k)
 #pragma unroll
@@ -296,11 +303,15 @@ template <bool F16, int NG, bool ZEROS, int NT>
 __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int cluster)
 {
     typedef typename W4Type<F16>::T T;
-    constexpr int J = NT * 8, STAGES = 2, RT = DOWN_RT;
-    extern __shared__ float sums[];         // [WARPS][DOWN_ROWS][pitch]
+    typedef W4Ring<NG, ZEROS, DOWN_RT, DOWN_STAGES> Ring;
+    constexpr int J = NT * 8, RT = DOWN_RT;
+    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps, then sums [WARPS][DOWN_ROWS][pitch]
     __shared__ Jobs jobs;
+    float* sums = reinterpret_cast<float*>(smem + WARPS * Ring::BYTES);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS, rb0 = blockIdx.x / cluster * RT, rank = blockIdx.x % cluster;
     const int tokens = g.T - t0 < PASS ? g.T - t0 : PASS, pitch = tokens + 1;
+    __shared__ uint64_t bars[WARPS][DOWN_STAGES];
+    Ring ring(smem, bars[warp], warp, lane);
     const unsigned char* down = dependent_begin(g.down);
     const __nv_bfloat16* hidden = behind_wait<__nv_bfloat16>(g.hi);
     find_jobs<J>(g, jobs, t0, WARPS * 32);
@@ -312,73 +323,61 @@ __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid
     const int full = l.K / W4_COLS, runs = cluster * WARPS, run = rank * WARPS + warp;
     const long long blocks = static_cast<long long>(jobs.n) * l.cbs;
     const int beg = static_cast<int>(blocks * run / runs), end = static_cast<int>(blocks * (run + 1) / runs);
-    W4Rows<NG, ZEROS> rows[RT];
-    W4Tile<NG, ZEROS> w[STAGES][RT];
-    int fjob = beg / l.cbs, fc = beg - fjob * l.cbs;        // the block that is fetched next
-    auto at = [&](int job) {
-        const unsigned char* p = down + jobs.expert[job] * matrix;
+    int f = beg, fjob = beg / l.cbs, fc = beg - fjob * l.cbs;        // the blocks that are fetched next
+    const unsigned char* from[RT];
+    auto locate = [&] {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) rows[r] = W4Rows<NG, ZEROS>(p, l, min(rb0 + r, l.rbs - 1), lane);
+        for (int r = 0; r < RT; ++r) from[r] = down + jobs.expert[fjob] * matrix + (static_cast<size_t>(min(rb0 + r, l.rbs - 1)) * l.cbs + fc) * Ring::BLOCK;
     };
-    auto fetch = [&](W4Tile<NG, ZEROS> (&to)[RT]) {
+    if (beg < end) locate();
+    auto put = [&] {
+        if (f >= end) return;
+        ring.put(from, lane);
+        ++f;
+        if (++fc < l.cbs) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) rows[r].load(to[r], l, fc);
-    };
-    if (beg < end) at(fjob);
-#pragma unroll
-    for (int s = 0; s < STAGES; ++s)
-        if (beg + s < end) {
-            fetch(w[s]);
-            if (++fc == l.cbs) { fc = 0; if (beg + s + 1 < end) at(++fjob); }
+            for (int r = 0; r < RT; ++r) from[r] += Ring::BLOCK;
+        } else {
+            fc = 0;
+            ++fjob;
+            if (f < end) locate();
         }
-    int job = beg / l.cbs, c = beg - job * l.cbs, first = 0, n = 0;
-    const __nv_bfloat16* row[NT];
+    };
+#pragma unroll 1
+    for (int s = 0; s < DOWN_STAGES - 1; ++s) put();
+    int job = beg / l.cbs, c = beg - job * l.cbs;
     const long long lo = g.lo - g.hi;
-    float tot[RT][NT][4];
-    auto begin = [&] {
-        first = jobs.first[job];
-        n = jobs.first[job + 1] - first;
+    for (int b = beg; b < end;) {       // jobs, or this warp's part of one
+        const int first = jobs.first[job], n = jobs.first[job + 1] - first, stop = min(l.cbs, c + end - b);
+        b += stop - c;
+        const __nv_bfloat16* row[NT];
+        float tot[RT][NT][4];
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
             row[k] = hidden + (static_cast<size_t>(t0) * g.top_k + jobs.slot[first + min(k * 8 + (lane >> 2), n - 1)]) * g.ldh;
 #pragma unroll
             for (int r = 0; r < RT; ++r) tot[r][k][0] = tot[r][k][1] = tot[r][k][2] = tot[r][k][3] = 0.f;
         }
-    };
-    if (beg < end) begin();
-    for (int b0 = beg; b0 < end; b0 += STAGES) {
-#pragma unroll
-        for (int s = 0; s < STAGES; ++s) {
-            const int b = b0 + s;
-            if (b < end) {
-                if (c < full) {
-                    const int k0 = c * W4_COLS + 8 * (lane & 3);
-                    w4_blocks<false, F16, 2>(w[s], [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + k0 + 32 * j)); }, tot);
-                } else {
-                    const int k0 = c * W4_COLS + 8 * (lane & 3);
-                    w4_blocks<false, F16, 2>(w[s], [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0), k0 + 32 * j, l.K); }, tot);
-                }
-                if (b + STAGES < end) {
-                    fetch(w[s]);
-                    if (++fc == l.cbs) { fc = 0; if (b + STAGES + 1 < end) at(++fjob); }
-                }
-                if (++c == l.cbs || b + 1 == end) {     // the end of the job, or of this warp's part of it
-#pragma unroll
-                    for (int k = 0; k < NT; ++k)
-#pragma unroll
-                        for (int r = 0; r < RT; ++r)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {       // lanes own different (row, slot): an expert has a token once
-                                const int q = k * 8 + 2 * (lane & 3) + (i & 1);
-                                if (q < n) own[(r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)) * pitch + jobs.token[first + q]] += tot[r][k][i];
-                            }
-                    __syncwarp();       // another job's slots meet the same tokens from other lanes
-                    c = 0;
-                    ++job;
-                    if (b + 1 < end) begin();
-                }
-            }
+        for (; c < stop; ++c) {
+            W4Tile<NG, ZEROS> w[RT];
+            const int k0 = c * W4_COLS + 8 * (lane & 3);
+            ring.get(w, lane, g.status);
+            put();      // into the stage before this one: its blocks have been multiplied
+            if (c < full) w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + k0 + 32 * j)); }, tot);
+            else w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0), k0 + 32 * j, l.K); }, tot);
         }
+        c = 0;
+        ++job;
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {       // lanes own different (row, slot): an expert has a token once
+                    const int q = k * 8 + 2 * (lane & 3) + (i & 1);
+                    if (q < n) own[(r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)) * pitch + jobs.token[first + q]] += tot[r][k][i];
+                }
+        __syncwarp();       // another job's slots meet the same tokens from other lanes
     }
     __syncthreads();
     for (int i = threadIdx.x; i < DOWN_ROWS * tokens; i += WARPS * 32) {
@@ -445,14 +444,16 @@ int launch_gate(const MoeArgs& g, int sms, cudaStream_t st)
     int split = WARPS;
     while (split > 1 && (2 * split > g.lu.cbs + 1 || items * split / 2 >= 16ll * sms)) split /= 2;
     const long long ctas = (items * split + WARPS - 1) / WARPS;
+    const size_t smem = WARPS * W4Ring<NG, ZEROS, 2, GATE_STAGES>::BYTES;
+    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
     return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(ctas < 2 * sms ? ctas : 2 * sms), ceil_div(g.T, PASS)),
-                            dim3(WARPS * 32), 0, st, g, split);
+                            dim3(WARPS * 32), smem, st, g, split);
 }
 template <bool F16, int NG, bool ZEROS, int NT>
 int launch_down(const MoeArgs& g, int sms, cudaStream_t st)
 {
     const int tokens = g.T < PASS ? g.T : PASS, rows = ceil_div(g.ld.rbs, DOWN_RT);
-    const size_t smem = sizeof(float) * WARPS * DOWN_ROWS * (tokens + 1);
+    const size_t smem = WARPS * W4Ring<NG, ZEROS, DOWN_RT, DOWN_STAGES>::BYTES + sizeof(float) * WARPS * DOWN_ROWS * (tokens + 1);
     if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
     // CTAs of a cluster until two fill every SM
     int cluster = 1;
@@ -520,8 +521,9 @@ extern "C" int bs_w4_moe(const void* x, long long ldx, int T, const void* router
         g.ldxa = (H + 7) & ~7;
     }
     g.experts = experts; g.weights = weights; g.y = y;
+    g.status = status_device_ptr();
     const int sms = device_sm_count();
-    if (sms <= 0) return BS_ERR_CUDA;
+    if (sms <= 0 || !g.status) return BS_ERR_CUDA;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     return type == BS_F16 ? launch_moe<true>(g, sms, st) : launch_moe<false>(g, sms, st);
 }

@@ -138,23 +138,25 @@ __global__ void __launch_bounds__(256) w4_quantise_rows_kernel(const T* w, long 
     }
 }
 
-// A thread writes the 16 bytes of (t, row): 32 codes of one row.  Set-up, once per matrix.
+// A thread writes the 16 bytes of (t, row): 32 codes of one row; the first of a block's 64 threads its steps too.  Set-up, once per matrix.
 __global__ void __launch_bounds__(256) w4_prepare_kernel(const int8_t* codes, const uint16_t* scales, const int8_t* zeros, W4Layout l, unsigned char* out)
 {
     codes = dependent_begin(codes);
     const size_t m = blockIdx.y;      // matrix
+    const int G = (l.K + l.group - 1) / l.group, in_block = l.group < W4_COLS ? W4_COLS / l.group : 1;
     codes += m * l.O * l.K;
-    scales += m * l.O * l.G;
-    if (zeros) zeros += m * l.O * l.G;
+    scales += m * l.O * G;
+    if (zeros) zeros += m * l.O * G;
     out += m * l.bytes();
-    const long long step = static_cast<long long>(gridDim.x) * blockDim.x, first = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const long long step = static_cast<long long>(gridDim.x) * blockDim.x;
     const bool wide = (l.K & 7) == 0;
     const uint32_t offset = zeros ? 0 : 8;
-    for (long long i = first; i < static_cast<long long>(l.rbs) * l.cbs * 64; i += step) {
+    for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < static_cast<long long>(l.rbs) * l.cbs * 64; i += step) {
         // the four threads of a row are neighbours: they read 32 bytes in a row
         const long long b = i >> 6;
-        const int t = static_cast<int>(i) & 3, r = (static_cast<int>(i) >> 2) & 15;
+        const int u = static_cast<int>(i) & 63, t = u & 3, r = u >> 2;
         const int rb = static_cast<int>(b / l.cbs), cb = static_cast<int>(b - static_cast<long long>(rb) * l.cbs), o = rb * 16 + r;
+        unsigned char* block = out + b * l.block;
         uint32_t word[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -165,27 +167,22 @@ __global__ void __launch_bounds__(256) w4_prepare_kernel(const int8_t* codes, co
 #pragma unroll
                 for (int e = 0; e < 8; ++e) c[e] = ((e < 4 ? v.x : v.y) >> (8 * (e & 3))) + offset;
             } else {
-                // columns behind K count for nothing: their x is zero
 #pragma unroll
-                for (int e = 0; e < 8; ++e) c[e] = (o < l.O && k0 + e < l.K ? static_cast<uint8_t>(codes[static_cast<size_t>(o) * l.K + k0 + e]) : 0u) + offset;
+                for (int e = 0; e < 8; ++e) c[e] = o < l.O && k0 + e < l.K ? static_cast<uint8_t>(codes[static_cast<size_t>(o) * l.K + k0 + e]) + offset : 0u;
             }
             word[j] = 0;
 #pragma unroll
             for (int e = 0; e < 8; ++e) word[j] |= (c[e] & 15u) << (4 * (e / 2 + 4 * (e & 1)));
         }
-        *reinterpret_cast<uint4*>(out + b * W4_BLOCK + t * 256 + r * 16) = make_uint4(word[0], word[1], word[2], word[3]);
-    }
-    uint32_t* steps = reinterpret_cast<uint32_t*>(out + l.codes_bytes());
-    for (long long i = first; i < static_cast<long long>(l.rbs) * l.G * 8; i += step) {
-        const long long b = i >> 3;
-        const int rb = static_cast<int>(b / l.G), g = static_cast<int>(b - static_cast<long long>(rb) * l.G), o = rb * 16 + (static_cast<int>(i) & 7);
-        const size_t at = static_cast<size_t>(o) * l.G + g, up = at + static_cast<size_t>(8) * l.G;
-        const uint32_t s = (o < l.O ? scales[at] : 0u) | (o + 8 < l.O ? scales[up] : 0u) << 16;
-        if (zeros) {
-            const uint32_t z = (o < l.O ? zeros[at] & 15u : 0u) | (o + 8 < l.O ? zeros[up] & 15u : 0u) << 16;
-            *reinterpret_cast<uint2*>(steps + 2 * i) = make_uint2(s, z);
-        } else {
-            steps[i] = s;
+        *reinterpret_cast<uint4*>(block + t * 256 + ((r & 8) | ((r & 7) ^ 2 * t)) * 16) = make_uint4(word[0], word[1], word[2], word[3]);
+        if (u < 8 * in_block) {
+            const int low = rb * 16 + (u & 7), high = low + 8, g = in_block > 1 ? cb * in_block + (u >> 3) : cb * 128 / l.group;
+            const size_t at = static_cast<size_t>(low) * G + g, up = static_cast<size_t>(high) * G + g;
+            const bool has_low = low < l.O && g < G, has_high = high < l.O && g < G;
+            const uint32_t s = (has_low ? scales[at] : 0u) | (has_high ? scales[up] : 0u) << 16;
+            uint32_t* steps = reinterpret_cast<uint32_t*>(block + W4_CODES);
+            if (zeros) *reinterpret_cast<uint2*>(steps + 2 * u) = make_uint2(s, (has_low ? zeros[at] & 15u : 0u) | (has_high ? zeros[up] & 15u : 0u) << 16);
+            else steps[u] = s;
         }
     }
 }

@@ -23,8 +23,8 @@ def at():
 
 def test_sizes(L):
     assert L.bs_w4_bytes(16, 128, 128, 0) == 1024 + 32
-    assert L.bs_w4_bytes(17, 129, 32, 0) == 4 * 1024 + 2 * 5 * 32
-    assert L.bs_w4_bytes(17, 129, 32, 1) == 4 * 1024 + 2 * 5 * 64
+    assert L.bs_w4_bytes(17, 129, 32, 0) == 4 * (1024 + 4 * 32)
+    assert L.bs_w4_bytes(17, 129, 64, 1) == 4 * (1024 + 2 * 64)
     assert L.bs_w4_bytes(1, 1, 1 << 20, 0) == 1024 + 32
     for bad in ((0, 128, 128), (16, 0, 128), (16, 128, 0), (16, 128, 48), (16, 128, 16), (16, 128, 192), (1 << 21, 128, 128), (16, 1 << 21, 128), (16, 128, 1 << 21), (16, 128, -128)):
         assert L.bs_w4_bytes(*bad, 0) == 0
