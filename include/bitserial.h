@@ -461,11 +461,12 @@ int bs_w4_prepare(const int8_t* codes, const void* scales, const int8_t* zeros, 
  * bs_w4_gemm -- y[m][o] = sum_k x[m][k] * W[o][k] + bias[o], one token (M = 1) or many.
  *   x     device, [M] rows of K values of `type`, `ldx` values apart;  y  device, [M] rows of O values, `ldy` apart;  bias  device [O] or NULL
  *   w     prepared matrix (its scales are of `type`)
- *   workspace  bs_w4_gemm_workspace_bytes(M, K, ldx) bytes (0 unless the rows of x start off 16-byte boundaries; NULL then)
+ *   workspace  bs_w4_gemm_workspace_bytes(...) bytes for the current device (0 and NULL for few rows of x on 16-byte boundaries); two calls that may
+ *              run at the same time need one each
  * Codes less their zero points are exact operands; products are summed in 32 bits over a group, scaled and added in 32 bits, rounded once.
  * The same call gives the same bits every time.  M = 0 is BS_OK and does nothing.  M up to 2^20.
  */
-size_t bs_w4_gemm_workspace_bytes(int M, int K, long long ldx);
+size_t bs_w4_gemm_workspace_bytes(int M, int O, int K, int group, long long ldx);
 int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K, int group, int zeros, bs_float_t type,
                const void* bias, void* y, long long ldy, void* workspace, size_t workspace_bytes, void* stream);
 

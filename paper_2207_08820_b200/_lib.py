@@ -175,7 +175,7 @@ def lib() -> ctypes.CDLL:
     L.bs_w4_prepare.restype = i
     L.bs_w4_prepare.argtypes = [vp, vp, vp, i, i, i, i, vp, vp]
     L.bs_w4_gemm_workspace_bytes.restype = sz
-    L.bs_w4_gemm_workspace_bytes.argtypes = [i, i, ll]
+    L.bs_w4_gemm_workspace_bytes.argtypes = [i, i, i, i, ll]
     L.bs_w4_gemm.restype = i
     L.bs_w4_gemm.argtypes = [vp, ll, i, vp, i, i, i, i, i, vp, vp, ll, vp, sz, vp]
     L.bs_w4_moe_workspace_bytes.restype = sz

@@ -469,7 +469,7 @@ PyObject* w4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n)
             y = fresh(shape, x.scalar_type(), x);
         }
         if (M == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(y));
-        const size_t need_ws = bs_w4_gemm_workspace_bytes(M, K, ldx);
+        const size_t need_ws = bs_w4_gemm_workspace_bytes(M, O, K, group, ldx);
         at::Tensor ws;
         if (need_ws) ws = fresh({static_cast<int64_t>(need_ws)}, at::kByte, x);
         void* yp = y.data_ptr();

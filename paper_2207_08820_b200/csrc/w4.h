@@ -50,4 +50,9 @@ struct W4Gemm {
     int* status;                // device status word
 };
 
+// csrc/w4_mma.cu: the product on tcgen05 for many rows of x, which start on 16-byte boundaries.  part: w4_mma_workspace bytes.
+bool w4_mma_wanted(int M, const W4Layout& l);
+size_t w4_mma_workspace(int M, const W4Layout& l, int sms);
+int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t st);
+
 }  // namespace bs

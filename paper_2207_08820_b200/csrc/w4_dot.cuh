@@ -11,17 +11,27 @@
 
 namespace bs {
 
-// The pair of codes in bits 0-3 and 16-19 of `w` as two numbers less the zero point, exact: 128 + code (bf16) or 1024 + code (fp16) is the
-// code under a fixed exponent, and the difference to 128 + zero or 1024 + zero is a whole number of at most four bits and a sign.
+// The eight codes of a word as four pairs of numbers less the zero point, exact: 128 + code (bf16) or 1024 + code (fp16) is the code under a fixed
+// exponent, and the difference to 128 + zero or 1024 + zero is a whole number of at most four bits and a sign.  Logic and shifts go through a pipe of half
+// rate, which bounds these kernels: the pairs that are not in place are moved by the upper half of a product, which takes another pipe (bf16), or
+// stay in place four bits up, as 1024 + 16 code, where the mantissa has room for them (fp16).
 template <bool F16> struct W4Type;
 template <> struct W4Type<false> {
     typedef __nv_bfloat16 T;
     static constexpr uint32_t BASE = 0x43004300u;
-    static __device__ __forceinline__ uint32_t centre(uint32_t w, uint32_t zero)
+    // z: the zero point in both halves
+    static __device__ __forceinline__ void pairs(uint32_t w, uint32_t z, uint32_t (&v)[4])
     {
-        const uint32_t v = (w & 0x000f000fu) | BASE;
-        const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&v), *reinterpret_cast<const __nv_bfloat162*>(&zero));
-        return *reinterpret_cast<const uint32_t*>(&d);
+        uint32_t u[4] = {(w & 0x000f000fu) | BASE, 0, 0, 0};
+        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[1]) : "r"(w & 0x00f000f0u), "r"(1u << 28), "r"(BASE));
+        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[2]) : "r"(w & 0x0f000f00u), "r"(1u << 24), "r"(BASE));
+        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[3]) : "r"(w & 0xf000f000u), "r"(1u << 20), "r"(BASE));
+        const uint32_t zero = BASE + z;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u[i]), *reinterpret_cast<const __nv_bfloat162*>(&zero));
+            v[i] = *reinterpret_cast<const uint32_t*>(&d);
+        }
     }
     static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
@@ -35,11 +45,17 @@ template <> struct W4Type<false> {
 template <> struct W4Type<true> {
     typedef __half T;
     static constexpr uint32_t BASE = 0x64006400u;
-    static __device__ __forceinline__ uint32_t centre(uint32_t w, uint32_t zero)
+    static __device__ __forceinline__ void pairs(uint32_t w, uint32_t z, uint32_t (&v)[4])
     {
-        const uint32_t v = (w & 0x000f000fu) | BASE;
-        const __half2 d = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&zero));
-        return *reinterpret_cast<const uint32_t*>(&d);
+        const uint32_t u[4] = {(w & 0x000f000fu) | BASE, (w & 0x00f000f0u) | BASE, (w >> 8 & 0x000f000fu) | BASE, (w >> 8 & 0x00f000f0u) | BASE};
+        const uint32_t zero = BASE + z, low = 0xd400d400u + 16 * z, sixteenth = 0x2c002c00u;        // low: -(64 + zero)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __half2 h = *reinterpret_cast<const __half2*>(&u[i]);
+            const __half2 d = i & 1 ? __hfma2(h, *reinterpret_cast<const __half2*>(&sixteenth), *reinterpret_cast<const __half2*>(&low))
+                                    : __hsub2(h, *reinterpret_cast<const __half2*>(&zero));
+            v[i] = *reinterpret_cast<const uint32_t*>(&d);
+        }
     }
     static __device__ __forceinline__ float lo(uint32_t v) { return __low2float(*reinterpret_cast<const __half2*>(&v)); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __high2float(*reinterpret_cast<const __half2*>(&v)); }
@@ -73,13 +89,14 @@ struct W4Tile {
 template <int NG, bool ZEROS, int RT, int STAGES>
 struct W4Ring {
     static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * RT * BLOCK;
-    uint32_t base, bars;        // the barriers' memory holds nothing else: only an invalidated one may be written over
-    int in, out;                // stages that are filled and read next
-    unsigned phase, limit;      // parity of the round of `out`; polls of a wait, 1 after one has run out
+    uint32_t bars;              // the barriers' memory holds nothing else: only an invalidated one may be written over
+    uint32_t base, mine;        // the stages; the lane's codes in the first one
+    unsigned limit;             // polls of a wait, 1 after one has run out
 
-    __device__ __forceinline__ W4Ring(unsigned char* smem, uint64_t (&bar)[STAGES], int warp, int lane) : in(0), out(0), phase(0), limit(1u << 20)
+    __device__ __forceinline__ W4Ring(unsigned char* smem, uint64_t (&bar)[STAGES], int warp, int lane) : limit(1u << 20)
     {
         base = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * BYTES;
+        mine = base + (lane & 3) * 256 + ((lane >> 2) ^ 2 * (lane & 3)) * 16;
         bars = static_cast<uint32_t>(__cvta_generic_to_shared(bar));
         if (lane == 0) {
 #pragma unroll
@@ -88,45 +105,140 @@ struct W4Ring {
         }
         __syncwarp();
     }
-    // Fills the next stage with the blocks at p; every lane has read what it held.
-    __device__ __forceinline__ void put(const unsigned char* const (&p)[RT], int lane)
+    // Fills a stage with the blocks at p; every lane has read what it held.
+    __device__ __forceinline__ void put(int stage, const unsigned char* const (&p)[RT], int lane) const
     {
         if (lane == 0) {
-            const uint32_t bar = bars + 8 * in;
+            const uint32_t bar = bars + 8 * stage;
             asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(RT * BLOCK) : "memory");
 #pragma unroll
             for (int r = 0; r < RT; ++r)
                 asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(base + (in * RT + r) * BLOCK), "l"(p[r]), "n"(BLOCK), "r"(bar) : "memory");
+                             ::"r"(base + (stage * RT + r) * BLOCK), "l"(p[r]), "n"(BLOCK), "r"(bar) : "memory");
         }
-        in = in + 1 == STAGES ? 0 : in + 1;
     }
-    // The blocks of the next stage that was filled.  A wait that runs out sets the status word; later ones then poll once.
-    __device__ __forceinline__ void get(W4Tile<NG, ZEROS> (&w)[RT], int lane, int* status)
+    // The blocks of a stage, in its round of parity `phase`.  A wait that runs out sets the status word; later ones then poll once.
+    __device__ __forceinline__ void get(int stage, unsigned phase, W4Tile<NG, ZEROS> (&w)[RT], int lane, int* status)
     {
-        const uint32_t bar = bars + 8 * out;
         unsigned ok = 0;
         for (unsigned it = 0; it < limit && !ok; ++it)
-            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(phase) : "memory");
+            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bars + 8 * stage), "r"(phase) : "memory");
         if (!ok) {
             if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
             limit = 1;
         }
         __syncwarp();
-        const int r8 = lane >> 2, t = lane & 3;
+        const uint32_t entry = base + W4_CODES + (lane >> 2) * ENTRY;
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const uint32_t block = base + (out * RT + r) * BLOCK, at = block + t * 256 + (r8 ^ 2 * t) * 16;
+            const uint32_t at = mine + (stage * RT + r) * BLOCK;
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].a.x), "=r"(w[r].a.y), "=r"(w[r].a.z), "=r"(w[r].a.w) : "r"(at) : "memory");
             asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].b.x), "=r"(w[r].b.y), "=r"(w[r].b.z), "=r"(w[r].b.w) : "r"(at + 128) : "memory");
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                const uint32_t step = block + W4_CODES + (g * 8 + r8) * ENTRY;
+                const uint32_t step = entry + (stage * RT + r) * BLOCK + g * 8 * ENTRY;
                 if (ZEROS) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[r].scale[g]), "=r"(w[r].zero[g]) : "r"(step) : "memory");
                 else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[r].scale[g]) : "r"(step) : "memory");
             }
         }
-        if (++out == STAGES) { out = 0; phase ^= 1; }
+    }
+};
+
+// The same for a CTA: a stage holds, for each of NB matrices, WARPS blocks, one a warp.  The `split` warps of a team share the reduction of 16 rows, WARPS /
+// split teams take neighbouring rows; a team's blocks of a stage are neighbours in memory and one copy.  One thread fills stages ahead of the warps that
+// read them: copies of 8 KB in flight reach 5.7 TB/s, where a hundred of 1 KB an SM reach 3 (measured, 104 MB).
+template <int NG, bool ZEROS, int NB, int WARPS, int STAGES>
+struct W4TeamRing {
+    static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * NB * WARPS * BLOCK;
+    static constexpr int STAGE = NB * WARPS * BLOCK;
+    uint32_t base, bar;         // stages; barriers [full, empty][STAGES], whose memory holds nothing else: only an invalidated one may be written over
+    uint32_t at, step;          // of the current stage: the warp's first block, as its lane reads codes and steps
+    int stage;
+    unsigned phase, limit;      // parity of the round; polls of a wait, 1 after one has run out
+
+    // bars: [2 STAGES].  All threads of the CTA.
+    __device__ __forceinline__ W4TeamRing(unsigned char* smem, uint64_t* bars, int warp, int lane) : stage(0), phase(0), limit(1u << 20)
+    {
+        base = static_cast<uint32_t>(__cvta_generic_to_shared(smem));
+        bar = static_cast<uint32_t>(__cvta_generic_to_shared(bars));
+        at = base + warp * BLOCK + (lane & 3) * 256 + ((lane >> 2) ^ 2 * (lane & 3)) * 16;
+        step = base + warp * BLOCK + W4_CODES + (lane >> 2) * ENTRY;
+        if (threadIdx.x == 0) {
+            for (int s = 0; s < STAGES; ++s) {
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
+                asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + 8 * (STAGES + s)), "r"(WARPS) : "memory");
+            }
+            asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ void next()
+    {
+        ++stage;
+        bar += 8;
+        at += STAGE;
+        step += STAGE;
+        if (stage == STAGES) {
+            stage = 0;
+            bar -= 8 * STAGES;
+            at -= STAGES * STAGE;
+            step -= STAGES * STAGE;
+            phase ^= 1;
+        }
+    }
+    // Bounded wait; one that runs out sets the status word, later ones then poll once.
+    __device__ __forceinline__ void wait(uint32_t on, unsigned parity, int* status)
+    {
+        unsigned left;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mov.u32 %0, %3;\n\t"
+            "W4_WAIT:\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "@p bra W4_DONE;\n\t"
+            "sub.u32 %0, %0, 1;\n\t"
+            "setp.ne.u32 p, %0, 0;\n\t"
+            "@p bra W4_WAIT;\n\t"
+            "W4_DONE:\n\t}"
+            : "=&r"(left) : "r"(on), "r"(parity), "r"(limit) : "memory");
+        if (left == 0) {
+            if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
+            limit = 1;
+        }
+    }
+    // The producer's thread: the stage is free; so many blocks are announced.  copy() starts their copies, next() goes on.
+    __device__ __forceinline__ void open(int blocks, int* status)
+    {
+        wait(bar + 8 * STAGES, phase ^ 1, status);
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(blocks * BLOCK) : "memory");
+    }
+    // `blocks` neighbouring blocks at p to the places of matrix m from warp `first` on.
+    __device__ __forceinline__ void copy(int m, int first, const unsigned char* p, int blocks) const
+    {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                     ::"r"(base + stage * STAGE + (m * WARPS + first) * BLOCK), "l"(p), "r"(blocks * BLOCK), "r"(bar) : "memory");
+    }
+    // The warps: the stage has landed; a warp's blocks of it; the warp has what it needs.
+    __device__ __forceinline__ void landed(int* status) { wait(bar, phase, status); }
+    __device__ __forceinline__ void take(W4Tile<NG, ZEROS> (&w)[NB]) const
+    {
+#pragma unroll
+        for (int m = 0; m < NB; ++m) {
+            const uint32_t c = at + m * WARPS * BLOCK;
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[m].a.x), "=r"(w[m].a.y), "=r"(w[m].a.z), "=r"(w[m].a.w) : "r"(c) : "memory");
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[m].b.x), "=r"(w[m].b.y), "=r"(w[m].b.z), "=r"(w[m].b.w) : "r"(c + 128) : "memory");
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                const uint32_t e = step + m * WARPS * BLOCK + g * 8 * ENTRY;
+                if (ZEROS) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[m].scale[g]), "=r"(w[m].zero[g]) : "r"(e) : "memory");
+                else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[m].scale[g]) : "r"(e) : "memory");
+            }
+        }
+    }
+    __device__ __forceinline__ void release(int lane) const
+    {
+        __syncwarp();
+        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar + 8 * STAGES) : "memory");
     }
 };
 
@@ -147,24 +259,24 @@ __device__ __forceinline__ void w4_blocks(const W4Tile<NG, ZEROS> (&w)[RT], cons
             for (int n = 0; n < NT; ++n) v[t][n] = x(n, j, t);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            uint32_t z0 = Ty::BASE + 0x00080008u, z1 = z0;
+            uint32_t z0 = 0x00080008u, z1 = z0;
             if (ZEROS) {
-                z0 = Ty::BASE + __byte_perm(w[r].zero[g], 0, 0x1010);
-                z1 = Ty::BASE + __byte_perm(w[r].zero[g], 0, 0x3232);
+                z0 = __byte_perm(w[r].zero[g], 0, 0x1010);
+                z1 = __byte_perm(w[r].zero[g], 0, 0x3232);
             }
             if (j % (4 / NG) == 0) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) acc[r][n][0] = acc[r][n][1] = acc[r][n][2] = acc[r][n][3] = 0.f;
             }
-            const uint32_t a = word_of(w[r].a, j), b = word_of(w[r].b, j);
-            const uint32_t a0 = Ty::centre(a, z0), a1 = Ty::centre(a >> 4, z0), a2 = Ty::centre(a >> 8, z0), a3 = Ty::centre(a >> 12, z0);
-            const uint32_t b0 = Ty::centre(b, z1), b1 = Ty::centre(b >> 4, z1), b2 = Ty::centre(b >> 8, z1), b3 = Ty::centre(b >> 12, z1);
+            uint32_t a[4], b[4];
+            Ty::pairs(word_of(w[r].a, j), z0, a);
+            Ty::pairs(word_of(w[r].b, j), z1, b);
 #pragma unroll
             for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    Ty::mma(acc[r][n], a0, b0, a1, b1, v[t][n].x, v[t][n].y);
-                    Ty::mma(acc[r][n], a2, b2, a3, b3, v[t][n].z, v[t][n].w);
+                    Ty::mma(acc[r][n], a[0], b[0], a[1], b[1], v[t][n].x, v[t][n].y);
+                    Ty::mma(acc[r][n], a[2], b[2], a[3], b[3], v[t][n].z, v[t][n].w);
                 }
             if ((j + 1) % (4 / NG) == 0) {      // the group's sums are scaled in 32 bits
                 const float s0 = W4Type<S16>::lo(w[r].scale[g]), s1 = W4Type<S16>::hi(w[r].scale[g]);
@@ -191,17 +303,18 @@ __device__ __forceinline__ uint4 load_x(const T* row, int k0, int K)
     return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 
-// The lane's columns of block cb of a row: v[j] for word j.  `full`: the whole block lies before K.
+// The lane's columns of block cb of a row, whose address includes the lane's first column: v[j] for word j.  `full`: the whole block lies before K.
 template <typename T>
 __device__ __forceinline__ void load_block_x(uint4 (&v)[4], const T* row, int cb, int K, bool full, int lane)
 {
-    const int k0 = cb * W4_COLS + 8 * (lane & 3);
+    row += cb * W4_COLS;
     if (full) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __ldg(reinterpret_cast<const uint4*>(row + k0 + 32 * j));
+        for (int j = 0; j < 4; ++j) v[j] = __ldg(reinterpret_cast<const uint4*>(row + 32 * j));
     } else {
+        const int left = K - cb * W4_COLS - 8 * (lane & 3);     // columns from the lane's first one on; none at all behind the last block
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = load_x(row, k0 + 32 * j, K);
+        for (int j = 0; j < 4; ++j) v[j] = load_x(row, 32 * j, left);
     }
 }
 

@@ -2,80 +2,84 @@
 //
 // Few rows of x: bound by the weights' bytes.  w4_gemm_kernel streams them through shared memory, every warp a part of the reduction of 16 rows, and
 // multiplies with mma.sync (w4_dot.cuh), where eight rows of x cost what one does; products are exact, sums of a group in 32 bits, scaled in
-// 32 bits, and rounded once.
-#include <cstdlib>
-
+// 32 bits, and rounded once.  More rows: csrc/w4_mma.cu.
 #include "w4_dot.cuh"
 
 namespace bs {
 namespace {
 
-constexpr int MOST_WARPS = 16;
+constexpr int WARPS = 8, STAGES = 6;
 
-// A CTA owns 16 RT rows of the weights and 8 NT rows of x; its warps take the blocks of the reduction in turn.
-template <bool F16, int NG, bool ZEROS, int NT, int RT, int STAGES>
-__global__ void __launch_bounds__(MOST_WARPS * 32, 1) w4_gemm_kernel(const __grid_constant__ W4Gemm g)
+// An item is 16 rows of the weights for each of WARPS / split teams and 8 NT rows of x; a team's warps take the blocks of the reduction in turn.  A CTA goes
+// through several items; the last warp copies their blocks ahead, also while the sums of an item are put together.
+template <int NT> constexpr int ctas_of() { return NT == 1 ? 3 : 2; }      // per SM
+template <bool F16, int NG, bool ZEROS, int NT>
+__global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel(const __grid_constant__ W4Gemm g, int split)
 {
     typedef typename W4Type<F16>::T T;
-    typedef W4Ring<NG, ZEROS, RT, STAGES> Ring;
-    constexpr int M = NT * 8, R = RT * W4_ROWS, PITCH = R + 1;
-    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps; in the end their sums, [warps][M][PITCH] floats
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, rb0 = blockIdx.x * RT, m0 = blockIdx.y * M;
-    __shared__ uint64_t bars[MOST_WARPS][STAGES];
-    Ring ring(smem, bars[warp], warp, lane);
-    const unsigned char* from[RT];
+    constexpr int M = NT * 8;
+    typedef W4TeamRing<NG, ZEROS, 1, WARPS, STAGES> Ring;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t bars[2 * STAGES];
+    __shared__ float part[WARPS][M][17];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m0 = blockIdx.y * M;
+    const int teams = WARPS / split, team = warp / split, k0 = warp % split;
+    Ring ring(smem, bars, warp, lane);
     const unsigned char* matrix = dependent_begin(g.w);
+    if (warp == WARPS) {
+        if (lane == 0)
+            for (int rb0 = blockIdx.x * teams; rb0 < g.l.rbs; rb0 += gridDim.x * teams) {
+                const int have = min(teams, g.l.rbs - rb0);
+                for (int c = 0; c < g.l.cbs; c += split) {
+                    const int n = min(split, g.l.cbs - c);
+                    ring.open(have * n, g.status);
+                    for (int r = 0; r < have; ++r) ring.copy(0, r * split, matrix + (static_cast<size_t>(rb0 + r) * g.l.cbs + c) * Ring::BLOCK, n);
+                    ring.next();
+                }
+            }
+        return;
+    }
     const T* x0 = behind_wait<T>(g.x);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) from[r] = matrix + (static_cast<size_t>(min(rb0 + r, g.l.rbs - 1)) * g.l.cbs + warp) * Ring::BLOCK;
-    int left = (g.l.cbs - warp + warps - 1) / warps;       // blocks that this warp has still to fetch
-    auto put = [&] {
-        if (left > 0) {
-            ring.put(from, lane);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) from[r] += warps * Ring::BLOCK;
-            --left;
-        }
-    };
-#pragma unroll 1
-    for (int s = 0; s < STAGES - 1; ++s) put();
     const T* row[NT];       // lanes without a row of x compute the last one's again
 #pragma unroll
-    for (int n = 0; n < NT; ++n) row[n] = x0 + min(m0 + n * 8 + (lane >> 2), g.M - 1) * g.ldx;
-    float tot[RT][NT][4];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) tot[r][n][0] = tot[r][n][1] = tot[r][n][2] = tot[r][n][3] = 0.f;
+    for (int n = 0; n < NT; ++n) row[n] = x0 + min(m0 + n * 8 + (lane >> 2), g.M - 1) * g.ldx + 8 * (lane & 3);
     const int full = g.l.K / W4_COLS;
-    for (int cb = warp; cb < g.l.cbs; cb += warps) {
-        uint4 x[NT][4];
+    for (int rb0 = blockIdx.x * teams; rb0 < g.l.rbs; rb0 += gridDim.x * teams) {
+        const int rb = rb0 + team;
+        float tot[1][NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) load_block_x(x[n], row[n], cb, g.l.K, cb < full, lane);
-        W4Tile<NG, ZEROS> w[RT];
-        ring.get(w, lane, g.status);
-        put();      // into the stage before this one: its blocks have been multiplied
-        w4_blocks<F16, F16, 1>(w, [&](int n, int j, int) { return x[n][j]; }, tot);
-    }
-    __syncthreads();
-    float* part = reinterpret_cast<float*>(smem);
-    float* mine = part + warp * M * PITCH;
+        for (int n = 0; n < NT; ++n) tot[0][n][0] = tot[0][n][1] = tot[0][n][2] = tot[0][n][3] = 0.f;
+        // teams without rows multiply what the stages hold, and drop it
+        for (int c = k0; c < g.l.cbs + k0; c += split) {
+            uint4 x[NT][4];
+            if (c < g.l.cbs) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(n * 8 + 2 * (lane & 3) + (i & 1)) * PITCH + r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)] = tot[r][n][i];
+                for (int n = 0; n < NT; ++n) load_block_x(x[n], row[n], c, g.l.K, c < full, lane);
+            }
+            ring.landed(g.status);
+            if (c < g.l.cbs) {
+                W4Tile<NG, ZEROS> w[1];
+                ring.take(w);
+                w4_blocks<F16, F16, 1>(w, [&](int n, int j, int) { return x[n][j]; }, tot);
+            }
+            ring.release(lane);
+            ring.next();
         }
-    __syncthreads();
-    // the warps' parts are added in their order: the same bits every time
-    for (int i = threadIdx.x; i < M * R; i += blockDim.x) {
-        const int m = i / R, r = i % R, o = rb0 * W4_ROWS + r;
-        if (m0 + m >= g.M || o >= g.l.O) continue;
-        float v = 0.f;
-        for (int k = 0; k < warps; ++k) v += part[(k * M + m) * PITCH + r];
-        if (g.bias) v += static_cast<float>(static_cast<const T*>(g.bias)[o]);
-        static_cast<T*>(g.y)[(m0 + m) * g.ldy + o] = W4Type<F16>::round(v);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[warp][n * 8 + 2 * (lane & 3) + (i & 1)][(lane >> 2) + 8 * (i >> 1)] = tot[0][n][i];
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
+        // the warps' parts are added in their order: the same bits every time
+        for (int i = k0 * 32 + lane; i < M * 16; i += split * 32) {
+            const int m = i >> 4, r = i & 15, o = rb * W4_ROWS + r;
+            if (m0 + m >= g.M || o >= g.l.O) continue;
+            float v = 0.f;
+            for (int k = 0; k < split; ++k) v += part[team * split + k][m][r];
+            if (g.bias) v += static_cast<float>(static_cast<const T*>(g.bias)[o]);
+            static_cast<T*>(g.y)[(m0 + m) * g.ldy + o] = W4Type<F16>::round(v);
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
     }
 }
 
@@ -94,43 +98,29 @@ __global__ void __launch_bounds__(256) w4_align_rows_kernel(const uint16_t* x, l
     }
 }
 
-template <bool F16, int NG, bool ZEROS, int NT, int RT, int STAGES>
+template <bool F16, int NG, bool ZEROS, int NT>
 int launch_tile(const W4Gemm& g, int sms, cudaStream_t st)
 {
-    auto kernel = w4_gemm_kernel<F16, NG, ZEROS, NT, RT, STAGES>;
-    const int items = ceil_div(g.l.rbs, RT), tiles = ceil_div(g.M, 8 * NT);
-    // enough warps for 16 an SM, each with two blocks of the reduction at least
-    int warps = MOST_WARPS;
-    while (warps > 1 && (2 * warps > g.l.cbs + 1 || static_cast<long long>(items) * tiles * warps / 2 >= 16ll * sms)) warps /= 2;
-#ifdef BS_TUNING
-    if (const char* e = getenv("BS_W4_WARPS")) warps = atoi(e);
-#endif
-    const int ring = warps * W4Ring<NG, ZEROS, RT, STAGES>::BYTES, part = static_cast<int>(sizeof(float)) * warps * NT * 8 * (RT * W4_ROWS + 1);
-    const int smem = ring > part ? ring : part;
+    auto kernel = w4_gemm_kernel<F16, NG, ZEROS, NT>;
+    constexpr int smem = W4TeamRing<NG, ZEROS, 1, WARPS, STAGES>::BYTES;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    return launch_dependent(kernel, dim3(items, tiles), dim3(warps * 32), smem, st, g);
+    // teams are as wide as the reduction has blocks
+    int split = WARPS;
+    while (split > 1 && split / 2 >= g.l.cbs) split /= 2;
+    const int items = ceil_div(g.l.rbs, WARPS / split), tiles = ceil_div(g.M, 8 * NT), places = ctas_of<NT>() * sms;
+    return launch_dependent(kernel, dim3(items < places ? items : places, tiles), dim3(WARPS * 32 + 32), smem, st, g, split);
 }
 template <bool F16, int NG, bool ZEROS>
-int launch_rows(const W4Gemm& g, int sms, cudaStream_t st)
+int launch_tiles(const W4Gemm& g, int sms, cudaStream_t st)
 {
-#ifdef BS_TUNING
-    if (const char* e = getenv("BS_W4_RT")) {
-        const int rt = atoi(e);
-        if (g.M <= 8) return rt == 1 ? launch_tile<F16, NG, ZEROS, 1, 1, 8>(g, sms, st) : launch_tile<F16, NG, ZEROS, 1, 2, 6>(g, sms, st);
-        if (g.M <= 16) return rt == 1 ? launch_tile<F16, NG, ZEROS, 2, 1, 8>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2, 2, 4>(g, sms, st);
-        return rt == 1 ? launch_tile<F16, NG, ZEROS, 4, 1, 4>(g, sms, st) : launch_tile<F16, NG, ZEROS, 4, 2, 4>(g, sms, st);
-    }
-#endif
-    if (g.M <= 8) return launch_tile<F16, NG, ZEROS, 1, 2, 4>(g, sms, st);
-    if (g.M <= 16) return launch_tile<F16, NG, ZEROS, 2, 2, 4>(g, sms, st);
-    return launch_tile<F16, NG, ZEROS, 4, 2, 4>(g, sms, st);
+    return g.M <= 8 ? launch_tile<F16, NG, ZEROS, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2>(g, sms, st);
 }
 template <bool F16>
 int launch(const W4Gemm& g, int sms, cudaStream_t st)
 {
     const int ng = g.l.group == 32 ? 4 : g.l.group == 64 ? 2 : 1;
-    if (g.l.zeros) return ng == 4 ? launch_rows<F16, 4, true>(g, sms, st) : ng == 2 ? launch_rows<F16, 2, true>(g, sms, st) : launch_rows<F16, 1, true>(g, sms, st);
-    return ng == 4 ? launch_rows<F16, 4, false>(g, sms, st) : ng == 2 ? launch_rows<F16, 2, false>(g, sms, st) : launch_rows<F16, 1, false>(g, sms, st);
+    if (g.l.zeros) return ng == 4 ? launch_tiles<F16, 4, true>(g, sms, st) : ng == 2 ? launch_tiles<F16, 2, true>(g, sms, st) : launch_tiles<F16, 1, true>(g, sms, st);
+    return ng == 4 ? launch_tiles<F16, 4, false>(g, sms, st) : ng == 2 ? launch_tiles<F16, 2, false>(g, sms, st) : launch_tiles<F16, 1, false>(g, sms, st);
 }
 
 bool rows_aligned(int M, long long ldx) { return M == 1 || ldx % 8 == 0; }
@@ -138,10 +128,23 @@ bool rows_aligned(int M, long long ldx) { return M == 1 || ldx % 8 == 0; }
 }  // namespace
 }  // namespace bs
 
-extern "C" size_t bs_w4_gemm_workspace_bytes(int M, int K, long long ldx)
+namespace bs {
+namespace {
+size_t aligned_bytes(int M, int K, long long ldx) { return rows_aligned(M, ldx) ? 0 : static_cast<size_t>(M) * ((static_cast<size_t>(K) + 7) & ~static_cast<size_t>(7)) * 2; }
+int sm_count()
 {
-    if (M <= 0 || K <= 0 || bs::rows_aligned(M, ldx)) return 0;
-    return static_cast<size_t>(M) * ((static_cast<size_t>(K) + 7) & ~static_cast<size_t>(7)) * 2;
+    const int sms = device_sm_count();
+    return sms > 0 ? sms : 148;     // a query without a device plans for a full B200
+}
+}  // namespace
+}  // namespace bs
+
+extern "C" size_t bs_w4_gemm_workspace_bytes(int M, int O, int K, int group, long long ldx)
+{
+    using namespace bs;
+    W4Layout l;
+    if (M <= 0 || M > W4_MAX_DIM || !w4_layout(O, K, group, 0, l)) return 0;
+    return aligned_bytes(M, K, ldx) + (w4_mma_wanted(M, l) ? w4_mma_workspace(M, l, sm_count()) : 0);
 }
 
 extern "C" int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K, int group, int zeros, bs_float_t type, const void* bias, void* y,
@@ -155,18 +158,22 @@ extern "C" int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, in
     if (M == 0) return BS_OK;
     g.x = x; g.w = static_cast<const unsigned char*>(w); g.bias = bias; g.y = y; g.ldx = ldx; g.ldy = ldy; g.M = M;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (!rows_aligned(M, ldx) && (!workspace || workspace_bytes < bs_w4_gemm_workspace_bytes(M, K, ldx))) return BS_ERR_INVALID_ARG;
+    const size_t need = bs_w4_gemm_workspace_bytes(M, O, K, group, ldx);
+    if (need && (!workspace || workspace_bytes < need)) return BS_ERR_INVALID_ARG;
     const int sms = device_sm_count();
     g.status = status_device_ptr();
     if (sms <= 0 || !g.status) return BS_ERR_CUDA;
+    unsigned char* ws = static_cast<unsigned char*>(workspace);
     if (!rows_aligned(M, ldx)) {
         const int ldo = (K + 7) & ~7;
         const long long want = (static_cast<long long>(M) * (ldo / 8) + 255) / 256, most = static_cast<long long>(sms) * 8;
         const int rc = launch_dependent(w4_align_rows_kernel, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(256), 0, st,
-                                        static_cast<const uint16_t*>(x), ldx, M, K, static_cast<uint16_t*>(workspace), ldo);
+                                        static_cast<const uint16_t*>(x), ldx, M, K, reinterpret_cast<uint16_t*>(ws), ldo);
         if (rc != BS_OK) return rc;
-        g.x = workspace;
+        g.x = ws;
         g.ldx = ldo;
+        ws += aligned_bytes(M, K, ldx);
     }
+    if (w4_mma_wanted(M, g.l)) return w4_mma_launch(g, type == BS_F16, reinterpret_cast<float*>(ws), sms, st);
     return type == BS_F16 ? launch<true>(g, sms, st) : launch<false>(g, sms, st);
 }

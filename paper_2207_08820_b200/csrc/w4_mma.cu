@@ -1,0 +1,499 @@
+// Product of many rows of x with 4-bit weights on tcgen05.mma: the weights are the A operand, 128 rows a tile, expanded to 16 bits in tensor memory; x is B.
+//
+// The codes less their zero points are exact in 16 bits and the scales are not folded into them: a group's sums of exact products come out of the tensor
+// core in an accumulator of their own, and warps with the running totals in registers take them over, scaled in 32 bits, while the next group is
+// multiplied.  Folding the scale in would round every weight and double the error of the result.
+//
+// Roles of a CTA, one per SM: tensor copies of x (128 columns a stage), bulk copies of weight blocks, MMA issue, warps that expand a row a thread into
+// tensor memory (two buffers of 128 columns), warps that scale and add (two accumulators).
+//
+// Work: tiles of 128 rows by up to 128 rows of x.  A CTA takes whole tiles, neighbours at a time, as long as every CTA gets one; what is left, less than
+// two tiles a CTA, is cut into equal runs of (tile, 128 columns), and a small kernel adds the parts of the tiles that were cut, in their order.
+#include <cuda.h>
+
+#include <mutex>
+
+#include "mma_kernel.cuh"
+#include "w4_dot.cuh"
+
+namespace bs {
+namespace {
+
+constexpr int ROWS = 128, BLOCKS = ROWS / W4_ROWS;      // of a tile
+constexpr int X_STAGES = 4, SCALE_SLOTS = 16;
+
+struct MmaTiles {
+    W4Gemm g;
+    int n;                      // rows of x in a tile, a multiple of 32
+    int mts, ots;               // tiles of x's rows and of the weights' rows
+    int waves;                  // whole tiles of every CTA
+    int per;                    // steps of 128 columns in a run
+    int ctas;
+    float* part;                // [2 ctas][n][ROWS]: the parts of the tiles that a run begins and ends in
+    int group_blocks;           // blocks of columns in a group (1 where a block holds several groups)
+};
+
+// Tile t: eight tiles of x's rows side by side, then the weights' next rows, so that what runs at the same time shares both.
+__device__ __forceinline__ void tile_place(const MmaTiles& a, int t, int& mt, int& ot)
+{
+    const int wide = 8 * a.ots, group = t / wide, in = t - group * wide, rows = min(8, a.mts - group * 8);
+    ot = in / rows;
+    mt = group * 8 + in - ot * rows;
+}
+// A CTA's stretches of work, one after the other: steps [c0, c1) of a tile.
+struct Stretch {
+    int wave, pos, end;         // whole tiles done; steps of the run
+    int tile, c0, c1, part;     // part: where a part of a tile goes, -1: the whole tile is here
+    __device__ __forceinline__ Stretch(const MmaTiles& a) : wave(0)
+    {
+        const long long steps = static_cast<long long>(a.mts) * a.ots * a.g.l.cbs - static_cast<long long>(a.waves) * a.ctas * a.g.l.cbs;
+        const long long b = static_cast<long long>(blockIdx.x) * a.per;
+        pos = static_cast<int>(b < steps ? b : steps);
+        end = static_cast<int>(b + a.per < steps ? b + a.per : steps);
+        first = pos;
+    }
+    __device__ __forceinline__ bool next(const MmaTiles& a)
+    {
+        const int cbs = a.g.l.cbs;
+        if (wave < a.waves) {
+            tile = wave++ * a.ctas + blockIdx.x;
+            c0 = 0; c1 = cbs; part = -1;
+            return true;
+        }
+        if (pos >= end) return false;
+        tile = pos / cbs;
+        c0 = pos - tile * cbs;
+        c1 = min(cbs, c0 + end - pos);
+        // a run begins in one tile and ends in another: two places; a tile that both begins before and ends behind the run has the first
+        part = c0 == 0 && c1 == cbs ? -1 : 2 * blockIdx.x + (pos != first);
+        pos += c1 - c0;
+        tile += a.waves * a.ctas;
+        return true;
+    }
+    int first;
+};
+
+__device__ __forceinline__ void w4_st32(uint32_t taddr, const uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+// D[128 x n] (+)= A (tensor memory) B (shared memory), 16 columns of the reduction.
+__device__ __forceinline__ void w4_mma(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc)
+{
+    if (mm_elect())
+        asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"((static_cast<uint64_t>(b_hi) << 32) | b_lo), "r"(idesc), "r"(acc) : "memory");
+}
+
+// A position in a ring of stages, and the parity of its round.
+template <int N>
+struct Turn {
+    int at;
+    unsigned phase;
+    __device__ __forceinline__ Turn() : at(0), phase(0) {}
+    __device__ __forceinline__ void next() { if (++at == N) { at = 0; phase ^= 1; } }
+};
+
+// FEW: up to 64 rows of x, bound by the weights: eight warps expand, four scale.  Otherwise four and eight.
+template <bool FEW> struct Roles {
+    static constexpr int EXPAND = FEW ? 8 : 4, SCALE = FEW ? 4 : 8, WARPS = 4 + EXPAND + SCALE, W_STAGES = FEW ? 8 : 4;
+    static constexpr int N = FEW ? 64 : 128;                    // most rows of x in a tile
+    static constexpr int COLUMNS = FEW ? 256 : 512;             // of tensor memory: two accumulators of N, two A buffers of 64
+    static constexpr int PIECES = N * 4 / SCALE / 16;           // 16 columns each, of a thread's totals
+};
+
+template <bool F16, int NG, bool ZEROS, bool FEW>
+__global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ MmaTiles a)
+{
+    typedef W4Type<F16> Ty;
+    typedef typename Ty::T T;
+    typedef Roles<FEW> Ro;
+    constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, WS = Ro::W_STAGES;
+    extern __shared__ unsigned char raw[];
+    // x [X_STAGES][2][n][128 bytes], swizzled by address: from a multiple of 1024 on; weights [WS][BLOCKS][BLOCK]
+    unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
+    __shared__ uint64_t x_full[X_STAGES], x_empty[X_STAGES], w_full[WS], w_empty[WS], a_full[2], a_empty[2], d_full[2], d_empty[2];
+    __shared__ float scales[SCALE_SLOTS][ROWS];
+    __shared__ uint32_t tmem_slot;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const W4Layout& l = a.g.l;
+    unsigned char* wsm = smem + static_cast<size_t>(X_STAGES) * a.n * 256;
+    if (warp == 3) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(Ro::COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        mm_fence_before();
+    } else if (warp == 0 && lane == 0) {
+        for (int s = 0; s < X_STAGES; ++s) { mbar_init(&x_full[s], 1); mbar_init(&x_empty[s], 1); }
+        for (int s = 0; s < WS; ++s) { mbar_init(&w_full[s], 1); mbar_init(&w_empty[s], 4); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&a_full[s], 4); mbar_init(&a_empty[s], 1); mbar_init(&d_full[s], 1); mbar_init(&d_empty[s], Ro::SCALE); }
+        fence_barrier_init();
+        fence_proxy_async();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tx)) : "memory");
+    }
+    __syncthreads();
+    mm_fence_after();
+    const uint32_t tmem = tmem_slot, tmem_a = tmem + 2 * Ro::N;
+    const unsigned char* matrix = dependent_begin(a.g.w);
+    bool late = false;          // a wait ran out: later ones are not waited for
+    auto wait = [&](uint64_t* bar, unsigned parity) {
+        if (!late && !mm_wait(bar, parity)) {
+            late = true;
+            atomicOr(a.g.status, STATUS_TIMEOUT);
+        }
+    };
+    // The last step of a round: a group's sums are complete, or the stretch ends.
+    auto ends = [&](int c, int c1) { return NG > 1 || c + 1 == c1 || (c + 1) % a.group_blocks == 0; };
+    Stretch s(a);
+    if (warp == 0) {
+        if (lane == 0) {
+            Turn<X_STAGES> x;
+            int issued = 0;
+            while (s.next(a)) {
+                int mt, ot;
+                tile_place(a, s.tile, mt, ot);
+                const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
+                for (int c = s.c0; c < s.c1; ++c) {
+                    wait(&x_empty[x.at], x.phase ^ 1);
+                    unsigned char* to = smem + static_cast<size_t>(x.at) * a.n * 256;
+                    mbar_expect_tx(&x_full[x.at], rows * 256);
+                    for (int h = 0; h < 2; ++h)
+                        for (int r = 0; r < rows; r += 32) tma_load_2d(to + (h * a.n + r) * 128, &tx, &x_full[x.at], c * W4_COLS + h * 64, m0 + r);
+                    x.next();
+                    ++issued;
+                }
+            }
+            for (int i = 0; i < X_STAGES && i < issued; ++i) {      // no copy outlives the CTA
+                x.at = x.at == 0 ? X_STAGES - 1 : x.at - 1;
+                if (x.at == X_STAGES - 1) x.phase ^= 1;
+                wait(&x_full[x.at], x.phase);
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        Turn<X_STAGES> x;
+        Turn<2> ab, d;
+        unsigned limit = 1u << 20;
+        const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
+        // K-major rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group
+        const uint32_t b_hi = 64u | (1u << 14) | (2u << 29);
+        while (s.next(a)) {
+            int mt, ot;
+            tile_place(a, s.tile, mt, ot);
+            const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
+            const uint32_t idesc = (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(rows >> 3) << 17) | (static_cast<uint32_t>(ROWS >> 4) << 24);
+            bool fresh = true;
+            for (int c = s.c0; c < s.c1; ++c) {
+                mm_wait_uniform(&x_full[x.at], x.phase, limit);
+                mm_wait_uniform(&a_full[ab.at], ab.phase, limit);
+                mm_fence_after();
+                const uint32_t xs = base + static_cast<uint32_t>(x.at * a.n * 16), as = tmem_a + ab.at * 64;
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    if (fresh) {
+                        mm_wait_uniform(&d_empty[d.at], d.phase ^ 1, limit);
+                        mm_fence_after();
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8 / NG; ++k) {
+                        const int step = g * (8 / NG) + k;      // 16 columns: 32 bytes of a row, 8 columns of A
+                        const uint32_t b = xs + static_cast<uint32_t>((step >> 2) * a.n * 8 + (step & 3) * 2);
+                        w4_mma(tmem + d.at * Ro::N, as + step * 8, (b & 0x3fff) | (1u << 16), b_hi, idesc, fresh && k == 0 ? 0u : 1u);
+                    }
+                    fresh = ends(c, s.c1);
+                    if (fresh) {
+                        mm_commit(&d_full[d.at]);
+                        d.next();
+                    }
+                }
+                mm_commit(&x_empty[x.at]);
+                mm_commit(&a_empty[ab.at]);
+                x.next();
+                ab.next();
+            }
+        }
+        if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
+    } else if (warp == 2) {
+        Turn<WS> w;
+        int issued = 0;
+        while (s.next(a)) {
+            int mt, ot;
+            tile_place(a, s.tile, mt, ot);
+            const int rb = ot * BLOCKS, have = min(BLOCKS, l.rbs - rb);
+            for (int c = s.c0; c < s.c1; ++c) {
+                wait(&w_empty[w.at], w.phase ^ 1);
+                if (lane == 0) mbar_expect_tx(&w_full[w.at], have * BLOCK);
+                __syncwarp();
+                if (lane < have) mm_bulk(wsm + (w.at * BLOCKS + lane) * BLOCK, matrix + (static_cast<size_t>(rb + lane) * l.cbs + c) * BLOCK, BLOCK, &w_full[w.at]);
+                w.next();
+                ++issued;
+            }
+        }
+        for (int i = 0; i < WS && i < issued; ++i) {
+            w.at = w.at == 0 ? WS - 1 : w.at - 1;
+            if (w.at == WS - 1) w.phase ^= 1;
+            wait(&w_full[w.at], w.phase);
+        }
+        __syncwarp();
+    } else if (warp >= 4 && warp < 4 + Ro::EXPAND) {
+        // a thread owns a row of the tile; with two groups of warps each takes every other step, and a buffer
+        const int team = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, r = row & 15;
+        const uint32_t mine = smem_u32(wsm) + (row >> 4) * BLOCK, lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        Turn<WS> w;
+        Turn<2> ab;
+        int round = 0;
+        while (s.next(a)) {
+            bool fresh = true;
+            for (int c = s.c0; c < s.c1; ++c) {
+                if (!FEW || ab.at == team) {
+                    wait(&w_full[w.at], w.phase);
+                    const uint32_t block = mine + w.at * BLOCKS * BLOCK;
+                    uint4 code[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(code[t].x), "=r"(code[t].y), "=r"(code[t].z), "=r"(code[t].w)
+                                     : "r"(block + t * 256 + ((r & 8) | ((r & 7) ^ 2 * t)) * 16) : "memory");
+                    uint32_t scale[NG], zero[NG];
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        const uint32_t e = block + W4_CODES + (g * 8 + (r & 7)) * ENTRY + (r >> 3) * 2;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=r"(scale[g]) : "r"(e) : "memory");
+                        zero[g] = 8;
+                        if (ZEROS) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(zero[g]) : "r"(e + 4) : "memory");
+                    }
+                    wait(&a_empty[ab.at], ab.phase ^ 1);
+                    mm_fence_after();
+                    // the MMAs of two steps ago are done, and the rounds but two of that step have been scaled: their slots are free
+                    if (fresh || NG > 1) {
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) scales[(round + g) % SCALE_SLOTS][row] = Ty::lo(scale[g]);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t v[32];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) {
+                                uint32_t p[4];
+                                Ty::pairs(word_of(code[t], 2 * h + j), zero[(2 * h + j) * NG / 4] * 0x00010001u, p);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[16 * j + 4 * t + i] = p[i];
+                            }
+                        w4_st32(tmem_a + ab.at * 64 + h * 32 + lanes, v);
+                    }
+                    mm_st_wait();
+                    mm_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mm_arrive(&w_empty[w.at]);
+                        mm_arrive(&a_full[ab.at]);
+                    }
+                }
+                fresh = ends(c, s.c1);
+                round += NG > 1 ? NG : fresh;
+                w.next();
+                ab.next();
+            }
+        }
+    } else if (warp >= 4 + Ro::EXPAND) {
+        // a thread owns a row of the tile and all of its columns, or with eight warps half of them
+        const int half = (warp - 4 - Ro::EXPAND) >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        Turn<2> d;
+        int round = 0;
+        while (s.next(a)) {
+            int mt, ot;
+            tile_place(a, s.tile, mt, ot);
+            const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31), width = rows * 4 / Ro::SCALE, n0 = half * width;
+            u64 tot[Ro::PIECES][8];
+#pragma unroll
+            for (int p = 0; p < Ro::PIECES; ++p)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) tot[p][i] = 0;
+            int rounds = 0;
+            if (NG > 1) rounds = (s.c1 - s.c0) * NG;
+            else rounds = (s.c1 - 1) / a.group_blocks - s.c0 / a.group_blocks + 1;
+            for (int k = 0; k < rounds; ++k) {
+                wait(&d_full[d.at], d.phase);
+                mm_fence_after();
+                const float sc = scales[round % SCALE_SLOTS][row];
+                const u64 ss = f2_pack(__float_as_uint(sc), __float_as_uint(sc));
+                const uint32_t from = tmem + d.at * Ro::N + n0 + lanes;
+#pragma unroll
+                for (int p = 0; p < Ro::PIECES; p += 2) {
+                    uint32_t v[2][16];
+                    if (p * 16 < width) mm_ld16(from + p * 16, v[0]);
+                    if (p * 16 + 16 < width) mm_ld16(from + p * 16 + 16, v[1]);
+                    mm_ld_wait();
+                    mm_landed(v[0]);
+                    mm_landed(v[1]);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+                        if ((p + q) * 16 < width) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) tot[p + q][i] = f2_fma(f2_pack(v[q][2 * i], v[q][2 * i + 1]), ss, tot[p + q][i]);
+                        }
+                }
+                mm_fence_before();
+                __syncwarp();
+                if (lane == 0) mm_arrive(&d_empty[d.at]);
+                d.next();
+                ++round;
+            }
+            const int o = ot * ROWS + row;
+            if (s.part < 0) {
+                if (o < l.O) {
+                    const float bias = a.g.bias ? static_cast<float>(static_cast<const T*>(a.g.bias)[o]) : 0.f;
+                    T* y = static_cast<T*>(a.g.y) + static_cast<long long>(m0 + n0) * a.g.ldy + o;
+#pragma unroll
+                    for (int p = 0; p < Ro::PIECES; ++p)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t lo, hi;
+                            f2_split(tot[p][i], lo, hi);
+                            const int m = p * 16 + 2 * i;
+                            if (m < width && m0 + n0 + m < a.g.M) y[m * a.g.ldy] = Ty::round(__uint_as_float(lo) + bias);
+                            if (m < width && m0 + n0 + m + 1 < a.g.M) y[(m + 1) * a.g.ldy] = Ty::round(__uint_as_float(hi) + bias);
+                        }
+                }
+            } else {
+                float* out = a.part + (static_cast<size_t>(s.part) * a.n + n0) * ROWS + row;
+#pragma unroll
+                for (int p = 0; p < Ro::PIECES; ++p)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t lo, hi;
+                        f2_split(tot[p][i], lo, hi);
+                        const int m = p * 16 + 2 * i;
+                        if (m < width && m0 + n0 + m < a.g.M) out[m * ROWS] = __uint_as_float(lo);
+                        if (m < width && m0 + n0 + m + 1 < a.g.M) out[(m + 1) * ROWS] = __uint_as_float(hi);
+                    }
+            }
+        }
+    }
+    mm_fence_before();
+    __syncthreads();
+    mm_fence_after();
+    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Ro::COLUMNS) : "memory");
+}
+
+// Adds the parts of the tiles that were cut, in the order of the reduction.  blockIdx.x: the run whose beginning is the first cut in its tile.
+template <bool F16>
+__global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ MmaTiles a)
+{
+    typedef typename W4Type<F16>::T T;
+    const float* part = dependent_begin(a.part);
+    const int cbs = a.g.l.cbs, run = blockIdx.x + 1;
+    const long long steps = static_cast<long long>(a.mts) * a.ots * cbs - static_cast<long long>(a.waves) * a.ctas * cbs;
+    const long long cut = static_cast<long long>(run) * a.per;
+    if (cut >= steps || cut % cbs == 0) return;
+    const long long t = cut / cbs, beg = t * cbs, end = beg + cbs;
+    if (cut - a.per > beg) return;          // an earlier run's beginning lies in this tile
+    const int last = static_cast<int>((end - 1) / a.per);
+    int mt, ot;
+    tile_place(a, static_cast<int>(t) + a.waves * a.ctas, mt, ot);
+    const int m0 = mt * a.n, rows = min(a.n, a.g.M - m0);
+    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rows * ROWS; i += gridDim.y * blockDim.x) {
+        const int m = i / ROWS, r = i % ROWS, o = ot * ROWS + r;
+        if (o >= a.g.l.O) continue;
+        float v = 0.f;
+        // the tile is what run - 1 ends in (or began in, where it is shorter than a tile), and what the others begin in
+        for (int c = run - 1; c <= last; ++c) {
+            const long long b = static_cast<long long>(c) * a.per;
+            v += part[(static_cast<size_t>(2 * c + (b < beg)) * a.n + m) * ROWS + r];
+        }
+        if (a.g.bias) v += static_cast<float>(static_cast<const T*>(a.g.bias)[o]);
+        static_cast<T*>(a.g.y)[(m0 + m) * a.g.ldy + o] = W4Type<F16>::round(v);
+    }
+}
+
+// Tensor map of the rows of x, fetched in boxes of 32 rows x 64 columns.
+bool encode_x(CUtensorMap* tm, const W4Gemm& g, bool f16)
+{
+    typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                           CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static Fn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* q = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &q, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess) fn = reinterpret_cast<Fn>(q);
+    });
+    if (!fn) return false;
+    const long long pitch = g.M == 1 ? (g.l.K + 7) & ~7 : g.ldx;       // one row: any pitch that the map takes
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(g.l.K), static_cast<cuuint64_t>(g.M)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
+    const cuuint32_t box[2] = {64, 32}, es[2] = {1, 1};
+    return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(g.x), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool plan(MmaTiles& a, int sms)
+{
+    const W4Layout& l = a.g.l;
+    const int n = a.g.M <= 64 ? (a.g.M + 31) & ~31 : ((a.g.M + ceil_div(a.g.M, 128) - 1) / ceil_div(a.g.M, 128) + 31) & ~31;
+    a.n = n;
+    a.mts = ceil_div(a.g.M, n);
+    a.ots = ceil_div(l.O, ROWS);
+    const long long tiles = static_cast<long long>(a.mts) * a.ots;
+    if (tiles * l.cbs > 0x7fffffff) return false;
+    a.ctas = static_cast<int>(tiles * l.cbs < sms ? tiles * l.cbs : sms);
+    a.waves = static_cast<int>(tiles % a.ctas == 0 ? tiles / a.ctas : tiles / a.ctas > 0 ? tiles / a.ctas - 1 : 0);
+    const long long steps = (tiles - static_cast<long long>(a.waves) * a.ctas) * l.cbs;
+    a.per = static_cast<int>((steps + a.ctas - 1) / a.ctas);
+    a.group_blocks = l.group > W4_COLS ? l.group / W4_COLS : 1;
+    return true;
+}
+
+template <bool F16, int NG, bool ZEROS, bool FEW>
+int launch(const CUtensorMap& tx, const MmaTiles& a, cudaStream_t st)
+{
+    auto kernel = w4_mma_kernel<F16, NG, ZEROS, FEW>;
+    const int smem = 1024 + X_STAGES * a.n * 256 + Roles<FEW>::W_STAGES * BLOCKS * a.g.l.block;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
+    int rc = launch_dependent(kernel, dim3(a.ctas), dim3(Roles<FEW>::WARPS * 32), smem, st, tx, a);
+    if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n >= 64 ? 4 : 1), dim3(256), 0, st, a);
+    return rc;
+}
+template <bool F16, bool FEW>
+int launch_group(const CUtensorMap& tx, const MmaTiles& a, cudaStream_t st)
+{
+    const int ng = a.g.l.group == 32 ? 4 : a.g.l.group == 64 ? 2 : 1;
+    if (a.g.l.zeros) return ng == 4 ? launch<F16, 4, true, FEW>(tx, a, st) : ng == 2 ? launch<F16, 2, true, FEW>(tx, a, st) : launch<F16, 1, true, FEW>(tx, a, st);
+    return ng == 4 ? launch<F16, 4, false, FEW>(tx, a, st) : ng == 2 ? launch<F16, 2, false, FEW>(tx, a, st) : launch<F16, 1, false, FEW>(tx, a, st);
+}
+
+}  // namespace
+
+bool w4_mma_wanted(int M, const W4Layout& l) { return M > 16; }
+
+size_t w4_mma_workspace(int M, const W4Layout& l, int sms)
+{
+    MmaTiles a{};
+    a.g.M = M;
+    a.g.l = l;
+    return plan(a, sms) && a.per > 0 ? static_cast<size_t>(2) * a.ctas * a.n * ROWS * sizeof(float) : 0;
+}
+
+int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t st)
+{
+    MmaTiles a{};
+    a.g = g;
+    a.part = part;
+    CUtensorMap tx;
+    if (!plan(a, sms)) return BS_ERR_UNSUPPORTED;
+    if (!encode_x(&tx, g, f16)) return BS_ERR_CUDA;
+    if (a.n <= 64) return f16 ? launch_group<true, true>(tx, a, st) : launch_group<false, true>(tx, a, st);
+    return f16 ? launch_group<true, false>(tx, a, st) : launch_group<false, false>(tx, a, st);
+}
+
+}  // namespace bs

@@ -198,75 +198,73 @@ __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int
     __syncthreads();
 }
 
-// h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  `split` warps, a team, share the reduction of an item; the blocks of their
-// next items are on their way while they put the sums of the current one together.
+// h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  The warps of a team share the reduction of 16 rows; the last warp copies
+// the blocks of the CTA's items ahead, also while the sums of an item are put together.
 template <bool F16, int NG, bool ZEROS, int NT>
-__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g, int split)
+__global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g, int split)
 {
     typedef typename W4Type<F16>::T T;
-    typedef W4Ring<NG, ZEROS, 2, GATE_STAGES> Ring;
+    typedef W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES> Ring;
     constexpr int J = NT * 8;
-    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t bars[2 * GATE_STAGES];
     __shared__ Jobs jobs;
     __shared__ float part[WARPS][2][J][17];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
     const int team = warp / split, k0 = warp % split, teams = WARPS / split;
-    __shared__ uint64_t bars[WARPS][GATE_STAGES];
-    Ring ring(smem, bars[warp], warp, lane);
+    Ring ring(smem, bars, warp, lane);
     const T* x = static_cast<const T*>(dependent_begin(g.xa ? g.xa : g.x));
     const long long ldx = g.xa ? g.ldxa : g.ldx;
-    find_jobs<J>(g, jobs, t0, WARPS * 32);
+    find_jobs<J>(g, jobs, t0, WARPS * 32 + 32);
     const W4Layout& l = g.lu;
     const size_t matrix = l.bytes();
-    const int items = jobs.n * l.rbs, full = l.K / W4_COLS;
-    // neighbouring teams work on neighbouring rows: they share the tokens' x in L1
-    const int step = gridDim.x * teams;
-    // the blocks that are fetched next
-    int fitem = blockIdx.x * teams + team, fc = k0;
-    const unsigned char* from[2];
-    auto locate = [&] {
-        const int job = fitem / l.rbs, rb = fitem - job * l.rbs;
-        const size_t at = jobs.expert[job] * matrix + (static_cast<size_t>(rb) * l.cbs + k0) * Ring::BLOCK;
-        from[0] = g.gate + at;
-        from[1] = g.up + at;
-    };
-    if (k0 >= l.cbs) fitem = items;
-    if (fitem < items) locate();
-    auto put = [&] {
-        if (fitem >= items) return;
-        ring.put(from, lane);
-        fc += split;
-        if (fc < l.cbs) {
-            from[0] += split * Ring::BLOCK;
-            from[1] += split * Ring::BLOCK;
-        } else {
-            fc = k0;
-            fitem += step;
-            if (fitem < items) locate();
-        }
-    };
-#pragma unroll 1
-    for (int s = 0; s < GATE_STAGES - 1; ++s) put();
-    for (int item = blockIdx.x * teams + team; item < items; item += step) {
-        const int job = item / l.rbs, rb = item - job * l.rbs, beg = jobs.first[job];
+    // an item: a job and the rows of all teams
+    const int per_job = (l.rbs + teams - 1) / teams, items = jobs.n * per_job, full = l.K / W4_COLS;
+    if (warp == WARPS) {
+        if (lane == 0)
+            for (int item = blockIdx.x; item < items; item += gridDim.x) {
+                const int job = item / per_job, rb0 = (item - job * per_job) * teams, rows = min(teams, l.rbs - rb0);
+                const size_t at = jobs.expert[job] * matrix;
+                for (int c = 0; c < l.cbs; c += split) {
+                    const int n = min(split, l.cbs - c);
+                    ring.open(2 * rows * n, g.status);
+                    for (int r = 0; r < rows; ++r) {
+                        const size_t p = at + (static_cast<size_t>(rb0 + r) * l.cbs + c) * Ring::BLOCK;
+                        ring.copy(0, r * split, g.gate + p, n);
+                        ring.copy(1, r * split, g.up + p, n);
+                    }
+                    ring.next();
+                }
+            }
+        return;
+    }
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int job = item / per_job, rb = (item - job * per_job) * teams + team, beg = jobs.first[job];
         // a job's slots end where the next one's begin; lanes without a slot compute the last one's again
         const int n = jobs.first[job + 1] - beg;
         const T* row[NT];
 #pragma unroll
-        for (int k = 0; k < NT; ++k) row[k] = x + (t0 + jobs.token[beg + min(k * 8 + (lane >> 2), n - 1)]) * ldx;
+        for (int k = 0; k < NT; ++k) row[k] = x + (t0 + jobs.token[beg + min(k * 8 + (lane >> 2), n - 1)]) * ldx + 8 * (lane & 3);
         float tot[2][NT][4];
 #pragma unroll
         for (int k = 0; k < NT; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
-        for (int c = k0; c < l.cbs; c += split) {
+        // teams without rows multiply what the stages hold, and drop it
+        for (int c = k0; c < l.cbs + k0; c += split) {
             uint4 v[NT][4];
+            if (c < l.cbs) {
 #pragma unroll
-            for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
-            W4Tile<NG, ZEROS> w[2];
-            ring.get(w, lane, g.status);
-            put();      // into the stage before this one: its blocks have been multiplied
-            w4_blocks<F16, F16, 1>(w, [&](int k, int j, int) { return v[k][j]; }, tot);
+                for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
+            }
+            ring.landed(g.status);
+            if (c < l.cbs) {
+                W4Tile<NG, ZEROS> w[2];
+                ring.take(w);
+                w4_blocks<F16, F16, 1>(w, [&](int k, int j, int) { return v[k][j]; }, tot);
+            }
+            ring.release(lane);
+            ring.next();
         }
 #pragma unroll
         for (int k = 0; k < NT; ++k)
@@ -330,9 +328,12 @@ __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid
         for (int r = 0; r < RT; ++r) from[r] = down + jobs.expert[fjob] * matrix + (static_cast<size_t>(min(rb0 + r, l.rbs - 1)) * l.cbs + fc) * Ring::BLOCK;
     };
     if (beg < end) locate();
+    int in = 0, out = 0;        // stages that are filled and read next
+    unsigned phase = 0;
     auto put = [&] {
         if (f >= end) return;
-        ring.put(from, lane);
+        ring.put(in, from, lane);
+        in = (in + 1) % DOWN_STAGES;
         ++f;
         if (++fc < l.cbs) {
 #pragma unroll
@@ -361,7 +362,9 @@ __global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid
         for (; c < stop; ++c) {
             W4Tile<NG, ZEROS> w[RT];
             const int k0 = c * W4_COLS + 8 * (lane & 3);
-            ring.get(w, lane, g.status);
+            ring.get(out, phase, w, lane, g.status);
+            out = (out + 1) % DOWN_STAGES;
+            phase ^= out == 0;
             put();      // into the stage before this one: its blocks have been multiplied
             if (c < full) w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + k0 + 32 * j)); }, tot);
             else w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0), k0 + 32 * j, l.K); }, tot);
@@ -439,15 +442,13 @@ template <bool F16, int NG, bool ZEROS, int NT>
 int launch_gate(const MoeArgs& g, int sms, cudaStream_t st)
 {
     const int slots = (g.T < PASS ? g.T : PASS) * g.top_k;
-    const long long items = static_cast<long long>(slots < g.E ? slots : g.E) * g.lu.rbs;
-    // enough warps for 16 an SM, each with two blocks of the reduction at least
     int split = WARPS;
-    while (split > 1 && (2 * split > g.lu.cbs + 1 || items * split / 2 >= 16ll * sms)) split /= 2;
-    const long long ctas = (items * split + WARPS - 1) / WARPS;
-    const size_t smem = WARPS * W4Ring<NG, ZEROS, 2, GATE_STAGES>::BYTES;
+    while (split / 2 >= g.lu.cbs) split /= 2;
+    const long long items = static_cast<long long>(slots < g.E ? slots : g.E) * ceil_div(g.lu.rbs, WARPS / split);
+    constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES>::BYTES;
     if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(ctas < 2 * sms ? ctas : 2 * sms), ceil_div(g.T, PASS)),
-                            dim3(WARPS * 32), smem, st, g, split);
+    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
+                            dim3(WARPS * 32 + 32), smem, st, g, split);
 }
 template <bool F16, int NG, bool ZEROS, int NT>
 int launch_down(const MoeArgs& g, int sms, cudaStream_t st)

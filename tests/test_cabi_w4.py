@@ -28,10 +28,12 @@ def test_sizes(L):
     assert L.bs_w4_bytes(1, 1, 1 << 20, 0) == 1024 + 32
     for bad in ((0, 128, 128), (16, 0, 128), (16, 128, 0), (16, 128, 48), (16, 128, 16), (16, 128, 192), (1 << 21, 128, 128), (16, 1 << 21, 128), (16, 128, 1 << 21), (16, 128, -128)):
         assert L.bs_w4_bytes(*bad, 0) == 0
-    assert L.bs_w4_gemm_workspace_bytes(1, 4611, 4611) == 0
-    assert L.bs_w4_gemm_workspace_bytes(5, 4616, 4616) == 0
-    assert L.bs_w4_gemm_workspace_bytes(5, 4611, 4616) == 0
-    assert L.bs_w4_gemm_workspace_bytes(5, 4611, 4611) == 5 * 4616 * 2
+    assert L.bs_w4_gemm_workspace_bytes(1, 64, 4611, 128, 4611) == 0
+    assert L.bs_w4_gemm_workspace_bytes(5, 64, 4616, 128, 4616) == 0
+    assert L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 128, 4616) == 0
+    assert L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 128, 4611) == 5 * 4616 * 2
+    assert L.bs_w4_gemm_workspace_bytes(0, 64, 4611, 128, 4611) == L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 96, 4611) == 0
+    assert L.bs_w4_gemm_workspace_bytes(300, 64, 4611, 128, 4611) > 300 * 4616 * 2
     assert L.bs_w4_moe_workspace_bytes(3, 2, 64, 50, 64) == 2 * 3 * 2 * 56 * 2
     assert L.bs_w4_moe_workspace_bytes(3, 2, 63, 50, 63) == 2 * 3 * 2 * 56 * 2 + 3 * 64 * 2
     assert L.bs_w4_moe_workspace_bytes(0, 2, 64, 50, 64) == 0
