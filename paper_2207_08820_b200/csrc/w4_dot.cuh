@@ -36,6 +36,11 @@ template <> struct W4Type<false> {
     static __device__ __forceinline__ float lo(uint32_t v) { return __uint_as_float(v << 16); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
     static __device__ __forceinline__ T round(float v) { return __float2bfloat16_rn(v); }
+    static __device__ __forceinline__ uint32_t round2(float lo, float hi)
+    {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
     {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -60,6 +65,11 @@ template <> struct W4Type<true> {
     static __device__ __forceinline__ float lo(uint32_t v) { return __low2float(*reinterpret_cast<const __half2*>(&v)); }
     static __device__ __forceinline__ float hi(uint32_t v) { return __high2float(*reinterpret_cast<const __half2*>(&v)); }
     static __device__ __forceinline__ T round(float v) { return __float2half_rn(v); }
+    static __device__ __forceinline__ uint32_t round2(float lo, float hi)
+    {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&v);
+    }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
     {
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"

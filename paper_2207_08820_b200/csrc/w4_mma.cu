@@ -4,8 +4,10 @@
 // core in an accumulator of their own, and warps with the running totals in registers take them over, scaled in 32 bits, while the next group is
 // multiplied.  Folding the scale in would round every weight and double the error of the result.
 //
-// Roles of a CTA, one per SM: tensor copies of x (128 columns a stage), bulk copies of weight blocks, MMA issue, warps that expand a row a thread into
-// tensor memory (two buffers of 128 columns), warps that scale and add (two accumulators).
+// Roles of a CTA, one per SM: tensor copies of x, bulk copies of weight blocks, MMA issue, warps that expand a row a thread into tensor memory, warps that scale
+// and add.  A step is 128 columns.  The MMA warp's waits and commits, 100 to 160 cycles each, would cost more than the 512 cycles of a step's MMAs:
+// whatever a step needs (x, its expanded weights, and with one group a step a free accumulator) arrives at one barrier, and one commit frees
+// all of it again.
 //
 // Work: tiles of 128 rows by up to 128 rows of x.  A CTA takes whole tiles, neighbours at a time, as long as every CTA gets one; what is left, less than
 // two tiles a CTA, is cut into equal runs of (tile, 128 columns), and a small kernel adds the parts of the tiles that were cut, in their order.
@@ -20,7 +22,7 @@ namespace bs {
 namespace {
 
 constexpr int ROWS = 128, BLOCKS = ROWS / W4_ROWS;      // of a tile
-constexpr int X_STAGES = 4, SCALE_SLOTS = 16;
+constexpr int RING = 4, SCALE_SLOTS = 32;         // steps on their way: stages of x, buffers of expanded weights
 
 struct MmaTiles {
     W4Gemm g;
@@ -30,7 +32,6 @@ struct MmaTiles {
     int per;                    // steps of 128 columns in a run
     int ctas;
     float* part;                // [2 ctas][n][ROWS]: the parts of the tiles that a run begins and ends in
-    int group_blocks;           // blocks of columns in a group (1 where a block holds several groups)
 };
 
 // Tile t: eight tiles of x's rows side by side, then the weights' next rows, so that what runs at the same time shares both.
@@ -65,7 +66,7 @@ struct Stretch {
         c0 = pos - tile * cbs;
         c1 = min(cbs, c0 + end - pos);
         // a run begins in one tile and ends in another: two places; a tile that both begins before and ends behind the run has the first
-        part = c0 == 0 && c1 == cbs ? -1 : 2 * blockIdx.x + (pos != first);
+        part = c0 == 0 && c1 == cbs ? -1 : 2 * static_cast<int>(blockIdx.x) + (pos != first);
         pos += c1 - c0;
         tile += a.waves * a.ctas;
         return true;
@@ -84,15 +85,24 @@ __device__ __forceinline__ void w4_st32(uint32_t taddr, const uint32_t (&v)[32])
           "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
           "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
-// D[128 x n] (+)= A (tensor memory) B (shared memory), 16 columns of the reduction.
+// D[128 x n] (+)= A (tensor memory) B (shared memory): STEPS times 16 columns of the reduction (8 columns of A, 32 bytes of B's rows each) under one elect, in
+// one statement: descriptors that leave it move through vector registers, 90 cycles an MMA.
+#define W4_MMA(A, B, P) "@p tcgen05.mma.cta_group::1.kind::f16 [%0], [" A "], " B ", %3, " P ";\n\t"
+#define W4_STEP "add.u32 u, u, 8;\n\tadd.s64 t, t, 2;\n\t" W4_MMA("u", "t", "1")
+template <int STEPS>
 __device__ __forceinline__ void w4_mma(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t acc)
 {
-    if (mm_elect())
+    const uint64_t b = (static_cast<uint64_t>(b_hi) << 32) | b_lo;
+    if constexpr (STEPS == 4)
         asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"((static_cast<uint64_t>(b_hi) << 32) | b_lo), "r"(idesc), "r"(acc) : "memory");
+            "{\n\t.reg .pred p, q;\n\t.reg .b32 u;\n\t.reg .b64 t;\n\t"
+            "setp.ne.b32 q, %4, 0;\n\tmov.b32 u, %1;\n\tmov.b64 t, %2;\n\telect.sync _|p, 0xffffffff;\n\t"
+            W4_MMA("u", "t", "q") W4_STEP W4_STEP W4_STEP "}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t.reg .b32 u;\n\t.reg .b64 t;\n\t"
+            "setp.ne.b32 q, %4, 0;\n\tmov.b32 u, %1;\n\tmov.b64 t, %2;\n\telect.sync _|p, 0xffffffff;\n\t"
+            W4_MMA("u", "t", "q") W4_STEP "}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
 
 // A position in a ring of stages, and the parity of its round.
@@ -104,13 +114,19 @@ struct Turn {
     __device__ __forceinline__ void next() { if (++at == N) { at = 0; phase ^= 1; } }
 };
 
-// FEW: up to 64 rows of x, bound by the weights: eight warps expand, four scale.  Otherwise four and eight.
+// FEW: up to 64 rows of x, bound by the weights: four warps scale, otherwise eight.  The threads' registers are dealt anew: 640 of 96 become 128 (copies, MMA
+// issue) of 40, 256 (expansion) of 72 and 256 (totals) of 144; with few rows 512 of 128 become 128 of 40, 256 of 104 and 128 of 168.
 template <bool FEW> struct Roles {
-    static constexpr int EXPAND = FEW ? 8 : 4, SCALE = FEW ? 4 : 8, WARPS = 4 + EXPAND + SCALE, W_STAGES = FEW ? 8 : 4;
+    static constexpr int EXPAND = 8, SCALE = FEW ? 4 : 8, WARPS = 4 + EXPAND + SCALE, W_STAGES = FEW ? 8 : 4;
     static constexpr int N = FEW ? 64 : 128;                    // most rows of x in a tile
-    static constexpr int COLUMNS = FEW ? 256 : 512;             // of tensor memory: two accumulators of N, two A buffers of 64
     static constexpr int PIECES = N * 4 / SCALE / 16;           // 16 columns each, of a thread's totals
 };
+constexpr int TMEM_COLUMNS = 512, TMEM_A = 256;                 // two accumulators of N columns; RING buffers of 64
+template <bool MORE, int N> __device__ __forceinline__ void registers()
+{
+    if (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
 
 template <bool F16, int NG, bool ZEROS, bool FEW>
 __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ MmaTiles a)
@@ -120,29 +136,29 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     typedef Roles<FEW> Ro;
     constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, WS = Ro::W_STAGES;
     extern __shared__ unsigned char raw[];
-    // x [X_STAGES][2][n][128 bytes], swizzled by address: from a multiple of 1024 on; weights [WS][BLOCKS][BLOCK]
+    // x [RING][2][n][128 bytes], swizzled by address: from a multiple of 1024 on; weights [WS][BLOCKS][BLOCK]
     unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
-    __shared__ uint64_t x_full[X_STAGES], x_empty[X_STAGES], w_full[WS], w_empty[WS], a_full[2], a_empty[2], d_full[2], d_empty[2];
+    __shared__ uint64_t full[RING], done[RING], w_full[WS], w_empty[WS], d_full[2], d_empty[2];     // the last two where a step has several groups
     __shared__ float scales[SCALE_SLOTS][ROWS];
     __shared__ uint32_t tmem_slot;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const W4Layout& l = a.g.l;
-    unsigned char* wsm = smem + static_cast<size_t>(X_STAGES) * a.n * 256;
+    unsigned char* wsm = smem + static_cast<size_t>(RING) * a.n * 256;
     if (warp == 3) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(Ro::COLUMNS) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         mm_fence_before();
     } else if (warp == 0 && lane == 0) {
-        for (int s = 0; s < X_STAGES; ++s) { mbar_init(&x_full[s], 1); mbar_init(&x_empty[s], 1); }
+        for (int s = 0; s < RING; ++s) { mbar_init(&full[s], 5 + (NG == 1 ? Ro::SCALE : 0)); mbar_init(&done[s], 1); }
         for (int s = 0; s < WS; ++s) { mbar_init(&w_full[s], 1); mbar_init(&w_empty[s], 4); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&a_full[s], 4); mbar_init(&a_empty[s], 1); mbar_init(&d_full[s], 1); mbar_init(&d_empty[s], Ro::SCALE); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&d_full[s], 1); mbar_init(&d_empty[s], Ro::SCALE); }
         fence_barrier_init();
         fence_proxy_async();
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tx)) : "memory");
     }
     __syncthreads();
     mm_fence_after();
-    const uint32_t tmem = tmem_slot, tmem_a = tmem + 2 * Ro::N;
+    const uint32_t tmem = tmem_slot, tmem_a = tmem + TMEM_A;
     const unsigned char* matrix = dependent_begin(a.g.w);
     bool late = false;          // a wait ran out: later ones are not waited for
     auto wait = [&](uint64_t* bar, unsigned parity) {
@@ -151,110 +167,105 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
             atomicOr(a.g.status, STATUS_TIMEOUT);
         }
     };
-    // The last step of a round: a group's sums are complete, or the stretch ends.
-    auto ends = [&](int c, int c1) { return NG > 1 || c + 1 == c1 || (c + 1) % a.group_blocks == 0; };
     Stretch s(a);
-    if (warp == 0) {
-        if (lane == 0) {
-            Turn<X_STAGES> x;
-            int issued = 0;
+    if (warp < 4) {
+        registers<false, 40>();
+        if (warp == 0) {
+            if (lane == 0) {
+                Turn<RING> x;
+                int issued = 0;
+                while (s.next(a)) {
+                    int mt, ot;
+                    tile_place(a, s.tile, mt, ot);
+                    const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
+                    for (int c = s.c0; c < s.c1; ++c) {
+                        wait(&done[x.at], x.phase ^ 1);
+                        unsigned char* to = smem + static_cast<size_t>(x.at) * a.n * 256;
+                        mbar_expect_tx(&full[x.at], rows * 256);
+                        for (int h = 0; h < 2; ++h)
+                            for (int r = 0; r < rows; r += 32) tma_load_2d(to + (h * a.n + r) * 128, &tx, &full[x.at], c * W4_COLS + h * 64, m0 + r);
+                        x.next();
+                        ++issued;
+                    }
+                }
+                for (int i = 0; i < RING && i < issued; ++i) {      // no copy outlives the CTA
+                    x.at = x.at == 0 ? RING - 1 : x.at - 1;
+                    if (x.at == RING - 1) x.phase ^= 1;
+                    wait(&full[x.at], x.phase);
+                }
+            }
+            __syncwarp();
+        } else if (warp == 1) {
+            Turn<RING> x;
+            Turn<2> d;
+            unsigned limit = 1u << 20;
+            const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
+            // K-major rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group
+            const uint32_t b_hi = 64u | (1u << 14) | (2u << 29);
             while (s.next(a)) {
                 int mt, ot;
                 tile_place(a, s.tile, mt, ot);
                 const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
+                const uint32_t idesc = (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(rows >> 3) << 17) | (static_cast<uint32_t>(ROWS >> 4) << 24);
                 for (int c = s.c0; c < s.c1; ++c) {
-                    wait(&x_empty[x.at], x.phase ^ 1);
-                    unsigned char* to = smem + static_cast<size_t>(x.at) * a.n * 256;
-                    mbar_expect_tx(&x_full[x.at], rows * 256);
-                    for (int h = 0; h < 2; ++h)
-                        for (int r = 0; r < rows; r += 32) tma_load_2d(to + (h * a.n + r) * 128, &tx, &x_full[x.at], c * W4_COLS + h * 64, m0 + r);
+                    mm_wait_uniform(&full[x.at], x.phase, limit);
+                    mm_fence_after();
+                    const uint32_t xs = base + static_cast<uint32_t>(x.at * a.n * 16), as = tmem_a + x.at * 64;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) {
+                        if (NG > 1) {
+                            mm_wait_uniform(&d_empty[d.at], d.phase ^ 1, limit);
+                            mm_fence_after();
+                        }
+                        constexpr int STEPS = NG == 4 ? 2 : 4;      // 64 columns of x lie together
+#pragma unroll
+                        for (int k = 0; k < 8 / NG; k += STEPS) {
+                            const int step = g * (8 / NG) + k;
+                            const uint32_t b = xs + static_cast<uint32_t>((step >> 2) * a.n * 8 + (step & 3) * 2);
+                            w4_mma<STEPS>(tmem + d.at * Ro::N, as + step * 8, (b & 0x3fff) | (1u << 16), b_hi, idesc, k == 0 ? 0u : 1u);
+                        }
+                        if (NG > 1) mm_commit(&d_full[d.at]);
+                        d.next();
+                    }
+                    mm_commit(&done[x.at]);
                     x.next();
+                }
+            }
+            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
+        } else if (warp == 2) {
+            Turn<WS> w;
+            int issued = 0;
+            while (s.next(a)) {
+                int mt, ot;
+                tile_place(a, s.tile, mt, ot);
+                const int rb = ot * BLOCKS, have = min(BLOCKS, l.rbs - rb);
+                for (int c = s.c0; c < s.c1; ++c) {
+                    wait(&w_empty[w.at], w.phase ^ 1);
+                    if (lane == 0) mbar_expect_tx(&w_full[w.at], have * BLOCK);
+                    __syncwarp();
+                    if (lane < have) mm_bulk(wsm + (w.at * BLOCKS + lane) * BLOCK, matrix + (static_cast<size_t>(rb + lane) * l.cbs + c) * BLOCK, BLOCK, &w_full[w.at]);
+                    w.next();
                     ++issued;
                 }
             }
-            for (int i = 0; i < X_STAGES && i < issued; ++i) {      // no copy outlives the CTA
-                x.at = x.at == 0 ? X_STAGES - 1 : x.at - 1;
-                if (x.at == X_STAGES - 1) x.phase ^= 1;
-                wait(&x_full[x.at], x.phase);
+            for (int i = 0; i < WS && i < issued; ++i) {
+                w.at = w.at == 0 ? WS - 1 : w.at - 1;
+                if (w.at == WS - 1) w.phase ^= 1;
+                wait(&w_full[w.at], w.phase);
             }
+            __syncwarp();
         }
-        __syncwarp();
-    } else if (warp == 1) {
-        Turn<X_STAGES> x;
-        Turn<2> ab, d;
-        unsigned limit = 1u << 20;
-        const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
-        // K-major rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group
-        const uint32_t b_hi = 64u | (1u << 14) | (2u << 29);
-        while (s.next(a)) {
-            int mt, ot;
-            tile_place(a, s.tile, mt, ot);
-            const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
-            const uint32_t idesc = (1u << 4) | (F16 ? 0u : (1u << 7) | (1u << 10)) | (static_cast<uint32_t>(rows >> 3) << 17) | (static_cast<uint32_t>(ROWS >> 4) << 24);
-            bool fresh = true;
-            for (int c = s.c0; c < s.c1; ++c) {
-                mm_wait_uniform(&x_full[x.at], x.phase, limit);
-                mm_wait_uniform(&a_full[ab.at], ab.phase, limit);
-                mm_fence_after();
-                const uint32_t xs = base + static_cast<uint32_t>(x.at * a.n * 16), as = tmem_a + ab.at * 64;
-#pragma unroll
-                for (int g = 0; g < NG; ++g) {
-                    if (fresh) {
-                        mm_wait_uniform(&d_empty[d.at], d.phase ^ 1, limit);
-                        mm_fence_after();
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8 / NG; ++k) {
-                        const int step = g * (8 / NG) + k;      // 16 columns: 32 bytes of a row, 8 columns of A
-                        const uint32_t b = xs + static_cast<uint32_t>((step >> 2) * a.n * 8 + (step & 3) * 2);
-                        w4_mma(tmem + d.at * Ro::N, as + step * 8, (b & 0x3fff) | (1u << 16), b_hi, idesc, fresh && k == 0 ? 0u : 1u);
-                    }
-                    fresh = ends(c, s.c1);
-                    if (fresh) {
-                        mm_commit(&d_full[d.at]);
-                        d.next();
-                    }
-                }
-                mm_commit(&x_empty[x.at]);
-                mm_commit(&a_empty[ab.at]);
-                x.next();
-                ab.next();
-            }
-        }
-        if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
-    } else if (warp == 2) {
-        Turn<WS> w;
-        int issued = 0;
-        while (s.next(a)) {
-            int mt, ot;
-            tile_place(a, s.tile, mt, ot);
-            const int rb = ot * BLOCKS, have = min(BLOCKS, l.rbs - rb);
-            for (int c = s.c0; c < s.c1; ++c) {
-                wait(&w_empty[w.at], w.phase ^ 1);
-                if (lane == 0) mbar_expect_tx(&w_full[w.at], have * BLOCK);
-                __syncwarp();
-                if (lane < have) mm_bulk(wsm + (w.at * BLOCKS + lane) * BLOCK, matrix + (static_cast<size_t>(rb + lane) * l.cbs + c) * BLOCK, BLOCK, &w_full[w.at]);
-                w.next();
-                ++issued;
-            }
-        }
-        for (int i = 0; i < WS && i < issued; ++i) {
-            w.at = w.at == 0 ? WS - 1 : w.at - 1;
-            if (w.at == WS - 1) w.phase ^= 1;
-            wait(&w_full[w.at], w.phase);
-        }
-        __syncwarp();
-    } else if (warp >= 4 && warp < 4 + Ro::EXPAND) {
-        // a thread owns a row of the tile; with two groups of warps each takes every other step, and a buffer
+    } else if (warp < 4 + Ro::EXPAND) {
+        registers<false, FEW ? 104 : 72>();
+        // a thread owns a row of the tile; each team of four warps takes every other step
         const int team = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, r = row & 15;
         const uint32_t mine = smem_u32(wsm) + (row >> 4) * BLOCK, lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         Turn<WS> w;
-        Turn<2> ab;
+        Turn<RING> ab;
         int round = 0;
         while (s.next(a)) {
-            bool fresh = true;
             for (int c = s.c0; c < s.c1; ++c) {
-                if (!FEW || ab.at == team) {
+                if ((ab.at & 1) == team) {
                     wait(&w_full[w.at], w.phase);
                     const uint32_t block = mine + w.at * BLOCKS * BLOCK;
                     uint4 code[4];
@@ -270,13 +281,11 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         zero[g] = 8;
                         if (ZEROS) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(zero[g]) : "r"(e + 4) : "memory");
                     }
-                    wait(&a_empty[ab.at], ab.phase ^ 1);
+                    wait(&done[ab.at], ab.phase ^ 1);
                     mm_fence_after();
-                    // the MMAs of two steps ago are done, and the rounds but two of that step have been scaled: their slots are free
-                    if (fresh || NG > 1) {
+                    // the step that had this buffer is done and all rounds before its last two are scaled: the slots of these are free
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) scales[(round + g) % SCALE_SLOTS][row] = Ty::lo(scale[g]);
-                    }
+                    for (int g = 0; g < NG; ++g) scales[(round + g) % SCALE_SLOTS][row] = Ty::lo(scale[g]);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t v[32];
@@ -295,22 +304,27 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                     mm_fence_before();
                     __syncwarp();
                     if (lane == 0) {
+                        mm_arrive(&full[ab.at]);
                         mm_arrive(&w_empty[w.at]);
-                        mm_arrive(&a_full[ab.at]);
                     }
                 }
-                fresh = ends(c, s.c1);
-                round += NG > 1 ? NG : fresh;
+                round += NG;
                 w.next();
                 ab.next();
             }
         }
-    } else if (warp >= 4 + Ro::EXPAND) {
+    } else {
+        registers<true, FEW ? 168 : 144>();
         // a thread owns a row of the tile and all of its columns, or with eight warps half of them
         const int half = (warp - 4 - Ro::EXPAND) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        Turn<RING> x;           // of the steps, where each is a round
         Turn<2> d;
         int round = 0;
+        if (NG == 1 && lane == 0) {     // the accumulators of the first two steps are free
+            mm_arrive(&full[0]);
+            mm_arrive(&full[1]);
+        }
         while (s.next(a)) {
             int mt, ot;
             tile_place(a, s.tile, mt, ot);
@@ -320,41 +334,54 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
             for (int p = 0; p < Ro::PIECES; ++p)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) tot[p][i] = 0;
-            int rounds = 0;
-            if (NG > 1) rounds = (s.c1 - s.c0) * NG;
-            else rounds = (s.c1 - 1) / a.group_blocks - s.c0 / a.group_blocks + 1;
+            const int rounds = (s.c1 - s.c0) * NG;
             for (int k = 0; k < rounds; ++k) {
-                wait(&d_full[d.at], d.phase);
+                wait(NG == 1 ? &done[x.at] : &d_full[d.at], NG == 1 ? x.phase : d.phase);
                 mm_fence_after();
-                const float sc = scales[round % SCALE_SLOTS][row];
-                const u64 ss = f2_pack(__float_as_uint(sc), __float_as_uint(sc));
                 const uint32_t from = tmem + d.at * Ro::N + n0 + lanes;
+                uint32_t v[Ro::PIECES][16];
 #pragma unroll
-                for (int p = 0; p < Ro::PIECES; p += 2) {
-                    uint32_t v[2][16];
-                    if (p * 16 < width) mm_ld16(from + p * 16, v[0]);
-                    if (p * 16 + 16 < width) mm_ld16(from + p * 16 + 16, v[1]);
-                    mm_ld_wait();
-                    mm_landed(v[0]);
-                    mm_landed(v[1]);
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if ((p + q) * 16 < width) {
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) tot[p + q][i] = f2_fma(f2_pack(v[q][2 * i], v[q][2 * i + 1]), ss, tot[p + q][i]);
-                        }
-                }
+                for (int p = 0; p < Ro::PIECES; ++p)
+                    if (p * 16 < width) mm_ld16(from + p * 16, v[p]);
+                const float sc = scales[round % SCALE_SLOTS][row];
+                mm_ld_wait();
                 mm_fence_before();
                 __syncwarp();
-                if (lane == 0) mm_arrive(&d_empty[d.at]);
+                if (lane == 0) mm_arrive(NG == 1 ? &full[(x.at + 2) % RING] : &d_empty[d.at]);      // the accumulator is free for the round after the next
+                const u64 ss = f2_pack(__float_as_uint(sc), __float_as_uint(sc));
+#pragma unroll
+                for (int p = 0; p < Ro::PIECES; ++p) {
+                    mm_landed(v[p]);
+                    if (p * 16 < width) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) tot[p][i] = f2_fma(f2_pack(v[p][2 * i], v[p][2 * i + 1]), ss, tot[p][i]);
+                    }
+                }
+                x.next();
                 d.next();
                 ++round;
             }
-            const int o = ot * ROWS + row;
+            const int o = ot * ROWS + row, left = a.g.M - m0 - n0;      // rows of x that there are
             if (s.part < 0) {
-                if (o < l.O) {
-                    const float bias = a.g.bias ? static_cast<float>(static_cast<const T*>(a.g.bias)[o]) : 0.f;
-                    T* y = static_cast<T*>(a.g.y) + static_cast<long long>(m0 + n0) * a.g.ldy + o;
+                const float bias = a.g.bias && o < l.O ? static_cast<float>(static_cast<const T*>(a.g.bias)[o]) : 0.f;
+                T* y = static_cast<T*>(a.g.y) + static_cast<long long>(m0 + n0) * a.g.ldy;
+                if (width <= left && ot * ROWS + ROWS <= l.O && (a.g.ldy & 1) == 0) {
+                    // neighbouring lanes trade: each stores two columns of y in one of two rows
+                    y += (lane & 1) * a.g.ldy + (o & ~1);
+#pragma unroll
+                    for (int p = 0; p < Ro::PIECES; ++p)
+                        if (p * 16 < width) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                uint32_t lo, hi;
+                                f2_split(tot[p][i], lo, hi);
+                                const uint32_t both = Ty::round2(__uint_as_float(lo) + bias, __uint_as_float(hi) + bias), other = __shfl_xor_sync(0xffffffffu, both, 1);
+                                *reinterpret_cast<uint32_t*>(y) = lane & 1 ? __byte_perm(other, both, 0x7632) : __byte_perm(both, other, 0x5410);
+                                y += 2 * a.g.ldy;
+                            }
+                        }
+                } else if (o < l.O) {
+                    y += o;
 #pragma unroll
                     for (int p = 0; p < Ro::PIECES; ++p)
 #pragma unroll
@@ -362,8 +389,8 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                             uint32_t lo, hi;
                             f2_split(tot[p][i], lo, hi);
                             const int m = p * 16 + 2 * i;
-                            if (m < width && m0 + n0 + m < a.g.M) y[m * a.g.ldy] = Ty::round(__uint_as_float(lo) + bias);
-                            if (m < width && m0 + n0 + m + 1 < a.g.M) y[(m + 1) * a.g.ldy] = Ty::round(__uint_as_float(hi) + bias);
+                            if (m < width && m < left) y[m * a.g.ldy] = Ty::round(__uint_as_float(lo) + bias);
+                            if (m < width && m + 1 < left) y[(m + 1) * a.g.ldy] = Ty::round(__uint_as_float(hi) + bias);
                         }
                 }
             } else {
@@ -375,8 +402,8 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         uint32_t lo, hi;
                         f2_split(tot[p][i], lo, hi);
                         const int m = p * 16 + 2 * i;
-                        if (m < width && m0 + n0 + m < a.g.M) out[m * ROWS] = __uint_as_float(lo);
-                        if (m < width && m0 + n0 + m + 1 < a.g.M) out[(m + 1) * ROWS] = __uint_as_float(hi);
+                        if (m < width && m < left) out[m * ROWS] = __uint_as_float(lo);
+                        if (m < width && m + 1 < left) out[(m + 1) * ROWS] = __uint_as_float(hi);
                     }
             }
         }
@@ -384,7 +411,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     mm_fence_before();
     __syncthreads();
     mm_fence_after();
-    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Ro::COLUMNS) : "memory");
+    if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLUMNS) : "memory");
 }
 
 // Adds the parts of the tiles that were cut, in the order of the reduction.  blockIdx.x: the run whose beginning is the first cut in its tile.
@@ -406,12 +433,11 @@ __global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ Mm
     for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rows * ROWS; i += gridDim.y * blockDim.x) {
         const int m = i / ROWS, r = i % ROWS, o = ot * ROWS + r;
         if (o >= a.g.l.O) continue;
-        float v = 0.f;
-        // the tile is what run - 1 ends in (or began in, where it is shorter than a tile), and what the others begin in
-        for (int c = run - 1; c <= last; ++c) {
-            const long long b = static_cast<long long>(c) * a.per;
-            v += part[(static_cast<size_t>(2 * c + (b < beg)) * a.n + m) * ROWS + r];
-        }
+        // the tile is what run - 1 ends in (or begins in, at the tile's own beginning), and what the others begin in
+        const size_t place = static_cast<size_t>(a.n) * ROWS, at = static_cast<size_t>(m) * ROWS + r;
+        float v = part[(2 * (run - 1) + (cut - a.per < beg)) * place + at];
+#pragma unroll 4
+        for (int c = run; c <= last; ++c) v += part[2 * c * place + at];
         if (a.g.bias) v += static_cast<float>(static_cast<const T*>(a.g.bias)[o]);
         static_cast<T*>(a.g.y)[(m0 + m) * a.g.ldy + o] = W4Type<F16>::round(v);
     }
@@ -450,7 +476,6 @@ bool plan(MmaTiles& a, int sms)
     a.waves = static_cast<int>(tiles % a.ctas == 0 ? tiles / a.ctas : tiles / a.ctas > 0 ? tiles / a.ctas - 1 : 0);
     const long long steps = (tiles - static_cast<long long>(a.waves) * a.ctas) * l.cbs;
     a.per = static_cast<int>((steps + a.ctas - 1) / a.ctas);
-    a.group_blocks = l.group > W4_COLS ? l.group / W4_COLS : 1;
     return true;
 }
 
@@ -458,10 +483,10 @@ template <bool F16, int NG, bool ZEROS, bool FEW>
 int launch(const CUtensorMap& tx, const MmaTiles& a, cudaStream_t st)
 {
     auto kernel = w4_mma_kernel<F16, NG, ZEROS, FEW>;
-    const int smem = 1024 + X_STAGES * a.n * 256 + Roles<FEW>::W_STAGES * BLOCKS * a.g.l.block;
+    const int smem = 1024 + RING * a.n * 256 + Roles<FEW>::W_STAGES * BLOCKS * a.g.l.block;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
     int rc = launch_dependent(kernel, dim3(a.ctas), dim3(Roles<FEW>::WARPS * 32), smem, st, tx, a);
-    if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n >= 64 ? 4 : 1), dim3(256), 0, st, a);
+    if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n * ROWS / 512), dim3(256), 0, st, a);
     return rc;
 }
 template <bool F16, bool FEW>
