@@ -171,30 +171,30 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     if (warp < 4) {
         registers<false, 40>();
         if (warp == 0) {
-            if (lane == 0) {
-                Turn<RING> x;
-                int issued = 0;
-                while (s.next(a)) {
-                    int mt, ot;
-                    tile_place(a, s.tile, mt, ot);
-                    const int m0 = mt * a.n, rows = min(a.n, (a.g.M - m0 + 31) & ~31);
-                    for (int c = s.c0; c < s.c1; ++c) {
-                        wait(&done[x.at], x.phase ^ 1);
+            Turn<RING> x;
+            unsigned limit = 1u << 20;
+            int issued = 0;
+            while (s.next(a)) {
+                int mt, ot;
+                tile_place(a, s.tile, mt, ot);
+                for (int c = s.c0; c < s.c1; ++c) {
+                    mm_wait_uniform(&done[x.at], x.phase ^ 1, limit);
+                    if (mm_elect()) {
                         unsigned char* to = smem + static_cast<size_t>(x.at) * a.n * 256;
-                        mbar_expect_tx(&full[x.at], rows * 256);
-                        for (int h = 0; h < 2; ++h)
-                            for (int r = 0; r < rows; r += 32) tma_load_2d(to + (h * a.n + r) * 128, &tx, &full[x.at], c * W4_COLS + h * 64, m0 + r);
-                        x.next();
-                        ++issued;
+                        mbar_expect_tx(&full[x.at], a.n * 256);
+                        tma_load_2d(to, &tx, &full[x.at], c * W4_COLS, mt * a.n);
+                        tma_load_2d(to + a.n * 128, &tx, &full[x.at], c * W4_COLS + 64, mt * a.n);
                     }
-                }
-                for (int i = 0; i < RING && i < issued; ++i) {      // no copy outlives the CTA
-                    x.at = x.at == 0 ? RING - 1 : x.at - 1;
-                    if (x.at == RING - 1) x.phase ^= 1;
-                    wait(&full[x.at], x.phase);
+                    x.next();
+                    ++issued;
                 }
             }
-            __syncwarp();
+            for (int i = 0; i < RING && i < issued; ++i) {      // no copy outlives the CTA
+                x.at = x.at == 0 ? RING - 1 : x.at - 1;
+                if (x.at == RING - 1) x.phase ^= 1;
+                mm_wait_uniform(&full[x.at], x.phase, limit);
+            }
+            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         } else if (warp == 1) {
             Turn<RING> x;
             Turn<2> d;
@@ -443,8 +443,8 @@ __global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ Mm
     }
 }
 
-// Tensor map of the rows of x, fetched in boxes of 32 rows x 64 columns.
-bool encode_x(CUtensorMap* tm, const W4Gemm& g, bool f16)
+// Tensor map of the rows of x, fetched in boxes of n rows x 64 columns.
+bool encode_x(CUtensorMap* tm, const W4Gemm& g, int n, bool f16)
 {
     typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                            CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -458,7 +458,7 @@ bool encode_x(CUtensorMap* tm, const W4Gemm& g, bool f16)
     if (!fn) return false;
     const long long pitch = g.M == 1 ? (g.l.K + 7) & ~7 : g.ldx;       // one row: any pitch that the map takes
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(g.l.K), static_cast<cuuint64_t>(g.M)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
-    const cuuint32_t box[2] = {64, 32}, es[2] = {1, 1};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(n)}, es[2] = {1, 1};
     return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(g.x), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -516,7 +516,7 @@ int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t 
     a.part = part;
     CUtensorMap tx;
     if (!plan(a, sms)) return BS_ERR_UNSUPPORTED;
-    if (!encode_x(&tx, g, f16)) return BS_ERR_CUDA;
+    if (!encode_x(&tx, g, a.n, f16)) return BS_ERR_CUDA;
     if (a.n <= 64) return f16 ? launch_group<true, true>(tx, a, st) : launch_group<false, true>(tx, a, st);
     return f16 ? launch_group<true, false>(tx, a, st) : launch_group<false, false>(tx, a, st);
 }
