@@ -4,7 +4,7 @@
 // core in an accumulator of their own, and warps with the running totals in registers take them over, scaled in 32 bits, while the next group is
 // multiplied.  Folding the scale in would round every weight and double the error of the result.
 //
-// Roles of a CTA, one per SM: tensor copies of x, bulk copies of weight blocks, MMA issue, warps that expand a row a thread into tensor memory, warps that scale
+// Roles of a CTA, one per SM: tensor copies of x and of the weights' blocks, MMA issue, warps that expand a row a thread into tensor memory, warps that scale
 // and add.  A step is 128 columns.  The MMA warp's waits and commits, 100 to 160 cycles each, would cost more than the 512 cycles of a step's MMAs:
 // whatever a step needs (x, its expanded weights, and with one group a step a free accumulator) arrives at one barrier, and one commit frees
 // all of it again.
@@ -22,7 +22,7 @@ namespace bs {
 namespace {
 
 constexpr int ROWS = 128, BLOCKS = ROWS / W4_ROWS;      // of a tile
-constexpr int RING = 4, SCALE_SLOTS = 32;         // steps on their way: stages of x, buffers of expanded weights
+constexpr int RING = 4, SCALE_SLOTS = 32;         // stages of x: steps on their way
 
 struct MmaTiles {
     W4Gemm g;
@@ -121,7 +121,8 @@ template <bool FEW> struct Roles {
     static constexpr int N = FEW ? 64 : 128;                    // most rows of x in a tile
     static constexpr int PIECES = N * 4 / SCALE / 16;           // 16 columns each, of a thread's totals
 };
-constexpr int TMEM_COLUMNS = 512, TMEM_A = 256;                 // two accumulators of N columns; RING buffers of 64
+// Three accumulators of N columns (reading one takes 750 cycles while the next one's MMAs run: with two the MMAs wait for it), two buffers of 64 of weights.
+constexpr int SUMS = 3, TMEM_COLUMNS = 512, TMEM_A = 384;
 template <bool MORE, int N> __device__ __forceinline__ void registers()
 {
     if (MORE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -129,7 +130,7 @@ template <bool MORE, int N> __device__ __forceinline__ void registers()
 }
 
 template <bool F16, int NG, bool ZEROS, bool FEW>
-__global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ MmaTiles a)
+__global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const __grid_constant__ CUtensorMap tx, const __grid_constant__ CUtensorMap tw, const __grid_constant__ MmaTiles a)
 {
     typedef W4Type<F16> Ty;
     typedef typename Ty::T T;
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     extern __shared__ unsigned char raw[];
     // x [RING][2][n][128 bytes], swizzled by address: from a multiple of 1024 on; weights [WS][BLOCKS][BLOCK]
     unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
-    __shared__ uint64_t full[RING], done[RING], w_full[WS], w_empty[WS], d_full[2], d_empty[2];     // the last two where a step has several groups
+    __shared__ uint64_t full[RING], done[RING], w_full[WS], w_empty[WS], d_full[SUMS], d_empty[SUMS];     // the last two where a step has several groups
     __shared__ float scales[SCALE_SLOTS][ROWS];
     __shared__ uint32_t tmem_slot;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -151,15 +152,16 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     } else if (warp == 0 && lane == 0) {
         for (int s = 0; s < RING; ++s) { mbar_init(&full[s], 5 + (NG == 1 ? Ro::SCALE : 0)); mbar_init(&done[s], 1); }
         for (int s = 0; s < WS; ++s) { mbar_init(&w_full[s], 1); mbar_init(&w_empty[s], 4); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&d_full[s], 1); mbar_init(&d_empty[s], Ro::SCALE); }
+        for (int s = 0; s < SUMS; ++s) { mbar_init(&d_full[s], 1); mbar_init(&d_empty[s], Ro::SCALE); }
         fence_barrier_init();
         fence_proxy_async();
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tx)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tw)) : "memory");
     }
     __syncthreads();
     mm_fence_after();
     const uint32_t tmem = tmem_slot, tmem_a = tmem + TMEM_A;
-    const unsigned char* matrix = dependent_begin(a.g.w);
+    dependent_begin(a.g.w);
     bool late = false;          // a wait ran out: later ones are not waited for
     auto wait = [&](uint64_t* bar, unsigned parity) {
         if (!late && !mm_wait(bar, parity)) {
@@ -197,7 +199,8 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
             if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         } else if (warp == 1) {
             Turn<RING> x;
-            Turn<2> d;
+            Turn<2> ab;
+            Turn<SUMS> d;
             unsigned limit = 1u << 20;
             const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
             // K-major rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group
@@ -210,7 +213,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                 for (int c = s.c0; c < s.c1; ++c) {
                     mm_wait_uniform(&full[x.at], x.phase, limit);
                     mm_fence_after();
-                    const uint32_t xs = base + static_cast<uint32_t>(x.at * a.n * 16), as = tmem_a + x.at * 64;
+                    const uint32_t xs = base + static_cast<uint32_t>(x.at * a.n * 16), as = tmem_a + ab.at * 64;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
                         if (NG > 1) {
@@ -229,21 +232,24 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                     }
                     mm_commit(&done[x.at]);
                     x.next();
+                    ab.next();
                 }
             }
             if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         } else if (warp == 2) {
+            // the blocks of eight rows of blocks in one copy: as copies of their own they took 130 cycles each to start, twice the time of a step
             Turn<WS> w;
+            unsigned limit = 1u << 20;
             int issued = 0;
             while (s.next(a)) {
                 int mt, ot;
                 tile_place(a, s.tile, mt, ot);
-                const int rb = ot * BLOCKS, have = min(BLOCKS, l.rbs - rb);
                 for (int c = s.c0; c < s.c1; ++c) {
-                    wait(&w_empty[w.at], w.phase ^ 1);
-                    if (lane == 0) mbar_expect_tx(&w_full[w.at], have * BLOCK);
-                    __syncwarp();
-                    if (lane < have) mm_bulk(wsm + (w.at * BLOCKS + lane) * BLOCK, matrix + (static_cast<size_t>(rb + lane) * l.cbs + c) * BLOCK, BLOCK, &w_full[w.at]);
+                    mm_wait_uniform(&w_empty[w.at], w.phase ^ 1, limit);
+                    if (mm_elect()) {
+                        mbar_expect_tx(&w_full[w.at], BLOCKS * BLOCK);
+                        tma_load_2d(wsm + w.at * BLOCKS * BLOCK, &tw, &w_full[w.at], c * (BLOCK / 8), ot * BLOCKS);
+                    }
                     w.next();
                     ++issued;
                 }
@@ -251,9 +257,9 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
             for (int i = 0; i < WS && i < issued; ++i) {
                 w.at = w.at == 0 ? WS - 1 : w.at - 1;
                 if (w.at == WS - 1) w.phase ^= 1;
-                wait(&w_full[w.at], w.phase);
+                mm_wait_uniform(&w_full[w.at], w.phase, limit);
             }
-            __syncwarp();
+            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         }
     } else if (warp < 4 + Ro::EXPAND) {
         registers<false, FEW ? 104 : 72>();
@@ -261,11 +267,11 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
         const int team = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, r = row & 15;
         const uint32_t mine = smem_u32(wsm) + (row >> 4) * BLOCK, lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         Turn<WS> w;
-        Turn<RING> ab;
+        Turn<RING> x;
         int round = 0;
         while (s.next(a)) {
             for (int c = s.c0; c < s.c1; ++c) {
-                if ((ab.at & 1) == team) {
+                if ((x.at & 1) == team) {
                     wait(&w_full[w.at], w.phase);
                     const uint32_t block = mine + w.at * BLOCKS * BLOCK;
                     uint4 code[4];
@@ -281,9 +287,9 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         zero[g] = 8;
                         if (ZEROS) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(zero[g]) : "r"(e + 4) : "memory");
                     }
-                    wait(&done[ab.at], ab.phase ^ 1);
+                    wait(&done[x.at ^ 2], x.at < 2 ? x.phase ^ 1 : x.phase);      // the step before the last one
                     mm_fence_after();
-                    // the step that had this buffer is done and all rounds before its last two are scaled: the slots of these are free
+                    // the step that had this buffer is done and all rounds before its last three are scaled: the slots of these are free
 #pragma unroll
                     for (int g = 0; g < NG; ++g) scales[(round + g) % SCALE_SLOTS][row] = Ty::lo(scale[g]);
 #pragma unroll
@@ -298,19 +304,19 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
 #pragma unroll
                                 for (int i = 0; i < 4; ++i) v[16 * j + 4 * t + i] = p[i];
                             }
-                        w4_st32(tmem_a + ab.at * 64 + h * 32 + lanes, v);
+                        w4_st32(tmem_a + team * 64 + h * 32 + lanes, v);
                     }
                     mm_st_wait();
                     mm_fence_before();
                     __syncwarp();
                     if (lane == 0) {
-                        mm_arrive(&full[ab.at]);
+                        mm_arrive(&full[x.at]);
                         mm_arrive(&w_empty[w.at]);
                     }
                 }
                 round += NG;
                 w.next();
-                ab.next();
+                x.next();
             }
         }
     } else {
@@ -319,12 +325,10 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
         const int half = (warp - 4 - Ro::EXPAND) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
         Turn<RING> x;           // of the steps, where each is a round
-        Turn<2> d;
+        Turn<SUMS> d;
         int round = 0;
-        if (NG == 1 && lane == 0) {     // the accumulators of the first two steps are free
-            mm_arrive(&full[0]);
-            mm_arrive(&full[1]);
-        }
+        if (NG == 1 && lane == 0)       // the accumulators of the first steps are free
+            for (int i = 0; i < SUMS; ++i) mm_arrive(&full[i]);
         while (s.next(a)) {
             int mt, ot;
             tile_place(a, s.tile, mt, ot);
@@ -340,14 +344,19 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                 mm_fence_after();
                 const uint32_t from = tmem + d.at * Ro::N + n0 + lanes;
                 uint32_t v[Ro::PIECES][16];
+                if (width == Ro::PIECES * 16) {
+                    mm_ld32(from, reinterpret_cast<uint32_t (&)[32]>(v[0]));
+                    mm_ld32(from + 32, reinterpret_cast<uint32_t (&)[32]>(v[2]));
+                } else {
 #pragma unroll
-                for (int p = 0; p < Ro::PIECES; ++p)
-                    if (p * 16 < width) mm_ld16(from + p * 16, v[p]);
+                    for (int p = 0; p < Ro::PIECES; ++p)
+                        if (p * 16 < width) mm_ld16(from + p * 16, v[p]);
+                }
                 const float sc = scales[round % SCALE_SLOTS][row];
                 mm_ld_wait();
                 mm_fence_before();
                 __syncwarp();
-                if (lane == 0) mm_arrive(NG == 1 ? &full[(x.at + 2) % RING] : &d_empty[d.at]);      // the accumulator is free for the round after the next
+                if (lane == 0) mm_arrive(NG == 1 ? &full[(x.at + SUMS) % RING] : &d_empty[d.at]);
                 const u64 ss = f2_pack(__float_as_uint(sc), __float_as_uint(sc));
 #pragma unroll
                 for (int p = 0; p < Ro::PIECES; ++p) {
@@ -443,24 +452,40 @@ __global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ Mm
     }
 }
 
-// Tensor map of the rows of x, fetched in boxes of n rows x 64 columns.
-bool encode_x(CUtensorMap* tm, const W4Gemm& g, int n, bool f16)
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn()
 {
-    typedef CUresult (*Fn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
-                           CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static Fn fn = nullptr;
+    static EncodeFn fn = nullptr;
     static std::once_flag once;
     std::call_once(once, [] {
         void* q = nullptr;
         cudaDriverEntryPointQueryResult r;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &q, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess) fn = reinterpret_cast<Fn>(q);
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &q, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess) fn = reinterpret_cast<EncodeFn>(q);
     });
+    return fn;
+}
+// Tensor map of the rows of x, fetched in boxes of n rows x 64 columns.
+bool encode_x(CUtensorMap* tm, const W4Gemm& g, int n, bool f16)
+{
+    const EncodeFn fn = encode_fn();
     if (!fn) return false;
     const long long pitch = g.M == 1 ? (g.l.K + 7) & ~7 : g.ldx;       // one row: any pitch that the map takes
     const cuuint64_t dims[2] = {static_cast<cuuint64_t>(g.l.K), static_cast<cuuint64_t>(g.M)}, strides[1] = {static_cast<cuuint64_t>(pitch) * 2};
     const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(n)}, es[2] = {1, 1};
     return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(g.x), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Tensor map of the prepared weights: rows of blocks, in elements of eight bytes so that a block is a box's width; fetched eight rows of blocks at a time.
+bool encode_w(CUtensorMap* tm, const W4Gemm& g)
+{
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t width = static_cast<cuuint64_t>(g.l.cbs) * g.l.block;
+    const cuuint64_t dims[2] = {width / 8, static_cast<cuuint64_t>(g.l.rbs)}, strides[1] = {width};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(g.l.block / 8), BLOCKS}, es[2] = {1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<unsigned char*>(g.w), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool plan(MmaTiles& a, int sms)
@@ -480,21 +505,21 @@ bool plan(MmaTiles& a, int sms)
 }
 
 template <bool F16, int NG, bool ZEROS, bool FEW>
-int launch(const CUtensorMap& tx, const MmaTiles& a, cudaStream_t st)
+int launch(const CUtensorMap& tx, const CUtensorMap& tw, const MmaTiles& a, cudaStream_t st)
 {
     auto kernel = w4_mma_kernel<F16, NG, ZEROS, FEW>;
     const int smem = 1024 + RING * a.n * 256 + Roles<FEW>::W_STAGES * BLOCKS * a.g.l.block;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    int rc = launch_dependent(kernel, dim3(a.ctas), dim3(Roles<FEW>::WARPS * 32), smem, st, tx, a);
+    int rc = launch_dependent(kernel, dim3(a.ctas), dim3(Roles<FEW>::WARPS * 32), smem, st, tx, tw, a);
     if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n * ROWS / 512), dim3(256), 0, st, a);
     return rc;
 }
 template <bool F16, bool FEW>
-int launch_group(const CUtensorMap& tx, const MmaTiles& a, cudaStream_t st)
+int launch_group(const CUtensorMap& tx, const CUtensorMap& tw, const MmaTiles& a, cudaStream_t st)
 {
     const int ng = a.g.l.group == 32 ? 4 : a.g.l.group == 64 ? 2 : 1;
-    if (a.g.l.zeros) return ng == 4 ? launch<F16, 4, true, FEW>(tx, a, st) : ng == 2 ? launch<F16, 2, true, FEW>(tx, a, st) : launch<F16, 1, true, FEW>(tx, a, st);
-    return ng == 4 ? launch<F16, 4, false, FEW>(tx, a, st) : ng == 2 ? launch<F16, 2, false, FEW>(tx, a, st) : launch<F16, 1, false, FEW>(tx, a, st);
+    if (a.g.l.zeros) return ng == 4 ? launch<F16, 4, true, FEW>(tx, tw, a, st) : ng == 2 ? launch<F16, 2, true, FEW>(tx, tw, a, st) : launch<F16, 1, true, FEW>(tx, tw, a, st);
+    return ng == 4 ? launch<F16, 4, false, FEW>(tx, tw, a, st) : ng == 2 ? launch<F16, 2, false, FEW>(tx, tw, a, st) : launch<F16, 1, false, FEW>(tx, tw, a, st);
 }
 
 }  // namespace
@@ -514,11 +539,11 @@ int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t 
     MmaTiles a{};
     a.g = g;
     a.part = part;
-    CUtensorMap tx;
+    CUtensorMap tx, tw;
     if (!plan(a, sms)) return BS_ERR_UNSUPPORTED;
-    if (!encode_x(&tx, g, a.n, f16)) return BS_ERR_CUDA;
-    if (a.n <= 64) return f16 ? launch_group<true, true>(tx, a, st) : launch_group<false, true>(tx, a, st);
-    return f16 ? launch_group<true, false>(tx, a, st) : launch_group<false, false>(tx, a, st);
+    if (!encode_x(&tx, g, a.n, f16) || !encode_w(&tw, g)) return BS_ERR_CUDA;
+    if (a.n <= 64) return f16 ? launch_group<true, true>(tx, tw, a, st) : launch_group<false, true>(tx, tw, a, st);
+    return f16 ? launch_group<true, false>(tx, tw, a, st) : launch_group<false, false>(tx, tw, a, st);
 }
 
 }  // namespace bs
