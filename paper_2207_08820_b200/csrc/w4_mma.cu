@@ -403,16 +403,18 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         }
                 }
             } else {
+                // rows of x that are not there are written too: their places are the tile's
                 float* out = a.part + (static_cast<size_t>(s.part) * a.n + n0) * ROWS + row;
 #pragma unroll
                 for (int p = 0; p < Ro::PIECES; ++p)
+                    if (p * 16 < width) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t lo, hi;
-                        f2_split(tot[p][i], lo, hi);
-                        const int m = p * 16 + 2 * i;
-                        if (m < width && m < left) out[m * ROWS] = __uint_as_float(lo);
-                        if (m < width && m + 1 < left) out[(m + 1) * ROWS] = __uint_as_float(hi);
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t lo, hi;
+                            f2_split(tot[p][i], lo, hi);
+                            out[(p * 16 + 2 * i) * ROWS] = __uint_as_float(lo);
+                            out[(p * 16 + 2 * i + 1) * ROWS] = __uint_as_float(hi);
+                        }
                     }
             }
         }
@@ -423,33 +425,35 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
     if (warp == 3) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLUMNS) : "memory");
 }
 
-// Adds the parts of the tiles that were cut, in the order of the reduction.  blockIdx.x: the run whose beginning is the first cut in its tile.
+// Adds the parts of the tiles that were cut, in the order of the reduction.  blockIdx.x: the run whose beginning is the first cut in its tile.  A thread: four
+// columns of y in one row.
 template <bool F16>
 __global__ void __launch_bounds__(256) w4_join_kernel(const __grid_constant__ MmaTiles a)
 {
     typedef typename W4Type<F16>::T T;
     const float* part = dependent_begin(a.part);
-    const int cbs = a.g.l.cbs, run = blockIdx.x + 1;
-    const long long steps = static_cast<long long>(a.mts) * a.ots * cbs - static_cast<long long>(a.waves) * a.ctas * cbs;
-    const long long cut = static_cast<long long>(run) * a.per;
-    if (cut >= steps || cut % cbs == 0) return;
-    const long long t = cut / cbs, beg = t * cbs, end = beg + cbs;
-    if (cut - a.per > beg) return;          // an earlier run's beginning lies in this tile
-    const int last = static_cast<int>((end - 1) / a.per);
+    const int cbs = a.g.l.cbs, run = blockIdx.x + 1, steps = (a.mts * a.ots - a.waves * a.ctas) * cbs, cut = run * a.per;       // below 2^31, as all steps are
+    const int t = cut / cbs, beg = t * cbs;
+    if (cut >= steps || cut == beg || cut - a.per > beg) return;       // no cut, or an earlier run's beginning lies in this tile
+    const int last = (beg + cbs - 1) / a.per;
     int mt, ot;
-    tile_place(a, static_cast<int>(t) + a.waves * a.ctas, mt, ot);
-    const int m0 = mt * a.n, rows = min(a.n, a.g.M - m0);
-    for (int i = blockIdx.y * blockDim.x + threadIdx.x; i < rows * ROWS; i += gridDim.y * blockDim.x) {
-        const int m = i / ROWS, r = i % ROWS, o = ot * ROWS + r;
-        if (o >= a.g.l.O) continue;
-        // the tile is what run - 1 ends in (or begins in, at the tile's own beginning), and what the others begin in
-        const size_t place = static_cast<size_t>(a.n) * ROWS, at = static_cast<size_t>(m) * ROWS + r;
-        float v = part[(2 * (run - 1) + (cut - a.per < beg)) * place + at];
+    tile_place(a, t + a.waves * a.ctas, mt, ot);
+    const int m0 = mt * a.n, i = blockIdx.y * blockDim.x + threadIdx.x, m = i / (ROWS / 4), r = i % (ROWS / 4) * 4, o = ot * ROWS + r;
+    if (m >= min(a.n, a.g.M - m0) || o >= a.g.l.O) return;
+    // the tile is what run - 1 ends in (or begins in, at the tile's own beginning), and what the others begin in
+    const size_t place = static_cast<size_t>(a.n) * ROWS, at = static_cast<size_t>(m) * ROWS + r;
+    float4 v = *reinterpret_cast<const float4*>(part + (2 * (run - 1) + (cut - a.per < beg)) * place + at);
 #pragma unroll 4
-        for (int c = run; c <= last; ++c) v += part[2 * c * place + at];
-        if (a.g.bias) v += static_cast<float>(static_cast<const T*>(a.g.bias)[o]);
-        static_cast<T*>(a.g.y)[(m0 + m) * a.g.ldy + o] = W4Type<F16>::round(v);
+    for (int c = run; c <= last; ++c) {
+        const float4 w = *reinterpret_cast<const float4*>(part + 2 * c * place + at);
+        v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
     }
+    T* y = static_cast<T*>(a.g.y) + (m0 + m) * a.g.ldy + o;
+    const T* bias = static_cast<const T*>(a.g.bias);
+    const float sums[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (o + k < a.g.l.O) y[k] = W4Type<F16>::round(bias ? sums[k] + static_cast<float>(bias[o + k]) : sums[k]);
 }
 
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -511,7 +515,7 @@ int launch(const CUtensorMap& tx, const CUtensorMap& tw, const MmaTiles& a, cuda
     const int smem = 1024 + RING * a.n * 256 + Roles<FEW>::W_STAGES * BLOCKS * a.g.l.block;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
     int rc = launch_dependent(kernel, dim3(a.ctas), dim3(Roles<FEW>::WARPS * 32), smem, st, tx, tw, a);
-    if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n * ROWS / 512), dim3(256), 0, st, a);
+    if (rc == BS_OK && a.per > 0 && a.ctas > 1) rc = launch_dependent(w4_join_kernel<F16>, dim3(a.ctas - 1, a.n * ROWS / 1024), dim3(256), 0, st, a);
     return rc;
 }
 template <bool F16, bool FEW>

@@ -12,6 +12,32 @@ template <> __device__ __forceinline__ float to_f(float v) { return v; }
 template <> __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
 template <> __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 
+// Least and largest of V values and 0 (a NaN does not count): two of 16 bits at a time.
+template <int V>
+__device__ __forceinline__ void extremes(const float* v, float& lo, float& hi)
+{
+    lo = hi = 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) { lo = fminf(lo, v[e]); hi = fmaxf(hi, v[e]); }
+}
+template <int V, typename T2>
+__device__ __forceinline__ void extremes2(const T2* v, T2 zero, float& lo, float& hi)
+{
+    T2 l = zero, h = zero;
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) { l = __hmin2(l, v[e]); h = __hmax2(h, v[e]); }
+    lo = fminf(to_f(l.x), to_f(l.y));
+    hi = fmaxf(to_f(h.x), to_f(h.y));
+}
+template <int V> __device__ __forceinline__ void extremes(const __half* v, float& lo, float& hi)
+{
+    extremes2<V>(reinterpret_cast<const __half2*>(v), __floats2half2_rn(0.f, 0.f), lo, hi);
+}
+template <int V> __device__ __forceinline__ void extremes(const __nv_bfloat16* v, float& lo, float& hi)
+{
+    extremes2<V>(reinterpret_cast<const __nv_bfloat162*>(v), __floats2bfloat162_rn(0.f, 0.f), lo, hi);
+}
+
 template <typename S> struct Step;
 template <> struct Step<__half> {
     static constexpr float MAX = 65504.f;
@@ -22,85 +48,110 @@ template <> struct Step<__nv_bfloat16> {
     static __device__ __nv_bfloat16 round(float v) { return __float2bfloat16_rn(v); }
 };
 
-// Nearest whole number of the exact quotient w / s (s > 0), ties to even.  The rounded quotient can sit on a tie that the exact one misses: the
-// residual, exact in one fused multiply-add where the quotient is small enough to matter, tells the side.
-__device__ __forceinline__ float nearest_quotient(float w, float s)
-{
-    const float q = __fdiv_rn(w, s), n = rintf(q);
-    if (fabsf(q) < 64.f && fabsf(q - truncf(q)) == 0.5f) {
-        const float left = __fmaf_rn(-q, s, w);
-        if (left > 0.f) return ceilf(q);
-        if (left < 0.f) return floorf(q);
+// clip(round_half_even(w / s)) of the Section IV quantiser for the values of one group, of the exact quotient; a NaN gets the lowest code (fmaxf returns the
+// other operand).  The quotient is w times the reciprocal, corrected once by its residual: exact where it is a tie, because a tie is a float, and
+// for weights of 16 bits on the right side everywhere else, because a quotient of theirs that is no tie is 2^-17 of it away.  For float32
+// weights the exact residual tells the side of what rounds to a tie.  Groups with infinite weights or a scale whose reciprocal a float does not
+// hold well take the division, which made the quantiser four times as slow as its bytes.
+template <bool F32>
+struct GroupCodes {
+    float s, r, lo, hi;
+    bool divide;
+    // The whole number in the last places of a float: whole() of it, or its low byte.
+    static constexpr float MAGIC = 12582912.f;      // 1.5 * 2^23: a last place is one
+    template <bool DIVIDE>
+    __device__ __forceinline__ float place(float w) const
+    {
+        float q = DIVIDE ? __fdiv_rn(w, s) : w * r;
+        if (!DIVIDE) q = fmaf(fmaf(-q, s, w), r, q);
+        q = fminf(fmaxf(q, lo), hi);
+        float m = q + MAGIC;
+        if ((F32 || DIVIDE) && fabsf(q - (m - MAGIC)) == 0.5f) {
+            const float left = __fmaf_rn(-q, s, w);
+            if (left != 0.f) m = (q + copysignf(0.5f, left)) + MAGIC;
+        }
+        return m;
     }
-    return n;
-}
+    static __device__ __forceinline__ int whole(float m) { return static_cast<int>(__float_as_uint(m) - __float_as_uint(MAGIC)); }
+};
 
-// The scale of a group from its extremes, and its zero point.
-template <typename S, bool ZEROS>
-__device__ __forceinline__ void group_step(float lo, float hi, S& scale, float& s, float& z)
+// The scale of a group from its extremes, its zero point, and what makes codes of its values (less the zero point).
+template <typename S, bool ZEROS, bool F32>
+__device__ __forceinline__ GroupCodes<F32> group_step(float lo, float hi, S& scale, int& z)
 {
     // clip in place of overflow: a group whose scale the type cannot hold gets the largest one (fminf also where hi - lo is infinite)
-    const float wide = ZEROS ? __fdiv_rn(__fsub_rn(hi, lo), 15.f) : __fdiv_rn(fmaxf(hi, -lo), 7.f);
-    scale = Step<S>::round(fminf(wide, Step<S>::MAX));
-    s = to_f(scale);
-    z = ZEROS && s > 0.f ? fminf(fmaxf(nearest_quotient(-lo, s), 0.f), 15.f) : 0.f;
+    const float span = ZEROS ? __fsub_rn(hi, lo) : fmaxf(hi, -lo);
+    scale = Step<S>::round(fminf(__fdiv_rn(span, ZEROS ? 15.f : 7.f), Step<S>::MAX));
+    GroupCodes<F32> g;
+    g.s = to_f(scale);
+    g.divide = !(g.s > 1e-30f && g.s < 1e30f && span < 1e37f);
+    g.r = g.divide ? 0.f : __frcp_rn(g.s);
+    g.lo = ZEROS ? 0.f : -8.f;
+    g.hi = ZEROS ? 15.f : 7.f;
+    z = 0;
+    if (!(g.s > 0.f)) {     // every code is the zero point
+        g.divide = false;
+        g.lo = g.hi = 0.f;
+    } else if (ZEROS) {
+        z = GroupCodes<F32>::whole(g.divide ? g.template place<true>(-lo) : g.template place<false>(-lo));
+        g.lo = static_cast<float>(-z);
+        g.hi = static_cast<float>(15 - z);
+    }
+    return g;
 }
 
-// round_half_even(clip) of the Section IV quantiser; a NaN gets the lowest code (fmaxf returns the other operand).
-template <bool ZEROS>
-__device__ __forceinline__ int group_code(float w, float s, float z)
-{
-    if (!(s > 0.f)) return static_cast<int>(z);
-    const float q = nearest_quotient(w, s) + z;
-    return ZEROS ? static_cast<int>(fminf(fmaxf(q, 0.f), 15.f)) : static_cast<int>(fminf(fmaxf(q, -8.f), 7.f));
-}
-
-// Groups of 32, 64, 128 or 256 columns of rows that allow wide loads: a thread keeps eight columns in registers, group / 8 neighbouring threads
-// share the extremes by shuffles, one pass over the weights.  Bound by HBM.
-template <typename T, typename S, bool ZEROS>
-__global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long ld, int O, int K, int group, int8_t* codes, S* scales, int8_t* zeros)
+// Groups of 32, 64, 128 or 256 columns of rows that allow wide loads: a thread keeps V columns in registers, group / V neighbouring threads share the extremes
+// by shuffles, one pass over the weights.  2^log_row threads take a row, the others of the CTA the next ones.  Bound by HBM.
+template <typename T, typename S, bool ZEROS, int V>
+__global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long ld, int O, int K, int log_group, int log_row, int8_t* codes, S* scales, int8_t* zeros)
 {
     w = dependent_begin(w);
-    constexpr int V = 8;
-    const int lanes = group / V, per_row = (K + group - 1) / group * lanes;      // threads of a row, its short last group filled up
-    const long long total = static_cast<long long>(O) * per_row;
-    const long long first = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x, step = static_cast<long long>(gridDim.x) * blockDim.x;
-    const long long rounds = (total + step - 1) / step;                     // the same for every thread: the shuffles need whole warps
-    for (long long k = 0; k < rounds; ++k) {
-        const long long i = first + k * step;
-        const int o = total >> 31 ? static_cast<int>(i / per_row) : static_cast<int>(static_cast<unsigned>(i) / static_cast<unsigned>(per_row));
-        const int u = static_cast<int>(i - static_cast<long long>(o) * per_row), c0 = u * V;
-        const bool live = i < total && c0 < K;      // K is a multiple of eight here
-        float v[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = 0.f;
-        if (live) {
-            const T* src = w + o * ld + c0;
+    const int group = 1 << log_group, lanes = group / V, G = (K + group - 1) >> log_group, units = G * lanes;     // threads of a row, its short last group filled up
+    const int rows = blockDim.x >> log_row, t = threadIdx.x & ((1 << log_row) - 1), step = gridDim.x * rows;
+    // every thread goes through the same rounds: the shuffles need whole warps
+    for (int first = blockIdx.x * rows; first < O; first += step) {
+        const int o = first + (threadIdx.x >> log_row);
+        for (int u0 = 0; u0 < units; u0 += 1 << log_row) {
+            const int u = u0 + t, c0 = u * V;
+            const bool live = o < O && c0 < K;      // K is a multiple of V here
             uint4 raw[sizeof(T) * V / 16];
+            const T* v = reinterpret_cast<const T*>(raw);
+            const uint4* src = reinterpret_cast<const uint4*>(w + o * ld + c0);
 #pragma unroll
-            for (int e = 0; e < static_cast<int>(sizeof(T)) * V / 16; ++e) raw[e] = __ldcs(reinterpret_cast<const uint4*>(src) + e);
+            for (int e = 0; e < static_cast<int>(sizeof(T)) * V / 16; ++e) raw[e] = live ? __ldcs(src + e) : make_uint4(0, 0, 0, 0);
+            float lo, hi;
+            extremes<V>(v, lo, hi);
+            for (int d = 1; d < lanes; d <<= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+            }
+            S scale;
+            int z;
+            const auto g = group_step<S, ZEROS, sizeof(T) == 4>(lo, hi, scale, z);
+            if (!live) continue;
+            uint32_t c[V];
+            // the low byte is the code's, but for the zero point
+            if (g.divide) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = to_f(reinterpret_cast<const T*>(raw)[e]);
-        }
-        float lo = 0.f, hi = 0.f;
+                for (int e = 0; e < V; ++e) c[e] = __float_as_uint(g.template place<true>(to_f(v[e])));
+            } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) { lo = fminf(lo, v[e]); hi = fmaxf(hi, v[e]); }
-        for (int d = 1; d < lanes; d <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-        }
-        S scale;
-        float s, z;
-        group_step<S, ZEROS>(lo, hi, scale, s, z);
-        if (!live) continue;
-        uint32_t out[2] = {0, 0};
+                for (int e = 0; e < V; ++e) c[e] = __float_as_uint(g.template place<false>(to_f(v[e])));
+            }
+            // 15 at most: the sum of a byte does not reach the next one (codes without zero points are signed and have z = 0)
+            uint32_t out[V / 4];
 #pragma unroll
-        for (int e = 0; e < V; ++e) out[e >> 2] |= (static_cast<uint32_t>(group_code<ZEROS>(v[e], s, z)) & 255u) << (8 * (e & 3));
-        *reinterpret_cast<uint2*>(codes + static_cast<long long>(o) * K + c0) = make_uint2(out[0], out[1]);
-        if (u % lanes == 0) {
-            const long long at = static_cast<long long>(o) * (per_row / lanes) + u / lanes;
-            scales[at] = scale;
-            if (ZEROS) zeros[at] = static_cast<int8_t>(z);
+            for (int e = 0; e < V; e += 4)
+                out[e / 4] = ZEROS ? __vadd4(__byte_perm(__byte_perm(c[e], c[e + 1], 0x0040), __byte_perm(c[e + 2], c[e + 3], 0x0040), 0x5410), z * 0x01010101u)
+                                   : __byte_perm(__byte_perm(c[e], c[e + 1], 0x0040), __byte_perm(c[e + 2], c[e + 3], 0x0040), 0x5410);
+            int8_t* to = codes + static_cast<long long>(o) * K + c0;
+            if (V == 16) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[V / 4 - 2], out[V / 4 - 1]);
+            else *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+            if ((u & (lanes - 1)) == 0) {
+                const long long at = static_cast<long long>(o) * G + u / lanes;
+                scales[at] = scale;
+                if (ZEROS) zeros[at] = static_cast<int8_t>(z);
+            }
         }
     }
 }
@@ -113,8 +164,8 @@ __global__ void __launch_bounds__(256) w4_quantise_rows_kernel(const T* w, long 
     const int lane = threadIdx.x & 31, G = (K + group - 1) / group;
     const long long total = static_cast<long long>(O) * G, step = static_cast<long long>(gridDim.x) * (blockDim.x / 32);
     for (long long i = static_cast<long long>(blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32; i < total; i += step) {
-        const int o = static_cast<int>(i / G), g = static_cast<int>(i - static_cast<long long>(o) * G);
-        const int beg = g * group, end = K - beg < group ? K : beg + group;
+        const int o = static_cast<int>(i / G);
+        const int beg = static_cast<int>(i - static_cast<long long>(o) * G) * group, end = K - beg < group ? K : beg + group;
         const T* row = w + o * ld;
         float lo = 0.f, hi = 0.f;
         for (int c = beg + lane; c < end; c += 32) {
@@ -128,9 +179,12 @@ __global__ void __launch_bounds__(256) w4_quantise_rows_kernel(const T* w, long 
             hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
         }
         S scale;
-        float s, z;
-        group_step<S, ZEROS>(lo, hi, scale, s, z);
-        for (int c = beg + lane; c < end; c += 32) codes[static_cast<long long>(o) * K + c] = static_cast<int8_t>(group_code<ZEROS>(to_f(row[c]), s, z));
+        int z;
+        const auto g = group_step<S, ZEROS, sizeof(T) == 4>(lo, hi, scale, z);
+        for (int c = beg + lane; c < end; c += 32) {
+            const float w = to_f(row[c]);
+            codes[static_cast<long long>(o) * K + c] = static_cast<int8_t>(g.whole(g.divide ? g.template place<true>(w) : g.template place<false>(w)) + z);
+        }
         if (lane == 0) {
             scales[i] = scale;
             if (ZEROS) zeros[i] = static_cast<int8_t>(z);
@@ -195,13 +249,23 @@ int quantise(const void* w, long long ld, int O, int K, int group, int8_t* codes
     const int sms = device_sm_count();
     if (sms <= 0) return BS_ERR_CUDA;
     const bool wide = group <= 256 && (group & (group - 1)) == 0 && (K & 7) == 0 && (ld * static_cast<long long>(sizeof(T))) % 16 == 0;
-    const long long threads = static_cast<long long>(O) * ceil_div(K, group) * (wide ? group / 8 : 32);
-    const long long want = (threads + 255) / 256, most = static_cast<long long>(sms) * 32;
+    const long long most = static_cast<long long>(sms) * 32;
+    if (!wide) {
+        const long long want = (static_cast<long long>(O) * ceil_div(K, group) + 7) / 8;
+        const dim3 grid(static_cast<unsigned>(want < most ? want : most));
+        return zeros ? launch_dependent(w4_quantise_rows_kernel<T, S, true>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros)
+                     : launch_dependent(w4_quantise_rows_kernel<T, S, false>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros);
+    }
+    const int V = K % 16 == 0 ? 16 : 8, units = ceil_div(K, group) * (group / V);
+    int log_group = 5, log_row = 5;
+    while (1 << log_group < group) ++log_group;
+    while (1 << log_row < units && log_row < 8) ++log_row;
+    const int want = ceil_div(O, 256 >> log_row);
     const dim3 grid(static_cast<unsigned>(want < most ? want : most));
-    if (wide) return zeros ? launch_dependent(w4_quantise_kernel<T, S, true>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros)
-                           : launch_dependent(w4_quantise_kernel<T, S, false>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros);
-    return zeros ? launch_dependent(w4_quantise_rows_kernel<T, S, true>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros)
-                 : launch_dependent(w4_quantise_rows_kernel<T, S, false>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros);
+    if (V == 16) return zeros ? launch_dependent(w4_quantise_kernel<T, S, true, 16>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros)
+                              : launch_dependent(w4_quantise_kernel<T, S, false, 16>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros);
+    return zeros ? launch_dependent(w4_quantise_kernel<T, S, true, 8>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros)
+                 : launch_dependent(w4_quantise_kernel<T, S, false, 8>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros);
 }
 
 }  // namespace
