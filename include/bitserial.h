@@ -479,7 +479,7 @@ int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K,
  *   gate, up prepared, E matrices of I rows and H columns each, group_up, zeros_up;  down  E matrices of H rows and I columns, group_down, zeros_down
  *   experts  device int32 [T][top_k] and weights device float [T][top_k]: the choices, best first
  *   workspace  bs_w4_moe_workspace_bytes(...) bytes; two calls that may run at the same time need one each
- * Supported: E up to 512, top_k up to 32, T up to 16384.  Three launches; hidden values keep 16 bits of mantissa and the range of binary32.
+ * Supported: E up to 512, top_k up to 32, T up to 16384.  Four launches; hidden values keep 16 bits of mantissa and the range of binary32.
  */
 size_t bs_w4_moe_workspace_bytes(int T, int top_k, int H, int I, long long ldx);
 int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, int H, int I, const void* gate, const void* up,

@@ -398,7 +398,7 @@ def moe_w4(x: torch.Tensor, router: torch.Tensor, gate: W4Weights, up: W4Weights
     st, y, experts, weights = native().w4_moe(x, router, gate.data, up.data, down.data, gate.O, gate.group, gate.zeros, down.group, down.zeros,
                                               _FLOAT_TYPES[gate.dtype], top_k, renormalise, out, stream)
     _check(st, "bs_w4_moe")
-    launch_count += 2
+    launch_count += 3
     return y, experts, weights
 
 

@@ -12,6 +12,8 @@
 //          entries in each of its blocks.
 // Columns beyond K meet zeros of x and hold code 0, rows beyond O too; the steps of groups and rows that do not exist are zero.
 #pragma once
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace bs {
@@ -50,6 +52,21 @@ struct W4Gemm {
     int* status;                // device status word
 };
 
+// csrc/w4_mma.cu: tensor map of `matrices` prepared matrices, fetched in boxes of `wide` neighbouring blocks of `high` rows of blocks: coordinates (0, block,
+// row of blocks, matrix), blocks that do not exist are zeros.
+bool w4_encode_blocks(CUtensorMap* tm, const void* prepared, const W4Layout& l, int matrices, int wide, int high);
+// Warps of a team, which share a reduction of so many blocks: the widest that leaves at most a fifth of its turns empty, or else the one that leaves the
+// fewest.  Wide teams read the weights in long pieces: eight teams of one warp, blocks of 1 KB from eight places, take 1.1 to 1.3 times the time.
+inline int w4_team_width(int warps, int blocks)
+{
+    int best = warps;
+    double used = 0;
+    for (int split = warps; split >= 1 && used < 0.8; split /= 2) {
+        const double u = static_cast<double>(blocks) / (ceil_div(blocks, split) * split);
+        if (u > used) { best = split; used = u; }
+    }
+    return best;
+}
 // csrc/w4_mma.cu: the product on tcgen05 for many rows of x, which start on 16-byte boundaries.  part: w4_mma_workspace bytes.
 bool w4_mma_wanted(int M, const W4Layout& l);
 size_t w4_mma_workspace(int M, const W4Layout& l, int sms);

@@ -94,69 +94,9 @@ struct W4Tile {
     uint32_t scale[NG], zero[NG];
 };
 
-// Blocks on their way through shared memory: a warp copies ahead into a ring of STAGES of its own, RT blocks a stage, one bulk copy each, and waits for
-// nobody else.  (Loads into registers a few blocks ahead wait for one another: the waits of a warp are counted in six places only.)
-template <int NG, bool ZEROS, int RT, int STAGES>
-struct W4Ring {
-    static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * RT * BLOCK;
-    uint32_t bars;              // the barriers' memory holds nothing else: only an invalidated one may be written over
-    uint32_t base, mine;        // the stages; the lane's codes in the first one
-    unsigned limit;             // polls of a wait, 1 after one has run out
-
-    __device__ __forceinline__ W4Ring(unsigned char* smem, uint64_t (&bar)[STAGES], int warp, int lane) : limit(1u << 20)
-    {
-        base = static_cast<uint32_t>(__cvta_generic_to_shared(smem)) + warp * BYTES;
-        mine = base + (lane & 3) * 256 + ((lane >> 2) ^ 2 * (lane & 3)) * 16;
-        bars = static_cast<uint32_t>(__cvta_generic_to_shared(bar));
-        if (lane == 0) {
-#pragma unroll
-            for (int s = 0; s < STAGES; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * s) : "memory");
-            asm volatile("fence.mbarrier_init.release.cluster;\n\tfence.proxy.async.shared::cta;" ::: "memory");
-        }
-        __syncwarp();
-    }
-    // Fills a stage with the blocks at p; every lane has read what it held.
-    __device__ __forceinline__ void put(int stage, const unsigned char* const (&p)[RT], int lane) const
-    {
-        if (lane == 0) {
-            const uint32_t bar = bars + 8 * stage;
-            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(RT * BLOCK) : "memory");
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                             ::"r"(base + (stage * RT + r) * BLOCK), "l"(p[r]), "n"(BLOCK), "r"(bar) : "memory");
-        }
-    }
-    // The blocks of a stage, in its round of parity `phase`.  A wait that runs out sets the status word; later ones then poll once.
-    __device__ __forceinline__ void get(int stage, unsigned phase, W4Tile<NG, ZEROS> (&w)[RT], int lane, int* status)
-    {
-        unsigned ok = 0;
-        for (unsigned it = 0; it < limit && !ok; ++it)
-            asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bars + 8 * stage), "r"(phase) : "memory");
-        if (!ok) {
-            if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
-            limit = 1;
-        }
-        __syncwarp();
-        const uint32_t entry = base + W4_CODES + (lane >> 2) * ENTRY;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const uint32_t at = mine + (stage * RT + r) * BLOCK;
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].a.x), "=r"(w[r].a.y), "=r"(w[r].a.z), "=r"(w[r].a.w) : "r"(at) : "memory");
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[r].b.x), "=r"(w[r].b.y), "=r"(w[r].b.z), "=r"(w[r].b.w) : "r"(at + 128) : "memory");
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                const uint32_t step = entry + (stage * RT + r) * BLOCK + g * 8 * ENTRY;
-                if (ZEROS) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[r].scale[g]), "=r"(w[r].zero[g]) : "r"(step) : "memory");
-                else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[r].scale[g]) : "r"(step) : "memory");
-            }
-        }
-    }
-};
-
-// The same for a CTA: a stage holds, for each of NB matrices, WARPS blocks, one a warp.  The `split` warps of a team share the reduction of 16 rows, WARPS /
-// split teams take neighbouring rows; a team's blocks of a stage are neighbours in memory and one copy.  One thread fills stages ahead of the warps that
-// read them: copies of 8 KB in flight reach 5.7 TB/s, where a hundred of 1 KB an SM reach 3 (measured, 104 MB).
+// Blocks on their way through the shared memory of a CTA: a stage holds, for each of NB matrices, WARPS blocks, one a warp.  The `split` warps of a team share the reduction of 16 rows, WARPS /
+// split teams take neighbouring rows.  One thread fills stages ahead of the warps that read them, with one tensor copy of all teams' blocks: copies of
+// 8 KB reach 5.7 TB/s, where a hundred of 1 KB in flight on every SM reach 3 (measured, 104 MB), and a copy takes its thread 130 cycles to start.  (Loads into registers a few blocks ahead wait for one another: the waits of a warp are counted in six places only.)
 template <int NG, bool ZEROS, int NB, int WARPS, int STAGES>
 struct W4TeamRing {
     static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * NB * WARPS * BLOCK;
@@ -216,17 +156,16 @@ struct W4TeamRing {
             limit = 1;
         }
     }
-    // The producer's thread: the stage is free; so many blocks are announced.  copy() starts their copies, next() goes on.
-    __device__ __forceinline__ void open(int blocks, int* status)
+    // The producer's thread: once the stage is free, the blocks from (c, rb) on of matrix e of each of the NB tensor maps.
+    __device__ __forceinline__ void fill(const CUtensorMap* const (&maps)[NB], const int (&rb)[NB], int c, int e, int* status)
     {
         wait(bar + 8 * STAGES, phase ^ 1, status);
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(blocks * BLOCK) : "memory");
-    }
-    // `blocks` neighbouring blocks at p to the places of matrix m from warp `first` on.
-    __device__ __forceinline__ void copy(int m, int first, const unsigned char* p, int blocks) const
-    {
-        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                     ::"r"(base + stage * STAGE + (m * WARPS + first) * BLOCK), "l"(p), "r"(blocks * BLOCK), "r"(bar) : "memory");
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(STAGE) : "memory");
+#pragma unroll
+        for (int m = 0; m < NB; ++m)
+            asm volatile("cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                         ::"r"(base + stage * STAGE + m * WARPS * BLOCK), "l"(reinterpret_cast<uint64_t>(maps[m])), "r"(bar), "r"(0), "r"(c), "r"(rb[m]), "r"(e) : "memory");
+        next();
     }
     // The warps: the stage has landed; a warp's blocks of it; the warp has what it needs.
     __device__ __forceinline__ void landed(int* status) { wait(bar, phase, status); }

@@ -14,7 +14,7 @@ constexpr int WARPS = 8, STAGES = 6;
 // through several items; the last warp copies their blocks ahead, also while the sums of an item are put together.
 template <int NT> constexpr int ctas_of() { return NT == 1 ? 3 : 2; }      // per SM
 template <bool F16, int NG, bool ZEROS, int NT>
-__global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel(const __grid_constant__ W4Gemm g, int split)
+__global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel(const __grid_constant__ W4Gemm g, const __grid_constant__ CUtensorMap tw, int split)
 {
     typedef typename W4Type<F16>::T T;
     constexpr int M = NT * 8;
@@ -25,18 +25,12 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, m0 = blockIdx.y * M;
     const int teams = WARPS / split, team = warp / split, k0 = warp % split;
     Ring ring(smem, bars, warp, lane);
-    const unsigned char* matrix = dependent_begin(g.w);
+    dependent_begin(g.w);
     if (warp == WARPS) {
+        const CUtensorMap* const maps[1] = {&tw};
         if (lane == 0)
-            for (int rb0 = blockIdx.x * teams; rb0 < g.l.rbs; rb0 += gridDim.x * teams) {
-                const int have = min(teams, g.l.rbs - rb0);
-                for (int c = 0; c < g.l.cbs; c += split) {
-                    const int n = min(split, g.l.cbs - c);
-                    ring.open(have * n, g.status);
-                    for (int r = 0; r < have; ++r) ring.copy(0, r * split, matrix + (static_cast<size_t>(rb0 + r) * g.l.cbs + c) * Ring::BLOCK, n);
-                    ring.next();
-                }
-            }
+            for (int rb0 = blockIdx.x * teams; rb0 < g.l.rbs; rb0 += gridDim.x * teams)
+                for (int c = 0; c < g.l.cbs; c += split) ring.fill(maps, {rb0}, c, 0, g.status);
         return;
     }
     const T* x0 = behind_wait<T>(g.x);
@@ -104,11 +98,12 @@ int launch_tile(const W4Gemm& g, int sms, cudaStream_t st)
     auto kernel = w4_gemm_kernel<F16, NG, ZEROS, NT>;
     constexpr int smem = W4TeamRing<NG, ZEROS, 1, WARPS, STAGES>::BYTES;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    // teams are as wide as the reduction has blocks
-    int split = WARPS;
-    while (split > 1 && split / 2 >= g.l.cbs) split /= 2;
-    const int items = ceil_div(g.l.rbs, WARPS / split), tiles = ceil_div(g.M, 8 * NT), places = ctas_of<NT>() * sms;
-    return launch_dependent(kernel, dim3(items < places ? items : places, tiles), dim3(WARPS * 32 + 32), smem, st, g, split);
+    const int places = ctas_of<NT>() * sms;
+    const int split = w4_team_width(WARPS, g.l.cbs);
+    const int items = ceil_div(g.l.rbs, WARPS / split), tiles = ceil_div(g.M, 8 * NT);
+    CUtensorMap tw;
+    if (!w4_encode_blocks(&tw, g.w, g.l, 1, split, WARPS / split)) return BS_ERR_CUDA;
+    return launch_dependent(kernel, dim3(items < places ? items : places, tiles), dim3(WARPS * 32 + 32), smem, st, g, tw, split);
 }
 template <bool F16, int NG, bool ZEROS>
 int launch_tiles(const W4Gemm& g, int sms, cudaStream_t st)

@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                     mm_wait_uniform(&w_empty[w.at], w.phase ^ 1, limit);
                     if (mm_elect()) {
                         mbar_expect_tx(&w_full[w.at], BLOCKS * BLOCK);
-                        tma_load_2d(wsm + w.at * BLOCKS * BLOCK, &tw, &w_full[w.at], c * (BLOCK / 8), ot * BLOCKS);
+                        tma_load_4d(wsm + w.at * BLOCKS * BLOCK, &tw, &w_full[w.at], 0, c, ot * BLOCKS, 0);
                     }
                     w.next();
                     ++issued;
@@ -480,18 +480,6 @@ bool encode_x(CUtensorMap* tm, const W4Gemm& g, int n, bool f16)
     return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(g.x), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Tensor map of the prepared weights: rows of blocks, in elements of eight bytes so that a block is a box's width; fetched eight rows of blocks at a time.
-bool encode_w(CUtensorMap* tm, const W4Gemm& g)
-{
-    const EncodeFn fn = encode_fn();
-    if (!fn) return false;
-    const cuuint64_t width = static_cast<cuuint64_t>(g.l.cbs) * g.l.block;
-    const cuuint64_t dims[2] = {width / 8, static_cast<cuuint64_t>(g.l.rbs)}, strides[1] = {width};
-    const cuuint32_t box[2] = {static_cast<cuuint32_t>(g.l.block / 8), BLOCKS}, es[2] = {1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_INT64, 2, const_cast<unsigned char*>(g.w), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 bool plan(MmaTiles& a, int sms)
 {
     const W4Layout& l = a.g.l;
@@ -528,6 +516,18 @@ int launch_group(const CUtensorMap& tx, const CUtensorMap& tw, const MmaTiles& a
 
 }  // namespace
 
+// In elements of eight bytes, so that a block is no wider than a box may be.
+bool w4_encode_blocks(CUtensorMap* tm, const void* prepared, const W4Layout& l, int matrices, int wide, int high)
+{
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(l.block / 8), static_cast<cuuint64_t>(l.cbs), static_cast<cuuint64_t>(l.rbs), static_cast<cuuint64_t>(matrices)};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(l.block), static_cast<cuuint64_t>(l.cbs) * l.block, l.bytes()};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(l.block / 8), static_cast<cuuint32_t>(wide), static_cast<cuuint32_t>(high), 1}, es[4] = {1, 1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_INT64, 4, const_cast<void*>(prepared), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool w4_mma_wanted(int M, const W4Layout& l) { return M > 16; }
 
 size_t w4_mma_workspace(int M, const W4Layout& l, int sms)
@@ -545,7 +545,7 @@ int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t 
     a.part = part;
     CUtensorMap tx, tw;
     if (!plan(a, sms)) return BS_ERR_UNSUPPORTED;
-    if (!encode_x(&tx, g, a.n, f16) || !encode_w(&tw, g)) return BS_ERR_CUDA;
+    if (!encode_x(&tx, g, a.n, f16) || !w4_encode_blocks(&tw, g.w, a.g.l, 1, 1, BLOCKS)) return BS_ERR_CUDA;
     if (a.n <= 64) return f16 ? launch_group<true, true>(tx, tw, a, st) : launch_group<false, true>(tx, tw, a, st);
     return f16 ? launch_group<true, false>(tx, tw, a, st) : launch_group<false, false>(tx, tw, a, st);
 }

@@ -1,7 +1,8 @@
-// A mixture-of-experts layer on 4-bit weights for a few tokens, in three launches:
+// A mixture-of-experts layer on 4-bit weights for a few tokens, in four launches:
 //   route   logits = x R^T, the top_k experts of every token, their softmax weights
 //   gate    h[slot] = weight * silu(Gate_e x) * (Up_e x) for every slot (token, choice)
-//   down    y[token] = sum over its slots of Down_e h[slot]
+//   down    z[slot] = Down_e h[slot]
+//   sum     y[token] = sum over its slots of z[slot]
 // Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), through
 // shared memory, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
 // of mantissa), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
@@ -22,10 +23,12 @@ struct MoeArgs {
     bool x_aligned, router_aligned;
     const unsigned char *gate, *up, *down;
     W4Layout lu, ld;                        // of one expert's gate or up, and down
+    CUtensorMap tg, tu, td;                 // their blocks, in boxes of a CTA's teams
     void* xa;                               // aligned copy of x, or null where x is
     long long ldxa;
     __nv_bfloat16 *hi, *lo;                 // [T top_k][ldh]
-    int ldh;
+    float* z;                               // [T top_k][ldz]
+    int ldh, ldz;
     int* status;                            // device status word
     int* experts;
     float* weights;
@@ -217,24 +220,14 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
     const long long ldx = g.xa ? g.ldxa : g.ldx;
     find_jobs<J>(g, jobs, t0, WARPS * 32 + 32);
     const W4Layout& l = g.lu;
-    const size_t matrix = l.bytes();
     // an item: a job and the rows of all teams
     const int per_job = (l.rbs + teams - 1) / teams, items = jobs.n * per_job, full = l.K / W4_COLS;
     if (warp == WARPS) {
+        const CUtensorMap* const maps[2] = {&g.tg, &g.tu};
         if (lane == 0)
             for (int item = blockIdx.x; item < items; item += gridDim.x) {
-                const int job = item / per_job, rb0 = (item - job * per_job) * teams, rows = min(teams, l.rbs - rb0);
-                const size_t at = jobs.expert[job] * matrix;
-                for (int c = 0; c < l.cbs; c += split) {
-                    const int n = min(split, l.cbs - c);
-                    ring.open(2 * rows * n, g.status);
-                    for (int r = 0; r < rows; ++r) {
-                        const size_t p = at + (static_cast<size_t>(rb0 + r) * l.cbs + c) * Ring::BLOCK;
-                        ring.copy(0, r * split, g.gate + p, n);
-                        ring.copy(1, r * split, g.up + p, n);
-                    }
-                    ring.next();
-                }
+                const int job = item / per_job, rb0 = (item - job * per_job) * teams;
+                for (int c = 0; c < l.cbs; c += split) ring.fill(maps, {rb0, rb0}, c, jobs.expert[job], g.status);
             }
         return;
     }
@@ -294,120 +287,103 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
     }
 }
 
-// y of 32 columns for the tokens of a pass: the warps of a cluster's CTAs share the blocks of all jobs, one run of them each, and add up per token in
-// shared memory of their own.  32 columns, because the hidden values of a slot are four times its weights' bytes.
-constexpr int DOWN_RT = 2, DOWN_ROWS = DOWN_RT * W4_ROWS;
+// z = Down_e h of 32 rows of an expert for the slots of a job, items and teams as above.  32 rows a warp, because the hidden values of eight slots are four
+// times the weights' bytes that they meet in 16.  (With the tokens' sums kept in the CTA instead, job after job, a job's few blocks waited for
+// barriers: 95 us where this and the sums behind it take 48, 64 tokens of 128 experts.)
 template <bool F16, int NG, bool ZEROS, int NT>
-__global__ void __launch_bounds__(WARPS * 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int cluster)
+__global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int split)
 {
-    typedef typename W4Type<F16>::T T;
-    typedef W4Ring<NG, ZEROS, DOWN_RT, DOWN_STAGES> Ring;
-    constexpr int J = NT * 8, RT = DOWN_RT;
-    extern __shared__ __align__(128) unsigned char smem[];      // rings of the warps, then sums [WARPS][DOWN_ROWS][pitch]
+    typedef W4TeamRing<NG, ZEROS, 2, WARPS, DOWN_STAGES> Ring;
+    constexpr int J = NT * 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t bars[2 * DOWN_STAGES];
     __shared__ Jobs jobs;
-    float* sums = reinterpret_cast<float*>(smem + WARPS * Ring::BYTES);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS, rb0 = blockIdx.x / cluster * RT, rank = blockIdx.x % cluster;
-    const int tokens = g.T - t0 < PASS ? g.T - t0 : PASS, pitch = tokens + 1;
-    __shared__ uint64_t bars[WARPS][DOWN_STAGES];
-    Ring ring(smem, bars[warp], warp, lane);
-    const unsigned char* down = dependent_begin(g.down);
+    __shared__ float part[WARPS][J][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
+    const int team = warp / split, k0 = warp % split, teams = WARPS / split;
+    Ring ring(smem, bars, warp, lane);
+    dependent_begin(g.down);
     const __nv_bfloat16* hidden = behind_wait<__nv_bfloat16>(g.hi);
-    find_jobs<J>(g, jobs, t0, WARPS * 32);
+    find_jobs<J>(g, jobs, t0, WARPS * 32 + 32);
     const W4Layout& l = g.ld;
-    const size_t matrix = l.bytes();
-    float* own = sums + warp * DOWN_ROWS * pitch;
-    for (int i = lane; i < DOWN_ROWS * pitch; i += 32) own[i] = 0.f;
-    __syncwarp();
-    const int full = l.K / W4_COLS, runs = cluster * WARPS, run = rank * WARPS + warp;
-    const long long blocks = static_cast<long long>(jobs.n) * l.cbs;
-    const int beg = static_cast<int>(blocks * run / runs), end = static_cast<int>(blocks * (run + 1) / runs);
-    int f = beg, fjob = beg / l.cbs, fc = beg - fjob * l.cbs;        // the blocks that are fetched next
-    const unsigned char* from[RT];
-    auto locate = [&] {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) from[r] = down + jobs.expert[fjob] * matrix + (static_cast<size_t>(min(rb0 + r, l.rbs - 1)) * l.cbs + fc) * Ring::BLOCK;
-    };
-    if (beg < end) locate();
-    int in = 0, out = 0;        // stages that are filled and read next
-    unsigned phase = 0;
-    auto put = [&] {
-        if (f >= end) return;
-        ring.put(in, from, lane);
-        in = (in + 1) % DOWN_STAGES;
-        ++f;
-        if (++fc < l.cbs) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) from[r] += Ring::BLOCK;
-        } else {
-            fc = 0;
-            ++fjob;
-            if (f < end) locate();
-        }
-    };
-#pragma unroll 1
-    for (int s = 0; s < DOWN_STAGES - 1; ++s) put();
-    int job = beg / l.cbs, c = beg - job * l.cbs;
+    const int per_job = (l.rbs + 2 * teams - 1) / (2 * teams), items = jobs.n * per_job, full = l.K / W4_COLS;
+    if (warp == WARPS) {
+        const CUtensorMap* const maps[2] = {&g.td, &g.td};
+        if (lane == 0)
+            for (int item = blockIdx.x; item < items; item += gridDim.x) {
+                const int job = item / per_job, rb0 = (item - job * per_job) * 2 * teams;
+                for (int c = 0; c < l.cbs; c += split) ring.fill(maps, {rb0, rb0 + teams}, c, jobs.expert[job], g.status);
+            }
+        return;
+    }
     const long long lo = g.lo - g.hi;
-    for (int b = beg; b < end;) {       // jobs, or this warp's part of one
-        const int first = jobs.first[job], n = jobs.first[job + 1] - first, stop = min(l.cbs, c + end - b);
-        b += stop - c;
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int job = item / per_job, rb = (item - job * per_job) * 2 * teams + team, beg = jobs.first[job], n = jobs.first[job + 1] - beg;
+        const size_t slot0 = static_cast<size_t>(t0) * g.top_k;
         const __nv_bfloat16* row[NT];
-        float tot[RT][NT][4];
+        float tot[2][NT][4];
 #pragma unroll
         for (int k = 0; k < NT; ++k) {
-            row[k] = hidden + (static_cast<size_t>(t0) * g.top_k + jobs.slot[first + min(k * 8 + (lane >> 2), n - 1)]) * g.ldh;
+            row[k] = hidden + (slot0 + jobs.slot[beg + min(k * 8 + (lane >> 2), n - 1)]) * g.ldh + 8 * (lane & 3);
 #pragma unroll
-            for (int r = 0; r < RT; ++r) tot[r][k][0] = tot[r][k][1] = tot[r][k][2] = tot[r][k][3] = 0.f;
+            for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
         }
-        for (; c < stop; ++c) {
-            W4Tile<NG, ZEROS> w[RT];
-            const int k0 = c * W4_COLS + 8 * (lane & 3);
-            ring.get(out, phase, w, lane, g.status);
-            out = (out + 1) % DOWN_STAGES;
-            phase ^= out == 0;
-            put();      // into the stage before this one: its blocks have been multiplied
-            if (c < full) w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + k0 + 32 * j)); }, tot);
-            else w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0), k0 + 32 * j, l.K); }, tot);
+        // teams without rows multiply what the stages hold, and drop it
+        for (int c = k0; c < l.cbs + k0; c += split) {
+            ring.landed(g.status);
+            if (c < l.cbs) {
+                W4Tile<NG, ZEROS> w[2];
+                ring.take(w);
+                if (c < full) w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + c * W4_COLS + 32 * j)); }, tot);
+                else w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0) + c * W4_COLS, 32 * j, l.K - c * W4_COLS - 8 * (lane & 3)); }, tot);
+            }
+            ring.release(lane);
+            ring.next();
         }
-        c = 0;
-        ++job;
 #pragma unroll
         for (int k = 0; k < NT; ++k)
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {       // lanes own different (row, slot): an expert has a token once
-                    const int q = k * 8 + 2 * (lane & 3) + (i & 1);
-                    if (q < n) own[(r * W4_ROWS + (lane >> 2) + 8 * (i >> 1)) * pitch + jobs.token[first + q]] += tot[r][k][i];
-                }
-        __syncwarp();       // another job's slots meet the same tokens from other lanes
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < DOWN_ROWS * tokens; i += WARPS * 32) {
-        const int m = i / DOWN_ROWS, r = i % DOWN_ROWS, o = rb0 * W4_ROWS + r;
-        float v = 0.f;
-#pragma unroll
-        for (int k = 0; k < WARPS; ++k) v += sums[(k * DOWN_ROWS + r) * pitch + m];
-        if (cluster > 1) sums[r * pitch + m] = v;
-        else if (o < g.H) static_cast<T*>(g.y)[static_cast<size_t>(t0 + m) * g.H + o] = W4Type<F16>::round(v);
-    }
-    if (cluster == 1) return;
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (rank == 0) {
-        for (int i = threadIdx.x; i < DOWN_ROWS * tokens; i += WARPS * 32) {
-            const int m = i / DOWN_ROWS, r = i % DOWN_ROWS, o = rb0 * W4_ROWS + r;
-            float v = sums[r * pitch + m];
-            for (int k = 1; k < cluster; ++k) {
-                uint32_t from = static_cast<uint32_t>(__cvta_generic_to_shared(&sums[r * pitch + m]));
-                float part;
-                asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(from) : "r"(k));
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(part) : "r"(from) : "memory");
-                v += part;
+            for (int i = 0; i < 4; ++i) {
+                const int m = k * 8 + 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
+                part[warp][m][r] = tot[0][k][i];
+                part[warp][m][r + 16] = tot[1][k][i];
             }
-            if (o < g.H) static_cast<T*>(g.y)[static_cast<size_t>(t0 + m) * g.H + o] = W4Type<F16>::round(v);
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
+        for (int q = k0 * 32 + lane; q < n * 32; q += 32 * split) {
+            const int m = q >> 5, r = q & 31, o = (rb + (r >> 4) * teams) * 16 + (r & 15);      // two blocks of rows, `teams` apart
+            if (o >= g.H) continue;
+            float v = 0.f;
+            for (int k = 0; k < split; ++k) v += part[team * split + k][m][r];
+            g.z[(slot0 + jobs.slot[beg + m]) * g.ldz + o] = v;
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
+    }
+}
+
+// y[token] = the sum of its slots' z, in the order of the choices.  A thread: four columns.
+template <bool F16>
+__global__ void __launch_bounds__(256) w4_moe_sum_kernel(const __grid_constant__ MoeArgs g)
+{
+    typedef typename W4Type<F16>::T T;
+    const float* z = dependent_begin(g.z);
+    const int quads = g.ldz / 4, step = gridDim.x * blockDim.x;
+    for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < static_cast<long long>(g.T) * quads; i += step) {
+        const int t = static_cast<int>(i / quads), h = static_cast<int>(i - static_cast<long long>(t) * quads) * 4;
+        const float* p = z + static_cast<size_t>(t) * g.top_k * g.ldz + h;
+        float4 v = *reinterpret_cast<const float4*>(p);
+#pragma unroll 8
+        for (int j = 1; j < g.top_k; ++j) {
+            const float4 w = *reinterpret_cast<const float4*>(p + static_cast<size_t>(j) * g.ldz);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        T* y = static_cast<T*>(g.y) + static_cast<size_t>(t) * g.H + h;
+        if (g.H % 4 == 0) {
+            *reinterpret_cast<uint2*>(y) = make_uint2(W4Type<F16>::round2(v.x, v.y), W4Type<F16>::round2(v.z, v.w));
+        } else {
+            const float s[4] = {v.x, v.y, v.z, v.w};
+            for (int k = 0; k < 4 && h + k < g.H; ++k) y[k] = W4Type<F16>::round(s[k]);
         }
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 template <typename K>
@@ -439,30 +415,31 @@ int launch_clusters(void (*kern)(P...), dim3 grid, int threads, size_t smem, int
     return BS_ERR_CUDA;
 }
 template <bool F16, int NG, bool ZEROS, int NT>
-int launch_gate(const MoeArgs& g, int sms, cudaStream_t st)
+int launch_gate(MoeArgs& g, int sms, cudaStream_t st)
 {
-    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k;
-    int split = WARPS;
-    while (split / 2 >= g.lu.cbs) split /= 2;
-    const long long items = static_cast<long long>(slots < g.E ? slots : g.E) * ceil_div(g.lu.rbs, WARPS / split);
+    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
+    const int split = w4_team_width(WARPS, g.lu.cbs);
+    const long long items = static_cast<long long>(jobs) * ceil_div(g.lu.rbs, WARPS / split);
     constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES>::BYTES;
-    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
+    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, smem) || !w4_encode_blocks(&g.tg, g.gate, g.lu, g.E, split, WARPS / split) ||
+        !w4_encode_blocks(&g.tu, g.up, g.lu, g.E, split, WARPS / split))
+        return BS_ERR_CUDA;
     return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
                             dim3(WARPS * 32 + 32), smem, st, g, split);
 }
 template <bool F16, int NG, bool ZEROS, int NT>
-int launch_down(const MoeArgs& g, int sms, cudaStream_t st)
+int launch_down(MoeArgs& g, int sms, cudaStream_t st)
 {
-    const int tokens = g.T < PASS ? g.T : PASS, rows = ceil_div(g.ld.rbs, DOWN_RT);
-    const size_t smem = WARPS * W4Ring<NG, ZEROS, DOWN_RT, DOWN_STAGES>::BYTES + sizeof(float) * WARPS * DOWN_ROWS * (tokens + 1);
-    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS, NT>, smem)) return BS_ERR_CUDA;
-    // CTAs of a cluster until two fill every SM
-    int cluster = 1;
-    while (cluster < 8 && rows * cluster * 2 <= 2 * sms) cluster *= 2;
-    return launch_clusters(w4_moe_down_kernel<F16, NG, ZEROS, NT>, dim3(rows * cluster, ceil_div(g.T, PASS)), WARPS * 32, smem, cluster, st, g, cluster);
+    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
+    const int split = w4_team_width(WARPS, g.ld.cbs);
+    const long long items = static_cast<long long>(jobs) * ceil_div(g.ld.rbs, 2 * WARPS / split);
+    constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, DOWN_STAGES>::BYTES;
+    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS, NT>, smem) || !w4_encode_blocks(&g.td, g.down, g.ld, g.E, split, WARPS / split)) return BS_ERR_CUDA;
+    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
+                            dim3(WARPS * 32 + 32), smem, st, g, split);
 }
 template <bool F16, int NT>
-int launch_experts(const MoeArgs& g, int sms, cudaStream_t st)
+int launch_experts(MoeArgs& g, int sms, cudaStream_t st)
 {
     int rc;
     const int nu = g.lu.group == 32 ? 4 : g.lu.group == 64 ? 2 : 1, nd = g.ld.group == 32 ? 4 : g.ld.group == 64 ? 2 : 1;
@@ -473,14 +450,18 @@ int launch_experts(const MoeArgs& g, int sms, cudaStream_t st)
     return nd == 4 ? launch_down<F16, 4, false, NT>(g, sms, st) : nd == 2 ? launch_down<F16, 2, false, NT>(g, sms, st) : launch_down<F16, 1, false, NT>(g, sms, st);
 }
 template <bool F16>
-int launch_moe(const MoeArgs& g, int sms, cudaStream_t st)
+int launch_moe(MoeArgs& g, int sms, cudaStream_t st)
 {
-    const int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
+    int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
     if (rc != BS_OK) return rc;
     // a second job of an expert reads its weights again: jobs of 16 slots where more than eight are likely
-    return (g.T < PASS ? g.T : PASS) * g.top_k > 5 * g.E ? launch_experts<F16, 2>(g, sms, st) : launch_experts<F16, 1>(g, sms, st);
+    rc = (g.T < PASS ? g.T : PASS) * g.top_k > 5 * g.E ? launch_experts<F16, 2>(g, sms, st) : launch_experts<F16, 1>(g, sms, st);
+    if (rc != BS_OK) return rc;
+    const long long want = (static_cast<long long>(g.T) * (g.ldz / 4) + 255) / 256, most = 8ll * sms;
+    return launch_dependent(w4_moe_sum_kernel<F16>, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(256), 0, st, g);
 }
 
+size_t slot_bytes(int T, int top_k, int H) { return static_cast<size_t>(T) * top_k * ((static_cast<size_t>(H) + 3) / 4 * 4) * 4; }
 size_t hidden_bytes(int T, int top_k, int I) { return static_cast<size_t>(T) * top_k * ((static_cast<size_t>(I) + 7) / 8 * 8) * 2; }
 size_t aligned_bytes(int T, int H, long long ldx) { return T == 1 || ldx % 8 == 0 ? 0 : static_cast<size_t>(T) * ((static_cast<size_t>(H) + 7) / 8 * 8) * 2; }
 
@@ -490,7 +471,7 @@ size_t aligned_bytes(int T, int H, long long ldx) { return T == 1 || ldx % 8 == 
 extern "C" size_t bs_w4_moe_workspace_bytes(int T, int top_k, int H, int I, long long ldx)
 {
     if (T <= 0 || top_k <= 0 || H <= 0 || I <= 0) return 0;
-    return 2 * bs::hidden_bytes(T, top_k, I) + bs::aligned_bytes(T, H, ldx);
+    return bs::slot_bytes(T, top_k, H) + 2 * bs::hidden_bytes(T, top_k, I) + bs::aligned_bytes(T, H, ldx);
 }
 
 extern "C" int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, int H, int I, const void* gate, const void* up, int group_up,
@@ -515,6 +496,9 @@ extern "C" int bs_w4_moe(const void* x, long long ldx, int T, const void* router
     g.gate = static_cast<const unsigned char*>(gate); g.up = static_cast<const unsigned char*>(up); g.down = static_cast<const unsigned char*>(down);
     g.ldh = (I + 7) & ~7;
     unsigned char* ws = static_cast<unsigned char*>(workspace);
+    g.z = reinterpret_cast<float*>(ws);
+    g.ldz = (H + 3) & ~3;
+    ws += slot_bytes(T, top_k, H);
     g.hi = reinterpret_cast<__nv_bfloat16*>(ws);
     g.lo = reinterpret_cast<__nv_bfloat16*>(ws + hidden_bytes(T, top_k, I));
     if (!g.x_aligned) {

@@ -34,8 +34,8 @@ def test_sizes(L):
     assert L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 128, 4611) == 5 * 4616 * 2
     assert L.bs_w4_gemm_workspace_bytes(0, 64, 4611, 128, 4611) == L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 96, 4611) == 0
     assert L.bs_w4_gemm_workspace_bytes(300, 64, 4611, 128, 4611) > 300 * 4616 * 2
-    assert L.bs_w4_moe_workspace_bytes(3, 2, 64, 50, 64) == 2 * 3 * 2 * 56 * 2
-    assert L.bs_w4_moe_workspace_bytes(3, 2, 63, 50, 63) == 2 * 3 * 2 * 56 * 2 + 3 * 64 * 2
+    assert L.bs_w4_moe_workspace_bytes(3, 2, 64, 50, 64) == 3 * 2 * 64 * 4 + 2 * 3 * 2 * 56 * 2
+    assert L.bs_w4_moe_workspace_bytes(3, 2, 63, 50, 63) == 3 * 2 * 64 * 4 + 2 * 3 * 2 * 56 * 2 + 3 * 64 * 2
     assert L.bs_w4_moe_workspace_bytes(0, 2, 64, 50, 64) == 0
 
 
@@ -72,7 +72,7 @@ def test_moe_refuses(L, at):
         assert moe(**{name: at + 4}) == ALIGN
     assert moe(T=-1) == moe(E=0) == moe(H=0) == moe(I=0) == moe(ldx=63) == moe(k=0) == moe(k=5) == moe(t=F32) == moe(gu=0) == INVALID
     assert moe(E=513) == moe(E=64, k=33) == moe(gu=48) == moe(gd=192) == moe(T=16385) == UNSUPPORTED
-    assert moe(ws=None) == moe(n=2 * 3 * 2 * 48 * 2 - 1) == INVALID and moe(ws=at + 8) == ALIGN
+    assert moe(ws=None) == moe(n=3 * 2 * 64 * 4 + 2 * 3 * 2 * 48 * 2 - 1) == INVALID and moe(ws=at + 8) == ALIGN
     assert moe(T=0) == OK
 
 
