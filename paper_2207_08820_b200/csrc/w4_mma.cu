@@ -528,7 +528,14 @@ bool w4_encode_blocks(CUtensorMap* tm, const void* prepared, const W4Layout& l, 
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool w4_mma_wanted(int M, const W4Layout& l) { return M > 16; }
+// Up to 16 rows of x: csrc/w4_gemm.cu is faster at every size.  Above, by fitted times (24 measured pairs, bf16 and fp16, 512 x 512 to 24576 x 8192): 0.43 ns a
+// block of weights and 16 rows of x there; here 8 us more in the beginning, for the second launch and the tensor memory, and 0.5 ns a block
+// and tile of 64 or 128 rows.
+bool w4_mma_wanted(int M, const W4Layout& l)
+{
+    const double blocks = static_cast<double>(l.rbs) * l.cbs;
+    return M > 16 && 0.43 * ceil_div(M, 16) * blocks > 0.5 * ceil_div(M, 128) * blocks + 8000;
+}
 
 size_t w4_mma_workspace(int M, const W4Layout& l, int sms)
 {

@@ -45,7 +45,7 @@ __device__ __forceinline__ uint4 load8(const T* row, int k0, int K, bool aligned
     return make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
 }
 
-// Whole numbers in the order of the doubles, a NaN above all of them (0 is below all).
+// Whole numbers in the order of the doubles, a NaN above all of them.
 __device__ __forceinline__ unsigned long long order_key(double v)
 {
     if (isnan(v)) return ~0ull;
@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     __shared__ double part[ROUTE_WARPS][16][8];
     __shared__ double logits[MAX_EXPERTS];
     __shared__ unsigned long long keys[MAX_EXPERTS];
+    __shared__ int choice[MAX_TOP];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x, m0 = blockIdx.y * 8;
     const T* x = static_cast<const T*>(dependent_begin(g.x));
     const T* router = behind_wait<T>(g.router);
@@ -112,29 +113,29 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     }
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     const int m = m0 + rank;
-    if (warp != 0 || m >= g.T) return;
-    // the warp picks the best of what is left, top_k times; lane j keeps choice j
-    for (int e = lane; e < g.E; e += 32) keys[e] = order_key(logits[e]);
-    __syncwarp();
-    int expert = 0;
-    for (int j = 0; j < g.top_k; ++j) {
-        unsigned long long best = 0;
-        int at = MAX_EXPERTS;
-        for (int e = lane; e < g.E; e += 32)
-            if (keys[e] > best) { best = keys[e]; at = e; }
-        const unsigned hi = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(best >> 32));
-        const unsigned lo = __reduce_max_sync(0xffffffffu, static_cast<unsigned>(best >> 32) == hi ? static_cast<unsigned>(best) : 0u);
-        const int e = __reduce_min_sync(0xffffffffu, best == (static_cast<unsigned long long>(hi) << 32 | lo) ? at : MAX_EXPERTS);     // ties: the lowest index
-        if (lane == (e & 31)) keys[e] = 0;      // below every value
-        if (lane == j) expert = e;
-        __syncwarp();
+    if (m >= g.T) return;
+    // an expert's place is the number of experts before it: larger logits, and equal ones of lower index.  `share` neighbouring threads count for one.
+    for (int e = threadIdx.x; e < g.E; e += ROUTE_WARPS * 32) keys[e] = order_key(logits[e]);
+    __syncthreads();
+    int share = 32;
+    while (share > 1 && share * g.E > ROUTE_WARPS * 32) share /= 2;
+    const int e = threadIdx.x / share;
+    int place = 0;
+    if (e < g.E) {
+        const unsigned long long key = keys[e];
+        for (int k = threadIdx.x % share; k < g.E; k += share) place += keys[k] > key || (keys[k] == key && k < e);
     }
-    const double most = logits[__shfl_sync(0xffffffffu, expert, 0)];
+    for (int d = 1; d < share; d <<= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
+    if (e < g.E && threadIdx.x % share == 0 && place < g.top_k) choice[place] = e;
+    __syncthreads();
+    if (warp != 0) return;
+    const int expert = lane < g.top_k ? choice[lane] : 0;
+    const double most = logits[choice[0]];
     const float p = lane < g.top_k ? expf(static_cast<float>(logits[expert] - most)) : 0.f;
     float sum = p;
     if (!g.renormalise) {
         sum = 0.f;
-        for (int e = lane; e < g.E; e += 32) sum += expf(static_cast<float>(logits[e] - most));
+        for (int k = lane; k < g.E; k += 32) sum += expf(static_cast<float>(logits[k] - most));
     }
 #pragma unroll
     for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
