@@ -167,6 +167,21 @@ struct W4TeamRing {
                          ::"r"(base + stage * STAGE + m * WARPS * BLOCK), "l"(reinterpret_cast<uint64_t>(maps[m])), "r"(bar), "r"(0), "r"(c), "r"(rb[m]), "r"(e) : "memory");
         next();
     }
+    // Behind the last one: no copy outlives the CTA, whatever the warps waited for.
+    __device__ __forceinline__ void drain(int filled, int* status)
+    {
+        limit = 1u << 20;
+        for (int i = 0; i < STAGES && i < filled; ++i) {
+            if (stage == 0) {
+                stage = STAGES;
+                bar += 8 * STAGES;
+                phase ^= 1;
+            }
+            --stage;
+            bar -= 8;
+            wait(bar, phase, status);
+        }
+    }
     // The warps: the stage has landed; a warp's blocks of it; the warp has what it needs.
     __device__ __forceinline__ void landed(int* status) { wait(bar, phase, status); }
     __device__ __forceinline__ void take(W4Tile<NG, ZEROS> (&w)[NB]) const

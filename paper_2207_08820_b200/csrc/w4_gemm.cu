@@ -28,9 +28,12 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel
     dependent_begin(g.w);
     if (warp == WARPS) {
         const CUtensorMap* const maps[1] = {&tw};
-        if (lane == 0)
+        if (lane == 0) {
+            int filled = 0;
             for (int rb0 = blockIdx.x * teams; rb0 < g.l.rbs; rb0 += gridDim.x * teams)
-                for (int c = 0; c < g.l.cbs; c += split) ring.fill(maps, {rb0}, c, 0, g.status);
+                for (int c = 0; c < g.l.cbs; c += split, ++filled) ring.fill(maps, {rb0}, c, 0, g.status);
+            ring.drain(filled, g.status);
+        }
         return;
     }
     const T* x0 = behind_wait<T>(g.x);

@@ -115,7 +115,7 @@ struct Turn {
 };
 
 // FEW: up to 64 rows of x, bound by the weights: four warps scale, otherwise eight.  The threads' registers are dealt anew: 640 of 96 become 128 (copies, MMA
-// issue) of 40, 256 (expansion) of 72 and 256 (totals) of 144; with few rows 512 of 128 become 128 of 40, 256 of 104 and 128 of 168.
+// issue) of 40, 256 (expansion) of 96 and 256 (totals) of 120; with few rows 512 of 128 become 128 of 40, 256 of 104 and 128 of 168.
 template <bool FEW> struct Roles {
     static constexpr int EXPAND = 8, SCALE = FEW ? 4 : 8, WARPS = 4 + EXPAND + SCALE, W_STAGES = FEW ? 8 : 4;
     static constexpr int N = FEW ? 64 : 128;                    // most rows of x in a tile
@@ -191,17 +191,19 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                     ++issued;
                 }
             }
-            for (int i = 0; i < RING && i < issued; ++i) {      // no copy outlives the CTA
+            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
+            limit = 1u << 20;
+            for (int i = 0; i < RING && i < issued; ++i) {      // no copy outlives the CTA, whatever else was waited for
                 x.at = x.at == 0 ? RING - 1 : x.at - 1;
                 if (x.at == RING - 1) x.phase ^= 1;
                 mm_wait_uniform(&full[x.at], x.phase, limit);
             }
-            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         } else if (warp == 1) {
             Turn<RING> x;
             Turn<2> ab;
             Turn<SUMS> d;
             unsigned limit = 1u << 20;
+            bool any = false;
             const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
             // K-major rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group
             const uint32_t b_hi = 64u | (1u << 14) | (2u << 29);
@@ -231,11 +233,14 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         d.next();
                     }
                     mm_commit(&done[x.at]);
+                    any = true;
                     x.next();
                     ab.next();
                 }
             }
             if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
+            limit = 1u << 20;           // nor do the MMAs outlive the tensor memory
+            if (any) mm_wait_uniform(&done[x.at == 0 ? RING - 1 : x.at - 1], x.at == 0 ? x.phase ^ 1 : x.phase, limit);
         } else if (warp == 2) {
             // the blocks of eight rows of blocks in one copy: as copies of their own they took 130 cycles each to start, twice the time of a step
             Turn<WS> w;
@@ -254,15 +259,16 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                     ++issued;
                 }
             }
+            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
+            limit = 1u << 20;
             for (int i = 0; i < WS && i < issued; ++i) {
                 w.at = w.at == 0 ? WS - 1 : w.at - 1;
                 if (w.at == WS - 1) w.phase ^= 1;
                 mm_wait_uniform(&w_full[w.at], w.phase, limit);
             }
-            if (limit == 1 && lane == 0) atomicOr(a.g.status, STATUS_TIMEOUT);
         }
     } else if (warp < 4 + Ro::EXPAND) {
-        registers<false, FEW ? 104 : 72>();
+        registers<false, FEW ? 104 : 96>();
         // a thread owns a row of the tile; each team of four warps takes every other step
         const int team = (warp - 4) >> 2, row = (warp & 3) * 32 + lane, r = row & 15;
         const uint32_t mine = smem_u32(wsm) + (row >> 4) * BLOCK, lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -287,25 +293,24 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         zero[g] = 8;
                         if (ZEROS) asm volatile("ld.shared.u16 %0, [%1];" : "=r"(zero[g]) : "r"(e + 4) : "memory");
                     }
+                    // the numbers first: the buffer's last MMAs may still run
+                    uint32_t v[2][32];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            uint32_t p[4];
+                            Ty::pairs(word_of(code[t], j), zero[j * NG / 4] * 0x00010001u, p);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) v[j >> 1][16 * (j & 1) + 4 * t + i] = p[i];
+                        }
                     wait(&done[x.at ^ 2], x.at < 2 ? x.phase ^ 1 : x.phase);      // the step before the last one
                     mm_fence_after();
-                    // the step that had this buffer is done and all rounds before its last three are scaled: the slots of these are free
+                    w4_st32(tmem_a + team * 64 + lanes, v[0]);
+                    w4_st32(tmem_a + team * 64 + 32 + lanes, v[1]);
+                    // that step is done and all rounds before its last three are scaled: the slots of these are free
 #pragma unroll
                     for (int g = 0; g < NG; ++g) scales[(round + g) % SCALE_SLOTS][row] = Ty::lo(scale[g]);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t v[32];
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int t = 0; t < 4; ++t) {
-                                uint32_t p[4];
-                                Ty::pairs(word_of(code[t], 2 * h + j), zero[(2 * h + j) * NG / 4] * 0x00010001u, p);
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) v[16 * j + 4 * t + i] = p[i];
-                            }
-                        w4_st32(tmem_a + team * 64 + h * 32 + lanes, v);
-                    }
                     mm_st_wait();
                     mm_fence_before();
                     __syncwarp();
@@ -320,7 +325,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
             }
         }
     } else {
-        registers<true, FEW ? 168 : 144>();
+        registers<true, FEW ? 168 : 120>();
         // a thread owns a row of the tile and all of its columns, or with eight warps half of them
         const int half = (warp - 4 - Ro::EXPAND) >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -343,28 +348,26 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                 wait(NG == 1 ? &done[x.at] : &d_full[d.at], NG == 1 ? x.phase : d.phase);
                 mm_fence_after();
                 const uint32_t from = tmem + d.at * Ro::N + n0 + lanes;
-                uint32_t v[Ro::PIECES][16];
-                if (width == Ro::PIECES * 16) {
-                    mm_ld32(from, reinterpret_cast<uint32_t (&)[32]>(v[0]));
-                    mm_ld32(from + 32, reinterpret_cast<uint32_t (&)[32]>(v[2]));
-                } else {
-#pragma unroll
-                    for (int p = 0; p < Ro::PIECES; ++p)
-                        if (p * 16 < width) mm_ld16(from + p * 16, v[p]);
-                }
                 const float sc = scales[round % SCALE_SLOTS][row];
-                mm_ld_wait();
-                mm_fence_before();
-                __syncwarp();
-                if (lane == 0) mm_arrive(NG == 1 ? &full[(x.at + SUMS) % RING] : &d_empty[d.at]);
                 const u64 ss = f2_pack(__float_as_uint(sc), __float_as_uint(sc));
 #pragma unroll
-                for (int p = 0; p < Ro::PIECES; ++p) {
-                    mm_landed(v[p]);
-                    if (p * 16 < width) {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) tot[p][i] = f2_fma(f2_pack(v[p][2 * i], v[p][2 * i + 1]), ss, tot[p][i]);
+                for (int h = 0; h < Ro::PIECES; h += 2) {
+                    uint32_t v[32];
+                    if (h * 16 + 32 <= width) mm_ld32(from + h * 16, v);
+                    else if (h * 16 < width) mm_ld16(from + h * 16, reinterpret_cast<uint32_t (&)[16]>(v[0]));
+                    mm_ld_wait();
+                    mm_landed(v);
+                    if (h + 2 >= Ro::PIECES) {      // the accumulator is free
+                        mm_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mm_arrive(NG == 1 ? &full[(x.at + SUMS) % RING] : &d_empty[d.at]);
                     }
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        if ((h + p) * 16 < width) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) tot[h + p][i] = f2_fma(f2_pack(v[16 * p + 2 * i], v[16 * p + 2 * i + 1]), ss, tot[h + p][i]);
+                        }
                 }
                 x.next();
                 d.next();
@@ -488,7 +491,7 @@ bool plan(MmaTiles& a, int sms)
     a.mts = ceil_div(a.g.M, n);
     a.ots = ceil_div(l.O, ROWS);
     const long long tiles = static_cast<long long>(a.mts) * a.ots;
-    if (tiles * l.cbs > 0x7fffffff) return false;
+    if (tiles * l.cbs > 0x7fff0000) return false;
     a.ctas = static_cast<int>(tiles * l.cbs < sms ? tiles * l.cbs : sms);
     a.waves = static_cast<int>(tiles % a.ctas == 0 ? tiles / a.ctas : tiles / a.ctas > 0 ? tiles / a.ctas - 1 : 0);
     const long long steps = (tiles - static_cast<long long>(a.waves) * a.ctas) * l.cbs;

@@ -225,11 +225,14 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
     const int per_job = (l.rbs + teams - 1) / teams, items = jobs.n * per_job, full = l.K / W4_COLS;
     if (warp == WARPS) {
         const CUtensorMap* const maps[2] = {&g.tg, &g.tu};
-        if (lane == 0)
+        if (lane == 0) {
+            int filled = 0;
             for (int item = blockIdx.x; item < items; item += gridDim.x) {
                 const int job = item / per_job, rb0 = (item - job * per_job) * teams;
-                for (int c = 0; c < l.cbs; c += split) ring.fill(maps, {rb0, rb0}, c, jobs.expert[job], g.status);
+                for (int c = 0; c < l.cbs; c += split, ++filled) ring.fill(maps, {rb0, rb0}, c, jobs.expert[job], g.status);
             }
+            ring.drain(filled, g.status);
+        }
         return;
     }
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
@@ -310,11 +313,14 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
     const int per_job = (l.rbs + 2 * teams - 1) / (2 * teams), items = jobs.n * per_job, full = l.K / W4_COLS;
     if (warp == WARPS) {
         const CUtensorMap* const maps[2] = {&g.td, &g.td};
-        if (lane == 0)
+        if (lane == 0) {
+            int filled = 0;
             for (int item = blockIdx.x; item < items; item += gridDim.x) {
                 const int job = item / per_job, rb0 = (item - job * per_job) * 2 * teams;
-                for (int c = 0; c < l.cbs; c += split) ring.fill(maps, {rb0, rb0 + teams}, c, jobs.expert[job], g.status);
+                for (int c = 0; c < l.cbs; c += split, ++filled) ring.fill(maps, {rb0, rb0 + teams}, c, jobs.expert[job], g.status);
             }
+            ring.drain(filled, g.status);
+        }
         return;
     }
     const long long lo = g.lo - g.hi;

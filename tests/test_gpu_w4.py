@@ -7,7 +7,7 @@ import torch
 
 import w4_reference as ref
 from paper_2207_08820_b200 import api
-from paper_2207_08820_b200._lib import BitserialError
+from paper_2207_08820_b200._lib import BitserialError, lib
 
 pytestmark = pytest.mark.gpu
 
@@ -119,9 +119,29 @@ def test_gemm_small(dtype, zeros, bias, group, M, O, K):
     (31, 1383, 4611, 32, BF16, True, True), (64, 512, 4608, 128, F16, False, True), (65, 300, 640, 64, BF16, False, False),
     (127, 257, 2304, 128, BF16, True, False), (128, 128, 576, 128, F16, False, False), (129, 640, 1024, 1024, BF16, False, True),
     (200, 1024, 1000, 32, F16, True, True), (257, 384, 2056, 64, BF16, True, True), (300, 100, 264, 128, F16, False, False),
-    (513, 2000, 512, 256, BF16, True, True), (1000, 129, 1153, 128, F16, True, False)])
+    (513, 2000, 512, 256, BF16, True, True), (65, 1100, 5003, 256, BF16, False, False),
+    (128, 1024, 4200, 128, F16, True, True), (129, 700, 5760, 32, F16, False, True), (777, 130, 6000, 384, F16, False, True), (1000, 129, 1153, 128, F16, True, False)])
 def test_gemm_larger(M, O, K, group, dtype, zeros, bias):
     check_gemm(np.random.default_rng(M + O + K), M, O, K, group, dtype, zeros, bias)
+
+
+@pytest.mark.parametrize("M,O,K,group,dtype,zeros,bias", [
+    (17, 8192, 5632, 128, BF16, False, True), (33, 4000, 5200, 64, F16, True, False), (64, 2047, 6600, 32, BF16, True, True),
+    (65, 2000, 5003, 256, BF16, False, False), (128, 2048, 4200, 128, F16, True, True), (129, 1000, 5760, 32, F16, False, True),
+    (200, 1000, 4096, 64, BF16, True, False), (300, 512, 4900, 128, BF16, True, True), (777, 200, 6000, 384, F16, False, True),
+    (1000, 129, 5121, 1024, BF16, True, True), (2048, 100, 3333, 64, BF16, False, False), (4096, 1, 11000, 128, BF16, False, True),
+    (4000, 333, 700, 32, BF16, True, True), (4096, 128, 1664, 128, F16, False, False), (9000, 2000, 100, 128, BF16, True, True)])
+def test_gemm_many_rows(M, O, K, group, dtype, zeros, bias):
+    """The kernel for many rows of x, which asks for a workspace: one tile and many, cut and whole, all ways of groups."""
+    assert lib().bs_w4_gemm_workspace_bytes(M, O, K, group, (K + 7) // 8 * 8) > 0
+    check_gemm(np.random.default_rng(M + O + K), M, O, K, group, dtype, zeros, bias)
+
+
+def test_gemm_whole_tiles_only():
+    """As many tiles as multiprocessors, or twice as many: none is cut."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    check_gemm(np.random.default_rng(1), 128, 128 * sms, 264, 128, BF16, True, False)
+    check_gemm(np.random.default_rng(2), 256, 128 * sms, 140, 64, F16, False, True)
 
 
 @pytest.mark.parametrize("M", [1, 5, 20, 40, 150])
@@ -149,12 +169,12 @@ def test_gemm_leading_dimensions_and_no_rows():
     assert api.gemm_w4(x[:0], w).shape == (0, 3, 40)
 
 
-@pytest.mark.parametrize("M", [5, 150])
-def test_gemm_special_values_stay_in_their_rows(M):
+@pytest.mark.parametrize("M,K", [(5, 300), (150, 300), (4096, 1700)])
+def test_gemm_special_values_stay_in_their_rows(M, K):
     rng = np.random.default_rng(M)
-    w = weights(rng, 70, 300, 32, BF16, True)
-    x = normal(rng, (M, 300), BF16)
-    x[1, 7], x[3, 299] = float("inf"), float("nan")
+    w = weights(rng, 70, K, 32, BF16, True)
+    x = normal(rng, (M, K), BF16)
+    x[1, 7], x[3, K - 1] = float("inf"), float("nan")
     w[1][4, 2] = float("inf")
     want, far = ref.gemm(x, ref.matrix(*w, 32), None, BF16)
     y = api.gemm_w4(x.cuda(), prepared(w, 32)).cpu().double()
@@ -164,7 +184,7 @@ def test_gemm_special_values_stay_in_their_rows(M):
     assert fine[0].sum() == 69 and not fine[1].any() and not fine[3].any()
 
 
-@pytest.mark.parametrize("M,O,K", [(1, 2048, 2048), (16, 512, 1000), (64, 384, 2304), (300, 1000, 1152)])
+@pytest.mark.parametrize("M,O,K", [(1, 2048, 2048), (16, 512, 1000), (64, 384, 2304), (300, 1000, 1152), (64, 2048, 6600), (300, 1000, 5000)])
 def test_gemm_same_bits_every_time(M, O, K):
     rng = np.random.default_rng(M)
     w = prepared(weights(rng, O, K, 64, BF16, True), 64)
@@ -174,7 +194,7 @@ def test_gemm_same_bits_every_time(M, O, K):
         assert torch.equal(api.gemm_w4(x, w), first)
 
 
-@pytest.mark.parametrize("M,K", [(1, 512), (6, 515), (150, 512), (150, 515)])
+@pytest.mark.parametrize("M,K", [(1, 512), (6, 515), (150, 512), (150, 515), (1500, 1030), (1500, 1031)])
 def test_gemm_captured_beside_other_calls(M, K):
     """Two graphs of different products replayed in turn with eager calls between them: none reads what another keeps."""
     rng = np.random.default_rng(M)
@@ -199,7 +219,7 @@ def test_gemm_captured_beside_other_calls(M, K):
         assert torch.equal(eager, api.gemm_w4(xs[1], ws[0]))
 
 
-@pytest.mark.parametrize("M,K", [(3, 1024), (3, 1023), (140, 1023)])
+@pytest.mark.parametrize("M,K", [(3, 1024), (3, 1023), (140, 1023), (1200, 1023)])
 def test_gemm_on_another_stream(M, K):
     rng = np.random.default_rng(K)
     w = prepared(weights(rng, 300, K, 128, BF16, True), 128)
