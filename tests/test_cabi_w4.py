@@ -33,7 +33,8 @@ def test_sizes(L):
     assert L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 128, 4616) == 0
     assert L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 128, 4611) == 5 * 4616 * 2
     assert L.bs_w4_gemm_workspace_bytes(0, 64, 4611, 128, 4611) == L.bs_w4_gemm_workspace_bytes(5, 64, 4611, 96, 4611) == 0
-    assert L.bs_w4_gemm_workspace_bytes(300, 64, 4611, 128, 4611) > 300 * 4616 * 2
+    assert L.bs_w4_gemm_workspace_bytes(300, 64, 4611, 128, 4611) == 300 * 4616 * 2
+    assert L.bs_w4_gemm_workspace_bytes(4096, 64, 4611, 128, 4611) > 4096 * 4616 * 2       # parts of tiles as well
     assert L.bs_w4_moe_workspace_bytes(3, 2, 64, 50, 64) == 3 * 2 * 64 * 4 + 2 * 3 * 2 * 56 * 2
     assert L.bs_w4_moe_workspace_bytes(3, 2, 63, 50, 63) == 3 * 2 * 64 * 4 + 2 * 3 * 2 * 56 * 2 + 3 * 64 * 2
     assert L.bs_w4_moe_workspace_bytes(0, 2, 64, 50, 64) == 0
