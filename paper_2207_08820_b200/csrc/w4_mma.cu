@@ -10,7 +10,7 @@
 // all of it again.
 //
 // Work: tiles of 128 rows by up to 128 rows of x.  A CTA takes whole tiles, neighbours at a time, as long as every CTA gets one; what is left, less than
-// two tiles a CTA, is cut into equal runs of (tile, 128 columns), and a small kernel adds the parts of the tiles that were cut, in their order.
+// two tiles a CTA, is cut (unless that saves little) into equal runs of (tile, 128 columns), and a small kernel adds the parts of the tiles that were cut, in their order.
 #include <cuda.h>
 
 #include <mutex>
@@ -49,8 +49,8 @@ struct Stretch {
     {
         const long long steps = static_cast<long long>(a.mts) * a.ots * a.g.l.cbs - static_cast<long long>(a.waves) * a.ctas * a.g.l.cbs;
         const long long b = static_cast<long long>(blockIdx.x) * a.per;
-        pos = static_cast<int>(b < steps ? b : steps);
-        end = static_cast<int>(b + a.per < steps ? b + a.per : steps);
+        pos = a.per == 0 ? 0 : static_cast<int>(b < steps ? b : steps);
+        end = a.per == 0 ? 0 : static_cast<int>(b + a.per < steps ? b + a.per : steps);
         first = pos;
     }
     __device__ __forceinline__ bool next(const MmaTiles& a)
@@ -59,7 +59,7 @@ struct Stretch {
         if (wave < a.waves) {
             tile = wave++ * a.ctas + blockIdx.x;
             c0 = 0; c1 = cbs; part = -1;
-            return true;
+            return tile < a.mts * a.ots;
         }
         if (pos >= end) return false;
         tile = pos / cbs;
@@ -493,9 +493,16 @@ bool plan(MmaTiles& a, int sms)
     const long long tiles = static_cast<long long>(a.mts) * a.ots;
     if (tiles * l.cbs > 0x7fff0000) return false;
     a.ctas = static_cast<int>(tiles * l.cbs < sms ? tiles * l.cbs : sms);
-    a.waves = static_cast<int>(tiles % a.ctas == 0 ? tiles / a.ctas : tiles / a.ctas > 0 ? tiles / a.ctas - 1 : 0);
-    const long long steps = (tiles - static_cast<long long>(a.waves) * a.ctas) * l.cbs;
-    a.per = static_cast<int>((steps + a.ctas - 1) / a.ctas);
+    // Cutting the last tiles saves steps of 0.6 us each and costs the parts' way through memory and the second launch, 4 us.
+    const long long whole = (tiles + a.ctas - 1) / a.ctas;
+    if (whole * l.cbs - tiles * l.cbs / a.ctas < 7) {
+        a.waves = static_cast<int>(whole);
+        a.per = 0;
+    } else {
+        a.waves = static_cast<int>(tiles / a.ctas > 0 ? tiles / a.ctas - 1 : 0);
+        const long long steps = (tiles - static_cast<long long>(a.waves) * a.ctas) * l.cbs;
+        a.per = static_cast<int>((steps + a.ctas - 1) / a.ctas);
+    }
     return true;
 }
 
