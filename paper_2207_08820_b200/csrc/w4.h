@@ -68,7 +68,7 @@ inline int w4_team_width(int warps, int blocks)
     return best;
 }
 // csrc/w4_mma.cu: the product on tcgen05 for many rows of x, which start on 16-byte boundaries.  part: w4_mma_workspace bytes.
-bool w4_mma_wanted(int M, const W4Layout& l);
+bool w4_mma_wanted(int M, const W4Layout& l, int sms);
 size_t w4_mma_workspace(int M, const W4Layout& l, int sms);
 int w4_mma_launch(const W4Gemm& g, bool f16, float* part, int sms, cudaStream_t st);
 

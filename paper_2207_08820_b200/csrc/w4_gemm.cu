@@ -142,7 +142,8 @@ extern "C" size_t bs_w4_gemm_workspace_bytes(int M, int O, int K, int group, lon
     using namespace bs;
     W4Layout l;
     if (M <= 0 || M > W4_MAX_DIM || !w4_layout(O, K, group, 0, l)) return 0;
-    return aligned_bytes(M, K, ldx) + (w4_mma_wanted(M, l) ? w4_mma_workspace(M, l, sm_count()) : 0);
+    const int sms = sm_count();
+    return aligned_bytes(M, K, ldx) + (w4_mma_wanted(M, l, sms) ? w4_mma_workspace(M, l, sms) : 0);
 }
 
 extern "C" int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K, int group, int zeros, bs_float_t type, const void* bias, void* y,
@@ -172,6 +173,6 @@ extern "C" int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, in
         g.ldx = ldo;
         ws += aligned_bytes(M, K, ldx);
     }
-    if (w4_mma_wanted(M, g.l)) return w4_mma_launch(g, type == BS_F16, reinterpret_cast<float*>(ws), sms, st);
+    if (w4_mma_wanted(M, g.l, sms)) return w4_mma_launch(g, type == BS_F16, reinterpret_cast<float*>(ws), sms, st);
     return type == BS_F16 ? launch<true>(g, sms, st) : launch<false>(g, sms, st);
 }

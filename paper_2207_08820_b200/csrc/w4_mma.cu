@@ -538,13 +538,19 @@ bool w4_encode_blocks(CUtensorMap* tm, const void* prepared, const W4Layout& l, 
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Up to 16 rows of x: csrc/w4_gemm.cu is faster at every size.  Above, by fitted times (24 measured pairs, bf16 and fp16, 512 x 512 to 24576 x 8192): 0.43 ns a
-// block of weights and 16 rows of x there; here 8 us more in the beginning, for the second launch and the tensor memory, and 0.5 ns a block
-// and tile of 64 or 128 rows.
-bool w4_mma_wanted(int M, const W4Layout& l)
+// Up to 16 rows of x csrc/w4_gemm.cu is faster at every size.  Above, by times fitted to 81 pairs (20 to 512 rows, 256 x 512 to 8192 x 4096): there 2 us and
+// 0.6 ns (groups of 32: 0.9) a block of weights and 16 rows of x; here 3.7 us, or 8.5 where tiles are cut, and for each of a CTA's steps 0.6 us with up to
+// 64 rows, 0.75 with more, and up to three times that with four groups a step.
+bool w4_mma_wanted(int M, const W4Layout& l, int sms)
 {
-    const double blocks = static_cast<double>(l.rbs) * l.cbs;
-    return M > 16 && 0.43 * ceil_div(M, 16) * blocks > 0.5 * ceil_div(M, 128) * blocks + 8000;
+    if (M <= 16) return false;
+    MmaTiles a{};
+    a.g.M = M;
+    a.g.l = l;
+    if (!plan(a, sms)) return false;
+    const double step = l.group == 32 ? 1.7 : l.group == 64 ? 0.85 : a.n <= 64 ? 0.6 : 0.75;
+    const double here = (a.per ? 8.5 : 3.7) + step * (static_cast<double>(a.waves) * l.cbs + a.per);
+    return 2 + (l.group == 32 ? 0.9e-3 : 0.6e-3) * l.rbs * l.cbs * ceil_div(M, 16) > here;
 }
 
 size_t w4_mma_workspace(int M, const W4Layout& l, int sms)

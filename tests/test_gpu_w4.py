@@ -133,8 +133,6 @@ def test_gemm_larger(M, O, K, group, dtype, zeros, bias):
     (4000, 333, 700, 32, BF16, True, True), (4096, 128, 1664, 128, F16, False, False), (9000, 2000, 100, 128, BF16, True, True)])
 def test_gemm_many_rows(M, O, K, group, dtype, zeros, bias):
     """The kernel for many rows of x: one tile and many, cut and whole, all ways of groups."""
-    blocks = -(-O // 16) * -(-K // 128)
-    assert 0.43 * -(-M // 16) * blocks > 0.5 * -(-M // 128) * blocks + 8000      # the library's rule for it
     check_gemm(np.random.default_rng(M + O + K), M, O, K, group, dtype, zeros, bias)
 
 
@@ -201,7 +199,7 @@ def test_gemm_same_bits_every_time(M, O, K):
         assert torch.equal(api.gemm_w4(x, w), first)
 
 
-@pytest.mark.parametrize("M,K", [(1, 512), (6, 515), (150, 512), (150, 515), (1500, 1030), (1500, 1031)])
+@pytest.mark.parametrize("M,K", [(1, 512), (6, 515), (150, 512), (150, 515), (2048, 3304), (2048, 3301)])
 def test_gemm_captured_beside_other_calls(M, K):
     """Two graphs of different products replayed in turn with eager calls between them: none reads what another keeps."""
     rng = np.random.default_rng(M)
@@ -226,7 +224,7 @@ def test_gemm_captured_beside_other_calls(M, K):
         assert torch.equal(eager, api.gemm_w4(xs[1], ws[0]))
 
 
-@pytest.mark.parametrize("M,K", [(3, 1024), (3, 1023), (140, 1023), (1200, 1023)])
+@pytest.mark.parametrize("M,K", [(3, 1024), (3, 1023), (140, 1023), (1200, 3001)])
 def test_gemm_on_another_stream(M, K):
     rng = np.random.default_rng(K)
     w = prepared(weights(rng, 300, K, 128, BF16, True), 128)
