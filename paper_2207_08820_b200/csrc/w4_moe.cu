@@ -337,12 +337,26 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
         }
         // teams without rows multiply what the stages hold, and drop it
         for (int c = k0; c < l.cbs + k0; c += split) {
+            // the first terms on their way while the weights are waited for, and with eight slots the second ones
+            uint4 v[NT == 1 ? 2 : 1][NT][4];
+            if (c < l.cbs) {
+#pragma unroll
+                for (int t = 0; t < (NT == 1 ? 2 : 1); ++t)
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) load_block_x(v[t][k], row[k] + (t ? lo : 0), c, l.K, c < full, lane);
+            }
             ring.landed(g.status);
             if (c < l.cbs) {
                 W4Tile<NG, ZEROS> w[2];
                 ring.take(w);
-                if (c < full) w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return __ldg(reinterpret_cast<const uint4*>(row[k] + (t ? lo : 0) + c * W4_COLS + 32 * j)); }, tot);
-                else w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return load_x(row[k] + (t ? lo : 0) + c * W4_COLS, 32 * j, l.K - c * W4_COLS - 8 * (lane & 3)); }, tot);
+                if (NT == 1) {
+                    w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return v[NT == 1 ? t : 0][k][j]; }, tot);
+                } else {
+                    w4_blocks<false, F16, 1>(w, [&](int k, int j, int) { return v[0][k][j]; }, tot);
+#pragma unroll
+                    for (int k = 0; k < NT; ++k) load_block_x(v[0][k], row[k] + lo, c, l.K, c < full, lane);
+                    w4_blocks<false, F16, 1>(w, [&](int k, int j, int) { return v[0][k][j]; }, tot);
+                }
             }
             ring.release(lane);
             ring.next();
