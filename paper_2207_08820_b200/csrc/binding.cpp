@@ -464,7 +464,7 @@ PyObject* w4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n)
             if (!y.is_cuda() || y.scalar_type() != x.scalar_type() || y.sizes() != at::IntArrayRef(shape)) mismatch("an output of x's type and the product's shape expected");
             same_device(y, x);
             ldy = row_pitch(y, O);
-            if (M > 0 && (overlap(y, ldy, x, ldx) || overlap(y, ldy, w, w.numel()))) mismatch("the output overlaps an input");
+            if (M > 0 && (overlap(y, ldy, x, ldx) || overlap(y, ldy, w, w.numel()) || (bias && overlap(y, ldy, tensor(a[7]), O)))) mismatch("the output overlaps an input");
         } else {
             y = fresh(shape, x.scalar_type(), x);
         }
@@ -509,7 +509,9 @@ PyObject* w4_moe(PyObject*, PyObject* const* a, Py_ssize_t n)
             if (y.scalar_type() != x.scalar_type() || y.sizes() != x.sizes()) mismatch("an output of x's type and shape expected");
             same_device(y, x);
             pointer(y);
-            if (T > 0 && overlap(y, H, x, ldx)) mismatch("the output overlaps an input");
+            if (T > 0 && (overlap(y, H, x, ldx) || overlap(y, H, router, H))) mismatch("the output overlaps an input");
+            for (int i = 2; i < 5 && T > 0; ++i)
+                if (overlap(y, H, tensor(a[i]), tensor(a[i]).numel())) mismatch("the output overlaps an input");
         } else {
             y = fresh(x.sizes(), x.scalar_type(), x);
         }

@@ -548,6 +548,7 @@ bool w4_mma_wanted(int M, const W4Layout& l, int sms)
     a.g.M = M;
     a.g.l = l;
     if (!plan(a, sms)) return false;
+    if (ceil_div(M, 16) > 65535) return true;       // a grid has no more tiles of 16 rows
     const double step = l.group == 32 ? 1.7 : l.group == 64 ? 0.85 : a.n <= 64 ? 0.6 : 0.75;
     const double here = (a.per ? 8.5 : 3.7) + step * (static_cast<double>(a.waves) * l.cbs + a.per);
     return 2 + (l.group == 32 ? 0.9e-3 : 0.6e-3) * l.rbs * l.cbs * ceil_div(M, 16) > here;

@@ -418,3 +418,47 @@ def test_refusals_on_the_device():
         api.gemm_w4(x, e)
     api.moe_w4(x, router, e, e, d, 2)
     api.bs_check_status()
+
+
+def test_gemm_as_many_rows_as_are_taken():
+    """The largest number of rows, with so little work in each that few-row tiles would be the fastest: more of them than a grid has."""
+    rng = np.random.default_rng(12)
+    w = weights(rng, 8, 16, 32, BF16, False)
+    x = normal(rng, (1 << 20, 16), BF16)
+    y = api.gemm_w4(x.cuda(), prepared(w, 32))
+    api.bs_check_status()
+    want, far = ref.gemm(x, ref.matrix(*w, 32), None, BF16)
+    assert ((y.cpu().double() - want).abs() <= far).all()
+    with pytest.raises(BitserialError):
+        api.gemm_w4(torch.zeros((1 << 20) + 1, 16, dtype=BF16, device="cuda"), prepared(w, 32))
+
+
+def test_one_token_without_a_batch():
+    rng = np.random.default_rng(13)
+    w = weights(rng, 40, 72, 32, F16, True)
+    x = normal(rng, (72,), F16)
+    y = api.gemm_w4(x.cuda(), prepared(w, 32))
+    want, far = ref.gemm(x[None], ref.matrix(*w, 32), None, F16)
+    assert y.shape == (40,) and ((y.cpu().double() - want[0]).abs() <= far[0]).all()
+    xm, router, gate, up, down = moe_case(rng, 1, 5, 72, 40, 32, 32, F16, False, True)
+    e = [prepared(p, 32) for p in (gate, up, down)]
+    batch = api.moe_w4(xm.cuda(), router.cuda(), *e, 2)
+    out = torch.empty(72, dtype=F16, device="cuda")
+    single = api.moe_w4(xm[0].cuda(), router.cuda(), *e, 2, out=out)
+    assert single[0].data_ptr() == out.data_ptr() and all(torch.equal(a, b[0]) for a, b in zip(single, batch))
+
+
+def test_outputs_that_are_inputs_are_refused():
+    rng = np.random.default_rng(14)
+    w = prepared(weights(rng, 64, 64, 32, BF16, False), 32)
+    x, bias = normal(rng, (1, 64), BF16).cuda(), normal(rng, (64,), BF16).cuda()
+    e = prepared(weights(rng, 64, 64, 32, BF16, False, (2,)), 32)
+    d = prepared(weights(rng, 64, 64, 32, BF16, False, (2,)), 32)
+    router = normal(rng, (2, 64), BF16).cuda()
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w, bias, out=bias.view(1, 64))
+    with pytest.raises(ValueError):
+        api.gemm_w4(x, w, out=w.data[:128].view(BF16).view(1, 64))
+    for out in (x, router[1:], e.data[:128].view(BF16).view(1, 64), d.data[:128].view(BF16).view(1, 64)):
+        with pytest.raises(ValueError):
+            api.moe_w4(x, router, e, e, d, 1, out=out)
