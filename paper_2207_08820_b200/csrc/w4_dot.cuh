@@ -167,6 +167,11 @@ struct W4TeamRing {
                          ::"r"(base + stage * STAGE + m * WARPS * BLOCK), "l"(reinterpret_cast<uint64_t>(maps[m])), "r"(bar), "r"(0), "r"(c), "r"(rb[m]), "r"(e) : "memory");
         next();
     }
+    // The same blocks on their way to L2, which may begin before the kernel in front has ended: whatever it writes there later, L2 holds.
+    static __device__ __forceinline__ void hint(const CUtensorMap* map, int rb, int c, int e)
+    {
+        asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(c), "r"(rb), "r"(e) : "memory");
+    }
     // Behind the last one: no copy outlives the CTA, whatever the warps waited for.
     __device__ __forceinline__ void drain(int filled, int* status)
     {

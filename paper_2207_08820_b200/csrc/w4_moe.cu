@@ -65,9 +65,15 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     __shared__ unsigned long long keys[MAX_EXPERTS];
     __shared__ int choice[MAX_TOP];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x, m0 = blockIdx.y * 8;
+    const int tiles = (g.E + 15) / 16, steps = (g.H + 31) / 32;
+    // the router's rows start for L2 while the kernel in front drains
+    if (blockIdx.y == 0 && threadIdx.x < 16)
+        for (int e = rank * 16 + threadIdx.x; e < g.E; e += ROUTE_CTAS * 16) {
+            const unsigned long long row = (reinterpret_cast<unsigned long long>(g.router) + static_cast<size_t>(e) * g.H * 2) & ~15ull;
+            if (g.H >= 8) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"(g.H / 8 * 16) : "memory");
+        }
     const T* x = static_cast<const T*>(dependent_begin(g.x));
     const T* router = behind_wait<T>(g.router);
-    const int tiles = (g.E + 15) / 16, steps = (g.H + 31) / 32;
     const int mx = m0 + (lane >> 2);
     // every CTA of the cluster runs before one writes to another's shared memory
     asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
