@@ -151,8 +151,10 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     }
 }
 
-// The work of a pass of 64 tokens: jobs of an expert and up to J of its slots, made by every CTA for itself (at most 2048 slots).
-constexpr int MOST_JOBS = MAX_EXPERTS + PASS * MAX_TOP / 8;
+// The work of a pass of 64 tokens: jobs of an expert and up to eight of its slots, made by every CTA for itself (at most 2048 slots).  An expert of more slots
+// has several jobs, which read its weights again, from L2: jobs of 16 slots (two tiles of x, twice the registers) took 105 us where these take 100,
+// with 16 slots an expert (64 tokens, 2 of 8 experts, 2048 x 4096), and 77 to 68 with eight.
+constexpr int J = 8, MOST_JOBS = MAX_EXPERTS + PASS * MAX_TOP / J;
 struct Jobs {
     unsigned tokens[2][MAX_EXPERTS];    // which tokens chose an expert, a bit each
     uint16_t begin[MAX_EXPERTS];        // where an expert's slots begin
@@ -163,7 +165,6 @@ struct Jobs {
     int n;
 };
 
-template <int J>
 __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int threads)
 {
     const int slots = (g.T - t0 < PASS ? g.T - t0 : PASS) * g.top_k;
@@ -210,12 +211,11 @@ __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int
 
 // h = weight * silu(gate) * up of 16 rows of an expert for the slots of a job.  The warps of a team share the reduction of 16 rows; the last warp copies
 // the blocks of the CTA's items ahead, also while the sums of an item are put together.
-template <bool F16, int NG, bool ZEROS, int NT>
+template <bool F16, int NG, bool ZEROS>
 __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const __grid_constant__ MoeArgs g, int split)
 {
     typedef typename W4Type<F16>::T T;
     typedef W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES> Ring;
-    constexpr int J = NT * 8;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[2 * GATE_STAGES];
     __shared__ Jobs jobs;
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
     Ring ring(smem, bars, warp, lane);
     const T* x = static_cast<const T*>(dependent_begin(g.xa ? g.xa : g.x));
     const long long ldx = g.xa ? g.ldxa : g.ldx;
-    find_jobs<J>(g, jobs, t0, WARPS * 32 + 32);
+    find_jobs(g, jobs, t0, WARPS * 32 + 32);
     const W4Layout& l = g.lu;
     // an item: a job and the rows of all teams
     const int per_job = (l.rbs + teams - 1) / teams, items = jobs.n * per_job, full = l.K / W4_COLS;
@@ -245,38 +245,27 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
         const int job = item / per_job, rb = (item - job * per_job) * teams + team, beg = jobs.first[job];
         // a job's slots end where the next one's begin; lanes without a slot compute the last one's again
         const int n = jobs.first[job + 1] - beg;
-        const T* row[NT];
-#pragma unroll
-        for (int k = 0; k < NT; ++k) row[k] = x + (t0 + jobs.token[beg + min(k * 8 + (lane >> 2), n - 1)]) * ldx + 8 * (lane & 3);
-        float tot[2][NT][4];
-#pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
+        const T* row = x + (t0 + jobs.token[beg + min(lane >> 2, n - 1)]) * ldx + 8 * (lane & 3);
+        float tot[2][1][4] = {};
         // teams without rows multiply what the stages hold, and drop it
         for (int c = k0; c < l.cbs + k0; c += split) {
-            uint4 v[NT][4];
-            if (c < l.cbs) {
-#pragma unroll
-                for (int k = 0; k < NT; ++k) load_block_x(v[k], row[k], c, l.K, c < full, lane);
-            }
+            uint4 v[4];
+            if (c < l.cbs) load_block_x(v, row, c, l.K, c < full, lane);
             ring.landed(g.status);
             if (c < l.cbs) {
                 W4Tile<NG, ZEROS> w[2];
                 ring.take(w);
-                w4_blocks<F16, F16, 1>(w, [&](int k, int j, int) { return v[k][j]; }, tot);
+                w4_blocks<F16, F16, 1>(w, [&](int, int j, int) { return v[j]; }, tot);
             }
             ring.release(lane);
             ring.next();
         }
 #pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int m = k * 8 + 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
-                part[warp][0][m][r] = tot[0][k][i];
-                part[warp][1][m][r] = tot[1][k][i];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int m = 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
+            part[warp][0][m][r] = tot[0][0][i];
+            part[warp][1][m][r] = tot[1][0][i];
+        }
         asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
         for (int q = k0 * 32 + lane; q < J * 16; q += 32 * split) {
             const int m = q >> 4, r = q & 15, i = rb * 16 + r;
@@ -300,11 +289,10 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
 // z = Down_e h of 32 rows of an expert for the slots of a job, items and teams as above.  32 rows a warp, because the hidden values of eight slots are four
 // times the weights' bytes that they meet in 16.  (With the tokens' sums kept in the CTA instead, job after job, a job's few blocks waited for
 // barriers: 95 us where this and the sums behind it take 48, 64 tokens of 128 experts.)
-template <bool F16, int NG, bool ZEROS, int NT>
+template <bool F16, int NG, bool ZEROS>
 __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int split)
 {
     typedef W4TeamRing<NG, ZEROS, 2, WARPS, DOWN_STAGES> Ring;
-    constexpr int J = NT * 8;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[2 * DOWN_STAGES];
     __shared__ Jobs jobs;
@@ -314,7 +302,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
     Ring ring(smem, bars, warp, lane);
     dependent_begin(g.down);
     const __nv_bfloat16* hidden = behind_wait<__nv_bfloat16>(g.hi);
-    find_jobs<J>(g, jobs, t0, WARPS * 32 + 32);
+    find_jobs(g, jobs, t0, WARPS * 32 + 32);
     const W4Layout& l = g.ld;
     const int per_job = (l.rbs + 2 * teams - 1) / (2 * teams), items = jobs.n * per_job, full = l.K / W4_COLS;
     if (warp == WARPS) {
@@ -333,48 +321,30 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         const int job = item / per_job, rb = (item - job * per_job) * 2 * teams + team, beg = jobs.first[job], n = jobs.first[job + 1] - beg;
         const size_t slot0 = static_cast<size_t>(t0) * g.top_k;
-        const __nv_bfloat16* row[NT];
-        float tot[2][NT][4];
-#pragma unroll
-        for (int k = 0; k < NT; ++k) {
-            row[k] = hidden + (slot0 + jobs.slot[beg + min(k * 8 + (lane >> 2), n - 1)]) * g.ldh + 8 * (lane & 3);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tot[0][k][i] = tot[1][k][i] = 0.f;
-        }
+        const __nv_bfloat16* row = hidden + (slot0 + jobs.slot[beg + min(lane >> 2, n - 1)]) * g.ldh + 8 * (lane & 3);
+        float tot[2][1][4] = {};
         // teams without rows multiply what the stages hold, and drop it
         for (int c = k0; c < l.cbs + k0; c += split) {
-            // the first terms on their way while the weights are waited for, and with eight slots the second ones
-            uint4 v[NT == 1 ? 2 : 1][NT][4];
+            uint4 v[2][4];          // both terms on their way while the weights are waited for
             if (c < l.cbs) {
-#pragma unroll
-                for (int t = 0; t < (NT == 1 ? 2 : 1); ++t)
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) load_block_x(v[t][k], row[k] + (t ? lo : 0), c, l.K, c < full, lane);
+                load_block_x(v[0], row, c, l.K, c < full, lane);
+                load_block_x(v[1], row + lo, c, l.K, c < full, lane);
             }
             ring.landed(g.status);
             if (c < l.cbs) {
                 W4Tile<NG, ZEROS> w[2];
                 ring.take(w);
-                if (NT == 1) {
-                    w4_blocks<false, F16, 2>(w, [&](int k, int j, int t) { return v[NT == 1 ? t : 0][k][j]; }, tot);
-                } else {
-                    w4_blocks<false, F16, 1>(w, [&](int k, int j, int) { return v[0][k][j]; }, tot);
-#pragma unroll
-                    for (int k = 0; k < NT; ++k) load_block_x(v[0][k], row[k] + lo, c, l.K, c < full, lane);
-                    w4_blocks<false, F16, 1>(w, [&](int k, int j, int) { return v[0][k][j]; }, tot);
-                }
+                w4_blocks<false, F16, 2>(w, [&](int, int j, int t) { return v[t][j]; }, tot);
             }
             ring.release(lane);
             ring.next();
         }
 #pragma unroll
-        for (int k = 0; k < NT; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int m = k * 8 + 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
-                part[warp][m][r] = tot[0][k][i];
-                part[warp][m][r + 16] = tot[1][k][i];
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int m = 2 * (lane & 3) + (i & 1), r = (lane >> 2) + 8 * (i >> 1);
+            part[warp][m][r] = tot[0][0][i];
+            part[warp][m][r + 16] = tot[1][0][i];
+        }
         asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
         for (int q = k0 * 32 + lane; q < n * 32; q += 32 * split) {
             const int m = q >> 5, r = q & 31, o = (rb + (r >> 4) * teams) * 16 + (r & 15);      // two blocks of rows, `teams` apart
@@ -441,48 +411,47 @@ int launch_clusters(void (*kern)(P...), dim3 grid, int threads, size_t smem, int
     cudaGetLastError();
     return BS_ERR_CUDA;
 }
-template <bool F16, int NG, bool ZEROS, int NT>
+template <bool F16, int NG, bool ZEROS>
 int launch_gate(MoeArgs& g, int sms, cudaStream_t st)
 {
     const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
     const int split = w4_team_width(WARPS, g.lu.cbs);
     const long long items = static_cast<long long>(jobs) * ceil_div(g.lu.rbs, WARPS / split);
     constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES>::BYTES;
-    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, smem) || !w4_encode_blocks(&g.tg, g.gate, g.lu, g.E, split, WARPS / split) ||
+    if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS>, smem) || !w4_encode_blocks(&g.tg, g.gate, g.lu, g.E, split, WARPS / split) ||
         !w4_encode_blocks(&g.tu, g.up, g.lu, g.E, split, WARPS / split))
         return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
+    return launch_dependent(w4_moe_gate_kernel<F16, NG, ZEROS>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
                             dim3(WARPS * 32 + 32), smem, st, g, split);
 }
-template <bool F16, int NG, bool ZEROS, int NT>
+template <bool F16, int NG, bool ZEROS>
 int launch_down(MoeArgs& g, int sms, cudaStream_t st)
 {
     const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
     const int split = w4_team_width(WARPS, g.ld.cbs);
     const long long items = static_cast<long long>(jobs) * ceil_div(g.ld.rbs, 2 * WARPS / split);
     constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, DOWN_STAGES>::BYTES;
-    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS, NT>, smem) || !w4_encode_blocks(&g.td, g.down, g.ld, g.E, split, WARPS / split)) return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS, NT>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
+    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS>, smem) || !w4_encode_blocks(&g.td, g.down, g.ld, g.E, split, WARPS / split)) return BS_ERR_CUDA;
+    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
                             dim3(WARPS * 32 + 32), smem, st, g, split);
 }
-template <bool F16, int NT>
+template <bool F16>
 int launch_experts(MoeArgs& g, int sms, cudaStream_t st)
 {
     int rc;
     const int nu = g.lu.group == 32 ? 4 : g.lu.group == 64 ? 2 : 1, nd = g.ld.group == 32 ? 4 : g.ld.group == 64 ? 2 : 1;
-    if (g.lu.zeros) rc = nu == 4 ? launch_gate<F16, 4, true, NT>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, true, NT>(g, sms, st) : launch_gate<F16, 1, true, NT>(g, sms, st);
-    else rc = nu == 4 ? launch_gate<F16, 4, false, NT>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, false, NT>(g, sms, st) : launch_gate<F16, 1, false, NT>(g, sms, st);
+    if (g.lu.zeros) rc = nu == 4 ? launch_gate<F16, 4, true>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, true>(g, sms, st) : launch_gate<F16, 1, true>(g, sms, st);
+    else rc = nu == 4 ? launch_gate<F16, 4, false>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, false>(g, sms, st) : launch_gate<F16, 1, false>(g, sms, st);
     if (rc != BS_OK) return rc;
-    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true, NT>(g, sms, st) : nd == 2 ? launch_down<F16, 2, true, NT>(g, sms, st) : launch_down<F16, 1, true, NT>(g, sms, st);
-    return nd == 4 ? launch_down<F16, 4, false, NT>(g, sms, st) : nd == 2 ? launch_down<F16, 2, false, NT>(g, sms, st) : launch_down<F16, 1, false, NT>(g, sms, st);
+    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true>(g, sms, st) : nd == 2 ? launch_down<F16, 2, true>(g, sms, st) : launch_down<F16, 1, true>(g, sms, st);
+    return nd == 4 ? launch_down<F16, 4, false>(g, sms, st) : nd == 2 ? launch_down<F16, 2, false>(g, sms, st) : launch_down<F16, 1, false>(g, sms, st);
 }
 template <bool F16>
 int launch_moe(MoeArgs& g, int sms, cudaStream_t st)
 {
     int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
     if (rc != BS_OK) return rc;
-    // a second job of an expert reads its weights again: jobs of 16 slots where more than eight are likely
-    rc = (g.T < PASS ? g.T : PASS) * g.top_k > 5 * g.E ? launch_experts<F16, 2>(g, sms, st) : launch_experts<F16, 1>(g, sms, st);
+    rc = launch_experts<F16>(g, sms, st);
     if (rc != BS_OK) return rc;
     const long long want = (static_cast<long long>(g.T) * (g.ldz / 4) + 255) / 256, most = 8ll * sms;
     return launch_dependent(w4_moe_sum_kernel<F16>, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(256), 0, st, g);
