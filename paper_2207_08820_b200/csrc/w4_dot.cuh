@@ -11,25 +11,27 @@
 
 namespace bs {
 
-// The eight codes of a word as four pairs of numbers less the zero point, exact: 128 + code (bf16) or 1024 + code (fp16) is the code under a fixed
-// exponent, and the difference to 128 + zero or 1024 + zero is a whole number of at most four bits and a sign.  Logic and shifts go through a pipe of half
-// rate, which bounds these kernels: the pairs that are not in place are moved by the upper half of a product, which takes another pipe (bf16), or
-// stay in place four bits up, as 1024 + 16 code, where the mantissa has room for them (fp16).
+// The eight codes of a word as four pairs of numbers (code - zero point) / PART, exact.  A code in a mantissa's lowest four bits under a fixed exponent is 128 +
+// code (bf16) or 1024 + code (fp16); four bits up it is 1024 + 16 code in fp16, and in bf16, whose mantissa ends there, a number below or just above the
+// smallest normal one, where numbers are evenly spaced: code 2^-129.  One fused operation takes either to (code - zero point) / PART, a whole
+// number of at most four bits and a sign in quarters (bf16) or ones.  So a word costs four masks, one shift and four of these; logic and shifts go
+// through a pipe of half rate, which bounds these kernels.
 template <bool F16> struct W4Type;
 template <> struct W4Type<false> {
     typedef __nv_bfloat16 T;
-    static constexpr uint32_t BASE = 0x43004300u;
+    static constexpr float PART = 4.f;
     // z: the zero point in both halves
     static __device__ __forceinline__ void pairs(uint32_t w, uint32_t z, uint32_t (&v)[4])
     {
-        uint32_t u[4] = {(w & 0x000f000fu) | BASE, 0, 0, 0};
-        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[1]) : "r"(w & 0x00f000f0u), "r"(1u << 28), "r"(BASE));
-        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[2]) : "r"(w & 0x0f000f00u), "r"(1u << 24), "r"(BASE));
-        asm("mad.hi.u32 %0, %1, %2, %3;" : "=r"(u[3]) : "r"(w & 0xf000f000u), "r"(1u << 20), "r"(BASE));
-        const uint32_t zero = BASE + z;
+        const uint32_t h = w >> 8;
+        const uint32_t u[4] = {(w & 0x000f000fu) | 0x43004300u, w & 0x00f000f0u, (h & 0x000f000fu) | 0x43004300u, h & 0x00f000f0u};
+        const uint32_t quarter = 0x3e803e80u, most = 0x7f007f00u, t32 = 0x42004200u, high = 0xc200c200u + z;      // most: 2^127; high: -(128 + zero) / 4
+        const __nv_bfloat162 low = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&high), *reinterpret_cast<const __nv_bfloat162*>(&t32));     // -zero / 4
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 d = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u[i]), *reinterpret_cast<const __nv_bfloat162*>(&zero));
+            const __nv_bfloat162 b = *reinterpret_cast<const __nv_bfloat162*>(&u[i]);
+            const __nv_bfloat162 d = i & 1 ? __hfma2(b, *reinterpret_cast<const __nv_bfloat162*>(&most), low)
+                                           : __hfma2(b, *reinterpret_cast<const __nv_bfloat162*>(&quarter), *reinterpret_cast<const __nv_bfloat162*>(&high));
             v[i] = *reinterpret_cast<const uint32_t*>(&d);
         }
     }
@@ -49,6 +51,7 @@ template <> struct W4Type<false> {
 };
 template <> struct W4Type<true> {
     typedef __half T;
+    static constexpr float PART = 1.f;
     static constexpr uint32_t BASE = 0x64006400u;
     static __device__ __forceinline__ void pairs(uint32_t w, uint32_t z, uint32_t (&v)[4])
     {
@@ -137,24 +140,19 @@ struct W4TeamRing {
         }
     }
     // Bounded wait; one that runs out sets the status word, later ones then poll once.
+    static __device__ __forceinline__ bool poll(uint32_t on, unsigned parity)
+    {
+        unsigned there;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(there) : "r"(on), "r"(parity) : "memory");
+        return there;
+    }
     __device__ __forceinline__ void wait(uint32_t on, unsigned parity, int* status)
     {
-        unsigned left;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mov.u32 %0, %3;\n\t"
-            "W4_WAIT:\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "@p bra W4_DONE;\n\t"
-            "sub.u32 %0, %0, 1;\n\t"
-            "setp.ne.u32 p, %0, 0;\n\t"
-            "@p bra W4_WAIT;\n\t"
-            "W4_DONE:\n\t}"
-            : "=&r"(left) : "r"(on), "r"(parity), "r"(limit) : "memory");
-        if (left == 0) {
-            if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
-            limit = 1;
-        }
+        if (poll(on, parity)) return;       // mostly there: nothing is counted
+        for (unsigned left = limit; left > 0; --left)
+            if (poll(on, parity)) return;
+        if (limit > 1) atomicOr(status, STATUS_TIMEOUT);
+        limit = 1;
     }
     // The producer's thread: once the stage is free, the blocks from (c, rb) on of matrix e of each of the NB tensor maps.
     __device__ __forceinline__ void fill(const CUtensorMap* const (&maps)[NB], const int (&rb)[NB], int c, int e, int* status)
@@ -211,7 +209,7 @@ struct W4TeamRing {
     }
 };
 
-// tot[r][n] += RT blocks of different rows times n tiles of eight rows of x: x(n, j, term) are the lane's eight columns of word j, of which there are TERMS
+// tot[r][n] += 1 / PART (of X16's type) of RT blocks of different rows times n tiles of eight rows of x: x(n, j, term) are the lane's eight columns of word j, of which there are TERMS
 // to be added up.  x is of the type that X16 says, the scales of S16's.
 template <bool X16, bool S16, int TERMS, int RT, int NT, int NG, bool ZEROS, typename X>
 __device__ __forceinline__ void w4_blocks(const W4Tile<NG, ZEROS> (&w)[RT], const X& x, float (&tot)[RT][NT][4])

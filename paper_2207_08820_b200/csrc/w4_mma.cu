@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                             for (int i = 0; i < 8; ++i) {
                                 uint32_t lo, hi;
                                 f2_split(tot[p][i], lo, hi);
-                                const uint32_t both = Ty::round2(__uint_as_float(lo) + bias, __uint_as_float(hi) + bias), other = __shfl_xor_sync(0xffffffffu, both, 1);
+                                const uint32_t both = Ty::round2(fmaf(__uint_as_float(lo), Ty::PART, bias), fmaf(__uint_as_float(hi), Ty::PART, bias)), other = __shfl_xor_sync(0xffffffffu, both, 1);
                                 *reinterpret_cast<uint32_t*>(y) = lane & 1 ? __byte_perm(other, both, 0x7632) : __byte_perm(both, other, 0x5410);
                                 y += 2 * a.g.ldy;
                             }
@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                             uint32_t lo, hi;
                             f2_split(tot[p][i], lo, hi);
                             const int m = p * 16 + 2 * i;
-                            if (m < width && m < left) y[m * a.g.ldy] = Ty::round(__uint_as_float(lo) + bias);
-                            if (m < width && m + 1 < left) y[(m + 1) * a.g.ldy] = Ty::round(__uint_as_float(hi) + bias);
+                            if (m < width && m < left) y[m * a.g.ldy] = Ty::round(fmaf(__uint_as_float(lo), Ty::PART, bias));
+                            if (m < width && m + 1 < left) y[(m + 1) * a.g.ldy] = Ty::round(fmaf(__uint_as_float(hi), Ty::PART, bias));
                         }
                 }
             } else {
@@ -415,8 +415,8 @@ __global__ void __launch_bounds__(Roles<FEW>::WARPS * 32, 1) w4_mma_kernel(const
                         for (int i = 0; i < 8; ++i) {
                             uint32_t lo, hi;
                             f2_split(tot[p][i], lo, hi);
-                            out[(p * 16 + 2 * i) * ROWS] = __uint_as_float(lo);
-                            out[(p * 16 + 2 * i + 1) * ROWS] = __uint_as_float(hi);
+                            out[(p * 16 + 2 * i) * ROWS] = __uint_as_float(lo) * Ty::PART;
+                            out[(p * 16 + 2 * i + 1) * ROWS] = __uint_as_float(hi) * Ty::PART;
                         }
                     }
             }

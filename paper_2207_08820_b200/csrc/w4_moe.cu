@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[2 * GATE_STAGES];
     __shared__ Jobs jobs;
-    __shared__ float part[WARPS][2][J][17];
+    __shared__ float parts[2][WARPS][2][J][17];     // items take turns: one barrier each
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
     const int team = warp / split, k0 = warp % split, teams = WARPS / split;
     Ring ring(smem, bars, warp, lane);
@@ -241,7 +241,9 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
         }
         return;
     }
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    int turn = 0;
+    for (int item = blockIdx.x; item < items; item += gridDim.x, turn ^= 1) {
+        float (*part)[2][J][17] = parts[turn];
         const int job = item / per_job, rb = (item - job * per_job) * teams + team, beg = jobs.first[job];
         // a job's slots end where the next one's begin; lanes without a slot compute the last one's again
         const int n = jobs.first[job + 1] - beg;
@@ -275,6 +277,8 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
                 gate += part[team * split + k][0][m][r];
                 up += part[team * split + k][1][m][r];
             }
+            gate *= W4Type<F16>::PART;
+            up *= W4Type<F16>::PART;
             const size_t slot = static_cast<size_t>(t0) * g.top_k + jobs.slot[beg + m];
             const float h = gate / (1.f + expf(-gate)) * up * g.weights[slot];
             const __nv_bfloat16 hi = __float2bfloat16_rn(h);
@@ -282,7 +286,6 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
             // an infinite or NaN value has no remainder
             g.lo[slot * g.ldh + i] = isfinite(__bfloat162float(hi)) ? __float2bfloat16_rn(h - __bfloat162float(hi)) : __float2bfloat16_rn(0.f);
         }
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
     }
 }
 
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[2 * DOWN_STAGES];
     __shared__ Jobs jobs;
-    __shared__ float part[WARPS][J][33];
+    __shared__ float parts[2][WARPS][J][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t0 = blockIdx.y * PASS;
     const int team = warp / split, k0 = warp % split, teams = WARPS / split;
     Ring ring(smem, bars, warp, lane);
@@ -318,7 +321,9 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
         return;
     }
     const long long lo = g.lo - g.hi;
-    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+    int turn = 0;
+    for (int item = blockIdx.x; item < items; item += gridDim.x, turn ^= 1) {
+        float (*part)[J][33] = parts[turn];
         const int job = item / per_job, rb = (item - job * per_job) * 2 * teams + team, beg = jobs.first[job], n = jobs.first[job + 1] - beg;
         const size_t slot0 = static_cast<size_t>(t0) * g.top_k;
         const __nv_bfloat16* row = hidden + (slot0 + jobs.slot[beg + min(lane >> 2, n - 1)]) * g.ldh + 8 * (lane & 3);
@@ -351,9 +356,8 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const _
             if (o >= g.H) continue;
             float v = 0.f;
             for (int k = 0; k < split; ++k) v += part[team * split + k][m][r];
-            g.z[(slot0 + jobs.slot[beg + m]) * g.ldz + o] = v;
+            g.z[(slot0 + jobs.slot[beg + m]) * g.ldz + o] = v * W4Type<false>::PART;
         }
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * split) : "memory");
     }
 }
 
