@@ -1,8 +1,10 @@
 // Product of 16-bit activations with 4-bit weights: y[m][o] = sum_g s[o][g] * sum_{k in g} x[m][k] (q[o][k] - z[o][g]) + bias[o].
 //
-// Few rows of x: bound by the weights' bytes.  w4_gemm_kernel streams them through shared memory, every warp a part of the reduction of 16 rows, and
-// multiplies with mma.sync (w4_dot.cuh), where eight rows of x cost what one does; products are exact, sums of a group in 32 bits, scaled in
-// 32 bits, and rounded once.  More rows: csrc/w4_mma.cu.
+// Few rows of x: w4_gemm_kernel streams the weights through shared memory, every warp a part of the reduction of 16 rows, and multiplies with mma.sync
+// (w4_dot.cuh), where eight rows of x cost what one does; products are exact, sums of a group in 32 bits, scaled in 32 bits, and rounded once.
+// The bytes of the weights would bound it; what does is the expansion of the codes, whose instructions fill 60 % of the issue slots, the rest waits for
+// one another.  One row, 24576 x 8192: 28.7 us, 3.6 TB/s, where the bare stream takes 18 and the copy rate 16 (with 8 rows 31, with 16 46).  More rows:
+// csrc/w4_mma.cu.
 #include "w4_dot.cuh"
 
 namespace bs {
@@ -12,7 +14,8 @@ constexpr int WARPS = 8, STAGES = 6;
 
 // An item is 16 rows of the weights for each of WARPS / split teams and 8 NT rows of x; a team's warps take the blocks of the reduction in turn.  A CTA goes
 // through several items; the last warp copies their blocks ahead, also while the sums of an item are put together.
-template <int NT> constexpr int ctas_of() { return NT == 1 ? 3 : 2; }      // per SM
+// Per SM, as the registers allow: a fourth CTA of one tile spills (1 x 4096 x 4096 6.4 us in place of 5.3).
+template <int NT> constexpr int ctas_of() { return NT == 1 ? 3 : 2; }
 template <bool F16, int NG, bool ZEROS, int NT>
 __global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel(const __grid_constant__ W4Gemm g, const __grid_constant__ CUtensorMap tw, int split)
 {
@@ -94,7 +97,8 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel
     }
 }
 
-// Rows of x that do not start on 16-byte boundaries, brought to ones that do, zeros behind K.
+// Rows of x that do not start on 16-byte boundaries, brought to ones that do, zeros behind K: the products' loads and tensor copies are of 16 bytes.  One more
+// launch, 2.9 us with 33 rows of 4611 columns (1383 outputs: 10.5 in place of 7.6 us), bound by its latency.
 __global__ void __launch_bounds__(256) w4_align_rows_kernel(const uint16_t* x, long long ldx, int M, int K, uint16_t* out, int ldo)
 {
     x = dependent_begin(x);
@@ -125,6 +129,7 @@ int launch_tile(const W4Gemm& g, int sms, cudaStream_t st)
 template <bool F16, int NG, bool ZEROS>
 int launch_tiles(const W4Gemm& g, int sms, cudaStream_t st)
 {
+    // a tile of 16 rows costs more than one of 8 (24576 x 8192: 9 rows 41 us, 8 rows 31) and less than two of them, which would read the weights twice
     return g.M <= 8 ? launch_tile<F16, NG, ZEROS, 1>(g, sms, st) : launch_tile<F16, NG, ZEROS, 2>(g, sms, st);
 }
 template <bool F16>

@@ -3,8 +3,10 @@
 //   gate    h[slot] = weight * silu(Gate_e x) * (Up_e x) for every slot (token, choice)
 //   down    z[slot] = Down_e h[slot]
 //   sum     y[token] = sum over its slots of z[slot]
-// Bound by the bytes of the chosen experts' weights: each of their blocks is read once for up to 64 tokens (more tokens are further passes), through
-// shared memory, and multiplied with mma.sync (w4_dot.cuh).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
+// Each block of the chosen experts' weights comes from HBM once for up to 64 tokens (more tokens are further passes), through shared memory, and is multiplied
+// with mma.sync (w4_dot.cuh).  What bounds it: for one token the four launches (12 us with next to no weights; 64 experts of 2048 x 1024, 8 chosen: 26 us, of
+// which their bytes take 4), with more the expansion of the codes (64 tokens, 128 experts of 2048 x 768: 121 us at 2.5 TB/s; 8 tokens, 2 of 16
+// experts of 4096 x 8192: 134 to 180 us at 4.1 to 3.0 TB/s, as the choices fall).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
 // of mantissa), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
 #include "w4_dot.cuh"
 
@@ -291,7 +293,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
 
 // z = Down_e h of 32 rows of an expert for the slots of a job, items and teams as above.  32 rows a warp, because the hidden values of eight slots are four
 // times the weights' bytes that they meet in 16.  (With the tokens' sums kept in the CTA instead, job after job, a job's few blocks waited for
-// barriers: 95 us where this and the sums behind it take 48, 64 tokens of 128 experts.)
+// barriers: 95 us where this and the sums behind it took 64, 64 tokens of 128 experts.)
 template <bool F16, int NG, bool ZEROS>
 __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_down_kernel(const __grid_constant__ MoeArgs g, int split)
 {
