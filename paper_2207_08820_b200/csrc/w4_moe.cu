@@ -171,6 +171,16 @@ __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int
 {
     const int slots = (g.T - t0 < PASS ? g.T - t0 : PASS) * g.top_k;
     const int* experts = g.experts + static_cast<size_t>(t0) * g.top_k;
+    if (slots == g.top_k) {     // one token: its experts are all different, a job each
+        for (int s = threadIdx.x; s < slots; s += threads) {
+            c.expert[s] = static_cast<uint16_t>(experts[s]);
+            c.first[s] = c.slot[s] = static_cast<uint16_t>(s);
+            c.token[s] = 0;
+        }
+        if (threadIdx.x == 0) { c.n = slots; c.first[slots] = static_cast<uint16_t>(slots); }
+        __syncthreads();
+        return;
+    }
     for (int e = threadIdx.x; e < g.E; e += threads) c.tokens[0][e] = c.tokens[1][e] = 0;
     __syncthreads();
     for (int s = threadIdx.x; s < slots; s += threads) {
