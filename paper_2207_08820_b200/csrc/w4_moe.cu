@@ -4,7 +4,7 @@
 //   down    z[slot] = Down_e h[slot]
 //   sum     y[token] = sum over its slots of z[slot]
 // Each block of the chosen experts' weights comes from HBM once for up to 64 tokens (more tokens are further passes), through shared memory, and is multiplied
-// with mma.sync (w4_dot.cuh).  What bounds it: for one token the four launches (12 us with next to no weights; 64 experts of 2048 x 1024, 8 chosen: 26 us, of
+// with mma.sync (w4_dot.cuh).  What bounds it: for one token the four launches (11 us with next to no weights; 64 experts of 2048 x 1024, 8 chosen: 24 us, of
 // which their bytes take 4), with more the expansion of the codes (64 tokens, 128 experts of 2048 x 768: 121 us at 2.5 TB/s; 8 tokens, 2 of 16
 // experts of 4096 x 8192: 134 to 180 us at 4.1 to 3.0 TB/s, as the choices fall).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits
 // of mantissa), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
@@ -26,6 +26,7 @@ struct MoeArgs {
     const unsigned char *gate, *up, *down;
     W4Layout lu, ld;                        // of one expert's gate or up, and down
     CUtensorMap tg, tu, td;                 // their blocks, in boxes of a CTA's teams
+    int down_split, down_ctas;              // of the second product: warps of a team, CTAs
     void* xa;                               // aligned copy of x, or null where x is
     long long ldxa;
     __nv_bfloat16 *hi, *lo;                 // [T top_k][ldh]
@@ -171,7 +172,7 @@ __device__ __forceinline__ void find_jobs(const MoeArgs& g, Jobs& c, int t0, int
 {
     const int slots = (g.T - t0 < PASS ? g.T - t0 : PASS) * g.top_k;
     const int* experts = g.experts + static_cast<size_t>(t0) * g.top_k;
-    if (slots == g.top_k) {     // one token: its experts are all different, a job each
+    if (slots == g.top_k) {     // one token: its experts are all different, a job each; a search of 1.2 us less in either product
         for (int s = threadIdx.x; s < slots; s += threads) {
             c.expert[s] = static_cast<uint16_t>(experts[s]);
             c.first[s] = c.slot[s] = static_cast<uint16_t>(s);
@@ -248,6 +249,16 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, 2) w4_moe_gate_kernel(const _
             for (int item = blockIdx.x; item < items; item += gridDim.x) {
                 const int job = item / per_job, rb0 = (item - job * per_job) * teams;
                 for (int c = 0; c < l.cbs; c += split, ++filled) ring.fill(maps, {rb0, rb0}, c, jobs.expert[job], g.status);
+            }
+            // what the second product's CTA of this place takes first starts for L2 (one token, 2 of 16 experts of 4096 x 4096: 31.4 in place of 32.2 us)
+            const int high = WARPS / g.down_split, per_down = (g.ld.rbs + 2 * high - 1) / (2 * high);
+            int left = DOWN_STAGES;
+            for (int item = blockIdx.x; item < jobs.n * per_down && left > 0; item += g.down_ctas) {
+                const int job = item / per_down, rb0 = (item - job * per_down) * 2 * high;
+                for (int c = 0; c < g.ld.cbs && left > 0; c += g.down_split, --left) {
+                    Ring::hint(&g.td, rb0, c, jobs.expert[job]);
+                    Ring::hint(&g.td, rb0 + high, c, jobs.expert[job]);
+                }
             }
             ring.drain(filled, g.status);
         }
@@ -441,15 +452,12 @@ int launch_gate(MoeArgs& g, int sms, cudaStream_t st)
                             dim3(WARPS * 32 + 32), smem, st, g, split);
 }
 template <bool F16, int NG, bool ZEROS>
-int launch_down(MoeArgs& g, int sms, cudaStream_t st)
+int launch_down(MoeArgs& g, cudaStream_t st)
 {
-    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
-    const int split = w4_team_width(WARPS, g.ld.cbs);
-    const long long items = static_cast<long long>(jobs) * ceil_div(g.ld.rbs, 2 * WARPS / split);
     constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, DOWN_STAGES>::BYTES;
-    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS>, smem) || !w4_encode_blocks(&g.td, g.down, g.ld, g.E, split, WARPS / split)) return BS_ERR_CUDA;
-    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS>, dim3(static_cast<unsigned>(items < 2 * sms ? items : 2 * sms), ceil_div(g.T, PASS)),
-                            dim3(WARPS * 32 + 32), smem, st, g, split);
+    if (!allow_smem(w4_moe_down_kernel<F16, NG, ZEROS>, smem)) return BS_ERR_CUDA;
+    return launch_dependent(w4_moe_down_kernel<F16, NG, ZEROS>, dim3(static_cast<unsigned>(g.down_ctas), ceil_div(g.T, PASS)), dim3(WARPS * 32 + 32), smem, st, g,
+                            g.down_split);
 }
 template <bool F16>
 int launch_experts(MoeArgs& g, int sms, cudaStream_t st)
@@ -459,14 +467,19 @@ int launch_experts(MoeArgs& g, int sms, cudaStream_t st)
     if (g.lu.zeros) rc = nu == 4 ? launch_gate<F16, 4, true>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, true>(g, sms, st) : launch_gate<F16, 1, true>(g, sms, st);
     else rc = nu == 4 ? launch_gate<F16, 4, false>(g, sms, st) : nu == 2 ? launch_gate<F16, 2, false>(g, sms, st) : launch_gate<F16, 1, false>(g, sms, st);
     if (rc != BS_OK) return rc;
-    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true>(g, sms, st) : nd == 2 ? launch_down<F16, 2, true>(g, sms, st) : launch_down<F16, 1, true>(g, sms, st);
-    return nd == 4 ? launch_down<F16, 4, false>(g, sms, st) : nd == 2 ? launch_down<F16, 2, false>(g, sms, st) : launch_down<F16, 1, false>(g, sms, st);
+    if (g.ld.zeros) return nd == 4 ? launch_down<F16, 4, true>(g, st) : nd == 2 ? launch_down<F16, 2, true>(g, st) : launch_down<F16, 1, true>(g, st);
+    return nd == 4 ? launch_down<F16, 4, false>(g, st) : nd == 2 ? launch_down<F16, 2, false>(g, st) : launch_down<F16, 1, false>(g, st);
 }
 template <bool F16>
 int launch_moe(MoeArgs& g, int sms, cudaStream_t st)
 {
     int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
     if (rc != BS_OK) return rc;
+    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
+    g.down_split = w4_team_width(WARPS, g.ld.cbs);
+    const long long items = static_cast<long long>(jobs) * ceil_div(g.ld.rbs, 2 * WARPS / g.down_split);
+    g.down_ctas = static_cast<int>(items < 2 * sms ? items : 2 * sms);
+    if (!w4_encode_blocks(&g.td, g.down, g.ld, g.E, g.down_split, WARPS / g.down_split)) return BS_ERR_CUDA;
     rc = launch_experts<F16>(g, sms, st);
     if (rc != BS_OK) return rc;
     const long long want = (static_cast<long long>(g.T) * (g.ldz / 4) + 255) / 256, most = 8ll * sms;
