@@ -100,11 +100,13 @@ __device__ __forceinline__ GroupCodes<F32> group_step(float lo, float hi, S& sca
     return g;
 }
 
-// Groups of 32, 64, 128 or 256 columns of rows that allow wide loads: a thread keeps V columns in registers, group / V neighbouring threads share the extremes
-// by shuffles, one pass over the weights.  2^log_row threads take a row, the others of the CTA the next ones.  Bound by HBM, then by the instructions of
-// the codes: 24576 x 8192 from bfloat16 129 us (4.7 TB/s), with zero points 146 (4.2), from float32 169 (6.0).  V: 16 columns where K allows, 8 otherwise
-// (8184 columns: 215 us with zero points, of which the narrower loads and stores are the cause).
-template <typename T, typename S, bool ZEROS, int V>
+// Groups of 32, 64, 128 or 256 columns: a thread keeps V columns in registers, group / V neighbouring threads share the extremes by shuffles, one pass over the
+// weights.  2^log_row threads take a row, the others of the CTA the next ones.  Bound by HBM, then by the instructions of the codes: 24576 x 8192 from
+// bfloat16 129 us (4.7 TB/s), with zero points 146 (4.2), from float32 169 (6.0).  WIDE: rows allow 16-byte loads, a thread's columns are neighbours, 16 of
+// them where K allows, 8 otherwise (8184 columns: 215 us with zero points, of which the narrower loads and stores are the cause).  Otherwise the threads of a
+// group take its columns in turn, so that a load or store of single values meets few sectors: 8191 columns 283 us with groups of 128 (neighbours: 483; a
+// warp a group: 499) and 298 with groups of 32 (8 columns a thread: four threads a group; 506 with 16).
+template <typename T, typename S, bool ZEROS, int V, bool WIDE>
 __global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long ld, int O, int K, int log_group, int log_row, int8_t* codes, S* scales, int8_t* zeros)
 {
     w = dependent_begin(w);
@@ -114,13 +116,20 @@ __global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long 
     for (int first = blockIdx.x * rows; first < O; first += step) {
         const int o = first + (threadIdx.x >> log_row);
         for (int u0 = 0; u0 < units; u0 += 1 << log_row) {
-            const int u = u0 + t, c0 = u * V;
-            const bool live = o < O && c0 < K;      // K is a multiple of V here
+            // a thread's first column, and how far apart its columns are
+            const int u = u0 + t, c0 = WIDE ? u * V : (u / lanes << log_group) + (u & (lanes - 1)), apart = WIDE ? 1 : lanes;
+            const bool live = o < O && c0 < K;      // WIDE: K is a multiple of V
             uint4 raw[sizeof(T) * V / 16];
-            const T* v = reinterpret_cast<const T*>(raw);
-            const uint4* src = reinterpret_cast<const uint4*>(w + o * ld + c0);
+            T* v = reinterpret_cast<T*>(raw);
+            const T* from = w + o * ld + c0;
+            if constexpr (WIDE) {
 #pragma unroll
-            for (int e = 0; e < static_cast<int>(sizeof(T)) * V / 16; ++e) raw[e] = live ? __ldcs(src + e) : make_uint4(0, 0, 0, 0);
+                for (int e = 0; e < static_cast<int>(sizeof(T)) * V / 16; ++e) raw[e] = live ? __ldcs(reinterpret_cast<const uint4*>(from) + e) : make_uint4(0, 0, 0, 0);
+            } else {
+                const int left = live ? K - c0 : 0;
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] = e * apart < left ? from[e * apart] : T(0.f);
+            }
             float lo, hi;
             extremes<V>(v, lo, hi);
             for (int d = 1; d < lanes; d <<= 1) {
@@ -147,7 +156,11 @@ __global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long 
                 out[e / 4] = ZEROS ? __vadd4(__byte_perm(__byte_perm(c[e], c[e + 1], 0x0040), __byte_perm(c[e + 2], c[e + 3], 0x0040), 0x5410), z * 0x01010101u)
                                    : __byte_perm(__byte_perm(c[e], c[e + 1], 0x0040), __byte_perm(c[e + 2], c[e + 3], 0x0040), 0x5410);
             int8_t* to = codes + static_cast<long long>(o) * K + c0;
-            if (V == 16) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[V / 4 - 2], out[V / 4 - 1]);
+            if constexpr (!WIDE) {
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    if (e * apart < K - c0) to[e * apart] = static_cast<int8_t>(out[e / 4] >> (8 * (e & 3)));
+            } else if (V == 16) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[V / 4 - 2], out[V / 4 - 1]);
             else *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
             if ((u & (lanes - 1)) == 0) {
                 const long long at = static_cast<long long>(o) * G + u / lanes;
@@ -158,8 +171,8 @@ __global__ void __launch_bounds__(256) w4_quantise_kernel(const T* w, long long 
     }
 }
 
-// Any group and any row: a warp a group, which it reads twice, from L2 or L1 the second time.  24576 x 8191 from bfloat16 with zero points 499 us, 3.4 times the
-// other kernel's time: loads and stores of single values bound it.
+// Any other group, and any row: a warp a group, which it reads twice, from L2 or L1 the second time.  24576 x 8192 from bfloat16 with zero points, groups of
+// 384: 321 us; loads and stores of single values bound it.
 template <typename T, typename S, bool ZEROS>
 __global__ void __launch_bounds__(256) w4_quantise_rows_kernel(const T* w, long long ld, int O, int K, int group, int8_t* codes, S* scales, int8_t* zeros)
 {
@@ -252,24 +265,25 @@ int quantise(const void* w, long long ld, int O, int K, int group, int8_t* codes
     S* sc = static_cast<S*>(scales);
     const int sms = device_sm_count();
     if (sms <= 0) return BS_ERR_CUDA;
-    const bool wide = group <= 256 && (group & (group - 1)) == 0 && (K & 7) == 0 && (ld * static_cast<long long>(sizeof(T))) % 16 == 0;
+    const bool wide = (K & 7) == 0 && (ld * static_cast<long long>(sizeof(T))) % 16 == 0;
     const long long most = static_cast<long long>(sms) * 32;
-    if (!wide) {
+    if (group > 256 || (group & (group - 1)) != 0) {
         const long long want = (static_cast<long long>(O) * ceil_div(K, group) + 7) / 8;
         const dim3 grid(static_cast<unsigned>(want < most ? want : most));
         return zeros ? launch_dependent(w4_quantise_rows_kernel<T, S, true>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros)
                      : launch_dependent(w4_quantise_rows_kernel<T, S, false>, grid, dim3(256), 0, st, wt, ld, O, K, group, codes, sc, zeros);
     }
-    const int V = K % 16 == 0 ? 16 : 8, units = ceil_div(K, group) * (group / V);
+    const int V = (wide ? K % 16 == 0 : group >= 128) ? 16 : 8, units = ceil_div(K, group) * (group / V);
     int log_group = 5, log_row = 5;
     while (1 << log_group < group) ++log_group;
     while (1 << log_row < units && log_row < 8) ++log_row;
     const int want = ceil_div(O, 256 >> log_row);
     const dim3 grid(static_cast<unsigned>(want < most ? want : most));
-    if (V == 16) return zeros ? launch_dependent(w4_quantise_kernel<T, S, true, 16>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros)
-                              : launch_dependent(w4_quantise_kernel<T, S, false, 16>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros);
-    return zeros ? launch_dependent(w4_quantise_kernel<T, S, true, 8>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros)
-                 : launch_dependent(w4_quantise_kernel<T, S, false, 8>, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros);
+    auto go = [&](auto kernel) { return launch_dependent(kernel, grid, dim3(256), 0, st, wt, ld, O, K, log_group, log_row, codes, sc, zeros); };
+    if (!wide && V == 16) return zeros ? go(w4_quantise_kernel<T, S, true, 16, false>) : go(w4_quantise_kernel<T, S, false, 16, false>);
+    if (!wide) return zeros ? go(w4_quantise_kernel<T, S, true, 8, false>) : go(w4_quantise_kernel<T, S, false, 8, false>);
+    if (V == 16) return zeros ? go(w4_quantise_kernel<T, S, true, 16, true>) : go(w4_quantise_kernel<T, S, false, 16, true>);
+    return zeros ? go(w4_quantise_kernel<T, S, true, 8, true>) : go(w4_quantise_kernel<T, S, false, 8, true>);
 }
 
 }  // namespace

@@ -462,3 +462,17 @@ def test_outputs_that_are_inputs_are_refused():
     for out in (x, router[1:], e.data[:128].view(BF16).view(1, 64), d.data[:128].view(BF16).view(1, 64)):
         with pytest.raises(ValueError):
             api.moe_w4(x, router, e, e, d, 1, out=out)
+
+
+@pytest.mark.parametrize("source", [F32, BF16, F16], ids=str)
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("O,K,pitch,group", [(33, 513, 513, 128), (6, 1001, 1001, 256), (70, 259, 259, 32), (300, 31, 31, 64), (19, 264, 267, 128), (5, 384, 385, 32), (2, 129, 129, 128)])
+def test_quantise_rows_off_wide_loads(source, zeros, O, K, pitch, group):
+    """Rows of an odd number of columns or an odd distance apart; what lies between them is not read."""
+    rng = np.random.default_rng(O + K)
+    room = torch.full((O, pitch), float("inf"), dtype=source)
+    room[:, :K] = normal(rng, (O, K), source) * 0.05
+    codes, scales, z = api.quantise_w4(room.cuda()[:, :K], group, zeros=zeros, dtype=BF16)
+    c, s, p = ref.quantise(room[:, :K], group, zeros, BF16)
+    assert np.array_equal(scales.double().cpu().numpy(), s) and np.array_equal(codes.cpu().numpy(), c)
+    assert not zeros or np.array_equal(z.cpu().numpy(), p)
