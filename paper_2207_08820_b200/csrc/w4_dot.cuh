@@ -97,9 +97,10 @@ struct W4Tile {
     uint32_t scale[NG], zero[NG];
 };
 
-// Blocks on their way through the shared memory of a CTA: a stage holds, for each of NB matrices, WARPS blocks, one a warp.  The `split` warps of a team share the reduction of 16 rows, WARPS /
-// split teams take neighbouring rows.  One thread fills stages ahead of the warps that read them, with one tensor copy of all teams' blocks: copies of
-// 8 KB reach 5.7 TB/s, where a hundred of 1 KB in flight on every SM reach 3 (measured, 104 MB), and a copy takes its thread 130 cycles to start.  (Loads into registers a few blocks ahead wait for one another: the waits of a warp are counted in six places only.)
+// Blocks on their way through the shared memory of a CTA: a stage holds, for each of NB matrices, WARPS blocks, one a warp.  The `split` warps of a team share
+// the reduction of 16 rows, WARPS / split teams take neighbouring rows.  One thread fills stages ahead of the warps that read them, with one tensor copy of
+// all teams' blocks: copies of 8 KB reach 5.7 TB/s, where a hundred of 1 KB in flight on every SM reach 3 (measured, 104 MB), and a copy takes its
+// thread 130 cycles to start.  (Loads into registers a few blocks ahead wait for one another: the waits of a warp are counted in six places only.)
 template <int NG, bool ZEROS, int NB, int WARPS, int STAGES>
 struct W4TeamRing {
     static constexpr int ENTRY = ZEROS ? 8 : 4, BLOCK = W4_CODES + NG * 8 * ENTRY, BYTES = STAGES * NB * WARPS * BLOCK;
@@ -209,8 +210,8 @@ struct W4TeamRing {
     }
 };
 
-// tot[r][n] += 1 / PART (of X16's type) of RT blocks of different rows times n tiles of eight rows of x: x(n, j, term) are the lane's eight columns of word j, of which there are TERMS
-// to be added up.  x is of the type that X16 says, the scales of S16's.
+// tot[r][n] += 1 / PART (of X16's type) of RT blocks of different rows times n tiles of eight rows of x: x(n, j, term) are the lane's eight columns of word j,
+// of which there are TERMS to be added up.  x is of the type that X16 says, the scales of S16's.  What adds the warps' parts up multiplies by PART.
 template <bool X16, bool S16, int TERMS, int RT, int NT, int NG, bool ZEROS, typename X>
 __device__ __forceinline__ void w4_blocks(const W4Tile<NG, ZEROS> (&w)[RT], const X& x, float (&tot)[RT][NT][4])
 {

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(WARPS * 32 + 32, ctas_of<NT>()) w4_gemm_kernel
 }
 
 // Rows of x that do not start on 16-byte boundaries, brought to ones that do, zeros behind K: the products' loads and tensor copies are of 16 bytes.  One more
-// launch, 2.9 us with 33 rows of 4611 columns (1383 outputs: 10.5 in place of 7.6 us), bound by its latency.
+// launch, 2.9 us with 33 rows of 4611 columns (1383 outputs: 10.5 in place of 7.6 us), bound by its latency and by the host; 1.7 us in a graph (8 rows of 4097).
 __global__ void __launch_bounds__(256) w4_align_rows_kernel(const uint16_t* x, long long ldx, int M, int K, uint16_t* out, int ldo)
 {
     x = dependent_begin(x);
