@@ -56,8 +56,14 @@ __device__ __forceinline__ unsigned long long order_key(double v)
     return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-// Logits of eight tokens by a cluster: a CTA takes tiles of 16 experts, its warps split the reduction, each MMA's sum of 16 products is added in 64 bits
-// (32 bits would decide the order of experts that are nearly equal by the order of the sums).  CTA r then ranks token r.
+// An MMA's sum of 16 products is at most this far off, of their magnitudes' sum: it holds 24 bits of the largest one's place, so that 15 products lose less than
+// 2^-23 of it each and the sum as much again; a sixteenth more for the sum of the magnitudes, which is in 32 bits itself.
+constexpr float SUM_CUT = 1.0625f / (1 << 19);
+
+// Logits of eight tokens by a cluster: a CTA takes tiles of 16 experts, its warps split the reduction, each MMA's sum of 16 products is added in 64 bits, and
+// the products' magnitudes by MMAs beside them.  CTA r then ranks token r.  What an MMA cuts off can exceed what two logits differ by: experts that may change
+// places with a chosen one get their products summed in 64 bits, one by one, and are ranked again (a token in a hundred with 128 experts of normal
+// weights; 1 us).
 template <bool F16>
 __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __grid_constant__ MoeArgs g)
 {
@@ -65,7 +71,9 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     typedef typename Ty::T T;
     __shared__ double part[ROUTE_WARPS][16][8];
     __shared__ double logits[MAX_EXPERTS];
+    __shared__ float sizes[ROUTE_WARPS][16][8], cut[MAX_EXPERTS];       // cut: how far a logit may be off
     __shared__ unsigned long long keys[MAX_EXPERTS];
+    __shared__ unsigned char open[MAX_EXPERTS];
     __shared__ int choice[MAX_TOP];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x, m0 = blockIdx.y * 8;
     const int tiles = (g.E + 15) / 16, steps = (g.H + 31) / 32;
@@ -83,6 +91,7 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     for (int tile = rank; tile < tiles; tile += ROUTE_CTAS) {
         const int e0 = tile * 16 + (lane >> 2), e1 = e0 + 8;
         double sum[4] = {0, 0, 0, 0};
+        float size[4] = {0, 0, 0, 0};
 #pragma unroll 4
         for (int s = warp; s < steps; s += ROUTE_WARPS) {
             const int k0 = s * 32 + 8 * (lane & 3);
@@ -95,22 +104,34 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
             Ty::mma(d, a.z, b.z, a.w, b.w, v.z, v.w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] += static_cast<double>(c[i]) + static_cast<double>(d[i]);
+            const uint32_t m = 0x7fff7fffu;
+            Ty::mma(size, a.x & m, b.x & m, a.y & m, b.y & m, v.x & m, v.y & m);
+            Ty::mma(size, a.z & m, b.z & m, a.w & m, b.w & m, v.z & m, v.w & m);
         }
         const int r = lane >> 2, n = 2 * (lane & 3);
         part[warp][r][n] = sum[0];
         part[warp][r][n + 1] = sum[1];
         part[warp][r + 8][n] = sum[2];
         part[warp][r + 8][n + 1] = sum[3];
+        sizes[warp][r][n] = size[0];
+        sizes[warp][r][n + 1] = size[1];
+        sizes[warp][r + 8][n] = size[2];
+        sizes[warp][r + 8][n + 1] = size[3];
         __syncthreads();
         if (threadIdx.x < 128) {
             const int e = threadIdx.x >> 3, m = threadIdx.x & 7;
             double v = 0;
+            float far = 0;
 #pragma unroll
-            for (int k = 0; k < ROUTE_WARPS; ++k) v += part[k][e][m];
+            for (int k = 0; k < ROUTE_WARPS; ++k) {
+                v += part[k][e][m];
+                far += sizes[k][e][m];
+            }
             if (tile * 16 + e < g.E) {      // to the CTA that ranks this token
-                uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(&logits[tile * 16 + e]));
-                asm volatile("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(to) : "r"(m));
+                uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(&logits[tile * 16 + e])), at = static_cast<uint32_t>(__cvta_generic_to_shared(&cut[tile * 16 + e]));
+                asm volatile("mapa.shared::cluster.u32 %0, %0, %2;\n\tmapa.shared::cluster.u32 %1, %1, %2;" : "+r"(to), "+r"(at) : "r"(m));
                 asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(v) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(far * SUM_CUT) : "memory");
             }
         }
         __syncthreads();
@@ -124,19 +145,52 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     const int m = m0 + rank;
     if (m >= g.T) return;
     // an expert's place is the number of experts before it: larger logits, and equal ones of lower index.  `share` neighbouring threads count for one.
-    for (int e = threadIdx.x; e < g.E; e += ROUTE_WARPS * 32) keys[e] = order_key(logits[e]);
-    __syncthreads();
     int share = 32;
     while (share > 1 && share * g.E > ROUTE_WARPS * 32) share /= 2;
-    const int e = threadIdx.x / share;
-    int place = 0;
-    if (e < g.E) {
-        const unsigned long long key = keys[e];
-        for (int k = threadIdx.x % share; k < g.E; k += share) place += keys[k] > key || (keys[k] == key && k < e);
+    const int e = threadIdx.x / share, turn = threadIdx.x % share;
+    auto rank_all = [&] {
+        for (int i = threadIdx.x; i < g.E; i += ROUTE_WARPS * 32) {
+            keys[i] = order_key(logits[i]);
+            open[i] = 0;
+        }
+        __syncthreads();
+        int place = 0;
+        if (e < g.E) {
+            const unsigned long long key = keys[e];
+            for (int k = turn; k < g.E; k += share) place += keys[k] > key || (keys[k] == key && k < e);
+        }
+        for (int d = 1; d < share; d <<= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
+        if (e < g.E && turn == 0 && place < g.top_k) choice[place] = e;
+        __syncthreads();
+    };
+    rank_all();
+    bool near = false;
+    if (e < g.E)
+        for (int c = turn; c < g.top_k; c += share) {
+            const int k = choice[c];
+            const double far = static_cast<double>(cut[e]) + cut[k];        // 0: a token of zeros, whose sums are exact
+            if (k != e && far > 0 && fabs(logits[e] - logits[k]) <= far) near = open[e] = open[k] = 1;
+        }
+    if (__syncthreads_or(near)) {
+        // what is not open keeps its order with all that is: it is farther from every chosen expert than both sums may be off
+        for (int i = warp; i < g.E; i += ROUTE_WARPS) {
+            if (!open[i]) continue;
+            double s = 0;
+            for (int k0 = lane * 8; k0 < g.H; k0 += 256) {
+                const uint4 v = load8(x + m * g.ldx, k0, g.H, g.x_aligned), w = load8(router + static_cast<size_t>(i) * g.H, k0, g.H, g.router_aligned);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s = fma(static_cast<double>(Ty::lo(word_of(v, j))), static_cast<double>(Ty::lo(word_of(w, j))), s);
+                    s = fma(static_cast<double>(Ty::hi(word_of(v, j))), static_cast<double>(Ty::hi(word_of(w, j))), s);
+                }
+            }
+#pragma unroll
+            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+            if (lane == 0) logits[i] = s;
+        }
+        __syncthreads();
+        rank_all();
     }
-    for (int d = 1; d < share; d <<= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
-    if (e < g.E && threadIdx.x % share == 0 && place < g.top_k) choice[place] = e;
-    __syncthreads();
     if (warp != 0) return;
     const int expert = lane < g.top_k ? choice[lane] : 0;
     const double most = logits[choice[0]];

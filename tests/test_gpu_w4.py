@@ -476,3 +476,65 @@ def test_quantise_rows_off_wide_loads(source, zeros, O, K, pitch, group):
     c, s, p = ref.quantise(room[:, :K], group, zeros, BF16)
     assert np.array_equal(scales.double().cpu().numpy(), s) and np.array_equal(codes.cpu().numpy(), c)
     assert not zeros or np.array_equal(z.cpu().numpy(), p)
+
+
+def route(x, router, top_k, renormalise=True):
+    """The choices and weights of a layer whose experts do not matter."""
+    rng = np.random.default_rng(0)
+    E, H = router.shape
+    w = prepared(weights(rng, 16, H, 128, x.dtype, False, (E,)), 128)
+    d = prepared(weights(rng, H, 16, 128, x.dtype, False, (E,)), 128)
+    _, e, s = api.moe_w4(x.cuda(), router.cuda(), w, w, d, top_k, renormalise=renormalise)
+    return e.cpu().long(), s.cpu().double()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("T,E,top_k,H", [(1, 2, 1, 64), (64, 16, 5, 64), (9, 40, 8, 71), (33, 128, 8, 264), (7, 512, 32, 64), (3, 200, 1, 1024)])
+def test_moe_ties_between_different_sums(dtype, T, E, top_k, H):
+    """Experts in pairs whose products are the same numbers in other columns, so that their logits are equal and 32-bit sums of them are not: the lower index
+    first.  Every sum is exact in 64 bits: products are multiples of 2^-24 below 2^12, and there are fewer than 2^12 of them."""
+    rng = np.random.default_rng(T + E)
+    half = H // 2
+
+    def wide(*shape):       # numbers of 8 bits, 2^-12 to 2^6
+        return rng.integers(-128, 129, shape) * 2.0 ** rng.integers(-12, -1, shape)
+    x = wide(T, H)
+    x[:, half:2 * half] = x[:, :half]
+    router = wide(E, H)
+    swap = rng.random(half) < 0.5
+    for e in range(1, E, 2):
+        router[e] = router[e - 1]
+        router[e, :half][swap], router[e, half:2 * half][swap] = router[e - 1, half:2 * half][swap], router[e - 1, :half][swap]
+    x, router = torch.from_numpy(x).to(dtype), torch.from_numpy(router).to(dtype)
+    logits = x.double() @ router.double().T
+    assert E < 2 or torch.equal(logits[:, 0:E - 1:2], logits[:, 1::2])
+    want = torch.sort(-logits, dim=-1, stable=True).indices[:, :top_k]
+    got, _ = route(x, router, top_k)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("renormalise", [True, False])
+def test_moe_logits_smaller_than_what_cancels(dtype, renormalise):
+    """Products of 2^30 that cancel beside ones of 2^-2 and 2^-3, in one MMA's 16 products and in different ones: logits of 0.25, 0.125 and others near them."""
+    E, H, T = 7, 128, 5
+    x = torch.zeros(T, H, dtype=dtype)
+    x[:, [0, 1, 2, 16, 32, 64, 100]] = 1
+    x[:, 0] = x[:, 1] = x[:, 64] = 2.0 ** 15
+    router = torch.zeros(E, H, dtype=dtype)
+    router[0, 2] = 0.125
+    router[1, [0, 1]] = torch.tensor([2.0 ** 15, -2.0 ** 15], dtype=dtype)
+    router[1, 2] = 0.25
+    router[2, [0, 64]] = torch.tensor([2.0 ** 15, -2.0 ** 15], dtype=dtype)
+    router[2, 2] = 0.1875
+    router[3, [1, 64]] = torch.tensor([-2.0 ** 15, 2.0 ** 15], dtype=dtype)
+    router[3, [16, 100]] = 0.125
+    router[4:, 2] = -1
+    logits = x.double() @ router.double().T
+    assert logits[0].tolist() == [0.125, 0.25, 0.1875, 0.25, -1, -1, -1]
+    got, share = route(x, router, 4, renormalise)
+    assert got.tolist() == [[1, 3, 2, 0]] * T
+    p = torch.exp(logits)
+    want = p.gather(1, got) / (p.gather(1, got) if renormalise else p).sum(1, keepdim=True)
+    # expf of a difference rounded to 32 bits, its sum and the quotient: a few steps of a float
+    assert ((share - want).abs() <= want * 2.0 ** -19).all()
