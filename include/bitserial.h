@@ -474,6 +474,7 @@ int bs_w4_gemm(const void* x, long long ldx, int M, const void* w, int O, int K,
  * bs_w4_moe -- a mixture-of-experts layer for a few tokens (any number is taken, 64 at a time: each further 64 read the experts' weights again).
  *       logits[t][e] = sum_h x[t][h] * router[e][h];   the top_k experts of a token by their logits, ties to the lowest index
  *       weight       = softmax of the logits over all experts; with `renormalise` over the chosen ones
+ *       (which experts, and in which order, is decided by sums in 64 bits; the logits behind the weights may be off by 2^-19 of the sum of |x router|)
  *       y[t]         = sum over the choices of weight * Down_e (silu(Gate_e x[t]) * (Up_e x[t]))
  *   x        device, [T] rows of H values of `type`, `ldx` values apart;  router  device [E][H] of `type`;  y  device [T][H]
  *   gate, up prepared, E matrices of I rows and H columns each, group_up, zeros_up;  down  E matrices of H rows and I columns, group_down, zeros_down

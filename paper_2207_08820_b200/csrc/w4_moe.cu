@@ -60,10 +60,51 @@ __device__ __forceinline__ unsigned long long order_key(double v)
 // 2^-23 of it each and the sum as much again; a sixteenth more for the sum of the magnitudes, which is in 32 bits itself.
 constexpr float SUM_CUT = 1.0625f / (1 << 19);
 
+// The logits of the experts that `open` names, from products that are exact in 64 bits and summed there: warps share the columns, `parts` [OPEN][ROUTE_WARPS] holds
+// their sums.  All threads.  Not inlined: few tokens need it, and its instructions would be in the others' way.
+constexpr int OPEN = 128;       // experts at a time
+template <bool F16>
+__device__ __noinline__ void exact_logits(const MoeArgs& g, const typename W4Type<F16>::T* x, const typename W4Type<F16>::T* router, const unsigned char* open, double* parts, double* logits)
+{
+    typedef W4Type<F16> Ty;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int first = 0; first < g.E; first += OPEN) {
+        for (int at = 0; at < OPEN; at += 32) {
+            const int e = first + at + lane;
+            for (unsigned left = __ballot_sync(0xffffffffu, e < g.E && open[e]); left; left &= left - 1) {
+                const int i = at + __ffs(left) - 1;
+                const auto* row = router + static_cast<size_t>(first + i) * g.H;
+                double s[2] = {0, 0};
+                for (int k0 = threadIdx.x * 8; k0 < g.H; k0 += ROUTE_WARPS * 32 * 8) {
+                    const uint4 v = load8(x, k0, g.H, g.x_aligned), w = load8(row, k0, g.H, g.router_aligned);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s[0] = fma(static_cast<double>(Ty::lo(word_of(v, j))), static_cast<double>(Ty::lo(word_of(w, j))), s[0]);
+                        s[1] = fma(static_cast<double>(Ty::hi(word_of(v, j))), static_cast<double>(Ty::hi(word_of(w, j))), s[1]);
+                    }
+                }
+                s[0] += s[1];
+#pragma unroll
+                for (int d = 16; d; d >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], d);
+                if (lane == 0) parts[i * ROUTE_WARPS + warp] = s[0];
+            }
+        }
+        __syncthreads();
+        const int i = threadIdx.x;
+        if (i < OPEN && first + i < g.E && open[first + i]) {
+            double s = 0;
+            for (int k = 0; k < ROUTE_WARPS; ++k) s += parts[i * ROUTE_WARPS + k];
+            logits[first + i] = s;
+        }
+        __syncthreads();
+    }
+}
+
 // Logits of eight tokens by a cluster: a CTA takes tiles of 16 experts, its warps split the reduction, each MMA's sum of 16 products is added in 64 bits, and
 // the products' magnitudes by MMAs beside them.  CTA r then ranks token r.  What an MMA cuts off can exceed what two logits differ by: experts that may change
-// places with a chosen one get their products summed in 64 bits, one by one, and are ranked again (a token in a hundred with 128 experts of normal
-// weights; 1 us).
+// places with a chosen one get their products summed in 64 bits, one by one, and are ranked again (one token in a hundred, 8 of 128 experts of normal weights
+// and 2048 columns).  The check takes 0.6 us (1 token, 8 of 64 experts of 2048 x 1024: 24.6 in place of 24.1), and with it 64 tokens of 128 experts of 2048 x 768 take
+// 121 in place of 119, as nearly every other call has such a token.
 template <bool F16>
 __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __grid_constant__ MoeArgs g)
 {
@@ -148,7 +189,7 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
     int share = 32;
     while (share > 1 && share * g.E > ROUTE_WARPS * 32) share /= 2;
     const int e = threadIdx.x / share, turn = threadIdx.x % share;
-    auto rank_all = [&] {
+    for (bool again = false;; again = true) {
         for (int i = threadIdx.x; i < g.E; i += ROUTE_WARPS * 32) {
             keys[i] = order_key(logits[i]);
             open[i] = 0;
@@ -162,34 +203,21 @@ __global__ void __launch_bounds__(ROUTE_WARPS * 32) w4_moe_route_kernel(const __
         for (int d = 1; d < share; d <<= 1) place += __shfl_xor_sync(0xffffffffu, place, d);
         if (e < g.E && turn == 0 && place < g.top_k) choice[place] = e;
         __syncthreads();
-    };
-    rank_all();
-    bool near = false;
-    if (e < g.E)
-        for (int c = turn; c < g.top_k; c += share) {
-            const int k = choice[c];
-            const double far = static_cast<double>(cut[e]) + cut[k];        // 0: a token of zeros, whose sums are exact
-            if (k != e && far > 0 && fabs(logits[e] - logits[k]) <= far) near = open[e] = open[k] = 1;
-        }
-    if (__syncthreads_or(near)) {
-        // what is not open keeps its order with all that is: it is farther from every chosen expert than both sums may be off
-        for (int i = warp; i < g.E; i += ROUTE_WARPS) {
-            if (!open[i]) continue;
-            double s = 0;
-            for (int k0 = lane * 8; k0 < g.H; k0 += 256) {
-                const uint4 v = load8(x + m * g.ldx, k0, g.H, g.x_aligned), w = load8(router + static_cast<size_t>(i) * g.H, k0, g.H, g.router_aligned);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    s = fma(static_cast<double>(Ty::lo(word_of(v, j))), static_cast<double>(Ty::lo(word_of(w, j))), s);
-                    s = fma(static_cast<double>(Ty::hi(word_of(v, j))), static_cast<double>(Ty::hi(word_of(w, j))), s);
-                }
+        if (again) break;
+        bool near = false;
+        if (e < g.E) {
+            const double own = logits[e];
+            const float far = cut[e];
+            for (int c = turn; c < g.top_k; c += share) {
+                const int k = choice[c];
+                const float both = far + cut[k];        // 0: a token of zeros, whose sums are exact
+                if (k != e && both > 0 && fabs(own - logits[k]) <= both) near = open[e] = open[k] = 1;
             }
-#pragma unroll
-            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-            if (lane == 0) logits[i] = s;
         }
-        __syncthreads();
-        rank_all();
+        if (!__syncthreads_or(near)) break;
+        // what is not open keeps its order with all that is: it is farther from every chosen expert than both sums may be off
+        static_assert(sizeof(part) == OPEN * ROUTE_WARPS * sizeof(double), "the sums' place");
+        exact_logits<F16>(g, x + m * g.ldx, router, open, &part[0][0][0], logits);
     }
     if (warp != 0) return;
     const int expert = lane < g.top_k ? choice[lane] : 0;
