@@ -353,7 +353,7 @@ def _group(group: Optional[int], K: int) -> int:
 def quantise_w4(w: torch.Tensor, group: Optional[int] = 128, *, zeros: bool = False, dtype: Optional[torch.dtype] = None, stream=None):
     """Float weights [..., O, K] to 4 bits, a scale (and with ``zeros`` a zero point) per ``group`` columns of a row (None: per row): returns (codes int8
     [..., O, K], scales [..., O, G], zero points int8 [..., O, G] or None), with w ~ scales * (codes - zero points).  ``dtype``: of the scales,
-    float16 or bfloat16 (default: w's, bfloat16 where w is float32).  Rounding as stated at ``bs_w4_quantise``."""
+    float16 or bfloat16 (default: w's, bfloat16 where w is float32).  Any number of matrices of up to 2^20 rows.  Rounding as stated at ``bs_w4_quantise``."""
     if dtype is None:
         dtype = w.dtype if w.dtype != torch.float32 else torch.bfloat16
     if w.dim() < 2:

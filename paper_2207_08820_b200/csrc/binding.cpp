@@ -378,19 +378,25 @@ PyObject* w4_quantise(PyObject*, PyObject* const* a, Py_ssize_t n)
         const bs_float_t type = static_cast<bs_float_t>(integer(a[3])), from = float_type(w);
         if (group <= 0 || (type != BS_F16 && type != BS_BF16)) mismatch("a positive group and scales of float16 or bfloat16 expected");
         const OnStream on(w, a[4]);
-        const int K = small(w.size(-1)), O = small(w.numel() / K);
-        const int64_t ld = row_pitch(w, K);
+        const int K = small(w.size(-1));
+        const int64_t ld = row_pitch(w, K), rows = w.numel() / K;
+        // a stack of matrices is one of all their rows, as many of them in a call as it takes (a multiple of 16: parts begin on 16-byte boundaries)
+        const int64_t most = w.size(-2) <= 1 << 20 ? 1 << 20 : small(rows);
         std::vector<int64_t> shape(w.sizes().begin(), w.sizes().end());
         const at::Tensor codes = fresh(shape, at::kChar, w);
         shape.back() = (K + static_cast<int64_t>(group) - 1) / group;
         const at::Tensor scales = fresh(shape, type == BS_F16 ? at::kHalf : at::kBFloat16, w);
         at::Tensor z;
         if (zeros) z = fresh(shape, at::kChar, w);
-        int rc;
+        const char* wp = static_cast<const char*>(w.const_data_ptr());
+        char *cp = static_cast<char*>(codes.data_ptr()), *sp = static_cast<char*>(scales.data_ptr()), *zp = zeros ? static_cast<char*>(z.data_ptr()) : nullptr;
+        const int64_t G = shape.back(), w_size = w.element_size(), s_size = scales.element_size();
+        int rc = BS_OK;
         {
             NoGil free;
-            rc = bs_w4_quantise(w.const_data_ptr(), from, O, K, ld, group, type, static_cast<int8_t*>(codes.data_ptr()), scales.data_ptr(),
-                                zeros ? static_cast<int8_t*>(z.data_ptr()) : nullptr, on.stream);
+            for (int64_t o = 0; o < rows && rc == BS_OK; o += most)
+                rc = bs_w4_quantise(wp + o * ld * w_size, from, static_cast<int>(rows - o < most ? rows - o : most), K, ld, group, type, reinterpret_cast<int8_t*>(cp + o * K),
+                                    sp + o * G * s_size, zp ? reinterpret_cast<int8_t*>(zp + o * G) : nullptr, on.stream);
         }
         return Py_BuildValue("(iNNN)", rc, give(codes), give(scales), give(z));
     });

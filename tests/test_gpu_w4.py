@@ -538,3 +538,24 @@ def test_moe_logits_smaller_than_what_cancels(dtype, renormalise):
     want = p.gather(1, got) / (p.gather(1, got) if renormalise else p).sum(1, keepdim=True)
     # expf of a difference rounded to 32 bits, its sum and the quotient: a few steps of a float
     assert ((share - want).abs() <= want * 2.0 ** -19).all()
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("E,O,K", [(260, 4099, 9), (3, 1 << 19, 8), (2, 1 << 20, 3)])
+def test_quantise_stack_of_many_rows(zeros, E, O, K):
+    """Experts that together have more rows than one matrix may have."""
+    rng = np.random.default_rng(E)
+    w = normal(rng, (E, O, K), BF16)
+    codes, scales, z = api.quantise_w4(w.cuda(), 32, zeros=zeros)
+    c, s, p = ref.quantise(w.view(E * O, K), 32, zeros, BF16)
+    assert codes.shape == w.shape and scales.shape == (E, O, 1)
+    assert np.array_equal(scales.view(E * O, 1).double().cpu().numpy(), s) and np.array_equal(codes.view(E * O, K).cpu().numpy(), c)
+    assert not zeros or np.array_equal(z.view(E * O, 1).cpu().numpy(), p)
+    api.prepare_w4(codes, scales, z, group=32)
+    api.bs_check_status()
+
+
+def test_quantise_matrix_of_too_many_rows():
+    for shape in (((1 << 20) + 1, 2), (1, (1 << 20) + 1, 2)):
+        with pytest.raises(BitserialError):
+            api.quantise_w4(torch.zeros(shape, dtype=BF16, device="cuda"), 32)
