@@ -376,7 +376,7 @@ def prepare_w4(codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.
 
 def gemm_w4(x: torch.Tensor, w: W4Weights, bias: Optional[torch.Tensor] = None, *, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """x [..., K] float16 or bfloat16 times the transpose of weights of 4 bits [O, K], plus ``bias`` [O]: [..., O] of x's type (``bs_w4_gemm``).  One row
-    of x (a token) or many; the rows of a matrix may be apart.  No gradients."""
+    of x (a token) or many; the rows of a matrix may be apart.  No gradients: tensors that require one are refused while gradients are recorded."""
     global launch_count
     if w.matrices != 1:
         raise ValueError("the weights of one matrix expected")
@@ -390,7 +390,8 @@ def gemm_w4(x: torch.Tensor, w: W4Weights, bias: Optional[torch.Tensor] = None, 
 def moe_w4(x: torch.Tensor, router: torch.Tensor, gate: W4Weights, up: W4Weights, down: W4Weights, top_k: int, *, renormalise: bool = True,
            out: Optional[torch.Tensor] = None, stream=None):
     """A mixture-of-experts layer for a few tokens (``bs_w4_moe``): x [..., H], ``router`` [E, H], experts ``gate`` and ``up`` [E, I, H], ``down`` [E, H, I].
-    Returns (y [..., H] of x's type, the chosen experts int32 [..., top_k], best first, and their weights float32 [..., top_k]).  No gradients."""
+    Returns (y [..., H] of x's type, the chosen experts int32 [..., top_k], best first, and their weights float32 [..., top_k]).  No gradients: tensors that
+    require one are refused while gradients are recorded."""
     global launch_count
     E, H = router.shape
     if not (gate[1:] == up[1:] and gate.K == H and down[1:4] == (E, H, gate.O) and gate.matrices == E and gate.dtype == down.dtype):

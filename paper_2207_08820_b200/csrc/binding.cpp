@@ -1,6 +1,7 @@
 // Native argument marshalling of the hot entry points (api.py): tensors in, output allocation, one C ABI call (without the GIL).  The
 // same work through ctypes costs 10-20 us a call, more than a small layer takes on the GPU.  No arithmetic of the method and no decision
 // about it is made here.
+#include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <Python.h>
 #include <c10/cuda/CUDAGuard.h>
@@ -367,6 +368,12 @@ const void* prepared_w4(const at::Tensor& t, const at::Tensor& x, int64_t matric
     return pointer(t);
 }
 
+// The products have no backward pass: a result without a gradient must not stand where one is recorded.
+void no_gradient(const at::Tensor& t)
+{
+    if (t.requires_grad() && at::GradMode::is_enabled()) mismatch("there is no gradient through 4-bit weights: a tensor that requires one is taken under torch.no_grad() only");
+}
+
 // w, group, zeros, type (bs_float_t of the scales), stream
 PyObject* w4_quantise(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -448,6 +455,8 @@ PyObject* w4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n)
         need(n, 10);
         const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
         const int O = integer(a[2]), K = integer(a[3]), group = integer(a[4]), zeros = integer(a[5]), type = integer(a[6]);
+        for (int i : {0, 7, 8})
+            if (a[i] != Py_None) no_gradient(tensor(a[i]));
         if (x.dim() < 1 || x.size(-1) != K) mismatch("the last dimension of x is not the weights' number of columns");
         if (float_type(x) != type) mismatch("x is not of the scales' type");
         const OnStream on(x, a[9]);
@@ -497,6 +506,8 @@ PyObject* w4_moe(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor &x = tensor(a[0]), &router = tensor(a[1]);
         const int I = integer(a[5]), gu = integer(a[6]), zu = integer(a[7]), gd = integer(a[8]), zd = integer(a[9]), type = integer(a[10]), top_k = integer(a[11]),
                   renormalise = PyObject_IsTrue(a[12]);
+        for (int i : {0, 1, 13})
+            if (a[i] != Py_None) no_gradient(tensor(a[i]));
         if (router.dim() != 2 || router.numel() == 0) mismatch("a router [E, H] expected");
         const int E = small(router.size(0)), H = small(router.size(1));
         if (x.dim() < 1 || x.size(-1) != H) mismatch("the last dimension of x is not the router's number of columns");

@@ -93,3 +93,36 @@ def test_binding_refuses_tensors_off_the_device():
         api.gemm_w4(torch.zeros(1, 128, dtype=torch.float16), w)
     with pytest.raises(ValueError):
         api.gemm_w4(torch.zeros(1, 128, dtype=torch.bfloat16), w)
+
+
+def test_binding_refuses_what_requires_a_gradient():
+    """Before the device is looked at: the messages tell the refusals apart."""
+    import torch
+    from paper_2207_08820_b200 import api
+    t = torch.float16
+
+    def weights(E, O, K):
+        return api.W4Weights(torch.zeros(8, dtype=torch.uint8), E, O, K, 128, False, t)
+
+    def tensors(*shapes, grad=None):
+        return [torch.zeros(s, dtype=t, requires_grad=i == grad) for i, s in enumerate(shapes)]
+    shapes = (2, 128), (16,), (2, 16)
+    for grad in range(3):
+        x, bias, out = tensors(*shapes, grad=grad)
+        with pytest.raises(ValueError, match="gradient"):
+            api.gemm_w4(x, weights(1, 16, 128), bias, out=out)
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+            api.gemm_w4(x, weights(1, 16, 128), bias, out=out)
+    x, bias, out = tensors(*shapes)
+    with pytest.raises(ValueError, match="CUDA"):
+        api.gemm_w4(x, weights(1, 16, 128), bias, out=out)
+    with pytest.raises(ValueError, match="gradient"):       # not a leaf
+        api.gemm_w4(tensors((2, 128), grad=0)[0] * 2, weights(1, 16, 128))
+    shapes = (2, 128), (4, 128), (2, 128)
+    experts = weights(4, 16, 128), weights(4, 16, 128), weights(4, 128, 16)
+    for grad in range(3):
+        x, router, out = tensors(*shapes, grad=grad)
+        with pytest.raises(ValueError, match="gradient"):
+            api.moe_w4(x, router, *experts, 2, out=out)
+        with torch.no_grad(), pytest.raises(ValueError, match="CUDA"):
+            api.moe_w4(x, router, *experts, 2, out=out)
