@@ -352,13 +352,16 @@ int64_t row_pitch(const at::Tensor& t, int64_t K)
     return t.size(0) == 1 ? K : t.stride(0);
 }
 int small(int64_t v) { if (v > 0x7fffffff) mismatch("tensor too large"); return static_cast<int>(v); }
+// Whether the rows of two tensors share memory.  Rows as far apart as the others may lie between them; what else reaches into the other's range is taken to overlap.
 bool overlap(const at::Tensor& a, int64_t a_pitch, const at::Tensor& b, int64_t b_pitch)
 {
-    auto end = [](const at::Tensor& t, int64_t pitch) {
-        const int64_t K = t.size(-1), rows = t.numel() / K;
-        return static_cast<const char*>(t.const_data_ptr()) + ((rows - 1) * pitch + K) * t.element_size();
-    };
-    return static_cast<const char*>(a.const_data_ptr()) < end(b, b_pitch) && static_cast<const char*>(b.const_data_ptr()) < end(a, a_pitch);
+    const int64_t a_wide = a.size(-1) * a.element_size(), b_wide = b.size(-1) * b.element_size(), a_step = a_pitch * a.element_size(), b_step = b_pitch * b.element_size();
+    const int64_t from = static_cast<const char*>(b.const_data_ptr()) - static_cast<const char*>(a.const_data_ptr());       // b's first row from a's
+    auto length = [](const at::Tensor& t, int64_t step, int64_t wide) { return (t.numel() / t.size(-1) - 1) * step + wide; };
+    if (from >= length(a, a_step, a_wide) || -from >= length(b, b_step, b_wide)) return false;
+    if (a_step != b_step || a_step <= 0) return true;
+    const int64_t in = (from % a_step + a_step) % a_step;       // where b's rows begin, from the rows of a before them
+    return in < a_wide || in + b_wide > a_step;
 }
 const void* prepared_w4(const at::Tensor& t, const at::Tensor& x, int64_t matrices, int O, int K, int group, int zeros)
 {

@@ -559,3 +559,30 @@ def test_quantise_matrix_of_too_many_rows():
     for shape in (((1 << 20) + 1, 2), (1, (1 << 20) + 1, 2)):
         with pytest.raises(BitserialError):
             api.quantise_w4(torch.zeros(shape, dtype=BF16, device="cuda"), 32)
+
+
+@pytest.mark.parametrize("M,O,K", [(3, 40, 72), (40, 200, 1000), (300, 1000, 4904), (2, 8, 8)])
+@pytest.mark.parametrize("first", ["x", "out"])
+def test_gemm_output_beside_its_input(M, O, K, first):
+    """x and the output are columns of one buffer; a column in common, in the same row or in the next one, is refused."""
+    rng = np.random.default_rng(M)
+    w = weights(rng, O, K, 128, BF16, False)
+    x = normal(rng, (M, K), BF16)
+    want, far = ref.gemm(x, ref.matrix(*w, 128), None, BF16)
+    wp = prepared(w, 128)
+    pitch = K + O + 8
+    room = torch.full((M, pitch), GUARD, dtype=BF16, device="cuda")
+    x0, o0 = (0, K) if first == "x" else (O + 8, 0)
+    room[:, x0:x0 + K] = x.cuda()
+    out = room[:, o0:o0 + O]
+    api.gemm_w4(room[:, x0:x0 + K], wp, out=out)
+    assert ((out.cpu().double() - want).abs() <= far).all()
+    assert torch.equal(room[:, x0:x0 + K].cpu(), x)
+    room[:, x0:x0 + K], room[:, o0:o0 + O] = GUARD, GUARD
+    assert (room == GUARD).all()
+    flat = torch.zeros(M * pitch + 64, dtype=BF16, device="cuda")
+    for step, at in ((K + O, K - 8), (K + O, K + 8), (K + O - 8, K)):       # into x's row; into the next one
+        with pytest.raises(ValueError):
+            api.gemm_w4(flat.as_strided((M, K), (step, 1), 0), wp, out=flat.as_strided((M, O), (step, 1), at))
+    with pytest.raises(ValueError):
+        api.gemm_w4(flat.as_strided((M, K), (K + O, 1), O - 8), wp, out=flat.as_strided((M, O), (K + O, 1), 0))
