@@ -520,12 +520,17 @@ int launch_clusters(void (*kern)(P...), dim3 grid, int threads, size_t smem, int
     cudaGetLastError();
     return BS_ERR_CUDA;
 }
+// The most jobs that a pass can have, as find_jobs cuts them: a slot each, or one more than its slots fill for every expert.
+int most_jobs(const MoeArgs& g)
+{
+    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, cut = g.E + slots / J;
+    return slots < cut ? slots : cut;
+}
 template <bool F16, int NG, bool ZEROS>
 int launch_gate(MoeArgs& g, int sms, cudaStream_t st)
 {
-    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
     const int split = w4_team_width(WARPS, g.lu.cbs);
-    const long long items = static_cast<long long>(jobs) * ceil_div(g.lu.rbs, WARPS / split);
+    const long long items = static_cast<long long>(most_jobs(g)) * ceil_div(g.lu.rbs, WARPS / split);
     constexpr int smem = W4TeamRing<NG, ZEROS, 2, WARPS, GATE_STAGES>::BYTES;
     if (!allow_smem(w4_moe_gate_kernel<F16, NG, ZEROS>, smem) || !w4_encode_blocks(&g.tg, g.gate, g.lu, g.E, split, WARPS / split) ||
         !w4_encode_blocks(&g.tu, g.up, g.lu, g.E, split, WARPS / split))
@@ -557,9 +562,8 @@ int launch_moe(MoeArgs& g, int sms, cudaStream_t st)
 {
     int rc = launch_clusters(w4_moe_route_kernel<F16>, dim3(ROUTE_CTAS, ceil_div(g.T, 8)), ROUTE_WARPS * 32, 0, ROUTE_CTAS, st, g);
     if (rc != BS_OK) return rc;
-    const int slots = (g.T < PASS ? g.T : PASS) * g.top_k, jobs = slots < g.E ? slots : g.E;
     g.down_split = w4_team_width(WARPS, g.ld.cbs);
-    const long long items = static_cast<long long>(jobs) * ceil_div(g.ld.rbs, 2 * WARPS / g.down_split);
+    const long long items = static_cast<long long>(most_jobs(g)) * ceil_div(g.ld.rbs, 2 * WARPS / g.down_split);
     g.down_ctas = static_cast<int>(items < 2 * sms ? items : 2 * sms);
     if (!w4_encode_blocks(&g.td, g.down, g.ld, g.E, g.down_split, WARPS / g.down_split)) return BS_ERR_CUDA;
     rc = launch_experts<F16>(g, sms, st);

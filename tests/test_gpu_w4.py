@@ -6,6 +6,7 @@ import pytest
 import torch
 
 import w4_reference as ref
+from graph_launches import launches
 from paper_2207_08820_b200 import api
 from paper_2207_08820_b200._lib import BitserialError, lib
 
@@ -586,3 +587,21 @@ def test_gemm_output_beside_its_input(M, O, K, first):
             api.gemm_w4(flat.as_strided((M, K), (step, 1), 0), wp, out=flat.as_strided((M, O), (step, 1), at))
     with pytest.raises(ValueError):
         api.gemm_w4(flat.as_strided((M, K), (K + O, 1), O - 8), wp, out=flat.as_strided((M, O), (K + O, 1), 0))
+
+
+@pytest.mark.parametrize("T,E,top_k,H,I,items", [(64, 4, 4, 2048, 768, 512), (64, 8, 8, 512, 512, 512), (130, 4, 1, 2048, 768, 192)])
+def test_moe_few_experts_with_many_slots(T, E, top_k, H, I, items):
+    """An expert's slots are cut in jobs of eight: both products get a CTA for every place of the GPU, as there are jobs enough, or one for every item.  The second
+    product's items: 32, 64 and at most 4 + 64 / 8 jobs, of 16, 8 and 16 times 32 rows by teams of two (768 columns) or four warps (512)."""
+    rng = np.random.default_rng(T + E + H)
+    x, router, gate, up, down = moe_case(rng, T, E, H, I, 128, 128, BF16, False, False)
+    w = [prepared(p, 128) for p in (gate, up, down)]
+    xd, rd = x.cuda(), router.cuda()
+    grids = dict(launches(lambda: api.moe_w4(xd, rd, *w, top_k)))
+    places = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    for name, want in (("w4_moe_gate_kernel", places), ("w4_moe_down_kernel", min(places, items))):
+        assert [grid[0] for kernel, grid in grids.items() if name in kernel] == [want]
+    some = x[:9]        # the definition, of some of the tokens
+    want, far, _, _ = ref.moe(some, router, ref.matrix(*gate, 128), ref.matrix(*up, 128), ref.matrix(*down, 128), top_k, True, BF16)
+    y = api.moe_w4(xd, rd, *w, top_k)[0][:9]
+    assert ((y.cpu().double() - want).abs() <= far).all()
