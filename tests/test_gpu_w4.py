@@ -605,3 +605,36 @@ def test_moe_few_experts_with_many_slots(T, E, top_k, H, I, items):
     want, far, _, _ = ref.moe(some, router, ref.matrix(*gate, 128), ref.matrix(*up, 128), ref.matrix(*down, 128), top_k, True, BF16)
     y = api.moe_w4(xd, rd, *w, top_k)[0][:9]
     assert ((y.cpu().double() - want).abs() <= far).all()
+
+
+def product_kernel(M, O, K, group, dtype, zeros, bias):
+    """Which of the two kernels a product launches."""
+    w = prepared(weights(np.random.default_rng(0), O, K, group, dtype, zeros), group)
+    x, b = torch.zeros(M, K, dtype=dtype, device="cuda"), torch.zeros(O, dtype=dtype, device="cuda") if bias else None
+    names = [name for name, _ in launches(lambda: api.gemm_w4(x, w, b))]
+    return [kernel for kernel in ("w4_gemm_kernel", "w4_mma_kernel") if any(kernel in name for name in names)]
+
+
+MANY_ROWS = [
+    (17, 8192, 5632, 128, BF16, False, True), (33, 4000, 5200, 64, F16, True, False), (64, 2047, 6600, 32, BF16, True, True),
+    (65, 2000, 5003, 256, BF16, False, False), (128, 2048, 4200, 128, F16, True, True), (129, 1000, 5760, 32, F16, False, True),
+    (200, 1000, 4096, 64, BF16, True, False), (300, 512, 4900, 128, BF16, True, True), (777, 200, 6000, 384, F16, False, True),
+    (1000, 129, 5121, 1024, BF16, True, True), (2048, 100, 3333, 64, BF16, False, False), (4000, 333, 700, 32, BF16, True, True),
+    (4096, 128, 1664, 128, F16, False, False), (9000, 2000, 100, 128, BF16, True, True)]
+FEW_OUTPUTS = [(4096, 20, 11000, 128, BF16, False, True), (4096, 17, 11001, 128, F16, True, False), (1 << 20, 1, 16, 32, BF16, True, True)]
+
+
+@pytest.mark.parametrize("case", MANY_ROWS + FEW_OUTPUTS, ids=str)
+def test_gemm_products_of_the_kernel_for_many_rows(case):
+    assert product_kernel(*case) == ["w4_mma_kernel"]
+
+
+@pytest.mark.parametrize("case", [(1, 24576, 8192, 128, BF16, False, False), (16, 4096, 4096, 128, BF16, False, False), (33, 31, 2050, 32, F16, True, True), (4096, 1, 11000, 128, BF16, False, True)], ids=str)
+def test_gemm_products_of_the_kernel_for_few_rows(case):
+    """Up to 16 rows, and more where there is little work in each."""
+    assert product_kernel(*case) == ["w4_gemm_kernel"]
+
+
+@pytest.mark.parametrize("M,O,K,group,dtype,zeros,bias", FEW_OUTPUTS)
+def test_gemm_many_rows_of_few_outputs(M, O, K, group, dtype, zeros, bias):
+    check_gemm(np.random.default_rng(O + K), M, O, K, group, dtype, zeros, bias)
