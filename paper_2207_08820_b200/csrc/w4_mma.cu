@@ -9,9 +9,9 @@
 // whatever a step needs (x, its expanded weights, and with one group a step a free accumulator) arrives at one barrier, and one commit frees
 // all of it again.
 //
-// 4096 x 16384 x 4096: 670 us, 820 TFLOP/s (half of what the tensor core does): a step takes about 1100 cycles, the 512 of its MMAs beside 750 in which an
-// accumulator is read out, which the other two hide only in part, and hand-offs.  200 x 4096 x 4096: 19.9 us, of which 4 are MMAs: the first blocks' way in, 15
-// steps a CTA, the parts' way through memory and the second launch.
+// 4096 x 16384 x 4096: 680 us, 810 TFLOP/s (half of what the tensor core does; 585 us in a short run, before the power limit is met): a step takes about
+// 1100 cycles, the 512 of its MMAs beside 750 in which an accumulator is read out, which the other two hide only in part, and hand-offs.  200 x 4096 x
+// 4096: 19.9 us, of which 4 are MMAs: the first blocks' way in, 14 steps a CTA, the parts' way through memory and the second launch.
 //
 // Work: tiles of 128 rows by up to 128 rows of x.  A CTA takes whole tiles, neighbours at a time, as long as every CTA gets one; what is left, less than
 // two tiles a CTA, is cut (unless that saves little) into equal runs of (tile, 128 columns), and a small kernel adds the parts of the tiles that were cut, in
