@@ -4,6 +4,7 @@
 #include <ATen/core/grad_mode.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <Python.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -306,10 +307,12 @@ PyObject* unchanged(PyObject*, PyObject* const* a, Py_ssize_t n)
 // ---- 4-bit weights with a scale per group
 
 // The device of a call's tensors and its stream are the current ones while its memory is taken and its work enqueued: what the call allocates belongs
-// to the stream that it runs on.  `stream` argument: None (the device's current stream) or a torch stream of that device.
+// to the stream that it runs on, and what the caller gives it is not taken for something else before that stream is done with it, though the caller lets
+// go of it at once.  `stream` argument: None (the device's current stream) or a torch stream of that device.
 struct OnStream {
     c10::cuda::OptionalCUDAGuard device;
     c10::cuda::OptionalCUDAStreamGuard guard;
+    std::optional<c10::cuda::CUDAStream> given;
     void* stream;
     OnStream(const at::Tensor& x, PyObject* o)
     {
@@ -324,7 +327,13 @@ struct OnStream {
         if (index != at) mismatch("the stream belongs to another device than the tensors");
         const c10::cuda::CUDAStream s = c10::cuda::CUDAStream::unpack3(id, static_cast<c10::DeviceIndex>(index), static_cast<c10::DeviceType>(type));
         guard.reset_stream(s);
+        given = s;
         stream = s.stream();
+    }
+    void keep(std::initializer_list<PyObject*> objects) const
+    {
+        for (PyObject* o : objects)
+            if (given && o != Py_None) c10::cuda::CUDACachingAllocator::recordStream(tensor(o).storage().data_ptr(), *given);
     }
     static int64_t attribute(PyObject* o, const char* name)
     {
@@ -402,6 +411,7 @@ PyObject* w4_quantise(PyObject*, PyObject* const* a, Py_ssize_t n)
         char *cp = static_cast<char*>(codes.data_ptr()), *sp = static_cast<char*>(scales.data_ptr()), *zp = zeros ? static_cast<char*>(z.data_ptr()) : nullptr;
         const int64_t G = shape.back(), w_size = w.element_size(), s_size = scales.element_size();
         int rc = BS_OK;
+        on.keep({a[0]});
         {
             NoGil free;
             for (int64_t o = 0; o < rows && rc == BS_OK; o += most)
@@ -443,6 +453,7 @@ PyObject* w4_prepare(PyObject*, PyObject* const* a, Py_ssize_t n)
         const void *cp = pointer(codes), *sp = pointer(scales);
         const at::Tensor out = fresh({static_cast<int64_t>(bytes * E)}, at::kByte, codes);
         int rc;
+        on.keep({a[0], a[1], a[2]});
         {
             NoGil free;
             rc = bs_w4_prepare(static_cast<const int8_t*>(cp), sp, z, E, O, K, group, out.data_ptr(), on.stream);
@@ -492,6 +503,7 @@ PyObject* w4_gemm(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (need_ws) ws = fresh({static_cast<int64_t>(need_ws)}, at::kByte, x);
         void* yp = y.data_ptr();
         int rc;
+        on.keep({a[0], a[1], a[7], a[8]});
         {
             NoGil free;
             rc = bs_w4_gemm(x.const_data_ptr(), ldx, M, wp, O, K, group, zeros, static_cast<bs_float_t>(type), bias, yp, ldy, need_ws ? ws.data_ptr() : nullptr, need_ws,
@@ -543,6 +555,7 @@ PyObject* w4_moe(PyObject*, PyObject* const* a, Py_ssize_t n)
         const at::Tensor ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, x);
         void *yp = y.data_ptr(), *wsp = ws.data_ptr();
         int rc;
+        on.keep({a[0], a[1], a[2], a[3], a[4], a[13]});
         {
             NoGil free;
             rc = bs_w4_moe(x.const_data_ptr(), ldx, T, rp, E, H, I, gate, up, gu, zu, down, gd, zd, static_cast<bs_float_t>(type), top_k, renormalise, yp,

@@ -638,3 +638,54 @@ def test_gemm_products_of_the_kernel_for_few_rows(case):
 @pytest.mark.parametrize("M,O,K,group,dtype,zeros,bias", FEW_OUTPUTS)
 def test_gemm_many_rows_of_few_outputs(M, O, K, group, dtype, zeros, bias):
     check_gemm(np.random.default_rng(O + K), M, O, K, group, dtype, zeros, bias)
+
+
+@pytest.mark.parametrize("what", ["quantise", "prepare", "gemm", "moe"])
+def test_inputs_let_go_of_before_another_stream_has_read_them(what):
+    """A call on a stream that is still busy, its inputs dropped at once and their memory asked for again on the current stream."""
+    rng = np.random.default_rng(15)
+    H, T = 256, 64
+    plain = normal(rng, (H, H), BF16)
+    codes, scales, _ = weights(rng, H, H, 128, BF16, False)
+    w = prepared((codes, scales, None), 128)
+    e = [prepared(weights(rng, H, H, 128, BF16, False, (4,)), 128) for _ in range(3)]
+    x, router, bias = normal(rng, (T, H), BF16), normal(rng, (4, H), BF16), normal(rng, (H,), BF16)
+    calls = dict(quantise=((plain,), lambda w, **k: api.quantise_w4(w, **k)[:2]),
+                 prepare=((codes, scales), lambda c, s, **k: (api.prepare_w4(c, s, **k).data,)),
+                 gemm=((x, bias), lambda x, b, **k: (api.gemm_w4(x, w, b, **k),)),
+                 moe=((x, router), lambda x, r, **k: api.moe_w4(x, r, *e, 2, **k)))
+    inputs, call = calls[what]
+    want = call(*[t.cuda() for t in inputs])
+    side = torch.cuda.Stream()
+    for t in inputs:        # a kernel's first launch waits for all streams
+        torch.full(t.shape, 3, dtype=t.dtype, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    given = [t.cuda() for t in inputs]
+    places = {t.data_ptr() for t in given}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)      # 0.2 s
+    got = call(*given, stream=side)
+    del given
+    junk = [torch.full(t.shape, 3, dtype=t.dtype, device="cuda") for t in inputs for _ in range(3)]
+    assert not side.query(), "the stream was to be busy until here"
+    assert not places & {t.data_ptr() for t in junk}
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_captured_with_the_stream_named():
+    """The capturing stream given by name, with an input that lives in the capture alone."""
+    rng = np.random.default_rng(16)
+    w = prepared(weights(rng, 100, 136, 64, F16, True), 64)
+    x = normal(rng, (5, 136), F16).cuda()
+    out = torch.empty(5, 100, dtype=F16, device="cuda")
+    api.gemm_w4(x + x, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        api.gemm_w4(x + x, w, out=out, stream=torch.cuda.current_stream())
+    for _ in range(2):
+        x.copy_(normal(rng, (5, 136), F16))
+        graph.replay()
+        assert torch.equal(out, api.gemm_w4(x + x, w))
