@@ -5,11 +5,12 @@
 //   sum     y[token] = sum over its slots of z[slot]
 // Each block of the chosen experts' weights comes from HBM once for up to 64 tokens (more tokens are further passes), through shared memory, and is multiplied
 // with mma.sync (w4_dot.cuh).  What bounds it: for one token the four launches (12 us with next to no weights; 64 experts of 2048 x 1024, 8 chosen: 24.6 us, of
-// which their bytes take 4), with more the expansion of the codes (64 tokens, 128 experts of 2048 x 768, 126 of them chosen: 121 us, 2.5 TB/s; 8 tokens, 2 of 16
-// experts of 4096 x 8192, alone: 137 us with 8 of them chosen, 160 with 10, 184 with 12, 3.0 to 3.4 TB/s).  Hidden values stay in 32 bits until they are split in two bf16
-// terms (hi + lo, 16 bits of mantissa and the sign between them), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.
-// All 24 bits, as three terms split in the second product from the 32-bit values, took 139 us in place of 121; the error against 64 bits, which the
-// rounding of y makes, is that of float32 hidden values to five digits in bf16, four in fp16.
+// which their bytes take 4), with more the expansion of the codes, which fills half of the issue slots, and x, hidden values and sums, which 17 warps an SM wait for
+// (64 tokens, 128 experts of 2048 x 768, 126 of them chosen: 121 us, 2.5 TB/s; 8 tokens, 2 of 16 experts of 4096 x 8192, alone: 137 us with 8 of them chosen, 160
+// with 10, 184 with 12, 3.0 to 3.4 TB/s).  Hidden values stay in 32 bits until they are split in two bf16 terms (hi + lo, 16 bits of mantissa and the sign
+// between them), which costs the second product twice the MMAs and no bytes of weights; the range of fp16 would not hold them.  All 24 bits, as three terms split in the
+// second product from the 32-bit values, took 139 us in place of 121; the error against 64 bits, which the rounding of y makes, is that of float32 hidden
+// values to five digits in bf16, four in fp16.
 #include "w4_dot.cuh"
 
 namespace bs {
