@@ -180,6 +180,8 @@ def prepare(case, seed):
         s["weights"] = torch.rand(B, H, max(lens), device="cuda", generator=gen) if case["weights"] else None
     else:
         w = torch.exp(2 * torch.randn(B, H, max(lens), device="cuda", generator=gen))
+        stay = [min(n, case["keep"]) for n in lens]        # what goes in and comes out again
+        s["first"], s["starts"], s["total"] = torch.zeros(B, dtype=torch.int32, device="cuda"), _starts(stay), sum(stay)
         s["weights"] = torch.where(w < 0.2, torch.zeros_like(w), torch.where(w < 1, (w * 64).round() / 64, w))        # ties
     return s
 
@@ -291,8 +293,7 @@ def run(s):
             return [out] + ([] if weights is None else [weights])
         if kind == "evict":
             lengths, weights, kept = api.evict_kv4(s["cache"], s["table"], s["lengths"], s["weights"], case["keep"], recent=case["recent"], into=s["into"])
-            stay = [min(n, case["keep"]) for n in s["lens"]]
-            return [lengths, weights, kept, *api.read_kv4(s["cache"], s["into"], torch.zeros_like(lengths), _starts(stay), total=sum(stay))]
+            return [lengths, weights, kept, *api.read_kv4(s["cache"], s["into"], s["first"], s["starts"], total=s["total"])]
         return api.attend_prompt(s["q"], s["k"], s["v"], s["starts"], s["starts_k"], causal=case["causal"])
     if kind == "store":
         i = torch.arange(s["k"].shape[0], device="cuda")
