@@ -488,6 +488,67 @@ int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, in
               int renormalise, void* y, int32_t* experts, float* weights, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention for language models over keys and values of 4 bits (no counterpart in the paper; the codes are those of its Section IV quantiser with a step and an
+ * offset per group of channels), next to the products on 4-bit weights above.
+ *
+ * A cache is `pages` pages of `page` entries for each of `heads` heads: device memory of pages * bs_kv4_page_bytes(...) bytes, 16-byte aligned.  Sequence b's
+ * entry i lies in page table[b * table_pitch + i / page]: int32, B rows of `width` pages.  Sequences may share pages that are only read.  An entry whose page
+ * is not one of the cache's is not there: it is neither stored nor read.  Of a vector x of `group` channels of a key or a value the cache holds
+ *       m = min x,  s = type((max x - min x) / 15), difference and quotient in binary32,  c = clip(round((x - m) / s), 0, 15)
+ * round is half-even of the exact quotient; where s is 0 c is 0.  It stands for c s + m.  A vector that holds an infinity or a NaN (or whose span binary32 does
+ * not hold) stands for NaN.
+ * Supported: D of 64, 96 or 128, groups of 32, 64 or D that divide D, pages of 16 to 1024 entries, a power of two.
+ *
+ * Rows of several sequences are packed: `starts` is int32 [B + 1], sequence b's rows are starts[b] .. starts[b + 1] - 1, in ascending order; rows that no sequence
+ * holds are neither read nor written.  NULL: T = B, a row a sequence.  Tables, lengths and starts are device memory; what lies outside of the tensors is not touched,
+ * whatever they hold.  Strides are in values and multiples of 8; tensors of values are 16-byte aligned.
+ */
+typedef struct { void* data; int pages, heads, D, page, group; bs_float_t type; } bs_kv4_cache;
+size_t bs_kv4_page_bytes(int heads, int D, int page, int group);
+
+/*
+ * bs_kv4_append -- keys and values of new tokens into a cache.  k, v: device, T rows of `heads` vectors of D values of the cache's type, rows k_token (v_token)
+ * and heads k_head (v_head) values apart.  Row j of sequence b becomes its entry at[b] + j (at: device int32 [B]).  Entries behind the table are not stored.
+ * bs_kv4_read -- the same entries out of a cache: k, v [T][heads][D] of its type, c s + m in binary32, rounded once.  Rows whose entry is not there are zero.
+ */
+int bs_kv4_append(const void* k, long long k_token, long long k_head, const void* v, long long v_token, long long v_head, int T, const bs_kv4_cache* cache,
+                  const int32_t* table, long long table_pitch, int width, int B, const int32_t* at, const int32_t* starts, void* stream);
+int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width, int B, const int32_t* at, const int32_t* starts, int T,
+                void* k, void* v, void* stream);
+
+/*
+ * bs_kv4_attend -- the newest tokens of each sequence attend to its entries.
+ *   q        device, T rows of q_heads vectors of D values of the cache's type, q_token and q_head values apart; q_heads is a multiple of the cache's heads, and
+ *            head j of q goes with head j / (q_heads / heads) of the cache
+ *   lengths  device int32 [B]: entries of each sequence, those of the rows of q (stored before) among them: with t rows of q and n entries, row i sees the entries
+ *            below n - t + i + 1.  A row that sees nothing gives zeros.
+ *   out      device [T][q_heads][D]: softmax(scale q K^T) V, scale > 0
+ *   weights  device float [B][heads][N], rows weights_head and weights_sequence values apart, or NULL: the attention that each entry got, summed over the rows of q
+ *            and the heads that share it, is added to it.  Entries from N on are left out.
+ *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights); two calls that may run at the same time need one each
+ * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms; the same call gives the same bits every time.
+ */
+size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int N);
+int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int q_heads, const bs_kv4_cache* cache, const int32_t* table, long long table_pitch,
+                  int width, int B, const int32_t* lengths, const int32_t* starts, float scale, void* out, float* weights, long long weights_sequence,
+                  long long weights_head, int N, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * bs_kv4_evict -- cuts sequences of more than `keep` entries to `keep`.  Every head keeps its `recent` newest entries and of the others those with the largest
+ * weights (float [B][heads][N], N at least the longest sequence; ties to the lowest index, a NaN before everything), in their order.
+ *   into         int32 [B][into_width]: pages that take what stays, other ones than those of any sequence; room for keep entries.  NULL: the sequences' own pages,
+ *                which none of them may share; their entries from the new length on are then as good as gone
+ *   lengths_out  device int32 [B];  weights_out  device float [B][heads][N]: the weights of what stays, zeros behind;  kept  device int32 [B][heads][keep]: where
+ *                it was, -1 behind.  None of them may overlap what is read.
+ *   workspace    bs_kv4_evict_workspace_bytes(...) bytes (0 and NULL with `into`); two calls that may run at the same time need one each
+ * Sequences of up to `keep` entries stay as they are, and are brought to `into`.  B up to 65535.
+ */
+size_t bs_kv4_evict_workspace_bytes(const bs_kv4_cache* cache, int B, int keep, int into);
+int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width, const int32_t* into, long long into_pitch, int into_width,
+                 int B, const int32_t* lengths, const float* weights, long long weights_sequence, long long weights_head, int N, int keep, int recent,
+                 int32_t* lengths_out, float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * bs_popc_rate -- register-only micro-benchmark of the SM population-count pipe: every thread runs
  * `iters` rounds of independent  acc += popc(x & y)  chains.  Writes the measured rate in
  * popc32(AND) word-operations per second to *wordops_per_s (HOST pointer).  Synchronises the device.

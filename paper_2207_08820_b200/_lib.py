@@ -42,6 +42,11 @@ class SequenceLayer(ctypes.Structure):
                 ("p", ConvParams), ("chained", ctypes.c_int), ("aside", ctypes.c_int), ("join", ctypes.c_int * 4)]
 
 
+class KV4CacheDesc(ctypes.Structure):
+    """Mirror of ``bs_kv4_cache`` (include/bitserial.h)."""
+    _fields_ = [("data", ctypes.c_void_p)] + [(f, ctypes.c_int) for f in ("pages", "heads", "D", "page", "group", "type")]
+
+
 class LayerPlan(ctypes.Structure):
     """Mirror of ``bs_layer_plan`` (include/bitserial.h)."""
     _fields_ = [(f, ctypes.c_int) for f in ("filters", "row_tiles", "channels", "resident", "stages", "accumulators", "teams", "blocks", "items")]
@@ -182,6 +187,21 @@ def lib() -> ctypes.CDLL:
     L.bs_w4_moe_workspace_bytes.argtypes = [i, i, i, i, ll]
     L.bs_w4_moe.restype = i
     L.bs_w4_moe.argtypes = [vp, ll, i, vp, i, i, i, vp, vp, i, i, vp, i, i, i, i, i, vp, vp, vp, vp, sz, vp]
+    cache = ctypes.POINTER(KV4CacheDesc)
+    L.bs_kv4_page_bytes.restype = sz
+    L.bs_kv4_page_bytes.argtypes = [i] * 4
+    L.bs_kv4_append.restype = i
+    L.bs_kv4_append.argtypes = [vp, ll, ll, vp, ll, ll, i, cache, vp, ll, i, i, vp, vp, vp]
+    L.bs_kv4_read.restype = i
+    L.bs_kv4_read.argtypes = [cache, vp, ll, i, i, vp, vp, i, vp, vp, vp]
+    L.bs_kv4_attend_workspace_bytes.restype = sz
+    L.bs_kv4_attend_workspace_bytes.argtypes = [cache, i, i, i, i, i]
+    L.bs_kv4_attend.restype = i
+    L.bs_kv4_attend.argtypes = [vp, ll, ll, i, i, cache, vp, ll, i, i, vp, vp, ctypes.c_float, vp, vp, ll, ll, i, vp, sz, vp]
+    L.bs_kv4_evict_workspace_bytes.restype = sz
+    L.bs_kv4_evict_workspace_bytes.argtypes = [cache, i, i, i]
+    L.bs_kv4_evict.restype = i
+    L.bs_kv4_evict.argtypes = [cache, vp, ll, i, vp, ll, i, i, vp, vp, ll, ll, i, i, i, vp, vp, vp, vp, sz, vp]
     L.bs_popc_rate.restype = i
     L.bs_popc_rate.argtypes = [i, ctypes.POINTER(ctypes.c_double)]
     L.bs_status_string.restype = ctypes.c_char_p
@@ -197,4 +217,5 @@ EXPORTED = ("bs_packed_act_bytes", "bs_packed_wgt_bytes", "bs_packed_rows_bytes"
             "bs_tc_weights_bytes", "bs_tc_weights_read_bytes", "bs_tc_prepare_weights", "bs_tc_supported", "bitserial_conv2d_tc", "bitserial_conv2d_tc_chained", "bs_tc_chain_workspace_bytes", "bitserial_conv2d_tc_chain", "bitserial_gemm_tc", "bs_sequence_create", "bs_sequence_create_ws", "bs_sequence_workspace_bytes", "bs_sequence_launches", "bs_sequence_layer_plan", "bs_sequence_input", "bs_sequence_run_ready", "bitpack_activations_operands", "bs_stem_codes_operands_f32", "bs_sequence_run", "bs_sequence_destroy", "bs_l2_prefetch",
             "bs_conv2d_f32", "bs_maxpool2d_f32", "bs_stem_codes_f32", "bs_stem_codes_supported", "bs_avgpool_codes_f32", "bs_fc_f32",
             "bs_check_status", "bs_quantiser_bounds", "bs_requant_bounds", "bs_selftest_wait_timeout", "bs_popc_rate", "bs_status_string",
-            "bs_w4_quantise", "bs_w4_bytes", "bs_w4_prepare", "bs_w4_gemm_workspace_bytes", "bs_w4_gemm", "bs_w4_moe_workspace_bytes", "bs_w4_moe")
+            "bs_w4_quantise", "bs_w4_bytes", "bs_w4_prepare", "bs_w4_gemm_workspace_bytes", "bs_w4_gemm", "bs_w4_moe_workspace_bytes", "bs_w4_moe",
+            "bs_kv4_page_bytes", "bs_kv4_append", "bs_kv4_read", "bs_kv4_attend_workspace_bytes", "bs_kv4_attend", "bs_kv4_evict_workspace_bytes", "bs_kv4_evict")

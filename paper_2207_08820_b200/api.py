@@ -403,6 +403,75 @@ def moe_w4(x: torch.Tensor, router: torch.Tensor, gate: W4Weights, up: W4Weights
     return y, experts, weights
 
 
+class KV4Cache(NamedTuple):
+    """Keys and values of 4 bits in pages (:func:`cache_kv4`), for :func:`append_kv4`, :func:`read_kv4`, :func:`attend_kv4` and :func:`evict_kv4`."""
+    data: torch.Tensor      # uint8 [pages, bytes of a page]
+    heads: int
+    D: int                  # channels of a head
+    page: int               # entries (tokens) of a page
+    group: int              # channels that share a step and an offset
+    dtype: torch.dtype      # of steps and offsets, and of the keys, values and queries that go with them
+
+    @property
+    def _native(self):
+        return self.data, self.heads, self.D, self.page, self.group, _FLOAT_TYPES[self.dtype]
+
+
+def cache_kv4(pages: int, heads: int, D: int, *, page: int = 64, group: Optional[int] = None, dtype: torch.dtype = torch.bfloat16, device="cuda") -> KV4Cache:
+    """A cache of ``pages`` pages of ``page`` entries for ``heads`` heads of ``D`` channels (64, 96 or 128), with a step and an offset (``dtype``: float16 or
+    bfloat16) for every ``group`` channels (32, 64 or D; None: D).  Which pages a sequence has is the caller's: a table int32 [sequences, pages] goes with each call."""
+    group = D if group is None else group
+    size = lib().bs_kv4_page_bytes(heads, D, page, group)
+    if size == 0:
+        raise ValueError("heads of 64, 96 or 128 channels, groups of 32, 64 or all of them, pages of a power of two from 16 to 1024 expected")
+    if dtype not in (torch.float16, torch.bfloat16) or pages < 1:
+        raise ValueError("float16 or bfloat16 and at least one page expected")
+    return KV4Cache(torch.zeros(pages, size, dtype=torch.uint8, device=device), heads, D, page, group, dtype)
+
+
+def append_kv4(k: torch.Tensor, v: torch.Tensor, cache: KV4Cache, table: torch.Tensor, at: torch.Tensor, starts: Optional[torch.Tensor] = None, *, stream=None) -> None:
+    """Stores keys and values [T, heads, D] of new tokens in the cache (``bs_kv4_append``): token j of sequence b as its entry ``at[b] + j``.  ``starts`` int32
+    [sequences + 1] says whose the tokens are; without it each sequence has one.  Tokens and heads may be apart (views of a fused projection)."""
+    global launch_count
+    _check(native().kv4_append(k, v, *cache._native, table, at, starts, stream), "bs_kv4_append")
+    launch_count += 1
+
+
+def read_kv4(cache: KV4Cache, table: torch.Tensor, at: torch.Tensor, starts: Optional[torch.Tensor] = None, total: Optional[int] = None, *, stream=None):
+    """The keys and values [T, heads, D] that the cache holds (``bs_kv4_read``): of sequence b its entries from ``at[b]`` on, as many as ``starts`` says (``total``: how
+    many in all, starts' last value), or one each."""
+    global launch_count
+    if (starts is None) != (total is None):
+        raise ValueError("starts and their total, or neither, expected")
+    st, k, v = native().kv4_read(*cache._native, table, at, starts, total if total is not None else 0, stream)
+    _check(st, "bs_kv4_read")
+    launch_count += 1
+    return k, v
+
+
+def attend_kv4(q: torch.Tensor, cache: KV4Cache, table: torch.Tensor, lengths: torch.Tensor, starts: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+               weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of q [T, q_heads, D], the newest tokens of each sequence (``starts`` as in :func:`append_kv4`, without it one each), over the sequence's entries:
+    ``lengths`` int32 [sequences], those of the tokens themselves included; each sees the entries up to its own.  ``scale``: 1 / sqrt(D) unless given.
+    ``weights`` float32 [sequences, heads, entries]: what each entry got is added to it (for :func:`evict_kv4`).  No gradients."""
+    global launch_count
+    st, o = native().kv4_attend(q, *cache._native, table, lengths, starts, cache.D ** -0.5 if scale is None else scale, weights, out, stream)
+    _check(st, "bs_kv4_attend")
+    launch_count += 2 if weights is None else 3
+    return o
+
+
+def evict_kv4(cache: KV4Cache, table: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor, keep: int, *, recent: int = 0, into: Optional[torch.Tensor] = None, stream=None):
+    """Cuts sequences of more than ``keep`` entries to ``keep`` (``bs_kv4_evict``): each head keeps its ``recent`` newest entries and of the others those with the largest
+    ``weights`` [sequences, heads, entries], in their order, either in the sequence's pages or in those of the table ``into``, which are other ones than ``table`` has.
+    Returns (lengths int32 [sequences], weights of what stays with zeros behind, and where it was, int32 [sequences, heads, keep], -1 behind)."""
+    global launch_count
+    st, n, w, kept = native().kv4_evict(*cache._native, table, lengths, weights, keep, recent, into, stream)
+    _check(st, "bs_kv4_evict")
+    launch_count += 3 if into is None else 2
+    return n, w, kept
+
+
 def bs_check_status(stream=None) -> None:
     st = lib().bs_check_status(_stream_ptr(stream))
     if st != 0:

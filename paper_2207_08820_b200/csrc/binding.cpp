@@ -9,6 +9,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+
 #include "bitserial.h"
 
 namespace {
@@ -565,9 +567,229 @@ PyObject* w4_moe(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// ---- keys and values of 4 bits, and attention
+
+void no_gradient_attention(const at::Tensor& t)
+{
+    if (t.requires_grad() && at::GradMode::is_enabled()) mismatch("there is no gradient through attention: a tensor that requires one is taken under torch.no_grad() only");
+}
+// cache: data, heads, D, page, group, type, as six arguments.  Pages: what the data holds.
+bs_kv4_cache cache_of(PyObject* const* a)
+{
+    const at::Tensor& t = tensor(a[0]);
+    bs_kv4_cache c{};
+    c.heads = integer(a[1]); c.D = integer(a[2]); c.page = integer(a[3]); c.group = integer(a[4]); c.type = static_cast<bs_float_t>(integer(a[5]));
+    const size_t bytes = bs_kv4_page_bytes(c.heads, c.D, c.page, c.group);
+    if (bytes == 0 || t.scalar_type() != at::kByte || t.nbytes() == 0 || t.nbytes() % bytes != 0) mismatch("the data of a cache of this layout expected");
+    c.data = pointer(t);
+    c.pages = small(static_cast<int64_t>(t.nbytes() / bytes));
+    return c;
+}
+constexpr int CACHE = 6;
+// A vector of int32, `n` of them.
+const int32_t* counts(PyObject* o, int64_t n, const at::Tensor& like, const char* what)
+{
+    const at::Tensor& t = tensor(o);
+    if (t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) != n) mismatch(what);
+    same_device(t, like);
+    return static_cast<const int32_t*>(pointer(t));
+}
+struct Table { const int32_t* pages; int64_t pitch; int width, B; };
+Table table_of(PyObject* o, const at::Tensor& like)
+{
+    const at::Tensor& t = tensor(o);
+    if (!t.is_cuda() || t.scalar_type() != at::kInt || t.dim() != 2 || t.numel() == 0) mismatch("a table of pages expected: int32 [sequences, pages], on the GPU");
+    if (t.size(1) > 1 && t.stride(1) != 1) mismatch("a table of pages with contiguous rows expected");
+    same_device(t, like);
+    return {static_cast<const int32_t*>(t.const_data_ptr()), t.size(0) == 1 ? t.size(1) : t.stride(0), small(t.size(1)), small(t.size(0))};
+}
+// Rows of vectors [T, heads, D], with strides of their own.
+struct Vectors { const void* p; int64_t token, head; };
+Vectors vectors(const at::Tensor& t, bs_float_t type, int64_t heads, int64_t D, const at::Tensor& like, const char* what)
+{
+    if (!t.is_cuda() || t.dim() != 3 || (heads >= 0 && t.size(1) != heads) || t.size(2) != D || float_type(t) != type) mismatch(what);
+    if (D > 1 && t.stride(2) != 1 && t.numel() > 0) mismatch("vectors with contiguous channels expected");
+    same_device(t, like);
+    // a single row or head may have any stride
+    return {t.const_data_ptr(), t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0};
+}
+// Whether the memory that two tensors span has anything in common.
+bool meet(const at::Tensor& a, const at::Tensor& b)
+{
+    if (a.numel() == 0 || b.numel() == 0) return false;
+    auto span = [](const at::Tensor& t) {
+        int64_t last = 0;
+        for (int64_t i = 0; i < t.dim(); ++i) last += (t.size(i) - 1) * t.stride(i);
+        return static_cast<int64_t>((last + 1) * t.element_size());
+    };
+    const char *p = static_cast<const char*>(a.const_data_ptr()), *q = static_cast<const char*>(b.const_data_ptr());
+    return p < q + span(b) && q < p + span(a);
+}
+
+// k, v, cache (6), table, at, starts or None, stream
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 6 + CACHE);
+        const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &data = tensor(a[2]);
+        PyObject* const* r = a + 2 + CACHE;
+        for (int i : {0, 1}) no_gradient_attention(tensor(a[i]));
+        const OnStream on(data, r[3]);
+        const bs_kv4_cache c = cache_of(a + 2);
+        const Vectors kv = vectors(k, c.type, c.heads, c.D, data, "keys [tokens, heads, channels] of the cache's type expected"),
+                      vv = vectors(v, c.type, c.heads, c.D, data, "values [tokens, heads, channels] of the cache's type expected");
+        if (k.size(0) != v.size(0)) mismatch("as many keys as values expected");
+        if (meet(k, data) || meet(v, data)) mismatch("the cache overlaps an input");
+        const int T = small(k.size(0));
+        const Table t = table_of(r[0], data);
+        const int32_t *at = counts(r[1], t.B, data, "the first new entry of each sequence, int32, expected"),
+                      *starts = r[2] == Py_None ? nullptr : counts(r[2], t.B + 1LL, data, "the starts of all sequences and the end, int32, expected");
+        if (!starts && T != t.B) mismatch("one token a sequence expected where there are no starts");
+        int rc;
+        on.keep({a[0], a[1], a[2], r[0], r[1], r[2]});
+        {
+            NoGil free;
+            rc = bs_kv4_append(T ? kv.p : c.data, kv.token, kv.head, T ? vv.p : c.data, vv.token, vv.head, T, &c, t.pages, t.pitch, t.width, t.B, at, starts, on.stream);
+        }
+        return Py_BuildValue("i", rc);
+    });
+}
+
+// cache (6), table, at, starts or None, total, stream
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 5 + CACHE);
+        const at::Tensor& data = tensor(a[0]);
+        PyObject* const* r = a + CACHE;
+        const OnStream on(data, r[4]);
+        const bs_kv4_cache c = cache_of(a);
+        const Table t = table_of(r[0], data);
+        const int32_t *at = counts(r[1], t.B, data, "the first entry of each sequence, int32, expected"),
+                      *starts = r[2] == Py_None ? nullptr : counts(r[2], t.B + 1LL, data, "the starts of all sequences and the end, int32, expected");
+        const int T = starts ? integer(r[3]) : t.B;
+        if (T < 0) mismatch("a number of entries that is not negative expected");
+        const at::ScalarType type = c.type == BS_F16 ? at::kHalf : at::kBFloat16;
+        // rows that no sequence holds are zero, too
+        const at::Tensor k = fresh({T, c.heads, c.D}, type, data), v = fresh({T, c.heads, c.D}, type, data);
+        int rc;
+        on.keep({a[0], r[0], r[1], r[2]});
+        {
+            NoGil free;
+            rc = T == 0 ? BS_OK : bs_kv4_read(&c, t.pages, t.pitch, t.width, t.B, at, starts, T, k.data_ptr(), v.data_ptr(), on.stream);
+        }
+        return Py_BuildValue("(iNN)", rc, give(k), give(v));
+    });
+}
+
+// q, cache (6), table, lengths, starts or None, scale, weights or None, out or None, stream
+PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 8 + CACHE);
+        const at::Tensor &q = tensor(a[0]), &data = tensor(a[1]);
+        PyObject* const* r = a + 1 + CACHE;
+        no_gradient_attention(q);
+        const OnStream on(data, r[6]);
+        const bs_kv4_cache c = cache_of(a + 1);
+        const Vectors qv = vectors(q, c.type, -1, c.D, data, "queries [tokens, heads, channels] of the cache's type expected");
+        const int T = small(q.size(0)), heads = small(q.size(1));
+        if (heads == 0 || heads % c.heads != 0) mismatch("heads of q that are a multiple of the cache's expected");
+        const Table t = table_of(r[0], data);
+        const int32_t *lengths = counts(r[1], t.B, data, "the length of each sequence, int32, expected"),
+                      *starts = r[2] == Py_None ? nullptr : counts(r[2], t.B + 1LL, data, "the starts of all sequences and the end, int32, expected");
+        if (!starts && T != t.B) mismatch("one token a sequence expected where there are no starts");
+        const float scale = real(r[3]);
+        float* wp = nullptr;
+        int64_t w_sequence = 0, w_head = 0;
+        int N = 0;
+        if (r[4] != Py_None) {
+            const at::Tensor& w = tensor(r[4]);
+            if (!w.is_cuda() || w.scalar_type() != at::kFloat || w.dim() != 3 || w.size(0) != t.B || w.size(1) != c.heads || w.numel() == 0)
+                mismatch("weights float32 [sequences, heads, entries] expected");
+            if (w.size(2) > 1 && w.stride(2) != 1) mismatch("weights with contiguous entries expected");
+            same_device(w, data);
+            no_gradient_attention(w);
+            N = small(w.size(2));
+            w_head = w.size(1) > 1 ? w.stride(1) : N;
+            w_sequence = w.size(0) > 1 ? w.stride(0) : 0;
+            if (w_head < N || (w.size(0) > 1 && w_sequence < (w.size(1) - 1) * w_head + N)) mismatch("weights whose rows do not overlap expected");
+            wp = static_cast<float*>(w.data_ptr());
+            if (meet(w, q) || meet(w, data)) mismatch("the weights overlap an input");
+        }
+        at::Tensor out;
+        if (r[5] != Py_None) {
+            out = tensor(r[5]);
+            if (out.scalar_type() != q.scalar_type() || out.sizes() != q.sizes()) mismatch("an output of q's type and shape expected");
+            same_device(out, data);
+            no_gradient_attention(out);
+            if (out.numel() > 0) pointer(out);
+            if (meet(out, q) || meet(out, data) || (wp && meet(out, tensor(r[4])))) mismatch("the output overlaps an input");
+        } else {
+            out = fresh(q.sizes(), q.scalar_type(), data);
+        }
+        if (T == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(out));
+        const size_t bytes = bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, N);
+        if (bytes == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_ERR_UNSUPPORTED), give(out));
+        const at::Tensor ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, data);
+        void *op = out.data_ptr(), *wsp = ws.data_ptr();
+        int rc;
+        on.keep({a[0], a[1], r[0], r[1], r[2], r[4], r[5]});
+        {
+            NoGil free;
+            rc = bs_kv4_attend(qv.p, qv.token, qv.head, T, heads, &c, t.pages, t.pitch, t.width, t.B, lengths, starts, scale, op, wp, w_sequence, w_head, N, wsp, bytes, on.stream);
+        }
+        return Py_BuildValue("(iN)", rc, give(out));
+    });
+}
+
+// cache (6), table, lengths, weights, keep, recent, into or None, stream
+PyObject* kv4_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 7 + CACHE);
+        const at::Tensor& data = tensor(a[0]);
+        PyObject* const* r = a + CACHE;
+        const OnStream on(data, r[6]);
+        const bs_kv4_cache c = cache_of(a);
+        const Table t = table_of(r[0], data);
+        const int32_t* lengths = counts(r[1], t.B, data, "the length of each sequence, int32, expected");
+        const at::Tensor& w = tensor(r[2]);
+        if (!w.is_cuda() || w.scalar_type() != at::kFloat || w.dim() != 3 || w.size(0) != t.B || w.size(1) != c.heads || w.numel() == 0)
+            mismatch("weights float32 [sequences, heads, entries] expected");
+        if (w.size(2) > 1 && w.stride(2) != 1) mismatch("weights with contiguous entries expected");
+        same_device(w, data);
+        no_gradient_attention(w);
+        const int N = small(w.size(2)), keep = integer(r[3]), recent = integer(r[4]);
+        const int64_t w_head = w.size(1) > 1 ? w.stride(1) : N, w_sequence = w.size(0) > 1 ? w.stride(0) : 0;
+        if (keep < 1 || recent < 0 || recent > keep) mismatch("at least one entry to keep, and no more of the newest than that, expected");
+        Table into{};
+        if (r[5] != Py_None) {
+            into = table_of(r[5], data);
+            if (into.B != t.B) mismatch("a row of pages for each sequence expected");
+            if (static_cast<int64_t>(into.width) * c.page < std::min({static_cast<int64_t>(keep), static_cast<int64_t>(N), static_cast<int64_t>(t.width) * c.page}))
+                mismatch("pages for all that stays expected");
+        }
+        const at::Tensor lengths_out = fresh({t.B}, at::kInt, data), weights_out = fresh({t.B, c.heads, N}, at::kFloat, data), kept = fresh({t.B, c.heads, keep}, at::kInt, data);
+        const size_t bytes = bs_kv4_evict_workspace_bytes(&c, t.B, keep, into.pages != nullptr);
+        at::Tensor ws;
+        if (bytes) ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, data);
+        int rc;
+        on.keep({a[0], r[0], r[1], r[2], r[5]});
+        {
+            NoGil free;
+            rc = bs_kv4_evict(&c, t.pages, t.pitch, t.width, into.pages, into.pitch, into.width, t.B, lengths, static_cast<const float*>(w.const_data_ptr()), w_sequence, w_head < N ? N : w_head, N,
+                              keep, recent, static_cast<int32_t*>(lengths_out.data_ptr()), static_cast<float*>(weights_out.data_ptr()), static_cast<int32_t*>(kept.data_ptr()),
+                              bytes ? ws.data_ptr() : nullptr, bytes, on.stream);
+        }
+        return Py_BuildValue("(iNNN)", rc, give(lengths_out), give(weights_out), give(kept));
+    });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(conv2d), FAST(gemm), FAST(bitpack), FAST(bitpack_operands), FAST(sequence_run), FAST(unchanged),
-                         FAST(w4_quantise), FAST(w4_prepare), FAST(w4_gemm), FAST(w4_moe), {nullptr, nullptr, 0, nullptr}};
+                         FAST(w4_quantise), FAST(w4_prepare), FAST(w4_gemm), FAST(w4_moe),
+                         FAST(kv4_append), FAST(kv4_read), FAST(kv4_attend), FAST(kv4_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

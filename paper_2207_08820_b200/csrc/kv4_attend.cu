@@ -1,0 +1,727 @@
+// Attention of the newest tokens of each sequence over its entries in a cache of 4-bit keys and values: o = softmax(scale q K^T) V, one token or a few.
+//
+// Codes less 8 are exact in fp16 and are what the tensor cores multiply (mma.sync; eight rows of queries cost what one does): with c the codes, s and m a
+// group's step and offset, a score is the sum over its groups of s (q . (c - 8)) + (m + 8 s) sum(q), scaled in 32 bits; the keys are never rounded.
+// An output is the sum over entries of (p s)(c - 8), p s as two fp16 terms under a common power of two, plus the sum of p (m + 8 s), in 32 bits.
+//
+// A warp takes 64 entries at a time, in one piece where the page allows, through two buffers of its own in shared memory, and keeps the running maximum, sum
+// and outputs of eight or sixteen rows (query tokens times the heads that share keys) in registers.  Four warps of a CTA share a run of entries; the
+// sequences are cut into runs of equal length for the whole grid, which every CTA finds by itself from the lengths; a second kernel joins runs.
+#include "kv4.h"
+#include "mma_kernel.cuh"
+#include "w4_dot.cuh"
+
+namespace bs {
+namespace {
+
+constexpr int WARPS = 4, STAGES = 2, UNIT = 4;          // tiles of 16 entries that a warp takes at a time
+constexpr int LEAST = 8;                                // tiles of a run, at least
+
+struct Attend {
+    Kv4 l;
+    Kv4Table t;
+    const int32_t* lengths;
+    const int32_t* starts;      // null: one row of q a sequence
+    const void* q;
+    long long q_token, q_head;
+    int T, Hq, per;             // rows of q, its heads, how many share a head of the cache
+    float scale;                // times log2(e)
+    void* out;                  // [T][Hq][D]
+    float* part;                // [runs][R][D], and behind them
+    float2* stat;               // [runs][R] maximum and sum
+    int4* info;                 // [B] first run, runs of a column, columns, tiles of rows
+    float* scores;              // [T][Hq][N], where weights are wanted
+    float* lse;                 // [T][Hq]
+    float* weights;
+    long long w_sequence, w_head;
+    int N;
+    int target;                 // runs that fill the GPU
+    int* status;
+};
+
+// Sequence b: entries, query tokens, tiles of entries and of rows.
+struct Seq {
+    int n, first, tq, tiles, rts;
+    __device__ __forceinline__ Seq(const Attend& a, const int32_t* lengths, const int32_t* starts, int b, int R)
+    {
+        const long long room = min(static_cast<long long>(a.t.width) * a.l.page, 0x7fffff00LL);
+        n = lengths[b];
+        n = n < 0 ? 0 : n > room ? static_cast<int>(room) : n;
+        first = b;
+        tq = 1;
+        if (starts) {
+            first = min(max(starts[b], 0), a.T);
+            tq = min(max(starts[b + 1], first), a.T) - first;
+        }
+        tiles = (n + KV4_TILE - 1) / KV4_TILE;
+        rts = static_cast<int>((static_cast<long long>(tq) * a.per + R - 1) / R);
+    }
+};
+
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// Nibbles i and i + 4 of x, less 8, as pairs of fp16.
+__device__ __forceinline__ void expand(uint32_t x, uint32_t (&v)[4])
+{
+    const uint32_t y = x >> 8, base = 0x64006400u, low = 0x64086408u, sixteenth = 0x2c002c00u, high = 0xd480d480u;     // 1024 + 8; -(64 + 8)
+    const uint32_t u[4] = {(x & 0x000f000fu) | base, (x & 0x00f000f0u) | base, (y & 0x000f000fu) | base, (y & 0x00f000f0u) | base};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __half2 h = *reinterpret_cast<const __half2*>(&u[i]);
+        const __half2 d = i & 1 ? __hfma2(h, *reinterpret_cast<const __half2*>(&sixteenth), *reinterpret_cast<const __half2*>(&high))
+                                : __hsub2(h, *reinterpret_cast<const __half2*>(&low));
+        v[i] = *reinterpret_cast<const uint32_t*>(&d);
+    }
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi)
+{
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <int W> __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t (&w)[W])
+{
+    if constexpr (W == 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (W == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+    }
+}
+// The D / 32 pieces of two bytes of a part of a values' row.
+template <int C> __device__ __forceinline__ void load_pieces(const unsigned char* p, uint32_t (&w)[C])
+{
+    if constexpr (C == 4) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x; w[1] = v.x >> 16; w[2] = v.y; w[3] = v.y >> 16;
+    } else if constexpr (C == 2) {
+        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+        w[0] = v; w[1] = v >> 16;
+    } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) w[i] = reinterpret_cast<const uint16_t*>(p)[i];
+    }
+}
+
+template <bool F16, int D, int G, int NT>
+__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel(const __grid_constant__ Attend a)
+{
+    typedef W4Type<F16> Ty;
+    typedef W4Type<true> Half;
+    constexpr int R = 8 * NT, BLOCKS = D / 32, MT = D / 16, TILE = KV4_TILE * (D + 8 * G), PER_G = BLOCKS / G;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ uint64_t bars[WARPS][STAGES];
+    __shared__ float2 stat[WARPS][R];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tid = lane & 3;
+    if (lane == 0) {
+        for (int s = 0; s < STAGES; ++s) mbar_init(&bars[warp][s], 1);
+        fence_barrier_init();
+        fence_proxy_async();
+    }
+    __syncwarp();
+    dependent_begin(a.t.pages);
+    const int32_t *lengths = behind_wait<int32_t>(a.lengths), *starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr, *table = behind_wait<int32_t>(a.t.pages);
+
+    // the run that this CTA takes: its sequence, head, tile of rows and tiles of entries
+    int b = 0, runs = 1, run = 0, column = 0, base = 0;
+    {
+        long long all = 0;
+        for (int i = lane; i < a.t.B; i += 32) {
+            const Seq s(a, lengths, starts, i, R);
+            all += static_cast<long long>(s.tiles) * s.rts * a.l.H;
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
+        const int chunk = static_cast<int>(min(max((all + a.target - 1) / a.target, static_cast<long long>(LEAST)), 1LL << 30));
+        int before = 0;
+        bool found = false;
+        for (int i0 = 0; i0 < a.t.B && !found; i0 += 32) {
+            int n = 0, r = 1, c = 1;
+            if (i0 + lane < a.t.B) {
+                const Seq s(a, lengths, starts, i0 + lane, R);
+                r = max(1, (s.tiles + chunk - 1) / chunk);
+                c = s.rts * a.l.H;
+                n = r * c;
+            }
+            int sum = n;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, sum, d);
+                if (lane >= d) sum += v;
+            }
+            const int from = before + sum - n;
+            const unsigned here = __ballot_sync(0xffffffffu, static_cast<int>(blockIdx.x) >= from && static_cast<int>(blockIdx.x) < from + n);
+            if (here) {
+                const int who = __ffs(here) - 1;
+                b = i0 + who;
+                runs = __shfl_sync(0xffffffffu, r, who);
+                base = __shfl_sync(0xffffffffu, from, who);
+                c = __shfl_sync(0xffffffffu, c, who);
+                run = (blockIdx.x - base) / c;
+                column = (blockIdx.x - base) - run * c;
+                found = true;
+            }
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (!found) return;
+    }
+    const Seq s(a, lengths, starts, b, R);
+    const int h = column % a.l.H, r0 = column / a.l.H * R, rows = s.tq * a.per;
+    if (column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
+
+    // how many entries a row sees; rows behind the last one see all and are dropped
+    int limit[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r0 + n * 8 + 2 * tid + i;
+            limit[n][i] = r < rows ? s.n - s.tq + r / a.per + 1 : s.n;
+        }
+    const int least = s.n - s.tq + r0 / a.per + 1;                             // entries that all rows see
+    const int most = s.n - s.tq + min(rows - 1, r0 + R - 1) / a.per + 1;       // and that any row sees
+    const int tiles = max(0, (min(most, s.n) + KV4_TILE - 1) / KV4_TILE);
+    const int t0 = min(tiles, static_cast<int>(static_cast<long long>(s.tiles) * run / runs)), t1 = min(tiles, static_cast<int>(static_cast<long long>(s.tiles) * (run + 1) / runs));
+    const int unit = min(UNIT, max(1, (t1 - t0 + WARPS - 1) / WARPS));
+    const int units = (t1 - t0 + unit - 1) / unit, mine = units > warp ? (units - warp + WARPS - 1) / WARPS : 0;
+
+    // copies ahead: lane 4 i + j looks up the page of tile j of the warp's unit i, eight units at a time
+    unsigned char* ring = smem + warp * STAGES * UNIT * TILE;
+    const int in_page = a.l.page / KV4_TILE;
+    int page = -1;
+    unsigned there = 0, flags = 0;          // which of the eight units' tiles have a page; the same of the stages, four bits each
+    auto issue = [&](int k) {
+        if ((k & 7) == 0) {
+            const int t = t0 + (warp + WARPS * (k + (lane >> 2))) * unit + (lane & 3);
+            page = -1;
+            if ((lane & 3) < unit && t < t1) page = table[b * a.t.pitch + t / in_page];
+            if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.l.pages)) page = -1;
+            there = __ballot_sync(0xffffffffu, page >= 0);
+        }
+        const int stage = k % STAGES, f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
+        flags = (flags & ~(15u << 4 * stage)) | (there >> 4 * (k & 7) & 15u) << 4 * stage;
+        if (lane == 0) mbar_expect_tx(&bars[warp][stage], count * TILE);
+        __syncwarp();
+        const int j = lane & 3, t = f + j;
+        if ((lane >> 2) == (k & 7) && j < count && (j == 0 || t % in_page == 0)) {
+            const int len = min(count - j, in_page - t % in_page);
+            const unsigned char* from = a.l.data + max(page, 0) * a.l.whole + h * a.l.head + static_cast<long long>(t % in_page) * TILE;
+            mm_bulk(ring + (stage * UNIT + j) * TILE, from, len * TILE, &bars[warp][stage]);
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k)
+        if (k < mine) issue(k);
+
+    // queries as fragments: row gid of each tile, the channels in the order of the keys' words.  bf16 is brought into fp16's range by a power of two, exactly but for
+    // values below 2^-27 of the row's largest, which keep an error of 2^-38 of it
+    uint32_t qf[NT][BLOCKS * 2][2];
+    float factor[NT][2], qsum[G][NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = r0 + n * 8 + gid;
+        uint4 raw[BLOCKS];
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) raw[k] = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+            const uint16_t* q = behind_wait<uint16_t>(a.q) + (s.first + r / a.per) * a.q_token + (h * a.per + r % a.per) * a.q_head + 8 * tid;
+#pragma unroll
+            for (int k = 0; k < BLOCKS; ++k) raw[k] = *reinterpret_cast<const uint4*>(q + 32 * k);
+        }
+        float up = 1.f, down = 1.f;
+        if (!F16) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int k = 0; k < BLOCKS; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t w = word_of(raw[k], j);
+                    big = max(big, max(w & 0x7f80u, w >> 16 & 0x7f80u));
+                }
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+            const int e = min(max(static_cast<int>(big >> 7) - 127, -112), 126);       // the largest value's exponent becomes 13
+            up = __uint_as_float(static_cast<uint32_t>(127 + 13 - e) << 23);
+            down = __uint_as_float(static_cast<uint32_t>(127 - 13 + e) << 23);
+        }
+        float sums[G];
+#pragma unroll
+        for (int g = 0; g < G; ++g) sums[g] = 0.f;
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[2 * j] = Ty::lo(word_of(raw[k], j)) * up;
+                x[2 * j + 1] = Ty::hi(word_of(raw[k], j)) * up;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[k / PER_G] += x[j];
+            qf[n][2 * k][0] = half2_of(x[0], x[4]);
+            qf[n][2 * k][1] = half2_of(x[1], x[5]);
+            qf[n][2 * k + 1][0] = half2_of(x[2], x[6]);
+            qf[n][2 * k + 1][1] = half2_of(x[3], x[7]);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 1);
+            sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 2);
+        }
+        // from the rows' lanes to the columns'
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int from = 4 * (2 * tid + i);
+            factor[n][i] = __shfl_sync(0xffffffffu, down, from) * a.scale;
+#pragma unroll
+            for (int g = 0; g < G; ++g) qsum[g][n][i] = __shfl_sync(0xffffffffu, sums[g], from);
+        }
+    }
+
+    float o[MT][NT][4], offs[G][NT][2], top[NT][2], total[NT][2];
+    int power = -126;           // outputs are in units of 2^power
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            top[n][i] = -INFINITY;
+            total[n][i] = 0.f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) offs[g][n][i] = 0.f;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) o[m][n][i] = o[m][n][2 + i] = 0.f;
+        }
+    const int place[2] = {(gid >> 1) + 4 * (gid & 1), (gid >> 1) + 4 * (gid & 1) + 8};     // entries of rows gid and gid + 8 of a fragment
+    bool late = false;
+
+    auto take = [&](int k, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit) * KV4_TILE, count = min(unit, t1 - first / KV4_TILE);
+        const unsigned flag = flags >> 4 * stage & 15u;
+        const unsigned char* unit_at = ring + stage * UNIT * TILE;
+        float p[UNIT][NT][4], high[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
+        float step_top = 0.f;
+#pragma unroll
+        for (int t = 0; t < UNIT; ++t) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) p[t][n][0] = p[t][n][1] = p[t][n][2] = p[t][n][3] = -INFINITY;
+            if (t >= count) continue;
+            const unsigned char* tile = unit_at + t * TILE;
+            uint32_t key[2][BLOCKS], step[2][G];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                load_words(tile + kv4_key_row(place[i]) * (D / 2) + tid * (D / 8), key[i]);
+                load_words(tile + KV4_TILE * D + place[i] * (4 * G), step[i]);
+            }
+            float sum[NT][4];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                float acc[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+#pragma unroll
+                for (int k2 = g * PER_G; k2 < (g + 1) * PER_G; ++k2) {
+                    uint32_t x[4], y[4];
+                    expand(key[0][k2], x);
+                    expand(key[1][k2], y);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        Half::mma(acc[n], x[0], y[0], x[1], y[1], qf[n][2 * k2][0], qf[n][2 * k2][1]);
+                        Half::mma(acc[n], x[2], y[2], x[3], y[3], qf[n][2 * k2 + 1][0], qf[n][2 * k2 + 1][1]);
+                    }
+                }
+                const float s0 = Ty::lo(step[0][g]), s1 = Ty::lo(step[1][g]), m0 = fmaf(8.f, s0, Ty::hi(step[0][g])), m1 = fmaf(8.f, s1, Ty::hi(step[1][g]));
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float c0 = m0 * qsum[g][n][i], c1 = m1 * qsum[g][n][i];
+                        sum[n][i] = g == 0 ? fmaf(acc[n][i], s0, c0) : sum[n][i] + fmaf(acc[n][i], s0, c0);
+                        sum[n][2 + i] = g == 0 ? fmaf(acc[n][2 + i], s1, c1) : sum[n][2 + i] + fmaf(acc[n][2 + i], s1, c1);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v = sum[n][i] * factor[n][i & 1];
+                    if (MASKED && (first + t * KV4_TILE + place[i >> 1] >= limit[n][i & 1] || !(flag >> t & 1))) v = -INFINITY;
+                    p[t][n][i] = v;
+                    high[n][i & 1] = fmaxf(high[n][i & 1], v);
+                }
+            // the largest step of the values, for the common power of two
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t vs[G];
+                load_words(tile + KV4_TILE * D + 64 * G + place[i] * (4 * G), vs);
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && (flag >> t & 1))) step_top = fmaxf(step_top, Ty::lo(vs[g]));
+            }
+        }
+        if (a.scores) {
+#pragma unroll
+            for (int t = 0; t < UNIT; ++t)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = r0 + n * 8 + 2 * tid + (i & 1), e = first + t * KV4_TILE + place[i >> 1];
+                        if (t < count && r < rows && e < a.N)
+                            a.scores[(static_cast<long long>(s.first + r / a.per) * a.Hq + h * a.per + r % a.per) * a.N + e] = p[t][n][i];
+                    }
+        }
+        // the running maximum, and what is there so far brought to it
+        const int power_new = max(power, static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(step_top)) >> 23) - 126);
+        float fall[NT][2];
+        bool same = power_new == power;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float v = high[n][i];
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+                v = fmaxf(v, top[n][i]);
+                same &= v == top[n][i];
+                fall[n][i] = v == -INFINITY ? 1.f : exp2_of(top[n][i] - v);
+                top[n][i] = v;
+            }
+        if (!__all_sync(0xffffffffu, same)) {
+            const float less = __uint_as_float(static_cast<uint32_t>(max(127 + power - power_new, 0)) << 23);
+            power = power_new;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    total[n][i] *= fall[n][i];
+#pragma unroll
+                    for (int g = 0; g < G; ++g) offs[g][n][i] *= fall[n][i];
+                    const float f = fall[n][i] * less;
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        o[m][n][i] *= f;
+                        o[m][n][2 + i] *= f;
+                    }
+                }
+        }
+        const float scaled = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
+#pragma unroll
+        for (int t = 0; t < UNIT; ++t) {
+            if (t >= count) continue;
+            const unsigned char* tile = unit_at + t * TILE;
+            uint32_t step[2][G], word[4][BLOCKS];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) load_words(tile + KV4_TILE * D + 64 * G + place[i] * (4 * G), step[i]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_pieces(tile + KV4_TILE * (D / 2) + (tid + 4 * i) * (D / 2) + kv4_value_part(D, tid + 4 * i, gid) * (D / 16), word[i]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float base_of = top[n][i & 1] == -INFINITY ? 0.f : top[n][i & 1];
+                    p[t][n][i] = exp2_of(p[t][n][i] - base_of);
+                    total[n][i & 1] += p[t][n][i];
+                }
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float st = Ty::lo(step[i][g]), off = fmaf(8.f, st, Ty::hi(step[i][g]));
+                    const int e = first + t * KV4_TILE + place[i];
+                    if (MASKED && (e >= s.n || !(flag >> t & 1))) st = off = 0.f;
+                    st *= scaled;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        const float p0 = p[t][n][2 * i], p1 = p[t][n][2 * i + 1], w0 = p0 * st, w1 = p1 * st;
+                        offs[g][n][0] = MASKED && e >= limit[n][0] ? offs[g][n][0] : fmaf(p0, off, offs[g][n][0]);
+                        offs[g][n][1] = MASKED && e >= limit[n][1] ? offs[g][n][1] : fmaf(p1, off, offs[g][n][1]);
+                        const uint32_t w = half2_of(w0, w1);
+                        hi[n][i] = transposed(w);
+                        lo[n][i] = transposed(half2_of(w0 - Half::lo(w), w1 - Half::hi(w)));
+                    }
+                }
+#pragma unroll
+                for (int c = g * PER_G; c < (g + 1) * PER_G; ++c) {
+                    uint32_t x[4], y[4];
+                    expand(__byte_perm(word[0][c], word[1][c], 0x5410), x);
+                    expand(__byte_perm(word[2][c], word[3][c], 0x5410), y);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], hi[n][0], hi[n][1]);
+                        Half::mma(o[2 * c + 1][n], x[2], x[3], y[2], y[3], hi[n][0], hi[n][1]);
+                        Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], lo[n][0], lo[n][1]);
+                        Half::mma(o[2 * c + 1][n], x[2], x[3], y[2], y[3], lo[n][0], lo[n][1]);
+                    }
+                }
+            }
+        }
+    };
+    for (int k = 0; k < mine; ++k) {
+        const int stage = k % STAGES;
+        if (!late && !mm_wait(&bars[warp][stage], k / STAGES & 1)) {
+            late = true;
+            atomicOr(a.status, STATUS_TIMEOUT);
+        }
+        const int f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
+        const unsigned whole = (1u << count) - 1u;
+        if ((f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, std::integral_constant<bool, false>());
+        else take(k, std::integral_constant<bool, true>());
+        __syncwarp();
+        if (k + STAGES < mine) issue(k + STAGES);
+    }
+
+    // the warps' parts: rows of outputs [R][D], put together in the ring's memory
+    __syncthreads();
+    float* outs = reinterpret_cast<float*>(smem);
+    constexpr int PITCH = D + 4;
+    const float back = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) {
+                total[n][i] += __shfl_xor_sync(0xffffffffu, total[n][i], d);
+#pragma unroll
+                for (int g = 0; g < G; ++g) offs[g][n][i] += __shfl_xor_sync(0xffffffffu, offs[g][n][i], d);
+            }
+            const int r = n * 8 + 2 * tid + i;
+            if (gid == 0) stat[warp][r] = make_float2(top[n][i], total[n][i]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                outs[(warp * R + r) * PITCH + 16 * m + gid] = fmaf(o[m][n][i], back, offs[m / (2 * PER_G)][n][i]);
+                outs[(warp * R + r) * PITCH + 16 * m + gid + 8] = fmaf(o[m][n][2 + i], back, offs[m / (2 * PER_G)][n][i]);
+            }
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < R * (D / 4); i += WARPS * 32) {
+        const int r = i / (D / 4), d = i % (D / 4) * 4, row = r0 + r;
+        float m = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, stat[w][r].x);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float f = stat[w][r].x == -INFINITY ? 0.f : exp2_of(stat[w][r].x - m);
+            const float4 x = *reinterpret_cast<const float4*>(outs + (w * R + r) * PITCH + d);
+            if (stat[w][r].x == -INFINITY && stat[w][r].y == 0.f) continue;        // saw nothing
+            sum = fmaf(stat[w][r].y, f, sum);
+            v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+        }
+        if (row >= rows) continue;
+        if (runs == 1) {
+            const long long at = static_cast<long long>(s.first + row / a.per) * a.Hq + h * a.per + row % a.per;
+            const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+            uint32_t* to = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D + d);
+            *reinterpret_cast<uint2*>(to) = make_uint2(Ty::round2(v.x * inverse, v.y * inverse), Ty::round2(v.z * inverse, v.w * inverse));
+            if (a.scores && d == 0) a.lse[at] = sum == 0.f ? INFINITY : m + log2f(sum);
+        } else {
+            *reinterpret_cast<float4*>(a.part + (static_cast<long long>(blockIdx.x) * R + r) * D + d) = v;
+            if (d == 0) a.stat[static_cast<long long>(blockIdx.x) * R + r] = make_float2(m, sum);
+        }
+    }
+}
+
+// Joins the runs of each row that was cut: a CTA a row of q and head, its warps every fourth run.
+template <bool F16, int D>
+__global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ Attend a, int R, int all)
+{
+    typedef W4Type<F16> Ty;
+    __shared__ float4 outs[WARPS][D / 4];
+    __shared__ float2 stat[WARPS];
+    dependent_begin(a.out);
+    const int32_t* starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr;
+    const int t = blockIdx.x, b = kv4_sequence_of(starts, a.t.B, t), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (starts && (t < starts[b] || t >= starts[b + 1])) return;
+    const int i = starts ? t - max(starts[b], 0) : 0;
+    const int4 info = *behind_wait<int4>(a.info + b);
+    if (info.y <= 1) return;            // whole already
+    const int hq = blockIdx.y, h = hq / a.per, row = i * a.per + hq % a.per, r = row % R;
+    const long long first = info.x + static_cast<long long>(row / R) * a.l.H + h;
+    // starts in disorder may leave a sequence without its runs
+    if (info.x < 0 || info.z <= 0 || first + (info.y - 1LL) * info.z >= all) return;
+    const float2* stats = behind_wait<float2>(a.stat);
+    const float* part = behind_wait<float>(a.part);
+    float m = -INFINITY;
+    for (int k = lane; k < info.y; k += 32) m = fmaxf(m, stats[(first + static_cast<long long>(k) * info.z) * R + r].x);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+    const bool live = lane < D / 4;
+#pragma unroll 8
+    for (int k = warp; k < info.y; k += WARPS) {
+        const long long at = (first + static_cast<long long>(k) * info.z) * R + r;
+        const float2 st = stats[at];
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (live) x = *reinterpret_cast<const float4*>(part + at * D + 4 * lane);
+        const bool empty = st.x == -INFINITY && st.y == 0.f;
+        const float f = empty ? 0.f : exp2_of(st.x - m);
+        sum = fmaf(st.y, f, sum);
+        v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
+    }
+    if (live) outs[warp][lane] = v;
+    if (lane == 0) stat[warp].y = sum;
+    __syncthreads();
+    if (warp > 0) return;
+    sum = stat[0].y + stat[1].y + stat[2].y + stat[3].y;
+    const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+    const long long at = static_cast<long long>(t) * a.Hq + hq;
+    if (live) {
+        v = outs[0][lane];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) { v.x += outs[w][lane].x; v.y += outs[w][lane].y; v.z += outs[w][lane].z; v.w += outs[w][lane].w; }
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * D + 4 * lane) =
+            make_uint2(Ty::round2(v.x * inverse, v.y * inverse), Ty::round2(v.z * inverse, v.w * inverse));
+    }
+    if (a.scores && lane == 0) a.lse[at] = sum == 0.f ? INFINITY : m + log2f(sum);
+}
+
+// What each entry got: the sum over the rows that share its head of exp2(score - lse), rows in their order.
+__global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant__ Attend a)
+{
+    dependent_begin(a.weights);
+    const int32_t *lengths = behind_wait<int32_t>(a.lengths), *starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr;
+    const int h = blockIdx.y;
+    for (int b = blockIdx.z; b < a.t.B; b += gridDim.z) {
+        const Seq s(a, lengths, starts, b, 8);
+        const int n = min(s.n, a.N);
+        const float* lse = behind_wait<float>(a.lse);
+        const float* scores = behind_wait<float>(a.scores);
+        for (int e = blockIdx.x * 256 + threadIdx.x; e < n; e += gridDim.x * 256) {
+            float w = 0.f;
+            for (int i = max(0, e - (s.n - s.tq)); i < s.tq; ++i) {        // query tokens that see it
+                const long long row = static_cast<long long>(s.first + i) * a.Hq + h * a.per;
+#pragma unroll 4
+                for (int j = 0; j < a.per; ++j) w += exp2_of(scores[(row + j) * a.N + e] - lse[row + j]);
+            }
+            a.weights[b * a.w_sequence + h * a.w_head + e] += w;
+        }
+    }
+}
+
+// Tiles of rows and runs that a call may have, and its workspace.
+struct Plan {
+    int NT, target;
+    long long runs;
+    size_t part, stat, info, lse, scores;
+    size_t bytes() const { return part + stat + info + lse + scores; }
+};
+bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int N, int sms, Plan& p)
+{
+    const int per = Hq / l.H;
+    const long long rows = starts ? ceil_div_ll(T, B) * per : per;
+    p.NT = rows > 8 ? 2 : 1;
+    const int R = 8 * p.NT;
+    p.target = sms * 12;
+    const long long columns = starts ? l.H * (ceil_div_ll(static_cast<long long>(T) * per, R) + B) : static_cast<long long>(l.H) * B * ceil_div(per, R);
+    p.runs = columns + p.target;
+    if (p.runs > 0x7fffffff / (R * 2)) return false;
+    auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };
+    p.part = up(p.runs * R * l.D * 4);
+    p.stat = up(p.runs * R * 8);
+    p.info = up(static_cast<long long>(B) * 16);
+    p.lse = N > 0 ? up(static_cast<long long>(T) * Hq * 4) : 0;
+    p.scores = N > 0 ? up(static_cast<long long>(T) * Hq * N * 4) : 0;
+    return true;
+}
+
+template <bool F16, int D, int G, int NT>
+int launch(const Attend& a, const Plan& p, cudaStream_t st)
+{
+    auto kernel = kv4_attend_kernel<F16, D, G, NT>;
+    constexpr int ring = WARPS * STAGES * UNIT * KV4_TILE * (D + 8 * G), parts = WARPS * 8 * NT * (D + 4) * 4, smem = ring > parts ? ring : parts;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
+    return launch_dependent(kernel, dim3(static_cast<unsigned>(p.runs)), dim3(WARPS * 32), smem, st, a);
+}
+template <bool F16, int D, int G>
+int launch_rows(const Attend& a, const Plan& p, cudaStream_t st) { return p.NT == 1 ? launch<F16, D, G, 1>(a, p, st) : launch<F16, D, G, 2>(a, p, st); }
+template <bool F16>
+int launch_form(const Attend& a, const Plan& p, cudaStream_t st)
+{
+    int rc;
+    if (a.l.D == 64) rc = a.l.G == 1 ? launch_rows<F16, 64, 1>(a, p, st) : launch_rows<F16, 64, 2>(a, p, st);
+    else if (a.l.D == 96) rc = a.l.G == 1 ? launch_rows<F16, 96, 1>(a, p, st) : launch_rows<F16, 96, 3>(a, p, st);
+    else rc = a.l.G == 1 ? launch_rows<F16, 128, 1>(a, p, st) : a.l.G == 2 ? launch_rows<F16, 128, 2>(a, p, st) : launch_rows<F16, 128, 4>(a, p, st);
+    if (rc != BS_OK) return rc;
+    // no sequence is cut where none can be longer than a run
+    if (static_cast<long long>(a.t.width) * a.l.page > LEAST * KV4_TILE) {
+        const dim3 grid(a.T, a.Hq);
+        rc = a.l.D == 64 ? launch_dependent(kv4_join_kernel<F16, 64>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
+             : a.l.D == 96 ? launch_dependent(kv4_join_kernel<F16, 96>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
+                           : launch_dependent(kv4_join_kernel<F16, 128>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs));
+    }
+    if (rc == BS_OK && a.weights) {
+        const int chunks = ceil_div(a.N, 256);
+        rc = launch_dependent(kv4_weights_kernel, dim3(chunks < 65535 ? chunks : 65535, a.l.H, a.t.B < 65535 ? a.t.B : 65535), dim3(256), 0, st, a);
+    }
+    return rc;
+}
+
+}  // namespace
+}  // namespace bs
+
+using namespace bs;
+
+extern "C" size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int N)
+{
+    Kv4 l;
+    Plan p;
+    const int sms = device_sm_count();
+    if (!cache || B <= 0 || T < 0 || N < 0 || q_heads <= 0 || !kv4_layout(*cache, l) || q_heads % l.H != 0 || sms <= 0 || !plan(l, B, T, q_heads, starts != 0, N, sms, p)) return 0;
+    return p.bytes();
+}
+
+extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int q_heads, const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width,
+                             int B, const int32_t* lengths, const int32_t* starts, float scale, void* out, float* weights, long long weights_sequence, long long weights_head, int N,
+                             void* workspace, size_t workspace_bytes, void* stream)
+{
+    Attend a{};
+    if (!q || !cache || !cache->data || !table || !lengths || !out || !workspace || T < 0 || B <= 0 || width <= 0 || table_pitch < width || q_token < 0 || q_head < 0) return BS_ERR_INVALID_ARG;
+    if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
+    if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0 || q_heads <= 0 || q_heads % cache->heads != 0) return BS_ERR_INVALID_ARG;
+    if (!(scale > 0.f) || !(scale < INFINITY) || (!starts && T != B)) return BS_ERR_INVALID_ARG;
+    if (weights && (N <= 0 || weights_head < N || weights_sequence < 0)) return BS_ERR_INVALID_ARG;
+    if (!kv4_layout(*cache, a.l) || q_heads > 65535) return BS_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(cache->data) || !aligned16(out) || !aligned16(workspace) || (q_token | q_head) % 8 != 0) return BS_ERR_ALIGNMENT;
+    if (T == 0) return BS_OK;
+    const int sms = device_sm_count();
+    a.status = status_device_ptr();
+    if (sms <= 0 || !a.status) return BS_ERR_CUDA;
+    Plan p;
+    if (!plan(a.l, B, T, q_heads, starts != nullptr, weights ? N : 0, sms, p)) return BS_ERR_UNSUPPORTED;
+    if (workspace_bytes < p.bytes()) return BS_ERR_INVALID_ARG;
+    a.t = {table, table_pitch, width, B};
+    a.lengths = lengths; a.starts = starts;
+    a.q = q; a.q_token = q_token; a.q_head = q_head;
+    a.T = T; a.Hq = q_heads; a.per = q_heads / a.l.H;
+    a.scale = scale * 1.4426950408889634f;
+    a.out = out;
+    char* ws = static_cast<char*>(workspace);
+    a.part = reinterpret_cast<float*>(ws);
+    a.stat = reinterpret_cast<float2*>(ws += p.part);
+    a.info = reinterpret_cast<int4*>(ws += p.stat);
+    if (weights) {
+        a.lse = reinterpret_cast<float*>(ws += p.info);
+        a.scores = reinterpret_cast<float*>(ws += p.lse);
+        a.weights = weights; a.w_sequence = weights_sequence; a.w_head = weights_head; a.N = N;
+    }
+    a.target = p.target;
+    return cache->type == BS_F16 ? launch_form<true>(a, p, static_cast<cudaStream_t>(stream)) : launch_form<false>(a, p, static_cast<cudaStream_t>(stream));
+}

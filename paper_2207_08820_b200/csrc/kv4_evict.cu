@@ -1,0 +1,250 @@
+// Eviction from a cache of 4-bit keys and values: every head keeps its newest entries and, of the others, those that got most attention, in their order.
+//
+// A cluster of eight CTAs takes a head of a sequence.  The least weight that stays is found by its digits, 11, 11 and 10 bits from the top of a key whose order as
+// a whole number is that of the weights: each CTA counts its part of the entries by digit in shared memory, and all read one another's counts.  Entries above
+// it stay, of those equal to it the first ones.  A second pass over the entries writes the indices, ranked by sums over warps and CTAs.  What stays is then
+// moved by a kernel over all heads and sequences: into other pages at once, into their own through a copy, since what one CTA writes another may still have to read.
+#include "kv4.h"
+#include "mma_kernel.cuh"
+#include "w4_dot.cuh"
+
+namespace bs {
+namespace {
+
+constexpr int CTAS = 8, THREADS = 512, BINS = 2048;
+
+struct Evict {
+    Kv4 l;
+    Kv4Table from, into;
+    const int32_t* lengths;
+    const float* weights;
+    long long w_sequence, w_head;
+    int N, keep, recent;
+    int32_t* lengths_out;       // [B]
+    float* weights_out;         // [B][H][N]
+    int32_t* kept;              // [B][H][keep]
+    unsigned char* copy;        // [B][H][ceil(keep / 16)] tiles, for moves within a sequence's own pages
+};
+
+__device__ __forceinline__ uint32_t key_of(float w)
+{
+    if (w != w) return 0xffffffffu;         // NaN comes first
+    const uint32_t u = __float_as_uint(w + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ uint32_t remote(uint32_t addr, int rank)
+{
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ int entries_of(const Evict& a, const int32_t* lengths, int b)
+{
+    const long long room = min(static_cast<long long>(a.from.width) * a.l.page, static_cast<long long>(a.N));
+    const int n = lengths[b];
+    return n < 0 ? 0 : n > room ? static_cast<int>(room) : n;
+}
+// Sum over the threads before this one; all: over all of them.
+__device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* sums, uint32_t& all)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t s = v;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, s, d);
+        if (lane >= d) s += u;
+    }
+    if (lane == 31) sums[warp] = s;
+    __syncthreads();
+    uint32_t front = 0;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const uint32_t u = sums[w];
+        if (w < warp) front += u;
+        all += u;
+    }
+    __syncthreads();
+    return front + s - v;
+}
+
+__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(THREADS) kv4_select_kernel(const __grid_constant__ Evict a)
+{
+    __shared__ uint32_t bins[3][BINS], sums[THREADS / 32], found[2], mine[2];
+    dependent_begin(a.kept);
+    const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z, th = threadIdx.x;
+    const int n = entries_of(a, behind_wait<int32_t>(a.lengths), b);
+    const float* w = behind_wait<float>(a.weights) + b * a.w_sequence + h * a.w_head;
+    const long long head = static_cast<long long>(b) * a.l.H + h;
+    int32_t* kept = a.kept + head * a.keep;
+    float* out = a.weights_out + head * a.N;
+    const int stay = min(n, a.keep), old = n > a.keep ? n - a.recent : 0, need = n > a.keep ? a.keep - a.recent : 0;
+    const int from = static_cast<int>(static_cast<long long>(old) * rank / CTAS), to = static_cast<int>(static_cast<long long>(old) * (rank + 1) / CTAS);
+    if (need > 0) {
+        for (int i = th; i < 3 * BINS; i += THREADS) (&bins[0][0])[i] = 0;
+        __syncthreads();
+        uint32_t prefix = 0, left = need;           // digits found; how many entries of that prefix stay
+#pragma unroll
+        for (int pass = 0; pass < 3; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, wide = pass == 2 ? 10 : 11;
+            for (int i = from + th; i < to; i += THREADS) {
+                const uint32_t k = key_of(w[i]);
+                if (pass == 0 || k >> (shift + wide) == prefix) atomicAdd(&bins[pass][k >> shift & ((1u << wide) - 1)], 1u);
+            }
+            mm_cluster_sync();
+            // four digits a thread, from the top down
+            uint32_t count[4], sum = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int digit = BINS - 1 - (4 * th + j);
+                count[j] = 0;
+#pragma unroll
+                for (int c = 0; c < CTAS; ++c) count[j] += remote(smem_u32(&bins[pass][digit]), c);
+                sum += count[j];
+            }
+            uint32_t all, above = before_me(sum, sums, all);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (above < left && left <= above + count[j]) { found[0] = BINS - 1 - (4 * th + j); found[1] = left - above; }
+                above += count[j];
+            }
+            __syncthreads();
+            prefix = prefix << wide | found[0];
+            left = found[1];
+            __syncthreads();
+        }
+        // `left` entries equal to `prefix` stay, and all above it
+        uint32_t more = 0, equal = 0;
+        for (int i = from + th; i < to; i += THREADS) {
+            const uint32_t k = key_of(w[i]);
+            more += k > prefix;
+            equal += k == prefix;
+        }
+        uint32_t all_more, all_equal;
+        before_me(more, sums, all_more);
+        before_me(equal, sums, all_equal);
+        if (th == 0) { mine[0] = all_more; mine[1] = all_equal; }
+        mm_cluster_sync();
+        uint32_t at_more = 0, at_equal = 0;
+        for (int c = 0; c < rank; ++c) {
+            at_more += remote(smem_u32(&mine[0]), c);
+            at_equal += remote(smem_u32(&mine[1]), c);
+        }
+        mm_cluster_sync();          // nobody leaves while its memory is read
+        for (int i0 = from; i0 < to; i0 += THREADS) {
+            const int i = i0 + th;
+            const float v = i < to ? w[i] : 0.f;
+            const uint32_t k = i < to ? key_of(v) : 0, is_more = i < to && k > prefix, is_equal = i < to && k == prefix;
+            uint32_t all;
+            const uint32_t front = before_me(is_more | is_equal << 16, sums, all), e = at_equal + (front >> 16), place = at_more + (front & 0xffff) + min(e, left);
+            if (is_more || (is_equal && e < left)) {
+                kept[place] = i;
+                out[place] = v;
+            }
+            at_more += all & 0xffff;
+            at_equal += all >> 16;
+        }
+    }
+    // the newest ones (all of them where nothing goes), and what is behind
+    for (int i = need + rank * THREADS + th; i < a.keep; i += CTAS * THREADS) kept[i] = i < stay ? old + i - need : -1;
+    for (int i = need + rank * THREADS + th; i < a.N; i += CTAS * THREADS) out[i] = i < stay ? w[old + i - need] : 0.f;
+    if (h == 0 && rank == 0 && th == 0) a.lengths_out[b] = stay;
+}
+
+// Eight lanes an entry: 16 bytes of keys or values each, then its steps.  STEP 0: into the other table's pages; 1: into the copy; 2: out of it.
+template <int STEP>
+__global__ void __launch_bounds__(256) kv4_move_kernel(const __grid_constant__ Evict a)
+{
+    constexpr int AHEAD = 4, WIDE = 32;       // entries that eight lanes have on their way; of a CTA side by side
+    const int32_t* kept = dependent_begin(a.kept);
+    const int lane = threadIdx.x & 7, h = blockIdx.y, D = a.l.D, half = D / 32, tiles = (a.keep + KV4_TILE - 1) / KV4_TILE;
+    for (int b = blockIdx.z; b < a.from.B; b += gridDim.z) {
+        const int stay = min(entries_of(a, behind_wait<int32_t>(a.lengths), b), a.keep);
+        const long long head = static_cast<long long>(b) * a.l.H + h;
+        unsigned char* copy = STEP == 0 ? nullptr : a.copy + head * tiles * a.l.tile;
+        Kv4Table from = a.from, into = a.into;
+        from.pages = behind_wait<int32_t>(a.from.pages);
+        into.pages = behind_wait<int32_t>(a.into.pages);
+        for (int r0 = blockIdx.x * WIDE * AHEAD + (threadIdx.x >> 3); r0 < stay; r0 += gridDim.x * WIDE * AHEAD) {
+            unsigned char *src[AHEAD], *dst[AHEAD];
+            int es[AHEAD], ed[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int r = r0 + k * WIDE, i = r < stay ? kept[head * a.keep + r] : -1;
+                src[k] = dst[k] = nullptr;
+                es[k] = i & (KV4_TILE - 1);
+                ed[k] = r & (KV4_TILE - 1);
+                if (i < 0 || (STEP > 0 && i == r)) continue;          // in place already
+                const int ps = kv4_page_of(a.l, from, b, i), pd = STEP == 0 ? kv4_page_of(a.l, into, b, r) : kv4_page_of(a.l, from, b, r);
+                if (ps < 0 || pd < 0) continue;
+                unsigned char* held = STEP == 0 ? nullptr : copy + static_cast<long long>(r / KV4_TILE) * a.l.tile;
+                src[k] = STEP == 2 ? held : kv4_tile_of(a.l, ps, h, i & (a.l.page - 1));
+                dst[k] = STEP == 1 ? held : kv4_tile_of(a.l, pd, h, r & (a.l.page - 1));
+                if (STEP == 2) es[k] = ed[k];
+            }
+            uint4 v[AHEAD];
+            uint32_t s[AHEAD];
+            // lanes below half: parts of the keys' row, the next ones of the values'
+            auto part_of = [&](int e) {
+                const int p = lane < half ? lane : lane - half;
+                return lane < half ? kv4_key_row(e) * (D / 2) + 16 * p : KV4_TILE * (D / 2) + e * (D / 2) + 8 * kv4_value_part(D, e, 2 * p);
+            };
+            auto step_of = [&](int e) { return KV4_TILE * D + (lane < a.l.G ? e * a.l.G + lane : (KV4_TILE + e) * a.l.G + lane - a.l.G) * 4; };
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (src[k] && lane < 2 * half) v[k] = *reinterpret_cast<const uint4*>(src[k] + part_of(es[k]));
+                if (src[k] && lane < 2 * a.l.G) s[k] = *reinterpret_cast<const uint32_t*>(src[k] + step_of(es[k]));
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                if (dst[k] && lane < 2 * half) *reinterpret_cast<uint4*>(dst[k] + part_of(ed[k])) = v[k];
+                if (dst[k] && lane < 2 * a.l.G) *reinterpret_cast<uint32_t*>(dst[k] + step_of(ed[k])) = s[k];
+            }
+        }
+    }
+}
+
+}  // namespace
+}  // namespace bs
+
+using namespace bs;
+
+extern "C" size_t bs_kv4_evict_workspace_bytes(const bs_kv4_cache* cache, int B, int keep, int into)
+{
+    Kv4 l;
+    if (!cache || B <= 0 || keep <= 0 || !kv4_layout(*cache, l)) return 0;
+    return into ? 0 : static_cast<size_t>(B) * l.H * ceil_div(keep, KV4_TILE) * l.tile;
+}
+
+extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width, const int32_t* into, long long into_pitch, int into_width, int B,
+                            const int32_t* lengths, const float* weights, long long weights_sequence, long long weights_head, int N, int keep, int recent, int32_t* lengths_out,
+                            float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream)
+{
+    Evict a{};
+    if (!cache || !cache->data || !table || !lengths || !weights || !lengths_out || !weights_out || !kept || B <= 0 || width <= 0 || table_pitch < width) return BS_ERR_INVALID_ARG;
+    if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
+    if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0) return BS_ERR_INVALID_ARG;
+    if (N <= 0 || keep <= 0 || recent < 0 || recent > keep || weights_head < N || weights_sequence < 0) return BS_ERR_INVALID_ARG;
+    if (into && (into_width <= 0 || into_pitch < into_width)) return BS_ERR_INVALID_ARG;
+    if (!kv4_layout(*cache, a.l) || B > 65535) return BS_ERR_UNSUPPORTED;
+    const long long most = static_cast<long long>(width) * a.l.page < N ? static_cast<long long>(width) * a.l.page : N, stays = keep < most ? keep : most;
+    if (into && static_cast<long long>(into_width) * a.l.page < stays) return BS_ERR_INVALID_ARG;
+    const size_t need = bs_kv4_evict_workspace_bytes(cache, B, keep, into != nullptr);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return BS_ERR_INVALID_ARG;
+    if (!aligned16(cache->data) || !aligned16(workspace)) return BS_ERR_ALIGNMENT;
+    a.from = {table, table_pitch, width, B};
+    a.into = into ? Kv4Table{into, into_pitch, into_width, B} : a.from;
+    a.lengths = lengths; a.weights = weights; a.w_sequence = weights_sequence; a.w_head = weights_head;
+    a.N = N; a.keep = keep; a.recent = recent;
+    a.lengths_out = lengths_out; a.weights_out = weights_out; a.kept = kept;
+    a.copy = static_cast<unsigned char*>(workspace);
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int rc = launch_dependent(kv4_select_kernel, dim3(CTAS, a.l.H, B), dim3(THREADS), 0, st, a);
+    if (rc != BS_OK) return rc;
+    const long long chunks = ceil_div_ll(stays, 128);
+    const dim3 grid(static_cast<unsigned>(chunks < 4096 ? chunks : 4096), a.l.H, B);
+    if (into) return launch_dependent(kv4_move_kernel<0>, grid, dim3(256), 0, st, a);
+    rc = launch_dependent(kv4_move_kernel<1>, grid, dim3(256), 0, st, a);
+    return rc == BS_OK ? launch_dependent(kv4_move_kernel<2>, grid, dim3(256), 0, st, a) : rc;
+}
