@@ -549,6 +549,20 @@ int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long tabl
                  int32_t* lengths_out, float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * bs_attend_prompt -- attention of whole prompts over their keys and values of 16 bits, packed.
+ *   q        device, T rows of q_heads vectors of D values, strides as above;  k, v  device, Tk rows of `heads` vectors; q_heads a multiple of heads
+ *   starts   rows of q of each of B sequences, starts_k their rows of k and v (both device int32 [B + 1], or both NULL: one sequence of all rows, B = 1)
+ *   causal   row i of n rows of q over m keys sees the keys below m - n + i + 1; else all of them.  A row that sees nothing gives zeros.
+ *   out      device [T][q_heads][D] of the type (BS_F16 or BS_BF16): softmax(scale q k^T) v, scale > 0
+ * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k.  Scores, softmax and sums have 32 bits; weights are rounded to the type before they meet
+ * the values.  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
+ * its rows that do not see it.  The same call gives the same bits every time.
+ */
+int bs_attend_prompt(const void* q, long long q_token, long long q_head, int T, int q_heads, const void* k, long long k_token, long long k_head, const void* v,
+                     long long v_token, long long v_head, int Tk, int heads, int D, bs_float_t type, int B, const int32_t* starts, const int32_t* starts_k,
+                     float scale, int causal, void* out, void* stream);
+
+/*
  * bs_popc_rate -- register-only micro-benchmark of the SM population-count pipe: every thread runs
  * `iters` rounds of independent  acc += popc(x & y)  chains.  Writes the measured rate in
  * popc32(AND) word-operations per second to *wordops_per_s (HOST pointer).  Synchronises the device.

@@ -10,7 +10,7 @@ import importlib
 _API_NAMES = ("bitpack_activations", "bitunpack_activations", "pack_weights", "bs_pack_rows",
               "bitserial_conv2d", "bitserial_gemm", "bs_check_status", "bs_popc_rate",
               "quantise_w4", "prepare_w4", "gemm_w4", "moe_w4", "W4Weights",
-              "cache_kv4", "append_kv4", "read_kv4", "attend_kv4", "evict_kv4", "KV4Cache",
+              "cache_kv4", "append_kv4", "read_kv4", "attend_kv4", "evict_kv4", "attend_prompt", "KV4Cache",
               "UNSIGNED", "SIGNED", "BIPOLAR", "NCHW", "NHWC")
 
 

@@ -202,6 +202,8 @@ def lib() -> ctypes.CDLL:
     L.bs_kv4_evict_workspace_bytes.argtypes = [cache, i, i, i]
     L.bs_kv4_evict.restype = i
     L.bs_kv4_evict.argtypes = [cache, vp, ll, i, vp, ll, i, i, vp, vp, ll, ll, i, i, i, vp, vp, vp, vp, sz, vp]
+    L.bs_attend_prompt.restype = i
+    L.bs_attend_prompt.argtypes = [vp, ll, ll, i, i, vp, ll, ll, vp, ll, ll, i, i, i, i, i, vp, vp, ctypes.c_float, i, vp, vp]
     L.bs_popc_rate.restype = i
     L.bs_popc_rate.argtypes = [i, ctypes.POINTER(ctypes.c_double)]
     L.bs_status_string.restype = ctypes.c_char_p
@@ -218,4 +220,4 @@ EXPORTED = ("bs_packed_act_bytes", "bs_packed_wgt_bytes", "bs_packed_rows_bytes"
             "bs_conv2d_f32", "bs_maxpool2d_f32", "bs_stem_codes_f32", "bs_stem_codes_supported", "bs_avgpool_codes_f32", "bs_fc_f32",
             "bs_check_status", "bs_quantiser_bounds", "bs_requant_bounds", "bs_selftest_wait_timeout", "bs_popc_rate", "bs_status_string",
             "bs_w4_quantise", "bs_w4_bytes", "bs_w4_prepare", "bs_w4_gemm_workspace_bytes", "bs_w4_gemm", "bs_w4_moe_workspace_bytes", "bs_w4_moe",
-            "bs_kv4_page_bytes", "bs_kv4_append", "bs_kv4_read", "bs_kv4_attend_workspace_bytes", "bs_kv4_attend", "bs_kv4_evict_workspace_bytes", "bs_kv4_evict")
+            "bs_kv4_page_bytes", "bs_kv4_append", "bs_kv4_read", "bs_kv4_attend_workspace_bytes", "bs_kv4_attend", "bs_kv4_evict_workspace_bytes", "bs_kv4_evict", "bs_attend_prompt")

@@ -472,6 +472,20 @@ def evict_kv4(cache: KV4Cache, table: torch.Tensor, lengths: torch.Tensor, weigh
     return n, w, kept
 
 
+def attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, starts_k: Optional[torch.Tensor] = None, *, causal: bool = True,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Attention of whole prompts (``bs_attend_prompt``): q [T, q_heads, D], k and v [Tk, heads, D], float16 or bfloat16, sequences one behind the other as ``starts`` and
+    ``starts_k`` (int32 [sequences + 1]; None: those of q) say, or a single one.  Causal: the last row of q sees all keys, each one before it one fewer.
+    Tokens and heads may be apart.  Rows that no sequence holds are not written.  No gradients."""
+    global launch_count
+    if starts is not None and starts_k is None:
+        starts_k = starts
+    st, o = native().attend_prompt(q, k, v, starts, starts_k, q.shape[-1] ** -0.5 if scale is None else scale, causal, out, stream)
+    _check(st, "bs_attend_prompt")
+    launch_count += 1
+    return o
+
+
 def bs_check_status(stream=None) -> None:
     st = lib().bs_check_status(_stream_ptr(stream))
     if st != 0:

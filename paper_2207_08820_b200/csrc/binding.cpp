@@ -786,10 +786,62 @@ PyObject* kv4_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
     });
 }
 
+// q, k, v, starts or None, starts_k or None, scale, causal, out or None, stream
+PyObject* attend_prompt(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return guarded([&] {
+        need(n, 9);
+        const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]), &v = tensor(a[2]);
+        for (int i : {0, 1, 2}) no_gradient_attention(tensor(a[i]));
+        const OnStream on(q, a[8]);
+        if (q.dim() != 3 || k.dim() != 3) mismatch("queries and keys [tokens, heads, channels] expected");
+        const bs_float_t type = float_type(q);
+        if (type == BS_F32) mismatch("float16 or bfloat16 expected");
+        const int64_t D = q.size(2);
+        const Vectors qv = vectors(q, type, -1, D, q, "queries [tokens, heads, channels] expected"), kv = vectors(k, type, -1, D, q, "keys of the queries' type and channels expected"),
+                      vv = vectors(v, type, k.size(1), D, q, "values of the keys' heads, and of the queries' type and channels, expected");
+        if (k.size(0) != v.size(0)) mismatch("as many keys as values expected");
+        const int T = small(q.size(0)), Tk = small(k.size(0)), heads = small(k.size(1)), q_heads = small(q.size(1));
+        if (heads == 0 || q_heads == 0 || q_heads % heads != 0) mismatch("heads of q that are a multiple of the keys' expected");
+        const bool packed = a[3] != Py_None;
+        if (packed != (a[4] != Py_None)) mismatch("starts of queries and of keys, or neither, expected");
+        const int32_t *starts = nullptr, *starts_k = nullptr;
+        int B = 1;
+        if (packed) {
+            if (tensor(a[3]).dim() != 1 || tensor(a[3]).size(0) < 2) mismatch("the starts of all sequences and the end, int32, expected");
+            B = small(tensor(a[3]).size(0) - 1);
+            starts = counts(a[3], B + 1LL, q, "the starts of all sequences and the end, int32, expected");
+            starts_k = counts(a[4], B + 1LL, q, "the starts of all sequences and the end, int32, expected");
+        }
+        const float scale = real(a[5]);
+        const int causal = PyObject_IsTrue(a[6]);
+        at::Tensor out;
+        if (a[7] != Py_None) {
+            out = tensor(a[7]);
+            if (out.scalar_type() != q.scalar_type() || out.sizes() != q.sizes()) mismatch("an output of q's type and shape expected");
+            same_device(out, q);
+            no_gradient_attention(out);
+            if (out.numel() > 0) pointer(out);
+            if (meet(out, q) || meet(out, k) || meet(out, v)) mismatch("the output overlaps an input");
+        } else {
+            out = fresh(q.sizes(), q.scalar_type(), q);
+        }
+        if (T == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(out));
+        int rc;
+        on.keep({a[0], a[1], a[2], a[3], a[4], a[7]});
+        {
+            NoGil free;
+            rc = bs_attend_prompt(qv.p, qv.token, qv.head, T, q_heads, Tk ? kv.p : qv.p, kv.token, kv.head, Tk ? vv.p : qv.p, vv.token, vv.head, Tk, heads, static_cast<int>(D), type, B, starts,
+                                  starts_k, scale, causal, out.data_ptr(), on.stream);
+        }
+        return Py_BuildValue("(iN)", rc, give(out));
+    });
+}
+
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(conv2d), FAST(gemm), FAST(bitpack), FAST(bitpack_operands), FAST(sequence_run), FAST(unchanged),
                          FAST(w4_quantise), FAST(w4_prepare), FAST(w4_gemm), FAST(w4_moe),
-                         FAST(kv4_append), FAST(kv4_read), FAST(kv4_attend), FAST(kv4_evict), {nullptr, nullptr, 0, nullptr}};
+                         FAST(kv4_append), FAST(kv4_read), FAST(kv4_attend), FAST(kv4_evict), FAST(attend_prompt), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

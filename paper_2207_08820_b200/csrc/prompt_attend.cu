@@ -1,0 +1,461 @@
+// Attention of whole prompts over 16-bit keys and values, packed, causal or not, with heads of queries that share keys: o = softmax(scale q k^T) v on tcgen05.
+//
+// A tile is 128 rows of queries, row r of it token r / G and head r % G of the G that share a head of keys, so that short prompts fill tiles too.  A CTA, one
+// per SM, takes two neighbouring tiles over the same keys, 128 at a time from the last ones that either sees: scores of both in tensor memory (a row a
+// lane), two groups of four warps that turn a row's scores into weights, a row a thread, and write them over the scores as 16-bit operands of the
+// second product, whose sums stay in tensor memory as well.  While one tile's weights are made the tensor core works for the other.
+//
+// Weights are relative to a maximum that is replaced only when the row's has grown by more than 2^8: sums then have room for it in 32 bits, and the outputs
+// are seldom rescaled.  Scores, maxima, sums and outputs have 32 bits; weights are rounded to the type of the values, which is what multiplies them.
+#include <cuda.h>
+
+#include <mutex>
+
+#include "kv4.h"
+#include "mma_kernel.cuh"
+#include "w4_dot.cuh"
+
+namespace bs {
+namespace {
+
+constexpr int ROWS = 128, KEYS = 128;
+// Warps that make weights, with most of the registers, and a group of four of which one copies and one issues MMAs: 384 threads of 168 registers become 256 of 216
+// and 128 of 72.
+constexpr int SOFTMAX = 8, THREADS = (SOFTMAX + 4) * 32;
+
+struct Prompt {
+    const int32_t* starts;      // null: one sequence of all rows
+    const int32_t* starts_k;
+    int B, T, Tk, Hq, H, D, G;
+    int tokens;                 // of a tile
+    int causal;
+    float scale;                // times log2(e)
+    void* out;                  // [T][Hq][D]
+    int* status;
+};
+
+// What a CTA does: two tiles of a sequence and head.
+struct Work {
+    int q0, nq, k0, nk;         // rows of the sequence
+    int h, token;               // first token of the first tile
+    int blocks[2];              // of keys that a tile sees, 0 without rows
+};
+
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float exp2_of(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+struct Rows { int q0, nq, k0, nk, pairs; };
+__device__ __forceinline__ Rows rows_of(const Prompt& a, const int32_t* starts, const int32_t* starts_k, int b)
+{
+    Rows s{0, a.T, 0, a.Tk, 0};
+    if (starts) {
+        s.q0 = min(max(starts[b], 0), a.T);
+        s.nq = min(max(starts[b + 1], s.q0), a.T) - s.q0;
+        s.k0 = min(max(starts_k[b], 0), a.Tk);
+        s.nk = min(max(starts_k[b + 1], s.k0), a.Tk) - s.k0;
+    }
+    s.pairs = (s.nq + 2 * a.tokens - 1) / (2 * a.tokens);
+    return s;
+}
+// Blocks of keys that the tokens before `end` of a sequence see.
+__device__ __forceinline__ int blocks_of(const Prompt& a, const Rows& s, int end)
+{
+    const int seen = a.causal ? s.nk - s.nq + min(end, s.nq) : s.nk;
+    return seen <= 0 ? 0 : (seen + KEYS - 1) / KEYS;
+}
+// The n-th pair of tiles of all sequences, sequences in their order, a sequence's last tiles first.  By one warp; false: there is none.
+__device__ __forceinline__ bool find(const Prompt& a, const int32_t* starts, const int32_t* starts_k, int n, Work& w)
+{
+    const int lane = threadIdx.x & 31;
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        Rows s{0, 0, 0, 0, 0};
+        if (b0 + lane < a.B) s = rows_of(a, starts, starts_k, b0 + lane);
+        int sum = s.pairs;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, d);
+            if (lane >= d) sum += v;
+        }
+        const unsigned here = __ballot_sync(0xffffffffu, n >= before + sum - s.pairs && n < before + sum);
+        if (here) {
+            const int who = __ffs(here) - 1, pair = s.pairs - 1 - (n - (before + sum - s.pairs));
+            w.q0 = s.q0; w.nq = s.nq; w.k0 = s.k0; w.nk = s.nk;
+            w.token = pair * 2 * a.tokens;
+            for (int t = 0; t < 2; ++t) w.blocks[t] = w.token + t * a.tokens < s.nq ? blocks_of(a, s, w.token + (t + 1) * a.tokens) : 0;
+            int* v = &w.q0;
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(Work) / 4); ++i) v[i] = __shfl_sync(0xffffffffu, v[i], who);
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+}
+
+// D [128 x n] = A (shared memory) B^T (shared memory): 64 channels, rows of 128 bytes, swizzled: four steps of 32 bytes, under one elect in one statement.
+#define PROMPT_SS(P) "@p tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, " P ";\n\t"
+#define PROMPT_NEXT "add.s64 a, a, 2;\n\tadd.s64 b, b, 2;\n\t"
+__device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\t"
+        "setp.ne.b32 q, %4, 0;\n\tmov.b64 a, %1;\n\tmov.b64 b, %2;\n\telect.sync _|p, 0xffffffff;\n\t"
+        PROMPT_SS("q") PROMPT_NEXT PROMPT_SS("1") PROMPT_NEXT PROMPT_SS("1") PROMPT_NEXT PROMPT_SS("1") "}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+// D [128 x n] (+)= A (tensor memory) B (shared memory, channels side by side): 128 keys, eight steps of 16.
+#define PROMPT_TS(P) "@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, " P ";\n\t"
+#define PROMPT_STEP "add.u32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t" PROMPT_TS("1")
+__device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
+        "setp.ne.b32 q, %4, 0;\n\tmov.b32 a, %1;\n\tmov.b64 b, %2;\n\telect.sync _|p, 0xffffffff;\n\t"
+        PROMPT_TS("q") PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP "}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+
+// HALVES: of 64 channels.  Tensor memory: scores (and weights over them) of both tiles, outputs of both.
+template <bool F16, int HALVES>
+__global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+                                                                   const __grid_constant__ Prompt a)
+{
+    typedef W4Type<F16> Ty;
+    constexpr int HALF = ROWS * 128, TILE = HALVES * HALF, RING = HALVES == 2 ? 5 : 8, N = HALVES * 64;
+    extern __shared__ unsigned char raw[];
+    // queries of the tiles, then the ring of keys and values, all in rows of 128 bytes swizzled by address: from a multiple of 1024 on
+    unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
+    __shared__ uint64_t q_full, full[RING], empty[RING], s_full[2], p_full[2], o_full[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ Work work;
+    __shared__ int any;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (warp == SOFTMAX) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        mm_fence_before();
+    } else if (warp == 0 && lane == 0) {
+        mbar_init(&q_full, 1);
+        for (int s = 0; s < RING; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 4); mbar_init(&o_full[t], 1); }
+        fence_barrier_init();
+        fence_proxy_async();
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tq)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tk)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tv)) : "memory");
+    }
+    __syncthreads();
+    mm_fence_after();
+    const uint32_t tmem = tmem_slot;
+    dependent_begin(a.out);
+    if (warp == 0) {
+        Work w{};
+        const bool there = find(a, a.starts ? behind_wait<int32_t>(a.starts) : nullptr, a.starts ? behind_wait<int32_t>(a.starts_k) : nullptr, blockIdx.x / a.H, w);
+        if (lane == 0) {
+            w.h = blockIdx.x % a.H;
+            work = w;
+            any = there;
+        }
+    }
+    __syncthreads();
+    Work w = work;
+    if (!any) w.blocks[0] = w.blocks[1] = w.nq = 0;         // nothing to do, and no rows
+    const int n0 = w.blocks[0], n1 = w.blocks[1], most = max(n0, n1);
+    auto blocks_in = [&](int t) { return t == 0 ? n0 : n1; };
+    bool late = false;
+    auto wait = [&](uint64_t* bar, unsigned parity) {
+        if (!late && !mm_wait(bar, parity)) {
+            late = true;
+            atomicOr(a.status, STATUS_TIMEOUT);
+        }
+    };
+    if (warp >= SOFTMAX) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;" ::: "memory");
+        if (warp == SOFTMAX) {
+            unsigned limit = 1u << 20;
+            if (most > 0) {
+                if (mm_elect()) {
+                    const int bytes = 128 * a.G * a.tokens;        // rows that no tile has keep what the memory holds: they meet nothing
+                    mbar_expect_tx(&q_full, 2 * HALVES * bytes);
+                    for (int t = 0; t < 2; ++t)
+                        for (int i = 0; i < HALVES; ++i) tma_load_3d(smem + t * TILE + i * HALF, &tq, &q_full, 64 * i, w.h * a.G, w.q0 + w.token + t * a.tokens);
+                }
+                int at = 0;
+                unsigned phase = 1;
+                for (int j = 2 * most - 1; j >= 0; --j) {           // keys, then values, of each block
+                    mm_wait_uniform(&empty[at], phase, limit);
+                    if (mm_elect()) {
+                        unsigned char* to = smem + (2 + at) * TILE;
+                        mbar_expect_tx(&full[at], TILE);
+                        for (int i = 0; i < HALVES; ++i) tma_load_3d(to + i * HALF, j & 1 ? &tk : &tv, &full[at], 64 * i, w.h, w.k0 + (j >> 1) * KEYS);
+                    }
+                    if (++at == RING) { at = 0; phase ^= 1; }
+                }
+                if (limit == 1 && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+                // no copy outlives the CTA, whatever else was waited for
+                limit = 1u << 20;
+                mm_wait_uniform(&q_full, 0, limit);
+                for (int i = 0; i < RING && i < 2 * most; ++i) {
+                    at = at == 0 ? RING - 1 : at - 1;
+                    if (at == RING - 1) phase ^= 1;
+                    mm_wait_uniform(&full[at], phase ^ 1, limit);
+                }
+            }
+        } else if (warp == SOFTMAX + 1) {
+            unsigned limit = 1u << 20;
+            const uint32_t type = F16 ? 0u : (1u << 7) | (1u << 10);
+            const uint32_t score_desc = (1u << 4) | type | (KEYS >> 3) << 17 | (ROWS >> 4) << 24;
+            const uint32_t value_desc = (1u << 4) | type | (1u << 16) | (N >> 3) << 17 | (ROWS >> 4) << 24;      // B with its columns side by side
+            const uint32_t base = (smem_u32(smem) & 0x3ffff) >> 4;
+            // rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group; of the values, whose rows are the reduction, HALF from 64 channels to the next
+            const uint64_t major = static_cast<uint64_t>(64u | (1u << 14) | (2u << 29)) << 32;
+            auto scores = [&](int t, int stage) {
+                for (int i = 0; i < HALVES; ++i)
+                    mma_scores(tmem + t * 128, major | 1u << 16 | (base + (t * TILE + i * HALF) / 16), major | 1u << 16 | (base + ((2 + stage) * TILE + i * HALF) / 16), score_desc, i);
+            };
+            int at = 0;
+            unsigned phase = 0, p_phase[2] = {0, 0};
+            auto next = [&] { if (++at == RING) { at = 0; phase ^= 1; } };
+            if (most > 0) {
+                mm_wait_uniform(&q_full, 0, limit);
+                mm_wait_uniform(&full[at], phase, limit);
+                mm_fence_after();
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+                    if (most - 1 < blocks_in(t)) {
+                        scores(t, at);
+                        mm_commit(&s_full[t]);
+                    }
+                mm_commit(&empty[at]);
+                next();
+            }
+            for (int j = most - 1; j >= 0; --j) {
+                const int v = at;
+                mm_wait_uniform(&full[v], phase, limit);
+                const int left = w.nk - j * KEYS;
+                if (left < KEYS) {      // rows behind the sequence's last one may hold anything, which zero weights would not keep out
+                    for (int i = left * 128 + lane * 16; i < HALF; i += 512)
+                        for (int k = 0; k < HALVES; ++k) *reinterpret_cast<uint4*>(smem + (2 + v) * TILE + k * HALF + i) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                next();
+                const int k = at;
+                if (j > 0) mm_wait_uniform(&full[k], phase, limit);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (j < blocks_in(t)) {
+                        mm_wait_uniform(&p_full[t], p_phase[t], limit);
+                        p_phase[t] ^= 1;
+                        mm_fence_after();
+                        mma_values(tmem + 256 + t * 128, tmem + t * 128, major | static_cast<uint64_t>(HALF / 16) << 16 | (base + (2 + v) * TILE / 16), value_desc, j != blocks_in(t) - 1);
+                        if (j == 0) mm_commit(&o_full[t]);
+                    }
+                    if (j > 0 && j - 1 < blocks_in(t)) {
+                        scores(t, k);
+                        mm_commit(&s_full[t]);
+                    }
+                }
+                mm_commit(&empty[v]);
+                if (j > 0) {
+                    mm_commit(&empty[k]);
+                    next();
+                }
+            }
+            if (limit == 1 && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+            limit = 1u << 20;           // nor do the MMAs outlive the tensor memory
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                if (blocks_in(t) > 0) mm_wait_uniform(&o_full[t], 0, limit);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;" ::: "memory");
+        const int t = warp >> 2, row = (warp & 3) * 32 + lane, blocks = blocks_in(t);
+        const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+        const int first = w.token + t * a.tokens, token = first + row / a.G;
+        const int seen = a.causal ? min(w.nk - w.nq + token + 1, w.nk) : w.nk;                 // keys that the row sees
+        const int all = a.causal ? w.nk - w.nq + first + 1 : w.nk;                             // and that all rows of the tile see
+        float top = -INFINITY, total = 0.f;
+        for (int j = blocks - 1; j >= 0; --j) {
+            wait(&s_full[t], (blocks - 1 - j) & 1);
+            mm_fence_after();
+            uint32_t v[4][32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mm_ld32(s_at + 32 * i, v[i]);
+            mm_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mm_landed(v[i]);
+            if ((j + 1) * KEYS > all || (j + 1) * KEYS > w.nk) {
+                const int left = seen - j * KEYS;
+#pragma unroll
+                for (int i = 0; i < 128; ++i)
+                    if (i >= left) v[i / 32][i % 32] = 0xff800000u;
+            }
+            float high[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                high[i] = __uint_as_float(v[i][0]);
+#pragma unroll
+                for (int k = 1; k < 31; k += 2) high[i] = max3(high[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
+                high[i] = fmaxf(high[i], __uint_as_float(v[i][31]));
+            }
+            const float now = fmaxf(max3(high[0], high[1], high[2]), high[3]);
+            const bool grown = (now - top) * a.scale > 8.f || (top == -INFINITY && now > -INFINITY);
+            if (__any_sync(0xffffffffu, grown)) {
+                const float to = grown ? now : top, f = grown ? exp2_of((top - to) * a.scale) : 1.f;
+                top = to;
+                total *= f;
+                if (j != blocks - 1) {      // the outputs so far: the scores' barrier says that their last product is done
+#pragma unroll
+                    for (int i = 0; i < N; i += 32) {
+                        uint32_t o[32];
+                        mm_ld32(o_at + i, o);
+                        mm_ld_wait();
+                        mm_landed(o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                        mm_st16(o_at + i, o);
+                        mm_st16(o_at + i + 16, o + 16);
+                    }
+                }
+            }
+            const float base_of = top == -INFINITY ? 0.f : -top * a.scale;
+            const u64 scale2 = f2_pack(__float_as_uint(a.scale), __float_as_uint(a.scale)), base2 = f2_pack(__float_as_uint(base_of), __float_as_uint(base_of));
+            u64 sums[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t p[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    uint32_t lo, hi;
+                    f2_split(f2_fma(f2_pack(v[i][2 * k], v[i][2 * k + 1]), scale2, base2), lo, hi);
+                    const float x = exp2_of(__uint_as_float(lo)), y = exp2_of(__uint_as_float(hi));
+                    sums[k & 3] = f2_add(sums[k & 3], f2_pack(__float_as_uint(x), __float_as_uint(y)));
+                    p[k] = Ty::round2(x, y);
+                }
+                mm_st16(s_at + 16 * i, p);
+            }
+            mm_st_wait();
+            mm_fence_before();
+            __syncwarp();
+            if (lane == 0) mm_arrive(&p_full[t]);
+            uint32_t lo, hi;
+            f2_split(f2_add(f2_add(sums[0], sums[1]), f2_add(sums[2], sums[3])), lo, hi);
+            total += __uint_as_float(lo) + __uint_as_float(hi);
+        }
+        const bool live = row < a.tokens * a.G && token < w.nq;
+        uint16_t* out = static_cast<uint16_t*>(a.out) + (static_cast<long long>(w.q0 + token) * a.Hq + w.h * a.G + row % a.G) * a.D;
+        if (blocks > 0) {
+            wait(&o_full[t], 0);
+            mm_fence_after();
+        }
+        const float inverse = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int i = 0; i < N; i += 32) {
+            uint32_t o[32];
+            if (blocks > 0) {
+                mm_ld32(o_at + i, o);
+                mm_ld_wait();
+                mm_landed(o);
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 8) {
+                uint32_t p[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+                    p[m] = total == 0.f ? 0u : Ty::round2(__uint_as_float(o[k + 2 * m]) * inverse, __uint_as_float(o[k + 2 * m + 1]) * inverse);
+                if (live && i + k < a.D) *reinterpret_cast<uint4*>(out + i + k) = make_uint4(p[0], p[1], p[2], p[3]);
+            }
+        }
+        mm_fence_before();
+    }
+    __syncthreads();
+    if (warp == SOFTMAX) {
+        mm_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn()
+{
+    static EncodeFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* q = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &q, cudaEnableDefault, &r) == cudaSuccess && r == cudaDriverEntryPointSuccess) fn = reinterpret_cast<EncodeFn>(q);
+    });
+    return fn;
+}
+// Vectors [n][heads][D], fetched in boxes of 64 channels, `wide` heads and `high` rows.  A single row or head may be any distance from the next.
+bool encode(CUtensorMap* tm, const void* p, bool f16, int n, int heads, int D, long long token, long long head, int wide, int high)
+{
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(D), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(n)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(heads == 1 ? D : head) * 2, static_cast<cuuint64_t>(n == 1 ? static_cast<long long>(D) * heads : token) * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(wide), static_cast<cuuint32_t>(high)}, es[3] = {1, 1, 1};
+    return fn(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool F16, int HALVES>
+int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Prompt& a, long long ctas, cudaStream_t st)
+{
+    auto kernel = prompt_attend_kernel<F16, HALVES>;
+    constexpr int smem = 1024 + (2 + (HALVES == 2 ? 5 : 8)) * HALVES * ROWS * 128;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
+    return launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), smem, st, tq, tk, tv, a);
+}
+
+}  // namespace
+}  // namespace bs
+
+using namespace bs;
+
+extern "C" int bs_attend_prompt(const void* q, long long q_token, long long q_head, int T, int q_heads, const void* k, long long k_token, long long k_head, const void* v,
+                                long long v_token, long long v_head, int Tk, int heads, int D, bs_float_t type, int B, const int32_t* starts, const int32_t* starts_k, float scale, int causal,
+                                void* out, void* stream)
+{
+    if (!q || !k || !v || !out || T < 0 || Tk < 0 || q_heads <= 0 || heads <= 0 || D <= 0 || q_heads % heads != 0 || B <= 0) return BS_ERR_INVALID_ARG;
+    if ((type != BS_F16 && type != BS_BF16) || !(scale > 0.f) || !(scale < INFINITY)) return BS_ERR_INVALID_ARG;
+    if (q_token < 0 || q_head < 0 || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return BS_ERR_INVALID_ARG;
+    if ((starts == nullptr) != (starts_k == nullptr) || (!starts && B != 1)) return BS_ERR_INVALID_ARG;
+    Prompt a{};
+    a.G = q_heads / heads;
+    if (D > 128 || D % 8 != 0 || a.G > ROWS) return BS_ERR_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (q_token | q_head | k_token | k_head | v_token | v_head) % 8 != 0) return BS_ERR_ALIGNMENT;
+    if (T == 0) return BS_OK;
+    a.starts = starts; a.starts_k = starts_k;
+    a.B = B; a.T = T; a.Tk = Tk; a.Hq = q_heads; a.H = heads; a.D = D;
+    a.tokens = ROWS / a.G;
+    a.causal = causal != 0;
+    a.scale = scale * 1.4426950408889634f;
+    a.out = out;
+    a.status = status_device_ptr();
+    if (!a.status) return BS_ERR_CUDA;
+    const long long ctas = (ceil_div_ll(T, 2 * a.tokens) + (B - 1)) * heads;
+    if (ctas > 0x7fffffff) return BS_ERR_UNSUPPORTED;
+    const bool f16 = type == BS_F16;
+    CUtensorMap tq, tk, tv;
+    // without keys nothing is fetched; a map has to have rows all the same
+    const int rows_k = Tk > 0 ? Tk : 1, heads_k = Tk > 0 ? heads : 1;
+    if (!encode(&tq, q, f16, T, q_heads, D, q_token, q_head, a.G, a.tokens) || !encode(&tk, k, f16, rows_k, heads_k, D, k_token, k_head, 1, KEYS) ||
+        !encode(&tv, v, f16, rows_k, heads_k, D, v_token, v_head, 1, KEYS))
+        return BS_ERR_UNSUPPORTED;
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (D <= 64) return f16 ? launch<true, 1>(tq, tk, tv, a, ctas, st) : launch<false, 1>(tq, tk, tv, a, ctas, st);
+    return f16 ? launch<true, 2>(tq, tk, tv, a, ctas, st) : launch<false, 2>(tq, tk, tv, a, ctas, st);
+}
