@@ -528,7 +528,7 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights); two calls that may run at the same time need one each
  * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms; the same call gives the same bits every time.
  */
-size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int N);
+size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int width, int N);
 int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int q_heads, const bs_kv4_cache* cache, const int32_t* table, long long table_pitch,
                   int width, int B, const int32_t* lengths, const int32_t* starts, float scale, void* out, float* weights, long long weights_sequence,
                   long long weights_head, int N, void* workspace, size_t workspace_bytes, void* stream);

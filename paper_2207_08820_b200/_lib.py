@@ -195,7 +195,7 @@ def lib() -> ctypes.CDLL:
     L.bs_kv4_read.restype = i
     L.bs_kv4_read.argtypes = [cache, vp, ll, i, i, vp, vp, i, vp, vp, vp]
     L.bs_kv4_attend_workspace_bytes.restype = sz
-    L.bs_kv4_attend_workspace_bytes.argtypes = [cache, i, i, i, i, i]
+    L.bs_kv4_attend_workspace_bytes.argtypes = [cache, i, i, i, i, i, i]
     L.bs_kv4_attend.restype = i
     L.bs_kv4_attend.argtypes = [vp, ll, ll, i, i, cache, vp, ll, i, i, vp, vp, ctypes.c_float, vp, vp, ll, ll, i, vp, sz, vp]
     L.bs_kv4_evict_workspace_bytes.restype = sz

@@ -729,7 +729,7 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
             out = fresh(q.sizes(), q.scalar_type(), data);
         }
         if (T == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(out));
-        const size_t bytes = bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, N);
+        const size_t bytes = bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, t.width, N);
         if (bytes == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_ERR_UNSUPPORTED), give(out));
         const at::Tensor ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, data);
         void *op = out.data_ptr(), *wsp = ws.data_ptr();

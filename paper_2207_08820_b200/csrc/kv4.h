@@ -18,6 +18,7 @@ constexpr int KV4_TILE = 16;        // entries
 struct Kv4 {
     unsigned char* data;
     int pages, H, D, page, group, G;
+    int log_page;
     int tile;                       // bytes of a tile
     long long head, whole;          // bytes of a head's part of a page, of a page
 };
@@ -30,6 +31,7 @@ inline bool kv4_layout(const bs_kv4_cache& c, Kv4& l)
     if (c.D % c.group != 0 || c.page < KV4_TILE || c.page > 1024 || (c.page & (c.page - 1))) return false;
     l.data = static_cast<unsigned char*>(c.data);
     l.pages = c.pages; l.H = c.heads; l.D = c.D; l.page = c.page; l.group = c.group; l.G = c.D / c.group;
+    for (l.log_page = 4; 1 << l.log_page < c.page; ++l.log_page) {}
     l.tile = KV4_TILE * (c.D + 8 * l.G);
     l.head = static_cast<long long>(c.page / KV4_TILE) * l.tile;
     l.whole = l.head * c.heads;
@@ -49,7 +51,7 @@ __device__ __forceinline__ int kv4_value_part(int D, int r, int g) { return D ==
 // Entry i's page, -1 where there is none.  The caller has i below width * page.
 __device__ __forceinline__ int kv4_page_of(const Kv4& l, const Kv4Table& t, int b, long long i)
 {
-    const int p = t.pages[b * t.pitch + i / l.page];
+    const int p = t.pages[b * t.pitch + (i >> l.log_page)];
     return static_cast<unsigned>(p) < static_cast<unsigned>(l.pages) ? p : -1;
 }
 __device__ __forceinline__ unsigned char* kv4_tile_of(const Kv4& l, int page, int h, int slot)

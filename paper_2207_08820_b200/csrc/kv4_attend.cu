@@ -14,8 +14,17 @@
 namespace bs {
 namespace {
 
-constexpr int WARPS = 4, STAGES = 2, UNIT = 4;          // tiles of 16 entries that a warp takes at a time
-constexpr int LEAST = 8;                                // tiles of a run, at least
+#ifndef KV4_UNIT
+#define KV4_UNIT 4
+#define KV4_STAGES 2
+#define KV4_CTAS 3
+#define KV4_LEAST 8
+#endif
+constexpr int WARPS = 4, STAGES = KV4_STAGES, UNIT = KV4_UNIT;          // tiles of 16 entries that a warp takes at a time
+constexpr int LEAST = KV4_LEAST;                        // tiles of a run, at least
+// CTAs of an SM, as registers and shared memory allow.
+template <int D, int G> constexpr int ring_bytes() { return WARPS * STAGES * UNIT * KV4_TILE * (D + 8 * G); }
+constexpr int ctas_of(int ring, int NT) { return (NT == 1 ? KV4_CTAS : 2) < 227 * 1024 / (ring + 2048) ? (NT == 1 ? KV4_CTAS : 2) : 227 * 1024 / (ring + 2048); }
 
 struct Attend {
     Kv4 l;
@@ -35,7 +44,7 @@ struct Attend {
     float* weights;
     long long w_sequence, w_head;
     int N;
-    int target;                 // runs that fill the GPU
+    int slots;                  // CTAs that the GPU holds at a time
     int* status;
 };
 
@@ -57,6 +66,8 @@ struct Seq {
         rts = static_cast<int>((static_cast<long long>(tq) * a.per + R - 1) / R);
     }
 };
+
+__host__ __device__ __forceinline__ long long runs_of(long long columns, int slots) { return max((2 * columns + slots - 1) / slots, 1LL) * slots; }
 
 __device__ __forceinline__ float exp2_of(float x)
 {
@@ -101,23 +112,24 @@ template <int W> __device__ __forceinline__ void load_words(const unsigned char*
         for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
     }
 }
-// The D / 32 pieces of two bytes of a part of a values' row.
-template <int C> __device__ __forceinline__ void load_pieces(const unsigned char* p, uint32_t (&w)[C])
+// The D / 32 pieces of two bytes of a part of a values' row, two a word but for D = 96.
+template <int C> constexpr int words_of = C == 3 ? 3 : C / 2;
+template <int C> __device__ __forceinline__ void load_pieces(const unsigned char* p, uint32_t (&w)[words_of<C>])
 {
-    if constexpr (C == 4) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        w[0] = v.x; w[1] = v.x >> 16; w[2] = v.y; w[3] = v.y >> 16;
-    } else if constexpr (C == 2) {
-        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
-        w[0] = v; w[1] = v >> 16;
-    } else {
+    if constexpr (C == 3) {
 #pragma unroll
         for (int i = 0; i < C; ++i) w[i] = reinterpret_cast<const uint16_t*>(p)[i];
+    } else {
+        load_words(p, w);
     }
+}
+template <int C> __device__ __forceinline__ uint32_t pair_of(const uint32_t (&a)[words_of<C>], const uint32_t (&b)[words_of<C>], int c)
+{
+    return C == 3 ? __byte_perm(a[c], b[c], 0x5410) : __byte_perm(a[c / 2], b[c / 2], c & 1 ? 0x7632 : 0x5410);
 }
 
 template <bool F16, int D, int G, int NT>
-__global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel(const __grid_constant__ Attend a)
+__global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) kv4_attend_kernel(const __grid_constant__ Attend a)
 {
     typedef W4Type<F16> Ty;
     typedef W4Type<true> Half;
@@ -138,14 +150,20 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
     // the run that this CTA takes: its sequence, head, tile of rows and tiles of entries
     int b = 0, runs = 1, run = 0, column = 0, base = 0;
     {
-        long long all = 0;
+        long long all = 0, columns = 0;
         for (int i = lane; i < a.t.B; i += 32) {
             const Seq s(a, lengths, starts, i, R);
             all += static_cast<long long>(s.tiles) * s.rts * a.l.H;
+            columns += s.rts * a.l.H;
         }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) all += __shfl_xor_sync(0xffffffffu, all, d);
-        const int chunk = static_cast<int>(min(max((all + a.target - 1) / a.target, static_cast<long long>(LEAST)), 1LL << 30));
+        for (int d = 16; d; d >>= 1) {
+            all += __shfl_xor_sync(0xffffffffu, all, d);
+            columns += __shfl_xor_sync(0xffffffffu, columns, d);
+        }
+        // as many runs as fill the GPU once, or as often as it takes for half of them to be cuts: every column may end in a short one
+        const long long target = max(runs_of(columns, a.slots) - columns, 1LL);
+        const int chunk = static_cast<int>(min(max((all + target - 1) / target, static_cast<long long>(LEAST)), 1LL << 30));
         int before = 0;
         bool found = false;
         for (int i0 = 0; i0 < a.t.B && !found; i0 += 32) {
@@ -291,7 +309,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
     }
 
     float o[MT][NT][4], offs[G][NT][2], top[NT][2], total[NT][2];
-    int power = -126;           // outputs are in units of 2^power
+    int power = -126;           // outputs are in units of 2^power, above all steps so far
+    float limit_step = 0x1p-126f;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -358,7 +377,7 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float v = sum[n][i] * factor[n][i & 1];
+                    float v = sum[n][i];
                     if (MASKED && (first + t * KV4_TILE + place[i >> 1] >= limit[n][i & 1] || !(flag >> t & 1))) v = -INFINITY;
                     p[t][n][i] = v;
                     high[n][i & 1] = fmaxf(high[n][i & 1], v);
@@ -382,36 +401,34 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
                     for (int i = 0; i < 4; ++i) {
                         const int r = r0 + n * 8 + 2 * tid + (i & 1), e = first + t * KV4_TILE + place[i >> 1];
                         if (t < count && r < rows && e < a.N)
-                            a.scores[(static_cast<long long>(s.first + r / a.per) * a.Hq + h * a.per + r % a.per) * a.N + e] = p[t][n][i];
+                            a.scores[(static_cast<long long>(s.first + r / a.per) * a.Hq + h * a.per + r % a.per) * a.N + e] = p[t][n][i] * factor[n][i & 1];
                     }
         }
-        // the running maximum, and what is there so far brought to it
-        const int power_new = max(power, static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(step_top)) >> 23) - 126);
-        float fall[NT][2];
-        bool same = power_new == power;
+        // weights are relative to a maximum that is replaced, with what is there so far, only when a score is above it by 8 (weights then stay below 2^8) or a
+        // step needs a larger power of two
+        bool grown = step_top > limit_step;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float v = high[n][i];
-#pragma unroll
-                for (int d = 4; d < 32; d *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-                v = fmaxf(v, top[n][i]);
-                same &= v == top[n][i];
-                fall[n][i] = v == -INFINITY ? 1.f : exp2_of(top[n][i] - v);
-                top[n][i] = v;
-            }
-        if (!__all_sync(0xffffffffu, same)) {
+            for (int i = 0; i < 2; ++i) grown |= high[n][i] * factor[n][i] > top[n][i] + 8.f;
+        if (__any_sync(0xffffffffu, grown)) {
+            const int power_new = max(power, static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(step_top)) >> 23) - 126);
             const float less = __uint_as_float(static_cast<uint32_t>(max(127 + power - power_new, 0)) << 23);
             power = power_new;
+            limit_step = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    total[n][i] *= fall[n][i];
+                    float v = high[n][i] * factor[n][i];
 #pragma unroll
-                    for (int g = 0; g < G; ++g) offs[g][n][i] *= fall[n][i];
-                    const float f = fall[n][i] * less;
+                    for (int d = 4; d < 32; d *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+                    v = fmaxf(v, top[n][i]);
+                    const float fall = v == -INFINITY ? 1.f : exp2_of(top[n][i] - v), f = fall * less;
+                    top[n][i] = v;
+                    total[n][i] *= fall;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) offs[g][n][i] *= fall;
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
                         o[m][n][i] *= f;
@@ -424,17 +441,16 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
         for (int t = 0; t < UNIT; ++t) {
             if (t >= count) continue;
             const unsigned char* tile = unit_at + t * TILE;
-            uint32_t step[2][G], word[4][BLOCKS];
+            uint32_t step[2][G], word[4][words_of<BLOCKS>];
 #pragma unroll
             for (int i = 0; i < 2; ++i) load_words(tile + KV4_TILE * D + 64 * G + place[i] * (4 * G), step[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_pieces(tile + KV4_TILE * (D / 2) + (tid + 4 * i) * (D / 2) + kv4_value_part(D, tid + 4 * i, gid) * (D / 16), word[i]);
+            for (int i = 0; i < 4; ++i) load_pieces<BLOCKS>(tile + KV4_TILE * (D / 2) + (tid + 4 * i) * (D / 2) + kv4_value_part(D, tid + 4 * i, gid) * (D / 16), word[i]);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float base_of = top[n][i & 1] == -INFINITY ? 0.f : top[n][i & 1];
-                    p[t][n][i] = exp2_of(p[t][n][i] - base_of);
+                    p[t][n][i] = exp2_of(fmaf(p[t][n][i], factor[n][i & 1], top[n][i & 1] == -INFINITY ? 0.f : -top[n][i & 1]));
                     total[n][i & 1] += p[t][n][i];
                 }
 #pragma unroll
@@ -459,8 +475,8 @@ __global__ void __launch_bounds__(WARPS * 32, NT == 1 ? 3 : 2) kv4_attend_kernel
 #pragma unroll
                 for (int c = g * PER_G; c < (g + 1) * PER_G; ++c) {
                     uint32_t x[4], y[4];
-                    expand(__byte_perm(word[0][c], word[1][c], 0x5410), x);
-                    expand(__byte_perm(word[2][c], word[3][c], 0x5410), y);
+                    expand(pair_of<BLOCKS>(word[0], word[1], c), x);
+                    expand(pair_of<BLOCKS>(word[2], word[3], c), y);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], hi[n][0], hi[n][1]);
@@ -618,20 +634,21 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant_
 
 // Tiles of rows and runs that a call may have, and its workspace.
 struct Plan {
-    int NT, target;
+    int NT, slots;
     long long runs;
     size_t part, stat, info, lse, scores;
     size_t bytes() const { return part + stat + info + lse + scores; }
 };
-bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int N, int sms, Plan& p)
+bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int sms, Plan& p)
 {
     const int per = Hq / l.H;
     const long long rows = starts ? ceil_div_ll(T, B) * per : per;
     p.NT = rows > 8 ? 2 : 1;
     const int R = 8 * p.NT;
-    p.target = sms * 12;
+    p.slots = sms * ctas_of(WARPS * STAGES * UNIT * l.tile, p.NT);
     const long long columns = starts ? l.H * (ceil_div_ll(static_cast<long long>(T) * per, R) + B) : static_cast<long long>(l.H) * B * ceil_div(per, R);
-    p.runs = columns + p.target;
+    const long long cuts = ceil_div_ll(static_cast<long long>(width) * l.page, LEAST * KV4_TILE), most = runs_of(columns, p.slots);
+    p.runs = cuts < most / columns + 1 ? (columns * cuts < most ? columns * cuts : most) : most;
     if (p.runs > 0x7fffffff / (R * 2)) return false;
     auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };
     p.part = up(p.runs * R * l.D * 4);
@@ -646,7 +663,7 @@ template <bool F16, int D, int G, int NT>
 int launch(const Attend& a, const Plan& p, cudaStream_t st)
 {
     auto kernel = kv4_attend_kernel<F16, D, G, NT>;
-    constexpr int ring = WARPS * STAGES * UNIT * KV4_TILE * (D + 8 * G), parts = WARPS * 8 * NT * (D + 4) * 4, smem = ring > parts ? ring : parts;
+    constexpr int ring = ring_bytes<D, G>(), parts = WARPS * 8 * NT * (D + 4) * 4, smem = ring > parts ? ring : parts;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
     return launch_dependent(kernel, dim3(static_cast<unsigned>(p.runs)), dim3(WARPS * 32), smem, st, a);
 }
@@ -679,12 +696,12 @@ int launch_form(const Attend& a, const Plan& p, cudaStream_t st)
 
 using namespace bs;
 
-extern "C" size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int N)
+extern "C" size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int width, int N)
 {
     Kv4 l;
     Plan p;
     const int sms = device_sm_count();
-    if (!cache || B <= 0 || T < 0 || N < 0 || q_heads <= 0 || !kv4_layout(*cache, l) || q_heads % l.H != 0 || sms <= 0 || !plan(l, B, T, q_heads, starts != 0, N, sms, p)) return 0;
+    if (!cache || B <= 0 || T < 0 || N < 0 || q_heads <= 0 || width <= 0 || !kv4_layout(*cache, l) || q_heads % l.H != 0 || sms <= 0 || !plan(l, B, T, q_heads, starts != 0, width, N, sms, p)) return 0;
     return p.bytes();
 }
 
@@ -705,7 +722,7 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     a.status = status_device_ptr();
     if (sms <= 0 || !a.status) return BS_ERR_CUDA;
     Plan p;
-    if (!plan(a.l, B, T, q_heads, starts != nullptr, weights ? N : 0, sms, p)) return BS_ERR_UNSUPPORTED;
+    if (!plan(a.l, B, T, q_heads, starts != nullptr, width, weights ? N : 0, sms, p)) return BS_ERR_UNSUPPORTED;
     if (workspace_bytes < p.bytes()) return BS_ERR_INVALID_ARG;
     a.t = {table, table_pitch, width, B};
     a.lengths = lengths; a.starts = starts;
@@ -722,6 +739,6 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
         a.scores = reinterpret_cast<float*>(ws += p.lse);
         a.weights = weights; a.w_sequence = weights_sequence; a.w_head = weights_head; a.N = N;
     }
-    a.target = p.target;
+    a.slots = p.slots;
     return cache->type == BS_F16 ? launch_form<true>(a, p, static_cast<cudaStream_t>(stream)) : launch_form<false>(a, p, static_cast<cudaStream_t>(stream));
 }

@@ -1,9 +1,10 @@
 // Eviction from a cache of 4-bit keys and values: every head keeps its newest entries and, of the others, those that got most attention, in their order.
 //
-// A cluster of eight CTAs takes a head of a sequence.  The least weight that stays is found by its digits, 11, 11 and 10 bits from the top of a key whose order as
-// a whole number is that of the weights: each CTA counts its part of the entries by digit in shared memory, and all read one another's counts.  Entries above
-// it stay, of those equal to it the first ones.  A second pass over the entries writes the indices, ranked by sums over warps and CTAs.  What stays is then
-// moved by a kernel over all heads and sequences: into other pages at once, into their own through a copy, since what one CTA writes another may still have to read.
+// A CTA, or a cluster of them where the entries are many, takes a head of a sequence.  The least weight that stays is found by its digits, 11, 11 and 10 bits from
+// the top of a key whose order as a whole number is that of the weights: each CTA counts its part of the entries by digit in shared memory, adds a part of
+// the digits up over the cluster and hands the sums to all.  Entries above it stay, of those equal to it the first ones.  A second pass over the entries writes the
+// indices, ranked by sums over warps and CTAs.  What stays is then moved by a kernel over all heads and sequences: into other pages at once, into their own
+// through a copy, since what one CTA writes another may still have to read.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"
@@ -11,7 +12,7 @@
 namespace bs {
 namespace {
 
-constexpr int CTAS = 8, THREADS = 512, BINS = 2048;
+constexpr int THREADS = 1024, BINS = 2048, MOST = 8;            // MOST: CTAs of a cluster
 
 struct Evict {
     Kv4 l;
@@ -32,11 +33,16 @@ __device__ __forceinline__ uint32_t key_of(float w)
     const uint32_t u = __float_as_uint(w + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-__device__ __forceinline__ uint32_t remote(uint32_t addr, int rank)
+__device__ __forceinline__ uint32_t mapped(const void* p, int rank)
 {
-    uint32_t at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ uint32_t remote(const void* p, int rank)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(mapped(p, rank)));
     return v;
 }
 __device__ __forceinline__ int entries_of(const Evict& a, const int32_t* lengths, int b)
@@ -45,33 +51,36 @@ __device__ __forceinline__ int entries_of(const Evict& a, const int32_t* lengths
     const int n = lengths[b];
     return n < 0 ? 0 : n > room ? static_cast<int>(room) : n;
 }
-// Sum over the threads before this one; all: over all of them.
-__device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* sums, uint32_t& all)
+__device__ __forceinline__ uint32_t up_to_lane(uint32_t s)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    uint32_t s = v;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         const uint32_t u = __shfl_up_sync(0xffffffffu, s, d);
-        if (lane >= d) s += u;
+        if ((threadIdx.x & 31) >= d) s += u;
     }
+    return s;
+}
+// Sum over the threads before this one; all: over all of them.  32 warps.
+__device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* sums, uint32_t& all)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t s = up_to_lane(v);
     if (lane == 31) sums[warp] = s;
     __syncthreads();
-    uint32_t front = 0;
-    all = 0;
-#pragma unroll
-    for (int w = 0; w < THREADS / 32; ++w) {
-        const uint32_t u = sums[w];
-        if (w < warp) front += u;
-        all += u;
-    }
+    const uint32_t w = up_to_lane(sums[lane]);
+    all = __shfl_sync(0xffffffffu, w, 31);
+    const uint32_t front = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
     __syncthreads();
-    return front + s - v;
+    return (warp ? front : 0u) + s - v;
 }
 
-__global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(THREADS) kv4_select_kernel(const __grid_constant__ Evict a)
+// CTAS: of the cluster.
+template <int CTAS>
+__global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_constant__ Evict a)
 {
     __shared__ uint32_t bins[3][BINS], sums[THREADS / 32], found[2], mine[2];
+    __shared__ uint32_t digits[CTAS == 1 ? 1 : BINS];           // sums over the cluster
+    auto sync = [] { if (CTAS == 1) __syncthreads(); else mm_cluster_sync(); };
     dependent_begin(a.kept);
     const int rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z, th = threadIdx.x;
     const int n = entries_of(a, behind_wait<int32_t>(a.lengths), b);
@@ -88,54 +97,65 @@ __global__ void __cluster_dims__(CTAS, 1, 1) __launch_bounds__(THREADS) kv4_sele
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, wide = pass == 2 ? 10 : 11;
+#pragma unroll 8
             for (int i = from + th; i < to; i += THREADS) {
                 const uint32_t k = key_of(w[i]);
                 if (pass == 0 || k >> (shift + wide) == prefix) atomicAdd(&bins[pass][k >> shift & ((1u << wide) - 1)], 1u);
             }
-            mm_cluster_sync();
-            // four digits a thread, from the top down
-            uint32_t count[4], sum = 0;
+            sync();
+            const uint32_t* count = bins[pass];
+            if (CTAS > 1) {
+                constexpr int SLICE = BINS / CTAS;
+                for (int i = th; i < SLICE; i += THREADS) {
+                    const int digit = rank * SLICE + i;
+                    uint32_t v[CTAS], sum = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int digit = BINS - 1 - (4 * th + j);
-                count[j] = 0;
+                    for (int c = 0; c < CTAS; ++c) v[c] = remote(&bins[pass][digit], c);
 #pragma unroll
-                for (int c = 0; c < CTAS; ++c) count[j] += remote(smem_u32(&bins[pass][digit]), c);
-                sum += count[j];
+                    for (int c = 0; c < CTAS; ++c) sum += v[c];
+#pragma unroll
+                    for (int c = 0; c < CTAS; ++c) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapped(&digits[digit], c)), "r"(sum) : "memory");
+                }
+                sync();
+                count = digits;
             }
-            uint32_t all, above = before_me(sum, sums, all);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (above < left && left <= above + count[j]) { found[0] = BINS - 1 - (4 * th + j); found[1] = left - above; }
-                above += count[j];
-            }
+            // two digits a thread, from the top down
+            const int top = BINS - 1 - 2 * th;
+            const uint32_t c0 = count[top], c1 = count[top - 1];
+            uint32_t all, above = before_me(c0 + c1, sums, all);
+            if (above < left && left <= above + c0) { found[0] = top; found[1] = left - above; }
+            above += c0;
+            if (above < left && left <= above + c1) { found[0] = top - 1; found[1] = left - above; }
             __syncthreads();
             prefix = prefix << wide | found[0];
             left = found[1];
             __syncthreads();
         }
         // `left` entries equal to `prefix` stay, and all above it
-        uint32_t more = 0, equal = 0;
-        for (int i = from + th; i < to; i += THREADS) {
-            const uint32_t k = key_of(w[i]);
-            more += k > prefix;
-            equal += k == prefix;
-        }
-        uint32_t all_more, all_equal;
-        before_me(more, sums, all_more);
-        before_me(equal, sums, all_equal);
-        if (th == 0) { mine[0] = all_more; mine[1] = all_equal; }
-        mm_cluster_sync();
         uint32_t at_more = 0, at_equal = 0;
-        for (int c = 0; c < rank; ++c) {
-            at_more += remote(smem_u32(&mine[0]), c);
-            at_equal += remote(smem_u32(&mine[1]), c);
+        if (CTAS > 1) {
+            uint32_t more = 0, equal = 0;
+#pragma unroll 8
+            for (int i = from + th; i < to; i += THREADS) {
+                const uint32_t k = key_of(w[i]);
+                more += k > prefix;
+                equal += k == prefix;
+            }
+            uint32_t all_more, all_equal;
+            before_me(more, sums, all_more);
+            before_me(equal, sums, all_equal);
+            if (th == 0) { mine[0] = all_more; mine[1] = all_equal; }
+            sync();
+            for (int c = 0; c < rank; ++c) {
+                at_more += remote(&mine[0], c);
+                at_equal += remote(&mine[1], c);
+            }
+            sync();             // nobody leaves while its memory is read
         }
-        mm_cluster_sync();          // nobody leaves while its memory is read
         for (int i0 = from; i0 < to; i0 += THREADS) {
             const int i = i0 + th;
             const float v = i < to ? w[i] : 0.f;
-            const uint32_t k = i < to ? key_of(v) : 0, is_more = i < to && k > prefix, is_equal = i < to && k == prefix;
+            const uint32_t k = key_of(v), is_more = i < to && k > prefix, is_equal = i < to && k == prefix;
             uint32_t all;
             const uint32_t front = before_me(is_more | is_equal << 16, sums, all), e = at_equal + (front >> 16), place = at_more + (front & 0xffff) + min(e, left);
             if (is_more || (is_equal && e < left)) {
@@ -176,7 +196,7 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const __grid_constant__ E
                 es[k] = i & (KV4_TILE - 1);
                 ed[k] = r & (KV4_TILE - 1);
                 if (i < 0 || (STEP > 0 && i == r)) continue;          // in place already
-                const int ps = kv4_page_of(a.l, from, b, i), pd = STEP == 0 ? kv4_page_of(a.l, into, b, r) : kv4_page_of(a.l, from, b, r);
+                const int ps = kv4_page_of(a.l, from, b, i), pd = kv4_page_of(a.l, into, b, r);
                 if (ps < 0 || pd < 0) continue;
                 unsigned char* held = STEP == 0 ? nullptr : copy + static_cast<long long>(r / KV4_TILE) * a.l.tile;
                 src[k] = STEP == 2 ? held : kv4_tile_of(a.l, ps, h, i & (a.l.page - 1));
@@ -203,6 +223,27 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const __grid_constant__ E
             }
         }
     }
+}
+
+template <int CTAS>
+int launch_select(const Evict& a, int B, cudaStream_t st)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(CTAS, a.l.H, B);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {CTAS, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kv4_select_kernel<CTAS>, a) != cudaSuccess) {
+        cudaGetLastError();
+        return BS_ERR_CUDA;
+    }
+    return BS_OK;
 }
 
 }  // namespace
@@ -240,7 +281,9 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     a.lengths_out = lengths_out; a.weights_out = weights_out; a.kept = kept;
     a.copy = static_cast<unsigned char*>(workspace);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int rc = launch_dependent(kv4_select_kernel, dim3(CTAS, a.l.H, B), dim3(THREADS), 0, st, a);
+    // a CTA takes 16384 weights in about 10 us; more of them where there are so many and the heads leave SMs free
+    const int heads = a.l.H * B, sms = device_sm_count();
+    int rc = most <= 16384 || heads * 2 > sms ? launch_select<1>(a, B, st) : most <= 65536 || heads * 8 > sms ? launch_select<2>(a, B, st) : launch_select<MOST>(a, B, st);
     if (rc != BS_OK) return rc;
     const long long chunks = ceil_div_ll(stays, 128);
     const dim3 grid(static_cast<unsigned>(chunks < 4096 ? chunks : 4096), a.l.H, B);

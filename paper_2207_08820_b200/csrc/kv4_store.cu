@@ -1,10 +1,13 @@
 // Keys and values of new tokens into pages of 4-bit codes, and the values that codes stand for out of them.
 //
 // A vector of `group` channels is c s + m: m its least value, s a fifteenth of its span.  Half a warp takes one token of one head, eight channels a
-// lane.  A code is the quotient rounded half to even, decided without a division: the product with the reciprocal is off by less than one, and the borders
-// between codes, (c + 1/2) s, are exact in binary32 (s has at most 11 bits, 2 c + 1 five), so that the difference is compared with them.  Where the
-// rounded difference x - m lies on a border, what the subtraction lost decides.
+// lane; a CTA takes neighbouring tokens of one head, whose entries lie side by side.  A code is the product with the reciprocal, rounded; what it leaves of the
+// difference, x - m - c s, is exact in binary32 and shows whether the quotient was rounded the right way: it is compared with s / 2.  On that border
+// what the subtraction x - m lost decides, then half-even.
+//
+// The values' rows hold nibble i of eight channels 8 i + g in part g (kv4.h): eight lanes with a word of nibbles each exchange them in three steps.
 #include "kv4.h"
+#include "mma_kernel.cuh"
 #include "w4_dot.cuh"
 
 namespace bs {
@@ -36,29 +39,52 @@ __device__ __forceinline__ int place_of(const Store& a, int i, int& slot)
         entry += static_cast<long long>(i) - a.starts[b];
     }
     if (entry < 0 || entry >= static_cast<long long>(a.t.width) * a.l.page) return -1;
-    slot = static_cast<int>(entry % a.l.page);
+    slot = static_cast<int>(entry) & (a.l.page - 1);
     return kv4_page_of(a.l, a.t, b, entry);
+}
+
+// Lane i of eight has nibbles [i][0..7], afterwards [0..7][i].
+__device__ __forceinline__ uint32_t exchanged(uint32_t w)
+{
+    const int lane = threadIdx.x;
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) {
+        const uint32_t low = d == 1 ? 0x0f0f0f0fu : d == 2 ? 0x00ff00ffu : 0x0000ffffu;        // nibbles whose index lacks d
+        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, d);
+        w = lane & d ? (w & ~low) | (other >> 4 * d & low) : (w & low) | (other << 4 * d & ~low);
+    }
+    return w;
 }
 
 // Codes of eight values of a group that has least value m and step s.
 __device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float m, float s)
 {
-    // steps near the ends of binary32 are brought to where their reciprocals and borders are exact
-    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, inverse = __frcp_rn(t);
-    uint32_t word = 0;
+    // steps near the ends of binary32 are brought to where their reciprocals and products are exact
+    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, half = 0.5f * t;
+    const float inverse = __frcp_rn(t), magic = 12582912.f;         // 1.5 * 2^23: the lowest bits of a sum are the whole number
+    float code[8], rest[8];
+    bool wrong = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float d = x[i] - m, e = d * up;
-        float c = fminf(rintf(e * inverse), 15.f);
-        const float above = (c + 0.5f) * t, below = (c - 0.5f) * t;
-        if (e >= above || e <= below) {
-            const float back = x[i] - d, lost = (x[i] - (d + back)) + (back - m);       // of the difference, exact
-            const bool odd = static_cast<int>(c) & 1;
-            if (e > above || (e == above && (lost > 0.f || (lost == 0.f && odd)))) c += 1.f;
-            else if (e < below || (e == below && (lost < 0.f || (lost == 0.f && odd)))) c -= 1.f;
-        }
-        word |= static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f)) << 4 * i;
+        const float e = (x[i] - m) * up;
+        code[i] = fminf(e * inverse, 15.f) + magic;
+        rest[i] = fmaf(magic - code[i], t, e);
+        wrong |= fabsf(rest[i]) >= half;
     }
+    if (wrong) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (fabsf(rest[i]) >= half) {
+                const float d = x[i] - m, back = x[i] - d, lost = (x[i] - (d + back)) + (back - m);         // of the difference, exact
+                const bool odd = __float_as_uint(code[i]) & 1;
+                if (rest[i] > half || (rest[i] == half && (lost > 0.f || (lost == 0.f && odd)))) code[i] += 1.f;
+                else if (rest[i] < -half || (rest[i] == -half && (lost < 0.f || (lost == 0.f && odd)))) code[i] -= 1.f;
+                code[i] = fminf(fmaxf(code[i], magic), magic + 15.f);
+            }
+    }
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) word = word * 16 + (__float_as_uint(code[i]) - 0x4b400000u);
     return s > 0.f ? word : 0u;
 }
 
@@ -69,89 +95,88 @@ __device__ __forceinline__ uint32_t quantise(const uint4& raw, int group, bool l
     typedef W4Type<F16> Ty;
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
     float x[8], lo = INFINITY, hi = -INFINITY;
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         x[2 * i] = Ty::lo(w[i]);
         x[2 * i + 1] = Ty::hi(w[i]);
     }
+    // a NaN stays one
+    auto least = [](float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; };
+    auto most = [](float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; };
     if (live)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            lo = fminf(lo, x[i]);
-            hi = fmaxf(hi, x[i]);
-            bad |= !(fabsf(x[i]) < INFINITY);
+            lo = least(lo, x[i]);
+            hi = most(hi, x[i]);
         }
-    int any = bad;
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) {
         if (8 * d >= group) break;
-        lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-        any |= __shfl_xor_sync(0xffffffffu, any, d);
+        lo = least(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+        hi = most(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
     const float span = hi - lo;
-    uint32_t s = Ty::round2(__fdiv_rn(span, 15.f), lo);
-    if (any || !(span < INFINITY)) {        // a vector with an infinity or a NaN, or a span that binary32 does not hold: reads as NaN
+    if (!(span < INFINITY)) {        // a vector with an infinity or a NaN, or a span that binary32 does not hold: reads as NaN
         step = 0x7fff0000u;
         return 0;
     }
-    step = s;
-    return codes_of(x, lo, Ty::lo(s));
+    step = Ty::round2(__fdiv_rn(span, 15.f), lo);
+    return codes_of(x, lo, Ty::lo(step));
+}
+
+// Block i of the grid's work: ROWS tokens of a head, the heads of the same tokens side by side.
+__device__ __forceinline__ bool row_of(const Store& a, long long i, int& token, int& h)
+{
+    const long long chunk = i / a.l.H;
+    h = static_cast<int>(i - chunk * a.l.H);
+    const long long t = chunk * ROWS + (threadIdx.x >> 4);
+    token = static_cast<int>(t);
+    return t < a.T;
 }
 
 template <bool F16>
 __global__ void __launch_bounds__(THREADS) kv4_append_kernel(const __grid_constant__ Store a, const __grid_constant__ Rows r)
 {
-    __shared__ uint32_t words[ROWS][17];
-    const int32_t* pages = dependent_begin(a.t.pages);
     Store b = a;
-    b.t.pages = pages;
+    b.t.pages = dependent_begin(a.t.pages);
     b.at = behind_wait<int32_t>(a.at);
     b.starts = behind_wait<int32_t>(a.starts);
-    const int m = threadIdx.x & 15, mine = threadIdx.x >> 4, D = a.l.D;
-    const long long rows = static_cast<long long>(a.T) * a.l.H;
-    for (long long first = static_cast<long long>(blockIdx.x) * ROWS; first < rows; first += static_cast<long long>(gridDim.x) * ROWS) {
-        const long long row = first + mine;
-        int page = -1, slot = 0, h = 0;
+    const uint16_t *k = behind_wait<uint16_t>(r.k), *v = behind_wait<uint16_t>(r.v);
+    const int m = threadIdx.x & 15, D = a.l.D;
+    const long long blocks = static_cast<long long>((a.T + ROWS - 1) / ROWS) * a.l.H;
+    const bool live = 8 * m < D;
+    for (long long i = blockIdx.x; i < blocks; i += gridDim.x) {
+        int token, h, page = -1, slot = 0;
         uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        const bool live = 8 * m < D;
-        if (row < rows) {
-            const int token = static_cast<int>(row / a.l.H);
-            h = static_cast<int>(row - static_cast<long long>(token) * a.l.H);
+        if (row_of(a, i, token, h)) {
             if (live) {
-                x[0] = *reinterpret_cast<const uint4*>(behind_wait<uint16_t>(r.k) + token * r.k_token + h * r.k_head + 8 * m);
-                x[1] = *reinterpret_cast<const uint4*>(behind_wait<uint16_t>(r.v) + token * r.v_token + h * r.v_head + 8 * m);
+                x[0] = *reinterpret_cast<const uint4*>(k + token * r.k_token + h * r.k_head + 8 * m);
+                x[1] = *reinterpret_cast<const uint4*>(v + token * r.v_token + h * r.v_head + 8 * m);
             }
             page = place_of(b, token, slot);
         }
         uint32_t step[2], code[2];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) code[i] = quantise<F16>(x[i], a.l.group, live, step[i]);
-        words[mine][m] = code[1];
-        __syncwarp();
-        if (page >= 0) {
-            unsigned char* tile = kv4_tile_of(a.l, page, h, slot);
-            const int e = slot % KV4_TILE;
-            if (live) {
-                *reinterpret_cast<uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4) = code[0];
-                if (8 * m % a.l.group == 0) {
-                    uint32_t* steps = reinterpret_cast<uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
-                    steps[0] = step[0];
-                    steps[KV4_TILE * a.l.G] = step[1];
-                }
-            }
-            // part g of the values' row: nibble g of each of the D / 8 words.  Two lanes a part, half of its bytes each
-            const int g = m >> 1, bytes = D / 32;
-            unsigned char* to = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, g) * (D / 16) + (m & 1) * bytes;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (i >= bytes) break;
-                const int w = 2 * ((m & 1) * bytes + i);
-                to[i] = static_cast<unsigned char>((words[mine][w] >> 4 * g & 15) | (words[mine][w + 1] >> 4 * g & 15) << 4);
+        for (int j = 0; j < 2; ++j) code[j] = quantise<F16>(x[j], a.l.group, live, step[j]);
+        const uint32_t part = exchanged(live ? code[1] : 0u);        // of part m & 7: nibbles 8 (m >> 3) .. + 7
+        if (page < 0) continue;
+        unsigned char* tile = kv4_tile_of(a.l, page, h, slot);
+        const int e = slot % KV4_TILE;
+        if (live) {
+            *reinterpret_cast<uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4) = code[0];
+            if (8 * m % a.l.group == 0) {
+                uint32_t* steps = reinterpret_cast<uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
+                steps[0] = step[0];
+                steps[KV4_TILE * a.l.G] = step[1];
             }
         }
-        __syncwarp();
+        unsigned char* to = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, m & 7) * (D / 16) + (m >> 3) * 4;
+        if (D == 96) {          // parts of six bytes
+            *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(part);
+            if (m < 8) *reinterpret_cast<uint16_t*>(to + 2) = static_cast<uint16_t>(part >> 16);
+        } else if (m < 8 || D == 128) {
+            *reinterpret_cast<uint32_t*>(to) = part;
+        }
     }
 }
 
@@ -164,35 +189,43 @@ __global__ void __launch_bounds__(THREADS) kv4_read_kernel(const __grid_constant
     b.at = behind_wait<int32_t>(a.at);
     b.starts = behind_wait<int32_t>(a.starts);
     const int m = threadIdx.x & 15, D = a.l.D;
-    if (8 * m >= D) return;
-    const long long rows = static_cast<long long>(a.T) * a.l.H;
-    for (long long row = static_cast<long long>(blockIdx.x) * ROWS + (threadIdx.x >> 4); row < rows; row += static_cast<long long>(gridDim.x) * ROWS) {
-        const int token = static_cast<int>(row / a.l.H), h = static_cast<int>(row - static_cast<long long>(token) * a.l.H);
-        int slot = 0;
-        const int page = place_of(b, token, slot);
-        uint4 out[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    const long long blocks = static_cast<long long>((a.T + ROWS - 1) / ROWS) * a.l.H;
+    const bool live = 8 * m < D;
+    for (long long i = blockIdx.x; i < blocks; i += gridDim.x) {
+        int token, h, page = -1, slot = 0;
+        const bool there = row_of(a, i, token, h);
+        if (there) page = place_of(b, token, slot);
+        uint32_t code[2] = {0, 0}, step[2] = {0, 0};
         if (page >= 0) {
             const unsigned char* tile = behind_wait<unsigned char>(kv4_tile_of(a.l, page, h, slot));
             const int e = slot % KV4_TILE;
-            const uint32_t key = *reinterpret_cast<const uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4);
-            const unsigned char* from = tile + KV4_TILE * (D / 2) + e * (D / 2) + m / 2;
-            uint32_t value = 0;
-#pragma unroll
-            for (int g = 0; g < 8; ++g) value |= (from[kv4_value_part(D, e, g) * (D / 16)] >> 4 * (m & 1) & 15u) << 4 * g;
-            const uint32_t* steps = reinterpret_cast<const uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
-            const uint32_t code[2] = {key, value}, step[2] = {steps[0], steps[KV4_TILE * a.l.G]};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float s = Ty::lo(step[i]), o = Ty::hi(step[i]);
-                uint32_t w[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    w[j] = Ty::round2(fmaf(static_cast<float>(code[i] >> 8 * j & 15u), s, o), fmaf(static_cast<float>(code[i] >> (8 * j + 4) & 15u), s, o));
-                out[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            const unsigned char* from = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, m & 7) * (D / 16) + (m >> 3) * 4;
+            if (D == 96) {
+                code[1] = *reinterpret_cast<const uint16_t*>(from);
+                if (m < 8) code[1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + 2)) << 16;
+            } else if (m < 8 || D == 128) {
+                code[1] = *reinterpret_cast<const uint32_t*>(from);
+            }
+            if (live) {
+                code[0] = *reinterpret_cast<const uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4);
+                const uint32_t* steps = reinterpret_cast<const uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
+                step[0] = steps[0];
+                step[1] = steps[KV4_TILE * a.l.G];
             }
         }
-        *reinterpret_cast<uint4*>(k + row * D + 8 * m) = out[0];
-        *reinterpret_cast<uint4*>(v + row * D + 8 * m) = out[1];
+        code[1] = exchanged(code[1]);
+        if (!there || !live) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float s = Ty::lo(step[j]), o = Ty::hi(step[j]), whole = 8388608.f;       // 2^23 under a code is 2^23 + code
+            uint32_t w[4];
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                const float lo = __uint_as_float((code[j] >> 8 * n & 15u) | 0x4b000000u) - whole, hi = __uint_as_float((code[j] >> (8 * n + 4) & 15u) | 0x4b000000u) - whole;
+                w[n] = Ty::round2(fmaf(lo, s, o), fmaf(hi, s, o));
+            }
+            *reinterpret_cast<uint4*>((j == 0 ? k : v) + (static_cast<long long>(token) * a.l.H + h) * D + 8 * m) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
     }
 }
 
@@ -212,7 +245,7 @@ int check(const bs_kv4_cache* c, const int32_t* table, long long pitch, int widt
 }
 dim3 grid_of(const Store& a)
 {
-    const long long blocks = ceil_div_ll(static_cast<long long>(a.T) * a.l.H, ROWS), most = 8LL * device_sm_count();
+    const long long blocks = ceil_div_ll(a.T, ROWS) * a.l.H, most = 8LL * device_sm_count();
     return dim3(static_cast<unsigned>(blocks < most ? blocks : most));
 }
 
