@@ -99,28 +99,27 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi)
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
-template <int W> __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t (&w)[W])
+template <int W> __device__ __forceinline__ void load_words(uint32_t at, uint32_t (&w)[W])
 {
-    if constexpr (W == 4) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-    } else if constexpr (W == 2) {
-        const uint2 v = *reinterpret_cast<const uint2*>(p);
-        w[0] = v.x; w[1] = v.y;
-    } else {
+    if constexpr (W == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+    else if constexpr (W == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+    else
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = reinterpret_cast<const uint32_t*>(p)[i];
-    }
+        for (int i = 0; i < W; ++i) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i) : "memory");
 }
 // The D / 32 pieces of two bytes of a part of a values' row, two a word but for D = 96.
 template <int C> constexpr int words_of = C == 3 ? 3 : C / 2;
-template <int C> __device__ __forceinline__ void load_pieces(const unsigned char* p, uint32_t (&w)[words_of<C>])
+template <int C> __device__ __forceinline__ void load_pieces(uint32_t at, uint32_t (&w)[words_of<C>])
 {
     if constexpr (C == 3) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) w[i] = reinterpret_cast<const uint16_t*>(p)[i];
+        for (int i = 0; i < C; ++i) {
+            uint16_t v;
+            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + 2 * i) : "memory");
+            w[i] = v;
+        }
     } else {
-        load_words(p, w);
+        load_words(at, w);
     }
 }
 template <int C> __device__ __forceinline__ uint32_t pair_of(const uint32_t (&a)[words_of<C>], const uint32_t (&b)[words_of<C>], int c)
@@ -218,14 +217,17 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 
     // copies ahead: lane 4 i + j looks up the page of tile j of the warp's unit i, eight units at a time
     unsigned char* ring = smem + warp * STAGES * UNIT * TILE;
-    const int in_page = a.l.page / KV4_TILE;
+    const uint32_t ring_at = smem_u32(ring);
+    const int log_tiles = a.l.log_page - 4, in_page = (1 << log_tiles) - 1;        // of a page
+    const int32_t* row = table + b * a.t.pitch;
+    const unsigned char* mine_at = a.l.data + h * a.l.head;
     int page = -1;
     unsigned there = 0, flags = 0;          // which of the eight units' tiles have a page; the same of the stages, four bits each
     auto issue = [&](int k) {
         if ((k & 7) == 0) {
             const int t = t0 + (warp + WARPS * (k + (lane >> 2))) * unit + (lane & 3);
             page = -1;
-            if ((lane & 3) < unit && t < t1) page = table[b * a.t.pitch + t / in_page];
+            if ((lane & 3) < unit && t < t1) page = row[t >> log_tiles];
             if (static_cast<unsigned>(page) >= static_cast<unsigned>(a.l.pages)) page = -1;
             there = __ballot_sync(0xffffffffu, page >= 0);
         }
@@ -234,9 +236,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         if (lane == 0) mbar_expect_tx(&bars[warp][stage], count * TILE);
         __syncwarp();
         const int j = lane & 3, t = f + j;
-        if ((lane >> 2) == (k & 7) && j < count && (j == 0 || t % in_page == 0)) {
-            const int len = min(count - j, in_page - t % in_page);
-            const unsigned char* from = a.l.data + max(page, 0) * a.l.whole + h * a.l.head + static_cast<long long>(t % in_page) * TILE;
+        if ((lane >> 2) == (k & 7) && j < count && (j == 0 || (t & in_page) == 0)) {
+            const int len = min(count - j, in_page + 1 - (t & in_page));
+            const unsigned char* from = mine_at + max(page, 0) * a.l.whole + (t & in_page) * TILE;
             mm_bulk(ring + (stage * UNIT + j) * TILE, from, len * TILE, &bars[warp][stage]);
         }
     };
@@ -323,13 +325,21 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             for (int m = 0; m < MT; ++m) o[m][n][i] = o[m][n][2 + i] = 0.f;
         }
     const int place[2] = {(gid >> 1) + 4 * (gid & 1), (gid >> 1) + 4 * (gid & 1) + 8};     // entries of rows gid and gid + 8 of a fragment
+    // where a lane reads in a tile: its rows of the keys, their steps, and its part of the values' rows tid, tid + 4, tid + 8, tid + 12 (whose parts lie alike)
+    uint32_t key_at[2], step_at[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        key_at[i] = kv4_key_row(place[i]) * (D / 2) + tid * (D / 8);
+        step_at[i] = place[i] * (4 * G);
+    }
+    const uint32_t value_at = tid * (D / 2) + kv4_value_part(D, tid, gid) * (D / 16);
     bool late = false;
 
     auto take = [&](int k, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
         const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit) * KV4_TILE, count = min(unit, t1 - first / KV4_TILE);
         const unsigned flag = flags >> 4 * stage & 15u;
-        const unsigned char* unit_at = ring + stage * UNIT * TILE;
+        const uint32_t unit_at = ring_at + stage * UNIT * TILE;
         float p[UNIT][NT][4], high[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
@@ -339,12 +349,12 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
             for (int n = 0; n < NT; ++n) p[t][n][0] = p[t][n][1] = p[t][n][2] = p[t][n][3] = -INFINITY;
             if (t >= count) continue;
-            const unsigned char* tile = unit_at + t * TILE;
+            const uint32_t tile = unit_at + t * TILE;
             uint32_t key[2][BLOCKS], step[2][G];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                load_words(tile + kv4_key_row(place[i]) * (D / 2) + tid * (D / 8), key[i]);
-                load_words(tile + KV4_TILE * D + place[i] * (4 * G), step[i]);
+                load_words(tile + key_at[i], key[i]);
+                load_words(tile + KV4_TILE * D + step_at[i], step[i]);
             }
             float sum[NT][4];
 #pragma unroll
@@ -386,7 +396,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint32_t vs[G];
-                load_words(tile + KV4_TILE * D + 64 * G + place[i] * (4 * G), vs);
+                load_words(tile + KV4_TILE * D + 64 * G + step_at[i], vs);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
                     if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && (flag >> t & 1))) step_top = fmaxf(step_top, Ty::lo(vs[g]));
@@ -440,12 +450,12 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
         for (int t = 0; t < UNIT; ++t) {
             if (t >= count) continue;
-            const unsigned char* tile = unit_at + t * TILE;
+            const uint32_t tile = unit_at + t * TILE;
             uint32_t step[2][G], word[4][words_of<BLOCKS>];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) load_words(tile + KV4_TILE * D + 64 * G + place[i] * (4 * G), step[i]);
+            for (int i = 0; i < 2; ++i) load_words(tile + KV4_TILE * D + 64 * G + step_at[i], step[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_pieces<BLOCKS>(tile + KV4_TILE * (D / 2) + (tid + 4 * i) * (D / 2) + kv4_value_part(D, tid + 4 * i, gid) * (D / 16), word[i]);
+            for (int i = 0; i < 4; ++i) load_pieces<BLOCKS>(tile + KV4_TILE * (D / 2) + value_at + i * 2 * D, word[i]);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll

@@ -56,36 +56,34 @@ __device__ __forceinline__ uint32_t exchanged(uint32_t w)
     return w;
 }
 
-// Codes of eight values of a group that has least value m and step s.
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], float m, float s)
+// Codes of eight values of a group that has least value m and step s, whatever they are.
+__device__ __noinline__ uint32_t codes_at_borders(uint4 raw, bool f16, float m, float s)
 {
     // steps near the ends of binary32 are brought to where their reciprocals and products are exact
-    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, half = 0.5f * t;
-    const float inverse = __frcp_rn(t), magic = 12582912.f;         // 1.5 * 2^23: the lowest bits of a sum are the whole number
-    float code[8], rest[8];
-    bool wrong = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float e = (x[i] - m) * up;
-        code[i] = fminf(e * inverse, 15.f) + magic;
-        rest[i] = fmaf(magic - code[i], t, e);
-        wrong |= fabsf(rest[i]) >= half;
-    }
-    if (wrong) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (fabsf(rest[i]) >= half) {
-                const float d = x[i] - m, back = x[i] - d, lost = (x[i] - (d + back)) + (back - m);         // of the difference, exact
-                const bool odd = __float_as_uint(code[i]) & 1;
-                if (rest[i] > half || (rest[i] == half && (lost > 0.f || (lost == 0.f && odd)))) code[i] += 1.f;
-                else if (rest[i] < -half || (rest[i] == -half && (lost < 0.f || (lost == 0.f && odd)))) code[i] -= 1.f;
-                code[i] = fminf(fmaxf(code[i], magic), magic + 15.f);
-            }
-    }
+    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, half = 0.5f * t, inverse = __frcp_rn(t);
     uint32_t word = 0;
-#pragma unroll
-    for (int i = 7; i >= 0; --i) word = word * 16 + (__float_as_uint(code[i]) - 0x4b400000u);
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) {
+        const uint32_t w = i >= 6 ? raw.w : i >= 4 ? raw.z : i >= 2 ? raw.y : raw.x;
+        const float x = f16 ? (i & 1 ? W4Type<true>::hi(w) : W4Type<true>::lo(w)) : (i & 1 ? W4Type<false>::hi(w) : W4Type<false>::lo(w)), d = x - m, e = d * up;
+        float c = fminf(rintf(e * inverse), 15.f);
+        const float rest = fmaf(-c, t, e), back = x - d, lost = (x - (d + back)) + (back - m);         // of the difference, exact
+        const bool odd = static_cast<int>(c) & 1;
+        if (rest > half || (rest == half && (lost > 0.f || (lost == 0.f && odd)))) c += 1.f;
+        else if (rest < -half || (rest == -half && (lost < 0.f || (lost == 0.f && odd)))) c -= 1.f;
+        word = word * 16 + static_cast<uint32_t>(fminf(fmaxf(c, 0.f), 15.f));
+    }
     return s > 0.f ? word : 0u;
+}
+
+// The lesser ones of two pairs of values; a NaN stays one.
+template <bool F16>
+__device__ __forceinline__ uint32_t least(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    if (F16) asm("min.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 // One vector of a half warp: its codes (eight a lane, lanes from D / 8 on have none) and the group's step and offset as a word of the layout.
@@ -93,45 +91,48 @@ template <bool F16>
 __device__ __forceinline__ uint32_t quantise(const uint4& raw, int group, bool live, uint32_t& step)
 {
     typedef W4Type<F16> Ty;
+    constexpr uint32_t SIGNS = 0x80008000u, INF = F16 ? 0x7c007c00u : 0x7f807f80u;
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    float x[8], lo = INFINITY, hi = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = Ty::lo(w[i]);
-        x[2 * i + 1] = Ty::hi(w[i]);
-    }
-    // a NaN stays one
-    auto least = [](float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; };
-    auto most = [](float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; };
-    if (live)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            lo = least(lo, x[i]);
-            hi = most(hi, x[i]);
-        }
+    // the least value in one half, minus the largest one in the other
+    const uint32_t lo = least<F16>(least<F16>(w[0], w[1]), least<F16>(w[2], w[3]));
+    const uint32_t hi = least<F16>(least<F16>(w[0] ^ SIGNS, w[1] ^ SIGNS), least<F16>(w[2] ^ SIGNS, w[3] ^ SIGNS));
+    uint32_t ends = live ? least<F16>(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632)) : INF;
 #pragma unroll
     for (int d = 1; d < 16; d *= 2) {
         if (8 * d >= group) break;
-        lo = least(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-        hi = most(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+        ends = least<F16>(ends, __shfl_xor_sync(0xffffffffu, ends, d));
     }
-    const float span = hi - lo;
+    const float m = Ty::lo(ends), span = -Ty::hi(ends) - m;
     if (!(span < INFINITY)) {        // a vector with an infinity or a NaN, or a span that binary32 does not hold: reads as NaN
         step = 0x7fff0000u;
         return 0;
     }
-    step = Ty::round2(__fdiv_rn(span, 15.f), lo);
-    return codes_of(x, lo, Ty::lo(step));
-}
-
-// Block i of the grid's work: ROWS tokens of a head, the heads of the same tokens side by side.
-__device__ __forceinline__ bool row_of(const Store& a, long long i, int& token, int& h)
-{
-    const long long chunk = i / a.l.H;
-    h = static_cast<int>(i - chunk * a.l.H);
-    const long long t = chunk * ROWS + (threadIdx.x >> 4);
-    token = static_cast<int>(t);
-    return t < a.T;
+    step = Ty::round2(__fdiv_rn(span, 15.f), m);
+    const float s = Ty::lo(step), inverse = __frcp_rn(s), magic = 12582912.f;       // 1.5 * 2^23: the lowest bits of a sum are the whole number
+    auto both = [](float v) { return f2_pack(__float_as_uint(v), __float_as_uint(v)); };
+    const u64 m2 = both(-m), s2 = both(-s), inverse2 = both(inverse), magic2 = both(magic), less2 = both(-magic);
+    uint32_t code[8];
+    float far = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u64 x = f2_pack(__float_as_uint(Ty::lo(w[i])), __float_as_uint(Ty::hi(w[i])));
+        const u64 d = f2_add(x, m2), q = f2_fma(d, inverse2, 0), near = f2_fma(f2_fma(q, s2, d), inverse2, q), c = f2_add(near, magic2);
+        uint32_t r0, r1;
+        f2_split(f2_fma(f2_add(c, less2), s2, d), r0, r1);
+        f2_split(c, code[2 * i], code[2 * i + 1]);
+        far = fmaxf(far, fmaxf(fabsf(__uint_as_float(r0)), fabsf(__uint_as_float(r1))));
+    }
+    // The quotients are rounded correctly, so that ties come out half-even, where the difference is exact: no value and no offset is then below 2^-12 of the span.
+    // Steps of few bits (the type's smallest) may leave quotients above 15.
+    const float half = 0.5f * s;
+    const uint32_t small = least<F16>(least<F16>(w[0] & ~SIGNS, w[1] & ~SIGNS), least<F16>(w[2] & ~SIGNS, w[3] & ~SIGNS));
+    const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s &&
+                       (far < half || (far == half && fminf(fminf(Ty::lo(small), Ty::hi(small)), fabsf(m)) >= span * 0x1p-12f));
+    if (!plain) return codes_at_borders(raw, F16, m, s);
+    uint32_t word = code[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) word = word * 16 + code[i];
+    return word - 0x3f400000u;          // magic's bits times 16^i, summed
 }
 
 template <bool F16>
@@ -143,12 +144,13 @@ __global__ void __launch_bounds__(THREADS) kv4_append_kernel(const __grid_consta
     b.starts = behind_wait<int32_t>(a.starts);
     const uint16_t *k = behind_wait<uint16_t>(r.k), *v = behind_wait<uint16_t>(r.v);
     const int m = threadIdx.x & 15, D = a.l.D;
-    const long long blocks = static_cast<long long>((a.T + ROWS - 1) / ROWS) * a.l.H;
+    const int h = blockIdx.y;
     const bool live = 8 * m < D;
-    for (long long i = blockIdx.x; i < blocks; i += gridDim.x) {
-        int token, h, page = -1, slot = 0;
+    for (long long first = blockIdx.x * ROWS; first < a.T; first += gridDim.x * ROWS) {
+        const int token = static_cast<int>(first) + (threadIdx.x >> 4);
+        int page = -1, slot = 0;
         uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        if (row_of(a, i, token, h)) {
+        if (token < a.T) {
             if (live) {
                 x[0] = *reinterpret_cast<const uint4*>(k + token * r.k_token + h * r.k_head + 8 * m);
                 x[1] = *reinterpret_cast<const uint4*>(v + token * r.v_token + h * r.v_head + 8 * m);
@@ -189,11 +191,12 @@ __global__ void __launch_bounds__(THREADS) kv4_read_kernel(const __grid_constant
     b.at = behind_wait<int32_t>(a.at);
     b.starts = behind_wait<int32_t>(a.starts);
     const int m = threadIdx.x & 15, D = a.l.D;
-    const long long blocks = static_cast<long long>((a.T + ROWS - 1) / ROWS) * a.l.H;
+    const int h = blockIdx.y;
     const bool live = 8 * m < D;
-    for (long long i = blockIdx.x; i < blocks; i += gridDim.x) {
-        int token, h, page = -1, slot = 0;
-        const bool there = row_of(a, i, token, h);
+    for (long long first = blockIdx.x * ROWS; first < a.T; first += gridDim.x * ROWS) {
+        const int token = static_cast<int>(first) + (threadIdx.x >> 4);
+        int page = -1, slot = 0;
+        const bool there = token < a.T;
         if (there) page = place_of(b, token, slot);
         uint32_t code[2] = {0, 0}, step[2] = {0, 0};
         if (page >= 0) {
@@ -243,10 +246,11 @@ int check(const bs_kv4_cache* c, const int32_t* table, long long pitch, int widt
     a.T = T;
     return BS_OK;
 }
+// Neighbouring tokens of a head a CTA, as many as fill the GPU twice.
 dim3 grid_of(const Store& a)
 {
-    const long long blocks = ceil_div_ll(a.T, ROWS) * a.l.H, most = 8LL * device_sm_count();
-    return dim3(static_cast<unsigned>(blocks < most ? blocks : most));
+    const long long blocks = ceil_div_ll(a.T, ROWS), most = ceil_div(16 * device_sm_count(), a.l.H);
+    return dim3(static_cast<unsigned>(blocks < most ? blocks : most), a.l.H);
 }
 
 }  // namespace
