@@ -1,11 +1,12 @@
 // Keys and values of new tokens into pages of 4-bit codes, and the values that codes stand for out of them.
 //
-// A vector of `group` channels is c s + m: m its least value, s a fifteenth of its span.  Half a warp takes one token of one head, eight channels a
-// lane; a CTA takes neighbouring tokens of one head, whose entries lie side by side.  A code is the product with the reciprocal, rounded; what it leaves of the
-// difference, x - m - c s, is exact in binary32 and shows whether the quotient was rounded the right way: it is compared with s / 2.  On that border
-// what the subtraction x - m lost decides, then half-even.
+// A vector of `group` channels is c s + m: m its least value, s a fifteenth of its span.  Four lanes take one token of one head, lane t the channels 32 w + 8 t +
+// (0..7), 16 bytes of each 64, so that what a group costs once is shared by many values; a CTA takes neighbouring tokens of one head, whose entries lie side
+// by side.  A code is the quotient, corrected once and so rounded as a division rounds it, plus 1.5 * 2^23, which leaves the whole number, ties half-even, in
+// the lowest bits.  What remains of the difference, x - m - c s, is exact and shows the few values for which that may be wrong (codes_at_borders).
 //
-// The values' rows hold nibble i of eight channels 8 i + g in part g (kv4.h): eight lanes with a word of nibbles each exchange them in three steps.
+// Lane t's codes of the keys are part t of their row.  The values' rows hold nibble i of eight channels 8 i + g in part g (kv4.h): the four lanes exchange bytes,
+// and each writes two parts.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"
@@ -13,7 +14,7 @@
 namespace bs {
 namespace {
 
-constexpr int THREADS = 256, ROWS = THREADS / 16;
+constexpr int THREADS = 128, ROWS = THREADS / 4;
 
 struct Rows {                   // [T][H] vectors of D values, as far apart as the caller has them
     const void* k;
@@ -43,17 +44,25 @@ __device__ __forceinline__ int place_of(const Store& a, int i, int& slot)
     return kv4_page_of(a.l, a.t, b, entry);
 }
 
-// Lane i of eight has nibbles [i][0..7], afterwards [0..7][i].
+// Lane t of four has bytes [t][0..3], afterwards [0..3][t].
 __device__ __forceinline__ uint32_t exchanged(uint32_t w)
 {
-    const int lane = threadIdx.x;
-#pragma unroll
-    for (int d = 1; d < 8; d *= 2) {
-        const uint32_t low = d == 1 ? 0x0f0f0f0fu : d == 2 ? 0x00ff00ffu : 0x0000ffffu;        // nibbles whose index lacks d
-        const uint32_t other = __shfl_xor_sync(0xffffffffu, w, d);
-        w = lane & d ? (w & ~low) | (other >> 4 * d & low) : (w & low) | (other << 4 * d & ~low);
-    }
-    return w;
+    const int t = threadIdx.x & 3;
+    w = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), t & 1 ? 0x3715 : 0x6240);
+    return __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 2), t & 2 ? 0x3276 : 0x5410);
+}
+// The lower (shift 0) or upper (4) nibbles of the bytes of two words, side by side: four of a, four of b.
+__device__ __forceinline__ uint32_t gathered(uint32_t a, uint32_t b, int shift)
+{
+    a = a >> shift & 0x0f0f0f0fu;
+    b = b >> shift & 0x0f0f0f0fu;
+    return __byte_perm(a | a >> 4, b | b >> 4, 0x6420);
+}
+// The four nibbles of a word's lower half, one a byte.
+__device__ __forceinline__ uint32_t spread(uint32_t w)
+{
+    w = __byte_perm(w, 0, 0x4140);
+    return (w | w << 4) & 0x0f0f0f0fu;
 }
 
 // Codes of eight values of a group that has least value m and step s, whatever they are.
@@ -86,149 +95,207 @@ __device__ __forceinline__ uint32_t least(uint32_t a, uint32_t b)
     return r;
 }
 
-// One vector of a half warp: its codes (eight a lane, lanes from D / 8 on have none) and the group's step and offset as a word of the layout.
 template <bool F16>
-__device__ __forceinline__ uint32_t quantise(const uint4& raw, int group, bool live, uint32_t& step)
+__device__ __forceinline__ uint32_t most(uint32_t a, uint32_t b)
 {
-    typedef W4Type<F16> Ty;
-    constexpr uint32_t SIGNS = 0x80008000u, INF = F16 ? 0x7c007c00u : 0x7f807f80u;
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-    // the least value in one half, minus the largest one in the other
-    const uint32_t lo = least<F16>(least<F16>(w[0], w[1]), least<F16>(w[2], w[3]));
-    const uint32_t hi = least<F16>(least<F16>(w[0] ^ SIGNS, w[1] ^ SIGNS), least<F16>(w[2] ^ SIGNS, w[3] ^ SIGNS));
-    uint32_t ends = live ? least<F16>(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632)) : INF;
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) {
-        if (8 * d >= group) break;
-        ends = least<F16>(ends, __shfl_xor_sync(0xffffffffu, ends, d));
-    }
-    const float m = Ty::lo(ends), span = -Ty::hi(ends) - m;
-    if (!(span < INFINITY)) {        // a vector with an infinity or a NaN, or a span that binary32 does not hold: reads as NaN
-        step = 0x7fff0000u;
-        return 0;
-    }
-    step = Ty::round2(__fdiv_rn(span, 15.f), m);
-    const float s = Ty::lo(step), inverse = __frcp_rn(s), magic = 12582912.f;       // 1.5 * 2^23: the lowest bits of a sum are the whole number
-    auto both = [](float v) { return f2_pack(__float_as_uint(v), __float_as_uint(v)); };
-    const u64 m2 = both(-m), s2 = both(-s), inverse2 = both(inverse), magic2 = both(magic), less2 = both(-magic);
-    uint32_t code[8];
-    float far = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const u64 x = f2_pack(__float_as_uint(Ty::lo(w[i])), __float_as_uint(Ty::hi(w[i])));
-        const u64 d = f2_add(x, m2), q = f2_fma(d, inverse2, 0), near = f2_fma(f2_fma(q, s2, d), inverse2, q), c = f2_add(near, magic2);
-        uint32_t r0, r1;
-        f2_split(f2_fma(f2_add(c, less2), s2, d), r0, r1);
-        f2_split(c, code[2 * i], code[2 * i + 1]);
-        far = fmaxf(far, fmaxf(fabsf(__uint_as_float(r0)), fabsf(__uint_as_float(r1))));
-    }
-    // The quotients are rounded correctly, so that ties come out half-even, where the difference is exact: no value and no offset is then below 2^-12 of the span.
-    // Steps of few bits (the type's smallest) may leave quotients above 15.
-    const float half = 0.5f * s;
-    const uint32_t small = least<F16>(least<F16>(w[0] & ~SIGNS, w[1] & ~SIGNS), least<F16>(w[2] & ~SIGNS, w[3] & ~SIGNS));
-    const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s &&
-                       (far < half || (far == half && fminf(fminf(Ty::lo(small), Ty::hi(small)), fabsf(m)) >= span * 0x1p-12f));
-    if (!plain) return codes_at_borders(raw, F16, m, s);
-    uint32_t word = code[7];
-#pragma unroll
-    for (int i = 6; i >= 0; --i) word = word * 16 + code[i];
-    return word - 0x3f400000u;          // magic's bits times 16^i, summed
+    uint32_t r;
+    if (F16) asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    else asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
-template <bool F16>
+// A vector of four lanes: eight codes a word, and the groups' steps and offsets as words of the layout.  W words, PER of them a group.
+template <bool F16, int W, int PER>
+__device__ __forceinline__ void quantise(const uint4 (&raw)[W], uint32_t (&code)[W], uint32_t (&step)[W / PER])
+{
+    typedef W4Type<F16> Ty;
+    constexpr uint32_t SIGNS = 0x80008000u;
+#pragma unroll
+    for (int g = 0; g < W / PER; ++g) {
+        // the least value in one half, minus the largest one in the other
+        uint32_t lo, hi;
+#pragma unroll
+        for (int w = g * PER; w < (g + 1) * PER; ++w) {
+            const uint32_t l = least<F16>(least<F16>(raw[w].x, raw[w].y), least<F16>(raw[w].z, raw[w].w)), h = most<F16>(most<F16>(raw[w].x, raw[w].y), most<F16>(raw[w].z, raw[w].w));
+            lo = w == g * PER ? l : least<F16>(lo, l);
+            hi = w == g * PER ? h : most<F16>(hi, h);
+        }
+        hi ^= SIGNS;
+        uint32_t ends = least<F16>(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+        ends = least<F16>(ends, __shfl_xor_sync(0xffffffffu, ends, 1));
+        ends = least<F16>(ends, __shfl_xor_sync(0xffffffffu, ends, 2));
+        const float m = Ty::lo(ends), span = -Ty::hi(ends) - m;
+        if (!(span < INFINITY)) {        // a vector with an infinity or a NaN, or a span that binary32 does not hold: reads as NaN
+            step[g] = 0x7fff0000u;
+#pragma unroll
+            for (int w = g * PER; w < (g + 1) * PER; ++w) code[w] = 0;
+            continue;
+        }
+        step[g] = Ty::round2(__fdiv_rn(span, 15.f), m);
+        const float s = Ty::lo(step[g]), inverse = __frcp_rn(s), magic = 12582912.f;       // 1.5 * 2^23
+        auto both = [](float v) { return f2_pack(__float_as_uint(v), __float_as_uint(v)); };
+        const u64 m2 = both(-m), s2 = both(-s), inverse2 = both(inverse), magic2 = both(magic), less2 = both(-magic);
+        float far = 0.f;
+        uint32_t small = 0x7bff7bffu;           // a large number of either type
+#pragma unroll
+        for (int w = g * PER; w < (g + 1) * PER; ++w) {
+            uint32_t c8[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t v = word_of(raw[w], i);
+                const u64 x = f2_pack(__float_as_uint(Ty::lo(v)), __float_as_uint(Ty::hi(v)));
+                const u64 d = f2_add(x, m2), q = f2_fma(d, inverse2, 0), near = f2_fma(f2_fma(q, s2, d), inverse2, q), c = f2_add(near, magic2);
+                uint32_t r0, r1;
+                f2_split(f2_fma(f2_add(c, less2), s2, d), r0, r1);
+                f2_split(c, c8[2 * i], c8[2 * i + 1]);
+                far = fmaxf(far, fmaxf(fabsf(__uint_as_float(r0)), fabsf(__uint_as_float(r1))));
+                small = least<F16>(small, v & ~SIGNS);
+            }
+            uint32_t word = c8[7];
+#pragma unroll
+            for (int i = 6; i >= 0; --i) word = word * 16 + c8[i];
+            code[w] = word - 0x3f400000u;          // magic's bits times 16^i, summed
+        }
+        // Quotients are rounded correctly where the difference is exact: no value and no offset is then below 2^-12 of the span.  Steps of few bits (the type's
+        // smallest) may leave quotients above 15.
+        const float half = 0.5f * s;
+        const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s &&
+                           (far < half || (far == half && fminf(fminf(Ty::lo(small), Ty::hi(small)), fabsf(m)) >= span * 0x1p-12f));
+        if (!plain)
+#pragma unroll
+            for (int w = g * PER; w < (g + 1) * PER; ++w) code[w] = codes_at_borders(raw[w], F16, m, s);
+    }
+}
+
+// W: words of 32 channels, D / 32; PER: of a group.
+template <bool F16, int W, int PER>
 __global__ void __launch_bounds__(THREADS) kv4_append_kernel(const __grid_constant__ Store a, const __grid_constant__ Rows r)
 {
+    constexpr int D = 32 * W, G = W / PER;
     Store b = a;
     b.t.pages = dependent_begin(a.t.pages);
     b.at = behind_wait<int32_t>(a.at);
     b.starts = behind_wait<int32_t>(a.starts);
     const uint16_t *k = behind_wait<uint16_t>(r.k), *v = behind_wait<uint16_t>(r.v);
-    const int m = threadIdx.x & 15, D = a.l.D;
-    const int h = blockIdx.y;
-    const bool live = 8 * m < D;
-    for (long long first = blockIdx.x * ROWS; first < a.T; first += gridDim.x * ROWS) {
-        const int token = static_cast<int>(first) + (threadIdx.x >> 4);
+    const int t = threadIdx.x & 3, h = blockIdx.y;
+    for (long long first = static_cast<long long>(blockIdx.x) * ROWS; first < a.T; first += static_cast<long long>(gridDim.x) * ROWS) {
+        const int token = static_cast<int>(first) + (threadIdx.x >> 2);
         int page = -1, slot = 0;
-        uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-        if (token < a.T) {
-            if (live) {
-                x[0] = *reinterpret_cast<const uint4*>(k + token * r.k_token + h * r.k_head + 8 * m);
-                x[1] = *reinterpret_cast<const uint4*>(v + token * r.v_token + h * r.v_head + 8 * m);
-            }
-            page = place_of(b, token, slot);
-        }
-        uint32_t step[2], code[2];
+        uint4 x[2][W];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) code[j] = quantise<F16>(x[j], a.l.group, live, step[j]);
-        const uint32_t part = exchanged(live ? code[1] : 0u);        // of part m & 7: nibbles 8 (m >> 3) .. + 7
-        if (page < 0) continue;
-        unsigned char* tile = kv4_tile_of(a.l, page, h, slot);
-        const int e = slot % KV4_TILE;
-        if (live) {
-            *reinterpret_cast<uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4) = code[0];
-            if (8 * m % a.l.group == 0) {
-                uint32_t* steps = reinterpret_cast<uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
-                steps[0] = step[0];
-                steps[KV4_TILE * a.l.G] = step[1];
+        for (int w = 0; w < W; ++w) {
+            x[0][w] = x[1][w] = make_uint4(0, 0, 0, 0);
+            if (token < a.T) {
+                x[0][w] = *reinterpret_cast<const uint4*>(k + token * r.k_token + h * r.k_head + 32 * w + 8 * t);
+                x[1][w] = *reinterpret_cast<const uint4*>(v + token * r.v_token + h * r.v_head + 32 * w + 8 * t);
             }
         }
-        unsigned char* to = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, m & 7) * (D / 16) + (m >> 3) * 4;
-        if (D == 96) {          // parts of six bytes
-            *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(part);
-            if (m < 8) *reinterpret_cast<uint16_t*>(to + 2) = static_cast<uint16_t>(part >> 16);
-        } else if (m < 8 || D == 128) {
-            *reinterpret_cast<uint32_t*>(to) = part;
+        if (token < a.T) page = place_of(b, token, slot);
+        unsigned char* tile = kv4_tile_of(a.l, max(page, 0), h, slot);
+        const int e = slot % KV4_TILE;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t code[W], step[G], out[W];
+            quantise<F16, W, PER>(x[j], code, step);
+            unsigned char* to;
+            if (j == 0) {
+                to = tile + kv4_key_row(e) * (D / 2) + t * (D / 8);
+#pragma unroll
+                for (int w = 0; w < W; ++w) out[w] = code[w];
+            } else {
+                to = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, 2 * t) * (D / 16);
+#pragma unroll
+                for (int w = 0; w < W; ++w) code[w] = exchanged(code[w]);        // byte i: channels 32 w + 8 i + 2 t, and the next one's code
+                if constexpr (W == 3) {
+                    const uint32_t low = gathered(code[2], code[0], 0), high = gathered(code[0], code[1], 4);
+                    out[0] = gathered(code[0], code[1], 0);
+                    out[1] = __byte_perm(low, high, 0x5410);
+                    out[2] = __byte_perm(high, gathered(code[2], code[2], 4), 0x5432);
+                } else {
+#pragma unroll
+                    for (int w = 0; w < W; ++w) out[w] = gathered(code[2 * w % W], code[2 * w % W + 1], w < W / 2 ? 0 : 4);
+                }
+            }
+            if (page >= 0) {
+                if constexpr (W == 4) *reinterpret_cast<uint4*>(to) = make_uint4(out[0], out[1], out[2], out[3]);
+                else if constexpr (W == 2) *reinterpret_cast<uint2*>(to) = make_uint2(out[0], out[1]);
+                else
+#pragma unroll
+                    for (int w = 0; w < W; ++w) reinterpret_cast<uint32_t*>(to)[w] = out[w];
+                uint32_t mine = step[0];
+#pragma unroll
+                for (int g = 1; g < G; ++g) mine = t == g ? step[g] : mine;
+                if (t < G) reinterpret_cast<uint32_t*>(tile + KV4_TILE * D)[(j * KV4_TILE + e) * G + t] = mine;
+            }
         }
     }
 }
 
-template <bool F16>
+template <bool F16, int W>
 __global__ void __launch_bounds__(THREADS) kv4_read_kernel(const __grid_constant__ Store a, uint16_t* k, uint16_t* v)
 {
     typedef W4Type<F16> Ty;
+    constexpr int D = 32 * W;
     Store b = a;
     b.t.pages = dependent_begin(a.t.pages);
     b.at = behind_wait<int32_t>(a.at);
     b.starts = behind_wait<int32_t>(a.starts);
-    const int m = threadIdx.x & 15, D = a.l.D;
-    const int h = blockIdx.y;
-    const bool live = 8 * m < D;
-    for (long long first = blockIdx.x * ROWS; first < a.T; first += gridDim.x * ROWS) {
-        const int token = static_cast<int>(first) + (threadIdx.x >> 4);
+    const int t = threadIdx.x & 3, h = blockIdx.y;
+    for (long long first = static_cast<long long>(blockIdx.x) * ROWS; first < a.T; first += static_cast<long long>(gridDim.x) * ROWS) {
+        const int token = static_cast<int>(first) + (threadIdx.x >> 2);
         int page = -1, slot = 0;
-        const bool there = token < a.T;
-        if (there) page = place_of(b, token, slot);
-        uint32_t code[2] = {0, 0}, step[2] = {0, 0};
+        if (token < a.T) page = place_of(b, token, slot);
+        uint32_t code[2][W], step[2][W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) code[0][w] = code[1][w] = step[0][w] = step[1][w] = 0;
         if (page >= 0) {
             const unsigned char* tile = behind_wait<unsigned char>(kv4_tile_of(a.l, page, h, slot));
             const int e = slot % KV4_TILE;
-            const unsigned char* from = tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, m & 7) * (D / 16) + (m >> 3) * 4;
-            if (D == 96) {
-                code[1] = *reinterpret_cast<const uint16_t*>(from);
-                if (m < 8) code[1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(from + 2)) << 16;
-            } else if (m < 8 || D == 128) {
-                code[1] = *reinterpret_cast<const uint32_t*>(from);
-            }
-            if (live) {
-                code[0] = *reinterpret_cast<const uint32_t*>(tile + kv4_key_row(e) * (D / 2) + (m & 3) * (D / 8) + (m >> 2) * 4);
-                const uint32_t* steps = reinterpret_cast<const uint32_t*>(tile + KV4_TILE * D) + e * a.l.G + 8 * m / a.l.group;
-                step[0] = steps[0];
-                step[1] = steps[KV4_TILE * a.l.G];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const unsigned char* from = j == 0 ? tile + kv4_key_row(e) * (D / 2) + t * (D / 8) : tile + KV4_TILE * (D / 2) + e * (D / 2) + kv4_value_part(D, e, 2 * t) * (D / 16);
+                if constexpr (W == 4) {
+                    const uint4 c = *reinterpret_cast<const uint4*>(from);
+                    code[j][0] = c.x; code[j][1] = c.y; code[j][2] = c.z; code[j][3] = c.w;
+                } else if constexpr (W == 2) {
+                    const uint2 c = *reinterpret_cast<const uint2*>(from);
+                    code[j][0] = c.x; code[j][1] = c.y;
+                } else {
+#pragma unroll
+                    for (int w = 0; w < W; ++w) code[j][w] = reinterpret_cast<const uint32_t*>(from)[w];
+                }
+                const uint32_t* steps = reinterpret_cast<const uint32_t*>(tile + KV4_TILE * D) + (j * KV4_TILE + e) * a.l.G;
+#pragma unroll
+                for (int w = 0; w < W; ++w) step[j][w] = steps[a.l.G == W ? w : a.l.G == 1 ? 0 : w >> 1];
             }
         }
-        code[1] = exchanged(code[1]);
-        if (!there || !live) continue;
+        // the values' parts 2 t and 2 t + 1: halves of words, one after the other
+        uint32_t part[W];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float s = Ty::lo(step[j]), o = Ty::hi(step[j]), whole = 8388608.f;       // 2^23 under a code is 2^23 + code
-            uint32_t w[4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const float lo = __uint_as_float((code[j] >> 8 * n & 15u) | 0x4b000000u) - whole, hi = __uint_as_float((code[j] >> (8 * n + 4) & 15u) | 0x4b000000u) - whole;
-                w[n] = Ty::round2(fmaf(lo, s, o), fmaf(hi, s, o));
-            }
-            *reinterpret_cast<uint4*>((j == 0 ? k : v) + (static_cast<long long>(token) * a.l.H + h) * D + 8 * m) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int w = 0; w < W; ++w) {
+            const uint32_t low = code[1][w / 2] >> 16 * (w & 1), high = code[1][(W + w) / 2] >> 16 * (W + w & 1);
+            part[w] = exchanged(spread(low) | spread(high) << 4);
         }
+#pragma unroll
+        for (int w = 0; w < W; ++w) code[1][w] = part[w];
+        if (token >= a.T) continue;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                // a byte under the exponent of 2^23 is 2^23 + code
+                const uint32_t low = code[j][w] & 0x0f0f0f0fu, high = code[j][w] >> 4 & 0x0f0f0f0fu, whole = 0x4b000000u;
+                auto both = [](float f) { return f2_pack(__float_as_uint(f), __float_as_uint(f)); };
+                const u64 s2 = both(Ty::lo(step[j][w])), m2 = both(Ty::hi(step[j][w])), less2 = both(-8388608.f);
+                uint32_t out[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    uint32_t lo, hi;
+                    f2_split(f2_fma(f2_add(f2_pack(__byte_perm(low, whole, 0x7440 + n), __byte_perm(high, whole, 0x7440 + n)), less2), s2, m2), lo, hi);
+                    out[n] = Ty::round2(__uint_as_float(lo), __uint_as_float(hi));
+                }
+                *reinterpret_cast<uint4*>((j == 0 ? k : v) + (static_cast<long long>(token) * a.l.H + h) * D + 32 * w + 8 * t) = make_uint4(out[0], out[1], out[2], out[3]);
+            }
     }
 }
 
@@ -251,6 +318,25 @@ dim3 grid_of(const Store& a)
 {
     const long long blocks = ceil_div_ll(a.T, ROWS), most = ceil_div(16 * device_sm_count(), a.l.H);
     return dim3(static_cast<unsigned>(blocks < most ? blocks : most), a.l.H);
+}
+
+template <bool F16>
+int append(const Store& a, const Rows& r, cudaStream_t st)
+{
+    const dim3 grid = grid_of(a), block(THREADS);
+    if (a.l.D == 64) return a.l.G == 1 ? launch_dependent(kv4_append_kernel<F16, 2, 2>, grid, block, 0, st, a, r) : launch_dependent(kv4_append_kernel<F16, 2, 1>, grid, block, 0, st, a, r);
+    if (a.l.D == 96) return a.l.G == 1 ? launch_dependent(kv4_append_kernel<F16, 3, 3>, grid, block, 0, st, a, r) : launch_dependent(kv4_append_kernel<F16, 3, 1>, grid, block, 0, st, a, r);
+    return a.l.G == 1   ? launch_dependent(kv4_append_kernel<F16, 4, 4>, grid, block, 0, st, a, r)
+           : a.l.G == 2 ? launch_dependent(kv4_append_kernel<F16, 4, 2>, grid, block, 0, st, a, r)
+                        : launch_dependent(kv4_append_kernel<F16, 4, 1>, grid, block, 0, st, a, r);
+}
+template <bool F16>
+int read(const Store& a, uint16_t* k, uint16_t* v, cudaStream_t st)
+{
+    const dim3 grid = grid_of(a), block(THREADS);
+    return a.l.D == 64   ? launch_dependent(kv4_read_kernel<F16, 2>, grid, block, 0, st, a, k, v)
+           : a.l.D == 96 ? launch_dependent(kv4_read_kernel<F16, 3>, grid, block, 0, st, a, k, v)
+                         : launch_dependent(kv4_read_kernel<F16, 4>, grid, block, 0, st, a, k, v);
 }
 
 }  // namespace
@@ -276,8 +362,7 @@ extern "C" int bs_kv4_append(const void* k, long long k_token, long long k_head,
     if (T == 0) return BS_OK;
     const Rows r{k, v, k_token, k_head, v_token, v_head};
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return cache->type == BS_F16 ? launch_dependent(kv4_append_kernel<true>, grid_of(a), dim3(THREADS), 0, st, a, r)
-                                 : launch_dependent(kv4_append_kernel<false>, grid_of(a), dim3(THREADS), 0, st, a, r);
+    return cache->type == BS_F16 ? append<true>(a, r, st) : append<false>(a, r, st);
 }
 
 extern "C" int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width, int B, const int32_t* at, const int32_t* starts, int T,
@@ -291,6 +376,5 @@ extern "C" int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long
     if (T == 0) return BS_OK;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     uint16_t *ko = static_cast<uint16_t*>(k), *vo = static_cast<uint16_t*>(v);
-    return cache->type == BS_F16 ? launch_dependent(kv4_read_kernel<true>, grid_of(a), dim3(THREADS), 0, st, a, ko, vo)
-                                 : launch_dependent(kv4_read_kernel<false>, grid_of(a), dim3(THREADS), 0, st, a, ko, vo);
+    return cache->type == BS_F16 ? read<true>(a, ko, vo, st) : read<false>(a, ko, vo, st);
 }
