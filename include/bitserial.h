@@ -526,7 +526,8 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *   weights  device float [B][heads][N], rows weights_head and weights_sequence values apart, or NULL: the attention that each entry got, summed over the rows of q
  *            and the heads that share it, is added to it.  Entries from N on are left out.
  *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights); two calls that may run at the same time need one each
- * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms; the same call gives the same bits every time.
+ * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms (one, 11 bits, where the
+ * output is bf16); the same call gives the same bits every time.
  */
 size_t bs_kv4_attend_workspace_bytes(const bs_kv4_cache* cache, int B, int T, int q_heads, int starts, int width, int N);
 int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int q_heads, const bs_kv4_cache* cache, const int32_t* table, long long table_pitch,

@@ -1,8 +1,9 @@
 // Attention of the newest tokens of each sequence over its entries in a cache of 4-bit keys and values: o = softmax(scale q K^T) V, one token or a few.
 //
-// Codes less 8 are exact in fp16 and are what the tensor cores multiply (mma.sync; eight rows of queries cost what one does): with c the codes, s and m a
-// group's step and offset, a score is the sum over its groups of s (q . (c - 8)) + (m + 8 s) sum(q), scaled in 32 bits; the keys are never rounded.
-// An output is the sum over entries of (p s)(c - 8), p s as two fp16 terms under a common power of two, plus the sum of p (m + 8 s), in 32 bits.
+// Codes are exact in fp16 and are what the tensor cores multiply (mma.sync; eight rows of queries cost what one does): with c the codes, s and m a group's step
+// and offset, a score is the sum over its groups of s (q . c) + m sum(q), scaled in 32 bits; the keys are never rounded.  An output is the sum over
+// entries of (p s) c, p s in fp16 under a common power of two, plus the sum of p m, in 32 bits.  A code costs a mask: as the last bits of an fp16
+// number without an exponent it counts 2^-24, which the sums' scales take back.
 //
 // A warp takes 64 entries at a time, in one piece where the page allows, through two buffers of its own in shared memory, and keeps the running maximum, sum
 // and outputs of eight or sixteen rows (query tokens times the heads that share keys) in registers.  Four warps of a CTA share a run of entries; the
@@ -34,6 +35,7 @@ struct Attend {
     const void* q;
     long long q_token, q_head;
     int T, Hq, per;             // rows of q, its heads, how many share a head of the cache
+    FastDiv d_per, d_heads;
     float scale;                // times log2(e)
     void* out;                  // [T][Hq][D]
     float* part;                // [runs][R][D], and behind them
@@ -81,31 +83,29 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
-// Nibbles i and i + 4 of x, less 8, as pairs of fp16.
+// Nibbles i and i + 4 of x as pairs of fp16: bits at the end of a mantissa without an exponent are a number of 2^-24 each, four places up of 2^-20, exactly.
 __device__ __forceinline__ void expand(uint32_t x, uint32_t (&v)[4])
 {
-    const uint32_t y = x >> 8, base = 0x64006400u, low = 0x64086408u, sixteenth = 0x2c002c00u, high = 0xd480d480u;     // 1024 + 8; -(64 + 8)
-    const uint32_t u[4] = {(x & 0x000f000fu) | base, (x & 0x00f000f0u) | base, (y & 0x000f000fu) | base, (y & 0x00f000f0u) | base};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __half2 h = *reinterpret_cast<const __half2*>(&u[i]);
-        const __half2 d = i & 1 ? __hfma2(h, *reinterpret_cast<const __half2*>(&sixteenth), *reinterpret_cast<const __half2*>(&high))
-                                : __hsub2(h, *reinterpret_cast<const __half2*>(&low));
-        v[i] = *reinterpret_cast<const uint32_t*>(&d);
-    }
+    const uint32_t y = x >> 8;
+    v[0] = x & 0x000f000fu;
+    v[1] = x & 0x00f000f0u;
+    v[2] = y & 0x000f000fu;
+    v[3] = y & 0x00f000f0u;
 }
 __device__ __forceinline__ uint32_t half2_of(float lo, float hi)
 {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Loads of what the bulk copies brought.  They may move, but not in front of the wait, whose statement their address comes out of, nor behind the next copy into
+// the same place, in front of which the results of all of them are asked for.
 template <int W> __device__ __forceinline__ void load_words(uint32_t at, uint32_t (&w)[W])
 {
-    if constexpr (W == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
-    else if constexpr (W == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+    if constexpr (W == 4) asm("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+    else if constexpr (W == 2) asm("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
     else
 #pragma unroll
-        for (int i = 0; i < W; ++i) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i) : "memory");
+        for (int i = 0; i < W; ++i) asm("ld.shared.u32 %0, [%1];" : "=r"(w[i]) : "r"(at + 4 * i));
 }
 // The D / 32 pieces of two bytes of a part of a values' row, two a word but for D = 96.
 template <int C> constexpr int words_of = C == 3 ? 3 : C / 2;
@@ -115,7 +115,7 @@ template <int C> __device__ __forceinline__ void load_pieces(uint32_t at, uint32
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             uint16_t v;
-            asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + 2 * i) : "memory");
+            asm("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + 2 * i));
             w[i] = v;
         }
     } else {
@@ -132,6 +132,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 {
     typedef W4Type<F16> Ty;
     typedef W4Type<true> Half;
+    // The weights' second fp16 term: without it outputs are off by up to 2^-12 of the weights' part of them, which an output of 11 bits would show and one of 8
+    // does not (64 sequences: 109 us in place of 99).
+    constexpr bool TWO = F16;
     constexpr int R = 8 * NT, BLOCKS = D / 32, MT = D / 16, TILE = KV4_TILE * (D + 8 * G), PER_G = BLOCKS / G;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[WARPS][STAGES];
@@ -196,7 +199,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         if (!found) return;
     }
     const Seq s(a, lengths, starts, b, R);
-    const int h = column % a.l.H, r0 = column / a.l.H * R, rows = s.tq * a.per;
+    auto token_of = [&](int r) { return fdiv(r, a.d_per); };                // of the sequence's query tokens, the one of row r
+    const int h = column - fdiv(column, a.d_heads) * a.l.H, r0 = fdiv(column, a.d_heads) * R, rows = s.tq * a.per;
+    auto row_of = [&](int r) { return static_cast<long long>(s.first + token_of(r)) * a.Hq + h * a.per + r - token_of(r) * a.per; };       // of q and out
     if (column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
 
     // how many entries a row sees; rows behind the last one see all and are dropped
@@ -206,10 +211,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = r0 + n * 8 + 2 * tid + i;
-            limit[n][i] = r < rows ? s.n - s.tq + r / a.per + 1 : s.n;
+            limit[n][i] = r < rows ? s.n - s.tq + token_of(r) + 1 : s.n;
         }
-    const int least = s.n - s.tq + r0 / a.per + 1;                             // entries that all rows see
-    const int most = s.n - s.tq + min(rows - 1, r0 + R - 1) / a.per + 1;       // and that any row sees
+    const int least = s.n - s.tq + token_of(r0) + 1;                              // entries that all rows see
+    const int most = s.n - s.tq + token_of(min(rows - 1, r0 + R - 1)) + 1;        // and that any row sees
     const int tiles = max(0, (min(most, s.n) + KV4_TILE - 1) / KV4_TILE);
     const int t0 = min(tiles, static_cast<int>(static_cast<long long>(s.tiles) * run / runs)), t1 = min(tiles, static_cast<int>(static_cast<long long>(s.tiles) * (run + 1) / runs));
     const int unit = min(UNIT, max(1, (t1 - t0 + WARPS - 1) / WARPS));
@@ -257,7 +262,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
         for (int k = 0; k < BLOCKS; ++k) raw[k] = make_uint4(0, 0, 0, 0);
         if (r < rows) {
-            const uint16_t* q = behind_wait<uint16_t>(a.q) + (s.first + r / a.per) * a.q_token + (h * a.per + r % a.per) * a.q_head + 8 * tid;
+            const int i = token_of(r);
+            const uint16_t* q = behind_wait<uint16_t>(a.q) + (s.first + i) * a.q_token + (h * a.per + r - i * a.per) * a.q_head + 8 * tid;
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) raw[k] = *reinterpret_cast<const uint4*>(q + 32 * k);
         }
@@ -290,10 +296,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) sums[k / PER_G] += x[j];
+            // the odd pairs meet codes that count sixteen times as much
             qf[n][2 * k][0] = half2_of(x[0], x[4]);
-            qf[n][2 * k][1] = half2_of(x[1], x[5]);
+            qf[n][2 * k][1] = half2_of(x[1] * 0.0625f, x[5] * 0.0625f);
             qf[n][2 * k + 1][0] = half2_of(x[2], x[6]);
-            qf[n][2 * k + 1][1] = half2_of(x[3], x[7]);
+            qf[n][2 * k + 1][1] = half2_of(x[3] * 0.0625f, x[7] * 0.0625f);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
@@ -304,9 +311,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int from = 4 * (2 * tid + i);
-            factor[n][i] = __shfl_sync(0xffffffffu, down, from) * a.scale;
+            factor[n][i] = __shfl_sync(0xffffffffu, down, from) * (a.scale * 0x1p24f);        // sums are in units of 2^-24
 #pragma unroll
-            for (int g = 0; g < G; ++g) qsum[g][n][i] = __shfl_sync(0xffffffffu, sums[g], from);
+            for (int g = 0; g < G; ++g) qsum[g][n][i] = __shfl_sync(0xffffffffu, sums[g], from) * 0x1p-24f;
         }
     }
 
@@ -339,8 +346,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         constexpr bool MASKED = decltype(masked)::value;
         const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit) * KV4_TILE, count = min(unit, t1 - first / KV4_TILE);
         const unsigned flag = flags >> 4 * stage & 15u;
-        const uint32_t unit_at = ring_at + stage * UNIT * TILE;
+        uint32_t unit_at = ring_at + stage * UNIT * TILE;
+        asm volatile("" : "+r"(unit_at) : : "memory");
         float p[UNIT][NT][4], high[NT][2];
+        uint32_t value_step[UNIT][2][G];
 #pragma unroll
         for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
         float step_top = 0.f;
@@ -359,9 +368,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             float sum[NT][4];
 #pragma unroll
             for (int g = 0; g < G; ++g) {
-                float acc[NT][4];
+                float acc[NT][4], more[NT][4];         // two sums, so that half as many products wait for one another
 #pragma unroll
-                for (int n = 0; n < NT; ++n) acc[n][0] = acc[n][1] = acc[n][2] = acc[n][3] = 0.f;
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][i] = more[n][i] = 0.f;
 #pragma unroll
                 for (int k2 = g * PER_G; k2 < (g + 1) * PER_G; ++k2) {
                     uint32_t x[4], y[4];
@@ -370,10 +381,14 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         Half::mma(acc[n], x[0], y[0], x[1], y[1], qf[n][2 * k2][0], qf[n][2 * k2][1]);
-                        Half::mma(acc[n], x[2], y[2], x[3], y[3], qf[n][2 * k2 + 1][0], qf[n][2 * k2 + 1][1]);
+                        Half::mma(more[n], x[2], y[2], x[3], y[3], qf[n][2 * k2 + 1][0], qf[n][2 * k2 + 1][1]);
                     }
                 }
-                const float s0 = Ty::lo(step[0][g]), s1 = Ty::lo(step[1][g]), m0 = fmaf(8.f, s0, Ty::hi(step[0][g])), m1 = fmaf(8.f, s1, Ty::hi(step[1][g]));
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][i] += more[n][i];
+                const float s0 = Ty::lo(step[0][g]), s1 = Ty::lo(step[1][g]), m0 = Ty::hi(step[0][g]), m1 = Ty::hi(step[1][g]);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -395,11 +410,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             // the largest step of the values, for the common power of two
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                uint32_t vs[G];
-                load_words(tile + KV4_TILE * D + 64 * G + step_at[i], vs);
+                load_words(tile + KV4_TILE * D + 64 * G + step_at[i], value_step[t][i]);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
-                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && (flag >> t & 1))) step_top = fmaxf(step_top, Ty::lo(vs[g]));
+                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && (flag >> t & 1))) step_top = fmaxf(step_top, Ty::lo(value_step[t][i][g]));
             }
         }
         if (a.scores) {
@@ -411,7 +425,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                     for (int i = 0; i < 4; ++i) {
                         const int r = r0 + n * 8 + 2 * tid + (i & 1), e = first + t * KV4_TILE + place[i >> 1];
                         if (t < count && r < rows && e < a.N)
-                            a.scores[(static_cast<long long>(s.first + r / a.per) * a.Hq + h * a.per + r % a.per) * a.N + e] = p[t][n][i] * factor[n][i & 1];
+                            a.scores[row_of(r) * a.N + e] = p[t][n][i] * factor[n][i & 1];
                     }
         }
         // weights are relative to a maximum that is replaced, with what is there so far, only when a score is above it by 8 (weights then stay below 2^8) or a
@@ -447,20 +461,23 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 }
         }
         const float scaled = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
+        float from[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) from[n][i] = top[n][i] == -INFINITY ? 0.f : -top[n][i];
 #pragma unroll
         for (int t = 0; t < UNIT; ++t) {
             if (t >= count) continue;
             const uint32_t tile = unit_at + t * TILE;
-            uint32_t step[2][G], word[4][words_of<BLOCKS>];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) load_words(tile + KV4_TILE * D + 64 * G + step_at[i], step[i]);
+            uint32_t word[4][words_of<BLOCKS>];
 #pragma unroll
             for (int i = 0; i < 4; ++i) load_pieces<BLOCKS>(tile + KV4_TILE * (D / 2) + value_at + i * 2 * D, word[i]);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    p[t][n][i] = exp2_of(fmaf(p[t][n][i], factor[n][i & 1], top[n][i & 1] == -INFINITY ? 0.f : -top[n][i & 1]));
+                    p[t][n][i] = exp2_of(fmaf(p[t][n][i], factor[n][i & 1], from[n][i & 1]));
                     total[n][i & 1] += p[t][n][i];
                 }
 #pragma unroll
@@ -468,7 +485,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float st = Ty::lo(step[i][g]), off = fmaf(8.f, st, Ty::hi(step[i][g]));
+                    float st = Ty::lo(value_step[t][i][g]), off = Ty::hi(value_step[t][i][g]);
                     const int e = first + t * KV4_TILE + place[i];
                     if (MASKED && (e >= s.n || !(flag >> t & 1))) st = off = 0.f;
                     st *= scaled;
@@ -479,7 +496,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                         offs[g][n][1] = MASKED && e >= limit[n][1] ? offs[g][n][1] : fmaf(p1, off, offs[g][n][1]);
                         const uint32_t w = half2_of(w0, w1);
                         hi[n][i] = transposed(w);
-                        lo[n][i] = transposed(half2_of(w0 - Half::lo(w), w1 - Half::hi(w)));
+                        if (TWO) lo[n][i] = transposed(half2_of(w0 - Half::lo(w), w1 - Half::hi(w)));
                     }
                 }
 #pragma unroll
@@ -491,8 +508,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                     for (int n = 0; n < NT; ++n) {
                         Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], hi[n][0], hi[n][1]);
                         Half::mma(o[2 * c + 1][n], x[2], x[3], y[2], y[3], hi[n][0], hi[n][1]);
-                        Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], lo[n][0], lo[n][1]);
-                        Half::mma(o[2 * c + 1][n], x[2], x[3], y[2], y[3], lo[n][0], lo[n][1]);
+                        if (TWO) {
+                            Half::mma(o[2 * c][n], x[0], x[1], y[0], y[1], lo[n][0], lo[n][1]);
+                            Half::mma(o[2 * c + 1][n], x[2], x[3], y[2], y[3], lo[n][0], lo[n][1]);
+                        }
                     }
                 }
             }
@@ -508,6 +527,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         const unsigned whole = (1u << count) - 1u;
         if ((f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, std::integral_constant<bool, false>());
         else take(k, std::integral_constant<bool, true>());
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) asm volatile("" : "+f"(o[m][n][0]), "+f"(o[m][n][1]), "+f"(o[m][n][2]), "+f"(o[m][n][3]) : : "memory");
         __syncwarp();
         if (k + STAGES < mine) issue(k + STAGES);
     }
@@ -516,7 +539,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     __syncthreads();
     float* outs = reinterpret_cast<float*>(smem);
     constexpr int PITCH = D + 4;
-    const float back = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);
+    const float back = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);       // and codes were in units of 2^-24, in rows gid + 8 of 2^-20
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -531,8 +554,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             if (gid == 0) stat[warp][r] = make_float2(top[n][i], total[n][i]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                outs[(warp * R + r) * PITCH + 16 * m + gid] = fmaf(o[m][n][i], back, offs[m / (2 * PER_G)][n][i]);
-                outs[(warp * R + r) * PITCH + 16 * m + gid + 8] = fmaf(o[m][n][2 + i], back, offs[m / (2 * PER_G)][n][i]);
+                outs[(warp * R + r) * PITCH + 16 * m + gid] = fmaf(o[m][n][i] * 0x1p24f, back, offs[m / (2 * PER_G)][n][i]);
+                outs[(warp * R + r) * PITCH + 16 * m + gid + 8] = fmaf(o[m][n][2 + i] * 0x1p20f, back, offs[m / (2 * PER_G)][n][i]);
             }
         }
     __syncthreads();
@@ -552,7 +575,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         }
         if (row >= rows) continue;
         if (runs == 1) {
-            const long long at = static_cast<long long>(s.first + row / a.per) * a.Hq + h * a.per + row % a.per;
+            const long long at = row_of(row);
             const float inverse = sum == 0.f ? 0.f : 1.f / sum;
             uint32_t* to = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D + d);
             *reinterpret_cast<uint2*>(to) = make_uint2(Ty::round2(v.x * inverse, v.y * inverse), Ty::round2(v.z * inverse, v.w * inverse));
@@ -738,6 +761,8 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     a.lengths = lengths; a.starts = starts;
     a.q = q; a.q_token = q_token; a.q_head = q_head;
     a.T = T; a.Hq = q_heads; a.per = q_heads / a.l.H;
+    a.d_per = make_div(a.per);
+    a.d_heads = make_div(a.l.H);
     a.scale = scale * 1.4426950408889634f;
     a.out = out;
     char* ws = static_cast<char*>(workspace);

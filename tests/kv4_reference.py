@@ -29,9 +29,9 @@ def read(x, group):
 
 
 def parts(x, group):
-    """Bounds of what the kernels add up for a value: |c - 8| s + |m + 8 s|, and the steps."""
+    """Bounds of what the kernels add up for a value: c s + |m|, and the steps."""
     c, s, m = quantise(x, group)
-    return ((c - 8).abs() * s.unsqueeze(-1) + (m + 8 * s).abs().unsqueeze(-1)).flatten(-2), s
+    return (c * s.unsqueeze(-1) + m.abs().unsqueeze(-1)).flatten(-2), s
 
 
 def attend(q, k, v, group, scale=None):
@@ -56,17 +56,17 @@ def attend(q, k, v, group, scale=None):
         total = e.sum(1, keepdim=True)
         p = torch.where(total > 0, e / total, 0.0)
         out[:, j] = p @ vv[:, h]
-        # a score: D / 16 + a few additions in 32 bits (the tensor core's may lose a unit of the last place of the largest term each), of terms q (c - 8) s and q (m + 8 s);
+        # a score: D / 16 + a few additions in 32 bits (the tensor core's may lose a unit of the last place of the largest term each), of terms q c s and q m;
         # then three roundings of the product with the scale and the distance from the maximum, and the exponential's 2^-22
         # (the queries brought to fp16 lose 2^-38 of the largest one)
         size = q[:, j].double().abs() @ kp[:, h].T
         off = scale * size * (D / 16 + 8) * 2.0 ** -23 + 2.0 ** -38 * scale * q[:, j].double().abs().amax(1, keepdim=True) * kp[:, h].sum(1)
         off = off + 3 * 2.0 ** -24 * (scale * size).amax(1, keepdim=True) * 2
         rel = torch.where(seen, torch.expm1((off.amax(1, keepdim=True) + off).clamp(max=50)) + 2.0 ** -20, 0.0)
-        # outputs: n sums in 32 bits, weights in two fp16 terms (2^-22 of them, 2^-25 of the largest step where they are small, times codes up to 8)
+        # outputs: n sums in 32 bits, weights in two fp16 terms (2^-22 of them, 2^-25 of the largest step where they are small, times codes up to 15), or for bf16 in one (2^-11)
         sums = (n / 16 + 16) * 2.0 ** -24
-        weight = p * (2 * rel + 2 * (p * rel).sum(1, keepdim=True) + sums + 2.0 ** -22)
-        floor = torch.where(total > 0, n * 8 * 2.0 ** -25 * 2 * vs[:, h].max() / total.clamp(min=1e-300), 0.0)
+        weight = p * (2 * rel + 2 * (p * rel).sum(1, keepdim=True) + sums + (2.0 ** -22 if q.dtype == torch.float16 else 2.0 ** -11))
+        floor = torch.where(total > 0, n * 15 * 2.0 ** -25 * 2 * vs[:, h].max() / total.clamp(min=1e-300), 0.0)
         far[:, j] = weight @ vp[:, h] + floor
         far[:, j] += half * (out[:, j].abs() + far[:, j]) + torch.finfo(q.dtype).smallest_normal * torch.finfo(q.dtype).eps
         got[h] += p.sum(0)
