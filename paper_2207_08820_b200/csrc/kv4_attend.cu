@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         for (int t = 0; t < UNIT; ++t) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) p[t][n][0] = p[t][n][1] = p[t][n][2] = p[t][n][3] = -INFINITY;
-            if (t >= count) continue;
+            if (MASKED && t >= count) continue;
             const uint32_t tile = unit_at + t * TILE;
             uint32_t key[2][BLOCKS], step[2][G];
 #pragma unroll
@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = r0 + n * 8 + 2 * tid + (i & 1), e = first + t * KV4_TILE + place[i >> 1];
-                        if (t < count && r < rows && e < a.N)
+                        if ((!MASKED || t < count) && r < rows && e < a.N)
                             a.scores[row_of(r) * a.N + e] = p[t][n][i] * factor[n][i & 1];
                     }
         }
@@ -468,7 +468,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             for (int i = 0; i < 2; ++i) from[n][i] = top[n][i] == -INFINITY ? 0.f : -top[n][i];
 #pragma unroll
         for (int t = 0; t < UNIT; ++t) {
-            if (t >= count) continue;
+            if (MASKED && t >= count) continue;
             const uint32_t tile = unit_at + t * TILE;
             uint32_t word[4][words_of<BLOCKS>];
 #pragma unroll
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         }
         const int f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
         const unsigned whole = (1u << count) - 1u;
-        if ((f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, std::integral_constant<bool, false>());
+        if (count == UNIT && (f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, std::integral_constant<bool, false>());
         else take(k, std::integral_constant<bool, true>());
 #pragma unroll
         for (int m = 0; m < MT; ++m)
