@@ -5,6 +5,9 @@
 // lane), two groups of four warps that turn a row's scores into weights, a row a thread, and write them over the scores as 16-bit operands of the
 // second product, whose sums stay in tensor memory as well.  While one tile's weights are made the tensor core works for the other.
 //
+// CTAs go through such pairs, the longest ones first and back and forth, so that all end at about the same time; copies and the first scores of a pair
+// begin while the outputs of the one before leave.  Prompts so short that pairs would leave half of the SMs without work take a tile a CTA.
+//
 // Weights are relative to a maximum that is replaced only when the row's has grown by more than 2^8: sums then have room for it in 32 bits, and the outputs
 // are seldom rescaled.  Scores, maxima, sums and outputs have 32 bits; weights are rounded to the type of the values, which is what multiplies them.
 #include <cuda.h>
@@ -19,26 +22,27 @@ namespace bs {
 namespace {
 
 constexpr int ROWS = 128, KEYS = 128;
-// Warps that make weights, with most of the registers, and a group of four of which one copies and one issues MMAs: 384 threads of 168 registers become 256 of 216
-// and 128 of 72.
-constexpr int SOFTMAX = 8, THREADS = (SOFTMAX + 4) * 32;
+// Warps that make weights, with most of the registers, and four others: one copies, one issues MMAs, one looks for work.  384 threads of 168 registers become 256 of
+// 216 and 128 of 72.
+constexpr int SOFTMAX = 8, COPY = SOFTMAX, ISSUE = SOFTMAX + 1, FIND = SOFTMAX + 2, THREADS = (SOFTMAX + 4) * 32;
 
 struct Prompt {
     const int32_t* starts;      // null: one sequence of all rows
     const int32_t* starts_k;
     int B, T, Tk, Hq, H, D, G;
-    int tokens;                 // of a tile
+    int tokens, tiles;          // of a tile; of a CTA's piece of work
     int causal;
     float scale;                // times log2(e)
     void* out;                  // [T][Hq][D]
     int* status;
 };
 
-// What a CTA does: two tiles of a sequence and head.
+// What a CTA does at a time: two tiles of a sequence and head.
 struct Work {
     int q0, nq, k0, nk;         // rows of the sequence
     int h, token;               // first token of the first tile
     int blocks[2];              // of keys that a tile sees, 0 without rows
+    int any;                    // 0: no more work
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c)
@@ -53,17 +57,22 @@ __device__ __forceinline__ float exp2_of(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-struct Rows { int q0, nq, k0, nk, pairs; };
+// A value that all lanes have, in a register of the warp, where loops over it stay as well.
+__device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
+struct Rows { int q0, nq, k0, nk, pieces; };
 __device__ __forceinline__ Rows rows_of(const Prompt& a, const int32_t* starts, const int32_t* starts_k, int b)
 {
-    Rows s{0, a.T, 0, a.Tk, 0};
+    Rows s{0, 0, 0, 0, 0};
+    if (b >= a.B) return s;
+    s.nq = a.T;
+    s.nk = a.Tk;
     if (starts) {
         s.q0 = min(max(starts[b], 0), a.T);
         s.nq = min(max(starts[b + 1], s.q0), a.T) - s.q0;
         s.k0 = min(max(starts_k[b], 0), a.Tk);
         s.nk = min(max(starts_k[b + 1], s.k0), a.Tk) - s.k0;
     }
-    s.pairs = (s.nq + 2 * a.tokens - 1) / (2 * a.tokens);
+    s.pieces = (s.nq + a.tiles * a.tokens - 1) / (a.tiles * a.tokens);
     return s;
 }
 // Blocks of keys that the tokens before `end` of a sequence see.
@@ -72,29 +81,59 @@ __device__ __forceinline__ int blocks_of(const Prompt& a, const Rows& s, int end
     const int seen = a.causal ? s.nk - s.nq + min(end, s.nq) : s.nk;
     return seen <= 0 ? 0 : (seen + KEYS - 1) / KEYS;
 }
-// The n-th pair of tiles of all sequences, sequences in their order, a sequence's last tiles first.  By one warp; false: there is none.
-__device__ __forceinline__ bool find(const Prompt& a, const int32_t* starts, const int32_t* starts_k, int n, Work& w)
+// Pieces of a sequence that see w blocks or more: its last ones.
+__device__ __forceinline__ int pieces_from(const Prompt& a, const Rows& s, int w)
+{
+    if (w <= 0) return s.pieces;
+    if (!a.causal) return blocks_of(a, s, 0) >= w ? s.pieces : 0;
+    const int step = a.tiles * a.tokens, before = (w - 1) * KEYS - (s.nk - s.nq);      // tokens that see fewer
+    return before >= s.nq ? 0 : before < 0 ? s.pieces : s.pieces - before / step;
+}
+__device__ __forceinline__ int sum_of(int v) { return __reduce_add_sync(0xffffffffu, v); }
+__device__ __forceinline__ int up_to_lane(int v)
+{
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int u = __shfl_up_sync(0xffffffffu, v, d);
+        if ((threadIdx.x & 31) >= d) v += u;
+    }
+    return v;
+}
+// The n-th piece of all sequences.  By one warp.  Up to 32 sequences (`mine`: the lane's): those with most blocks first.  More: sequences in their order, a sequence's
+// last pieces first; their work is spread by their number.
+__device__ __forceinline__ bool find(const Prompt& a, const int32_t* starts, const int32_t* starts_k, const Rows& mine, int longest, int n, Work& w)
 {
     const int lane = threadIdx.x & 31;
-    int before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-        Rows s{0, 0, 0, 0, 0};
-        if (b0 + lane < a.B) s = rows_of(a, starts, starts_k, b0 + lane);
-        int sum = s.pairs;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int v = __shfl_up_sync(0xffffffffu, sum, d);
-            if (lane >= d) sum += v;
+    Rows s = mine;
+    int count = s.pieces, behind = 0, before = 0;       // pieces of the lane's sequence that may be the one, how many of its pieces come behind them; pieces in front
+    if (a.B <= 32) {
+        int lo = 0, hi = longest + 1;                   // more than n pieces see lo blocks or more, but not hi
+        if (sum_of(mine.pieces) <= n) return false;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (sum_of(pieces_from(a, mine, mid)) > n) lo = mid;
+            else hi = mid;
         }
-        const unsigned here = __ballot_sync(0xffffffffu, n >= before + sum - s.pairs && n < before + sum);
+        behind = pieces_from(a, mine, hi);
+        before = sum_of(behind);
+        count = pieces_from(a, mine, lo) - behind;
+    }
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        if (a.B > 32) {
+            s = rows_of(a, starts, starts_k, b0 + lane);
+            count = s.pieces;
+        }
+        const int sum = up_to_lane(count), from = before + sum - count;
+        const unsigned here = __ballot_sync(0xffffffffu, n >= from && n < from + count);
         if (here) {
-            const int who = __ffs(here) - 1, pair = s.pairs - 1 - (n - (before + sum - s.pairs));
+            const int piece = s.pieces - 1 - behind - (n - from);
             w.q0 = s.q0; w.nq = s.nq; w.k0 = s.k0; w.nk = s.nk;
-            w.token = pair * 2 * a.tokens;
-            for (int t = 0; t < 2; ++t) w.blocks[t] = w.token + t * a.tokens < s.nq ? blocks_of(a, s, w.token + (t + 1) * a.tokens) : 0;
+            w.token = piece * a.tiles * a.tokens;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) w.blocks[t] = t < a.tiles && w.token + t * a.tokens < s.nq ? blocks_of(a, s, w.token + (t + 1) * a.tokens) : 0;
             int* v = &w.q0;
 #pragma unroll
-            for (int i = 0; i < static_cast<int>(sizeof(Work) / 4); ++i) v[i] = __shfl_sync(0xffffffffu, v[i], who);
+            for (int i = 0; i < static_cast<int>(sizeof(Work) / 4); ++i) v[i] = __shfl_sync(0xffffffffu, v[i], __ffs(here) - 1);
             return true;
         }
         before += __shfl_sync(0xffffffffu, sum, 31);
@@ -113,7 +152,7 @@ __device__ __forceinline__ void mma_scores(uint32_t d, uint64_t a, uint64_t b, u
         PROMPT_SS("q") PROMPT_NEXT PROMPT_SS("1") PROMPT_NEXT PROMPT_SS("1") PROMPT_NEXT PROMPT_SS("1") "}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
-// D [128 x n] (+)= A (tensor memory) B (shared memory, channels side by side): 128 keys, eight steps of 16.
+// D [128 x n] (+)= A (tensor memory) B (shared memory, channels side by side): 64 keys, four steps of 16.
 #define PROMPT_TS(P) "@p tcgen05.mma.cta_group::1.kind::f16 [%0], [a], b, %3, " P ";\n\t"
 #define PROMPT_STEP "add.u32 a, a, 8;\n\tadd.s64 b, b, 128;\n\t" PROMPT_TS("1")
 __device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
@@ -121,7 +160,7 @@ __device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, u
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t.reg .b32 a;\n\t.reg .b64 b;\n\t"
         "setp.ne.b32 q, %4, 0;\n\tmov.b32 a, %1;\n\tmov.b64 b, %2;\n\telect.sync _|p, 0xffffffff;\n\t"
-        PROMPT_TS("q") PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP PROMPT_STEP "}"
+        PROMPT_TS("q") PROMPT_STEP PROMPT_STEP PROMPT_STEP "}"
         ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
 
@@ -135,19 +174,21 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
     extern __shared__ unsigned char raw[];
     // queries of the tiles, then the ring of keys and values, all in rows of 128 bytes swizzled by address: from a multiple of 1024 on
     unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
-    __shared__ uint64_t q_full, full[RING], empty[RING], s_full[2], p_full[2], o_full[2];
+    __shared__ uint64_t q_full, q_empty, full[RING], empty[RING], s_full[2], p_half[2], p_full[2], o_full[2], work_full[2], work_empty[2];
     __shared__ uint32_t tmem_slot;
-    __shared__ Work work;
-    __shared__ int any;
+    __shared__ Work works[2];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (warp == SOFTMAX) {
+    if (warp == COPY) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         mm_fence_before();
     } else if (warp == 0 && lane == 0) {
-        mbar_init(&q_full, 1);
+        mbar_init(&q_full, 1); mbar_init(&q_empty, 1);
         for (int s = 0; s < RING; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 4); mbar_init(&o_full[t], 1); }
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&s_full[t], 1); mbar_init(&p_half[t], 4); mbar_init(&p_full[t], 4); mbar_init(&o_full[t], 1);
+            mbar_init(&work_full[t], 1); mbar_init(&work_empty[t], SOFTMAX + 2);
+        }
         fence_barrier_init();
         fence_proxy_async();
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tq)) : "memory");
@@ -158,20 +199,6 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
     mm_fence_after();
     const uint32_t tmem = tmem_slot;
     dependent_begin(a.out);
-    if (warp == 0) {
-        Work w{};
-        const bool there = find(a, a.starts ? behind_wait<int32_t>(a.starts) : nullptr, a.starts ? behind_wait<int32_t>(a.starts_k) : nullptr, blockIdx.x / a.H, w);
-        if (lane == 0) {
-            w.h = blockIdx.x % a.H;
-            work = w;
-            any = there;
-        }
-    }
-    __syncthreads();
-    Work w = work;
-    if (!any) w.blocks[0] = w.blocks[1] = w.nq = 0;         // nothing to do, and no rows
-    const int n0 = w.blocks[0], n1 = w.blocks[1], most = max(n0, n1);
-    auto blocks_in = [&](int t) { return t == 0 ? n0 : n1; };
     bool late = false;
     auto wait = [&](uint64_t* bar, unsigned parity) {
         if (!late && !mm_wait(bar, parity)) {
@@ -179,39 +206,74 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
             atomicOr(a.status, STATUS_TIMEOUT);
         }
     };
+    // the next piece of work, for every warp but the one that finds it; false: there is none.  After a wait that ran out there is none either.
+    int turn = 0;
+    auto take = [&](Work& w) {
+        wait(&work_full[turn & 1], turn >> 1 & 1);
+        w = works[turn & 1];
+        __syncwarp();
+        if (lane == 0) mm_arrive(&work_empty[turn & 1]);
+        ++turn;
+        return !__any_sync(0xffffffffu, late || !w.any);
+    };
     if (warp >= SOFTMAX) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;" ::: "memory");
-        if (warp == SOFTMAX) {
-            unsigned limit = 1u << 20;
-            if (most > 0) {
+        if (warp == FIND) {
+            const int32_t *starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr, *starts_k = a.starts ? behind_wait<int32_t>(a.starts_k) : nullptr;
+            const Rows mine = rows_of(a, starts, starts_k, lane);
+            const int longest = uniform(blocks_of(a, mine, mine.nq));
+            for (int k = 0, go = 1; go && !late; ++k) {
+                // back and forth: who had the longest piece of a round has the shortest of the next
+                const int at = k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+                const long long item = static_cast<long long>(k) * gridDim.x + at;
+                Work w{};
+                w.any = item < 0x7fffffff && find(a, starts, starts_k, mine, longest, static_cast<int>(item / a.H), w);
+                w.h = static_cast<int>(item % a.H);
+                go = w.any;
+                wait(&work_empty[k & 1], k >> 1 & 1 ^ 1);
+                if (lane == 0) {
+                    works[k & 1] = w;
+                    mm_arrive(&work_full[k & 1]);
+                }
+                __syncwarp();
+            }
+        } else if (warp == COPY) {
+            Work w;
+            unsigned limit = 1u << 20, phase = 1, q_phase = 1;
+            int at = 0, issued = 0;
+            while (take(w)) {
+                const int most = uniform(max(w.blocks[0], w.blocks[1])), h = uniform(w.h), k0 = uniform(w.k0), q0 = uniform(w.q0 + w.token);
+                if (most == 0) continue;
+                mm_wait_uniform(&q_empty, q_phase, limit);
+                q_phase ^= 1;
                 if (mm_elect()) {
                     const int bytes = 128 * a.G * a.tokens;        // rows that no tile has keep what the memory holds: they meet nothing
-                    mbar_expect_tx(&q_full, 2 * HALVES * bytes);
-                    for (int t = 0; t < 2; ++t)
-                        for (int i = 0; i < HALVES; ++i) tma_load_3d(smem + t * TILE + i * HALF, &tq, &q_full, 64 * i, w.h * a.G, w.q0 + w.token + t * a.tokens);
+                    mbar_expect_tx(&q_full, a.tiles * HALVES * bytes);
+                    for (int t = 0; t < a.tiles; ++t)
+                        for (int i = 0; i < HALVES; ++i) tma_load_3d(smem + t * TILE + i * HALF, &tq, &q_full, 64 * i, h * a.G, q0 + t * a.tokens);
                 }
-                int at = 0;
-                unsigned phase = 1;
                 for (int j = 2 * most - 1; j >= 0; --j) {           // keys, then values, of each block
                     mm_wait_uniform(&empty[at], phase, limit);
                     if (mm_elect()) {
                         unsigned char* to = smem + (2 + at) * TILE;
                         mbar_expect_tx(&full[at], TILE);
-                        for (int i = 0; i < HALVES; ++i) tma_load_3d(to + i * HALF, j & 1 ? &tk : &tv, &full[at], 64 * i, w.h, w.k0 + (j >> 1) * KEYS);
+                        for (int i = 0; i < HALVES; ++i) tma_load_3d(to + i * HALF, j & 1 ? &tk : &tv, &full[at], 64 * i, h, k0 + (j >> 1) * KEYS);
                     }
                     if (++at == RING) { at = 0; phase ^= 1; }
-                }
-                if (limit == 1 && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
-                // no copy outlives the CTA, whatever else was waited for
-                limit = 1u << 20;
-                mm_wait_uniform(&q_full, 0, limit);
-                for (int i = 0; i < RING && i < 2 * most; ++i) {
-                    at = at == 0 ? RING - 1 : at - 1;
-                    if (at == RING - 1) phase ^= 1;
-                    mm_wait_uniform(&full[at], phase ^ 1, limit);
+                    ++issued;
                 }
             }
-        } else if (warp == SOFTMAX + 1) {
+            if (limit == 1 && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+            // no copy outlives the CTA, whatever else was waited for
+            limit = 1u << 20;
+            if (issued > 0) mm_wait_uniform(&q_full, q_phase, limit);
+            for (int i = 0; i < RING && i < issued; ++i) {
+                at = at == 0 ? RING - 1 : at - 1;
+                if (at == RING - 1) phase ^= 1;
+                mm_wait_uniform(&full[at], phase ^ 1, limit);
+            }
+        } else if (warp == ISSUE) {
+            Work w;
             unsigned limit = 1u << 20;
             const uint32_t type = F16 ? 0u : (1u << 7) | (1u << 10);
             const uint32_t score_desc = (1u << 4) | type | (KEYS >> 3) << 17 | (ROWS >> 4) << 24;
@@ -220,167 +282,188 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
             // rows of 128 bytes, swizzled in groups of eight: 1024 bytes from group to group; of the values, whose rows are the reduction, HALF from 64 channels to the next
             const uint64_t major = static_cast<uint64_t>(64u | (1u << 14) | (2u << 29)) << 32;
             auto scores = [&](int t, int stage) {
+#pragma unroll
                 for (int i = 0; i < HALVES; ++i)
                     mma_scores(tmem + t * 128, major | 1u << 16 | (base + (t * TILE + i * HALF) / 16), major | 1u << 16 | (base + ((2 + stage) * TILE + i * HALF) / 16), score_desc, i);
+                mm_commit(&s_full[t]);
             };
             int at = 0;
-            unsigned phase = 0, p_phase[2] = {0, 0};
+            unsigned phase = 0, q_phase = 0, p_phase[2] = {0, 0}, o_phase[2] = {0, 0};
             auto next = [&] { if (++at == RING) { at = 0; phase ^= 1; } };
-            if (most > 0) {
-                mm_wait_uniform(&q_full, 0, limit);
+            while (take(w)) {
+                const int n0 = uniform(w.blocks[0]), n1 = uniform(w.blocks[1]), most = max(n0, n1), nk = uniform(w.nk);
+                auto blocks_in = [&](int t) { return t == 0 ? n0 : n1; };
+                if (most == 0) continue;
+                mm_wait_uniform(&q_full, q_phase, limit);
+                q_phase ^= 1;
                 mm_wait_uniform(&full[at], phase, limit);
                 mm_fence_after();
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
-                    if (most - 1 < blocks_in(t)) {
-                        scores(t, at);
-                        mm_commit(&s_full[t]);
-                    }
+                    if (most - 1 < blocks_in(t)) scores(t, at);
                 mm_commit(&empty[at]);
                 next();
-            }
-            for (int j = most - 1; j >= 0; --j) {
-                const int v = at;
-                mm_wait_uniform(&full[v], phase, limit);
-                const int left = w.nk - j * KEYS;
-                if (left < KEYS) {      // rows behind the sequence's last one may hold anything, which zero weights would not keep out
-                    for (int i = left * 128 + lane * 16; i < HALF; i += 512)
-                        for (int k = 0; k < HALVES; ++k) *reinterpret_cast<uint4*>(smem + (2 + v) * TILE + k * HALF + i) = make_uint4(0, 0, 0, 0);
-                    fence_proxy_async();
-                    __syncwarp();
-                }
-                next();
-                const int k = at;
-                if (j > 0) mm_wait_uniform(&full[k], phase, limit);
+                for (int j = most - 1; j >= 0; --j) {
+                    const int v = at;
+                    mm_wait_uniform(&full[v], phase, limit);
+                    const int left = nk - j * KEYS;
+                    if (left < KEYS) {      // rows behind the sequence's last one may hold anything, which zero weights would not keep out
+                        for (int i = left * 128 + lane * 16; i < HALF; i += 512)
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (j < blocks_in(t)) {
-                        mm_wait_uniform(&p_full[t], p_phase[t], limit);
-                        p_phase[t] ^= 1;
-                        mm_fence_after();
-                        mma_values(tmem + 256 + t * 128, tmem + t * 128, major | static_cast<uint64_t>(HALF / 16) << 16 | (base + (2 + v) * TILE / 16), value_desc, j != blocks_in(t) - 1);
-                        if (j == 0) mm_commit(&o_full[t]);
+                            for (int k = 0; k < HALVES; ++k) *reinterpret_cast<uint4*>(smem + (2 + v) * TILE + k * HALF + i) = make_uint4(0, 0, 0, 0);
+                        fence_proxy_async();
+                        __syncwarp();
                     }
-                    if (j > 0 && j - 1 < blocks_in(t)) {
-                        scores(t, k);
-                        mm_commit(&s_full[t]);
-                    }
-                }
-                mm_commit(&empty[v]);
-                if (j > 0) {
-                    mm_commit(&empty[k]);
                     next();
+                    const int k = at;
+                    if (j > 0) mm_wait_uniform(&full[k], phase, limit);
+                    else mm_commit(&q_empty);               // all scores are on their way
+                    const uint64_t values = major | static_cast<uint64_t>(HALF / 16) << 16 | (base + (2 + v) * TILE / 16);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (j < blocks_in(t)) {             // the first 64 keys' weights, then the others'
+                            mm_wait_uniform(&p_half[t], p_phase[t], limit);
+                            mm_fence_after();
+                            mma_values(tmem + 256 + t * 128, tmem + t * 128, values, value_desc, j != blocks_in(t) - 1);
+                            mm_wait_uniform(&p_full[t], p_phase[t], limit);
+                            mm_fence_after();
+                            mma_values(tmem + 256 + t * 128, tmem + t * 128 + 32, values + 512, value_desc, 1);
+                            p_phase[t] ^= 1;
+                            if (j == 0) {
+                                mm_commit(&o_full[t]);
+                                o_phase[t] ^= 1;
+                            }
+                        }
+                        if (j > 0 && j - 1 < blocks_in(t)) scores(t, k);
+                    }
+                    mm_commit(&empty[v]);
+                    if (j > 0) {
+                        mm_commit(&empty[k]);
+                        next();
+                    }
                 }
             }
             if (limit == 1 && lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
             limit = 1u << 20;           // nor do the MMAs outlive the tensor memory
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
-                if (blocks_in(t) > 0) mm_wait_uniform(&o_full[t], 0, limit);
+            for (int t = 0; t < 2; ++t) mm_wait_uniform(&o_full[t], o_phase[t] ^ 1, limit);
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;" ::: "memory");
-        const int t = warp >> 2, row = (warp & 3) * 32 + lane, blocks = blocks_in(t);
+        const int t = warp >> 2, row = (warp & 3) * 32 + lane, row_token = row / a.G, row_head = row - row_token * a.G;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
-        const int first = w.token + t * a.tokens, token = first + row / a.G;
-        const int seen = a.causal ? min(w.nk - w.nq + token + 1, w.nk) : w.nk;                 // keys that the row sees
-        const int all = a.causal ? w.nk - w.nq + first + 1 : w.nk;                             // and that all rows of the tile see
-        float top = -INFINITY, total = 0.f;
-        for (int j = blocks - 1; j >= 0; --j) {
-            wait(&s_full[t], (blocks - 1 - j) & 1);
-            mm_fence_after();
-            uint32_t v[4][32];
+        const u64 scale2 = f2_pack(__float_as_uint(a.scale), __float_as_uint(a.scale));
+        unsigned s_phase = 0, o_phase = 0;
+        Work w;
+        while (take(w)) {
+            const int blocks = t == 0 ? w.blocks[0] : w.blocks[1];
+            const int first = w.token + t * a.tokens, token = first + row_token;
+            const int seen = a.causal ? min(w.nk - w.nq + token + 1, w.nk) : w.nk;                 // keys that the row sees
+            const int all = a.causal ? min(w.nk - w.nq + first + 1, w.nk) : w.nk;                  // and that all rows of the tile see
+            // where the row goes, null: nowhere
+            uint16_t* out = nullptr;
+            if (row < a.tokens * a.G && t < a.tiles && token < w.nq)
+                out = static_cast<uint16_t*>(a.out) + (static_cast<long long>(w.q0 + token) * a.Hq + w.h * a.G + row_head) * a.D;
+            float top = -INFINITY, total = 0.f;
+            for (int j = blocks - 1; j >= 0; --j) {
+                wait(&s_full[t], s_phase);
+                s_phase ^= 1;
+                mm_fence_after();
+                uint32_t v[4][32];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mm_ld32(s_at + 32 * i, v[i]);
-            mm_ld_wait();
+                for (int i = 0; i < 4; ++i) mm_ld32(s_at + 32 * i, v[i]);
+                mm_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mm_landed(v[i]);
-            if ((j + 1) * KEYS > all || (j + 1) * KEYS > w.nk) {
-                const int left = seen - j * KEYS;
+                for (int i = 0; i < 4; ++i) mm_landed(v[i]);
+                if ((j + 1) * KEYS > all) {
+                    const int left = seen - j * KEYS;
 #pragma unroll
-                for (int i = 0; i < 128; ++i)
-                    if (i >= left) v[i / 32][i % 32] = 0xff800000u;
-            }
-            float high[4];
+                    for (int i = 0; i < 128; ++i)
+                        if (i >= left) v[i / 32][i % 32] = 0xff800000u;
+                }
+                float high[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                high[i] = __uint_as_float(v[i][0]);
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t* x = &v[i / 2][i % 2 * 16];
+                    high[i] = max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
 #pragma unroll
-                for (int k = 1; k < 31; k += 2) high[i] = max3(high[i], __uint_as_float(v[i][k]), __uint_as_float(v[i][k + 1]));
-                high[i] = fmaxf(high[i], __uint_as_float(v[i][31]));
-            }
-            const float now = fmaxf(max3(high[0], high[1], high[2]), high[3]);
-            const bool grown = (now - top) * a.scale > 8.f || (top == -INFINITY && now > -INFINITY);
-            if (__any_sync(0xffffffffu, grown)) {
-                const float to = grown ? now : top, f = grown ? exp2_of((top - to) * a.scale) : 1.f;
-                top = to;
-                total *= f;
-                if (j != blocks - 1) {      // the outputs so far: the scores' barrier says that their last product is done
+                    for (int k = 3; k < 15; k += 2) high[i] = max3(high[i], __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+                    high[i] = fmaxf(high[i], __uint_as_float(x[15]));
+                }
+                const float now = fmaxf(max3(max3(high[0], high[1], high[2]), high[3], high[4]), max3(high[5], high[6], high[7]));
+                const bool grown = (now - top) * a.scale > 8.f || (top == -INFINITY && now > -INFINITY);
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float to = grown ? now : top, f = grown ? exp2_of((top - to) * a.scale) : 1.f;
+                    top = to;
+                    total *= f;
+                    if (j != blocks - 1) {      // the outputs so far: the scores' barrier says that their last product is done
 #pragma unroll
-                    for (int i = 0; i < N; i += 32) {
-                        uint32_t o[32];
-                        mm_ld32(o_at + i, o);
-                        mm_ld_wait();
-                        mm_landed(o);
+                        for (int i = 0; i < N; i += 32) {
+                            uint32_t o[32];
+                            mm_ld32(o_at + i, o);
+                            mm_ld_wait();
+                            mm_landed(o);
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
-                        mm_st16(o_at + i, o);
-                        mm_st16(o_at + i + 16, o + 16);
+                            for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * f);
+                            mm_st16(o_at + i, o);
+                            mm_st16(o_at + i + 16, o + 16);
+                        }
                     }
                 }
-            }
-            const float base_of = top == -INFINITY ? 0.f : -top * a.scale;
-            const u64 scale2 = f2_pack(__float_as_uint(a.scale), __float_as_uint(a.scale)), base2 = f2_pack(__float_as_uint(base_of), __float_as_uint(base_of));
-            u64 sums[4] = {0, 0, 0, 0};
+                const float base_of = top == -INFINITY ? 0.f : -top * a.scale;
+                const u64 base2 = f2_pack(__float_as_uint(base_of), __float_as_uint(base_of));
+                u64 sums[4] = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t p[16];
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t p[16];
 #pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    uint32_t lo, hi;
-                    f2_split(f2_fma(f2_pack(v[i][2 * k], v[i][2 * k + 1]), scale2, base2), lo, hi);
-                    const float x = exp2_of(__uint_as_float(lo)), y = exp2_of(__uint_as_float(hi));
-                    sums[k & 3] = f2_add(sums[k & 3], f2_pack(__float_as_uint(x), __float_as_uint(y)));
-                    p[k] = Ty::round2(x, y);
+                    for (int k = 0; k < 16; ++k) {
+                        uint32_t lo, hi;
+                        f2_split(f2_fma(f2_pack(v[i][2 * k], v[i][2 * k + 1]), scale2, base2), lo, hi);
+                        const float x = exp2_of(__uint_as_float(lo)), y = exp2_of(__uint_as_float(hi));
+                        sums[k & 3] = f2_add(sums[k & 3], f2_pack(__float_as_uint(x), __float_as_uint(y)));
+                        p[k] = Ty::round2(x, y);
+                    }
+                    mm_st16(s_at + 16 * i, p);
+                    if (i & 1) {
+                        mm_st_wait();
+                        mm_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mm_arrive(i == 1 ? &p_half[t] : &p_full[t]);
+                    }
                 }
-                mm_st16(s_at + 16 * i, p);
+                uint32_t lo, hi;
+                f2_split(f2_add(f2_add(sums[0], sums[1]), f2_add(sums[2], sums[3])), lo, hi);
+                total += __uint_as_float(lo) + __uint_as_float(hi);
             }
-            mm_st_wait();
-            mm_fence_before();
-            __syncwarp();
-            if (lane == 0) mm_arrive(&p_full[t]);
-            uint32_t lo, hi;
-            f2_split(f2_add(f2_add(sums[0], sums[1]), f2_add(sums[2], sums[3])), lo, hi);
-            total += __uint_as_float(lo) + __uint_as_float(hi);
-        }
-        const bool live = row < a.tokens * a.G && token < w.nq;
-        uint16_t* out = static_cast<uint16_t*>(a.out) + (static_cast<long long>(w.q0 + token) * a.Hq + w.h * a.G + row % a.G) * a.D;
-        if (blocks > 0) {
-            wait(&o_full[t], 0);
-            mm_fence_after();
-        }
-        const float inverse = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-        for (int i = 0; i < N; i += 32) {
-            uint32_t o[32];
             if (blocks > 0) {
-                mm_ld32(o_at + i, o);
-                mm_ld_wait();
-                mm_landed(o);
+                wait(&o_full[t], o_phase);
+                o_phase ^= 1;
+                mm_fence_after();
             }
+            const float inverse = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-            for (int k = 0; k < 32; k += 8) {
-                uint32_t p[4];
+            for (int i = 0; i < N; i += 32) {
+                uint32_t o[32];
+                if (blocks > 0) {
+                    mm_ld32(o_at + i, o);
+                    mm_ld_wait();
+                    mm_landed(o);
+                }
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-                    p[m] = total == 0.f ? 0u : Ty::round2(__uint_as_float(o[k + 2 * m]) * inverse, __uint_as_float(o[k + 2 * m + 1]) * inverse);
-                if (live && i + k < a.D) *reinterpret_cast<uint4*>(out + i + k) = make_uint4(p[0], p[1], p[2], p[3]);
+                for (int k = 0; k < 32; k += 8) {
+                    uint32_t p[4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        p[m] = total == 0.f ? 0u : Ty::round2(__uint_as_float(o[k + 2 * m]) * inverse, __uint_as_float(o[k + 2 * m + 1]) * inverse);
+                    if (out && i + k < a.D) *reinterpret_cast<uint4*>(out + i + k) = make_uint4(p[0], p[1], p[2], p[3]);
+                }
             }
+            mm_fence_before();          // the next piece's first product may write over them once its weights are there
         }
-        mm_fence_before();
     }
     __syncthreads();
-    if (warp == SOFTMAX) {
+    if (warp == COPY) {
         mm_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
@@ -446,8 +529,13 @@ extern "C" int bs_attend_prompt(const void* q, long long q_token, long long q_he
     a.out = out;
     a.status = status_device_ptr();
     if (!a.status) return BS_ERR_CUDA;
-    const long long ctas = (ceil_div_ll(T, 2 * a.tokens) + (B - 1)) * heads;
-    if (ctas > 0x7fffffff) return BS_ERR_UNSUPPORTED;
+    const int sms = device_sm_count();
+    if (sms <= 0) return BS_ERR_CUDA;
+    // pieces of two tiles, or of one while there are SMs for all of them (500 tokens: 14.3 us with two)
+    const long long singles = (ceil_div_ll(T, a.tokens) + (B - 1)) * heads, pairs = (ceil_div_ll(T, 2 * a.tokens) + (B - 1)) * heads;
+    a.tiles = singles <= sms ? 1 : 2;
+    const long long pieces = a.tiles == 1 ? singles : pairs, ctas = pieces < sms ? pieces : sms;
+    if (pieces > 0x7fff0000) return BS_ERR_UNSUPPORTED;
     const bool f16 = type == BS_F16;
     CUtensorMap tq, tk, tv;
     // without keys nothing is fetched; a map has to have rows all the same
