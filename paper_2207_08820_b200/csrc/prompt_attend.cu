@@ -24,6 +24,7 @@ namespace {
 constexpr int ROWS = 128, KEYS = 128;
 // Warps that make weights, with most of the registers, and four others: one copies, one issues MMAs, one looks for work.  384 threads of 168 registers become 256 of
 // 216 and 128 of 72.
+constexpr int RING = 4;             // tiles of keys or values on their way; with three the long prompt takes 5 % more
 constexpr int SOFTMAX = 8, COPY = SOFTMAX, ISSUE = SOFTMAX + 1, FIND = SOFTMAX + 2, THREADS = (SOFTMAX + 4) * 32;
 
 struct Prompt {
@@ -166,17 +167,18 @@ __device__ __forceinline__ void mma_values(uint32_t d, uint32_t a, uint64_t b, u
 
 // HALVES: of 64 channels.  Tensor memory: scores (and weights over them) of both tiles, outputs of both.
 template <bool F16, int HALVES>
-__global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv,
+__global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_constant__ CUtensorMap tq, const __grid_constant__ CUtensorMap tk, const __grid_constant__ CUtensorMap tv, const __grid_constant__ CUtensorMap to,
                                                                    const __grid_constant__ Prompt a)
 {
     typedef W4Type<F16> Ty;
-    constexpr int HALF = ROWS * 128, TILE = HALVES * HALF, RING = HALVES == 2 ? 5 : 8, N = HALVES * 64;
+    constexpr int HALF = ROWS * 128, TILE = HALVES * HALF, N = HALVES * 64;
     extern __shared__ unsigned char raw[];
-    // queries of the tiles, then the ring of keys and values, all in rows of 128 bytes swizzled by address: from a multiple of 1024 on
+    // queries of the tiles, the ring of keys and values, and outputs of 64 channels of each tile, all in rows of 128 bytes swizzled by address: from a multiple of 1024 on
     unsigned char* smem = raw + (1024 - (smem_u32(raw) & 1023) & 1023);
     __shared__ uint64_t q_full, q_empty, full[RING], empty[RING], s_full[2], p_half[2], p_full[2], o_full[2], work_full[2], work_empty[2];
     __shared__ uint32_t tmem_slot;
     __shared__ Work works[2];
+    __shared__ int4 held_work[SOFTMAX];        // first row of the tile, rows of the sequence from there on, first head
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (warp == COPY) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512) : "memory");
@@ -353,6 +355,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
         const int t = warp >> 2, row = (warp & 3) * 32 + lane, row_token = row / a.G, row_head = row - row_token * a.G;
         const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16, s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
         const u64 scale2 = f2_pack(__float_as_uint(a.scale), __float_as_uint(a.scale));
+        unsigned char* held = smem + (2 + RING) * TILE + t * HALF;
         unsigned s_phase = 0, o_phase = 0;
         Work w;
         while (take(w)) {
@@ -360,10 +363,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
             const int first = w.token + t * a.tokens, token = first + row_token;
             const int seen = a.causal ? min(w.nk - w.nq + token + 1, w.nk) : w.nk;                 // keys that the row sees
             const int all = a.causal ? min(w.nk - w.nq + first + 1, w.nk) : w.nk;                  // and that all rows of the tile see
-            // where the row goes, null: nowhere
-            uint16_t* out = nullptr;
-            if (row < a.tokens * a.G && t < a.tiles && token < w.nq)
-                out = static_cast<uint16_t*>(a.out) + (static_cast<long long>(w.q0 + token) * a.Hq + w.h * a.G + row_head) * a.D;
+            // what the outputs need waits in memory: the registers are the scores'
+            if (lane == 0) held_work[warp] = make_int4(w.q0 + first, w.nq - first, w.h * a.G, 0);
+            __syncwarp();
             float top = -INFINITY, total = 0.f;
             for (int j = blocks - 1; j >= 0; --j) {
                 wait(&s_full[t], s_phase);
@@ -378,8 +380,12 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
                 if ((j + 1) * KEYS > all) {
                     const int left = seen - j * KEYS;
 #pragma unroll
-                    for (int i = 0; i < 128; ++i)
-                        if (i >= left) v[i / 32][i % 32] = 0xff800000u;
+                    for (int i = 0; i < 4; ++i) {
+                        const int l = left - 32 * i;
+                        const uint32_t m = l >= 32 ? 0xffffffffu : l <= 0 ? 0u : (1u << l) - 1;
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[i][k] = m >> k & 1 ? v[i][k] : 0xff800000u;
+                    }
                 }
                 float high[8];
 #pragma unroll
@@ -442,25 +448,48 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
                 mm_fence_after();
             }
             const float inverse = total == 0.f ? 0.f : 1.f / total;
+            const int4 place = held_work[warp];
+            const bool box = t < a.tiles && a.tokens <= place.y;          // all of the tile's rows are there: they leave as boxes of 64 channels
+            uint16_t* out = nullptr;
+            if (row < a.tokens * a.G && t < a.tiles && row_token < place.y)
+                out = static_cast<uint16_t*>(a.out) + (static_cast<long long>(place.x + row_token) * a.Hq + place.z + row_head) * a.D;
 #pragma unroll
-            for (int i = 0; i < N; i += 32) {
-                uint32_t o[32];
-                if (blocks > 0) {
-                    mm_ld32(o_at + i, o);
-                    mm_ld_wait();
-                    mm_landed(o);
+            for (int i = 0; i < HALVES; ++i) {
+                if (box) {
+                    if (row == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");          // the box before has been read
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
                 }
 #pragma unroll
-                for (int k = 0; k < 32; k += 8) {
-                    uint32_t p[4];
+                for (int n = 0; n < 2; ++n) {
+                    uint32_t o[32];
+                    if (blocks > 0) {
+                        mm_ld32(o_at + 64 * i + 32 * n, o);
+                        mm_ld_wait();
+                        mm_landed(o);
+                    }
 #pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        p[m] = total == 0.f ? 0u : Ty::round2(__uint_as_float(o[k + 2 * m]) * inverse, __uint_as_float(o[k + 2 * m + 1]) * inverse);
-                    if (out && i + k < a.D) *reinterpret_cast<uint4*>(out + i + k) = make_uint4(p[0], p[1], p[2], p[3]);
+                    for (int k = 0; k < 4; ++k) {
+                        uint32_t p[4];
+#pragma unroll
+                        for (int m = 0; m < 4; ++m)
+                            p[m] = total == 0.f ? 0u : Ty::round2(__uint_as_float(o[8 * k + 2 * m]) * inverse, __uint_as_float(o[8 * k + 2 * m + 1]) * inverse);
+                        if (box) *reinterpret_cast<uint4*>(held + row * 128 + ((4 * n + k ^ (row & 7)) * 16)) = make_uint4(p[0], p[1], p[2], p[3]);
+                        else if (out && 64 * i + 32 * n + 8 * k < a.D) *reinterpret_cast<uint4*>(out + 64 * i + 32 * n + 8 * k) = make_uint4(p[0], p[1], p[2], p[3]);
+                    }
+                }
+                if (box) {
+                    fence_proxy_async();
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+                    if (row == 0) {
+                        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                                     ::"l"(reinterpret_cast<uint64_t>(&to)), "r"(smem_u32(held)), "r"(64 * i), "r"(place.z), "r"(place.x) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
                 }
             }
             mm_fence_before();          // the next piece's first product may write over them once its weights are there
         }
+        if (row == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
     }
     __syncthreads();
     if (warp == COPY) {
@@ -495,12 +524,12 @@ bool encode(CUtensorMap* tm, const void* p, bool f16, int n, int heads, int D, l
 }
 
 template <bool F16, int HALVES>
-int launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const Prompt& a, long long ctas, cudaStream_t st)
+int launch(const CUtensorMap (&maps)[4], const Prompt& a, long long ctas, cudaStream_t st)
 {
     auto kernel = prompt_attend_kernel<F16, HALVES>;
-    constexpr int smem = 1024 + (2 + (HALVES == 2 ? 5 : 8)) * HALVES * ROWS * 128;
+    constexpr int smem = 1024 + ((2 + RING) * HALVES + 2) * ROWS * 128;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    return launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), smem, st, tq, tk, tv, a);
+    return launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), smem, st, maps[0], maps[1], maps[2], maps[3], a);
 }
 
 }  // namespace
@@ -537,13 +566,14 @@ extern "C" int bs_attend_prompt(const void* q, long long q_token, long long q_he
     const long long pieces = a.tiles == 1 ? singles : pairs, ctas = pieces < sms ? pieces : sms;
     if (pieces > 0x7fff0000) return BS_ERR_UNSUPPORTED;
     const bool f16 = type == BS_F16;
-    CUtensorMap tq, tk, tv;
+    CUtensorMap maps[4];            // queries, keys, values, outputs
     // without keys nothing is fetched; a map has to have rows all the same
     const int rows_k = Tk > 0 ? Tk : 1, heads_k = Tk > 0 ? heads : 1;
-    if (!encode(&tq, q, f16, T, q_heads, D, q_token, q_head, a.G, a.tokens) || !encode(&tk, k, f16, rows_k, heads_k, D, k_token, k_head, 1, KEYS) ||
-        !encode(&tv, v, f16, rows_k, heads_k, D, v_token, v_head, 1, KEYS))
+    if (!encode(&maps[0], q, f16, T, q_heads, D, q_token, q_head, a.G, a.tokens) || !encode(&maps[1], k, f16, rows_k, heads_k, D, k_token, k_head, 1, KEYS) ||
+        !encode(&maps[2], v, f16, rows_k, heads_k, D, v_token, v_head, 1, KEYS) ||
+        !encode(&maps[3], out, f16, T, q_heads, D, static_cast<long long>(q_heads) * D, D, a.G, a.tokens))
         return BS_ERR_UNSUPPORTED;
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (D <= 64) return f16 ? launch<true, 1>(tq, tk, tv, a, ctas, st) : launch<false, 1>(tq, tk, tv, a, ctas, st);
-    return f16 ? launch<true, 2>(tq, tk, tv, a, ctas, st) : launch<false, 2>(tq, tk, tv, a, ctas, st);
+    if (D <= 64) return f16 ? launch<true, 1>(maps, a, ctas, st) : launch<false, 1>(maps, a, ctas, st);
+    return f16 ? launch<true, 2>(maps, a, ctas, st) : launch<false, 2>(maps, a, ctas, st);
 }
