@@ -342,22 +342,21 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     const uint32_t value_at = tid * (D / 2) + kv4_value_part(D, tid, gid) * (D / 16);
     bool late = false;
 
-    auto take = [&](int k, auto masked) {
+    // A whole unit that all rows see, or one tile `at` of any: code that runs once or twice should be short, it comes from memory.
+    auto take = [&](int k, int at, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
-        const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit) * KV4_TILE, count = min(unit, t1 - first / KV4_TILE);
-        const unsigned flag = flags >> 4 * stage & 15u;
-        uint32_t unit_at = ring_at + stage * UNIT * TILE;
+        constexpr int TILES = MASKED ? 1 : UNIT;
+        const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit + at) * KV4_TILE;
+        const bool there_is = flags >> (4 * stage + at) & 1;
+        uint32_t unit_at = ring_at + (stage * UNIT + at) * TILE;
         asm volatile("" : "+r"(unit_at) : : "memory");
-        float p[UNIT][NT][4], high[NT][2];
-        uint32_t value_step[UNIT][2][G];
+        float p[TILES][NT][4], high[NT][2];
+        uint32_t value_step[TILES][2][G];
 #pragma unroll
         for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
         float step_top = 0.f;
 #pragma unroll
-        for (int t = 0; t < UNIT; ++t) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) p[t][n][0] = p[t][n][1] = p[t][n][2] = p[t][n][3] = -INFINITY;
-            if (MASKED && t >= count) continue;
+        for (int t = 0; t < TILES; ++t) {
             const uint32_t tile = unit_at + t * TILE;
             uint32_t key[2][BLOCKS], step[2][G];
 #pragma unroll
@@ -403,7 +402,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v = sum[n][i];
-                    if (MASKED && (first + t * KV4_TILE + place[i >> 1] >= limit[n][i & 1] || !(flag >> t & 1))) v = -INFINITY;
+                    if (MASKED && (first + t * KV4_TILE + place[i >> 1] >= limit[n][i & 1] || !there_is)) v = -INFINITY;
                     p[t][n][i] = v;
                     high[n][i & 1] = fmaxf(high[n][i & 1], v);
                 }
@@ -413,18 +412,18 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 load_words(tile + KV4_TILE * D + 64 * G + step_at[i], value_step[t][i]);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
-                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && (flag >> t & 1))) step_top = fmaxf(step_top, Ty::lo(value_step[t][i][g]));
+                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && there_is)) step_top = fmaxf(step_top, Ty::lo(value_step[t][i][g]));
             }
         }
         if (a.scores) {
 #pragma unroll
-            for (int t = 0; t < UNIT; ++t)
+            for (int t = 0; t < TILES; ++t)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int r = r0 + n * 8 + 2 * tid + (i & 1), e = first + t * KV4_TILE + place[i >> 1];
-                        if ((!MASKED || t < count) && r < rows && e < a.N)
+                        if (r < rows && e < a.N)
                             a.scores[row_of(r) * a.N + e] = p[t][n][i] * factor[n][i & 1];
                     }
         }
@@ -467,8 +466,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
             for (int i = 0; i < 2; ++i) from[n][i] = top[n][i] == -INFINITY ? 0.f : -top[n][i];
 #pragma unroll
-        for (int t = 0; t < UNIT; ++t) {
-            if (MASKED && t >= count) continue;
+        for (int t = 0; t < TILES; ++t) {
             const uint32_t tile = unit_at + t * TILE;
             uint32_t word[4][words_of<BLOCKS>];
 #pragma unroll
@@ -487,7 +485,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 for (int i = 0; i < 2; ++i) {
                     float st = Ty::lo(value_step[t][i][g]), off = Ty::hi(value_step[t][i][g]);
                     const int e = first + t * KV4_TILE + place[i];
-                    if (MASKED && (e >= s.n || !(flag >> t & 1))) st = off = 0.f;
+                    if (MASKED && (e >= s.n || !there_is)) st = off = 0.f;
                     st *= scaled;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
@@ -525,8 +523,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         }
         const int f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
         const unsigned whole = (1u << count) - 1u;
-        if (count == UNIT && (f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, std::integral_constant<bool, false>());
-        else take(k, std::integral_constant<bool, true>());
+        if (count == UNIT && (f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, 0, std::false_type());
+        else
+#pragma unroll 1
+            for (int i = 0; i < count; ++i) take(k, i, std::true_type());
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll

@@ -5,8 +5,8 @@
 // by side.  Few tokens are spread: sixteen lanes take one, lane 4 w + t a word of 8 channels.
 //
 // A code is the quotient, corrected once, plus 1.5 * 2^23, which leaves the whole number, ties half-even, in the lowest bits.  That is right where the difference
-// x - m is exact and, since it and the borders (c + 1/2) s then lie on a grid, no quotient is nearer to a border than its own rounding; codes_at_borders
-// takes the few words of eight values for which the exponents do not show that.
+// x - m is exact and, since it and the borders (c + 1/2) s then lie on a grid, no quotient is nearer to a border than its own rounding.  Words of eight values
+// for which the exponents do not show that are right where x - m - c s is less than s / 2, and else left to codes_at_borders.
 //
 // Lane t's codes of the keys are part t of their row.  The values' rows hold nibble i of eight channels 8 i + g in part g (kv4.h): the four lanes exchange bytes,
 // and each writes two parts.
@@ -143,19 +143,26 @@ __device__ __forceinline__ void quantise(const uint4* raw, uint32_t* code, uint3
     // differences are exact, and a quotient that is not on a border is 15 * 2^-24 away from it, more than its rounding of 2^-21.  Steps near the ends of binary32 have
     // no reciprocals to use, and steps of few bits (the type's smallest) may leave quotients above 15.
     const float grid = span * (F16 ? 0x1p-14f : 0x1p-17f);
-    const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s && fabsf(m) >= grid;
+    const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        if (!(plain && fminf(Ty::lo(small[w]), Ty::hi(small[w])) >= grid)) {
-            code[w] = codes_at_borders(raw[w], F16, m, s);
-            continue;
-        }
         uint32_t c8[8];
+        float far = 0.f;            // how far the differences are from their codes, where that has to be known
+        const bool sure = fminf(fminf(Ty::lo(small[w]), Ty::hi(small[w])), fabsf(m)) >= grid;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t v = word_of(raw[w], i);
-            const u64 d = f2_add(f2_pack(__float_as_uint(Ty::lo(v)), __float_as_uint(Ty::hi(v))), m2), q = f2_fma(d, inverse2, 0);
-            f2_split(f2_add(f2_fma(f2_fma(q, s2, d), inverse2, q), magic2), c8[2 * i], c8[2 * i + 1]);
+            const u64 d = f2_add(f2_pack(__float_as_uint(Ty::lo(v)), __float_as_uint(Ty::hi(v))), m2), q = f2_fma(d, inverse2, 0), c = f2_add(f2_fma(f2_fma(q, s2, d), inverse2, q), magic2);
+            f2_split(c, c8[2 * i], c8[2 * i + 1]);
+            if (!sure) {
+                uint32_t r0, r1;
+                f2_split(f2_fma(f2_add(c, both(-magic)), s2, d), r0, r1);
+                far = fmaxf(far, fmaxf(fabsf(__uint_as_float(r0)), fabsf(__uint_as_float(r1))));
+            }
+        }
+        if (!plain || !(far < 0.5f * s)) {
+            code[w] = codes_at_borders(raw[w], F16, m, s);
+            continue;
         }
         uint32_t word = c8[7];
 #pragma unroll
