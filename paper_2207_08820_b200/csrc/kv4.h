@@ -9,6 +9,8 @@
 //            4, with the keys' rows the reason why a fragment's loads meet every bank of shared memory once.
 //   steps of the keys, then of the values: 16 entries of G words, the step in the lower half and the offset in the upper one, of the cache's type.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace bs {
@@ -46,6 +48,42 @@ struct Kv4Table {
 };
 
 #ifdef __CUDACC__
+// Lets a kernel have more than 48 KB of shared memory, once a device: the call costs the host half a microsecond.
+template <auto KERNEL>
+inline bool allow_shared(int bytes)
+{
+    static std::atomic<unsigned long long> done{0};
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) { cudaGetLastError(); return false; }
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return true;
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) { cudaGetLastError(); return false; }
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
+// Launch of clusters of `ctas` CTAs that may begin while the kernel before it drains.
+template <typename... P, typename... A>
+inline int launch_clusters(void (*kern)(P...), unsigned ctas, dim3 grid, dim3 block, size_t smem, cudaStream_t st, A... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    if (cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...) != cudaSuccess) {
+        cudaGetLastError();
+        return BS_ERR_CUDA;
+    }
+    return BS_OK;
+}
 __device__ __forceinline__ int kv4_key_row(int r) { return r ^ (r >> 2 & 1); }
 __device__ __forceinline__ int kv4_value_part(int D, int r, int g) { return D == 128 ? g ^ (r >> 1 & 1) << 2 : g; }
 // Entry i's page, -1 where there is none.  The caller has i below width * page.

@@ -23,6 +23,7 @@ namespace {
 #endif
 constexpr int WARPS = 4, STAGES = KV4_STAGES, UNIT = KV4_UNIT;          // tiles of 16 entries that a warp takes at a time
 constexpr int LEAST = KV4_LEAST;                        // tiles of a run, at least
+constexpr int TEAMS = 8;                                // runs of a column, where a cluster joins them
 // CTAs of an SM, as registers and shared memory allow.
 template <int D, int G> constexpr int ring_bytes() { return WARPS * STAGES * UNIT * KV4_TILE * (D + 8 * G); }
 constexpr int ctas_of(int ring, int NT) { return (NT == 1 ? KV4_CTAS : 2) < 227 * 1024 / (ring + 2048) ? (NT == 1 ? KV4_CTAS : 2) : 227 * 1024 / (ring + 2048); }
@@ -127,7 +128,8 @@ template <int C> __device__ __forceinline__ uint32_t pair_of(const uint32_t (&a)
     return C == 3 ? __byte_perm(a[c], b[c], 0x5410) : __byte_perm(a[c / 2], b[c / 2], c & 1 ? 0x7632 : 0x5410);
 }
 
-template <bool F16, int D, int G, int NT>
+// TEAM: the runs of a column are the CTAs of a cluster, which joins them.
+template <bool F16, int D, int G, int NT, bool TEAM>
 __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) kv4_attend_kernel(const __grid_constant__ Attend a)
 {
     typedef W4Type<F16> Ty;
@@ -138,7 +140,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     constexpr int R = 8 * NT, BLOCKS = D / 32, MT = D / 16, TILE = KV4_TILE * (D + 8 * G), PER_G = BLOCKS / G;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[WARPS][STAGES];
-    __shared__ float2 stat[WARPS][R];
+    __shared__ float2 stat[WARPS][R], whole[R];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, gid = lane >> 2, tid = lane & 3;
     if (lane == 0) {
         for (int s = 0; s < STAGES; ++s) mbar_init(&bars[warp][s], 1);
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             int n = 0, r = 1, c = 1;
             if (i0 + lane < a.t.B) {
                 const Seq s(a, lengths, starts, i0 + lane, R);
-                r = max(1, (s.tiles + chunk - 1) / chunk);
+                r = TEAM ? TEAMS : max(1, (s.tiles + chunk - 1) / chunk);
                 c = s.rts * a.l.H;
                 n = r * c;
             }
@@ -190,8 +192,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 runs = __shfl_sync(0xffffffffu, r, who);
                 base = __shfl_sync(0xffffffffu, from, who);
                 c = __shfl_sync(0xffffffffu, c, who);
-                run = (blockIdx.x - base) / c;
-                column = (blockIdx.x - base) - run * c;
+                run = TEAM ? (blockIdx.x - base) % TEAMS : (blockIdx.x - base) / c;
+                column = TEAM ? (blockIdx.x - base) / TEAMS : (blockIdx.x - base) - run * c;
                 found = true;
             }
             before += __shfl_sync(0xffffffffu, sum, 31);
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     auto token_of = [&](int r) { return fdiv(r, a.d_per); };                // of the sequence's query tokens, the one of row r
     const int h = column - fdiv(column, a.d_heads) * a.l.H, r0 = fdiv(column, a.d_heads) * R, rows = s.tq * a.per;
     auto row_of = [&](int r) { return static_cast<long long>(s.first + token_of(r)) * a.Hq + h * a.per + r - token_of(r) * a.per; };       // of q and out
-    if (column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
+    if (!TEAM && column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
 
     // how many entries a row sees; rows behind the last one see all and are dropped
     int limit[NT][2];
@@ -537,8 +539,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 
     // the warps' parts: rows of outputs [R][D], put together in the ring's memory
     __syncthreads();
-    float* outs = reinterpret_cast<float*>(smem);
     constexpr int PITCH = D + 4;
+    float *outs = reinterpret_cast<float*>(smem), *joined = outs + WARPS * R * PITCH;
     const float back = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);       // and codes were in units of 2^-24, in rows gid + 8 of 2^-20
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -573,6 +575,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             sum = fmaf(stat[w][r].y, f, sum);
             v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
         }
+        if (TEAM) {
+            *reinterpret_cast<float4*>(joined + r * D + d) = v;
+            if (d == 0) whole[r] = make_float2(m, sum);
+            continue;
+        }
         if (row >= rows) continue;
         if (runs == 1) {
             const long long at = row_of(row);
@@ -584,6 +591,41 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             *reinterpret_cast<float4*>(a.part + (static_cast<long long>(blockIdx.x) * R + r) * D + d) = v;
             if (d == 0) a.stat[static_cast<long long>(blockIdx.x) * R + r] = make_float2(m, sum);
         }
+    }
+    if (TEAM) {
+        __syncwarp();
+        mm_cluster_sync();
+        for (int i = run * (WARPS * 32) + threadIdx.x; i < R * (D / 4); i += TEAMS * WARPS * 32) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4, row = r0 + r;
+            float2 st[TEAMS];
+            float4 x[TEAMS], v = make_float4(0.f, 0.f, 0.f, 0.f);
+            float m = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < TEAMS; ++c) {
+                uint32_t at;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&whole[r])), "r"(c));
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(st[c].x), "=f"(st[c].y) : "r"(at));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(joined + r * D + d)), "r"(c));
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[c].x), "=f"(x[c].y), "=f"(x[c].z), "=f"(x[c].w) : "r"(at));
+            }
+#pragma unroll
+            for (int c = 0; c < TEAMS; ++c) m = fmaxf(m, st[c].x);
+#pragma unroll
+            for (int c = 0; c < TEAMS; ++c) {
+                const bool empty = st[c].x == -INFINITY && st[c].y == 0.f;
+                const float f = empty ? 0.f : exp2_of(st[c].x - m);
+                sum = fmaf(st[c].y, f, sum);
+                v.x = fmaf(x[c].x, f, v.x); v.y = fmaf(x[c].y, f, v.y); v.z = fmaf(x[c].z, f, v.z); v.w = fmaf(x[c].w, f, v.w);
+            }
+            if (row >= rows) continue;
+            const long long at = row_of(row);
+            const float inverse = sum == 0.f ? 0.f : 1.f / sum;
+            uint32_t* to = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(a.out) + at * D + d);
+            *reinterpret_cast<uint2*>(to) = make_uint2(Ty::round2(v.x * inverse, v.y * inverse), Ty::round2(v.z * inverse, v.w * inverse));
+            if (a.scores && d == 0) a.lse[at] = sum == 0.f ? INFINITY : m + log2f(sum);
+        }
+        __syncwarp();
+        mm_cluster_sync();          // nobody leaves while its memory is read
     }
 }
 
@@ -668,6 +710,7 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant_
 // Tiles of rows and runs that a call may have, and its workspace.
 struct Plan {
     int NT, slots;
+    bool team;
     long long runs;
     size_t part, stat, info, lse, scores;
     size_t bytes() const { return part + stat + info + lse + scores; }
@@ -682,6 +725,9 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
     const long long columns = starts ? l.H * (ceil_div_ll(static_cast<long long>(T) * per, R) + B) : static_cast<long long>(l.H) * B * ceil_div(per, R);
     const long long cuts = ceil_div_ll(static_cast<long long>(width) * l.page, LEAST * KV4_TILE), most = runs_of(columns, p.slots);
     p.runs = cuts < most / columns + 1 ? (columns * cuts < most ? columns * cuts : most) : most;
+    // Short sequences of few columns: a cluster a column, which spares the second launch (1 x 1000 entries 8.8 us with it)
+    p.team = static_cast<long long>(width) * l.page <= TEAMS * 512 && columns * TEAMS <= p.slots;
+    if (p.team) p.runs = columns * TEAMS;
     if (p.runs > 0x7fffffff / (R * 2)) return false;
     auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };
     p.part = up(p.runs * R * l.D * 4);
@@ -695,10 +741,11 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
 template <bool F16, int D, int G, int NT>
 int launch(const Attend& a, const Plan& p, cudaStream_t st)
 {
-    auto kernel = kv4_attend_kernel<F16, D, G, NT>;
-    constexpr int ring = ring_bytes<D, G>(), parts = WARPS * 8 * NT * (D + 4) * 4, smem = ring > parts ? ring : parts;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    return launch_dependent(kernel, dim3(static_cast<unsigned>(p.runs)), dim3(WARPS * 32), smem, st, a);
+    constexpr int ring = ring_bytes<D, G>(), parts = (WARPS * (D + 4) + D) * 8 * NT * 4, smem = ring > parts ? ring : parts;
+    const dim3 grid(static_cast<unsigned>(p.runs)), block(WARPS * 32);
+    if (p.team)
+        return allow_shared<kv4_attend_kernel<F16, D, G, NT, true>>(smem) ? launch_clusters(kv4_attend_kernel<F16, D, G, NT, true>, TEAMS, grid, block, smem, st, a) : BS_ERR_CUDA;
+    return allow_shared<kv4_attend_kernel<F16, D, G, NT, false>>(smem) ? launch_dependent(kv4_attend_kernel<F16, D, G, NT, false>, grid, block, smem, st, a) : BS_ERR_CUDA;
 }
 template <bool F16, int D, int G>
 int launch_rows(const Attend& a, const Plan& p, cudaStream_t st) { return p.NT == 1 ? launch<F16, D, G, 1>(a, p, st) : launch<F16, D, G, 2>(a, p, st); }
@@ -711,7 +758,7 @@ int launch_form(const Attend& a, const Plan& p, cudaStream_t st)
     else rc = a.l.G == 1 ? launch_rows<F16, 128, 1>(a, p, st) : a.l.G == 2 ? launch_rows<F16, 128, 2>(a, p, st) : launch_rows<F16, 128, 4>(a, p, st);
     if (rc != BS_OK) return rc;
     // no sequence is cut where none can be longer than a run
-    if (static_cast<long long>(a.t.width) * a.l.page > LEAST * KV4_TILE) {
+    if (!p.team && static_cast<long long>(a.t.width) * a.l.page > LEAST * KV4_TILE) {
         const dim3 grid(a.T, a.Hq);
         rc = a.l.D == 64 ? launch_dependent(kv4_join_kernel<F16, 64>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
              : a.l.D == 96 ? launch_dependent(kv4_join_kernel<F16, 96>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))

@@ -226,25 +226,7 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const __grid_constant__ E
 }
 
 template <int CTAS>
-int launch_select(const Evict& a, int B, cudaStream_t st)
-{
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(CTAS, a.l.H, B);
-    cfg.blockDim = dim3(THREADS);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim = {CTAS, 1, 1};
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, kv4_select_kernel<CTAS>, a) != cudaSuccess) {
-        cudaGetLastError();
-        return BS_ERR_CUDA;
-    }
-    return BS_OK;
-}
+int launch_select(const Evict& a, int B, cudaStream_t st) { return launch_clusters(kv4_select_kernel<CTAS>, CTAS, dim3(CTAS, a.l.H, B), dim3(THREADS), 0, st, a); }
 
 }  // namespace
 }  // namespace bs

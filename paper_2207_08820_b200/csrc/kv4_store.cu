@@ -135,8 +135,12 @@ __device__ __forceinline__ void quantise(const uint4* raw, uint32_t* code, uint3
         for (int w = 0; w < W; ++w) code[w] = 0;
         return;
     }
-    step = Ty::round2(__fdiv_rn(span, 15.f), m);
-    const float s = Ty::lo(step), inverse = __frcp_rn(s), magic = 12582912.f;       // 1.5 * 2^23
+    // span / 15 rounded as a division rounds it: a quotient by the rounded reciprocal, corrected by its remainder (Markstein), right for all numbers that have an exact one
+    const float fifteenth = 0x1.111112p-4f, near15 = span * fifteenth, part15 = span < 0x1p-90f ? __fdiv_rn(span, 15.f) : fmaf(fmaf(near15, -15.f, span), fifteenth, near15);
+    step = Ty::round2(part15, m);
+    const float s = Ty::lo(step), magic = 12582912.f;       // 1.5 * 2^23
+    float inverse;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(s));
     auto both = [](float v) { return f2_pack(__float_as_uint(v), __float_as_uint(v)); };
     const u64 m2 = both(-m), s2 = both(-s), inverse2 = both(inverse), magic2 = both(magic);
     // A value of 2^-14 (bf16: 2^-17) of the span or more is a multiple of 2^-24 of it, as the type has 11 (8) bits; with such values and such an offset

@@ -526,10 +526,9 @@ bool encode(CUtensorMap* tm, const void* p, bool f16, int n, int heads, int D, l
 template <bool F16, int HALVES>
 int launch(const CUtensorMap (&maps)[4], const Prompt& a, long long ctas, cudaStream_t st)
 {
-    auto kernel = prompt_attend_kernel<F16, HALVES>;
     constexpr int smem = 1024 + ((2 + RING) * HALVES + 2) * ROWS * 128;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) { cudaGetLastError(); return BS_ERR_CUDA; }
-    return launch_dependent(kernel, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), smem, st, maps[0], maps[1], maps[2], maps[3], a);
+    if (!allow_shared<prompt_attend_kernel<F16, HALVES>>(smem)) return BS_ERR_CUDA;
+    return launch_dependent(prompt_attend_kernel<F16, HALVES>, dim3(static_cast<unsigned>(ctas)), dim3(THREADS), smem, st, maps[0], maps[1], maps[2], maps[3], a);
 }
 
 }  // namespace
