@@ -15,18 +15,12 @@
 namespace bs {
 namespace {
 
-#ifndef KV4_UNIT
-#define KV4_UNIT 4
-#define KV4_STAGES 2
-#define KV4_CTAS 3
-#define KV4_LEAST 8
-#endif
-constexpr int WARPS = 4, STAGES = KV4_STAGES, UNIT = KV4_UNIT;          // tiles of 16 entries that a warp takes at a time
-constexpr int LEAST = KV4_LEAST;                        // tiles of a run, at least
-constexpr int TEAMS = 8;                                // runs of a column, where a cluster joins them
-// CTAs of an SM, as registers and shared memory allow.
+constexpr int WARPS = 4, STAGES = 2, UNIT = 4;          // tiles of 16 entries that a warp takes at a time; with two 64 sequences take 20 % more
+constexpr int LEAST = 8;                                // tiles of a run, at least
+// CTAs of an SM, as registers and shared memory allow.  A fourth one needs 128 registers a thread and units of two tiles: 25 % more.
 template <int D, int G> constexpr int ring_bytes() { return WARPS * STAGES * UNIT * KV4_TILE * (D + 8 * G); }
-constexpr int ctas_of(int ring, int NT) { return (NT == 1 ? KV4_CTAS : 2) < 227 * 1024 / (ring + 2048) ? (NT == 1 ? KV4_CTAS : 2) : 227 * 1024 / (ring + 2048); }
+constexpr int ctas_of(int ring, int NT) { return (NT == 1 ? 3 : 2) < 227 * 1024 / (ring + 2048) ? (NT == 1 ? 3 : 2) : 227 * 1024 / (ring + 2048); }
+constexpr int TEAMS = 8;                                // runs of a column, where a cluster joins them
 
 struct Attend {
     Kv4 l;
@@ -725,8 +719,10 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
     const long long columns = starts ? l.H * (ceil_div_ll(static_cast<long long>(T) * per, R) + B) : static_cast<long long>(l.H) * B * ceil_div(per, R);
     const long long cuts = ceil_div_ll(static_cast<long long>(width) * l.page, LEAST * KV4_TILE), most = runs_of(columns, p.slots);
     p.runs = cuts < most / columns + 1 ? (columns * cuts < most ? columns * cuts : most) : most;
-    // Short sequences of few columns: a cluster a column, which spares the second launch (1 x 1000 entries 8.8 us with it)
-    p.team = static_cast<long long>(width) * l.page <= TEAMS * 512 && columns * TEAMS <= p.slots;
+    // Few columns, of sequences so short that runs for the whole GPU would spare a warp no more than two turns of 1.2 us: a cluster a column, which spares the second
+    // launch (1 x 1000 entries 8.8 us with it, 6.7 without)
+    const long long tiles = ceil_div_ll(static_cast<long long>(width) * l.page, KV4_TILE), turn = WARPS * UNIT;
+    p.team = columns * TEAMS <= p.slots && ceil_div_ll(tiles, TEAMS * turn) <= ceil_div_ll(tiles * columns, p.slots * turn) + 2;
     if (p.team) p.runs = columns * TEAMS;
     if (p.runs > 0x7fffffff / (R * 2)) return false;
     auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };

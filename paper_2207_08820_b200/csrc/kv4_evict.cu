@@ -60,6 +60,17 @@ __device__ __forceinline__ uint32_t up_to_lane(uint32_t s)
     }
     return s;
 }
+// Four neighbouring weights, of those below `to`; others as keys that come last.
+__device__ __forceinline__ void load4(const float* w, int i, int to, bool vectors, float (&v)[4])
+{
+    if (vectors && i + 4 <= to) {
+        const float4 x = *reinterpret_cast<const float4*>(w + i);
+        v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = i + j < to ? w[i + j] : 0.f;
+    }
+}
 // Sum over the threads before this one; all: over all of them.  32 warps.
 __device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* sums, uint32_t& all)
 {
@@ -89,7 +100,9 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
     int32_t* kept = a.kept + head * a.keep;
     float* out = a.weights_out + head * a.N;
     const int stay = min(n, a.keep), old = n > a.keep ? n - a.recent : 0, need = n > a.keep ? a.keep - a.recent : 0;
-    const int from = static_cast<int>(static_cast<long long>(old) * rank / CTAS), to = static_cast<int>(static_cast<long long>(old) * (rank + 1) / CTAS);
+    // the CTA's part, in fours
+    const int from = static_cast<int>(static_cast<long long>(old) * rank / CTAS) & ~3, to = rank + 1 == CTAS ? old : static_cast<int>(static_cast<long long>(old) * (rank + 1) / CTAS) & ~3;
+    const bool vectors = (reinterpret_cast<uintptr_t>(w) & 15) == 0;
     if (need > 0) {
         for (int i = th; i < 3 * BINS; i += THREADS) (&bins[0][0])[i] = 0;
         __syncthreads();
@@ -97,10 +110,15 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, wide = pass == 2 ? 10 : 11;
-#pragma unroll 8
-            for (int i = from + th; i < to; i += THREADS) {
-                const uint32_t k = key_of(w[i]);
-                if (pass == 0 || k >> (shift + wide) == prefix) atomicAdd(&bins[pass][k >> shift & ((1u << wide) - 1)], 1u);
+#pragma unroll 4
+            for (int i = from + 4 * th; i < to; i += 4 * THREADS) {
+                float v[4];
+                load4(w, i, to, vectors, v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t k = key_of(v[j]);
+                    if (i + j < to && (pass == 0 || k >> (shift + wide) == prefix)) atomicAdd(&bins[pass][k >> shift & ((1u << wide) - 1)], 1u);
+                }
             }
             sync();
             const uint32_t* count = bins[pass];
@@ -135,11 +153,16 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
         uint32_t at_more = 0, at_equal = 0;
         if (CTAS > 1) {
             uint32_t more = 0, equal = 0;
-#pragma unroll 8
-            for (int i = from + th; i < to; i += THREADS) {
-                const uint32_t k = key_of(w[i]);
-                more += k > prefix;
-                equal += k == prefix;
+#pragma unroll 4
+            for (int i = from + 4 * th; i < to; i += 4 * THREADS) {
+                float v[4];
+                load4(w, i, to, vectors, v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t k = key_of(v[j]);
+                    more += i + j < to && k > prefix;
+                    equal += i + j < to && k == prefix;
+                }
             }
             uint32_t all_more, all_equal;
             before_me(more, sums, all_more);
@@ -152,15 +175,28 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
             }
             sync();             // nobody leaves while its memory is read
         }
-        for (int i0 = from; i0 < to; i0 += THREADS) {
-            const int i = i0 + th;
-            const float v = i < to ? w[i] : 0.f;
-            const uint32_t k = key_of(v), is_more = i < to && k > prefix, is_equal = i < to && k == prefix;
-            uint32_t all;
-            const uint32_t front = before_me(is_more | is_equal << 16, sums, all), e = at_equal + (front >> 16), place = at_more + (front & 0xffff) + min(e, left);
-            if (is_more || (is_equal && e < left)) {
-                kept[place] = i;
-                out[place] = v;
+        for (int i0 = from; i0 < to; i0 += 4 * THREADS) {
+            const int i = i0 + 4 * th;
+            float v[4];
+            load4(w, i, to, vectors, v);
+            uint32_t k[4], mine_of = 0, all;            // how many above in the lower half, how many equal in the upper one
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                k[j] = key_of(v[j]);
+                if (i + j < to) mine_of += (k[j] > prefix) | (k[j] == prefix) << 16;
+            }
+            const uint32_t front = before_me(mine_of, sums, all);
+            uint32_t e = at_equal + (front >> 16), m = at_more + (front & 0xffff);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool above = i + j < to && k[j] > prefix, same = i + j < to && k[j] == prefix;
+                if (above || (same && e < left)) {
+                    const uint32_t place = m + min(e, left);
+                    kept[place] = i + j;
+                    out[place] = v[j];
+                }
+                m += above;
+                e += same;
             }
             at_more += all & 0xffff;
             at_equal += all >> 16;

@@ -68,17 +68,33 @@ __device__ __forceinline__ uint32_t spread(uint32_t w)
     return (w | w << 4) & 0x0f0f0f0fu;
 }
 
-// Codes of eight values of a group that has least value m and step s, whatever they are.
-__device__ __noinline__ uint32_t codes_at_borders(uint4 raw, bool f16, float m, float s)
+// Codes of eight values of a group that has least value m and step s, whatever they are; plain: the step is far from the ends of binary32 and no quotient is above
+// 15.5.  Few words come here, so it is no part of their loop.
+template <bool F16>
+__device__ __noinline__ uint32_t codes_at_borders(uint4 raw, float m, float s, float inverse, bool plain)
 {
-    // steps near the ends of binary32 are brought to where their reciprocals and products are exact
-    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, half = 0.5f * t, inverse = __frcp_rn(t);
+    typedef W4Type<F16> Ty;
+    const float half_step = 0.5f * s;
     uint32_t word = 0;
+    if (plain) {            // all differences within half a step of their codes: no question of ties
+        float far = 0.f;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const uint32_t w = word_of(raw, i >> 1);
+            const float d = (i & 1 ? Ty::hi(w) : Ty::lo(w)) - m, c = rintf(d * inverse);
+            far = fmaxf(far, fabsf(fmaf(-c, s, d)));
+            word = word * 16 + static_cast<uint32_t>(c);
+        }
+        if (far < half_step) return word;
+        word = 0;
+    }
+    // steps near the ends of binary32 are brought to where their reciprocals and products are exact
+    const float up = s < 0x1p-60f ? 0x1p64f : s > 0x1p60f ? 0x1p-64f : 1.f, t = s * up, half = 0.5f * t, over = __frcp_rn(t);
 #pragma unroll 1
     for (int i = 7; i >= 0; --i) {
         const uint32_t w = i >= 6 ? raw.w : i >= 4 ? raw.z : i >= 2 ? raw.y : raw.x;
-        const float x = f16 ? (i & 1 ? W4Type<true>::hi(w) : W4Type<true>::lo(w)) : (i & 1 ? W4Type<false>::hi(w) : W4Type<false>::lo(w)), d = x - m, e = d * up;
-        float c = fminf(rintf(e * inverse), 15.f);
+        const float x = i & 1 ? Ty::hi(w) : Ty::lo(w), d = x - m, e = d * up;
+        float c = fminf(rintf(e * over), 15.f);
         const float rest = fmaf(-c, t, e), back = x - d, lost = (x - (d + back)) + (back - m);         // of the difference, exact
         const bool odd = static_cast<int>(c) & 1;
         if (rest > half || (rest == half && (lost > 0.f || (lost == 0.f && odd)))) c += 1.f;
@@ -150,23 +166,16 @@ __device__ __forceinline__ void quantise(const uint4* raw, uint32_t* code, uint3
     const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
+        if (!(plain && fminf(fminf(Ty::lo(small[w]), Ty::hi(small[w])), fabsf(m)) >= grid)) {
+            code[w] = codes_at_borders<F16>(raw[w], m, s, inverse, plain);
+            continue;
+        }
         uint32_t c8[8];
-        float far = 0.f;            // how far the differences are from their codes, where that has to be known
-        const bool sure = fminf(fminf(Ty::lo(small[w]), Ty::hi(small[w])), fabsf(m)) >= grid;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t v = word_of(raw[w], i);
-            const u64 d = f2_add(f2_pack(__float_as_uint(Ty::lo(v)), __float_as_uint(Ty::hi(v))), m2), q = f2_fma(d, inverse2, 0), c = f2_add(f2_fma(f2_fma(q, s2, d), inverse2, q), magic2);
-            f2_split(c, c8[2 * i], c8[2 * i + 1]);
-            if (!sure) {
-                uint32_t r0, r1;
-                f2_split(f2_fma(f2_add(c, both(-magic)), s2, d), r0, r1);
-                far = fmaxf(far, fmaxf(fabsf(__uint_as_float(r0)), fabsf(__uint_as_float(r1))));
-            }
-        }
-        if (!plain || !(far < 0.5f * s)) {
-            code[w] = codes_at_borders(raw[w], F16, m, s);
-            continue;
+            const u64 d = f2_add(f2_pack(__float_as_uint(Ty::lo(v)), __float_as_uint(Ty::hi(v))), m2), q = f2_fma(d, inverse2, 0);
+            f2_split(f2_add(f2_fma(f2_fma(q, s2, d), inverse2, q), magic2), c8[2 * i], c8[2 * i + 1]);
         }
         uint32_t word = c8[7];
 #pragma unroll

@@ -177,25 +177,32 @@ def check_attend(f, counts, per, seed=5, starts=True, weights=False, scale=None,
     return out
 
 
+# Tables that end with the longest sequence, and ones that could hold many times as much: short and long ones are cut and joined in different ways.
+ROOM = pytest.mark.parametrize("room", [0, 20000], ids=["narrow", "wide"])
+
+
+@ROOM
 @pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
 @pytest.mark.parametrize("D,page,group", LAYOUTS)
-def test_attend_single_tokens(D, page, group, dtype):
+def test_attend_single_tokens(D, page, group, dtype, room):
     """Lengths around tiles, units and runs; a group of heads that fills half a fragment."""
-    f = Filled(6, [1, 2, 15, 16, 17, 63, 64, 65, 128, 129, 300, 1111], 2, D, page, group, dtype)
+    f = Filled(6, [1, 2, 15, 16, 17, 63, 64, 65, 128, 129, 300, 1111], 2, D, page, group, dtype, room=room // page)
     check_attend(f, [1] * 12, 4, starts=False)
 
 
+@ROOM
 @pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
 @pytest.mark.parametrize("per", [1, 7, 8, 9, 16, 40])
-def test_attend_grouped_heads(per, dtype):
-    f = Filled(7, [77, 1, 530], 2, 64 if per == 40 else 128, 16, 32, dtype)
+def test_attend_grouped_heads(per, dtype, room):
+    f = Filled(7, [77, 1, 530], 2, 64 if per == 40 else 128, 16, 32, dtype, room=room // 16)
     check_attend(f, [1, 1, 1], per, starts=False, weights=True)
 
 
+@ROOM
 @pytest.mark.parametrize("D,page,group", LAYOUTS)
-def test_attend_several_tokens(D, page, group):
+def test_attend_several_tokens(D, page, group, room):
     """As many tokens as entries, more than rows of a tile, none, and one; attention of the entries."""
-    f = Filled(8, [5, 70, 33, 260, 700], 2, D, page, group, BF16)
+    f = Filled(8, [5, 70, 33, 260, 700], 2, D, page, group, BF16, room=room // page)
     check_attend(f, [5, 3, 0, 20, 1], 3, weights=True)
 
 
@@ -228,9 +235,10 @@ def test_attend_values_of_any_size():
     assert (check_attend(f, [1], 4, starts=False) == 2.5).all()
 
 
-def test_attend_nothing():
+@ROOM
+def test_attend_nothing(room):
     """Sequences of no entries, rows that see none, tokens of no sequence."""
-    f = Filled(13, [0, 2, 40], 2, 64, 16, 64, BF16)
+    f = Filled(13, [0, 2, 40], 2, 64, 16, 64, BF16, room=room // 16)
     q = torch.randn(9, 4, 64, device="cuda").to(BF16)
     out = torch.full_like(q, GUARD)
     w = torch.zeros(3, 2, 40, device="cuda")
@@ -265,8 +273,9 @@ def test_attend_missing_pages_and_lengths_beyond_the_table():
         assert ((api.attend_kv4(q.cuda(), cache, f.table, ints([n])).cpu().double() - want).abs() <= far).all()
 
 
-def test_starts_in_disorder_touch_nothing_else():
-    f = Filled(15, [300, 40, 700], 2, 64, 16, 64, BF16)
+@ROOM
+def test_starts_in_disorder_touch_nothing_else(room):
+    f = Filled(15, [300, 40, 700], 2, 64, 16, 64, BF16, room=room // 16)
     q = torch.randn(8, 4, 64, device="cuda").to(BF16)
     room = torch.full((10, 4, 64), GUARD, dtype=BF16, device="cuda")
     before = f.cache.data.clone()
@@ -276,9 +285,10 @@ def test_starts_in_disorder_touch_nothing_else():
     assert (room[0] == GUARD).all() and (room[9] == GUARD).all() and torch.equal(f.cache.data, before)
 
 
-def test_nan_stays_where_it_belongs():
+@ROOM
+def test_nan_stays_where_it_belongs(room):
     """A stored NaN reaches the rows that see its entry, the values' only in its group; queries' only their own row."""
-    f = Filled(16, [90, 90], 2, 128, 16, 32, F16, fill=False)
+    f = Filled(16, [90, 90], 2, 128, 16, 32, F16, fill=False, room=room // 16)
     f.v[0][80, 0, 40] = math.inf
     f.k[1][3, 1, 7] = math.nan
     api.append_kv4(torch.cat(f.k).cuda(), torch.cat(f.v).cuda(), f.cache, f.table, ints([0, 0]), ints([0, 90, 180]))
@@ -309,9 +319,10 @@ def test_shared_pages_strided_tables_and_repeated_calls():
         assert torch.equal(first, check_attend(f, [1, 1], 4, starts=False, weights=True))
 
 
-def test_streams_and_graphs():
+@ROOM
+def test_streams_and_graphs(room):
     """Calls on a named stream, two at once, and a captured step that is replayed with other lengths, queries and tables."""
-    f = Filled(18, [2000, 40, 700], 2, 128, 64, 128, BF16)
+    f = Filled(18, [2000, 40, 700], 2, 128, 64, 128, BF16, room=room // 64)
     lengths, q = ints(f.lengths), torch.randn(3, 8, 128, device="cuda").to(BF16)
     want = api.attend_kv4(q, f.cache, f.table, lengths).clone()
     torch.cuda.synchronize()
