@@ -508,7 +508,8 @@ size_t bs_kv4_page_bytes(int heads, int D, int page, int group);
 
 /*
  * bs_kv4_append -- keys and values of new tokens into a cache.  k, v: device, T rows of `heads` vectors of D values of the cache's type, rows k_token (v_token)
- * and heads k_head (v_head) values apart.  Row j of sequence b becomes its entry at[b] + j (at: device int32 [B]).  Entries behind the table are not stored.
+ * and heads k_head (v_head) values apart.  Row j of sequence b becomes its entry at[b] + j (at: device int32 [B]).  Entries behind the table are not stored.  No
+ * entry may be stored twice by one call.
  * bs_kv4_read -- the same entries out of a cache: k, v [T][heads][D] of its type, c s + m in binary32, rounded once.  Rows whose entry is not there are zero.
  */
 int bs_kv4_append(const void* k, long long k_token, long long k_head, const void* v, long long v_token, long long v_head, int T, const bs_kv4_cache* cache,
@@ -525,7 +526,8 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *   out      device [T][q_heads][D]: softmax(scale q K^T) V, scale > 0
  *   weights  device float [B][heads][N], rows weights_head and weights_sequence values apart, or NULL: the attention that each entry got, summed over the rows of q
  *            and the heads that share it, is added to it.  Entries from N on are left out.
- *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights); two calls that may run at the same time need one each
+ *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights; 0 and NULL for few short sequences); two calls that may run
+ *              at the same time need one each
  * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms (one, 11 bits, where the
  * output is bf16); the same call gives the same bits every time.
  */

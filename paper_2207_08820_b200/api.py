@@ -432,20 +432,16 @@ def cache_kv4(pages: int, heads: int, D: int, *, page: int = 64, group: Optional
 def append_kv4(k: torch.Tensor, v: torch.Tensor, cache: KV4Cache, table: torch.Tensor, at: torch.Tensor, starts: Optional[torch.Tensor] = None, *, stream=None) -> None:
     """Stores keys and values [T, heads, D] of new tokens in the cache (``bs_kv4_append``): token j of sequence b as its entry ``at[b] + j``.  ``starts`` int32
     [sequences + 1] says whose the tokens are; without it each sequence has one.  Tokens and heads may be apart (views of a fused projection)."""
-    global launch_count
     _check(native().kv4_append(k, v, *cache._native, table, at, starts, stream), "bs_kv4_append")
-    launch_count += 1
 
 
 def read_kv4(cache: KV4Cache, table: torch.Tensor, at: torch.Tensor, starts: Optional[torch.Tensor] = None, total: Optional[int] = None, *, stream=None):
     """The keys and values [T, heads, D] that the cache holds (``bs_kv4_read``): of sequence b its entries from ``at[b]`` on, as many as ``starts`` says (``total``: how
     many in all, starts' last value), or one each."""
-    global launch_count
     if (starts is None) != (total is None):
         raise ValueError("starts and their total, or neither, expected")
     st, k, v = native().kv4_read(*cache._native, table, at, starts, total if total is not None else 0, stream)
     _check(st, "bs_kv4_read")
-    launch_count += 1
     return k, v
 
 
@@ -455,9 +451,9 @@ def attend_kv4(q: torch.Tensor, cache: KV4Cache, table: torch.Tensor, lengths: t
     ``lengths`` int32 [sequences], those of the tokens themselves included; each sees the entries up to its own.  ``scale``: 1 / sqrt(D) unless given.
     ``weights`` float32 [sequences, heads, entries]: what each entry got is added to it (for :func:`evict_kv4`).  No gradients."""
     global launch_count
-    st, o = native().kv4_attend(q, *cache._native, table, lengths, starts, cache.D ** -0.5 if scale is None else scale, weights, out, stream)
+    st, o, launches = native().kv4_attend(q, *cache._native, table, lengths, starts, cache.D ** -0.5 if scale is None else scale, weights, out, stream)
     _check(st, "bs_kv4_attend")
-    launch_count += 2 if weights is None else 3
+    launch_count += launches - 1
     return o
 
 
@@ -468,7 +464,7 @@ def evict_kv4(cache: KV4Cache, table: torch.Tensor, lengths: torch.Tensor, weigh
     global launch_count
     st, n, w, kept = native().kv4_evict(*cache._native, table, lengths, weights, keep, recent, into, stream)
     _check(st, "bs_kv4_evict")
-    launch_count += 3 if into is None else 2
+    launch_count += 2 if into is None else 1
     return n, w, kept
 
 
@@ -477,12 +473,10 @@ def attend_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: Opt
     """Attention of whole prompts (``bs_attend_prompt``): q [T, q_heads, D], k and v [Tk, heads, D], float16 or bfloat16, sequences one behind the other as ``starts`` and
     ``starts_k`` (int32 [sequences + 1]; None: those of q) say, or a single one.  Causal: the last row of q sees all keys, each one before it one fewer.
     Tokens and heads may be apart.  Rows that no sequence holds are not written.  No gradients."""
-    global launch_count
     if starts is not None and starts_k is None:
         starts_k = starts
     st, o = native().attend_prompt(q, k, v, starts, starts_k, q.shape[-1] ** -0.5 if scale is None else scale, causal, out, stream)
     _check(st, "bs_attend_prompt")
-    launch_count += 1
     return o
 
 

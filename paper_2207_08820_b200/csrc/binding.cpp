@@ -728,18 +728,20 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
         } else {
             out = fresh(q.sizes(), q.scalar_type(), data);
         }
-        if (T == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_OK), give(out));
-        const size_t bytes = bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, t.width, N);
-        if (bytes == 0) return Py_BuildValue("(iN)", static_cast<int>(BS_ERR_UNSUPPORTED), give(out));
-        const at::Tensor ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, data);
-        void *op = out.data_ptr(), *wsp = ws.data_ptr();
+        if (T == 0) return Py_BuildValue("(iNi)", static_cast<int>(BS_OK), give(out), 0);
+        // runs that a second launch joins are what a call without weights asks memory for
+        const size_t runs = bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, t.width, 0),
+                     bytes = N > 0 ? bs_kv4_attend_workspace_bytes(&c, t.B, T, heads, starts != nullptr, t.width, N) : runs;
+        at::Tensor ws;
+        if (bytes) ws = fresh({static_cast<int64_t>(bytes)}, at::kByte, data);
+        void *op = out.data_ptr(), *wsp = bytes ? ws.data_ptr() : nullptr;
         int rc;
         on.keep({a[0], a[1], r[0], r[1], r[2], r[4], r[5]});
         {
             NoGil free;
             rc = bs_kv4_attend(qv.p, qv.token, qv.head, T, heads, &c, t.pages, t.pitch, t.width, t.B, lengths, starts, scale, op, wp, w_sequence, w_head, N, wsp, bytes, on.stream);
         }
-        return Py_BuildValue("(iN)", rc, give(out));
+        return Py_BuildValue("(iNi)", rc, give(out), 1 + (runs > 0) + (N > 0));
     });
 }
 

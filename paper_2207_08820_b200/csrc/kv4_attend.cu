@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     auto token_of = [&](int r) { return fdiv(r, a.d_per); };                // of the sequence's query tokens, the one of row r
     const int h = column - fdiv(column, a.d_heads) * a.l.H, r0 = fdiv(column, a.d_heads) * R, rows = s.tq * a.per;
     auto row_of = [&](int r) { return static_cast<long long>(s.first + token_of(r)) * a.Hq + h * a.per + r - token_of(r) * a.per; };       // of q and out
-    if (!TEAM && column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
+    if (!TEAM && a.info && column == 0 && run == 0 && threadIdx.x == 0) a.info[b] = make_int4(base, runs, s.rts * a.l.H, 0);
 
     // how many entries a row sees; rows behind the last one see all and are dropped
     int limit[NT][2];
@@ -704,7 +704,7 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant_
 // Tiles of rows and runs that a call may have, and its workspace.
 struct Plan {
     int NT, slots;
-    bool team;
+    bool team, join;            // joined by clusters; or, where a sequence may be longer than a run, by a second launch
     long long runs;
     size_t part, stat, info, lse, scores;
     size_t bytes() const { return part + stat + info + lse + scores; }
@@ -726,9 +726,10 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
     if (p.team) p.runs = columns * TEAMS;
     if (p.runs > 0x7fffffff / (R * 2)) return false;
     auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };
-    p.part = up(p.runs * R * l.D * 4);
-    p.stat = up(p.runs * R * 8);
-    p.info = up(static_cast<long long>(B) * 16);
+    p.join = !p.team && cuts > 1;
+    p.part = p.join ? up(p.runs * R * l.D * 4) : 0;
+    p.stat = p.join ? up(p.runs * R * 8) : 0;
+    p.info = p.join ? up(static_cast<long long>(B) * 16) : 0;
     p.lse = N > 0 ? up(static_cast<long long>(T) * Hq * 4) : 0;
     p.scores = N > 0 ? up(static_cast<long long>(T) * Hq * N * 4) : 0;
     return true;
@@ -753,8 +754,7 @@ int launch_form(const Attend& a, const Plan& p, cudaStream_t st)
     else if (a.l.D == 96) rc = a.l.G == 1 ? launch_rows<F16, 96, 1>(a, p, st) : launch_rows<F16, 96, 3>(a, p, st);
     else rc = a.l.G == 1 ? launch_rows<F16, 128, 1>(a, p, st) : a.l.G == 2 ? launch_rows<F16, 128, 2>(a, p, st) : launch_rows<F16, 128, 4>(a, p, st);
     if (rc != BS_OK) return rc;
-    // no sequence is cut where none can be longer than a run
-    if (!p.team && static_cast<long long>(a.t.width) * a.l.page > LEAST * KV4_TILE) {
+    if (p.join) {
         const dim3 grid(a.T, a.Hq);
         rc = a.l.D == 64 ? launch_dependent(kv4_join_kernel<F16, 64>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
              : a.l.D == 96 ? launch_dependent(kv4_join_kernel<F16, 96>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
@@ -786,7 +786,7 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
                              void* workspace, size_t workspace_bytes, void* stream)
 {
     Attend a{};
-    if (!q || !cache || !cache->data || !table || !lengths || !out || !workspace || T < 0 || B <= 0 || width <= 0 || table_pitch < width || q_token < 0 || q_head < 0) return BS_ERR_INVALID_ARG;
+    if (!q || !cache || !cache->data || !table || !lengths || !out || T < 0 || B <= 0 || width <= 0 || table_pitch < width || q_token < 0 || q_head < 0) return BS_ERR_INVALID_ARG;
     if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0 || q_heads <= 0 || q_heads % cache->heads != 0) return BS_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !(scale < INFINITY) || (!starts && T != B)) return BS_ERR_INVALID_ARG;
@@ -799,7 +799,7 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     if (sms <= 0 || !a.status) return BS_ERR_CUDA;
     Plan p;
     if (!plan(a.l, B, T, q_heads, starts != nullptr, width, weights ? N : 0, sms, p)) return BS_ERR_UNSUPPORTED;
-    if (workspace_bytes < p.bytes()) return BS_ERR_INVALID_ARG;
+    if (p.bytes() > 0 && (!workspace || workspace_bytes < p.bytes())) return BS_ERR_INVALID_ARG;
     a.t = {table, table_pitch, width, B};
     a.lengths = lengths; a.starts = starts;
     a.q = q; a.q_token = q_token; a.q_head = q_head;
@@ -809,11 +809,14 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     a.scale = scale * 1.4426950408889634f;
     a.out = out;
     char* ws = static_cast<char*>(workspace);
-    a.part = reinterpret_cast<float*>(ws);
-    a.stat = reinterpret_cast<float2*>(ws += p.part);
-    a.info = reinterpret_cast<int4*>(ws += p.stat);
+    if (p.join) {
+        a.part = reinterpret_cast<float*>(ws);
+        a.stat = reinterpret_cast<float2*>(ws + p.part);
+        a.info = reinterpret_cast<int4*>(ws + p.part + p.stat);
+        ws += p.part + p.stat + p.info;
+    }
     if (weights) {
-        a.lse = reinterpret_cast<float*>(ws += p.info);
+        a.lse = reinterpret_cast<float*>(ws);
         a.scores = reinterpret_cast<float*>(ws += p.lse);
         a.weights = weights; a.w_sequence = weights_sequence; a.w_head = weights_head; a.N = N;
     }

@@ -64,7 +64,7 @@ def test_append_and_read_refuse(L, at):
 def test_attend_refuses(L, at):
     def attend(q=at, qt=512, qh=128, T=2, heads=4, c=None, table=at, pitch=4, width=4, B=2, lengths=at, starts=None, scale=1.0, out=at, w=None, ws=256, wh=128, N=128, work=at, size=1 << 30):
         return L.bs_kv4_attend(q, qt, qh, T, heads, c or cache(at), table, pitch, width, B, lengths, starts, scale, out, w, ws, wh, N, work, size, None)
-    assert attend(q=None) == attend(table=None) == attend(lengths=None) == attend(out=None) == attend(work=None) == INVALID
+    assert attend(q=None) == attend(table=None) == attend(lengths=None) == attend(out=None) == INVALID
     assert attend(T=-1) == attend(T=3) == attend(heads=3) == attend(heads=0) == attend(B=0) == attend(width=0) == attend(pitch=3) == attend(qt=-8) == INVALID
     assert attend(scale=0.0) == attend(scale=-1.0) == attend(scale=float("inf")) == attend(scale=float("nan")) == INVALID
     assert attend(w=at, N=0) == attend(w=at, wh=127) == attend(w=at, ws=-1) == INVALID
@@ -86,3 +86,15 @@ def test_evict_refuses(L, at):
     assert all(evict(c=cache(at, **bad)) == INVALID for bad in BAD_CACHES)
     assert all(evict(c=cache(at, **bad)) == UNSUPPORTED for bad in BAD_LAYOUTS)
     assert evict(B=65536) == UNSUPPORTED
+
+
+def test_prompt_refuses(L, at):
+    def prompt(q=at, qt=256, qh=64, T=3, heads=4, k=at, kt=128, kh=64, v=at, vt=128, vh=64, Tk=3, kv=2, D=64, type=BF16, B=1, s=at, sk=at, scale=1.0, out=at):
+        return L.bs_attend_prompt(q, qt, qh, T, heads, k, kt, kh, v, vt, vh, Tk, kv, D, type, B, s, sk, scale, 1, out, None)
+    assert prompt(q=None) == prompt(k=None) == prompt(v=None) == prompt(out=None) == INVALID
+    assert prompt(T=-1) == prompt(Tk=-1) == prompt(heads=3) == prompt(heads=0) == prompt(kv=0) == prompt(D=0) == prompt(B=0) == INVALID
+    assert prompt(type=F32) == prompt(type=9) == prompt(scale=0.0) == prompt(scale=-2.0) == prompt(scale=float("inf")) == prompt(scale=float("nan")) == INVALID
+    assert prompt(s=None) == prompt(sk=None) == prompt(s=None, sk=None, B=2) == prompt(qt=-8) == prompt(kh=-8) == prompt(vt=-8) == INVALID
+    assert prompt(D=136) == prompt(D=60) == prompt(heads=258) == UNSUPPORTED
+    assert prompt(q=at + 2) == prompt(k=at + 8) == prompt(v=at + 4) == prompt(out=at + 2) == prompt(qt=257) == prompt(kh=4) == prompt(vh=2) == ALIGN
+    assert prompt(T=0) == OK

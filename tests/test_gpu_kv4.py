@@ -1,10 +1,12 @@
 """Keys and values of 4 bits on the GPU: stored, read back, attended to and evicted, against their definitions in 64 bits (kv4_reference.py)."""
 import math
+import re
 
 import pytest
 import torch
 
 import kv4_reference as ref
+from graph_launches import launches
 from paper_2207_08820_b200 import api
 from paper_2207_08820_b200._lib import BitserialError
 
@@ -353,6 +355,19 @@ def test_streams_and_graphs(room):
             for o in held:
                 assert ((o[b:b + 1].cpu().double() - out).abs() <= far).all()
             assert ((weights[b, :, :n].cpu().double() - 2 * got).abs() <= 2 * got_far + 1e-6).all()
+
+
+def test_which_kernels_run():
+    """Short sequences in one launch of clusters, long ones and many with a second launch, attention of the entries in one more; the count of launches follows."""
+    for lengths, room, names in (([500], 0, ["attend"]), ([500], 1000, ["attend", "join"]), ([500] * 40, 0, ["attend", "join"]), ([60] * 200, 0, ["attend"])):
+        f = Filled(23, lengths, 4, 64, 64, 64, BF16, room=room)
+        q, n = torch.randn(len(lengths), 4, 64, device="cuda").to(BF16), ints(lengths)
+        for weights, more in ((None, []), (torch.zeros(len(lengths), 4, 500, device="cuda"), ["weights"])):
+            got = launches(lambda: api.attend_kv4(q, f.cache, f.table, n, weights=weights))
+            assert sorted(re.search(r"kv4_(attend|join|weights)_kernel", name)[1] for name, _ in got) == sorted(names + more), (len(lengths), room)
+            before = api.launch_count
+            api.attend_kv4(q, f.cache, f.table, n, weights=weights)
+            assert api.launch_count - before == len(names + more)
 
 
 # --------------------------------------------------------------------------------------------------------------------- eviction
