@@ -623,16 +623,18 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     }
 }
 
-// Joins the runs of each row that was cut: a CTA a row of q and head, its warps every fourth run.
+// Joins the runs of each row that was cut: a CTA a row of q and head, its warps the runs in turn: eight where columns are cut into many (131072 entries 37.6 us, with four
+// 39.8), four else (64 sequences 66.5, with eight 69).
+constexpr int JOINERS = 8;
 template <bool F16, int D>
-__global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ Attend a, int R, int all)
+__global__ void __launch_bounds__(JOINERS * 32) kv4_join_kernel(const __grid_constant__ Attend a, int R, int all)
 {
     typedef W4Type<F16> Ty;
-    __shared__ float4 outs[WARPS][D / 4];
-    __shared__ float2 stat[WARPS];
+    __shared__ float4 outs[JOINERS][D / 4];
+    __shared__ float total[JOINERS];
     dependent_begin(a.out);
     const int32_t* starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr;
-    const int t = blockIdx.x, b = kv4_sequence_of(starts, a.t.B, t), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int t = blockIdx.x, b = kv4_sequence_of(starts, a.t.B, t), lane = threadIdx.x & 31, warp = threadIdx.x >> 5, joiners = blockDim.x >> 5;
     if (starts && (t < starts[b] || t >= starts[b + 1])) return;
     const int i = starts ? t - max(starts[b], 0) : 0;
     const int4 info = *behind_wait<int4>(a.info + b);
@@ -650,8 +652,8 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ A
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.f;
     const bool live = lane < D / 4;
-#pragma unroll 8
-    for (int k = warp; k < info.y; k += WARPS) {
+#pragma unroll 4
+    for (int k = warp; k < info.y; k += joiners) {
         const long long at = (first + static_cast<long long>(k) * info.z) * R + r;
         const float2 st = stats[at];
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -662,41 +664,52 @@ __global__ void __launch_bounds__(128) kv4_join_kernel(const __grid_constant__ A
         v.x = fmaf(x.x, f, v.x); v.y = fmaf(x.y, f, v.y); v.z = fmaf(x.z, f, v.z); v.w = fmaf(x.w, f, v.w);
     }
     if (live) outs[warp][lane] = v;
-    if (lane == 0) stat[warp].y = sum;
+    if (lane == 0) total[warp] = sum;
     __syncthreads();
     if (warp > 0) return;
-    sum = stat[0].y + stat[1].y + stat[2].y + stat[3].y;
+    sum = total[0];
+#pragma unroll
+    for (int w = 1; w < joiners; ++w) sum += total[w];
     const float inverse = sum == 0.f ? 0.f : 1.f / sum;
     const long long at = static_cast<long long>(t) * a.Hq + hq;
     if (live) {
         v = outs[0][lane];
 #pragma unroll
-        for (int w = 1; w < WARPS; ++w) { v.x += outs[w][lane].x; v.y += outs[w][lane].y; v.z += outs[w][lane].z; v.w += outs[w][lane].w; }
+        for (int w = 1; w < joiners; ++w) { v.x += outs[w][lane].x; v.y += outs[w][lane].y; v.z += outs[w][lane].z; v.w += outs[w][lane].w; }
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * D + 4 * lane) =
             make_uint2(Ty::round2(v.x * inverse, v.y * inverse), Ty::round2(v.z * inverse, v.w * inverse));
     }
     if (a.scores && lane == 0) a.lse[at] = sum == 0.f ? INFINITY : m + log2f(sum);
 }
 
-// What each entry got: the sum over the rows that share its head of exp2(score - lse), rows in their order.
+// What each entry got: the sum over the rows that share its head of exp2(score - lse).  Four threads an entry take every fourth row, their sums are added in order:
+// the same bits every time.
 __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant__ Attend a)
 {
+    __shared__ float parts[4][64];
     dependent_begin(a.weights);
     const int32_t *lengths = behind_wait<int32_t>(a.lengths), *starts = a.starts ? behind_wait<int32_t>(a.starts) : nullptr;
-    const int h = blockIdx.y;
+    const int h = blockIdx.y, group = threadIdx.x >> 6, mine = threadIdx.x & 63;
+    const float *lse = behind_wait<float>(a.lse), *scores = behind_wait<float>(a.scores);
     for (int b = blockIdx.z; b < a.t.B; b += gridDim.z) {
         const Seq s(a, lengths, starts, b, 8);
-        const int n = min(s.n, a.N);
-        const float* lse = behind_wait<float>(a.lse);
-        const float* scores = behind_wait<float>(a.scores);
-        for (int e = blockIdx.x * 256 + threadIdx.x; e < n; e += gridDim.x * 256) {
+        const int n = min(s.n, a.N), rows = s.tq * a.per;
+        for (int e0 = blockIdx.x * 64; e0 < n; e0 += gridDim.x * 64) {
+            const int e = e0 + mine;
             float w = 0.f;
-            for (int i = max(0, e - (s.n - s.tq)); i < s.tq; ++i) {        // query tokens that see it
-                const long long row = static_cast<long long>(s.first + i) * a.Hq + h * a.per;
+            if (e < n) {
+                const int first = max(0, e - (s.n - s.tq)) * a.per;         // rows before it do not see the entry
 #pragma unroll 4
-                for (int j = 0; j < a.per; ++j) w += exp2_of(scores[(row + j) * a.N + e] - lse[row + j]);
+                for (int r = first + group; r < rows; r += 4) {
+                    const int i = fdiv(r, a.d_per);
+                    const long long row = static_cast<long long>(s.first + i) * a.Hq + h * a.per + r - i * a.per;
+                    w += exp2_of(scores[row * a.N + e] - lse[row]);
+                }
             }
-            a.weights[b * a.w_sequence + h * a.w_head + e] += w;
+            parts[group][mine] = w;
+            __syncthreads();
+            if (group == 0 && e < n) a.weights[b * a.w_sequence + h * a.w_head + e] += (parts[0][mine] + parts[1][mine]) + (parts[2][mine] + parts[3][mine]);
+            __syncthreads();
         }
     }
 }
@@ -705,7 +718,7 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant_
 struct Plan {
     int NT, slots;
     bool team, join;            // joined by clusters; or, where a sequence may be longer than a run, by a second launch
-    long long runs;
+    long long runs, cuts;       // and of a column, about
     size_t part, stat, info, lse, scores;
     size_t bytes() const { return part + stat + info + lse + scores; }
 };
@@ -727,6 +740,7 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
     if (p.runs > 0x7fffffff / (R * 2)) return false;
     auto up = [](long long bytes) { return static_cast<size_t>((bytes + 255) / 256 * 256); };
     p.join = !p.team && cuts > 1;
+    p.cuts = p.runs / columns;
     p.part = p.join ? up(p.runs * R * l.D * 4) : 0;
     p.stat = p.join ? up(p.runs * R * 8) : 0;
     p.info = p.join ? up(static_cast<long long>(B) * 16) : 0;
@@ -755,13 +769,13 @@ int launch_form(const Attend& a, const Plan& p, cudaStream_t st)
     else rc = a.l.G == 1 ? launch_rows<F16, 128, 1>(a, p, st) : a.l.G == 2 ? launch_rows<F16, 128, 2>(a, p, st) : launch_rows<F16, 128, 4>(a, p, st);
     if (rc != BS_OK) return rc;
     if (p.join) {
-        const dim3 grid(a.T, a.Hq);
-        rc = a.l.D == 64 ? launch_dependent(kv4_join_kernel<F16, 64>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
-             : a.l.D == 96 ? launch_dependent(kv4_join_kernel<F16, 96>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
-                           : launch_dependent(kv4_join_kernel<F16, 128>, grid, dim3(128), 0, st, a, 8 * p.NT, static_cast<int>(p.runs));
+        const dim3 grid(a.T, a.Hq), block(p.cuts >= 16 ? JOINERS * 32 : JOINERS * 16);
+        rc = a.l.D == 64 ? launch_dependent(kv4_join_kernel<F16, 64>, grid, block, 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
+             : a.l.D == 96 ? launch_dependent(kv4_join_kernel<F16, 96>, grid, block, 0, st, a, 8 * p.NT, static_cast<int>(p.runs))
+                           : launch_dependent(kv4_join_kernel<F16, 128>, grid, block, 0, st, a, 8 * p.NT, static_cast<int>(p.runs));
     }
     if (rc == BS_OK && a.weights) {
-        const int chunks = ceil_div(a.N, 256);
+        const int chunks = ceil_div(a.N, 64);
         rc = launch_dependent(kv4_weights_kernel, dim3(chunks < 65535 ? chunks : 65535, a.l.H, a.t.B < 65535 ? a.t.B : 65535), dim3(256), 0, st, a);
     }
     return rc;
