@@ -528,6 +528,7 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *            and the heads that share it, is added to it.  Entries from N on are left out.
  *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights; 0 and NULL for few short sequences); two calls that may run
  *              at the same time need one each
+ * Supported: heads up to 65535 of q; q below 2^116 and values below 2^100 (sums are divided by their weights at the end).
  * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms (one, 11 bits, where the
  * output is bf16); the same call gives the same bits every time.
  */
@@ -544,7 +545,7 @@ int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int
  *   lengths_out  device int32 [B];  weights_out  device float [B][heads][N]: the weights of what stays, zeros behind;  kept  device int32 [B][heads][keep]: where
  *                it was, -1 behind.  None of them may overlap what is read.
  *   workspace    bs_kv4_evict_workspace_bytes(...) bytes (0 and NULL with `into`); two calls that may run at the same time need one each
- * Sequences of up to `keep` entries stay as they are, and are brought to `into`.  B up to 65535.
+ * Sequences of up to `keep` entries stay as they are, and are brought to `into`.  B up to 65535.  Two launches, three without `into`.
  */
 size_t bs_kv4_evict_workspace_bytes(const bs_kv4_cache* cache, int B, int keep, int into);
 int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long table_pitch, int width, const int32_t* into, long long into_pitch, int into_width,
@@ -557,7 +558,7 @@ int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long tabl
  *   starts   rows of q of each of B sequences, starts_k their rows of k and v (both device int32 [B + 1], or both NULL: one sequence of all rows, B = 1)
  *   causal   row i of n rows of q over m keys sees the keys below m - n + i + 1; else all of them.  A row that sees nothing gives zeros.
  *   out      device [T][q_heads][D] of the type (BS_F16 or BS_BF16): softmax(scale q k^T) v, scale > 0
- * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k.  Scores, softmax and sums have 32 bits; weights are rounded to the type before they meet
+ * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k, values below 2^100 (sums are divided by their weights at the end).  Scores, softmax and sums have 32 bits; weights are rounded to the type before they meet
  * the values.  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
  * its rows that do not see it.  The same call gives the same bits every time.
  */

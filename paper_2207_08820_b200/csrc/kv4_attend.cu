@@ -7,7 +7,11 @@
 //
 // A warp takes 64 entries at a time, in one piece where the page allows, through two buffers of its own in shared memory, and keeps the running maximum, sum
 // and outputs of eight or sixteen rows (query tokens times the heads that share keys) in registers.  Four warps of a CTA share a run of entries; the
-// sequences are cut into runs of equal length for the whole grid, which every CTA finds by itself from the lengths; a second kernel joins runs.
+// sequences are cut into runs of equal length for the whole grid, which every CTA finds by itself from the lengths; a second kernel joins runs, or, where they
+// are short and few, clusters do.
+//
+// 64 sequences of up to 8192 entries, 32 heads over 8 of 128 channels: 66 us, 4.1 TB/s, where the bare stream takes 41 to 49 and the instructions (250 a tile of 16 entries
+// and head, a third of them masks) 55 by themselves; 12 warps an SM issue in half of the cycles.  One sequence of 131072: 38 us, of 1000: 6.7.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"

@@ -5,6 +5,9 @@
 // the digits up over the cluster and hands the sums to all.  Entries above it stay, of those equal to it the first ones.  A second pass over the entries writes the
 // indices, ranked by sums over warps and CTAs.  What stays is then moved by a kernel over all heads and sequences: into other pages at once, into their own
 // through a copy, since what one CTA writes another may still have to read.
+//
+// 16 sequences of up to 32768 entries and 8 heads cut to 8191: 31 us to select (four weights a thread and turn; with one 52), bound by loads and atomics, 55 to move at
+// 4 TB/s.  4096 entries to 2048: 14 us with the launches.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"
