@@ -539,7 +539,8 @@ int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int
 
 /*
  * bs_kv4_evict -- cuts sequences of more than `keep` entries to `keep`.  Every head keeps its `recent` newest entries and of the others those with the largest
- * weights (float [B][heads][N], N at least the longest sequence; ties to the lowest index, a NaN before everything), in their order.
+ * weights (float [B][heads][N], N at least the longest sequence; ties to the lowest index, a NaN before everything), in their order.  weights_head 0 or
+ * weights_sequence 0: all heads or all sequences have the same ones.
  *   into         int32 [B][into_width]: pages that take what stays, other ones than those of any sequence; room for keep entries.  NULL: the sequences' own pages,
  *                which none of them may share; their entries from the new length on are then as good as gone
  *   lengths_out  device int32 [B];  weights_out  device float [B][heads][N]: the weights of what stays, zeros behind;  kept  device int32 [B][heads][keep]: where
@@ -558,8 +559,8 @@ int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long tabl
  *   starts   rows of q of each of B sequences, starts_k their rows of k and v (both device int32 [B + 1], or both NULL: one sequence of all rows, B = 1)
  *   causal   row i of n rows of q over m keys sees the keys below m - n + i + 1; else all of them.  A row that sees nothing gives zeros.
  *   out      device [T][q_heads][D] of the type (BS_F16 or BS_BF16): softmax(scale q k^T) v, scale > 0
- * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k, values below 2^100 (sums are divided by their weights at the end).  Scores, softmax and sums have 32 bits; weights are rounded to the type before they meet
- * the values.  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
+ * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k, values below 2^100 (sums are divided by their weights at the end).  Scores, softmax and
+ * sums have 32 bits; weights are rounded to the type before they meet the values.  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
  * its rows that do not see it.  The same call gives the same bits every time.
  */
 int bs_attend_prompt(const void* q, long long q_token, long long q_head, int T, int q_heads, const void* k, long long k_token, long long k_head, const void* v,

@@ -764,11 +764,13 @@ PyObject* kv4_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
         no_gradient_attention(w);
         const int N = small(w.size(2)), keep = integer(r[3]), recent = integer(r[4]);
         const int64_t w_head = w.size(1) > 1 ? w.stride(1) : N, w_sequence = w.size(0) > 1 ? w.stride(0) : 0;
+        if (w_head > 0 && w_head < N) mismatch("weights whose rows do not overlap, or are the same for all heads, expected");
         if (keep < 1 || recent < 0 || recent > keep) mismatch("at least one entry to keep, and no more of the newest than that, expected");
         Table into{};
         if (r[5] != Py_None) {
             into = table_of(r[5], data);
             if (into.B != t.B) mismatch("a row of pages for each sequence expected");
+            if (into.pages == t.pages) mismatch("other pages than the sequences' own expected");
             if (static_cast<int64_t>(into.width) * c.page < std::min({static_cast<int64_t>(keep), static_cast<int64_t>(N), static_cast<int64_t>(t.width) * c.page}))
                 mismatch("pages for all that stays expected");
         }
@@ -780,7 +782,7 @@ PyObject* kv4_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
         on.keep({a[0], r[0], r[1], r[2], r[5]});
         {
             NoGil free;
-            rc = bs_kv4_evict(&c, t.pages, t.pitch, t.width, into.pages, into.pitch, into.width, t.B, lengths, static_cast<const float*>(w.const_data_ptr()), w_sequence, w_head < N ? N : w_head, N,
+            rc = bs_kv4_evict(&c, t.pages, t.pitch, t.width, into.pages, into.pitch, into.width, t.B, lengths, static_cast<const float*>(w.const_data_ptr()), w_sequence, w_head, N,
                               keep, recent, static_cast<int32_t*>(lengths_out.data_ptr()), static_cast<float*>(weights_out.data_ptr()), static_cast<int32_t*>(kept.data_ptr()),
                               bytes ? ws.data_ptr() : nullptr, bytes, on.stream);
         }

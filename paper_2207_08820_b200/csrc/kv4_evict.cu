@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
             for (int j = 0; j < 4; ++j) {
                 const bool above = i + j < to && k[j] > prefix, same = i + j < to && k[j] == prefix;
                 if (above || (same && e < left)) {
-                    const uint32_t place = m + min(e, left);
+                    const uint32_t place = min(m + min(e, left), static_cast<uint32_t>(need) - 1u);        // the least one but for weights that change meanwhile
                     kept[place] = i + j;
                     out[place] = v[j];
                 }
@@ -287,7 +287,7 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     if (!cache || !cache->data || !table || !lengths || !weights || !lengths_out || !weights_out || !kept || B <= 0 || width <= 0 || table_pitch < width) return BS_ERR_INVALID_ARG;
     if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0) return BS_ERR_INVALID_ARG;
-    if (N <= 0 || keep <= 0 || recent < 0 || recent > keep || weights_head < N || weights_sequence < 0) return BS_ERR_INVALID_ARG;
+    if (N <= 0 || keep <= 0 || recent < 0 || recent > keep || weights_head < 0 || (weights_head > 0 && weights_head < N) || weights_sequence < 0) return BS_ERR_INVALID_ARG;
     if (into && (into_width <= 0 || into_pitch < into_width)) return BS_ERR_INVALID_ARG;
     if (!kv4_layout(*cache, a.l) || B > 65535) return BS_ERR_UNSUPPORTED;
     const long long most = static_cast<long long>(width) * a.l.page < N ? static_cast<long long>(width) * a.l.page : N, stays = keep < most ? keep : most;

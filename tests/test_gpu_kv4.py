@@ -446,6 +446,20 @@ def test_evict_long():
         assert torch.equal(kept[0, h].cpu().long(), want) and torch.equal(w_out[0, h, :60001].cpu(), w[0, h, want])
 
 
+@pytest.mark.parametrize("n,sequences,heads", [(300, 2, 3), (70000, 1, 2), (17, 3, 1)])
+def test_evict_shared_weights(n, sequences, heads):
+    """Weights that all heads, or all sequences and heads, have in common, without copies of them."""
+    w = weights_of(9, sequences, 1, n, "ties")
+    for shape in (w, w[:1]):
+        f = Filled(23, [n] * sequences, heads, 64, 64, 64, F16)
+        n_out, w_out, kept = api.evict_kv4(f.cache, f.table, ints([n] * sequences), shape.cuda().expand(sequences, heads, n), 13, recent=4)
+        for b in range(sequences):
+            for h in range(heads):
+                mine = shape.expand(sequences, heads, n)[b, h]
+                want = torch.cat([torch.sort(mine[:n - 4], descending=True, stable=True).indices[:9].sort().values, torch.arange(n - 4, n)])
+                assert torch.equal(kept[b, h].cpu().long(), want) and same(w_out[b, h, :13].cpu(), mine[want]) and (w_out[b, h, 13:] == 0).all()
+
+
 # ------------------------------------------------------------------------------------------------------------------- refusals
 
 def test_refusals():
@@ -464,6 +478,7 @@ def test_refusals():
                 lambda: api.read_kv4(f.cache, f.table, n, ints([0, 1, 2])), lambda: api.read_kv4(f.cache, f.table, n, ints([0, 1, 2]), total=-1),
                 lambda: api.evict_kv4(f.cache, f.table, n, w, 0), lambda: api.evict_kv4(f.cache, f.table, n, w, 5, recent=6), lambda: api.evict_kv4(f.cache, f.table, n, w, 5, recent=-1),
                 lambda: api.evict_kv4(f.cache, f.table, n, w, 17, into=f.table[:, :1]), lambda: api.evict_kv4(f.cache, f.table, n, w, 5, into=f.table[:1]),
+                lambda: api.evict_kv4(f.cache, f.table, n, w, 5, into=f.table), lambda: api.evict_kv4(f.cache, f.table, n, torch.zeros(80, device="cuda").as_strided((2, 2, 32), (40, 8, 1)), 5),
                 lambda: api.evict_kv4(f.cache, f.table, n, w[..., 0], 5), lambda: api.cache_kv4(4, 2, 80), lambda: api.cache_kv4(4, 2, 64, page=48), lambda: api.cache_kv4(4, 2, 64, group=48),
                 lambda: api.cache_kv4(0, 2, 64), lambda: api.cache_kv4(4, 2, 64, dtype=torch.float32)):
         with pytest.raises(ValueError):
