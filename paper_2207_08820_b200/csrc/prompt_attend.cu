@@ -544,7 +544,7 @@ extern "C" int bs_attend_prompt(const void* q, long long q_token, long long q_he
                                 void* out, void* stream)
 {
     if (!q || !k || !v || !out || T < 0 || Tk < 0 || q_heads <= 0 || heads <= 0 || D <= 0 || q_heads % heads != 0 || B <= 0) return BS_ERR_INVALID_ARG;
-    if ((type != BS_F16 && type != BS_BF16) || !(scale > 0.f) || !(scale < INFINITY)) return BS_ERR_INVALID_ARG;
+    if ((type != BS_F16 && type != BS_BF16) || !(scale > 0.f) || !(scale * 1.4426950408889634f < INFINITY)) return BS_ERR_INVALID_ARG;
     if (q_token < 0 || q_head < 0 || k_token < 0 || k_head < 0 || v_token < 0 || v_head < 0) return BS_ERR_INVALID_ARG;
     if ((starts == nullptr) != (starts_k == nullptr) || (!starts && B != 1)) return BS_ERR_INVALID_ARG;
     Prompt a{};

@@ -66,6 +66,7 @@ def test_attend_refuses(L, at):
         return L.bs_kv4_attend(q, qt, qh, T, heads, c or cache(at), table, pitch, width, B, lengths, starts, scale, out, w, ws, wh, N, work, size, None)
     assert attend(q=None) == attend(table=None) == attend(lengths=None) == attend(out=None) == INVALID
     assert attend(T=-1) == attend(T=3) == attend(heads=3) == attend(heads=0) == attend(B=0) == attend(width=0) == attend(pitch=3) == attend(qt=-8) == INVALID
+    assert attend(scale=3e38) == INVALID         # times log2(e) it is no number of binary32
     assert attend(scale=0.0) == attend(scale=-1.0) == attend(scale=float("inf")) == attend(scale=float("nan")) == INVALID
     assert attend(w=at, N=0) == attend(w=at, wh=127) == attend(w=at, ws=-1) == INVALID
     assert attend(q=at + 2) == attend(out=at + 4) == attend(work=at + 8) == attend(qt=1) == attend(qh=4) == ALIGN
@@ -79,7 +80,7 @@ def test_evict_refuses(L, at):
     def evict(c=None, table=at, pitch=4, width=4, into=None, ip=4, iw=4, B=2, lengths=at, w=at, ws=256, wh=128, N=128, keep=10, recent=3, n=at, wo=at, kept=at, work=at, size=1 << 30):
         return L.bs_kv4_evict(c or cache(at), table, pitch, width, into, ip, iw, B, lengths, w, ws, wh, N, keep, recent, n, wo, kept, work, size, None)
     assert evict(table=None) == evict(lengths=None) == evict(w=None) == evict(n=None) == evict(wo=None) == evict(kept=None) == INVALID
-    assert evict(width=0) == evict(pitch=3) == evict(B=0) == evict(N=0) == evict(keep=0) == evict(recent=-1) == evict(recent=11) == evict(wh=127) == evict(ws=-1) == INVALID
+    assert evict(width=0) == evict(pitch=3) == evict(B=0) == evict(N=0) == evict(keep=0) == evict(recent=-1) == evict(recent=11) == evict(wh=127) == evict(wh=-128) == evict(ws=-1) == INVALID
     assert evict(work=None) == evict(size=2 * 2 * 16 * 136 - 1) == INVALID
     assert evict(into=at, iw=0) == evict(into=at, ip=3) == evict(into=at, iw=1, keep=65) == INVALID
     assert evict(work=at + 8) == evict(c=cache(at, data=at + 4)) == ALIGN
@@ -93,6 +94,7 @@ def test_prompt_refuses(L, at):
         return L.bs_attend_prompt(q, qt, qh, T, heads, k, kt, kh, v, vt, vh, Tk, kv, D, type, B, s, sk, scale, 1, out, None)
     assert prompt(q=None) == prompt(k=None) == prompt(v=None) == prompt(out=None) == INVALID
     assert prompt(T=-1) == prompt(Tk=-1) == prompt(heads=3) == prompt(heads=0) == prompt(kv=0) == prompt(D=0) == prompt(B=0) == INVALID
+    assert prompt(scale=3e38) == INVALID
     assert prompt(type=F32) == prompt(type=9) == prompt(scale=0.0) == prompt(scale=-2.0) == prompt(scale=float("inf")) == prompt(scale=float("nan")) == INVALID
     assert prompt(s=None) == prompt(sk=None) == prompt(s=None, sk=None, B=2) == prompt(qt=-8) == prompt(kh=-8) == prompt(vt=-8) == INVALID
     assert prompt(D=136) == prompt(D=60) == prompt(heads=258) == UNSUPPORTED
