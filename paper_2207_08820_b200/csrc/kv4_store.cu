@@ -162,10 +162,11 @@ __device__ __forceinline__ void quantise(const uint4* raw, uint32_t* code, uint3
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(s));
     auto both = [](float v) { return f2_pack(__float_as_uint(v), __float_as_uint(v)); };
     const u64 m2 = both(-m), s2 = both(-s), inverse2 = both(inverse), magic2 = both(magic);
-    // A value of 2^-14 (bf16: 2^-17) of the span or more is a multiple of 2^-24 of it, as the type has 11 (8) bits; with such values and such an offset
-    // differences are exact, and a quotient that is not on a border is 15 * 2^-24 away from it, more than its rounding of 2^-21.  Steps near the ends of binary32 have
+    // With 2^e the power of two up to the span, a value of 2^(e - 13) (bf16: 2^(e - 16)) or more is a multiple of 2^(e - 23), as the type has 11 (8) bits; with such values
+    // and such an offset differences are multiples below 2^(e + 1), which 24 bits hold, and a quotient that is not on a border is 15 * 2^-24 away from it, more than its
+    // rounding of 2^-21.  (With half of that they may take 25 bits, and a difference beside a border be rounded onto it.)  Steps near the ends of binary32 have
     // no reciprocals to use, and steps of few bits (the type's smallest) may leave quotients above 15.
-    const float grid = span * (F16 ? 0x1p-14f : 0x1p-17f);
+    const float grid = __uint_as_float(__float_as_uint(span) & 0x7f800000u) * (F16 ? 0x1p-13f : 0x1p-16f);
     const bool plain = s > 0x1p-60f && s < 0x1p60f && span < 15.5f * s;
 #pragma unroll
     for (int w = 0; w < W; ++w) {

@@ -1,0 +1,69 @@
+"""Keys and values of 4 bits on the GPU where the kernels' arithmetic is at its ends, against their definitions in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import kv4_reference as ref
+from paper_2207_08820_b200 import api
+from test_gpu_kv4 import BF16, F16, ints, same
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------------------------- the quantiser
+
+def stored(x, group):
+    """What the cache gives back for vectors x [n, 1, D], as keys and as values."""
+    n, _, D = x.shape
+    cache, table = api.cache_kv4(-(-n // 256), 1, D, page=256, group=group, dtype=x.dtype), torch.arange(-(-n // 256), dtype=torch.int32, device="cuda").unsqueeze(0)
+    api.append_kv4(x.cuda(), x.cuda(), cache, table, ints([0]), ints([0, n]))
+    return [y.cpu() for y in api.read_kv4(cache, table, ints([0]), ints([0, n]), total=n)]
+
+
+def read(x, group):
+    """As kv4_reference.read, where a difference from the offset takes more than the 53 bits of a double as well: what its rounding lost decides on which side of a
+    border the quotient is."""
+    v = x.double().unflatten(-1, (-1, group))
+    _, step, lo = (y.unsqueeze(-1) if y.dim() < v.dim() else y for y in ref.quantise(x, group))
+    d = v - lo
+    back = v - d
+    lost = (v - (d + back)) + (back - lo)
+    c = torch.floor(d / step)
+    rest = d - c * step - step / 2          # exact beside a border
+    c = torch.where((rest > 0) | ((rest == 0) & ((lost > 0) | ((lost == 0) & (c % 2 == 1)))), c + 1, c).clamp(0, 15)
+    return (c * step + lo).flatten(-2).float().to(x.dtype)
+
+
+def test_differences_that_take_25_bits():
+    """A quotient of 8.50000047 whose difference, rounded to binary32, lies on the border below it."""
+    x = torch.full((1, 1, 64), 35296.0, dtype=F16)
+    x[0, 0, ::32], x[0, 0, 1::32] = 2047 / 512, 62272.0
+    codes, steps, _ = ref.quantise(x, 32)
+    assert steps[0, 0, 0] == 4152 and codes[0, 0, 0, 2] == 9
+    for back in stored(x, 32):
+        assert same(back, ref.read(x, 32)) and same(back, read(x, 32))
+
+
+@pytest.mark.parametrize("few", [True, False], ids=["few", "many"])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_borders_beside_small_offsets(dtype, few):
+    """Offsets of all magnitudes, with all ones in their mantissas, and values next to every border."""
+    bits = 8 if dtype == BF16 else 11
+    gen = torch.Generator().manual_seed(5)
+    n = 300 if few else 40000
+    span = 60000 * (0.25 + 0.75 * torch.rand(n, generator=gen).double())
+    least = torch.exp2(-torch.randint(0, 24, (n,), generator=gen).double()) * span.log2().floor().exp2() * (2 - 2.0 ** (1 - torch.randint(1, bits + 1, (n,), generator=gen).double()))
+    least = torch.where(least < span / 4, least, span / 4) * (torch.randint(0, 2, (n,), generator=gen) * 2 - 1)
+    least, span = least.to(dtype).double(), span.to(dtype).double()
+    most = torch.where(least + span < 65000, span, span / 2).to(dtype).double()
+    step = ((most - least).float() / torch.full((n,), 15.0)).to(dtype).double()
+    near = (torch.arange(15) + 0.5) * step.unsqueeze(1) + least.unsqueeze(1)
+    low = near.to(dtype)
+    ulp = torch.exp2(torch.floor(torch.log2(low.double().abs().clamp(min=1e-30)))) * torch.finfo(dtype).eps
+    other = (low.double() + torch.where(near > low.double(), ulp, -ulp)).to(dtype)        # the neighbour on the far side of the border
+    x = torch.cat([least.unsqueeze(1).to(dtype), most.unsqueeze(1).to(dtype), low, other], 1)
+    x = torch.where((x.double() < least.unsqueeze(1)) | (x.double() > most.unsqueeze(1)), least.unsqueeze(1).to(dtype), x)
+    x = torch.cat([x, x.flip(1)], 1).unsqueeze(1)
+    for back in stored(x, 32):
+        assert same(back, read(x, 32))
