@@ -76,6 +76,14 @@ __device__ __forceinline__ float exp2_of(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// x 2^n, n from -252 to 254, by two factors, as 2^n alone may be out of range.  At least the smallest number and at most the largest one: an infinity times it stays
+// one, and a zero a zero.
+__device__ __forceinline__ float times_power(float x, int n)
+{
+    const int half = n >> 1;
+    const float y = x * __uint_as_float(static_cast<uint32_t>(127 + half) << 23) * __uint_as_float(static_cast<uint32_t>(127 + n - half) << 23);
+    return fminf(fmaxf(y, 0x1p-149f), 0x1.fffffep127f);
+}
 __device__ __forceinline__ uint32_t transposed(uint32_t v)
 {
     uint32_t r;
@@ -267,7 +275,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) raw[k] = *reinterpret_cast<const uint4*>(q + 32 * k);
         }
-        float up = 1.f, down = 1.f;
+        float up = 1.f;
+        int down = 0;
         if (!F16) {
             uint32_t big = 0;
 #pragma unroll
@@ -281,7 +290,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
             const int e = min(max(static_cast<int>(big >> 7) - 127, -112), 126);       // the largest value's exponent becomes 13
             up = __uint_as_float(static_cast<uint32_t>(127 + 13 - e) << 23);
-            down = __uint_as_float(static_cast<uint32_t>(127 - 13 + e) << 23);
+            down = e - 13;
         }
         float sums[G];
 #pragma unroll
@@ -311,7 +320,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int from = 4 * (2 * tid + i);
-            factor[n][i] = __shfl_sync(0xffffffffu, down, from) * (a.scale * 0x1p24f);        // sums are in units of 2^-24
+            factor[n][i] = times_power(a.scale, __shfl_sync(0xffffffffu, down, from) + 24);        // sums are in units of 2^-24
 #pragma unroll
             for (int g = 0; g < G; ++g) qsum[g][n][i] = __shfl_sync(0xffffffffu, sums[g], from) * 0x1p-24f;
         }

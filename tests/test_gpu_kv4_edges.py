@@ -6,7 +6,7 @@ import torch
 
 import kv4_reference as ref
 from paper_2207_08820_b200 import api
-from test_gpu_kv4 import BF16, F16, ints, same
+from test_gpu_kv4 import BF16, F16, Filled, ints, same, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +67,47 @@ def test_borders_beside_small_offsets(dtype, few):
     x = torch.cat([x, x.flip(1)], 1).unsqueeze(1)
     for back in stored(x, 32):
         assert same(back, read(x, 32))
+
+
+
+# --------------------------------------------------------------------------------------------------------------------- attention
+
+def check(f, q, counts, scale=None, weights=False, reference=ref.attend):
+    """Attention of packed queries over a filled cache against a definition."""
+    w = torch.zeros(len(counts), f.H, max(f.lengths), device="cuda") if weights else None
+    out = api.attend_kv4(q.cuda(), f.cache, f.table, ints(f.lengths), starts_of(counts), scale=scale, weights=w).cpu().double()
+    i = 0
+    for b, t in enumerate(counts):
+        want, far, got, got_far = reference(q[i:i + t], f.k[b], f.v[b], f.group, scale)
+        off = (out[i:i + t] - want).abs()
+        assert (off <= far).all(), (b, off.max(), (off / far).max())
+        if weights:
+            assert ((w[b, :, :f.lengths[b]].cpu().double() - got).abs() <= got_far + 2.0 ** -23).all()
+        i += t
+
+
+@pytest.mark.parametrize("scale", [1e-44, 1e-38, 1e-30, 1e-20, 1e-15, 1e20, 1e31, 2e31, 1e35, 2.3e38])
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+def test_scales_near_the_ends_of_binary32(dtype, scale):
+    """Queries of zeros see the mean of the values whatever the scale is, and so do all where the scale leaves nothing of the scores; one that is large picks entries."""
+    f = Filled(30, [77, 300, 1], 2, 64, 16, 32, dtype)
+    q = torch.zeros(30, 6, 64, dtype=dtype)
+    check(f, q, [14, 15, 1], scale, weights=True)
+    if scale < 1:
+        q[::2] = torch.randn(15, 6, 64, generator=torch.Generator().manual_seed(1)).to(dtype)
+        check(f, q, [14, 15, 1], scale, weights=True)
+
+
+@pytest.mark.parametrize("power", [-110, -105, -100, -60, 60, 100, 105])
+def test_scales_that_make_up_for_the_size_of_queries(power):
+    """Scores of ordinary size out of products that are none."""
+    f = Filled(31, [77, 300], 2, 128, 64, 64, BF16)
+    q = (torch.randn(9, 6, 128, generator=torch.Generator().manual_seed(2)) * 2.0 ** power).to(BF16)
+    q[3] = 0
+    check(f, q, [4, 5], 2.0 ** -power / 128 ** 0.5, weights=True)
+
+
+@pytest.mark.parametrize("keys,scale", [(1.0, None), (6000.0, None), (1e-4, 1e20)])
+def test_keys_and_scales(keys, scale):
+    f = Filled(32, [200], 1, 64, 64, 64, F16, spread=keys * 0.1)
+    check(f, torch.zeros(3, 4, 64, dtype=F16), [3], scale)
