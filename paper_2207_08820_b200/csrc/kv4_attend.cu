@@ -259,8 +259,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     for (int k = 0; k < STAGES; ++k)
         if (k < mine) issue(k);
 
-    // queries as fragments: row gid of each tile, the channels in the order of the keys' words.  bf16 is brought into fp16's range by a power of two, exactly but for
-    // values below 2^-27 of the row's largest, which keep an error of 2^-38 of it
+    // queries as fragments: row gid of each tile, the channels in the order of the keys' words.  A power of two brings a row's largest value to 2^13 and more, so that its
+    // others fit fp16 exactly, those that meet codes of sixteenfold weight divided by sixteen, but for values below 2^-23 (bf16: 2^-26) of the largest, which
+    // may lose 2^-34 of it
     uint32_t qf[NT][BLOCKS * 2][2];
     float factor[NT][2], qsum[G][NT][2];
 #pragma unroll
@@ -275,23 +276,18 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
 #pragma unroll
             for (int k = 0; k < BLOCKS; ++k) raw[k] = *reinterpret_cast<const uint4*>(q + 32 * k);
         }
-        float up = 1.f;
-        int down = 0;
-        if (!F16) {
-            uint32_t big = 0;
+        uint32_t big = 0;
 #pragma unroll
-            for (int k = 0; k < BLOCKS; ++k)
+        for (int k = 0; k < BLOCKS; ++k)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t w = word_of(raw[k], j);
-                    big = max(big, max(w & 0x7f80u, w >> 16 & 0x7f80u));
-                }
-            big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
-            big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
-            const int e = min(max(static_cast<int>(big >> 7) - 127, -112), 126);       // the largest value's exponent becomes 13
-            up = __uint_as_float(static_cast<uint32_t>(127 + 13 - e) << 23);
-            down = e - 13;
-        }
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t w = word_of(raw[k], j);
+                big = max(big, max(__float_as_uint(fabsf(Ty::lo(w))), __float_as_uint(fabsf(Ty::hi(w)))));
+            }
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = min(max(static_cast<int>(big >> 23) - 127, -112), 126), down = e - 13;       // the largest value's exponent becomes 13
+        const float up = __uint_as_float(static_cast<uint32_t>(127 - down) << 23);
         float sums[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) sums[g] = 0.f;

@@ -111,3 +111,23 @@ def test_scales_that_make_up_for_the_size_of_queries(power):
 def test_keys_and_scales(keys, scale):
     f = Filled(32, [200], 1, 64, 64, 64, F16, spread=keys * 0.1)
     check(f, torch.zeros(3, 4, 64, dtype=F16), [3], scale)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("size", [1e-1, 1e-2, 1e-3, 1e-4, 1e-5, 1e-6, 5e-7])
+def test_small_queries(size, dtype):
+    """Queries far below one with a scale that makes up for it: no bits are lost on the way."""
+    f = Filled(33, [500, 40], 2, 128, 64, 128, dtype)
+    q = (torch.randn(7, 8, 128, generator=torch.Generator().manual_seed(3)) * size).to(dtype)
+    q[4:] = torch.where(torch.arange(128) % 2 == 0, q[4:], q[4:] / 64)
+    check(f, q, [4, 3], 1 / (size * 128 ** 0.5), weights=True)
+
+
+@pytest.mark.parametrize("size,keys,scale", [(3e-6, 6000.0, 5.0), (5e-7, 6000.0, 28.0), (1e-4, 10000.0, None), (6e4, 1.0, 1e-5)])
+def test_fp16_queries_and_keys_far_apart(size, keys, scale):
+    f = Filled(34, [300], 1, 128, 64, 64, F16, fill=False)
+    gen = torch.Generator().manual_seed(4)
+    f.k[0] = (torch.rand(300, 1, 128, generator=gen) * keys).to(F16)
+    api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, 300]))
+    q = ((torch.rand(2, 4, 128, generator=gen) * 2 - 1) * size).to(F16)
+    check(f, q, [2], scale)
