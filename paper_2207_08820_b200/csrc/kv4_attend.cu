@@ -2,7 +2,7 @@
 //
 // Codes are exact in fp16 and are what the tensor cores multiply (mma.sync; eight rows of queries cost what one does): with c the codes, s and m a group's step
 // and offset, a score is the sum over its groups of s (q . c) + m sum(q), scaled in 32 bits; the keys are never rounded.  An output is the sum over
-// entries of (p s) c, p s in fp16 under a common power of two, plus the sum of p m, in 32 bits.  A code costs a mask: as the last bits of an fp16
+// entries of (p s) c, p s in fp16 under a power of two of the row and the group, plus the sum of p m, in 32 bits.  A code costs a mask: as the last bits of an fp16
 // number without an exponent it counts 2^-24, which the sums' scales take back.
 //
 // A warp takes 64 entries at a time, in one piece where the page allows, through two buffers of its own in shared memory, and keeps the running maximum, sum
@@ -90,6 +90,7 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
     return r;
 }
+__device__ __forceinline__ u64 f2_mul(u64 a, u64 b) { u64 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 // Nibbles i and i + 4 of x as pairs of fp16: bits at the end of a mantissa without an exponent are a number of 2^-24 each, four places up of 2^-20, exactly.
 __device__ __forceinline__ void expand(uint32_t x, uint32_t (&v)[4])
 {
@@ -322,9 +323,11 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         }
     }
 
+    // Products p s of a row and group of channels are scaled by a power of two that keeps them below 2^15 and the largest one that was met above 1, so that fp16 loses no
+    // more than 2^-25 of that one, whatever steps the entries without weight and the other groups have.  cap: the bits of what stands for 2^15; the outputs' units follow.
+    constexpr int LEAST_CAP = 24 << 23;         // 2^-103
     float o[MT][NT][4], offs[G][NT][2], top[NT][2], total[NT][2];
-    int power = -126;           // outputs are in units of 2^power, above all steps so far
-    float limit_step = 0x1p-126f;
+    int cap[G][NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -332,7 +335,10 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             top[n][i] = -INFINITY;
             total[n][i] = 0.f;
 #pragma unroll
-            for (int g = 0; g < G; ++g) offs[g][n][i] = 0.f;
+            for (int g = 0; g < G; ++g) {
+                offs[g][n][i] = 0.f;
+                cap[g][n][i] = LEAST_CAP;
+            }
 #pragma unroll
             for (int m = 0; m < MT; ++m) o[m][n][i] = o[m][n][2 + i] = 0.f;
         }
@@ -347,19 +353,24 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     const uint32_t value_at = tid * (D / 2) + kv4_value_part(D, tid, gid) * (D / 16);
     bool late = false;
 
-    // A whole unit that all rows see, or one tile `at` of any: code that runs once or twice should be short, it comes from memory.
+    auto unit_of = [](int cap) { return __uint_as_float((269u << 23) - static_cast<uint32_t>(cap)); };          // 2^15 / cap
+
+    // A whole unit that all rows see, in halves where registers would not do (64 sequences, 4 tokens, fp16, groups of 64: 180 us whole, 170 in halves), or one tile `at`
+    // of any: code that runs once or twice should be short, it comes from memory.
+    constexpr int AT_ONCE = G * NT < 4 ? UNIT : UNIT / 2;
     auto take = [&](int k, int at, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
-        constexpr int TILES = MASKED ? 1 : UNIT;
+        constexpr int TILES = MASKED ? 1 : AT_ONCE;
         const int stage = k % STAGES, first = (t0 + (warp + WARPS * k) * unit + at) * KV4_TILE;
         const bool there_is = flags >> (4 * stage + at) & 1;
         uint32_t unit_at = ring_at + (stage * UNIT + at) * TILE;
         asm volatile("" : "+r"(unit_at) : : "memory");
-        float p[TILES][NT][4], high[NT][2];
+        float p[TILES][NT][4], high[NT][2], step_top[G];
         uint32_t value_step[TILES][2][G];
 #pragma unroll
         for (int n = 0; n < NT; ++n) high[n][0] = high[n][1] = -INFINITY;
-        float step_top = 0.f;
+#pragma unroll
+        for (int g = 0; g < G; ++g) step_top[g] = 0.f;
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const uint32_t tile = unit_at + t * TILE;
@@ -411,13 +422,14 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                     p[t][n][i] = v;
                     high[n][i & 1] = fmaxf(high[n][i & 1], v);
                 }
-            // the largest step of the values, for the common power of two
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 load_words(tile + KV4_TILE * D + 64 * G + step_at[i], value_step[t][i]);
+                if (MASKED && (first + t * KV4_TILE + place[i] >= s.n || !there_is))
 #pragma unroll
-                for (int g = 0; g < G; ++g)
-                    if (!MASKED || (first + t * KV4_TILE + place[i] < s.n && there_is)) step_top = fmaxf(step_top, Ty::lo(value_step[t][i][g]));
+                    for (int g = 0; g < G; ++g) value_step[t][i][g] = 0;
+#pragma unroll
+                for (int g = 0; g < G; ++g) step_top[g] = fmaxf(step_top[g], Ty::lo(value_step[t][i][g]));
             }
         }
         if (a.scores) {
@@ -432,39 +444,83 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                             a.scores[row_of(r) * a.N + e] = p[t][n][i] * factor[n][i & 1];
                     }
         }
-        // weights are relative to a maximum that is replaced, with what is there so far, only when a score is above it by 8 (weights then stay below 2^8) or a
-        // step needs a larger power of two
-        bool grown = step_top > limit_step;
+        // Weights are relative to a maximum, a whole number, that is replaced only when a score is above it by 8 (weights then stay below 2^8); what is there so far
+        // shrinks by a power of two, which the outputs' units take.  The units are looked at where the lane's largest weight times its largest step asks for it.
+        bool grown = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) grown |= high[n][i] * factor[n][i] > top[n][i] + 8.f;
+            for (int i = 0; i < 2; ++i) {
+                const float over = fmaf(high[n][i], factor[n][i], -top[n][i]), most = exp2_of(over);
+                grown |= over > 8.f;
+#pragma unroll
+                for (int g = 0; g < G; ++g) grown |= most * step_top[g] > __int_as_float(cap[g][n][i]);
+            }
         if (__any_sync(0xffffffffu, grown)) {
-            const int power_new = max(power, static_cast<int>(__reduce_max_sync(0xffffffffu, __float_as_uint(step_top)) >> 23) - 126);
-            const float less = __uint_as_float(static_cast<uint32_t>(max(127 + power - power_new, 0)) << 23);
-            power = power_new;
-            limit_step = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);
+            // the lane's largest weight times its least step is below what its entries have: often enough to find the units by; else they are looked at one by one
+            float step_least[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                step_least[g] = step_top[g];
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) step_least[g] = fminf(step_least[g], fminf(Ty::lo(value_step[t][0][g]), Ty::lo(value_step[t][1][g])));
+            }
+            auto of_all = [](float v) {           // the largest of the lanes that have the same rows
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+                return v;
+            };
+            auto peak_of = [&](int g, int n, int i) {
+                float v = 0.f;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) v = fmaxf(v, exp2_of(fmaf(p[t][n][2 * j + i], factor[n][i], -top[n][i])) * Ty::lo(value_step[t][j][g]));
+                return v;
+            };
+            auto exponent_of = [](float v) { return min(static_cast<int>(__float_as_uint(v) >> 23), 239); };
+            auto outputs_by = [&](int g, int n, int i, int exponent) {
+                const float f = __uint_as_float(static_cast<uint32_t>(max(127 + exponent, 0)) << 23);
+#pragma unroll
+                for (int m = 2 * g * PER_G; m < 2 * (g + 1) * PER_G; ++m) {
+                    o[m][n][i] *= f;
+                    o[m][n][2 + i] *= f;
+                }
+            };
+            bool tight = false;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float v = high[n][i] * factor[n][i];
-#pragma unroll
-                    for (int d = 4; d < 32; d *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-                    v = fmaxf(v, top[n][i]);
-                    const float fall = v == -INFINITY ? 1.f : exp2_of(top[n][i] - v), f = fall * less;
+                    float v = of_all(high[n][i] * factor[n][i]);
+                    v = v > top[n][i] + 8.f ? floorf(v) : top[n][i];
+                    const int fall = static_cast<int>(fmaxf(top[n][i] - v, -255.f));          // -255 where there was no maximum, too
+                    const float f = __uint_as_float(static_cast<uint32_t>(max(127 + fall, 0)) << 23), most = exp2_of(v == -INFINITY ? v : fmaf(high[n][i], factor[n][i], -v));
                     top[n][i] = v;
-                    total[n][i] *= fall;
+                    total[n][i] *= f;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) offs[g][n][i] *= fall;
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        o[m][n][i] *= f;
-                        o[m][n][2 + i] *= f;
+                    for (int g = 0; g < G; ++g) {
+                        offs[g][n][i] *= f;
+                        const float least = MASKED ? peak_of(g, n, i) : most * step_least[g];
+                        const int had = (cap[g][n][i] >> 23) + fall, has = max(max(had, LEAST_CAP >> 23), exponent_of(of_all(least)) + 15);
+                        cap[g][n][i] = has << 23;
+                        tight |= !MASKED && most * step_top[g] > __int_as_float(cap[g][n][i]);
+                        if (k + at > 0) outputs_by(g, n, i, had - has);
                     }
                 }
+            if (!MASKED && __any_sync(0xffffffffu, tight)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int g = 0; g < G; ++g) {
+                            const int had = cap[g][n][i] >> 23, e = exponent_of(of_all(peak_of(g, n, i))), has = e >= had ? e + 15 : had;
+                            cap[g][n][i] = has << 23;
+                            outputs_by(g, n, i, had - has);
+                        }
+            }
         }
-        const float scaled = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
         float from[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -488,18 +544,19 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
                 uint32_t hi[NT][2], lo[NT][2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float st = Ty::lo(value_step[t][i][g]), off = Ty::hi(value_step[t][i][g]);
+                    const float st = Ty::lo(value_step[t][i][g]), off = Ty::hi(value_step[t][i][g]);
                     const int e = first + t * KV4_TILE + place[i];
-                    if (MASKED && (e >= s.n || !there_is)) st = off = 0.f;
-                    st *= scaled;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        const float p0 = p[t][n][2 * i], p1 = p[t][n][2 * i + 1], w0 = p0 * st, w1 = p1 * st;
+                        const float p0 = p[t][n][2 * i], p1 = p[t][n][2 * i + 1];
+                        uint32_t w0, w1;
+                        f2_split(f2_mul(f2_mul(f2_pack(__float_as_uint(p0), __float_as_uint(p1)), f2_pack(__float_as_uint(st), __float_as_uint(st))),
+                                        f2_pack(__float_as_uint(unit_of(cap[g][n][0])), __float_as_uint(unit_of(cap[g][n][1])))), w0, w1);
                         offs[g][n][0] = MASKED && e >= limit[n][0] ? offs[g][n][0] : fmaf(p0, off, offs[g][n][0]);
                         offs[g][n][1] = MASKED && e >= limit[n][1] ? offs[g][n][1] : fmaf(p1, off, offs[g][n][1]);
-                        const uint32_t w = half2_of(w0, w1);
+                        const uint32_t w = half2_of(__uint_as_float(w0), __uint_as_float(w1));
                         hi[n][i] = transposed(w);
-                        if (TWO) lo[n][i] = transposed(half2_of(w0 - Half::lo(w), w1 - Half::hi(w)));
+                        if (TWO) lo[n][i] = transposed(half2_of(__uint_as_float(w0) - Half::lo(w), __uint_as_float(w1) - Half::hi(w)));
                     }
                 }
 #pragma unroll
@@ -528,7 +585,9 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         }
         const int f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
         const unsigned whole = (1u << count) - 1u;
-        if (count == UNIT && (f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole) take(k, 0, std::false_type());
+        if (count == UNIT && (f + count) * KV4_TILE <= least && (flags >> 4 * stage & whole) == whole)
+#pragma unroll 1
+            for (int i = 0; i < UNIT; i += AT_ONCE) take(k, i, std::false_type());
         else
 #pragma unroll 1
             for (int i = 0; i < count; ++i) take(k, i, std::true_type());
@@ -544,7 +603,6 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     __syncthreads();
     constexpr int PITCH = D + 4;
     float *outs = reinterpret_cast<float*>(smem), *joined = outs + WARPS * R * PITCH;
-    const float back = __uint_as_float(static_cast<uint32_t>(127 + power) << 23);       // and codes were in units of 2^-24, in rows gid + 8 of 2^-20
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -559,6 +617,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
             if (gid == 0) stat[warp][r] = make_float2(top[n][i], total[n][i]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
+                const float back = __int_as_float(cap[m / (2 * PER_G)][n][i] - (15 << 23));          // and codes were in units of 2^-24, in rows gid + 8 of 2^-20
                 outs[(warp * R + r) * PITCH + 16 * m + gid] = fmaf(o[m][n][i] * 0x1p24f, back, offs[m / (2 * PER_G)][n][i]);
                 outs[(warp * R + r) * PITCH + 16 * m + gid + 8] = fmaf(o[m][n][2 + i] * 0x1p20f, back, offs[m / (2 * PER_G)][n][i]);
             }

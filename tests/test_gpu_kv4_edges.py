@@ -131,3 +131,78 @@ def test_fp16_queries_and_keys_far_apart(size, keys, scale):
     api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, 300]))
     q = ((torch.rand(2, 4, 128, generator=gen) * 2 - 1) * size).to(F16)
     check(f, q, [2], scale)
+
+
+def attend_by_group(q, k, v, group, scale=None):
+    """As kv4_reference.attend, but what the products of weights and steps lose below fp16's range counts against the largest such product of the same row and group
+    of channels: half of fp16's last place, 2^-25 of it, for each entry's code up to 15."""
+    out, far, got, got_far = ref.attend(q, k, v, group, scale)
+    (t, Hq, D), (n, H) = q.shape, k.shape[:2]
+    scale = D ** -0.5 if scale is None else scale
+    vp, vs = ref.parts(v, group)        # [n, H, D], [n, H, groups]
+    (kp, _), kk, vv = ref.parts(k, group), ref.values(k, group), ref.values(v, group)
+    for j in range(Hq):
+        h = j // (Hq // H)
+        a = scale * (q[:, j].double() @ kk[:, h].T)
+        seen = torch.arange(n) <= (n - t + torch.arange(t)).unsqueeze(1)
+        p = torch.where(seen.any(1, keepdim=True), torch.softmax(torch.where(seen, a, -math.inf), 1), 0.0)
+        size = scale * (q[:, j].double().abs() @ kp[:, h].T)
+        off = size * (D / 16 + 8) * 2.0 ** -23 + 2.0 ** -34 * scale * q[:, j].double().abs().amax(1, keepdim=True) * kp[:, h].sum(1)
+        # what a row does not attend to may be as far off as it is: entries count by the weights that they may have
+        most = p * torch.exp(2 * off.clamp(max=50))
+        mean = (most * off).sum(1, keepdim=True)
+        weight = p * (2 * torch.expm1((off + mean + 6 * 2.0 ** -24 * size).clamp(max=50)) + 2.0 ** -19 + (n / 16 + 16) * 2.0 ** -24 + (2.0 ** -22 if q.dtype == F16 else 2.0 ** -11))
+        largest = (p.unsqueeze(-1) * vs[:, h]).amax(1)        # [t, groups]
+        lost = n * 15 * 2.0 ** -25 * 2 * largest.repeat_interleave(group, 1)
+        bound = weight @ vp[:, h] + lost
+        far[:, j] = bound + ref.HALF[q.dtype] * (out[:, j].abs() + bound) + torch.finfo(q.dtype).smallest_normal * torch.finfo(q.dtype).eps
+    return out, far, got, got_far
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("power", [4, 10, 14, 16])
+@pytest.mark.parametrize("where", ["first", "last", "among"])
+def test_large_values_that_get_no_attention(where, power, dtype):
+    """Entries whose values are far larger than the others', and whose scores leave them no weight: the others lose nothing by them."""
+    n, D = 400, 128
+    f = Filled(35, [n], 1, D, 64, 128, dtype, fill=False)
+    gen = torch.Generator().manual_seed(power)
+    q = torch.randn(3, 4, D, generator=gen)
+    q[..., 0] = 4.0
+    f.k[0][:, 0, 0] = 0
+    f.v[0] = (torch.randn(n, 1, D, generator=gen) * 2.0 ** -6).to(dtype)
+    at = {"first": slice(0, 3), "last": slice(n - 6, n - 3), "among": slice(5, n, 37)}[where]
+    f.k[0][at, 0, 0] = -400.0
+    f.v[0][at] = (torch.randn(f.v[0][at].shape, generator=gen) * 2.0 ** (power - 6)).to(dtype)
+    api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, n]))
+    check(f, q.to(dtype), [3], reference=attend_by_group)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("D,group", [(64, 32), (96, 32), (128, 32), (128, 64)])
+def test_groups_of_channels_of_other_sizes(D, group, dtype):
+    """Values whose groups of channels are powers of two apart, the smallest 2^-14 of the largest."""
+    f = Filled(36, [300, 33], 2, D, 16, group, dtype, fill=False)
+    groups = D // group
+    size = torch.exp2(torch.linspace(0, -14, groups)).repeat_interleave(group)
+    f.v = [(v.float() * size).to(dtype) for v in f.v]
+    api.append_kv4(torch.cat(f.k).cuda(), torch.cat(f.v).cuda(), f.cache, f.table, ints([0, 0]), starts_of([300, 33]))
+    q = torch.randn(8, 6, D, generator=torch.Generator().manual_seed(9)).to(dtype)
+    check(f, q, [5, 3], reference=attend_by_group)
+
+
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("step", [0.5, 3.0, 20.0, 300.0])
+def test_scores_and_values_that_climb_apart(step, order):
+    """Scores that grow along the sequence while the values shrink by as much or more, and the other way round."""
+    n = 600
+    f = Filled(37, [n], 1, 64, 32, 64, BF16, fill=False)
+    gen = torch.Generator().manual_seed(6)
+    q = torch.zeros(2, 3, 64)
+    q[..., 0] = 1.0
+    f.k[0] = torch.randn(n, 1, 64, generator=gen).to(BF16)
+    f.k[0][:, 0, 0] = (order * step * torch.arange(n) / 16).to(BF16)
+    for slope in (-1, 1):
+        f.v[0] = (torch.randn(n, 1, 64, generator=gen) * torch.exp2(slope * 90 * (torch.arange(n) / n - 0.5)).view(-1, 1, 1)).to(BF16)
+        api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, n]))
+        check(f, q.to(BF16), [2], 1.0, reference=attend_by_group)
