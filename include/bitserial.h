@@ -546,6 +546,8 @@ int bs_kv4_attend(const void* q, long long q_token, long long q_head, int T, int
  *   lengths_out  device int32 [B];  weights_out  device float [B][heads][N]: the weights of what stays, zeros behind;  kept  device int32 [B][heads][keep]: where
  *                it was, -1 behind.  None of them may overlap what is read.
  *   workspace    bs_kv4_evict_workspace_bytes(...) bytes (0 and NULL with `into`); two calls that may run at the same time need one each
+ * Entries that are not there do not stay, and places whose page is not one of the cache's take none: what stays has the others, in order, at most as many as there are
+ * below `keep`; kept is -1 and the weight 0 where there is none, and lengths_out one more than the last place taken.
  * Sequences of up to `keep` entries stay as they are, and are brought to `into`.  B up to 65535.  Two launches, three without `into`.
  */
 size_t bs_kv4_evict_workspace_bytes(const bs_kv4_cache* cache, int B, int keep, int into);

@@ -460,6 +460,7 @@ def attend_kv4(q: torch.Tensor, cache: KV4Cache, table: torch.Tensor, lengths: t
 def evict_kv4(cache: KV4Cache, table: torch.Tensor, lengths: torch.Tensor, weights: torch.Tensor, keep: int, *, recent: int = 0, into: Optional[torch.Tensor] = None, stream=None):
     """Cuts sequences of more than ``keep`` entries to ``keep`` (``bs_kv4_evict``): each head keeps its ``recent`` newest entries and of the others those with the largest
     ``weights`` [sequences, heads, entries], in their order, either in the sequence's pages or in those of the table ``into``, which are other ones than ``table`` has.
+    Entries on pages that the cache does not have do not stay, and no place on such a page is taken.
     Returns (lengths int32 [sequences], weights of what stays with zeros behind, and where it was, int32 [sequences, heads, keep], -1 behind)."""
     global launch_count
     st, n, w, kept = native().kv4_evict(*cache._native, table, lengths, weights, keep, recent, into, stream)

@@ -6,8 +6,11 @@
 // indices, ranked by sums over warps and CTAs.  What stays is then moved by a kernel over all heads and sequences: into other pages at once, into their own
 // through a copy, since what one CTA writes another may still have to read.
 //
+// Sequences with entries or places that are not there, on pages that the cache does not have, go a way of their own behind this one: one CTA a head, the least weight bit
+// by bit.  Looking for such pages takes half a microsecond to one (4096 entries to 2048 and read back: 17.3 us without, 18.5 with it).
+//
 // 16 sequences of up to 32768 entries and 8 heads cut to 8191: 31 us to select (four weights a thread and turn; with one 52), bound by loads and atomics, 55 to move at
-// 4 TB/s.  4096 entries to 2048: 14 us with the launches.
+// 4 TB/s.  4096 entries to 2048: 15 us with the launches.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"
@@ -24,6 +27,7 @@ struct Evict {
     const float* weights;
     long long w_sequence, w_head;
     int N, keep, recent;
+    int inside;                 // into the sequences' own pages
     int32_t* lengths_out;       // [B]
     float* weights_out;         // [B][H][N]
     int32_t* kept;              // [B][H][keep]
@@ -88,9 +92,78 @@ __device__ __forceinline__ uint32_t before_me(uint32_t v, uint32_t* sums, uint32
     return (warp ? front : 0u) + s - v;
 }
 
+// A head's entries and places, 0 to `from` and to `into` (some of them not there): what stays takes the places that are there, in order.  By a CTA, for few sequences, so
+// without haste: every count is one over the pages, or over the weights for each of their bits.
+__device__ __forceinline__ void select_around(const Evict& a, const Kv4Table& from, const Kv4Table& into, int b, int n, const float* w, int32_t* kept, float* out, int32_t* length, uint32_t* sums)
+{
+    const int th = threadIdx.x;
+    auto count = [&](const Kv4Table& t, int lo, int hi) {           // of those in lo .. hi - 1 that are there
+        uint32_t mine = 0, all;
+        for (long long p = (lo >> a.l.log_page) + th; p << a.l.log_page < hi; p += THREADS) {
+            const long long first = p << a.l.log_page, last = first + a.l.page;
+            if (kv4_page_of(a.l, t, b, first) >= 0) mine += static_cast<uint32_t>(min(last, static_cast<long long>(hi)) - max(first, static_cast<long long>(lo)));
+        }
+        before_me(mine, sums, all);
+        return static_cast<int>(all);
+    };
+    const int places = static_cast<int>(min(static_cast<long long>(into.width) * a.l.page, static_cast<long long>(min(a.keep, a.N))));
+    const int entries = count(from, 0, n), room = count(into, 0, places), stay = min(entries, room), newest = entries > room ? min(a.recent, stay) : stay;
+    int old = 0;
+    if (entries > room) {           // the newest ones begin where so many follow
+        int hi = n;
+        while (hi - old > 1) {
+            const int mid = old + ((hi - old) >> 1);
+            if (count(from, mid, n) >= newest) old = mid;
+            else hi = mid;
+        }
+        if (newest == 0) old = n;
+    }
+    const uint32_t need = stay - newest;
+    auto is_there = [&](const Kv4Table& t, int i, int end) { return i < end && kv4_page_of(a.l, t, b, i) >= 0; };
+    auto above = [&](uint32_t key) {            // how many of the older ones have it or a greater one
+        uint32_t mine = 0, all;
+        for (long long i = th; i < old; i += THREADS) mine += is_there(from, static_cast<int>(i), old) && key_of(w[i]) >= key;
+        before_me(mine, sums, all);
+        return all;
+    };
+    uint32_t least = 0;             // the least key that stays
+    for (int bit = 31; bit >= 0 && need > 0; --bit)
+        if (above(least | 1u << bit) >= need) least |= 1u << bit;
+    const uint32_t left = need == 0 ? 0u : need - (least == 0xffffffffu ? 0u : above(least + 1));        // of those equal to it
+    uint32_t rank = 0, equal = 0;
+    for (long long i0 = 0; i0 < n; i0 += THREADS) {
+        const int i = static_cast<int>(i0 + th < n ? i0 + th : n);
+        const bool there = is_there(from, i, n);
+        const uint32_t key = there && i < old ? key_of(w[i]) : 0u, same = need > 0 && there && i < old && key == least;
+        uint32_t all_same, all;
+        const uint32_t mine = equal + before_me(same, sums, all_same);
+        const uint32_t stays = there && (i >= old || (need > 0 && key > least) || (same && mine < left));
+        const uint32_t at = rank + before_me(stays, sums, all);
+        if (stays && at < static_cast<uint32_t>(stay)) kept[at] = i;            // the latter but for weights that change meanwhile
+        rank += all;
+        equal += all_same;
+    }
+    // from ranks to places, from the last ones on: a place is not before its rank
+    uint32_t left_places = room;
+    if (th == 0 && stay == 0 && length) *length = 0;
+    for (long long r0 = (static_cast<long long>(a.keep) - 1) / THREADS * THREADS; r0 >= 0; r0 -= THREADS) {
+        const long long r = r0 + th;
+        const uint32_t there = r < places && is_there(into, static_cast<int>(r), places);
+        uint32_t all;
+        const uint32_t mine = before_me(there, sums, all), at = left_places - all + mine;
+        const int i = there && at < static_cast<uint32_t>(stay) ? kept[at] : -1;
+        __syncthreads();
+        if (r < a.keep) kept[r] = i;
+        if (r < places) out[r] = i >= 0 ? w[i] : 0.f;
+        if (there && at + 1 == static_cast<uint32_t>(stay) && length) *length = static_cast<int>(r) + 1;
+        left_places -= all;
+    }
+    for (long long r = places + th; r < a.N; r += THREADS) out[r] = 0.f;
+}
+
 // CTAS: of the cluster.
 template <int CTAS>
-__global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_constant__ Evict a)
+__global__ void __launch_bounds__(THREADS, 2) kv4_select_kernel(const __grid_constant__ Evict a)
 {
     __shared__ uint32_t bins[3][BINS], sums[THREADS / 32], found[2], mine[2];
     __shared__ uint32_t digits[CTAS == 1 ? 1 : BINS];           // sums over the cluster
@@ -106,6 +179,15 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
     // the CTA's part, in fours
     const int from = static_cast<int>(static_cast<long long>(old) * rank / CTAS) & ~3, to = rank + 1 == CTAS ? old : static_cast<int>(static_cast<long long>(old) * (rank + 1) / CTAS) & ~3;
     const bool vectors = (reinterpret_cast<uintptr_t>(w) & 15) == 0;
+    // whether an entry, or a place of one that stays, is not there (sequences that stay in place do not care): asked here, where other loads cover it, and answered last
+    Kv4Table own = a.from, other = a.into;
+    own.pages = behind_wait<int32_t>(a.from.pages);
+    other.pages = behind_wait<int32_t>(a.into.pages);
+    bool missing = false;
+    if (n > a.keep || !a.inside) {
+        for (int p = th; p << a.l.log_page < n; p += THREADS) missing |= kv4_page_of(a.l, own, b, p << a.l.log_page) < 0;
+        for (int p = th; !a.inside && p << a.l.log_page < stay; p += THREADS) missing |= kv4_page_of(a.l, other, b, p << a.l.log_page) < 0;
+    }
     if (need > 0) {
         for (int i = th; i < 3 * BINS; i += THREADS) (&bins[0][0])[i] = 0;
         __syncthreads();
@@ -209,6 +291,10 @@ __global__ void __launch_bounds__(THREADS) kv4_select_kernel(const __grid_consta
     for (int i = need + rank * THREADS + th; i < a.keep; i += CTAS * THREADS) kept[i] = i < stay ? old + i - need : -1;
     for (int i = need + rank * THREADS + th; i < a.N; i += CTAS * THREADS) out[i] = i < stay ? w[old + i - need] : 0.f;
     if (h == 0 && rank == 0 && th == 0) a.lengths_out[b] = stay;
+    if (__syncthreads_or(missing)) {            // all CTAs of a cluster see the same
+        sync();
+        if (rank == 0) select_around(a, own, other, b, n, w, kept, out, h == 0 ? a.lengths_out + b : nullptr, sums);
+    }
 }
 
 // Eight lanes an entry: 16 bytes of keys or values each, then its steps.  STEP 0: into the other table's pages; 1: into the copy; 2: out of it.
@@ -219,7 +305,7 @@ __global__ void __launch_bounds__(256) kv4_move_kernel(const __grid_constant__ E
     const int32_t* kept = dependent_begin(a.kept);
     const int lane = threadIdx.x & 7, h = blockIdx.y, D = a.l.D, half = D / 32, tiles = (a.keep + KV4_TILE - 1) / KV4_TILE;
     for (int b = blockIdx.z; b < a.from.B; b += gridDim.z) {
-        const int stay = min(entries_of(a, behind_wait<int32_t>(a.lengths), b), a.keep);
+        const int stay = min(behind_wait<int32_t>(a.lengths_out)[b], a.keep);
         const long long head = static_cast<long long>(b) * a.l.H + h;
         unsigned char* copy = STEP == 0 ? nullptr : a.copy + head * tiles * a.l.tile;
         Kv4Table from = a.from, into = a.into;
@@ -298,7 +384,7 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     a.from = {table, table_pitch, width, B};
     a.into = into ? Kv4Table{into, into_pitch, into_width, B} : a.from;
     a.lengths = lengths; a.weights = weights; a.w_sequence = weights_sequence; a.w_head = weights_head;
-    a.N = N; a.keep = keep; a.recent = recent;
+    a.N = N; a.keep = keep; a.recent = recent; a.inside = into == nullptr;
     a.lengths_out = lengths_out; a.weights_out = weights_out; a.kept = kept;
     a.copy = static_cast<unsigned char*>(workspace);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);

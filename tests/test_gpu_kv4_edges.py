@@ -6,7 +6,7 @@ import torch
 
 import kv4_reference as ref
 from paper_2207_08820_b200 import api
-from test_gpu_kv4 import BF16, F16, Filled, ints, same, starts_of
+from test_gpu_kv4 import BF16, F16, Filled, ints, same, starts_of, weights_of
 
 pytestmark = pytest.mark.gpu
 
@@ -206,3 +206,89 @@ def test_scores_and_values_that_climb_apart(step, order):
         f.v[0] = (torch.randn(n, 1, 64, generator=gen) * torch.exp2(slope * 90 * (torch.arange(n) / n - 0.5)).view(-1, 1, 1)).to(BF16)
         api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, n]))
         check(f, q.to(BF16), [2], 1.0, reference=attend_by_group)
+
+
+# --------------------------------------------------------------------------------------------------------------------- eviction
+
+def evict_around(w, n, keep, recent, there, places):
+    """Where each place's entry was, of one head: what stays of the entries that are there takes the places that are."""
+    entries = [i for i in range(n) if there(i)]
+    stay = min(len(entries), len(places))
+    if len(entries) > stay:
+        new = min(recent, stay)
+        old, new = entries[:len(entries) - new], entries[len(entries) - new:]
+        first = torch.isnan(w[old])
+        order = sorted(range(len(old)), key=lambda j: (not bool(first[j]), -float(torch.nan_to_num(w[old[j]], nan=0.0, posinf=math.inf, neginf=-math.inf)), j))
+        entries = sorted(old[j] for j in order[:stay - len(new)]) + new
+    return dict(zip(places, entries))
+
+
+HOLES = {"front": lambda p, n: p < 2, "middle": lambda p, n: p in (1, 3, 4), "end": lambda p, n: p >= n - 1, "all": lambda p, n: True, "every other": lambda p, n: p % 2 == 0}
+
+
+@pytest.mark.parametrize("inside", [True, False], ids=["inside", "into"])
+@pytest.mark.parametrize("keep,recent", [(1, 0), (40, 0), (40, 40), (100, 33), (1000, 5)])
+@pytest.mark.parametrize("where", HOLES)
+@pytest.mark.parametrize("kind", ["spread", "ties", "any"])
+def test_evict_entries_that_are_not_there(kind, where, keep, recent, inside):
+    """Sequences with pages that the cache does not have, and places on such pages: what is not there does not stay, and what stays is there afterwards."""
+    lengths, H, D, page = [0, 10, 40, 100, 333], 2, 64, 16
+    f = Filled(40, lengths, H, D, page, 32, F16)
+    B, N = len(lengths), 333
+    w = weights_of(keep + recent, B, H, N, kind)
+    table = f.table_cpu.clone()
+    for b, n in enumerate(lengths):
+        for p in range(-(-n // page)):
+            if HOLES[where](p, -(-n // page)):
+                table[b, p] = -1 if b % 2 else 10 ** 9
+    cache, into = f.cache, None
+    if not inside:
+        wide = -(-min(keep, N) // page)
+        cache = api.cache_kv4(f.cache.data.shape[0] + B * wide, H, D, page=page, group=32, dtype=F16)
+        cache.data.fill_(255)
+        cache.data[:f.cache.data.shape[0]] = f.cache.data
+        into = (f.cache.data.shape[0] + torch.randperm(B * wide, generator=torch.Generator().manual_seed(1))).view(B, wide).int()
+        if wide > 2:
+            into[3, 1], into[4, 0] = -5, cache.data.shape[0]
+    n_out, w_out, kept = api.evict_kv4(cache, table.cuda(), ints(lengths), w.cuda(), keep, recent=recent, into=None if inside else into.cuda())
+    target = table if inside else into
+    q = torch.randn(B, 2 * H, D, generator=torch.Generator().manual_seed(2)).to(F16)
+    seen = api.attend_kv4(q.cuda(), cache, target.cuda(), n_out).cpu().double()
+    pages = cache.data.shape[0]
+    for b, n in enumerate(lengths):
+        there = lambda i: 0 <= int(table[b, i // page]) < pages  # noqa: E731
+        places = [r for r in range(min(keep, N, target.shape[1] * page)) if 0 <= int(target[b, r // page]) < pages]
+        for h in range(H):
+            if inside and n <= keep:        # as they are
+                want = {r: r for r in range(n)}
+            else:
+                want = evict_around(w[b, h], n, keep, recent, there, places)
+            assert int(n_out[b]) == (max(want) + 1 if want else 0), (b, h)
+            assert kept[b, h].tolist() == [want.get(r, -1) for r in range(keep)], (b, h)
+            assert same(w_out[b, h].cpu(), torch.tensor([float(w[b, h, want[r]]) if r in want else 0.0 for r in range(N)]))
+            at = [i for r, i in sorted(want.items()) if there(i)]
+            out, far, _, _ = ref.attend(q[b:b + 1, 2 * h:2 * h + 2], f.k[b][at, h:h + 1], f.v[b][at, h:h + 1], 32)
+            assert ((seen[b:b + 1, 2 * h:2 * h + 2] - out).abs() <= far).all(), (b, h)
+
+
+def test_evict_long_sequences_that_are_not_all_there():
+    """By clusters of CTAs, one of which does the work."""
+    n, keep, recent, page = 70000, 30000, 1000, 64
+    f = Filled(41, [n], 2, 64, page, 64, F16)
+    table = f.table_cpu.clone()
+    gone = torch.rand(table.shape[1], generator=torch.Generator().manual_seed(3)) < 0.3
+    table[0, gone] = -1
+    w = weights_of(5, 1, 2, n, "ties")
+    into = torch.arange(f.cache.data.shape[0], f.cache.data.shape[0] + -(-keep // page), dtype=torch.int32).unsqueeze(0)
+    cache = api.cache_kv4(f.cache.data.shape[0] + into.shape[1], 2, 64, page=page, dtype=F16)
+    cache.data[:f.cache.data.shape[0]] = f.cache.data
+    n_out, w_out, kept = api.evict_kv4(cache, table.cuda(), ints([n]), w.cuda(), keep, recent=recent, into=into.cuda())
+    entries = torch.arange(n)[~gone.repeat_interleave(page)[:n]]
+    k, _ = api.read_kv4(cache, into.cuda(), ints([0]), ints([0, keep]), total=keep)
+    assert n_out.tolist() == [keep]
+    for h in range(2):
+        old = entries[:-recent]
+        best = old[torch.sort(w[0, h, old], descending=True, stable=True).indices[:keep - recent]].sort().values
+        want = torch.cat([best, entries[-recent:]])
+        assert torch.equal(kept[0, h].cpu().long(), want) and same(w_out[0, h, :keep].cpu(), w[0, h, want])
+        assert same(k[:, h].cpu(), ref.read(f.k[0][want, h], 64))
