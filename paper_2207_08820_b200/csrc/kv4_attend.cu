@@ -351,7 +351,6 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
         step_at[i] = place[i] * (4 * G);
     }
     const uint32_t value_at = tid * (D / 2) + kv4_value_part(D, tid, gid) * (D / 16);
-    bool late = false;
 
     auto unit_of = [](int cap) { return __uint_as_float((269u << 23) - static_cast<uint32_t>(cap)); };          // 2^15 / cap
 
@@ -579,9 +578,12 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     };
     for (int k = 0; k < mine; ++k) {
         const int stage = k % STAGES;
-        if (!late && !mm_wait(&bars[warp][stage], k / STAGES & 1)) {
-            late = true;
-            atomicOr(a.status, STATUS_TIMEOUT);
+        if (__any_sync(0xffffffffu, !mm_wait(&bars[warp][stage], k / STAGES & 1))) {
+            // a wait that ran out: no more copies, and those on their way get as long again, since the outputs go where they land
+            if (lane == 0) atomicOr(a.status, STATUS_TIMEOUT);
+            for (int i = k; i < mine && i < k + STAGES; ++i) mm_wait(&bars[warp][i % STAGES], i / STAGES & 1);
+            __syncwarp();
+            break;
         }
         const int f = t0 + (warp + WARPS * k) * unit, count = min(unit, t1 - f);
         const unsigned whole = (1u << count) - 1u;
