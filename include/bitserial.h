@@ -497,7 +497,8 @@ int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, in
  *       m = min x,  s = type((max x - min x) / 15), difference and quotient in binary32,  c = clip(round((x - m) / s), 0, 15)
  * round is half-even of the exact quotient; where s is 0 c is 0.  It stands for c s + m.  A vector that holds an infinity or a NaN (or whose span binary32 does
  * not hold) stands for NaN.
- * Supported: D of 64, 96 or 128, groups of 32, 64 or D that divide D, pages of 16 to 1024 entries, a power of two.
+ * Supported: D of 64, 96 or 128, groups of 32, 64 or D that divide D, pages of 16 to 1024 entries, a power of two; up to 2^30 tokens stored or read, entries that are
+ * weighted (N) or kept, and tokens of prompts a call.
  *
  * Rows of several sequences are packed: `starts` is int32 [B + 1], sequence b's rows are starts[b] .. starts[b + 1] - 1, in ascending order; rows that no sequence
  * holds are neither read nor written.  NULL: T = B, a row a sequence.  Tables, lengths and starts are device memory; what lies outside of the tensors is not touched,

@@ -16,6 +16,7 @@
 namespace bs {
 
 constexpr int KV4_TILE = 16;        // entries
+constexpr int MOST_ROWS = 1 << 30;  // entries or tokens of a call: what loops over them step beyond the last one stays within 31 bits
 
 struct Kv4 {
     unsigned char* data;

@@ -875,7 +875,7 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0 || q_heads <= 0 || q_heads % cache->heads != 0) return BS_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !(scale * 1.4426950408889634f < INFINITY) || (!starts && T != B)) return BS_ERR_INVALID_ARG;
     if (weights && (N <= 0 || weights_head < N || weights_sequence < 0)) return BS_ERR_INVALID_ARG;
-    if (!kv4_layout(*cache, a.l) || q_heads > 65535) return BS_ERR_UNSUPPORTED;
+    if (!kv4_layout(*cache, a.l) || q_heads > 65535 || (weights && N > MOST_ROWS)) return BS_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(cache->data) || !aligned16(out) || !aligned16(workspace) || (q_token | q_head) % 8 != 0) return BS_ERR_ALIGNMENT;
     if (T == 0) return BS_OK;
     const int sms = device_sm_count();

@@ -361,7 +361,7 @@ using namespace bs;
 extern "C" size_t bs_kv4_evict_workspace_bytes(const bs_kv4_cache* cache, int B, int keep, int into)
 {
     Kv4 l;
-    if (!cache || B <= 0 || keep <= 0 || !kv4_layout(*cache, l)) return 0;
+    if (!cache || B <= 0 || keep <= 0 || keep > MOST_ROWS || !kv4_layout(*cache, l)) return 0;
     return into ? 0 : static_cast<size_t>(B) * l.H * ceil_div(keep, KV4_TILE) * l.tile;
 }
 
@@ -375,7 +375,7 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0) return BS_ERR_INVALID_ARG;
     if (N <= 0 || keep <= 0 || recent < 0 || recent > keep || weights_head < 0 || (weights_head > 0 && weights_head < N) || weights_sequence < 0) return BS_ERR_INVALID_ARG;
     if (into && (into_width <= 0 || into_pitch < into_width)) return BS_ERR_INVALID_ARG;
-    if (!kv4_layout(*cache, a.l) || B > 65535) return BS_ERR_UNSUPPORTED;
+    if (!kv4_layout(*cache, a.l) || B > 65535 || N > MOST_ROWS || keep > MOST_ROWS) return BS_ERR_UNSUPPORTED;
     const long long most = static_cast<long long>(width) * a.l.page < N ? static_cast<long long>(width) * a.l.page : N, stays = keep < most ? keep : most;
     if (into && static_cast<long long>(into_width) * a.l.page < stays) return BS_ERR_INVALID_ARG;
     const size_t need = bs_kv4_evict_workspace_bytes(cache, B, keep, into != nullptr);
@@ -389,7 +389,7 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     a.copy = static_cast<unsigned char*>(workspace);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     // a CTA takes 16384 weights in about 10 us; more of them where there are so many and the heads leave SMs free
-    const int heads = a.l.H * B, sms = device_sm_count();
+    const long long heads = static_cast<long long>(a.l.H) * B, sms = device_sm_count();
     int rc = most <= 16384 || heads * 2 > sms ? launch_select<1>(a, B, st) : most <= 65536 || heads * 8 > sms ? launch_select<2>(a, B, st) : launch_select<MOST>(a, B, st);
     if (rc != BS_OK) return rc;
     const long long chunks = ceil_div_ll(stays, 128);

@@ -347,7 +347,7 @@ int check(const bs_kv4_cache* c, const int32_t* table, long long pitch, int widt
     if (c->type != BS_F16 && c->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (c->pages <= 0 || c->heads <= 0 || c->D <= 0 || c->page <= 0 || c->group <= 0) return BS_ERR_INVALID_ARG;
     if (!starts && T != B) return BS_ERR_INVALID_ARG;
-    if (!kv4_layout(*c, a.l)) return BS_ERR_UNSUPPORTED;
+    if (!kv4_layout(*c, a.l) || T > MOST_ROWS) return BS_ERR_UNSUPPORTED;
     if (!aligned16(c->data)) return BS_ERR_ALIGNMENT;
     a.t = {table, pitch, width, B};
     a.at = at;

@@ -549,7 +549,7 @@ extern "C" int bs_attend_prompt(const void* q, long long q_token, long long q_he
     if ((starts == nullptr) != (starts_k == nullptr) || (!starts && B != 1)) return BS_ERR_INVALID_ARG;
     Prompt a{};
     a.G = q_heads / heads;
-    if (D > 128 || D % 8 != 0 || a.G > ROWS) return BS_ERR_UNSUPPORTED;
+    if (D > 128 || D % 8 != 0 || a.G > ROWS || T > MOST_ROWS || Tk > MOST_ROWS) return BS_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (q_token | q_head | k_token | k_head | v_token | v_head) % 8 != 0) return BS_ERR_ALIGNMENT;
     if (T == 0) return BS_OK;
     a.starts = starts; a.starts_k = starts_k;
