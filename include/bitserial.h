@@ -525,7 +525,7 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *   lengths  device int32 [B]: entries of each sequence, those of the rows of q (stored before) among them: with t rows of q and n entries, row i sees the entries
  *            below n - t + i + 1.  A row that sees nothing gives zeros.
  *   out      device [T][q_heads][D]: softmax(scale q K^T) V, scale > 0
- *   weights  device float [B][heads][N], rows weights_head and weights_sequence values apart, or NULL: the attention that each entry got, summed over the rows of q
+ *   weights  device float [B][heads][N], rows weights_head and weights_sequence values apart, none over another, or NULL: the attention that each entry got, summed over the rows of q
  *            and the heads that share it, is added to it.  Entries from N on are left out.
  *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights; 0 and NULL for few short sequences); two calls that may run
  *              at the same time need one each

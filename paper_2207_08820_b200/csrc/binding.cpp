@@ -713,7 +713,9 @@ PyObject* kv4_attend(PyObject*, PyObject* const* a, Py_ssize_t n)
             N = small(w.size(2));
             w_head = w.size(1) > 1 ? w.stride(1) : N;
             w_sequence = w.size(0) > 1 ? w.stride(0) : 0;
-            if (w_head < N || (w.size(0) > 1 && w_sequence < (w.size(1) - 1) * w_head + N)) mismatch("weights whose rows do not overlap expected");
+            // heads of a sequence side by side, or sequences of a head
+            if (w_head < N || (w.size(0) > 1 && w_sequence < (w.size(1) - 1) * w_head + N && (w_sequence < N || w_head < (w.size(0) - 1) * w_sequence + N)))
+                mismatch("weights whose rows do not overlap expected");
             wp = static_cast<float*>(w.data_ptr());
             if (meet(w, q) || meet(w, data)) mismatch("the weights overlap an input");
         }

@@ -875,6 +875,8 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0 || q_heads <= 0 || q_heads % cache->heads != 0) return BS_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !(scale * 1.4426950408889634f < INFINITY) || (!starts && T != B)) return BS_ERR_INVALID_ARG;
     if (weights && (N <= 0 || weights_head < N || weights_sequence < 0)) return BS_ERR_INVALID_ARG;
+    // rows that several CTAs add to: heads of a sequence side by side, or sequences of a head
+    if (weights && B > 1 && weights_sequence < (cache->heads - 1) * weights_head + N && (cache->heads == 1 || weights_sequence < N || weights_head < (B - 1) * weights_sequence + N)) return BS_ERR_INVALID_ARG;
     if (!kv4_layout(*cache, a.l) || q_heads > 65535 || (weights && N > MOST_ROWS)) return BS_ERR_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(cache->data) || !aligned16(out) || !aligned16(workspace) || (q_token | q_head) % 8 != 0) return BS_ERR_ALIGNMENT;
     if (T == 0) return BS_OK;

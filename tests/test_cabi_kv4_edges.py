@@ -1,5 +1,5 @@
 """Host-only checks of the entry points on keys and values of 4 bits: the largest sizes, refused before a device is touched."""
-from test_cabi_kv4 import OK, UNSUPPORTED, L, at, cache  # noqa: F401
+from test_cabi_kv4 import INVALID, OK, UNSUPPORTED, L, at, cache  # noqa: F401
 
 MOST = 1 << 30
 
@@ -26,3 +26,11 @@ def test_more_entries_than_indices_reach(L, at):  # noqa: F811
         assert L.bs_kv4_evict_workspace_bytes(cache(at), 1, n, 0) == 0
     assert L.bs_kv4_evict_workspace_bytes(cache(at), 1, MOST, 0) == MOST // 16 * 2 * 16 * (128 + 8)
     assert append(0) == read(0) == OK
+
+
+def test_weights_that_share_memory(L, at):  # noqa: F811
+    """Rows of weights that are added to may lie in any order, but not over one another."""
+    def attend(sequence, head, B=3, N=100, T=None):
+        return L.bs_kv4_attend(at, 512, 128, B if T is None else T, 4, cache(at), at, 4, 4, B, at, None if T is None else at, 1.0, at, at, sequence, head, N, at, 1 << 40, None)
+    assert attend(0, 100) == attend(100, 100) == attend(199, 100) == attend(99, 400) == attend(100, 299) == attend(150, 150) == INVALID
+    assert attend(200, 100, T=0) == attend(100, 300, T=0) == attend(0, 100, B=1, T=0) == OK

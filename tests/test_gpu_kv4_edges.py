@@ -292,3 +292,21 @@ def test_evict_long_sequences_that_are_not_all_there():
         want = torch.cat([best, entries[-recent:]])
         assert torch.equal(kept[0, h].cpu().long(), want) and same(w_out[0, h, :keep].cpu(), w[0, h, want])
         assert same(k[:, h].cpu(), ref.read(f.k[0][want, h], 64))
+
+
+def test_weights_in_any_order():
+    """Weights [heads, sequences, entries] as well as [sequences, heads, entries], added to and read; rows that lie over one another are refused."""
+    f = Filled(42, [70, 200, 33], 2, 64, 16, 64, BF16)
+    q, lengths = torch.randn(3, 6, 64, device="cuda").to(BF16), ints(f.lengths)
+    plain, room = torch.zeros(3, 2, 200, device="cuda"), torch.zeros(2, 3, 210, device="cuda")
+    turned = room.transpose(0, 1)[..., 5:205]
+    out = api.attend_kv4(q, f.cache, f.table, lengths, weights=plain)
+    assert torch.equal(out, api.attend_kv4(q, f.cache, f.table, lengths, weights=turned)) and torch.equal(plain, turned)
+    assert (room[..., :5] == 0).all() and (room[..., 205:] == 0).all()
+    data = f.cache.data.clone()
+    first = api.evict_kv4(f.cache, f.table, lengths, turned, 20, recent=3)
+    f.cache.data.copy_(data)
+    assert all(same(a, b) for a, b in zip(first, api.evict_kv4(f.cache, f.table, lengths, plain, 20, recent=3)))
+    for strides in ((100, 200, 1), (200, 100, 1), (0, 200, 1), (399, 200, 1)):
+        with pytest.raises(ValueError):
+            api.attend_kv4(q, f.cache, f.table, lengths, weights=torch.zeros(2000, device="cuda").as_strided((3, 2, 200), strides))
