@@ -492,7 +492,7 @@ int bs_w4_moe(const void* x, long long ldx, int T, const void* router, int E, in
  * offset per group of channels), next to the products on 4-bit weights above.
  *
  * A cache is `pages` pages of `page` entries for each of `heads` heads: device memory of pages * bs_kv4_page_bytes(...) bytes, 16-byte aligned.  Sequence b's
- * entry i lies in page table[b * table_pitch + i / page]: int32, B rows of `width` pages.  Sequences may share pages that are only read.  An entry whose page
+ * entry i lies in page table[b * table_pitch + i / page]: int32, B rows of `width` pages, or with a pitch of 0 one for all.  Sequences may share pages that are only read.  An entry whose page
  * is not one of the cache's is not there: it is neither stored nor read.  Of a vector x of `group` channels of a key or a value the cache holds
  *       m = min x,  s = type((max x - min x) / 15), difference and quotient in binary32,  c = clip(round((x - m) / s), 0, 15)
  * round is half-even of the exact quotient; where s is 0 c is 0.  It stands for c s + m.  A vector that holds an infinity or a NaN (or whose span binary32 does

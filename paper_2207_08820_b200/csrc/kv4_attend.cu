@@ -870,7 +870,7 @@ extern "C" int bs_kv4_attend(const void* q, long long q_token, long long q_head,
                              void* workspace, size_t workspace_bytes, void* stream)
 {
     Attend a{};
-    if (!q || !cache || !cache->data || !table || !lengths || !out || T < 0 || B <= 0 || width <= 0 || table_pitch < width || q_token < 0 || q_head < 0) return BS_ERR_INVALID_ARG;
+    if (!q || !cache || !cache->data || !table || !lengths || !out || T < 0 || B <= 0 || width <= 0 || (table_pitch != 0 && table_pitch < width) || q_token < 0 || q_head < 0) return BS_ERR_INVALID_ARG;
     if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0 || q_heads <= 0 || q_heads % cache->heads != 0) return BS_ERR_INVALID_ARG;
     if (!(scale > 0.f) || !(scale * 1.4426950408889634f < INFINITY) || (!starts && T != B)) return BS_ERR_INVALID_ARG;

@@ -370,7 +370,7 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
                             float* weights_out, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream)
 {
     Evict a{};
-    if (!cache || !cache->data || !table || !lengths || !weights || !lengths_out || !weights_out || !kept || B <= 0 || width <= 0 || table_pitch < width) return BS_ERR_INVALID_ARG;
+    if (!cache || !cache->data || !table || !lengths || !weights || !lengths_out || !weights_out || !kept || B <= 0 || width <= 0 || (table_pitch < width && (table_pitch != 0 || (!into && B > 1)))) return BS_ERR_INVALID_ARG;
     if (cache->type != BS_F16 && cache->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (cache->pages <= 0 || cache->heads <= 0 || cache->D <= 0 || cache->page <= 0 || cache->group <= 0) return BS_ERR_INVALID_ARG;
     if (N <= 0 || keep <= 0 || recent < 0 || recent > keep || weights_head < 0 || (weights_head > 0 && weights_head < N) || weights_sequence < 0) return BS_ERR_INVALID_ARG;

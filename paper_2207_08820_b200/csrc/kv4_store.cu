@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(THREADS) kv4_read_kernel(const __grid_constant
 
 int check(const bs_kv4_cache* c, const int32_t* table, long long pitch, int width, int B, const int32_t* at, const int32_t* starts, int T, Store& a)
 {
-    if (!c || !c->data || !table || !at || width <= 0 || B <= 0 || T < 0 || pitch < width) return BS_ERR_INVALID_ARG;
+    if (!c || !c->data || !table || !at || width <= 0 || B <= 0 || T < 0 || (pitch != 0 && pitch < width)) return BS_ERR_INVALID_ARG;
     if (c->type != BS_F16 && c->type != BS_BF16) return BS_ERR_INVALID_ARG;
     if (c->pages <= 0 || c->heads <= 0 || c->D <= 0 || c->page <= 0 || c->group <= 0) return BS_ERR_INVALID_ARG;
     if (!starts && T != B) return BS_ERR_INVALID_ARG;

@@ -6,6 +6,7 @@ import torch
 
 import kv4_reference as ref
 from paper_2207_08820_b200 import api
+from paper_2207_08820_b200._lib import BitserialError
 from test_gpu_kv4 import BF16, F16, Filled, ints, same, starts_of, weights_of
 
 pytestmark = pytest.mark.gpu
@@ -310,3 +311,29 @@ def test_weights_in_any_order():
     for strides in ((100, 200, 1), (200, 100, 1), (0, 200, 1), (399, 200, 1)):
         with pytest.raises(ValueError):
             api.attend_kv4(q, f.cache, f.table, lengths, weights=torch.zeros(2000, device="cuda").as_strided((3, 2, 200), strides))
+
+
+def test_one_row_of_pages_for_all_sequences():
+    """A prefix that several sequences share, by a row of the table that is expanded and not copied: read, attended to and cut into pages of their own."""
+    n, B = 100, 3
+    f = Filled(43, [n], 2, 64, 16, 64, BF16)
+    one, many = f.table.expand(B, -1), f.table.repeat(B, 1)
+    q, lengths = torch.randn(B, 4, 64, device="cuda").to(BF16), ints([n, 40, 0])
+    assert torch.equal(api.attend_kv4(q, f.cache, one, lengths), api.attend_kv4(q, f.cache, many, lengths))
+    for a, b in zip(api.read_kv4(f.cache, one, ints([0, 7, 20]), ints([0, 50, 60, 80]), total=80), api.read_kv4(f.cache, many, ints([0, 7, 20]), ints([0, 50, 60, 80]), total=80)):
+        assert same(a, b)
+    cache = api.cache_kv4(f.cache.data.shape[0] + 6, 2, 64, page=16)
+    cache.data[:f.cache.data.shape[0]] = f.cache.data
+    into = torch.arange(f.cache.data.shape[0], f.cache.data.shape[0] + 6, dtype=torch.int32, device="cuda").view(3, 2)
+    w = weights_of(7, B, 2, n, "ties").cuda()
+    first = api.evict_kv4(cache, one, lengths, w, 20, recent=3, into=into)
+    held = api.read_kv4(cache, into, ints([0, 0, 0]), ints([0, 20, 40, 40]), total=40)
+    cache.data[f.cache.data.shape[0]:] = 255
+    assert all(same(a, b) for a, b in zip(first, api.evict_kv4(cache, many, lengths, w, 20, recent=3, into=into)))
+    assert all(same(a, b) for a, b in zip(held, api.read_kv4(cache, into, ints([0, 0, 0]), ints([0, 20, 40, 40]), total=40)))
+    k, v = torch.randn(B, 2, 64, device="cuda").to(BF16), torch.randn(B, 2, 64, device="cuda").to(BF16)
+    api.append_kv4(k, v, f.cache, one, ints([3, 50, 99]))
+    back = api.read_kv4(f.cache, many, ints([3, 50, 99]))
+    assert same(back[0].cpu(), ref.read(k.cpu(), 64)) and same(back[1].cpu(), ref.read(v.cpu(), 64))
+    with pytest.raises(BitserialError):
+        api.evict_kv4(f.cache, one, lengths, w, 20)
