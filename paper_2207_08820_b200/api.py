@@ -449,7 +449,8 @@ def attend_kv4(q: torch.Tensor, cache: KV4Cache, table: torch.Tensor, lengths: t
                weights: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Attention of q [T, q_heads, D], the newest tokens of each sequence (``starts`` as in :func:`append_kv4`, without it one each), over the sequence's entries:
     ``lengths`` int32 [sequences], those of the tokens themselves included; each sees the entries up to its own.  ``scale``: 1 / sqrt(D) unless given.
-    ``weights`` float32 [sequences, heads, entries]: what each entry got is added to it (for :func:`evict_kv4`).  No gradients."""
+    ``weights`` float32 [sequences, heads, entries]: what each entry got is added to it (for :func:`evict_kv4`); takes 4 T q_heads entries bytes of scratch memory.
+    No gradients."""
     global launch_count
     st, o, launches = native().kv4_attend(q, *cache._native, table, lengths, starts, cache.D ** -0.5 if scale is None else scale, weights, out, stream)
     _check(st, "bs_kv4_attend")

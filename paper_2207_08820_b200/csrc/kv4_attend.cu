@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     typedef W4Type<F16> Ty;
     typedef W4Type<true> Half;
     // The weights' second fp16 term: without it outputs are off by up to 2^-12 of the weights' part of them, which an output of 11 bits would show and one of 8
-    // does not (64 sequences: 109 us in place of 99).
+    // does not (64 sequences: 73 us in place of 66, 131072 entries 41 in place of 38).
     constexpr bool TWO = F16;
     constexpr int R = 8 * NT, BLOCKS = D / 32, MT = D / 16, TILE = KV4_TILE * (D + 8 * G), PER_G = BLOCKS / G;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -693,8 +693,8 @@ __global__ void __launch_bounds__(WARPS * 32, ctas_of(ring_bytes<D, G>(), NT)) k
     }
 }
 
-// Joins the runs of each row that was cut: a CTA a row of q and head, its warps the runs in turn: eight where columns are cut into many (131072 entries 37.6 us, with four
-// 39.8), four else (64 sequences 66.5, with eight 69).
+// Joins the runs of each row that was cut: a CTA a row of q and head, its warps the runs in turn: eight where columns are cut into sixteen and more (131072 entries 38.0 us,
+// with four 39.9), four else (64 sequences of 8192 105.0, with eight 107.7; 128 of 2048 76.8 and 82.8; 4 of 32768, about where the two meet, 36.6 and 36.2).
 constexpr int JOINERS = 8;
 template <bool F16, int D>
 __global__ void __launch_bounds__(JOINERS * 32) kv4_join_kernel(const __grid_constant__ Attend a, int R, int all)
@@ -784,7 +784,7 @@ __global__ void __launch_bounds__(256) kv4_weights_kernel(const __grid_constant_
     }
 }
 
-// Tiles of rows and runs that a call may have, and its workspace.
+// Tiles of rows and runs that a call may have, and its workspace.  With weights the scores of all rows, 4 T Hq N bytes, are the most of it.
 struct Plan {
     int NT, slots;
     bool team, join;            // joined by clusters; or, where a sequence may be longer than a run, by a second launch
@@ -802,7 +802,7 @@ bool plan(const Kv4& l, int B, int T, int Hq, bool starts, int width, int N, int
     const long long columns = starts ? l.H * (ceil_div_ll(static_cast<long long>(T) * per, R) + B) : static_cast<long long>(l.H) * B * ceil_div(per, R);
     const long long cuts = ceil_div_ll(static_cast<long long>(width) * l.page, LEAST * KV4_TILE), most = runs_of(columns, p.slots);
     p.runs = cuts < most / columns + 1 ? (columns * cuts < most ? columns * cuts : most) : most;
-    // Few columns, of sequences so short that runs for the whole GPU would spare a warp no more than two turns of 1.2 us: a cluster a column, which spares the second
+    // By the width of the table, as lengths are on the device and change under a captured call.  Few columns, of sequences so short that runs for the whole GPU would spare a warp no more than two turns of 1.2 us: a cluster a column, which spares the second
     // launch (1 x 1000 entries 8.8 us with it, 6.7 without)
     const long long tiles = ceil_div_ll(static_cast<long long>(width) * l.page, KV4_TILE), turn = WARPS * UNIT;
     p.team = columns * TEAMS <= p.slots && ceil_div_ll(tiles, TEAMS * turn) <= ceil_div_ll(tiles * columns, p.slots * turn) + 2;

@@ -9,8 +9,9 @@
 // Sequences with entries or places that are not there, on pages that the cache does not have, go a way of their own behind this one: one CTA a head, the least weight bit
 // by bit.  Looking for such pages takes half a microsecond to one (4096 entries to 2048 and read back: 17.3 us without, 18.5 with it).
 //
-// 16 sequences of up to 32768 entries and 8 heads cut to 8191: 31 us to select (four weights a thread and turn; with one 52), bound by loads and atomics, 55 to move at
-// 4 TB/s.  4096 entries to 2048: 15 us with the launches.
+// 16 sequences of up to 32768 entries and 8 heads cut to 8191: 33 us to select (four weights a thread and turn; with one 52), bound by loads and atomics, 55 to move at
+// 4 TB/s.  16 sequences of 32768, bf16, one group a head: 120 us into other pages, 181 in place, where every byte moves twice; with weights that are all the same 112 into
+// other pages.  4096 entries to 2048: 12.6 us with the launches, 15.2 in place.
 #include "kv4.h"
 #include "mma_kernel.cuh"
 #include "w4_dot.cuh"
@@ -388,7 +389,9 @@ extern "C" int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, lon
     a.lengths_out = lengths_out; a.weights_out = weights_out; a.kept = kept;
     a.copy = static_cast<unsigned char*>(workspace);
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // a CTA takes 16384 weights in about 10 us; more of them where there are so many and the heads leave SMs free
+    // A CTA takes 16384 weights in about 10 us; more of them where there are so many and the heads leave SMs free.  By one, two and eight CTAs a head, with the moves:
+    // 8 heads of 4096 entries 12.0, 19.5, 21.1 us; of 16384 23.0, 22.2, 25.5; of 32768 32.1, 30.9, 27.6; of 131072 103, 71, 46; 64 of 32768 83, 76, 82; 256 of 16384 99, 119, 224;
+    // but 128 of 32768 120, 111, 157, and 32 of 131072 160, 129, 69, where the rule takes one and two.
     const long long heads = static_cast<long long>(a.l.H) * B, sms = device_sm_count();
     int rc = most <= 16384 || heads * 2 > sms ? launch_select<1>(a, B, st) : most <= 65536 || heads * 8 > sms ? launch_select<2>(a, B, st) : launch_select<MOST>(a, B, st);
     if (rc != BS_OK) return rc;
