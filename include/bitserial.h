@@ -563,7 +563,8 @@ int bs_kv4_evict(const bs_kv4_cache* cache, const int32_t* table, long long tabl
  *   causal   row i of n rows of q over m keys sees the keys below m - n + i + 1; else all of them.  A row that sees nothing gives zeros.
  *   out      device [T][q_heads][D] of the type (BS_F16 or BS_BF16): softmax(scale q k^T) v, scale > 0
  * Supported: D a multiple of 8 up to 128, up to 128 heads of q a head of k, values below 2^100 (sums are divided by their weights at the end).  Scores, softmax and
- * sums have 32 bits; weights are rounded to the type before they meet the values.  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
+ * sums have 32 bits; weights are rounded to the type before they meet the values (in fp16 those below
+ * 2^-21 of the row's largest to 2^-32 of it and less).  Rows of other sequences and behind the last one do not count, whatever they hold; a NaN or an infinity among a sequence's own values may reach
  * its rows that do not see it.  The same call gives the same bits every time.
  */
 int bs_attend_prompt(const void* q, long long q_token, long long q_head, int T, int q_heads, const void* k, long long k_token, long long k_head, const void* v,

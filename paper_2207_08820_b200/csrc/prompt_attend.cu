@@ -420,7 +420,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
                         }
                     }
                 }
-                const float base_of = top == -INFINITY ? 0.f : -top * a.scale;
+                // weights of up to 2^8 are times 2^7 where fp16 holds them, which leaves bits to those down to 2^-32 of the largest one
+                const float base_of = top == -INFINITY ? 0.f : fmaf(-top, a.scale, F16 ? 7.f : 0.f);
                 const u64 base2 = f2_pack(__float_as_uint(base_of), __float_as_uint(base_of));
                 u64 sums[4] = {0, 0, 0, 0};
 #pragma unroll
