@@ -421,7 +421,16 @@ __global__ void __launch_bounds__(THREADS, 1) prompt_attend_kernel(const __grid_
                     }
                 }
                 // weights of up to 2^8 are times 2^7 where fp16 holds them, which leaves bits to those down to 2^-32 of the largest one
-                const float base_of = top == -INFINITY ? 0.f : fmaf(-top, a.scale, F16 ? 7.f : 0.f);
+                const float lift = F16 ? 7.f : 0.f;
+                float base_of = top == -INFINITY ? 0.f : fmaf(-top, a.scale, lift);
+                if (__any_sync(0xffffffffu, fabsf(base_of) >= 0x1p20f)) {           // its last place would be an eighth and more: distances first
+                    const float less = top == -INFINITY ? 0.f : top;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[i][k] = __float_as_uint(__uint_as_float(v[i][k]) - less);
+                    base_of = lift;
+                }
                 const u64 base2 = f2_pack(__float_as_uint(base_of), __float_as_uint(base_of));
                 u64 sums[4] = {0, 0, 0, 0};
 #pragma unroll

@@ -70,3 +70,29 @@ def test_scales_that_make_up_for_the_size_of_queries(power):
     scale = 2.0 ** -power / 128 ** 0.5
     want, far = reference(q, k, v, True, scale)
     assert ((api.attend_prompt(q, k, v, scale=scale).double() - want).abs() <= far).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("order", ["up", "down", "mixed"])
+@pytest.mark.parametrize("power,gap", [(0, 1), (16, 1), (20, 1), (22, 1), (24, 2), (26, 8), (28, 32), (30, 128)])
+def test_large_scores(power, gap, order, dtype):
+    """Scores that binary32 holds exactly, 2^power and a few gaps more or less: what sets them apart counts, whatever their size."""
+    n, D = 600, 64
+    gen = torch.Generator("cuda").manual_seed(4)
+    steps = torch.arange(n, device="cuda") // 40 if order != "mixed" else torch.randint(0, 15, (n,), device="cuda", generator=gen)
+    steps = 15 - steps if order == "down" else steps
+    q, k = torch.zeros(70, 1, D, dtype=dtype, device="cuda"), torch.zeros(n, 1, D, dtype=dtype, device="cuda")
+    q[..., 0], k[..., 0], q[..., 1], k[:, 0, 1] = 2.0 ** (power // 2), 2.0 ** (power - power // 2), float(gap), steps.to(dtype)
+    q[35:, :, 0] *= -1          # and far below zero
+    v = torch.randn(n, 1, D, device="cuda", generator=gen).to(dtype)
+    out = api.attend_prompt(q, k, v, ints([0, 70]), ints([0, n]), causal=False, scale=1.0).double()[:, 0]
+    p = torch.softmax(gap * steps.double(), 0)
+    want = (p @ v[:, 0].double()).expand(70, D)
+    # distances of up to 15 gaps times log2(e), rounded: 2^-17 of a weight and less, for those that leave one.  Below 2^20 scores may be rounded before their distance is
+    # taken, by 2^(power - 23), for all of a row alike until its maximum is replaced: then for weights that are 2^-8 of the largest and less.  The exponential 2^-20
+    u = HALF[dtype]
+    rel = 2.0 ** -17 + (2.0 ** (power - 22 - 8) if power < 20 else 0.0)
+    bound = (2 * rel + u + (n / 16 + 8) * 2.0 ** -23) * (p @ v[:, 0].double().abs()) + 2.0 ** -32 * p.max() * v[:, 0].double().abs().sum(0)
+    far = bound + u * (want.abs() + bound)
+    off = (out - want).abs()
+    assert (off <= far).all(), (off.max(), (off / far).max())
