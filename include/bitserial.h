@@ -529,7 +529,7 @@ int bs_kv4_read(const bs_kv4_cache* cache, const int32_t* table, long long table
  *            and the heads that share it, is added to it.  Entries from N on are left out.
  *   workspace  bs_kv4_attend_workspace_bytes(...) bytes for the current device (N = 0 without weights; 0 and NULL for few short sequences), with weights 4 T q_heads N and
  *              some more; two calls that may run at the same time need one each
- * Supported: heads up to 65535 of q; scale times q below 2^116 and values below 2^100 (sums are divided by their weights at the end).
+ * Supported: heads up to 65535 of q; scores below 2^29, scale times q below 2^116 and values below 2^100 (sums are divided by their weights at the end).
  * Keys are exact operands, scores, softmax and sums have 32 bits, weights times the values' steps two fp16 terms (one, 11 bits, where the output is bf16), those below
  * 2^-14 of the largest one of their row and group of channels with an error of up to 2^-25 of that one.  The same call gives the same bits every time.
  */

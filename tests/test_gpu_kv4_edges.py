@@ -209,6 +209,37 @@ def test_scores_and_values_that_climb_apart(step, order):
         check(f, q.to(BF16), [2], 1.0, reference=attend_by_group)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=str)
+@pytest.mark.parametrize("order", ["up", "down", "mixed"])
+@pytest.mark.parametrize("power,gap", [(4, 1), (16, 1), (20, 1), (22, 1), (24, 4), (26, 16), (28, 64)])
+def test_large_scores(power, gap, order, dtype):
+    """Scores of the same large part each, and whole numbers of gaps that set them apart."""
+    n, D = 600, 64
+    gen = torch.Generator().manual_seed(7)
+    f = Filled(44, [n], 1, D, 32, 32, dtype, fill=False)
+    steps = torch.arange(n) // 40 if order != "mixed" else torch.randint(0, 16, (n,), generator=gen)
+    steps = 15 - steps if order == "down" else steps
+    steps[:2], steps[-2:] = 0, 15 if order == "up" else 0
+    f.k[0] = torch.zeros(n, 1, D, dtype=dtype)
+    f.k[0][:, 0, 0], f.k[0][:, 0, 33], f.k[0][:, 0, 34] = 15 * 2.0 ** (power - power // 2 - 4), (gap * steps).to(dtype), 15 * gap         # codes are exact
+    api.append_kv4(f.k[0].cuda(), f.v[0].cuda(), f.cache, f.table, ints([0]), ints([0, n]))
+    q = torch.zeros(6, 3, D, dtype=dtype)
+    q[..., 0], q[..., 33] = 2.0 ** (power // 2), 1.0
+    q[::2, :, 0] *= -1
+    k = ref.values(f.k[0], 32)[:, 0]
+    assert torch.equal(k[:, 33], gap * steps.double()) and (k[:, 0] == k[0, 0]).all()
+    seen = torch.arange(n) <= (n - 6 + torch.arange(6)).unsqueeze(1)
+    p = torch.softmax(torch.where(seen, gap * steps.double(), -math.inf), 1)
+    v, vs = ref.values(f.v[0], 32)[:, 0], ref.parts(f.v[0], 32)[1][:, 0].repeat_interleave(32, 1)
+    out = api.attend_kv4(q.cuda(), f.cache, f.table, ints([n]), ints([0, 6]), scale=1.0).cpu().double()
+    # distances of up to 15 gaps, of those that leave a weight: 2^-17 of it, and the exponential; a weight times a step in fp16, one or two terms; sums; the output's rounding
+    part = ref.parts(f.v[0], 32)[0][:, 0]
+    bound = (2.0 ** -16 + (2.0 ** -11 if dtype == BF16 else 2.0 ** -22) + (n / 16 + 16) * 2.0 ** -24) * (p @ part) + n * 15 * 2.0 ** -25 * 2 * (p.unsqueeze(-1) * vs).amax(1)
+    want = (p @ v).unsqueeze(1)
+    far = bound.unsqueeze(1) + ref.HALF[dtype] * (want.abs() + bound.unsqueeze(1))
+    assert ((out - want).abs() <= far).all(), ((out - want).abs().max(), ((out - want).abs() / far).max())
+
+
 # --------------------------------------------------------------------------------------------------------------------- eviction
 
 def evict_around(w, n, keep, recent, there, places):
