@@ -7,7 +7,7 @@
 // through a copy, since what one CTA writes another may still have to read.
 //
 // Sequences with entries or places that are not there, on pages that the cache does not have, go a way of their own behind this one: one CTA a head, the least weight bit
-// by bit.  Looking for such pages takes half a microsecond to one (4096 entries to 2048 and read back: 17.3 us without, 18.5 with it).
+// by bit.  Looking for such pages takes half a microsecond to one (4096 entries to 2048 and read back: 17.4 us without, 18.0 with it).
 //
 // 16 sequences of up to 32768 entries and 8 heads cut to 8191: 33 us to select (four weights a thread and turn; with one 52), bound by loads and atomics, 55 to move at
 // 4 TB/s.  16 sequences of 32768, bf16, one group a head: 120 us into other pages, 181 in place, where every byte moves twice; with weights that are all the same 112 into

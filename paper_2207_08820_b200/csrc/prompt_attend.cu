@@ -12,7 +12,7 @@
 // are seldom rescaled.  Scores, maxima, sums and outputs have 32 bits; weights are rounded to the type of the values, which is what multiplies them.
 //
 // 16384 tokens, 32 heads over 8 of 128 channels, causal: 1970 us, 1.12 PFLOP/s, at the power limit (990 W, 1640 MHz); without the weights' work 1590, without loads as well
-// 1480.  A tile's weights take 1700 cycles, its products 1050, and 3300 pass for both tiles and 128 keys.  Twelve prompts of up to 4096 tokens 549 us, 500 tokens 13.6.
+// 1480.  A tile's weights take 1700 cycles, its products 1050, and 3300 pass for both tiles and 128 keys.  Twelve prompts of up to 4096 tokens 549 us, 500 tokens 13.7.
 #include <cuda.h>
 
 #include <mutex>
